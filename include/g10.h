@@ -386,6 +386,134 @@ int32_t g10_characterize(int64_t num_kernels, int64_t num_tensors, const int64_t
 #define G10_STATIC_MAX_TENSORS 131072
 int32_t g10_pressure_timeline_static(const g10_trace *trace, g10_timeline_out *out, void *stream);
 
+/* ---- A key-value cache within a memory budget -------------------------------------------------------------------
+   The planner above decides which tensors of a traced program leave GPU memory; it can, because the trace says when each is used
+   again.  The key-value cache of a language model is the tensor for which no trace says so: it grows by a row with every token, and
+   what shows which rows will be needed are the attention weights that they received so far.  The four calls below keep such a
+   cache, one layer of it per call, within a budget: append (write the new tokens' rows), attend (read the cache; book the weight that
+   every cached token receives), plan_evictions (which tokens leave, as the moves that close the gaps) and evict (carry the
+   moves out).  All four take the same description of the cache.  All pointers are DEVICE pointers; nothing is staged.
+
+   A sequence holds `lengths[s]` slots; slot j of sequence s lies in page page_table[s * table_stride + j / page_size], place
+   j % page_size.  Entries of the table behind a sequence are not read.  `lengths` and `seen` belong to the sequences, not to a
+   layer: no call changes them, so the calls of all layers share them, a call may be repeated, and a program advances them once per
+   step, BEFORE the calls of that step (lengths and seen count the new tokens in).  After an eviction the program takes over the planned
+   lengths once all layers have been evicted.
+   Every call enqueues only kernels and may be captured in a CUDA graph, after one ordinary call of the same entry point.  What is
+   read on the device when a graph is replayed is what the arrays hold then.
+   Errors that depend on the data are OR-ed into *status (one word, never cleared by the library: a program clears it and
+   looks at it when it likes): G10_DEV_BAD_LENGTH (a length outside 0 .. max_pages * page_size or a count outside 0 .. new_tokens; the
+   call goes on with the nearest valid value), G10_DEV_BAD_PAGE (a page outside 0 .. num_pages - 1: a slot there is not
+   written and read as zeros), G10_DEV_BAD_POSITION (a position outside the rotation tables: not rotated), G10_DEV_BAD_MOVE.  Every access stays in
+   bounds.
+   A page may be shared by sequences that only attend; append, evict and booked weights want a page to belong to one sequence
+   and to stand once in its table (booked weights of a shared page are added up, in any order; the other two leave it unspecified). */
+#define G10_BF16 0
+#define G10_FP16 1
+
+#define G10_DEV_BAD_PAGE 0x400       /* page_table entry outside [0, num_pages)                    */
+#define G10_DEV_BAD_LENGTH 0x800     /* lengths / counts outside their range                        */
+#define G10_DEV_BAD_POSITION 0x1000  /* position of a new token outside the rotation tables         */
+#define G10_DEV_BAD_MOVE 0x2000      /* a move whose slots lie outside the sequence (not carried out) */
+
+typedef struct g10_cache {
+    int32_t dtype;                  /* G10_BF16 or G10_FP16: keys, values, queries, norm weights, outputs */
+    int32_t num_seqs;               /* 0 .. 65 535                                                 */
+    int32_t kv_heads;               /* 1 .. 1024                                                   */
+    int32_t head_dim;               /* a multiple of 8 up to 256                                   */
+    int32_t page_size;              /* slots of a page, 1 .. 65 536                                */
+    int32_t max_pages;              /* columns of the page table; max_pages * page_size < 2^31 - 64 */
+    int64_t num_pages;              /* pages of the pool, < 2^31                                   */
+    void *k, *v;                    /* element d of (page, place, head): page * page_stride + place * slot_stride + head * head_stride + d;
+                                       16-byte aligned, strides multiples of 8 elements            */
+    int64_t page_stride, slot_stride, head_stride;
+    const int32_t *page_table;      /* [num_seqs][table_stride], the first max_pages of a row are used */
+    int64_t table_stride;
+    const int32_t *lengths;         /* [num_seqs] slots that hold a token, those of this call's new tokens included */
+    const int32_t *seen;            /* [num_seqs] tokens the sequence has had so far, new ones included: the next position.
+                                       NULL: lengths (a cache that was never evicted)               */
+    float *scores;                  /* [num_pages][kv_heads][page_size] accumulated weight of each slot */
+    int32_t *positions;             /* [num_pages][kv_heads][page_size] position of the token in each slot */
+    int64_t *status;                /* [1] device status word                                      */
+} g10_cache;
+
+/* Writes new tokens to the cache.  Token t (0 <= t < c_s) of sequence s goes to slot lengths[s] - c_s + t and has position
+   seen[s] - c_s + t; c_s = counts[s], or new_tokens without counts (and never more than the slots that the sequence holds; tokens
+   t >= c_s are padding).  Queries and keys, per head, in 32 bits and rounded once:
+     x <- x * rsqrt(mean(x^2) + eps) * weight     (with q_weight / k_weight; each may be NULL: no norm)
+     (x_i, x_j) <- (x_i cos - x_j sin, x_j cos + x_i sin) for the rotary_dim / 2 pairs, with row `position` of the tables;
+       pairs are (i, i + rotary_dim / 2), or (2 i, 2 i + 1) with `interleaved`; dimensions from rotary_dim on stay.
+   Values are copied.  The new slots' scores become 0 and their positions are written (where the cache has these arrays).
+   q_out [num_seqs][new_tokens][q_heads][head_dim], contiguous, receives the queries, zero for padding.  q may be NULL (q_heads = 0). */
+typedef struct g10_cache_tokens {
+    int32_t new_tokens, q_heads;
+    const void *q, *k, *v;          /* element d of (seq, token, head): seq * *_seq_stride + token * *_token_stride + head * *_head_stride + d;
+                                       16-byte aligned, strides multiples of 8 elements             */
+    int64_t q_seq_stride, q_token_stride, q_head_stride;
+    int64_t k_seq_stride, k_token_stride, k_head_stride;
+    int64_t v_seq_stride, v_token_stride, v_head_stride;
+    void *q_out;
+    const int32_t *counts;          /* [num_seqs] or NULL                                           */
+    const void *q_weight, *k_weight; /* [head_dim] or NULL                                          */
+    float eps;
+    const float *cos_table, *sin_table; /* [table_rows][rotary_dim / 2], both or neither            */
+    int64_t table_rows;
+    int32_t rotary_dim;             /* even, 0 .. head_dim; 0: no rotation                          */
+    int32_t interleaved;
+} g10_cache_tokens;
+int32_t g10_cache_append(const g10_cache *cache, const g10_cache_tokens *tokens, void *stream);
+
+/* Attention of the new tokens over the cache.  Query t (t < c_s, as above) of sequence s stands at slot p = lengths[s] - c_s + t and
+   sees the slots j <= p; with window > 0 only those with j > p - window or j < sinks (slots count here: the call is refused
+   for a cache with positions, whose slots need not stand in order).  Query head h reads key-value head h / (q_heads / kv_heads).
+     s_j = scale * <q, k_j>,  lse = log sum_j exp s_j,  w_j = exp(s_j - lse),  out = sum_j w_j v_j
+   out [num_seqs][new_tokens][q_heads][head_dim]; lse (optional) [num_seqs][new_tokens][q_heads].  A row that sees nothing (padding, an
+   empty sequence) gives out = 0, lse = -inf.  What stands in slots that a row does not see has no influence on it, not even
+   as infinity or NaN.  With add_scores, scores of each slot grows by the sum of its w_j over the queries and the heads of its group.
+   Products take their operands as they are stored and are added up in 32 bits; the weights are rounded to the cache's type before they
+   multiply the values (relative 2^-9 / 2^-12 each), the booked ones are not.  The result does not depend on the timing of the
+   blocks; the way the work is split, and with it the rounding, depends on all lengths of the batch.
+   Limit: new_tokens * q_heads / kv_heads <= 1024. */
+typedef struct g10_cache_queries {
+    int32_t new_tokens, q_heads;
+    const void *q;                  /* strides as above                                             */
+    int64_t q_seq_stride, q_token_stride, q_head_stride;
+    const int32_t *counts;          /* [num_seqs] or NULL                                           */
+    void *out;
+    float *lse;
+    float scale;
+    int32_t window, sinks;          /* window 0: every earlier slot is visible, sinks unused        */
+    int32_t add_scores;
+} g10_cache_queries;
+int32_t g10_cache_attend(const g10_cache *cache, const g10_cache_queries *queries, void *ws, size_t ws_bytes, void *stream);
+/* Workspace of g10_cache_attend (its contents are scratch). */
+int32_t g10_cache_workspace_bytes(const g10_cache *cache, int32_t new_tokens, int32_t q_heads, int32_t window, int32_t sinks,
+                                  int32_t add_scores, size_t *out_bytes);
+
+/* Which tokens leave: for each sequence with more than `budget` slots, and each key-value head on its own, `budget` slots are kept:
+   first those whose position is below `sinks` or at least seen[s] - recent, then by score, the largest first (NaN counts as the
+   lowest); among equals the lower slot.  The r-th kept slot at or behind `budget`, counted in slot order, moves to the r-th slot
+   before `budget` that is not kept.  So no more rows move than must, and since attention does not ask for an order no other row
+   does; sources (>= budget) and destinations (< budget) are disjoint: the moves may be carried out in any order and repeated.
+   Nothing is changed.  moves [num_seqs][kv_heads][budget] (entries behind the count are left as they were), counts
+   [num_seqs][kv_heads], new_lengths [num_seqs] = min(lengths, budget).  Needs scores, and positions if sinks or recent is given
+   (without positions a slot's position is its index).  sinks + recent <= budget.  k and v may be NULL. */
+typedef struct g10_cache_move {
+    int32_t source, target;         /* slots of the sequence                                        */
+} g10_cache_move;
+typedef struct g10_cache_plan {
+    int32_t budget, sinks, recent;
+    g10_cache_move *moves;
+    int32_t *counts;
+    int32_t *new_lengths;           /* may be NULL                                                  */
+} g10_cache_plan;
+int32_t g10_cache_plan_evictions(const g10_cache *cache, const g10_cache_plan *plan, void *stream);
+
+/* Carries out the moves of a plan made for the same lengths (which still are the ones before the eviction): rows of k and v, scores and
+   positions (of the arrays that are given) of every source are copied to its target.  What stands behind the budget is left as it was.  Of the
+   plan, budget, moves and counts are used. */
+int32_t g10_cache_evict(const g10_cache *cache, const g10_cache_plan *plan, void *stream);
+
 /* Bytes of device workspace the call `which` (G10_WS_*) needs for a trace of K kernels, N tensors,
    E events whose arrays live in `mem`. */
 int32_t g10_workspace_bytes(int32_t which, int64_t num_kernels, int64_t num_tensors, int64_t num_events,

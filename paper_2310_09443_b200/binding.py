@@ -26,7 +26,8 @@ FLAG_MULTI_BLOCK = 4
 FLAG_SPREAD_STATE = 8
 STATUS = {0: "ALREADY_FITS", 1: "FIT", 2: "EXHAUSTED", 3: "ITERATION_LIMIT"}
 EXPORTS = ("g10_vitality", "g10_pressure_timeline", "g10_candidate_geometry", "g10_plan_migrations",
-           "g10_workspace_bytes", "g10_strerror", "g10_version", "g10_pressure_timeline_static", "g10_schedule_prefetch", "g10_emit_instructions", "g10_characterize", "g10_plan_batch", "g10_plan_cyclic", "g10_launch_count")
+           "g10_workspace_bytes", "g10_strerror", "g10_version", "g10_pressure_timeline_static", "g10_schedule_prefetch", "g10_emit_instructions", "g10_characterize", "g10_plan_batch", "g10_plan_cyclic", "g10_launch_count",
+           "g10_cache_append", "g10_cache_attend", "g10_cache_plan_evictions", "g10_cache_evict", "g10_cache_workspace_bytes")
 STATIC_MAX_KERNELS, STATIC_MAX_TENSORS = 32768, 131072
 
 INSTRUCTION_DTYPE = np.dtype([("opcode", "<i4"), ("tensor", "<i4"), ("target", "<i4"), ("record", "<i4"),
@@ -97,6 +98,33 @@ class _Options(C.Structure):
                 ("stage_events", C.POINTER(C.c_void_p)), ("num_stage_events", C.c_int32)]
 
 
+class _Cache(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("num_seqs", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("page_size", C.c_int32),
+                ("max_pages", C.c_int32), ("num_pages", C.c_int64), ("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64),
+                ("slot_stride", C.c_int64), ("head_stride", C.c_int64), ("page_table", C.c_void_p), ("table_stride", C.c_int64),
+                ("lengths", C.c_void_p), ("seen", C.c_void_p), ("scores", C.c_void_p), ("positions", C.c_void_p), ("status", C.c_void_p)]
+
+
+class _CacheTokens(C.Structure):
+    _fields_ = [("new_tokens", C.c_int32), ("q_heads", C.c_int32), ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_seq_stride", C.c_int64), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
+                ("k_seq_stride", C.c_int64), ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64),
+                ("v_seq_stride", C.c_int64), ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64),
+                ("q_out", C.c_void_p), ("counts", C.c_void_p), ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("eps", C.c_float),
+                ("cos_table", C.c_void_p), ("sin_table", C.c_void_p), ("table_rows", C.c_int64), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32)]
+
+
+class _CacheQueries(C.Structure):
+    _fields_ = [("new_tokens", C.c_int32), ("q_heads", C.c_int32), ("q", C.c_void_p), ("q_seq_stride", C.c_int64), ("q_token_stride", C.c_int64),
+                ("q_head_stride", C.c_int64), ("counts", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p), ("scale", C.c_float),
+                ("window", C.c_int32), ("sinks", C.c_int32), ("add_scores", C.c_int32)]
+
+
+class _CachePlan(C.Structure):
+    _fields_ = [("budget", C.c_int32), ("sinks", C.c_int32), ("recent", C.c_int32), ("moves", C.c_void_p), ("counts", C.c_void_p),
+                ("new_lengths", C.c_void_p)]
+
+
 _lib = None
 
 
@@ -142,6 +170,16 @@ def load_library():
         lib.g10_plan_migrations.restype = C.c_int32
         lib.g10_plan_migrations.argtypes = [C.POINTER(_Trace), C.c_uint64, C.c_uint64, C.c_uint64, C.POINTER(_Options),
                                             C.POINTER(_PlanOut), C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.g10_cache_append.restype = C.c_int32
+        lib.g10_cache_append.argtypes = [C.POINTER(_Cache), C.POINTER(_CacheTokens), C.c_void_p]
+        lib.g10_cache_attend.restype = C.c_int32
+        lib.g10_cache_attend.argtypes = [C.POINTER(_Cache), C.POINTER(_CacheQueries), C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.g10_cache_plan_evictions.restype = C.c_int32
+        lib.g10_cache_plan_evictions.argtypes = [C.POINTER(_Cache), C.POINTER(_CachePlan), C.c_void_p]
+        lib.g10_cache_evict.restype = C.c_int32
+        lib.g10_cache_evict.argtypes = [C.POINTER(_Cache), C.POINTER(_CachePlan), C.c_void_p]
+        lib.g10_cache_workspace_bytes.restype = C.c_int32
+        lib.g10_cache_workspace_bytes.argtypes = [C.POINTER(_Cache), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
         _lib = lib
     return _lib
 
@@ -491,6 +529,203 @@ def g10_characterize(K, N, use_ptr, uses, tensor_bytes, kernel_start_ns, num_per
                                 _ptr(period_tensor), _ptr(period_prev_use), _ptr(period_next_use), host_bw, ssd_bw, C.byref(out),
                                 _stream(stream)))
     return r
+
+
+# ---- a key-value cache within a budget -----------------------------------------------------------------------------------
+def _same_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise G10Error("all tensors of a cache call have to be on %s: got one on %s" % (device, t.device))
+
+
+def _typed(name, t, dtype, shape=None, contiguous=True):
+    if t.dtype != dtype or (contiguous and not t.is_contiguous()) or (shape is not None and tuple(t.shape) != shape):
+        raise G10Error("%s has to be %s%s%s: got %s of shape %s" % (name, "contiguous " if contiguous else "", dtype,
+                                                                    "" if shape is None else " of shape %s" % (shape,), t.dtype, tuple(t.shape)))
+
+
+class CacheBuffers:
+    """One layer of a paged key-value cache, as the g10_cache_* calls take it (device tensors, kept alive here).
+
+    k, v: bf16 or fp16 [pages, page_size, kv_heads, head_dim], any strides (the same for both, multiples of 8, the last one 1): a view of
+    [pages, kv_heads, page_size, head_dim] will do.  page_table: int32 [seqs, columns]; lengths, seen: int32 [seqs] (shared by all layers; no
+    call changes them).  scores: float32, positions: int32, both [pages, kv_heads, page_size].  status: int64 [1], made here unless given:
+    data-dependent errors are OR-ed into it.  k and v may be None for a cache that is only planned on (then page_size and kv_heads say
+    the sizes)."""
+
+    def __init__(self, k, v, page_table, lengths, seen=None, scores=None, positions=None, status=None, page_size=None, kv_heads=None):
+        self.k, self.v, self.page_table, self.lengths, self.seen = k, v, page_table, lengths, seen
+        self.scores, self.positions = scores, positions
+        self.device = lengths.device
+        if not lengths.is_cuda:
+            raise G10Error("the cache has to be on a CUDA device")
+        self.status = torch.zeros(1, dtype=torch.int64, device=self.device) if status is None else status
+        _same_device(self.device, k, v, page_table, lengths, seen, scores, positions, self.status)
+        self.num_seqs = int(lengths.shape[0])
+        if page_table.dim() != 2 or page_table.shape[0] != self.num_seqs or page_table.dtype != torch.int32 or page_table.stride(1) != 1 and page_table.shape[1] > 1:
+            raise G10Error("page_table has to be int32 [%d, columns]" % self.num_seqs)
+        _typed("lengths", lengths, torch.int32, (self.num_seqs,))
+        _typed("status", self.status, torch.int64, (1,))
+        if seen is not None:
+            _typed("seen", seen, torch.int32, (self.num_seqs,))
+        if (k is None) != (v is None):
+            raise G10Error("k and v come together")
+        if k is not None:
+            if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dtype not in _CACHE_TYPES or k.stride(3) != 1:
+                raise G10Error("k and v have to be bf16 or fp16 [pages, page_size, kv_heads, head_dim] of the same strides, the last one 1")
+            self.num_pages, self.page_size, self.kv_heads, self.head_dim = (int(n) for n in k.shape)
+            self.dtype = k.dtype
+            if page_size not in (None, self.page_size) or kv_heads not in (None, self.kv_heads):
+                raise G10Error("page_size and kv_heads are those of k")
+        else:
+            if page_size is None or kv_heads is None or scores is None:
+                raise G10Error("without k and v, page_size, kv_heads and scores are wanted")
+            self.num_pages, self.page_size, self.kv_heads, self.head_dim = int(scores.shape[0]), page_size, kv_heads, 8
+            self.dtype = torch.bfloat16
+        cells = (self.num_pages, self.kv_heads, self.page_size)
+        if scores is not None:
+            _typed("scores", scores, torch.float32, cells)
+        if positions is not None:
+            _typed("positions", positions, torch.int32, cells)
+        strides = k.stride() if k is not None else (0, 0, 0, 1)
+        self.c_struct = _Cache(_CACHE_TYPES[self.dtype], self.num_seqs, self.kv_heads, self.head_dim, self.page_size, int(page_table.shape[1]),
+                               self.num_pages, _ptr(k), _ptr(v), strides[0], strides[1], strides[2], _ptr(page_table), int(page_table.stride(0)),
+                               _ptr(lengths), _ptr(seen), _ptr(scores), _ptr(positions), _ptr(self.status))
+        self.ref = C.byref(self.c_struct)
+
+
+_CACHE_TYPES = {torch.bfloat16: 0, torch.float16: 1}
+
+
+def _rows(name, t, cache, heads=None):
+    """A tensor [seqs, new_tokens, heads, head_dim] of the cache's type, the last stride 1."""
+    if t.dim() != 4 or t.dtype != cache.dtype or t.shape[0] != cache.num_seqs or t.shape[3] != cache.head_dim or (t.stride(3) != 1) or \
+            (heads is not None and t.shape[2] != heads):
+        raise G10Error("%s has to be %s [%d, new_tokens, %s, %d], the last stride 1: got %s of shape %s" % (
+            name, cache.dtype, cache.num_seqs, "heads" if heads is None else heads, cache.head_dim, t.dtype, tuple(t.shape)))
+    _same_device(cache.device, t)
+
+
+def _cache_call(cache, call, stream):
+    """Runs call(stream handle) with the cache's device current."""
+    if stream is not None:
+        handle = stream.cuda_stream
+    if torch._C._cuda_getDevice() == cache.device.index:
+        _check(call(torch._C._cuda_getCurrentRawStream(cache.device.index) if stream is None else handle))
+        return
+    with torch.cuda.device(cache.device):
+        _check(call(torch._C._cuda_getCurrentRawStream(cache.device.index) if stream is None else handle))
+
+
+def g10_cache_append(cache: CacheBuffers, k, v, q=None, q_weight=None, k_weight=None, eps=1e-6, cos=None, sin=None, interleaved=False, counts=None,
+                     q_out=None, stream=None):
+    """Norm of queries and keys per head, position rotation and write to the cache's pages, in one pass.  k, v [seqs, new_tokens, kv_heads,
+    head_dim], q [seqs, new_tokens, q_heads, head_dim] (strided views, as of one projection's output); q_weight, k_weight [head_dim]; cos, sin
+    float32 [positions, rotary_dim / 2]; counts int32 [seqs]: tokens of each sequence that count (None: all).  cache.lengths (and seen) count the
+    new tokens in.  Returns the queries (q_out, made here if None), or None without q."""
+    _rows("k", k, cache, cache.kv_heads)
+    _rows("v", v, cache, cache.kv_heads)
+    new = int(k.shape[1])
+    if v.shape[1] != new or (q is not None and q.shape[1] != new):
+        raise G10Error("q, k and v have to hold as many tokens")
+    heads = 0
+    if q is not None:
+        _rows("q", q, cache)
+        heads = int(q.shape[2])
+        if q_out is None:
+            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        else:
+            _typed("q_out", q_out, cache.dtype, tuple(q.shape))
+    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
+        if w is not None:
+            _typed(name, w, cache.dtype, (cache.head_dim,))
+    if (cos is None) != (sin is None):
+        raise G10Error("cos and sin come together")
+    half = rows = 0
+    if cos is not None:
+        if cos.dim() != 2:
+            raise G10Error("cos and sin have to be float32 [positions, rotary_dim / 2]")
+        rows, half = int(cos.shape[0]), int(cos.shape[1])
+        _typed("cos", cos, torch.float32)
+        _typed("sin", sin, torch.float32, (rows, half))
+    if counts is not None:
+        _typed("counts", counts, torch.int32, (cache.num_seqs,))
+    _same_device(cache.device, q_out, q_weight, k_weight, cos, sin, counts)
+    qs, ks, vs = (q.stride() if q is not None else (0, 0, 0)), k.stride(), v.stride()
+    t = _CacheTokens(new, heads, _ptr(q), _ptr(k), _ptr(v), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], _ptr(q_out) if heads else None,
+                     _ptr(counts), _ptr(q_weight), _ptr(k_weight), eps, _ptr(cos), _ptr(sin), rows, 2 * half, 1 if interleaved else 0)
+    _cache_call(cache, lambda s: load_library().g10_cache_append(cache.ref, C.byref(t), s), stream)
+    return q_out if heads else None
+
+
+def g10_cache_workspace_bytes(cache: CacheBuffers, new_tokens, q_heads, window=0, sinks=0, add_scores=False) -> int:
+    """Bytes of workspace that g10_cache_attend needs."""
+    out = C.c_size_t(0)
+    _check(load_library().g10_cache_workspace_bytes(cache.ref, new_tokens, q_heads, window, sinks, 1 if add_scores else 0, C.byref(out)))
+    return int(out.value)
+
+
+def g10_cache_attend(cache: CacheBuffers, q, scale=None, window=0, sinks=0, counts=None, add_scores=False, out=None, lse=None, ws=None, stream=None):
+    """Attention of the new tokens' queries q [seqs, new_tokens, q_heads, head_dim] over the cache (scale: 1 / sqrt(head_dim) if None); returns
+    `out` (made here if None).  lse: float32 [seqs, new_tokens, q_heads] to write the logarithms of the sums to, or None.  window, sinks: only the
+    last `window` slots and the first `sinks` are visible (0: all).  add_scores: cache.scores grows by the weights that each slot received.
+    ws: a uint8 device tensor of at least g10_cache_workspace_bytes(...) bytes (allocated here when None); calls that may overlap on the GPU, those of
+    captured graphs among them, need one each."""
+    _rows("q", q, cache)
+    new, heads = int(q.shape[1]), int(q.shape[2])
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    else:
+        _typed("out", out, cache.dtype, tuple(q.shape))
+    if lse is not None:
+        _typed("lse", lse, torch.float32, tuple(q.shape[:3]))
+    if counts is not None:
+        _typed("counts", counts, torch.int32, (cache.num_seqs,))
+    if ws is None:
+        ws = torch.empty(max(256, g10_cache_workspace_bytes(cache, new, heads, window, sinks, add_scores)), dtype=torch.uint8, device=cache.device)
+        if stream is not None:
+            ws.record_stream(stream)
+    elif not ws.is_contiguous():
+        raise G10Error("ws has to be contiguous")
+    _same_device(cache.device, out, lse, counts, ws)
+    qs = q.stride()
+    u = _CacheQueries(new, heads, _ptr(q), qs[0], qs[1], qs[2], _ptr(counts), _ptr(out), _ptr(lse), cache.head_dim ** -0.5 if scale is None else scale,
+                      window, sinks, 1 if add_scores else 0)
+    size = ws.numel() * ws.element_size()
+    _cache_call(cache, lambda s: load_library().g10_cache_attend(cache.ref, C.byref(u), _ptr(ws), size, s), stream)
+    return out
+
+
+def _cache_plan(cache, budget, sinks, recent, moves, counts, new_lengths):
+    _typed("moves", moves, torch.int32, (cache.num_seqs, cache.kv_heads, budget, 2))
+    _typed("counts", counts, torch.int32, (cache.num_seqs, cache.kv_heads))
+    if new_lengths is not None:
+        _typed("new_lengths", new_lengths, torch.int32, (cache.num_seqs,))
+    _same_device(cache.device, moves, counts, new_lengths)
+    return _CachePlan(budget, sinks, recent, _ptr(moves), _ptr(counts), _ptr(new_lengths))
+
+
+def g10_cache_plan_evictions(cache: CacheBuffers, budget, sinks=0, recent=0, moves=None, counts=None, new_lengths=None, stream=None):
+    """Plans which `budget` slots of each (sequence, key-value head) stay: positions below `sinks` and the last `recent` first, then the largest
+    scores.  Returns moves int32 [seqs, kv_heads, budget, 2] (source, target slot; valid up to the count), counts int32 [seqs, kv_heads] and
+    new_lengths int32 [seqs]; changes nothing else."""
+    dev = cache.device
+    if moves is None:
+        moves = torch.empty((cache.num_seqs, cache.kv_heads, max(budget, 0), 2), dtype=torch.int32, device=dev)
+    if counts is None:
+        counts = torch.empty((cache.num_seqs, cache.kv_heads), dtype=torch.int32, device=dev)
+    if new_lengths is None:
+        new_lengths = torch.empty(cache.num_seqs, dtype=torch.int32, device=dev)
+    p = _cache_plan(cache, budget, sinks, recent, moves, counts, new_lengths)
+    _cache_call(cache, lambda s: load_library().g10_cache_plan_evictions(cache.ref, C.byref(p), s), stream)
+    return SimpleNamespace(moves=moves, counts=counts, new_lengths=new_lengths)
+
+
+def g10_cache_evict(cache: CacheBuffers, moves, counts, stream=None):
+    """Carries the moves of a plan out (rows of k and v, scores, positions).  cache.lengths still are those that the plan was made for; the
+    program takes new_lengths over once every layer has been evicted."""
+    p = _cache_plan(cache, int(moves.shape[2]) if moves.dim() == 4 else 0, 0, 0, moves, counts, None)
+    _cache_call(cache, lambda s: load_library().g10_cache_evict(cache.ref, C.byref(p), s), stream)
 
 
 def instructions_numpy(em) -> np.ndarray:

@@ -1,0 +1,130 @@
+// What the calls on the key-value cache share: the cache as the kernels see it, checked lengths and pages.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "g10_device.cuh"
+#include "g10_internal.h"
+
+namespace g10 {
+
+// g10_cache with checked sizes; passed to kernels by value.
+struct CacheView {
+    const char *k, *v;                   // (written by append and evict through the same addresses)
+    int64_t page_stride, slot_stride, head_stride;       // elements of 2 bytes
+    const int32_t *table;
+    int64_t table_stride, num_pages;
+    const int32_t *lengths, *seen;
+    float *scores;
+    int32_t *positions;
+    ull *status;
+    int num_seqs, kv_heads, head_dim, page_size, max_pages;
+    int capacity;                        // max_pages * page_size
+};
+
+// Slots that sequence s holds, as far as the table reaches.
+__device__ __forceinline__ int cache_length(const CacheView &c, int s, ull &bad)
+{
+    const int n = __ldg(&c.lengths[s]);
+    if (n < 0 || n > c.capacity) bad |= G10_DEV_BAD_LENGTH;
+    return n < 0 ? 0 : min(n, c.capacity);
+}
+// New tokens of sequence s that count, never more than its slots.
+__device__ __forceinline__ int cache_count(const int32_t *counts, int s, int new_tokens, int length, ull &bad)
+{
+    int n = new_tokens;
+    if (counts != nullptr) {
+        n = __ldg(&counts[s]);
+        if (n < 0 || n > new_tokens) bad |= G10_DEV_BAD_LENGTH;
+        n = n < 0 ? 0 : min(n, new_tokens);
+    }
+    return min(n, length);
+}
+// Page of a slot (slot < capacity), -1 if the table names none of the pool.
+__device__ __forceinline__ int cache_page(const CacheView &c, int s, int slot, ull &bad)
+{
+    const int page = __ldg(&c.table[(int64_t)s * c.table_stride + (unsigned)slot / (unsigned)c.page_size]);
+    if (page < 0 || page >= c.num_pages) { bad |= G10_DEV_BAD_PAGE; return -1; }
+    return page;
+}
+// First element of the row of (page, slot % page_size, head) in k or v.
+__device__ __forceinline__ int64_t cache_row(const CacheView &c, int page, int slot, int head)
+{
+    return (int64_t)page * c.page_stride + (int64_t)((unsigned)slot % (unsigned)c.page_size) * c.slot_stride + (int64_t)head * c.head_stride;
+}
+// Entry of scores and positions.
+__device__ __forceinline__ int64_t cache_cell(const CacheView &c, int page, int slot, int head)
+{
+    return ((int64_t)page * c.kv_heads + head) * c.page_size + (unsigned)slot % (unsigned)c.page_size;
+}
+
+template <typename T>
+struct Pair;
+template <>
+struct Pair<__nv_bfloat16> {
+    typedef __nv_bfloat162 type;
+    static __device__ __forceinline__ unsigned pack(float a, float b)
+    {
+        const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+        return *(const unsigned *)&p;
+    }
+    static __device__ __forceinline__ float2 unpack(unsigned u) { return __bfloat1622float2(*(const __nv_bfloat162 *)&u); }
+};
+template <>
+struct Pair<__half> {
+    typedef __half2 type;
+    static __device__ __forceinline__ unsigned pack(float a, float b)
+    {
+        const __half2 p = __floats2half2_rn(a, b);
+        return *(const unsigned *)&p;
+    }
+    static __device__ __forceinline__ float2 unpack(unsigned u) { return __half22float2(*(const __half2 *)&u); }
+};
+
+// ---- launchers ----
+struct AppendArgs {
+    CacheView c;
+    const char *q, *k, *v;
+    int64_t q_seq, q_token, q_head, k_seq, k_token, k_head, v_seq, v_token, v_head;
+    char *q_out;
+    const int32_t *counts;
+    const char *q_weight, *k_weight;
+    float eps;
+    const float *cos_table, *sin_table;
+    int64_t table_rows;
+    int new_tokens, q_heads, rotary, interleaved;
+};
+cudaError_t launch_cache_append(const AppendArgs &a, int dtype, cudaStream_t s);
+
+struct AttendArgs {
+    CacheView c;
+    const char *q;
+    int64_t q_seq, q_token, q_head;
+    const int32_t *counts;
+    char *out;
+    float *lse;
+    float scale_log2;                    // scale * log2 e
+    int new_tokens, q_heads, group, rows, window, sinks;
+    int row_tiles, row_blocks;           // 16-row tiles of a block; blocks of rows per key-value head
+    float2 *ml;                          // [pieces][block rows] running maximum and sum of every piece
+    float *part;                         // [pieces][block rows][padded head_dim] its sums, not divided yet
+    float *logits;                       // [tiles][block rows][64] scaled by log2 e (null: weights are not booked)
+};
+// Sizes that the workspace goes by.
+struct AttendShape {
+    int row_tiles, row_blocks, block_rows, padded_dim;
+    int64_t pieces, tiles;               // upper bounds for the sequences' capacity
+};
+AttendShape attend_shape(const CacheView &c, int rows, int new_tokens, int window, int sinks);
+cudaError_t launch_cache_attend(const AttendArgs &a, int dtype, cudaStream_t s);
+
+struct EvictArgs {
+    CacheView c;
+    int budget, sinks, recent;
+    g10_cache_move *moves;
+    int32_t *counts, *new_lengths;
+};
+cudaError_t launch_cache_plan(const EvictArgs &a, cudaStream_t s);
+cudaError_t launch_cache_evict(const EvictArgs &a, cudaStream_t s);
+
+}  // namespace g10
