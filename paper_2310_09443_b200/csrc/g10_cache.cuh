@@ -105,14 +105,14 @@ struct AttendArgs {
     float *lse;
     float scale_log2;                    // scale * log2 e
     int new_tokens, q_heads, group, rows, window, sinks;
-    int row_tiles, row_blocks;           // 16-row tiles of a block; blocks of rows per key-value head
+    int row_blocks;                      // blocks of rows per key-value head
     float2 *ml;                          // [pieces][block rows] running maximum and sum of every piece
     float *part;                         // [pieces][block rows][padded head_dim] its sums, not divided yet
-    float *logits;                       // [tiles][block rows][64] scaled by log2 e (null: weights are not booked)
+    float *logits;                       // [tiles][64][rows of a block] scaled by log2 e (null: weights are not booked)
 };
 // Sizes that the workspace goes by.
 struct AttendShape {
-    int row_tiles, row_blocks, block_rows, padded_dim;
+    int row_blocks, block_rows, padded_dim;
     int64_t pieces, tiles;               // upper bounds for the sequences' capacity
 };
 AttendShape attend_shape(const CacheView &c, int rows, int new_tokens, int window, int sinks);

@@ -128,7 +128,7 @@ int32_t g10_cache_attend(const g10_cache *cache, const g10_cache_queries *u, voi
     const AttendShape z = attend_shape(a.c, a.rows, a.new_tokens, a.window, a.sinks);
     const AttendLayout l = attend_layout(z, u->add_scores != 0);
     if (!ws || ((uintptr_t)ws & (kAlign - 1)) || ws_bytes < l.bytes) return G10_ERR_WORKSPACE;
-    a.row_tiles = z.row_tiles; a.row_blocks = z.row_blocks;
+    a.row_blocks = z.row_blocks;
     a.ml = (float2 *)((char *)ws + l.ml); a.part = (float *)((char *)ws + l.part);
     a.logits = u->add_scores ? (float *)((char *)ws + l.logits) : nullptr;
     return status_of(launch_cache_attend(a, cache->dtype, (cudaStream_t)stream));

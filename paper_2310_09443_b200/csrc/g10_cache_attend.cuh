@@ -24,11 +24,6 @@ constexpr int kMaxBlocks = 148 * 8;      // of the grid; the workspace has room 
 constexpr int kJoinThreads = 256;
 
 __device__ __forceinline__ unsigned smem_of(const void *p) { return (unsigned)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void copy16(unsigned dst, const void *src, bool there)
-{
-    const int n = there ? 16 : 0;        // (0: 16 zero bytes)
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
 __device__ __forceinline__ void ldsm4(unsigned (&r)[4], unsigned at)
 {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
@@ -173,40 +168,62 @@ __device__ __forceinline__ void cursor_next(const AttendArgs &a, Cursor &u, int 
 
 __device__ __forceinline__ bool sees(const AttendArgs &a, int p, int slot) { return slot <= p && (a.window == 0 || slot < a.sinks || slot > p - a.window); }
 
-template <typename T, int kSteps, int kRowTiles, int kParts, int kStages>
+__device__ __forceinline__ void copy16(unsigned dst, const void *src, bool there)
+{
+    const int n = there ? 16 : 0;        // (0: 16 zero bytes)
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ unsigned turned8x8(unsigned x)
+{
+    unsigned y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// Rows of the logits that the first kernel leaves for a slot: those of a block of rows, rounded up for wide accesses.
+__host__ __device__ __forceinline__ int logit_rows(int kept) { return kept <= 2 ? kept : (kept + 3) & ~3; }
+
+constexpr int kParts = 4;                // warps of a block; each takes 16 slots of a tile
+constexpr int kThreads = 32 * kParts;
+constexpr float kSlack = 8.0f;           // see below
+
+template <typename T, int kSteps, int kCols, int kStages>
 struct Config {
-    static constexpr int kWarps = kRowTiles * kParts, kThreads = 32 * kWarps;
     static constexpr int kDim = 16 * kSteps;             // head_dim, padded with zeros
     // bytes of a row in shared memory: an odd number of 16-byte units, so that the 8 rows of a matrix lie in different banks
     static constexpr int kPitch = 2 * kDim + 16;
-    static constexpr int kRows = 16 * kRowTiles;
-    static constexpr int kStageBytes = 2 * kTile * kPitch;
-    static constexpr int kSmem = kStages * kStageBytes + kRows * kPitch + kStages * kTile * 8 + kParts * kRows * 8;
-    static constexpr int kTokens = kTile / kParts;       // slots of a tile that one warp takes
-    // joining the warps' sums: half of them are put into the stage that the last tile has left
-    static constexpr int kMergeParts = kParts / 2;
-    static_assert(kMergeParts == 0 || kRowTiles * kMergeParts * 32 * kSteps * 8 * 4 <= kStageBytes, "the warps' sums fit one stage");
+    static constexpr int kRows = 8 * kCols;
+    static constexpr int kPartBytes = 2 * 16 * kPitch;   // a warp's part of a tile: 16 keys, 16 values
+    static constexpr bool kHeld = kCols * kSteps <= 16;  // the queries stay in registers
+    static constexpr int kSmem = kParts * kStages * kPartBytes + (kHeld ? 0 : kRows * kPitch) + kParts * kRows * 8;
+    // joining the warps' sums: so many columns at a time fit the part of the ring that the warp has just left
+    static constexpr int kMerge = kCols < 2 ? kCols : 2;
+    static constexpr int kMergePitch = kDim + 4;         // floats (2 rows apart: 8 banks)
+    static_assert(8 * kMerge * kMergePitch * 4 <= kPartBytes && kCols % kMerge == 0, "a warp's sums fit");
 };
 
-// A block has kRowTiles * kParts warps: warp (r, p) holds rows 16 r .. 16 r + 15 and looks at the p-th part of every tile, with a
-// maximum, a sum and accumulators of its own; the parts are joined when the piece ends.  Keys and values come by 16-byte asynchronous
-// copies into a ring of kStages tiles, row by row from wherever the page lies; the addresses of a tile are worked out one tile before its
-// copies are issued and the page numbers loaded before that tile's arithmetic, so that no wait for the table is on the way.
-template <typename T, int kSteps, int kRowTiles, int kParts, int kStages>
-__global__ void __launch_bounds__(32 * kRowTiles *kParts) k_cache_attend(const AttendArgs a, int min_tiles)
+// The block's four warps go through its tiles side by side, warp p at the 16 slots p of each, with maxima, sums and accumulators of their
+// own and a ring of kStages parts each: nothing is waited for across warps before the piece ends and the four are joined.  Keys and values come
+// by 16-byte asynchronous copies, row by row from wherever the page lies (bulk copies, one a row, are slower: a row of 256 bytes each 35
+// clocks of an SM was measured, 2.1 TB/s in all); a lane looks the page of one slot up two tiles before it is worked on.
+//   S^T [16 slots x rows] = K Q^T,  W^T = exp2(S^T - ref),  O^T [dims x rows] += V^T W^T,
+// so that 8 rows (one key-value head's group of up to 8 query heads) fill the narrow side of the matrix instruction and keys and values
+// its wide one.  W^T reaches the layout that the second product wants through one 8 x 8 transposition in registers.
+// ref is a maximum of the past: the weights are taken relative to it as long as no logit is more than kSlack above it (weights up to 2^8,
+// which either type holds), so that the sums are rescaled and the warp's lanes compared only when that fails, a few times per piece.
+template <typename T, int kSteps, int kCols, int kStages>
+__global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, int min_tiles)
 {
-    typedef Config<T, kSteps, kRowTiles, kParts, kStages> C;
+    typedef Config<T, kSteps, kCols, kStages> C;
     extern __shared__ __align__(128) char smem[];
-    char *const s_q = smem + kStages * C::kStageBytes;
-    int64_t *const s_from = (int64_t *)(s_q + C::kRows * C::kPitch);          // [kStages][kTile] first element of each row, -1: zeros
-    float2 *const s_ml = (float2 *)(s_from + kStages * kTile);                // [kParts][kRows]
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int wr = warp / kParts, wp = warp % kParts;
+    char *const s_q = smem + kParts * kStages * C::kPartBytes;
+    float2 *const s_ml = (float2 *)(s_q + (C::kHeld ? 0 : C::kRows * C::kPitch));      // [kParts][kRows]
+    __shared__ Place s_place;
+    const int tid = threadIdx.x, lane = tid & 31, part = tid >> 5;
     const int per = a.c.kv_heads * a.row_blocks;
     ull bad = 0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    __shared__ Place s_place;
-    const Tally tally = tally_of<C::kThreads>(a, bad);
+    const Tally tally = tally_of<kThreads>(a, bad);
     const Share share = share_of(tally.total, per, gridDim.x, min_tiles);
     const int64_t begin = begin_of(share, blockIdx.x);
     const int n = (int)(begin_of(share, blockIdx.x + 1) - begin);
@@ -219,154 +236,184 @@ __global__ void __launch_bounds__(32 * kRowTiles *kParts) k_cache_attend(const A
     Cursor now, ahead;
     cursor_at(a, now, s_place, begin);
     ahead = now;
-    // the page of a slot of the tile that `ahead` stands at, for threads 0 .. 63; -1: nothing to read
-    auto look_up = [&](int &slot) -> int {
-        slot = first_slot(ahead.q, ahead.idx) + tid;
+    const unsigned ring = smem_of(smem) + part * kStages * C::kPartBytes;
+    // where the row of this lane's slot lies (lanes 16 .. 31: as lanes 0 .. 15), in the tile that `ahead` stands at; -1: zeros
+    auto look_up = [&]() -> int64_t {
+        const int slot = first_slot(ahead.q, ahead.idx) + part * 16 + (lane & 15);
         if (slot >= ahead.q.length || !(a.window == 0 || slot < a.sinks || slot > ahead.q.length - ahead.q.count - a.window)) return -1;
-        return cache_page(a.c, ahead.s, slot, bad);
+        const int page = cache_page(a.c, ahead.s, slot, bad);
+        return page < 0 ? -1 : 2 * cache_row(a.c, page, slot, ahead.item / a.row_blocks);
     };
-    auto row_from = [&](int page, int slot) -> int64_t { return page < 0 ? -1 : cache_row(a.c, page, slot, ahead.item / a.row_blocks); };
-    // copies of one tile into its stage
-    auto issue = [&](int stage) {
+    auto issue = [&](int stage, int64_t row_at) {
         constexpr int kChunks = 2 * kSteps;              // of 16 bytes in a row
-        const unsigned to = smem_of(smem) + stage * C::kStageBytes;
-#pragma unroll 4
-        for (int i = tid; i < kTile * kChunks; i += C::kThreads) {
-            const int row = i / kChunks, chunk = i % kChunks;
-            const int64_t from = s_from[stage * kTile + row];
+        const unsigned to = ring + stage * C::kPartBytes;
+#pragma unroll
+        for (int i = 0; i < 16 * kChunks / 32; ++i) {
+            const int c = i * 32 + lane, row = c / kChunks, chunk = c % kChunks;
+            const int64_t from = __shfl_sync(0xffffffffu, row_at, row);
             const bool there = from >= 0 && chunk * 8 < a.c.head_dim;
-            const int64_t at = there ? 2 * from + 16 * chunk : 0;
+            const int64_t at = there ? from + 16 * chunk : 0;
             copy16(to + row * C::kPitch + chunk * 16, a.c.k + at, there);
-            copy16(to + (kTile + row) * C::kPitch + chunk * 16, a.c.v + at, there);
+            copy16(to + (16 + row) * C::kPitch + chunk * 16, a.c.v + at, there);
         }
     };
+    int64_t next_row = -1;                               // of the tile to be issued next
 #pragma unroll
     for (int i = 0; i < kStages; ++i) {
-        if (i < n) {
-            if (tid < kTile) { int slot; const int page = look_up(slot); s_from[i * kTile + tid] = row_from(page, slot); }
-            cursor_next(a, ahead, per);
+        if (i > 0) {
+            if (i - 1 < n) issue(i - 1, next_row);
+            asm volatile("cp.async.commit_group;" ::: "memory");
         }
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kStages - 1; ++i) {
-        if (i < n) issue(i);
-        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (i < n) { next_row = look_up(); cursor_next(a, ahead, per); }
     }
 
-    float acc[2 * kSteps][4], m[2], l[2];
+    float acc[kSteps][kCols][4], m[kCols][2], l[kCols][2];
+    unsigned held[C::kHeld ? kSteps * kCols * 2 : 1];
+    int p[kCols][2];                                     // slot at which a row's token stands, -1: no row
     bool fresh = true;
     int64_t item = 0;
-    int first_row = 0;
-    int stage = 0;
+    int first_row = 0, stage = 0;
+    const int kept = min(C::kRows, a.rows), logit_pitch = logit_rows(kept);
     for (int u = 0; u < n; ++u) {
         if (fresh) {                                     // a new item: its queries
             fresh = false;
             item = (int64_t)now.s * per + now.item;
             first_row = (now.item % a.row_blocks) * C::kRows;
             const int head = now.item / a.row_blocks;
-            for (int i = tid; i < C::kRows * 2 * kSteps; i += C::kThreads) {
-                const int r = i / (2 * kSteps), chunk = i % (2 * kSteps), row = first_row + r;
-                uint4 x = make_uint4(0, 0, 0, 0);
-                const int t = row / a.group;
-                if (row < a.rows && t < now.q.count && chunk * 8 < a.c.head_dim)
-                    x = __ldg((const uint4 *)(a.q + 2 * (now.s * a.q_seq + t * a.q_token + (head * a.group + row % a.group) * a.q_head) + 16 * chunk));
-                *(uint4 *)(s_q + r * C::kPitch + chunk * 16) = x;
+            auto row_of = [&](int r) -> const char * {   // (null: no such row)
+                const int row = first_row + r, t = row / a.group;
+                if (row >= a.rows || t >= now.q.count) return nullptr;
+                return a.q + 2 * (now.s * a.q_seq + t * a.q_token + (head * a.group + row % a.group) * a.q_head);
+            };
+            if (C::kHeld) {
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) {
+                    const char *from = row_of(j * 8 + (lane >> 2));
+#pragma unroll
+                    for (int k = 0; k < 2 * kSteps; ++k) {
+                        const int d = k * 8 + (lane & 3) * 2;
+                        held[j * 2 * kSteps + k] = from != nullptr && d < a.c.head_dim ? __ldg((const unsigned *)(from + 2 * d)) : 0u;
+                    }
+                }
+            } else {
+                // (all warps have left the queries of the item before: they met when it was joined)
+                for (int i = tid; i < C::kRows * 2 * kSteps; i += kThreads) {
+                    const int r = i / (2 * kSteps), chunk = i % (2 * kSteps);
+                    const char *from = row_of(r);
+                    *(uint4 *)(s_q + r * C::kPitch + chunk * 16) = from != nullptr && chunk * 8 < a.c.head_dim ? __ldg((const uint4 *)(from + 16 * chunk)) : make_uint4(0, 0, 0, 0);
+                }
+                __syncthreads();
             }
 #pragma unroll
-            for (int i = 0; i < 2 * kSteps; ++i)
+            for (int j = 0; j < kCols; ++j) {
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][e] = 0.0f;
-            m[0] = m[1] = -INFINITY; l[0] = l[1] = 0.0f;
-        }
-        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-        __syncthreads();
-        if (u + kStages - 1 < n) issue(stage == 0 ? kStages - 1 : stage - 1);
-        asm volatile("cp.async.commit_group;" ::: "memory");
-        int page = -1, slot_ahead = 0;
-        const bool more = u + kStages < n;
-        if (more && tid < kTile) page = look_up(slot_ahead);
-
-        // ---- the tile's products with the queries ----
-        const unsigned keys = smem_of(smem) + stage * C::kStageBytes + wp * C::kTokens * C::kPitch, values = keys + kTile * C::kPitch;
-        const unsigned queries = smem_of(s_q) + wr * 16 * C::kPitch;
-        constexpr int kN = C::kTokens / 8;
-        float x[kN][4];
+                for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-        for (int j = 0; j < kN; ++j)
+                    for (int e = 0; e < 4; ++e) acc[k][j][e] = 0.0f;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[j][e] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kSteps; ++k) {
-            unsigned qa[4], kb[4];
-            ldsm4(qa, queries + ((lane & 7) + ((lane >> 3) & 1) * 8) * C::kPitch + (2 * k + (lane >> 4)) * 16);
-#pragma unroll
-            for (int j = 0; j < kN; j += 2) {
-                ldsm4(kb, keys + (j * 8 + (lane & 7) + (lane >> 4) * 8) * C::kPitch + (2 * k + ((lane >> 3) & 1)) * 16);
-                mma<T>(x[j], qa, kb[0], kb[1]);
-                mma<T>(x[j + 1], qa, kb[2], kb[3]);
-            }
-        }
-        // ---- what each row sees ----
-        const int slot0 = first_slot(now.q, now.idx) + wp * C::kTokens, seen0 = now.q.length - now.q.count;
-        const bool whole = slot0 + C::kTokens - 1 <= seen0 && (a.window == 0 || slot0 > now.q.length - 1 - a.window);
-        int p[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int row = first_row + wr * 16 + (lane >> 2) + 8 * h, t = row / a.group;
-            p[h] = row < a.rows && t < now.q.count ? seen0 + t : -1;
-        }
-#pragma unroll
-        for (int j = 0; j < kN; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[j][e] *= a.scale_log2;
-                if (p[e >> 1] < 0 || (!whole && !sees(a, p[e >> 1], slot0 + j * 8 + (lane & 3) * 2 + (e & 1)))) x[j][e] = -INFINITY;
-            }
-        if (a.logits != nullptr) {
-            const int kept = min(C::kRows, a.rows);
-            float *to = a.logits + (begin + u) * (int64_t)(kept * kTile);
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = wr * 16 + (lane >> 2) + 8 * h;
-                if (r < kept) {
-#pragma unroll
-                    for (int j = 0; j < kN; ++j)
-                        *(float2 *)(to + r * kTile + wp * C::kTokens + j * 8 + (lane & 3) * 2) = make_float2(x[j][2 * h], x[j][2 * h + 1]);
+                for (int h = 0; h < 2; ++h) {
+                    m[j][h] = -INFINITY; l[j][h] = 0.0f;
+                    const int row = first_row + j * 8 + (lane & 3) * 2 + h, t = row / a.group;
+                    p[j][h] = row < a.rows && t < now.q.count ? now.q.length - now.q.count + t : -1;
                 }
             }
         }
-        // ---- running maximum and sum ----
-        bool scales = false;
-        float by[2];
+        asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+        __syncwarp();
+        if (u + kStages - 1 < n) issue(stage == 0 ? kStages - 1 : stage - 1, next_row);
+        asm volatile("cp.async.commit_group;" ::: "memory");
+        if (u + kStages < n) { next_row = look_up(); cursor_next(a, ahead, per); }
+
+        // ---- S^T ----
+        const unsigned keys = ring + stage * C::kPartBytes, values = keys + 16 * C::kPitch;
+        float x[kCols][4];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            float top = m[h];
+        for (int j = 0; j < kCols; ++j)
 #pragma unroll
-            for (int j = 0; j < kN; ++j) top = fmaxf(top, fmaxf(x[j][2 * h], x[j][2 * h + 1]));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-            const float ref = top == -INFINITY ? 0.0f : top;
-            by[h] = exp2_of(m[h] - ref);
-            scales |= top != m[h];
-            m[h] = top;
-            l[h] *= by[h];
+            for (int e = 0; e < 4; ++e) x[j][e] = 0.0f;
+        const unsigned k_at = keys + ((lane & 7) + ((lane >> 3) & 1) * 8) * C::kPitch + (lane >> 4) * 16;
+        if (C::kHeld) {
 #pragma unroll
-            for (int j = 0; j < kN; ++j)
+            for (int k = 0; k < kSteps; ++k) {
+                unsigned ka[4];
+                ldsm4(ka, k_at + k * 32);
 #pragma unroll
-                for (int e = 2 * h; e < 2 * h + 2; ++e) { x[j][e] = exp2_of(x[j][e] - ref); l[h] += x[j][e]; }
+                for (int j = 0; j < kCols; ++j) mma<T>(x[j], ka, held[j * 2 * kSteps + 2 * k], held[j * 2 * kSteps + 2 * k + 1]);
+            }
+        } else {
+            const unsigned q_at = smem_of(s_q) + ((lane & 7) + (kCols > 1 ? (lane >> 4) * 8 : 0)) * C::kPitch + ((lane >> 3) & 1) * 16;
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                unsigned ka[4];
+                ldsm4(ka, k_at + k * 32);
+#pragma unroll
+                for (int j = 0; j < kCols; j += 2) {
+                    unsigned qb[4];
+                    ldsm4(qb, q_at + j * 8 * C::kPitch + k * 32);
+                    mma<T>(x[j], ka, qb[0], qb[1]);
+                    if (j + 1 < kCols) mma<T>(x[j + 1], ka, qb[2], qb[3]);
+                }
+            }
         }
-        if (__any_sync(0xffffffffu, scales)) {
+        // ---- what each row sees ----
+        const int slot0 = first_slot(now.q, now.idx) + part * 16, seen0 = now.q.length - now.q.count;
+        const bool whole = slot0 + 15 <= seen0 && (a.window == 0 || slot0 > now.q.length - 1 - a.window);
 #pragma unroll
-            for (int i = 0; i < 2 * kSteps; ++i)
+        for (int j = 0; j < kCols; ++j)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][e] *= by[e >> 1];
+            for (int e = 0; e < 4; ++e) {
+                x[j][e] *= a.scale_log2;
+                if (!whole && !sees(a, p[j][e & 1], slot0 + (lane >> 2) + (e >> 1) * 8)) x[j][e] = -INFINITY;
+            }
+        if (a.logits != nullptr) {
+            float *const to = a.logits + (begin + u) * (int64_t)(logit_pitch * kTile) + (part * 16 + (lane >> 2)) * logit_pitch;
+#pragma unroll
+            for (int j = 0; j < kCols; ++j) {
+                const int r = j * 8 + (lane & 3) * 2;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float2 w = make_float2(p[j][0] < 0 ? -INFINITY : x[j][2 * e], p[j][1] < 0 ? -INFINITY : x[j][2 * e + 1]);
+                    float *const at = to + e * 8 * logit_pitch + r;
+                    if (logit_pitch > 1) { if (r < logit_pitch) *(float2 *)at = w; }
+                    else if (r == 0) *at = w.x;
+                }
+            }
         }
-        // ---- the weights' products with the values ----
+        // ---- weights ----
+        bool over = false;
+#pragma unroll
+        for (int j = 0; j < kCols; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) over |= fmaxf(x[j][h], x[j][h + 2]) > m[j][h] + kSlack;
+        if (__any_sync(0xffffffffu, over)) {
+#pragma unroll
+            for (int j = 0; j < kCols; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    float top = fmaxf(x[j][h], x[j][h + 2]);
+#pragma unroll
+                    for (int o = 4; o < 32; o *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                    top = fmaxf(top, m[j][h]);
+                    const float by = exp2_of(m[j][h] - (top == -INFINITY ? 0.0f : top));
+                    m[j][h] = top;
+                    l[j][h] *= by;
+#pragma unroll
+                    for (int k = 0; k < kSteps; ++k) { acc[k][j][h] *= by; acc[k][j][h + 2] *= by; }
+                }
+        }
+#pragma unroll
+        for (int j = 0; j < kCols; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float ref = m[j][h] == -INFINITY ? 0.0f : m[j][h];
+                x[j][h] = exp2_of(x[j][h] - ref); x[j][h + 2] = exp2_of(x[j][h + 2] - ref);
+                l[j][h] += x[j][h] + x[j][h + 2];
+            }
+        // ---- O^T ----
         bool apart = false;
         if (!whole && now.q.count > 1) {
             // Slots that only some rows see: a weight of zero times an infinite or undefined value is not zero.
-            for (int i = lane; i < C::kTokens * C::kDim / 2; i += 32) {
+            for (int i = lane; i < 16 * C::kDim / 2; i += 32) {
                 unsigned w;
                 asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(values + i / (C::kDim / 2) * C::kPitch + i % (C::kDim / 2) * 4) : "memory");
                 const float2 f = Pair<T>::unpack(w);
@@ -375,115 +422,104 @@ __global__ void __launch_bounds__(32 * kRowTiles *kParts) k_cache_attend(const A
             apart = __any_sync(0xffffffffu, apart);
         }
         if (!apart) {
+            unsigned wb[kCols][2];
 #pragma unroll
-            for (int j = 0; j < kN; j += 2) {
-                unsigned pa[4], vb[4];
-                pa[0] = Pair<T>::pack(x[j][0], x[j][1]); pa[1] = Pair<T>::pack(x[j][2], x[j][3]);
-                pa[2] = Pair<T>::pack(x[j + 1][0], x[j + 1][1]); pa[3] = Pair<T>::pack(x[j + 1][2], x[j + 1][3]);
+            for (int j = 0; j < kCols; ++j)
 #pragma unroll
-                for (int k = 0; k < kSteps; ++k) {
-                    ldsm4t(vb, values + (j * 8 + (lane & 7) + ((lane >> 3) & 1) * 8) * C::kPitch + (2 * k + (lane >> 4)) * 16);
-                    mma<T>(acc[2 * k], pa, vb[0], vb[1]);
-                    mma<T>(acc[2 * k + 1], pa, vb[2], vb[3]);
-                }
+                for (int e = 0; e < 2; ++e) wb[j][e] = turned8x8(Pair<T>::pack(x[j][2 * e], x[j][2 * e + 1]));
+            const unsigned v_at = values + ((lane & 7) + ((lane >> 4) & 1) * 8) * C::kPitch + ((lane >> 3) & 1) * 16;
+#pragma unroll
+            for (int k = 0; k < kSteps; ++k) {
+                unsigned va[4];
+                ldsm4t(va, v_at + k * 32);
+#pragma unroll
+                for (int j = 0; j < kCols; ++j) mma<T>(acc[k][j], va, wb[j][0], wb[j][1]);
             }
         } else {
+            for (int o = 0; o < 16; ++o)
 #pragma unroll
-            for (int j = 0; j < kN; ++j)
-                for (int o = 0; o < 8; ++o)
+                for (int j = 0; j < kCols; ++j) {
+                    float w[2];
+                    bool in[2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
-                        const float mine = (o & 1) ? x[j][2 * h + 1] : x[j][2 * h];
-                        const float w = __shfl_sync(0xffffffffu, mine, (lane & ~3) | (o >> 1));
-                        if (sees(a, p[h], slot0 + j * 8 + o)) {
-#pragma unroll
-                            for (int i = 0; i < 2 * kSteps; ++i) {
-                                unsigned v;
-                                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(v) : "r"(values + (j * 8 + o) * C::kPitch + i * 16 + (lane & 3) * 4) : "memory");
-                                const float2 f = Pair<T>::unpack(v);
-                                acc[i][2 * h] = fmaf(w, f.x, acc[i][2 * h]); acc[i][2 * h + 1] = fmaf(w, f.y, acc[i][2 * h + 1]);
-                            }
-                        }
+                        w[h] = __shfl_sync(0xffffffffu, o < 8 ? x[j][h] : x[j][h + 2], (o & 7) * 4 + (lane & 3));
+                        in[h] = sees(a, p[j][h], slot0 + o);
                     }
-        }
-        if (more) {
-            if (tid < kTile) s_from[stage * kTile + tid] = row_from(page, slot_ahead);
-            cursor_next(a, ahead, per);
+#pragma unroll
+                    for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            unsigned short v;
+                            asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(values + o * C::kPitch + (k * 16 + e * 8 + (lane >> 2)) * 2) : "memory");
+                            const float f = Pair<T>::unpack(v).x;
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) if (in[h]) acc[k][j][2 * e + h] = fmaf(w[h], f, acc[k][j][2 * e + h]);
+                        }
+                }
         }
         const Cursor was = now;
         cursor_next(a, now, per);
-        // ---- the piece's end: the warps' parts are joined ----
         if (now.idx == 0 || u == n - 1) {
+            // ---- the piece's end: the parts are joined, each warp's sums in the part of its ring that it is done with ----
+            __syncwarp();
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                l[h] += __shfl_xor_sync(0xffffffffu, l[h], 1);
-                l[h] += __shfl_xor_sync(0xffffffffu, l[h], 2);
-                if ((lane & 3) == 0) s_ml[wp * C::kRows + wr * 16 + (lane >> 2) + 8 * h] = make_float2(m[h], l[h]);
-            }
-            __syncthreads();                             // (and nobody reads the tile any more)
-            float sum[2], f[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = wr * 16 + (lane >> 2) + 8 * h;
-                float top = -INFINITY;
-#pragma unroll
-                for (int q = 0; q < kParts; ++q) top = fmaxf(top, s_ml[q * C::kRows + r].x);
-                const float ref = top == -INFINITY ? 0.0f : top;
-                sum[h] = 0.0f;
-#pragma unroll
-                for (int q = 0; q < kParts; ++q) { const float2 v = s_ml[q * C::kRows + r]; sum[h] += v.y * exp2_of(v.x - ref); }
-                f[h] = exp2_of(m[h] - ref);
-                m[h] = top;
-            }
-#pragma unroll
-            for (int i = 0; i < 2 * kSteps; ++i)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[i][e] *= f[e >> 1];
-            float4 *const room = (float4 *)(smem + stage * C::kStageBytes);
-#pragma unroll
-            for (int half = kParts / 2; half > 0; half >>= 1) {
-                if (wp >= half && wp < 2 * half) {
-#pragma unroll
-                    for (int i = 0; i < 2 * kSteps; ++i)
-                        room[((wr * half + wp - half) * 2 * kSteps + i) * 32 + lane] = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
-                }
-                __syncthreads();
-                if (wp < half) {
-#pragma unroll
-                    for (int i = 0; i < 2 * kSteps; ++i) {
-                        const float4 o = room[((wr * half + wp) * 2 * kSteps + i) * 32 + lane];
-                        acc[i][0] += o.x; acc[i][1] += o.y; acc[i][2] += o.z; acc[i][3] += o.w;
-                    }
-                }
-                __syncthreads();
-            }
-            // is this all of the item?
-            const int first = u - was.idx;               // (the item's first tile, counted from the share's)
-            const bool all = first >= 0 && now.idx == 0 && was.idx == was.q.tiles - 1;
-            if (wp == 0) {
-                const int64_t piece = (item + blockIdx.x) * C::kRows;
+            for (int j = 0; j < kCols; ++j)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const int r = wr * 16 + (lane >> 2) + 8 * h, row = first_row + r;
+#pragma unroll
+                    for (int o = 4; o < 32; o *= 2) l[j][h] += __shfl_xor_sync(0xffffffffu, l[j][h], o);
+                    if (lane < 4) s_ml[part * C::kRows + j * 8 + lane * 2 + h] = p[j][h] < 0 ? make_float2(-INFINITY, 0.0f) : make_float2(m[j][h], l[j][h]);
+                }
+            float *const room = (float *)(smem + stage * C::kPartBytes);
+            constexpr int kApart = kStages * C::kPartBytes / 4;      // floats from one warp's to the next's
+            // is this all of the item?
+            const bool all = u >= was.idx && was.idx == was.q.tiles - 1;
+            const int64_t piece = (item + blockIdx.x) * C::kRows;
+#pragma unroll
+            for (int j0 = 0; j0 < kCols; j0 += C::kMerge) {
+                if (j0 > 0) __syncthreads();
+                constexpr int kSome = 8 * C::kMerge;     // rows in this step
+#pragma unroll
+                for (int j = j0; j < j0 + C::kMerge; ++j)
+#pragma unroll
+                    for (int k = 0; k < kSteps; ++k)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            room[part * kApart + ((j - j0) * 8 + (lane & 3) * 2 + (e & 1)) * C::kMergePitch + k * 16 + (e >> 1) * 8 + (lane >> 2)] = acc[k][j][e];
+                __syncthreads();
+                for (int i = tid; i < kSome * (C::kDim / 4); i += kThreads) {
+                    const int some = i / (C::kDim / 4), d = i % (C::kDim / 4) * 4;
+                    const int r = j0 * 8 + some, row = first_row + r;
                     if (row >= a.rows) continue;
-                    if ((lane & 3) == 0) a.ml[piece + r] = make_float2(m[h], sum[h]);
-                    if (all) {
+                    float top = -INFINITY, sum = 0.0f;
+#pragma unroll
+                    for (int q = 0; q < kParts; ++q) top = fmaxf(top, s_ml[q * C::kRows + r].x);
+                    const float ref = top == -INFINITY ? 0.0f : top;
+                    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+                    for (int q = 0; q < kParts; ++q) {
+                        const float2 ml = s_ml[q * C::kRows + r];
+                        const float f = exp2_of(ml.x - ref);
+                        const float4 v = *(const float4 *)&room[q * kApart + some * C::kMergePitch + d];
+                        sum = fmaf(ml.y, f, sum);
+                        o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
+                    }
+                    if (d == 0) a.ml[piece + r] = make_float2(top, sum);
+                    if (!all) {
+                        *(float4 *)(a.part + (piece + r) * C::kDim + d) = o;
+                    } else if (d < a.c.head_dim) {
                         const int64_t at = ((int64_t)was.s * a.new_tokens + row / a.group) * a.q_heads + (was.item / a.row_blocks) * a.group + row % a.group;
-                        const float inv = 1.0f / sum[h];                   // (sees nothing: zero, whatever the sums hold)
-#pragma unroll
-                        for (int i = 0; i < 2 * kSteps; ++i)
-                            if (i * 8 < a.c.head_dim)
-                                *(unsigned *)(a.out + 2 * (at * a.c.head_dim + i * 8 + (lane & 3) * 2)) =
-                                    sum[h] == 0.0f ? 0u : Pair<T>::pack(acc[i][2 * h] * inv, acc[i][2 * h + 1] * inv);
-                        if (a.lse != nullptr && (lane & 3) == 0) a.lse[at] = sum[h] == 0.0f ? -INFINITY : (m[h] + log2f(sum[h])) * 0.69314718055994531f;
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 2 * kSteps; ++i)
-                            *(float2 *)(a.part + (piece + r) * C::kDim + i * 8 + (lane & 3) * 2) = make_float2(acc[i][2 * h], acc[i][2 * h + 1]);
+                        const float inv = 1.0f / sum;    // (sees nothing: zero, whatever the sums hold)
+                        uint2 w = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
+                        if (sum == 0.0f) w = make_uint2(0, 0);
+                        *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
+                        if (a.lse != nullptr && d == 0) a.lse[at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
                     }
                 }
             }
             fresh = true;
+            __syncthreads();                             // (the ring may be written again)
         }
         stage = stage == kStages - 1 ? 0 : stage + 1;
     }
@@ -596,7 +632,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
     // ---- (3) ----
     Cursor now;
     cursor_at(a, now, s_place[2], from);
-    const int kept = min(block_rows, a.rows);
+    const int pitch = logit_rows(min(block_rows, a.rows));
+    for (int r = tid; r < 1024; r += kJoinThreads) s_lse[r] = INFINITY;              // (rows that do not exist: weight 0)
     int64_t before = s_place[2].before;                  // (tiles of the sequences before, one block of rows)
     ull bad = 0;
     for (int64_t u = from; u < to;) {
@@ -620,10 +657,20 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
             float w = 0.0f;
             for (int b = 0; b < a.row_blocks; ++b) {
                 const int64_t tile = before * a.row_blocks + (int64_t)(now.item * a.row_blocks + b) * now.q.tiles + idx;
-                const float *logit = a.logits + tile * (kept * kTile) + e % kTile;
-                const int rows = min(block_rows, a.rows - b * block_rows);
+                const float *logit = a.logits + (tile * kTile + e % kTile) * pitch;
+                const float *lse = s_lse + b * block_rows;
+                if (pitch >= 4) {
 #pragma unroll 4
-                for (int r = 0; r < rows; ++r) w += exp2_of(__ldcg(logit + r * kTile) - s_lse[b * block_rows + r]);
+                    for (int r = 0; r < pitch; r += 4) {
+                        const float4 x = __ldcg((const float4 *)(logit + r));
+                        w += exp2_of(x.x - lse[r]) + exp2_of(x.y - lse[r + 1]) + exp2_of(x.z - lse[r + 2]) + exp2_of(x.w - lse[r + 3]);
+                    }
+                } else if (pitch == 2) {
+                    const float2 x = __ldcg((const float2 *)logit);
+                    w += exp2_of(x.x - lse[0]) + exp2_of(x.y - lse[1]);
+                } else {
+                    w += exp2_of(__ldcg(logit) - lse[0]);
+                }
             }
             if (w == 0.0f) continue;
             const int page = cache_page(a.c, now.s, slot, bad);
@@ -638,11 +685,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
 }
 
 // ---- host ----
-template <typename T, int kSteps, int kRowTiles, int kParts, int kStages>
+template <typename T, int kSteps, int kCols, int kStages>
 cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
 {
-    typedef Config<T, kSteps, kRowTiles, kParts, kStages> C;
-    const auto kernel = k_cache_attend<T, kSteps, kRowTiles, kParts, kStages>;
+    typedef Config<T, kSteps, kCols, kStages> C;
+    const auto kernel = k_cache_attend<T, kSteps, kCols, kStages>;
     static int known[kMaxDevices];                       // blocks that the device holds at a time
     int dev = 0, room = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -651,7 +698,7 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     if (dev < kMaxDevices) room = __atomic_load_n(&known[dev], __ATOMIC_ACQUIRE);
     if (room == 0) {
         int each = 0;
-        if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, C::kThreads, C::kSmem)) != cudaSuccess) return e;
+        if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, kThreads, C::kSmem)) != cudaSuccess) return e;
         room = each * current_sm_count();
         if (room < 1) return cudaErrorInvalidDevice;
         if (dev < kMaxDevices) __atomic_store_n(&known[dev], room, __ATOMIC_RELEASE);
@@ -660,7 +707,7 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     int64_t grid = z.tiles < room ? z.tiles : room;
     grid = grid < 1 ? 1 : grid > kMaxBlocks ? kMaxBlocks : grid;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(C::kThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = s;
     if ((e = cudaLaunchKernelEx(&cfg, kernel, a, min_tiles)) != cudaSuccess) return e;
     // (the second kernel is brought in, and does its sums over the lengths, while the first still runs)
     cudaLaunchAttribute at[1];
@@ -669,20 +716,20 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
     return cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, min_tiles, C::kDim, C::kRows);
 }
-// Tiles in the ring: as many as let two blocks of four warps share an SM, or fill it for one block of eight.
-constexpr int stages_of(int steps, int row_tiles)
+// Tiles in the ring: as many as let two blocks share an SM, or, for wide heads, fill it for one.
+constexpr int stages_of(int steps, int cols)
 {
-    const int stage = 2 * kTile * (32 * steps + 16), rest = 16 * row_tiles * (32 * steps + 16) + 4 * 16 * row_tiles * 8;
-    const int room = row_tiles == 1 && steps <= 8 ? 113 * 1024 : 226 * 1024;
-    int n = (room - rest) / (stage + kTile * 8);
+    const int rest = (cols * steps <= 16 ? 0 : 8 * cols * (32 * steps + 16)) + kParts * 8 * cols * 8 + 1024;
+    const int n = ((steps <= 8 ? 113 : 226) * 1024 - rest) / (2 * kTile * (32 * steps + 16));
     return n > 6 ? 6 : n;
 }
 template <typename T, int kSteps>
 cudaError_t launch_steps(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
 {
-    if (z.row_tiles == 1) return launch<T, kSteps, 1, 4, stages_of(kSteps, 1)>(a, z, s);
-    if (z.row_tiles == 2) return launch<T, kSteps, 2, 4, stages_of(kSteps, 2)>(a, z, s);
-    return launch<T, kSteps, 4, 2, stages_of(kSteps, 4)>(a, z, s);
+    if (z.block_rows == 8) return launch<T, kSteps, 1, stages_of(kSteps, 1)>(a, z, s);
+    if (z.block_rows == 16) return launch<T, kSteps, 2, stages_of(kSteps, 2)>(a, z, s);
+    if constexpr (kSteps <= 8) return launch<T, kSteps, 4, stages_of(kSteps, 4)>(a, z, s);
+    return cudaErrorInvalidValue;                        // (wide heads: 16 rows at most)
 }
 template <typename T>
 cudaError_t launch_type(const AttendArgs &a, const AttendShape &z, cudaStream_t s)

@@ -8,11 +8,11 @@ cudaError_t launch_cache_attend_fp16(const AttendArgs &a, const AttendShape &z, 
 AttendShape attend_shape(const CacheView &c, int rows, int new_tokens, int window, int sinks)
 {
     AttendShape z;
-    z.row_tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    z.block_rows = 16 * z.row_tiles;
-    z.row_blocks = (rows + z.block_rows - 1) / z.block_rows;
     const int steps = (c.head_dim + 15) / 16;
     z.padded_dim = 16 * (steps <= 4 ? 4 : steps <= 6 ? steps : steps <= 8 ? 8 : steps <= 12 ? 12 : 16);
+    // rows that one block takes at a time: the accumulators of 32 (16 of wide heads) fill its registers
+    z.block_rows = rows <= 8 ? 8 : rows <= 16 || z.padded_dim > 128 ? 16 : 32;
+    z.row_blocks = (rows + z.block_rows - 1) / z.block_rows;
     int64_t tiles = ((int64_t)c.capacity + attend::kTile - 1) / attend::kTile;
     if (window > 0) {
         const int64_t seen = ((int64_t)sinks + attend::kTile - 1) / attend::kTile + ((int64_t)window + new_tokens + attend::kTile - 2) / attend::kTile + 1;
