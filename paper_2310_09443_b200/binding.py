@@ -532,16 +532,22 @@ def g10_characterize(K, N, use_ptr, uses, tensor_bytes, kernel_start_ns, num_per
 
 
 # ---- a key-value cache within a budget -----------------------------------------------------------------------------------
-def _same_device(device, *tensors):
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise G10Error("all tensors of a cache call have to be on %s: got one on %s" % (device, t.device))
+# (the checks run in front of kernels of a few microseconds: one pass over what each tensor has to be, the message made only if it is not)
+def _typed(name, t, dtype, shape, device):
+    """t has to be a contiguous tensor of this type and shape on the device (an index)."""
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device or not t.is_contiguous():
+        raise G10Error("%s has to be contiguous %s of shape %s on device %d: got %s of shape %s, strides %s, on %s" % (
+            name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.stride(), t.device))
 
 
-def _typed(name, t, dtype, shape=None, contiguous=True):
-    if t.dtype != dtype or (contiguous and not t.is_contiguous()) or (shape is not None and tuple(t.shape) != shape):
-        raise G10Error("%s has to be %s%s%s: got %s of shape %s" % (name, "contiguous " if contiguous else "", dtype,
-                                                                    "" if shape is None else " of shape %s" % (shape,), t.dtype, tuple(t.shape)))
+def _rows(name, t, cache, heads=None):
+    """Shape and strides of a tensor [seqs, new_tokens, heads, head_dim] of the cache's type, the last stride 1."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) != 4 or t.dtype is not cache.dtype or shape[0] != cache.num_seqs or shape[3] != cache.head_dim or strides[3] != 1 or \
+            (heads is not None and shape[2] != heads) or t.get_device() != cache.index:
+        raise G10Error("%s has to be %s [%d, new_tokens, %s, %d] on %s, the last stride 1: got %s of shape %s, strides %s, on %s" % (
+            name, cache.dtype, cache.num_seqs, "heads" if heads is None else heads, cache.head_dim, cache.device, t.dtype, tuple(shape), strides, t.device))
+    return shape, strides
 
 
 class CacheBuffers:
@@ -560,14 +566,17 @@ class CacheBuffers:
         if not lengths.is_cuda:
             raise G10Error("the cache has to be on a CUDA device")
         self.status = torch.zeros(1, dtype=torch.int64, device=self.device) if status is None else status
-        _same_device(self.device, k, v, page_table, lengths, seen, scores, positions, self.status)
+        self.index = index = self.device.index
+        for t in (k, v, page_table):
+            if t is not None and t.get_device() != index:
+                raise G10Error("all tensors of the cache have to be on %s: got one on %s" % (self.device, t.device))
         self.num_seqs = int(lengths.shape[0])
         if page_table.dim() != 2 or page_table.shape[0] != self.num_seqs or page_table.dtype != torch.int32 or page_table.stride(1) != 1 and page_table.shape[1] > 1:
             raise G10Error("page_table has to be int32 [%d, columns]" % self.num_seqs)
-        _typed("lengths", lengths, torch.int32, (self.num_seqs,))
-        _typed("status", self.status, torch.int64, (1,))
+        _typed("lengths", lengths, torch.int32, (self.num_seqs,), index)
+        _typed("status", self.status, torch.int64, (1,), index)
         if seen is not None:
-            _typed("seen", seen, torch.int32, (self.num_seqs,))
+            _typed("seen", seen, torch.int32, (self.num_seqs,), index)
         if (k is None) != (v is None):
             raise G10Error("k and v come together")
         if k is not None:
@@ -584,9 +593,9 @@ class CacheBuffers:
             self.dtype = torch.bfloat16
         cells = (self.num_pages, self.kv_heads, self.page_size)
         if scores is not None:
-            _typed("scores", scores, torch.float32, cells)
+            _typed("scores", scores, torch.float32, cells, index)
         if positions is not None:
-            _typed("positions", positions, torch.int32, cells)
+            _typed("positions", positions, torch.int32, cells, index)
         strides = k.stride() if k is not None else (0, 0, 0, 1)
         self.c_struct = _Cache(_CACHE_TYPES[self.dtype], self.num_seqs, self.kv_heads, self.head_dim, self.page_size, int(page_table.shape[1]),
                                self.num_pages, _ptr(k), _ptr(v), strides[0], strides[1], strides[2], _ptr(page_table), int(page_table.stride(0)),
@@ -597,24 +606,15 @@ class CacheBuffers:
 _CACHE_TYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 
-def _rows(name, t, cache, heads=None):
-    """A tensor [seqs, new_tokens, heads, head_dim] of the cache's type, the last stride 1."""
-    if t.dim() != 4 or t.dtype != cache.dtype or t.shape[0] != cache.num_seqs or t.shape[3] != cache.head_dim or (t.stride(3) != 1) or \
-            (heads is not None and t.shape[2] != heads):
-        raise G10Error("%s has to be %s [%d, new_tokens, %s, %d], the last stride 1: got %s of shape %s" % (
-            name, cache.dtype, cache.num_seqs, "heads" if heads is None else heads, cache.head_dim, t.dtype, tuple(t.shape)))
-    _same_device(cache.device, t)
-
-
-def _cache_call(cache, call, stream):
-    """Runs call(stream handle) with the cache's device current."""
-    if stream is not None:
-        handle = stream.cuda_stream
-    if torch._C._cuda_getDevice() == cache.device.index:
-        _check(call(torch._C._cuda_getCurrentRawStream(cache.device.index) if stream is None else handle))
-        return
-    with torch.cuda.device(cache.device):
-        _check(call(torch._C._cuda_getCurrentRawStream(cache.device.index) if stream is None else handle))
+def _cache_call(call, cache, args, stream):
+    """call(cache, *args, stream) with the cache's device current."""
+    if torch._C._cuda_getDevice() == cache.index:
+        rc = call(cache.ref, *args, torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream)
+    else:
+        with torch.cuda.device(cache.index):
+            rc = call(cache.ref, *args, torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream)
+    if rc != 0:
+        _check(rc)
 
 
 def g10_cache_append(cache: CacheBuffers, k, v, q=None, q_weight=None, k_weight=None, eps=1e-6, cos=None, sin=None, interleaved=False, counts=None,
@@ -623,38 +623,36 @@ def g10_cache_append(cache: CacheBuffers, k, v, q=None, q_weight=None, k_weight=
     head_dim], q [seqs, new_tokens, q_heads, head_dim] (strided views, as of one projection's output); q_weight, k_weight [head_dim]; cos, sin
     float32 [positions, rotary_dim / 2]; counts int32 [seqs]: tokens of each sequence that count (None: all).  cache.lengths (and seen) count the
     new tokens in.  Returns the queries (q_out, made here if None), or None without q."""
-    _rows("k", k, cache, cache.kv_heads)
-    _rows("v", v, cache, cache.kv_heads)
-    new = int(k.shape[1])
-    if v.shape[1] != new or (q is not None and q.shape[1] != new):
-        raise G10Error("q, k and v have to hold as many tokens")
-    heads = 0
+    dev, heads = cache.index, 0
+    shape, ks = _rows("k", k, cache, cache.kv_heads)
+    v_shape, vs = _rows("v", v, cache, cache.kv_heads)
+    new = shape[1]
+    qs = (0, 0, 0)
     if q is not None:
-        _rows("q", q, cache)
-        heads = int(q.shape[2])
+        q_shape, qs = _rows("q", q, cache)
+        heads = q_shape[2]
         if q_out is None:
-            q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+            q_out = torch.empty(q_shape, dtype=q.dtype, device=q.device)
         else:
-            _typed("q_out", q_out, cache.dtype, tuple(q.shape))
-    for name, w in (("q_weight", q_weight), ("k_weight", k_weight)):
-        if w is not None:
-            _typed(name, w, cache.dtype, (cache.head_dim,))
-    if (cos is None) != (sin is None):
-        raise G10Error("cos and sin come together")
+            _typed("q_out", q_out, cache.dtype, q_shape, dev)
+    if v_shape[1] != new or (heads and q_shape[1] != new):
+        raise G10Error("q, k and v have to hold as many tokens")
+    if q_weight is not None:
+        _typed("q_weight", q_weight, cache.dtype, (cache.head_dim,), dev)
+    if k_weight is not None:
+        _typed("k_weight", k_weight, cache.dtype, (cache.head_dim,), dev)
     half = rows = 0
-    if cos is not None:
-        if cos.dim() != 2:
-            raise G10Error("cos and sin have to be float32 [positions, rotary_dim / 2]")
-        rows, half = int(cos.shape[0]), int(cos.shape[1])
-        _typed("cos", cos, torch.float32)
-        _typed("sin", sin, torch.float32, (rows, half))
+    if cos is not None or sin is not None:
+        if cos is None or sin is None or cos.dim() != 2:
+            raise G10Error("cos and sin come together, float32 [positions, rotary_dim / 2]")
+        rows, half = cos.shape
+        _typed("cos", cos, torch.float32, (rows, half), dev)
+        _typed("sin", sin, torch.float32, (rows, half), dev)
     if counts is not None:
-        _typed("counts", counts, torch.int32, (cache.num_seqs,))
-    _same_device(cache.device, q_out, q_weight, k_weight, cos, sin, counts)
-    qs, ks, vs = (q.stride() if q is not None else (0, 0, 0)), k.stride(), v.stride()
-    t = _CacheTokens(new, heads, _ptr(q), _ptr(k), _ptr(v), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], _ptr(q_out) if heads else None,
+        _typed("counts", counts, torch.int32, (cache.num_seqs,), dev)
+    t = _CacheTokens(new, heads, _ptr(q), k.data_ptr(), v.data_ptr(), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], _ptr(q_out) if heads else None,
                      _ptr(counts), _ptr(q_weight), _ptr(k_weight), eps, _ptr(cos), _ptr(sin), rows, 2 * half, 1 if interleaved else 0)
-    _cache_call(cache, lambda s: load_library().g10_cache_append(cache.ref, C.byref(t), s), stream)
+    _cache_call(load_library().g10_cache_append, cache, (t,), stream)
     return q_out if heads else None
 
 
@@ -671,38 +669,35 @@ def g10_cache_attend(cache: CacheBuffers, q, scale=None, window=0, sinks=0, coun
     last `window` slots and the first `sinks` are visible (0: all).  add_scores: cache.scores grows by the weights that each slot received.
     ws: a uint8 device tensor of at least g10_cache_workspace_bytes(...) bytes (allocated here when None); calls that may overlap on the GPU, those of
     captured graphs among them, need one each."""
-    _rows("q", q, cache)
-    new, heads = int(q.shape[1]), int(q.shape[2])
+    shape, qs = _rows("q", q, cache)
+    dev, new, heads = cache.index, shape[1], shape[2]
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = torch.empty(shape, dtype=q.dtype, device=q.device)
     else:
-        _typed("out", out, cache.dtype, tuple(q.shape))
+        _typed("out", out, cache.dtype, shape, dev)
     if lse is not None:
-        _typed("lse", lse, torch.float32, tuple(q.shape[:3]))
+        _typed("lse", lse, torch.float32, shape[:3], dev)
     if counts is not None:
-        _typed("counts", counts, torch.int32, (cache.num_seqs,))
+        _typed("counts", counts, torch.int32, (cache.num_seqs,), dev)
     if ws is None:
         ws = torch.empty(max(256, g10_cache_workspace_bytes(cache, new, heads, window, sinks, add_scores)), dtype=torch.uint8, device=cache.device)
         if stream is not None:
             ws.record_stream(stream)
-    elif not ws.is_contiguous():
-        raise G10Error("ws has to be contiguous")
-    _same_device(cache.device, out, lse, counts, ws)
-    qs = q.stride()
-    u = _CacheQueries(new, heads, _ptr(q), qs[0], qs[1], qs[2], _ptr(counts), _ptr(out), _ptr(lse), cache.head_dim ** -0.5 if scale is None else scale,
+    elif ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
+        raise G10Error("ws has to be contiguous uint8 on %s" % cache.device)
+    u = _CacheQueries(new, heads, q.data_ptr(), qs[0], qs[1], qs[2], _ptr(counts), out.data_ptr(), _ptr(lse), cache.head_dim ** -0.5 if scale is None else scale,
                       window, sinks, 1 if add_scores else 0)
-    size = ws.numel() * ws.element_size()
-    _cache_call(cache, lambda s: load_library().g10_cache_attend(cache.ref, C.byref(u), _ptr(ws), size, s), stream)
+    _cache_call(load_library().g10_cache_attend, cache, (u, ws.data_ptr(), ws.numel()), stream)
     return out
 
 
 def _cache_plan(cache, budget, sinks, recent, moves, counts, new_lengths):
-    _typed("moves", moves, torch.int32, (cache.num_seqs, cache.kv_heads, budget, 2))
-    _typed("counts", counts, torch.int32, (cache.num_seqs, cache.kv_heads))
+    dev = cache.index
+    _typed("moves", moves, torch.int32, (cache.num_seqs, cache.kv_heads, budget, 2), dev)
+    _typed("counts", counts, torch.int32, (cache.num_seqs, cache.kv_heads), dev)
     if new_lengths is not None:
-        _typed("new_lengths", new_lengths, torch.int32, (cache.num_seqs,))
-    _same_device(cache.device, moves, counts, new_lengths)
-    return _CachePlan(budget, sinks, recent, _ptr(moves), _ptr(counts), _ptr(new_lengths))
+        _typed("new_lengths", new_lengths, torch.int32, (cache.num_seqs,), dev)
+    return _CachePlan(budget, sinks, recent, moves.data_ptr(), counts.data_ptr(), _ptr(new_lengths))
 
 
 def g10_cache_plan_evictions(cache: CacheBuffers, budget, sinks=0, recent=0, moves=None, counts=None, new_lengths=None, stream=None):
@@ -717,7 +712,7 @@ def g10_cache_plan_evictions(cache: CacheBuffers, budget, sinks=0, recent=0, mov
     if new_lengths is None:
         new_lengths = torch.empty(cache.num_seqs, dtype=torch.int32, device=dev)
     p = _cache_plan(cache, budget, sinks, recent, moves, counts, new_lengths)
-    _cache_call(cache, lambda s: load_library().g10_cache_plan_evictions(cache.ref, C.byref(p), s), stream)
+    _cache_call(load_library().g10_cache_plan_evictions, cache, (p,), stream)
     return SimpleNamespace(moves=moves, counts=counts, new_lengths=new_lengths)
 
 
@@ -725,7 +720,7 @@ def g10_cache_evict(cache: CacheBuffers, moves, counts, stream=None):
     """Carries the moves of a plan out (rows of k and v, scores, positions).  cache.lengths still are those that the plan was made for; the
     program takes new_lengths over once every layer has been evicted."""
     p = _cache_plan(cache, int(moves.shape[2]) if moves.dim() == 4 else 0, 0, 0, moves, counts, None)
-    _cache_call(cache, lambda s: load_library().g10_cache_evict(cache.ref, C.byref(p), s), stream)
+    _cache_call(load_library().g10_cache_evict, cache, (p,), stream)
 
 
 def instructions_numpy(em) -> np.ndarray:

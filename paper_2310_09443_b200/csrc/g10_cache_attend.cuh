@@ -117,9 +117,15 @@ __device__ __forceinline__ Share share_of(int64_t tiles, int per, int grid, int 
     r.blocks = (int)min((int64_t)grid, max((int64_t)1, (r.total + min_tiles - 1) / min_tiles));
     return r;
 }
-__device__ __forceinline__ int64_t begin_of(const Share &r, int b) { return b >= r.blocks ? r.total : r.total * b / r.blocks; }
+// (a division of 32-bit numbers where they are: a third of the instructions)
+__device__ __forceinline__ int64_t divided(int64_t x, int64_t by)
+{
+    if (((x | by) >> 32) == 0) return (int64_t)((unsigned)x / (unsigned)by);
+    return x / by;
+}
+__device__ __forceinline__ int64_t begin_of(const Share &r, int b) { return b >= r.blocks ? r.total : divided(r.total * b, r.blocks); }
 // Block whose share holds tile u.
-__device__ __forceinline__ int owner_of(int64_t u, const Share &r) { return (int)(((u + 1) * r.blocks - 1) / r.total); }
+__device__ __forceinline__ int owner_of(int64_t u, const Share &r) { return (int)divided((u + 1) * r.blocks - 1, r.total); }
 
 // Sequence that tile u lies in, and the tiles before it: written by the one thread that has it among its sequences (u < total).
 struct Place {
@@ -151,7 +157,7 @@ __device__ __forceinline__ void cursor_at(const AttendArgs &a, Cursor &u, const 
     u.s = p.s;
     u.q = seq_of(a, p.s, ignored);
     const int64_t in = tile - p.before;
-    u.item = (int)(in / u.q.tiles); u.idx = (int)(in % u.q.tiles);
+    u.item = (int)divided(in, u.q.tiles); u.idx = (int)(in - (int64_t)u.item * u.q.tiles);
 }
 __device__ __forceinline__ void cursor_next(const AttendArgs &a, Cursor &u, int per)
 {
@@ -572,40 +578,70 @@ __device__ __forceinline__ int lanes_for(int pieces)
     return n;
 }
 
-// The second kernel.  (1) An item that was cut into pieces is joined by the blocks that made them, each taking a part of its rows and
-// dimensions; (2) rows of sequences without tiles are written; (3) weights are booked, the slots of all (sequence, head) shared out anew.
+// The pieces of an item: of the blocks b0 .. b1.
+struct Pieces {
+    int64_t item;
+    int b0, b1;
+};
+__device__ __forceinline__ Pieces pieces_of(int64_t item, int64_t first, int tiles, const Share &r)
+{
+    return Pieces{item, owner_of(first, r), owner_of(first + tiles - 1, r)};
+}
+
+// The second kernel.  (1) An item that was cut into pieces is joined by the blocks that made them (the first of this grid), each taking a part of
+// its rows and dimensions; (2) rows of sequences without tiles are written; (3) weights are booked, the slots of all (sequence, head) shared out
+// anew.  What follows from the lengths alone is worked out while the first kernel still runs.
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a, int min_tiles, int padded_dim, int block_rows)
+__global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a, int min_tiles, int first_blocks, int padded_dim, int block_rows)
 {
     __shared__ float s_lse[1024];
     __shared__ Place s_place[3];
     const int tid = threadIdx.x, per = a.c.kv_heads * a.row_blocks;
     ull ignored = 0;
     const Tally tally = tally_of<kJoinThreads>(a, ignored);
-    const Share share = share_of(tally.total, per, gridDim.x, min_tiles);          // the first kernel's
-    const int64_t begin = begin_of(share, blockIdx.x), end = begin_of(share, blockIdx.x + 1);
+    const Share share = share_of(tally.total, per, first_blocks, min_tiles);       // the first kernel's
+    const int64_t begin = begin_of(share, min((int)blockIdx.x, share.blocks)), end = begin_of(share, min((int)blockIdx.x + 1, share.blocks));
     const Share slots = share_of(tally.total, a.c.kv_heads, gridDim.x, 1);         // of (3)
-    const int64_t from = begin_of(slots, blockIdx.x), to = begin_of(slots, blockIdx.x + 1);
+    const int64_t from = begin_of(slots, blockIdx.x), to = a.logits != nullptr ? begin_of(slots, blockIdx.x + 1) : from;
     if (begin < end) { place_of(a, tally, begin, per, &s_place[0]); place_of(a, tally, end - 1, per, &s_place[1]); }
-    if (a.logits != nullptr && from < to) place_of(a, tally, from, a.c.kv_heads, &s_place[2]);
+    if (from < to) place_of(a, tally, from, a.c.kv_heads, &s_place[2]);
     __syncthreads();
+    // (1): the items of the block's first and last tile (those between are whole)
+    Cursor at_end[2];
+    Pieces cut[2];
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        cut[side].b0 = cut[side].b1 = 0; cut[side].item = -1;
+        if (begin < end) {
+            const int64_t tile = side == 0 ? begin : end - 1;
+            Cursor &u = at_end[side];
+            cursor_at(a, u, s_place[side], tile);
+            cut[side] = pieces_of((int64_t)u.s * per + u.item, tile - u.idx, u.q.tiles, share);
+        }
+    }
+    // (3): where the slots begin
+    Cursor now;
+    now.s = 0; now.item = 0; now.idx = 0; now.q = Seq{0, 0, 0, 0, 0};
+    int64_t before = 0;                                  // (tiles of the sequences before, one block of rows)
+    Pieces of_now{0, 0, 0};                              // of the (sequence, head)'s first block of rows
+    if (from < to) {
+        cursor_at(a, now, s_place[2], from);
+        before = s_place[2].before;
+        of_now = pieces_of((int64_t)now.s * per + now.item * a.row_blocks, before * a.row_blocks + (int64_t)now.item * a.row_blocks * now.q.tiles, now.q.tiles, share);
+    }
     asm volatile("griddepcontrol.wait;" ::: "memory");
 
-    // ---- (1): the items of the block's first and last tile (those between are whole) ----
-    int64_t done = -1;
-    for (int side = 0; side < 2 && begin < end; ++side) {
-        const int64_t tile = side == 0 ? begin : end - 1;
-        Cursor u;
-        cursor_at(a, u, s_place[side], tile);
-        const int64_t item = (int64_t)u.s * per + u.item, first = tile - u.idx;
-        if (item == done) continue;
-        done = item;
-        const int b0 = owner_of(first, share), b1 = owner_of(first + u.q.tiles - 1, share), pieces = b1 - b0 + 1;
-        if (pieces == 1) continue;
+    // ---- (1) ----
+#pragma unroll
+    for (int side = 0; side < 2; ++side) {
+        const Cursor &u = at_end[side];
+        const int64_t item = cut[side].item;
+        const int b0 = cut[side].b0, b1 = cut[side].b1, pieces = b1 - b0 + 1;
+        if (pieces == 1 || (side == 1 && item == cut[0].item)) continue;
         const int lanes = lanes_for(pieces), teams = kJoinThreads / lanes;
         const int first_row = (u.item % a.row_blocks) * block_rows, rows = min(block_rows, a.rows - first_row);
-        const int quads = (a.c.head_dim + 3) / 4, all = rows * quads;
-        const int e0 = (int)((int64_t)all * ((int)blockIdx.x - b0) / pieces), e1 = (int)((int64_t)all * ((int)blockIdx.x - b0 + 1) / pieces);
+        const int quads = a.c.head_dim / 4, all = rows * quads;
+        const int e0 = (int)divided((int64_t)all * ((int)blockIdx.x - b0), pieces), e1 = (int)divided((int64_t)all * ((int)blockIdx.x - b0 + 1), pieces);
         for (int e = e0; e < e1; e += teams) {           // (all threads take part in the shuffles)
             const int mine = min(e + tid / lanes, e1 - 1), r = mine / quads, d = mine % quads * 4, row = first_row + r;
             const Part p = part_join<true>(a, item, b0, b1, block_rows, r, padded_dim, d, lanes);
@@ -627,60 +663,73 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
         if (a.lse != nullptr)
             for (int64_t i = tid; i < rows; i += kJoinThreads) a.lse[s * rows + i] = -INFINITY;
     }
-    if (a.logits == nullptr || from >= to) return;
+    if (from >= to) return;
 
     // ---- (3) ----
-    Cursor now;
-    cursor_at(a, now, s_place[2], from);
-    const int pitch = logit_rows(min(block_rows, a.rows));
-    for (int r = tid; r < 1024; r += kJoinThreads) s_lse[r] = INFINITY;              // (rows that do not exist: weight 0)
-    int64_t before = s_place[2].before;                  // (tiles of the sequences before, one block of rows)
+    const int pitch = logit_rows(min(block_rows, a.rows)), all_rows = a.row_blocks > 1 ? a.row_blocks * block_rows : pitch;
     ull bad = 0;
     for (int64_t u = from; u < to;) {
         const int n = (int)min((int64_t)(now.q.tiles - now.idx), to - u);          // tiles of this (sequence, head)
         __syncthreads();
+        for (int r = a.rows + tid; r < all_rows; r += kJoinThreads) s_lse[r] = INFINITY;         // (no such row: weight 0)
         for (int b = 0; b < a.row_blocks; ++b) {
-            const int i = now.item * a.row_blocks + b;
-            const int64_t first = before * a.row_blocks + (int64_t)i * now.q.tiles;
-            const int b0 = owner_of(first, share), b1 = owner_of(first + now.q.tiles - 1, share), lanes = lanes_for(b1 - b0 + 1), teams = kJoinThreads / lanes;
+            const Pieces w = b == 0 ? of_now : pieces_of(of_now.item + b, before * a.row_blocks + (int64_t)(now.item * a.row_blocks + b) * now.q.tiles, now.q.tiles, share);
+            const int lanes = lanes_for(w.b1 - w.b0 + 1), teams = kJoinThreads / lanes;
             const int rows = min(block_rows, a.rows - b * block_rows);
             for (int r0 = 0; r0 < rows; r0 += teams) {
                 const int r = min(r0 + tid / lanes, rows - 1);
-                const Part p = part_join<false>(a, (int64_t)now.s * per + i, b0, b1, block_rows, r, 0, 0, lanes);
+                const Part p = part_join<false>(a, w.item, w.b0, w.b1, block_rows, r, 0, 0, lanes);
                 if ((tid & (lanes - 1)) == 0) s_lse[b * block_rows + r] = p.sum == 0.0f ? INFINITY : p.top + log2f(p.sum);
             }
         }
         __syncthreads();
-        for (int e = tid; e < n * kTile; e += kJoinThreads) {
-            const int idx = now.idx + e / kTile, slot = first_slot(now.q, idx) + e % kTile;
-            if (slot >= now.q.length) continue;
-            float w = 0.0f;
+        // four slots at a time, so that their logits and pages are on the way together
+        constexpr int kAhead = 4;
+        const int64_t first_tile = before * a.row_blocks + (int64_t)now.item * a.row_blocks * now.q.tiles + now.idx;
+        for (int e0 = tid; e0 < n * kTile; e0 += kAhead * kJoinThreads) {
+            int page[kAhead], slot[kAhead];
+            float w[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) {
+                const int e = e0 + i * kJoinThreads;
+                slot[i] = e < n * kTile ? first_slot(now.q, now.idx + e / kTile) + e % kTile : 0x7fffffff;
+                page[i] = slot[i] < now.q.length ? cache_page(a.c, now.s, slot[i], bad) : -1;
+                w[i] = 0.0f;
+            }
             for (int b = 0; b < a.row_blocks; ++b) {
-                const int64_t tile = before * a.row_blocks + (int64_t)(now.item * a.row_blocks + b) * now.q.tiles + idx;
-                const float *logit = a.logits + (tile * kTile + e % kTile) * pitch;
-                const float *lse = s_lse + b * block_rows;
+                const float *const logit = a.logits + (first_tile + (int64_t)b * now.q.tiles) * kTile * pitch, *const lse = s_lse + b * block_rows;
                 if (pitch >= 4) {
-#pragma unroll 4
+#pragma unroll 2
                     for (int r = 0; r < pitch; r += 4) {
-                        const float4 x = __ldcg((const float4 *)(logit + r));
-                        w += exp2_of(x.x - lse[r]) + exp2_of(x.y - lse[r + 1]) + exp2_of(x.z - lse[r + 2]) + exp2_of(x.w - lse[r + 3]);
+                        float4 x[kAhead];
+#pragma unroll
+                        for (int i = 0; i < kAhead; ++i)
+                            if (page[i] >= 0) x[i] = __ldcg((const float4 *)(logit + (int64_t)(e0 + i * kJoinThreads) * pitch + r));
+#pragma unroll
+                        for (int i = 0; i < kAhead; ++i)
+                            if (page[i] >= 0) w[i] += exp2_of(x[i].x - lse[r]) + exp2_of(x[i].y - lse[r + 1]) + exp2_of(x[i].z - lse[r + 2]) + exp2_of(x[i].w - lse[r + 3]);
                     }
-                } else if (pitch == 2) {
-                    const float2 x = __ldcg((const float2 *)logit);
-                    w += exp2_of(x.x - lse[0]) + exp2_of(x.y - lse[1]);
                 } else {
-                    w += exp2_of(__ldcg(logit) - lse[0]);
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i)
+                        if (page[i] >= 0) {
+                            const float *const x = logit + (int64_t)(e0 + i * kJoinThreads) * pitch;
+                            w[i] += exp2_of(__ldcg(x) - lse[0]);
+                            if (pitch == 2) w[i] += exp2_of(__ldcg(x + 1) - lse[1]);
+                        }
                 }
             }
-            if (w == 0.0f) continue;
-            const int page = cache_page(a.c, now.s, slot, bad);
-            if (page >= 0) atomicAdd(&a.c.scores[cache_cell(a.c, page, slot, now.item)], w);
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (page[i] >= 0 && w[i] != 0.0f) atomicAdd(&a.c.scores[cache_cell(a.c, page[i], slot[i], now.item)], w[i]);
         }
         u += n;
         now.idx += n - 1;
         const int was = now.s, tiles = now.q.tiles;
         cursor_next(a, now, a.c.kv_heads);
         if (now.s != was) before += (int64_t)tiles * a.c.kv_heads;
+        if (u < to)
+            of_now = pieces_of((int64_t)now.s * per + now.item * a.row_blocks, before * a.row_blocks + (int64_t)now.item * a.row_blocks * now.q.tiles, now.q.tiles, share);
     }
 }
 
@@ -714,7 +763,9 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
-    return cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, min_tiles, C::kDim, C::kRows);
+    // (booking is all loads and additions here and there: three blocks an SM)
+    if (a.logits != nullptr) cfg.gridDim = dim3((unsigned)(z.tiles < 3 * 148 ? (z.tiles > grid ? z.tiles : grid) : grid > 3 * 148 ? grid : 3 * 148));
+    return cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, min_tiles, (int)grid, C::kDim, C::kRows);
 }
 // Tiles in the ring: as many as let two blocks share an SM, or, for wide heads, fill it for one.
 constexpr int stages_of(int steps, int cols)
