@@ -425,7 +425,7 @@ typedef struct g10_cache {
     int32_t max_pages;              /* columns of the page table; max_pages * page_size < 2^31 - 64 */
     int64_t num_pages;              /* pages of the pool, < 2^31                                   */
     void *k, *v;                    /* element d of (page, place, head): page * page_stride + place * slot_stride + head * head_stride + d;
-                                       16-byte aligned, strides multiples of 8 elements            */
+                                       16-byte aligned, strides >= 0 and multiples of 8, all offsets below 2^35 elements */
     int64_t page_stride, slot_stride, head_stride;
     const int32_t *page_table;      /* [num_seqs][table_stride], the first max_pages of a row are used */
     int64_t table_stride;

@@ -11,7 +11,7 @@ namespace g10 {
 // g10_cache with checked sizes; passed to kernels by value.
 struct CacheView {
     const char *k, *v;                   // (written by append and evict through the same addresses)
-    int64_t page_stride, slot_stride, head_stride;       // elements of 2 bytes
+    int64_t page_stride, slot_stride, head_stride;       // units of 16 bytes
     const int32_t *table;
     int64_t table_stride, num_pages;
     const int32_t *lengths, *seen;
@@ -20,6 +20,12 @@ struct CacheView {
     ull *status;
     int num_seqs, kv_heads, head_dim, page_size, max_pages;
     int capacity;                        // max_pages * page_size
+    unsigned page_mul, page_shift;       // slot / page_size = slot * page_mul >> page_shift
+};
+
+// Where a slot lies.
+struct Spot {
+    int page, place;                     // page -1: nowhere
 };
 
 // Slots that sequence s holds, as far as the table reaches.
@@ -40,22 +46,26 @@ __device__ __forceinline__ int cache_count(const int32_t *counts, int s, int new
     }
     return min(n, length);
 }
-// Page of a slot (slot < capacity), -1 if the table names none of the pool.
-__device__ __forceinline__ int cache_page(const CacheView &c, int s, int slot, ull &bad)
+// Page and place of a slot (0 <= slot < capacity).  With l = ceil(log2 page_size), page_mul = floor(2^(31 + l) / page_size) + 1: the product is too
+// large by slot * e / (page_size * 2^(31 + l)), 0 < e <= page_size <= 2^l, which is less than 1 / page_size for slots below 2^31: the quotient is exact.
+__device__ __forceinline__ Spot cache_spot(const CacheView &c, int s, int slot, ull &bad)
 {
-    const int page = __ldg(&c.table[(int64_t)s * c.table_stride + (unsigned)slot / (unsigned)c.page_size]);
-    if (page < 0 || page >= c.num_pages) { bad |= G10_DEV_BAD_PAGE; return -1; }
-    return page;
+    const int at = (int)(((ull)(unsigned)slot * c.page_mul) >> c.page_shift);
+    Spot o;
+    o.page = __ldg(&c.table[(int64_t)s * c.table_stride + at]);
+    o.place = slot - at * c.page_size;
+    if (o.page < 0 || o.page >= (int)c.num_pages) { bad |= G10_DEV_BAD_PAGE; o.page = -1; }
+    return o;
 }
-// First element of the row of (page, slot % page_size, head) in k or v.
-__device__ __forceinline__ int64_t cache_row(const CacheView &c, int page, int slot, int head)
+// Where a row of k and v begins, in units of 16 bytes (the host has checked that it fits).
+__device__ __forceinline__ unsigned cache_row(const CacheView &c, const Spot &o, int head)
 {
-    return (int64_t)page * c.page_stride + (int64_t)((unsigned)slot % (unsigned)c.page_size) * c.slot_stride + (int64_t)head * c.head_stride;
+    return (unsigned)((int64_t)o.page * c.page_stride + (int64_t)o.place * c.slot_stride + (int64_t)head * c.head_stride);
 }
 // Entry of scores and positions.
-__device__ __forceinline__ int64_t cache_cell(const CacheView &c, int page, int slot, int head)
+__device__ __forceinline__ int64_t cache_cell(const CacheView &c, const Spot &o, int head)
 {
-    return ((int64_t)page * c.kv_heads + head) * c.page_size + (unsigned)slot % (unsigned)c.page_size;
+    return ((int64_t)o.page * c.kv_heads + head) * c.page_size + o.place;
 }
 
 template <typename T>
@@ -106,7 +116,8 @@ struct AttendArgs {
     float scale_log2;                    // scale * log2 e
     int new_tokens, q_heads, group, rows, window, sinks;
     int row_blocks;                      // blocks of rows per key-value head
-    float2 *ml;                          // [pieces][block rows] running maximum and sum of every piece
+    int64_t pieces;                      // (room for so many)
+    float2 *ml;                          // [block rows][pieces] running maximum and sum of every piece
     float *part;                         // [pieces][block rows][padded head_dim] its sums, not divided yet
     float *logits;                       // [tiles][64][rows of a block] scaled by log2 e (null: weights are not booked)
 };

@@ -27,9 +27,17 @@ int32_t view_of(const g10_cache *c, bool rows, CacheView &o)
     if (rows && c->num_pages > 0) {
         if (!c->k || !c->v || !aligned16(c->k) || !aligned16(c->v)) return G10_ERR_ARG;
         if (!row_stride(c->page_stride) || !row_stride(c->slot_stride) || !row_stride(c->head_stride)) return G10_ERR_ARG;
+        if (c->page_stride < 0 || c->slot_stride < 0 || c->head_stride < 0) return G10_ERR_ARG;
+        // (rows are found by numbers of 32 bits, in units of 16 bytes)
+        const __int128 last = (__int128)(c->num_pages - 1) * c->page_stride + (__int128)(c->page_size - 1) * c->slot_stride + (__int128)(c->kv_heads - 1) * c->head_stride;
+        if (last / 8 >= 0xffffffffll) return G10_ERR_LIMIT;
     }
     o.k = (const char *)c->k; o.v = (const char *)c->v;
-    o.page_stride = c->page_stride; o.slot_stride = c->slot_stride; o.head_stride = c->head_stride;
+    o.page_stride = c->page_stride / 8; o.slot_stride = c->slot_stride / 8; o.head_stride = c->head_stride / 8;
+    int l = 0;
+    while ((1 << l) < c->page_size) ++l;
+    o.page_shift = 31 + l;
+    o.page_mul = (unsigned)(((uint64_t)1 << (31 + l)) / (uint64_t)c->page_size + 1);
     o.table = c->page_table; o.table_stride = c->table_stride; o.num_pages = c->num_pages;
     o.lengths = c->lengths; o.seen = c->seen ? c->seen : c->lengths;
     o.scores = c->scores; o.positions = c->positions; o.status = (ull *)c->status;
@@ -128,7 +136,7 @@ int32_t g10_cache_attend(const g10_cache *cache, const g10_cache_queries *u, voi
     const AttendShape z = attend_shape(a.c, a.rows, a.new_tokens, a.window, a.sinks);
     const AttendLayout l = attend_layout(z, u->add_scores != 0);
     if (!ws || ((uintptr_t)ws & (kAlign - 1)) || ws_bytes < l.bytes) return G10_ERR_WORKSPACE;
-    a.row_blocks = z.row_blocks;
+    a.row_blocks = z.row_blocks; a.pieces = z.pieces;
     a.ml = (float2 *)((char *)ws + l.ml); a.part = (float *)((char *)ws + l.part);
     a.logits = u->add_scores ? (float *)((char *)ws + l.logits) : nullptr;
     return status_of(launch_cache_attend(a, cache->dtype, (cudaStream_t)stream));

@@ -26,10 +26,10 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache_append(const AppendArg
     const int length = cache_length(c, s, bad), count = cache_count(a.counts, s, a.new_tokens, length, bad);
     const bool counts = t < count;
     const int slot = length - count + t;
-    int page = -1;
+    Spot spot{-1, 0};
     int64_t position = 0;
     if (counts) {
-        page = cache_page(c, s, slot, bad);
+        spot = cache_spot(c, s, slot, bad);
         position = (int64_t)__ldg(&c.seen[s]) - count + t;
     }
     const int d0 = lane * 8, half = a.rotary / 2;
@@ -59,7 +59,7 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache_append(const AppendArg
             to = a.q_out + 2 * ((token * a.q_heads + head) * c.head_dim);
         } else if (is_k || is_v) {
             from = is_k ? a.k + 2 * (s * a.k_seq + t * a.k_token + head * a.k_head) : a.v + 2 * (s * a.v_seq + t * a.v_token + head * a.v_head);
-            if (page >= 0) to = const_cast<char *>(is_k ? c.k : c.v) + 2 * cache_row(c, page, slot, head);
+            if (spot.page >= 0) to = const_cast<char *>(is_k ? c.k : c.v) + 16 * (int64_t)cache_row(c, spot, head);
         }
         uint4 u = make_uint4(0, 0, 0, 0);
         if (counts && from != nullptr && mine) u = *(const uint4 *)(from + 2 * d0);
@@ -114,8 +114,8 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache_append(const AppendArg
             if (!counts) u = make_uint4(0, 0, 0, 0);           // (a padding token's query: zero)
             if (counts || is_q) *(uint4 *)(to + 2 * d0) = u;
         }
-        if (is_k && page >= 0 && counts && lane == 0) {
-            const int64_t cell = cache_cell(c, page, slot, head);
+        if (is_k && spot.page >= 0 && counts && lane == 0) {
+            const int64_t cell = cache_cell(c, spot, head);
             if (c.scores != nullptr) c.scores[cell] = 0.0f;
             if (c.positions != nullptr) c.positions[cell] = (int32_t)position;
         }

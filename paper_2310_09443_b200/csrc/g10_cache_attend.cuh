@@ -110,11 +110,15 @@ struct Share {
     int64_t total;                       // tiles in all
     int blocks;                          // that share them
 };
-__device__ __forceinline__ Share share_of(int64_t tiles, int per, int grid, int min_tiles)
+// `held` blocks run at a time, and each takes one share, of equal length.  Equal shares do not take equally long (with one share each, the first block of
+// 64 sequences of 16 000 slots ended after 75 % of the time): where they are long they are cut into kCuts, and the blocks that wait for a place even
+// it out (424 -> 412 us there).  Shorter ones are not: 320 blocks of 24 tiles, where 296 run at a time, take two rounds (49 -> 71 us).
+constexpr int kLong = 128, kCuts = 4;    // tiles
+__device__ __forceinline__ Share share_of(int64_t tiles, int per, int grid, int held)
 {
     Share r;
     r.total = tiles * per;
-    r.blocks = (int)min((int64_t)grid, max((int64_t)1, (r.total + min_tiles - 1) / min_tiles));
+    r.blocks = r.total >= (int64_t)kLong * held ? grid : (int)max((int64_t)1, min((int64_t)held, r.total));
     return r;
 }
 // (a division of 32-bit numbers where they are: a third of the instructions)
@@ -149,6 +153,7 @@ __device__ __forceinline__ void place_of(const AttendArgs &a, const Tally &t, in
 // A place in the run of tiles.
 struct Cursor {
     int s, item, idx;                    // sequence, item of the sequence, tile of the item
+    int head, block;                     // key-value head and block of rows: item = head * row_blocks + block
     Seq q;
 };
 __device__ __forceinline__ void cursor_at(const AttendArgs &a, Cursor &u, const Place &p, int64_t tile)
@@ -158,13 +163,15 @@ __device__ __forceinline__ void cursor_at(const AttendArgs &a, Cursor &u, const 
     u.q = seq_of(a, p.s, ignored);
     const int64_t in = tile - p.before;
     u.item = (int)divided(in, u.q.tiles); u.idx = (int)(in - (int64_t)u.item * u.q.tiles);
+    u.head = u.item / a.row_blocks; u.block = u.item - u.head * a.row_blocks;
 }
 __device__ __forceinline__ void cursor_next(const AttendArgs &a, Cursor &u, int per)
 {
     if (++u.idx < u.q.tiles) return;
     u.idx = 0;
+    if (++u.block == a.row_blocks) { u.block = 0; ++u.head; }
     if (++u.item < per) return;
-    u.item = 0;
+    u.item = u.head = u.block = 0;
     ull ignored = 0;
     do {
         if (++u.s >= a.c.num_seqs) { u.s = a.c.num_seqs; u.q.tiles = 0; return; }       // (behind the last: never used)
@@ -174,7 +181,11 @@ __device__ __forceinline__ void cursor_next(const AttendArgs &a, Cursor &u, int 
 
 __device__ __forceinline__ bool sees(const AttendArgs &a, int p, int slot) { return slot <= p && (a.window == 0 || slot < a.sinks || slot > p - a.window); }
 
-__device__ __forceinline__ void copy16(unsigned dst, const void *src, bool there)
+__device__ __forceinline__ void copy16(unsigned dst, const void *src)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copy16_or_zeros(unsigned dst, const void *src, bool there)
 {
     const int n = there ? 16 : 0;        // (0: 16 zero bytes)
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
@@ -218,7 +229,7 @@ struct Config {
 // ref is a maximum of the past: the weights are taken relative to it as long as no logit is more than kSlack above it (weights up to 2^8,
 // which either type holds), so that the sums are rescaled and the warp's lanes compared only when that fails, a few times per piece.
 template <typename T, int kSteps, int kCols, int kStages>
-__global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, int min_tiles)
+__global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, int held_blocks)
 {
     typedef Config<T, kSteps, kCols, kStages> C;
     extern __shared__ __align__(128) char smem[];
@@ -230,7 +241,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
     ull bad = 0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const Tally tally = tally_of<kThreads>(a, bad);
-    const Share share = share_of(tally.total, per, gridDim.x, min_tiles);
+    const Share share = share_of(tally.total, per, gridDim.x, held_blocks);
     const int64_t begin = begin_of(share, blockIdx.x);
     const int n = (int)(begin_of(share, blockIdx.x + 1) - begin);
     if (bad != 0) raise_status(a.c.status, bad);
@@ -243,27 +254,39 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
     cursor_at(a, now, s_place, begin);
     ahead = now;
     const unsigned ring = smem_of(smem) + part * kStages * C::kPartBytes;
-    // where the row of this lane's slot lies (lanes 16 .. 31: as lanes 0 .. 15), in the tile that `ahead` stands at; -1: zeros
-    auto look_up = [&]() -> int64_t {
+    // where the row of this lane's slot begins (lanes 16 .. 31: as lanes 0 .. 15), in the tile that `ahead` stands at
+    constexpr unsigned kNone = 0xffffffffu;              // (nothing to read: zeros)
+    auto look_up = [&]() -> unsigned {
         const int slot = first_slot(ahead.q, ahead.idx) + part * 16 + (lane & 15);
-        if (slot >= ahead.q.length || !(a.window == 0 || slot < a.sinks || slot > ahead.q.length - ahead.q.count - a.window)) return -1;
-        const int page = cache_page(a.c, ahead.s, slot, bad);
-        return page < 0 ? -1 : 2 * cache_row(a.c, page, slot, ahead.item / a.row_blocks);
+        if (slot >= ahead.q.length || !(a.window == 0 || slot < a.sinks || slot > ahead.q.length - ahead.q.count - a.window)) return kNone;
+        const Spot o = cache_spot(a.c, ahead.s, slot, bad);
+        return o.page < 0 ? kNone : cache_row(a.c, o, ahead.head);
     };
-    auto issue = [&](int stage, int64_t row_at) {
+    auto issue = [&](int stage, unsigned row_at) {
         constexpr int kChunks = 2 * kSteps;              // of 16 bytes in a row
         const unsigned to = ring + stage * C::kPartBytes;
+        const bool all = __all_sync(0xffffffffu, row_at != kNone) && a.c.head_dim == C::kDim;
+        if (all) {                                       // (nearly always: an address, a shuffle and two copies)
 #pragma unroll
-        for (int i = 0; i < 16 * kChunks / 32; ++i) {
-            const int c = i * 32 + lane, row = c / kChunks, chunk = c % kChunks;
-            const int64_t from = __shfl_sync(0xffffffffu, row_at, row);
-            const bool there = from >= 0 && chunk * 8 < a.c.head_dim;
-            const int64_t at = there ? from + 16 * chunk : 0;
-            copy16(to + row * C::kPitch + chunk * 16, a.c.k + at, there);
-            copy16(to + (16 + row) * C::kPitch + chunk * 16, a.c.v + at, there);
+            for (int i = 0; i < 16 * kChunks / 32; ++i) {
+                const int c = i * 32 + lane, row = c / kChunks, chunk = c % kChunks;
+                const int64_t at = 16 * (int64_t)__shfl_sync(0xffffffffu, row_at, row);
+                copy16(to + row * C::kPitch + chunk * 16, a.c.k + 16 * chunk + at);
+                copy16(to + (16 + row) * C::kPitch + chunk * 16, a.c.v + 16 * chunk + at);
+            }
+        } else {
+#pragma unroll 1
+            for (int i = 0; i < 16 * kChunks / 32; ++i) {
+                const int c = i * 32 + lane, row = c / kChunks, chunk = c % kChunks;
+                const unsigned from = __shfl_sync(0xffffffffu, row_at, row);
+                const bool there = from != kNone && chunk * 8 < a.c.head_dim;
+                const int64_t at = there ? 16 * ((int64_t)from + chunk) : 0;
+                copy16_or_zeros(to + row * C::kPitch + chunk * 16, a.c.k + at, there);
+                copy16_or_zeros(to + (16 + row) * C::kPitch + chunk * 16, a.c.v + at, there);
+            }
         }
     };
-    int64_t next_row = -1;                               // of the tile to be issued next
+    unsigned next_row = kNone;                           // of the tile to be issued next
 #pragma unroll
     for (int i = 0; i < kStages; ++i) {
         if (i > 0) {
@@ -284,8 +307,8 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
         if (fresh) {                                     // a new item: its queries
             fresh = false;
             item = (int64_t)now.s * per + now.item;
-            first_row = (now.item % a.row_blocks) * C::kRows;
-            const int head = now.item / a.row_blocks;
+            first_row = now.block * C::kRows;
+            const int head = now.head;
             auto row_of = [&](int r) -> const char * {   // (null: no such row)
                 const int row = first_row + r, t = row / a.group;
                 if (row >= a.rows || t >= now.q.count) return nullptr;
@@ -464,9 +487,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
                         }
                 }
         }
-        const Cursor was = now;
-        cursor_next(a, now, per);
-        if (now.idx == 0 || u == n - 1) {
+        if (now.idx == now.q.tiles - 1 || u == n - 1) {
             // ---- the piece's end: the parts are joined, each warp's sums in the part of its ring that it is done with ----
             __syncwarp();
 #pragma unroll
@@ -480,8 +501,8 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
             float *const room = (float *)(smem + stage * C::kPartBytes);
             constexpr int kApart = kStages * C::kPartBytes / 4;      // floats from one warp's to the next's
             // is this all of the item?
-            const bool all = u >= was.idx && was.idx == was.q.tiles - 1;
-            const int64_t piece = (item + blockIdx.x) * C::kRows;
+            const bool all = u >= now.idx && now.idx == now.q.tiles - 1;
+            const int64_t piece = item + blockIdx.x;
 #pragma unroll
             for (int j0 = 0; j0 < kCols; j0 += C::kMerge) {
                 if (j0 > 0) __syncthreads();
@@ -511,11 +532,11 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
                         sum = fmaf(ml.y, f, sum);
                         o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
                     }
-                    if (d == 0) a.ml[piece + r] = make_float2(top, sum);
+                    if (d == 0) a.ml[r * a.pieces + piece] = make_float2(top, sum);
                     if (!all) {
-                        *(float4 *)(a.part + (piece + r) * C::kDim + d) = o;
+                        *(float4 *)(a.part + (piece * C::kRows + r) * C::kDim + d) = o;
                     } else if (d < a.c.head_dim) {
-                        const int64_t at = ((int64_t)was.s * a.new_tokens + row / a.group) * a.q_heads + (was.item / a.row_blocks) * a.group + row % a.group;
+                        const int64_t at = ((int64_t)now.s * a.new_tokens + row / a.group) * a.q_heads + now.head * a.group + row % a.group;
                         const float inv = 1.0f / sum;    // (sees nothing: zero, whatever the sums hold)
                         uint2 w = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
                         if (sum == 0.0f) w = make_uint2(0, 0);
@@ -528,6 +549,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
             __syncthreads();                             // (the ring may be written again)
         }
         stage = stage == kStages - 1 ? 0 : stage + 1;
+        cursor_next(a, now, per);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (bad != 0) raise_status(a.c.status, bad);
@@ -555,10 +577,9 @@ __device__ __forceinline__ Part part_join(const AttendArgs &a, int64_t item, int
     p.top = -INFINITY; p.sum = 0.0f; p.o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
     for (int b = b0 + lane; b <= b1; b += lanes) {
-        const int64_t piece = (item + b) * block_rows + r;
-        const float2 ml = __ldcg(&a.ml[piece]);
+        const float2 ml = __ldcg(&a.ml[r * a.pieces + item + b]);
         float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (kSums) o = __ldcg((const float4 *)(a.part + piece * padded_dim + d));
+        if (kSums) o = __ldcg((const float4 *)(a.part + ((item + b) * block_rows + r) * padded_dim + d));
         part_add(p, ml.x, ml.y, o);
     }
     for (int o = lanes / 2; o > 0; o >>= 1) {
@@ -588,73 +609,84 @@ __device__ __forceinline__ Pieces pieces_of(int64_t item, int64_t first, int til
     return Pieces{item, owner_of(first, r), owner_of(first + tiles - 1, r)};
 }
 
-// The second kernel.  (1) An item that was cut into pieces is joined by the blocks that made them (the first of this grid), each taking a part of
-// its rows and dimensions; (2) rows of sequences without tiles are written; (3) weights are booked, the slots of all (sequence, head) shared out
-// anew.  What follows from the lengths alone is worked out while the first kernel still runs.
+// What a block of the second kernel has to do, worked out by one warp.
+struct Segment {                         // a run of slots of one (sequence, head)
+    Cursor at;
+    int64_t before;                      // tiles of the sequences before, one block of rows
+    Pieces pieces;                       // of its first block of rows
+};
+__device__ __forceinline__ Pieces pieces_at(const AttendArgs &a, const Segment &g, int per, int block, const Share &share)
+{
+    const int64_t i = (int64_t)g.at.item * a.row_blocks + block;
+    return pieces_of((int64_t)g.at.s * per + i, g.before * a.row_blocks + i * g.at.q.tiles, g.at.q.tiles, share);
+}
+
+// The second kernel.  (1) An item that was cut into pieces is joined by the blocks whose turn its pieces' shares are, each taking a part of its rows
+// and dimensions; (2) rows of sequences without tiles are written; (3) weights are booked, the slots of all (sequence, head) shared out
+// anew.  What follows from the lengths alone is worked out while the first kernel still runs, by one warp each.
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a, int min_tiles, int first_blocks, int padded_dim, int block_rows)
+__global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a, int first_grid, int held_blocks, int padded_dim, int block_rows)
 {
     __shared__ float s_lse[1024];
     __shared__ Place s_place[3];
-    const int tid = threadIdx.x, per = a.c.kv_heads * a.row_blocks;
+    __shared__ Cursor s_cut[2];
+    __shared__ Pieces s_pieces[2];
+    __shared__ Segment s_segment;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = a.c.kv_heads * a.row_blocks;
     ull ignored = 0;
     const Tally tally = tally_of<kJoinThreads>(a, ignored);
-    const Share share = share_of(tally.total, per, first_blocks, min_tiles);       // the first kernel's
-    const int64_t begin = begin_of(share, min((int)blockIdx.x, share.blocks)), end = begin_of(share, min((int)blockIdx.x + 1, share.blocks));
-    const Share slots = share_of(tally.total, a.c.kv_heads, gridDim.x, 1);         // of (3)
-    const int64_t from = begin_of(slots, blockIdx.x), to = a.logits != nullptr ? begin_of(slots, blockIdx.x + 1) : from;
-    if (begin < end) { place_of(a, tally, begin, per, &s_place[0]); place_of(a, tally, end - 1, per, &s_place[1]); }
+    const Share share = share_of(tally.total, per, first_grid, held_blocks);       // the first kernel's
+    Share slots;                                         // of (3)
+    slots.total = a.logits != nullptr ? tally.total * a.c.kv_heads : 0; slots.blocks = gridDim.x;
+    const int64_t from = begin_of(slots, blockIdx.x), to = begin_of(slots, blockIdx.x + 1);
     if (from < to) place_of(a, tally, from, a.c.kv_heads, &s_place[2]);
-    __syncthreads();
-    // (1): the items of the block's first and last tile (those between are whole)
-    Cursor at_end[2];
-    Pieces cut[2];
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        cut[side].b0 = cut[side].b1 = 0; cut[side].item = -1;
-        if (begin < end) {
-            const int64_t tile = side == 0 ? begin : end - 1;
-            Cursor &u = at_end[side];
-            cursor_at(a, u, s_place[side], tile);
-            cut[side] = pieces_of((int64_t)u.s * per + u.item, tile - u.idx, u.q.tiles, share);
+    bool waited = false;
+    // ---- (1): the items of a share's first and last tile (those between are whole) ----
+    for (int b = blockIdx.x; b < share.blocks; b += gridDim.x) {
+        const int64_t begin = begin_of(share, b), end = begin_of(share, b + 1);
+        place_of(a, tally, begin, per, &s_place[0]); place_of(a, tally, end - 1, per, &s_place[1]);
+        __syncthreads();
+        if (warp < 2) {
+            const int64_t tile = warp == 0 ? begin : end - 1;
+            Cursor u;
+            cursor_at(a, u, s_place[warp], tile);
+            const Pieces p = pieces_of((int64_t)u.s * per + u.item, tile - u.idx, u.q.tiles, share);
+            if (lane == 0) { s_cut[warp] = u; s_pieces[warp] = p; }
+        } else if (warp == 2 && !waited && from < to) {
+            Segment g;
+            cursor_at(a, g.at, s_place[2], from);
+            g.before = s_place[2].before;
+            g.pieces = pieces_at(a, g, per, 0, share);
+            if (lane == 0) s_segment = g;
         }
-    }
-    // (3): where the slots begin
-    Cursor now;
-    now.s = 0; now.item = 0; now.idx = 0; now.q = Seq{0, 0, 0, 0, 0};
-    int64_t before = 0;                                  // (tiles of the sequences before, one block of rows)
-    Pieces of_now{0, 0, 0};                              // of the (sequence, head)'s first block of rows
-    if (from < to) {
-        cursor_at(a, now, s_place[2], from);
-        before = s_place[2].before;
-        of_now = pieces_of((int64_t)now.s * per + now.item * a.row_blocks, before * a.row_blocks + (int64_t)now.item * a.row_blocks * now.q.tiles, now.q.tiles, share);
-    }
-    asm volatile("griddepcontrol.wait;" ::: "memory");
-
-    // ---- (1) ----
-#pragma unroll
-    for (int side = 0; side < 2; ++side) {
-        const Cursor &u = at_end[side];
-        const int64_t item = cut[side].item;
-        const int b0 = cut[side].b0, b1 = cut[side].b1, pieces = b1 - b0 + 1;
-        if (pieces == 1 || (side == 1 && item == cut[0].item)) continue;
-        const int lanes = lanes_for(pieces), teams = kJoinThreads / lanes;
-        const int first_row = (u.item % a.row_blocks) * block_rows, rows = min(block_rows, a.rows - first_row);
-        const int quads = a.c.head_dim / 4, all = rows * quads;
-        const int e0 = (int)divided((int64_t)all * ((int)blockIdx.x - b0), pieces), e1 = (int)divided((int64_t)all * ((int)blockIdx.x - b0 + 1), pieces);
-        for (int e = e0; e < e1; e += teams) {           // (all threads take part in the shuffles)
-            const int mine = min(e + tid / lanes, e1 - 1), r = mine / quads, d = mine % quads * 4, row = first_row + r;
-            const Part p = part_join<true>(a, item, b0, b1, block_rows, r, padded_dim, d, lanes);
-            if (e + tid / lanes < e1 && (tid & (lanes - 1)) == 0) {
-                const int64_t at = ((int64_t)u.s * a.new_tokens + row / a.group) * a.q_heads + (u.item / a.row_blocks) * a.group + row % a.group;
-                const float inv = 1.0f / p.sum;
-                uint2 w = make_uint2(Pair<T>::pack(p.o.x * inv, p.o.y * inv), Pair<T>::pack(p.o.z * inv, p.o.w * inv));
-                if (p.sum == 0.0f) w = make_uint2(0, 0);
-                *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
-                if (a.lse != nullptr && d == 0) a.lse[at] = p.sum == 0.0f ? -INFINITY : (p.top + log2f(p.sum)) * 0.69314718055994531f;
+        if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+        waited = true;
+        __syncthreads();
+#pragma unroll 1
+        for (int side = 0; side < 2; ++side) {
+            const Pieces w = s_pieces[side];
+            const int pieces = w.b1 - w.b0 + 1;
+            if (pieces == 1 || (side == 1 && w.item == s_pieces[0].item)) continue;
+            const int s = s_cut[side].s, head = s_cut[side].head, first_row = s_cut[side].block * block_rows, rows = min(block_rows, a.rows - first_row);
+            const int lanes = lanes_for(pieces), teams = kJoinThreads / lanes;
+            const int quads = a.c.head_dim / 4, all = rows * quads;
+            const int e0 = all * (b - w.b0) / pieces, e1 = all * (b - w.b0 + 1) / pieces;        // (64 rows at most: 32 bits)
+            for (int e = e0 + warp * 32 / lanes; e < e1; e += teams) {             // (whole warps: all lanes take part in the shuffles)
+                const int mine = min(e + lane / lanes, e1 - 1), r = mine / quads, d = mine % quads * 4, row = first_row + r;
+                const Part p = part_join<true>(a, w.item, w.b0, w.b1, block_rows, r, padded_dim, d, lanes);
+                if (e + lane / lanes < e1 && (lane & (lanes - 1)) == 0) {
+                    const int64_t at = ((int64_t)s * a.new_tokens + row / a.group) * a.q_heads + head * a.group + row % a.group;
+                    const float inv = 1.0f / p.sum;
+                    uint2 o = make_uint2(Pair<T>::pack(p.o.x * inv, p.o.y * inv), Pair<T>::pack(p.o.z * inv, p.o.w * inv));
+                    if (p.sum == 0.0f) o = make_uint2(0, 0);
+                    *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = o;
+                    if (a.lse != nullptr && d == 0) a.lse[at] = p.sum == 0.0f ? -INFINITY : (p.top + log2f(p.sum)) * 0.69314718055994531f;
+                }
             }
         }
+        __syncthreads();
     }
+    if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
     // ---- (2) ----
     for (int s = blockIdx.x; s < a.c.num_seqs; s += gridDim.x) {
         if (seq_of(a, s, ignored).tiles > 0) continue;
@@ -668,69 +700,90 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
     // ---- (3) ----
     const int pitch = logit_rows(min(block_rows, a.rows)), all_rows = a.row_blocks > 1 ? a.row_blocks * block_rows : pitch;
     ull bad = 0;
-    for (int64_t u = from; u < to;) {
-        const int n = (int)min((int64_t)(now.q.tiles - now.idx), to - u);          // tiles of this (sequence, head)
+    if (!waited || blockIdx.x >= share.blocks) {         // (a block without a share of its own)
         __syncthreads();
+        if (warp == 0) {
+            Segment g;
+            cursor_at(a, g.at, s_place[2], from);
+            g.before = s_place[2].before;
+            g.pieces = pieces_at(a, g, per, 0, share);
+            if (lane == 0) s_segment = g;
+        }
+    }
+    __syncthreads();
+    for (int64_t u = from; u < to;) {
+        const Segment g = s_segment;
+        const Cursor &now = g.at;
+        const int64_t before = g.before;
+        const int n = (int)min((int64_t)(now.q.tiles - now.idx), to - u);          // tiles of this (sequence, head)
         for (int r = a.rows + tid; r < all_rows; r += kJoinThreads) s_lse[r] = INFINITY;         // (no such row: weight 0)
         for (int b = 0; b < a.row_blocks; ++b) {
-            const Pieces w = b == 0 ? of_now : pieces_of(of_now.item + b, before * a.row_blocks + (int64_t)(now.item * a.row_blocks + b) * now.q.tiles, now.q.tiles, share);
+            const Pieces w = b == 0 ? g.pieces : pieces_at(a, g, per, b, share);
             const int lanes = lanes_for(w.b1 - w.b0 + 1), teams = kJoinThreads / lanes;
             const int rows = min(block_rows, a.rows - b * block_rows);
-            for (int r0 = 0; r0 < rows; r0 += teams) {
-                const int r = min(r0 + tid / lanes, rows - 1);
+            for (int r0 = warp * 32 / lanes; r0 < rows; r0 += teams) {             // (warps without a row have nothing to do)
+                const int r = min(r0 + lane / lanes, rows - 1);
                 const Part p = part_join<false>(a, w.item, w.b0, w.b1, block_rows, r, 0, 0, lanes);
-                if ((tid & (lanes - 1)) == 0) s_lse[b * block_rows + r] = p.sum == 0.0f ? INFINITY : p.top + log2f(p.sum);
+                if ((lane & (lanes - 1)) == 0) s_lse[b * block_rows + r] = p.sum == 0.0f ? INFINITY : p.top + log2f(p.sum);
             }
         }
         __syncthreads();
-        // four slots at a time, so that their logits and pages are on the way together
+        if (warp == kJoinThreads / 32 - 1 && u + n < to) {                         // the next one, meanwhile
+            Segment h = g;
+            h.at.idx += n - 1;
+            cursor_next(a, h.at, a.c.kv_heads);
+            if (h.at.s != now.s) h.before += (int64_t)now.q.tiles * a.c.kv_heads;
+            h.pieces = pieces_at(a, h, per, 0, share);
+            if (lane == 0) s_segment = h;
+        }
+        // A slot's rows lie side by side: as many neighbouring lanes as it has groups of four rows (a power of two up to 8) read them together and
+        // add their weights up.  Four slots of each team at a time, so that their logits and pages are on the way together.
         constexpr int kAhead = 4;
+        const int team = pitch <= 4 ? 1 : pitch <= 8 ? 2 : pitch <= 16 ? 4 : 8, mate = tid & (team - 1), teams = kJoinThreads / team;
         const int64_t first_tile = before * a.row_blocks + (int64_t)now.item * a.row_blocks * now.q.tiles + now.idx;
-        for (int e0 = tid; e0 < n * kTile; e0 += kAhead * kJoinThreads) {
-            int page[kAhead], slot[kAhead];
+        for (int e0 = tid / team; e0 - tid / team < n * kTile; e0 += kAhead * teams) {           // (the same number of rounds for all)
+            Spot spot[kAhead];
             float w[kAhead];
 #pragma unroll
             for (int i = 0; i < kAhead; ++i) {
-                const int e = e0 + i * kJoinThreads;
-                slot[i] = e < n * kTile ? first_slot(now.q, now.idx + e / kTile) + e % kTile : 0x7fffffff;
-                page[i] = slot[i] < now.q.length ? cache_page(a.c, now.s, slot[i], bad) : -1;
+                const int e = e0 + i * teams;
+                const int slot = e < n * kTile ? first_slot(now.q, now.idx + e / kTile) + e % kTile : 0x7fffffff;
+                spot[i] = slot < now.q.length ? cache_spot(a.c, now.s, slot, bad) : Spot{-1, 0};
                 w[i] = 0.0f;
             }
             for (int b = 0; b < a.row_blocks; ++b) {
                 const float *const logit = a.logits + (first_tile + (int64_t)b * now.q.tiles) * kTile * pitch, *const lse = s_lse + b * block_rows;
                 if (pitch >= 4) {
-#pragma unroll 2
-                    for (int r = 0; r < pitch; r += 4) {
+                    for (int r = 4 * mate; r < pitch; r += 4 * team) {
                         float4 x[kAhead];
 #pragma unroll
                         for (int i = 0; i < kAhead; ++i)
-                            if (page[i] >= 0) x[i] = __ldcg((const float4 *)(logit + (int64_t)(e0 + i * kJoinThreads) * pitch + r));
+                            if (spot[i].page >= 0) x[i] = __ldcg((const float4 *)(logit + (int64_t)(e0 + i * teams) * pitch + r));
 #pragma unroll
                         for (int i = 0; i < kAhead; ++i)
-                            if (page[i] >= 0) w[i] += exp2_of(x[i].x - lse[r]) + exp2_of(x[i].y - lse[r + 1]) + exp2_of(x[i].z - lse[r + 2]) + exp2_of(x[i].w - lse[r + 3]);
+                            if (spot[i].page >= 0) w[i] += (exp2_of(x[i].x - lse[r]) + exp2_of(x[i].y - lse[r + 1])) + (exp2_of(x[i].z - lse[r + 2]) + exp2_of(x[i].w - lse[r + 3]));
                     }
                 } else {
 #pragma unroll
                     for (int i = 0; i < kAhead; ++i)
-                        if (page[i] >= 0) {
-                            const float *const x = logit + (int64_t)(e0 + i * kJoinThreads) * pitch;
+                        if (spot[i].page >= 0) {
+                            const float *const x = logit + (int64_t)(e0 + i * teams) * pitch;
                             w[i] += exp2_of(__ldcg(x) - lse[0]);
                             if (pitch == 2) w[i] += exp2_of(__ldcg(x + 1) - lse[1]);
                         }
                 }
             }
+            for (int o = team / 2; o > 0; o >>= 1)
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) w[i] += __shfl_xor_sync(0xffffffffu, w[i], o);
 #pragma unroll
             for (int i = 0; i < kAhead; ++i)
-                if (page[i] >= 0 && w[i] != 0.0f) atomicAdd(&a.c.scores[cache_cell(a.c, page[i], slot[i], now.item)], w[i]);
+                if (mate == 0 && spot[i].page >= 0 && w[i] != 0.0f) atomicAdd(&a.c.scores[cache_cell(a.c, spot[i], now.item)], w[i]);
         }
         u += n;
-        now.idx += n - 1;
-        const int was = now.s, tiles = now.q.tiles;
-        cursor_next(a, now, a.c.kv_heads);
-        if (now.s != was) before += (int64_t)tiles * a.c.kv_heads;
-        if (u < to)
-            of_now = pieces_of((int64_t)now.s * per + now.item * a.row_blocks, before * a.row_blocks + (int64_t)now.item * a.row_blocks * now.q.tiles, now.q.tiles, share);
+        __syncthreads();
     }
+    if (bad != 0) raise_status(a.c.status, bad);
 }
 
 // ---- host ----
@@ -752,20 +805,20 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
         if (room < 1) return cudaErrorInvalidDevice;
         if (dev < kMaxDevices) __atomic_store_n(&known[dev], room, __ATOMIC_RELEASE);
     }
-    const int min_tiles = 1;
-    int64_t grid = z.tiles < room ? z.tiles : room;
-    grid = grid < 1 ? 1 : grid > kMaxBlocks ? kMaxBlocks : grid;
+    int64_t held = z.tiles < room ? z.tiles : room;
+    held = held < 1 ? 1 : held > kMaxBlocks ? kMaxBlocks : held;
+    const int64_t grid = z.tiles >= kLong * held && kCuts * held <= kMaxBlocks ? kCuts * held : held;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = s;
-    if ((e = cudaLaunchKernelEx(&cfg, kernel, a, min_tiles)) != cudaSuccess) return e;
+    if ((e = cudaLaunchKernelEx(&cfg, kernel, a, (int)held)) != cudaSuccess) return e;
     // (the second kernel is brought in, and does its sums over the lengths, while the first still runs)
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
-    // (booking is all loads and additions here and there: three blocks an SM)
-    if (a.logits != nullptr) cfg.gridDim = dim3((unsigned)(z.tiles < 3 * 148 ? (z.tiles > grid ? z.tiles : grid) : grid > 3 * 148 ? grid : 3 * 148));
-    return cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, min_tiles, (int)grid, C::kDim, C::kRows);
+    const int64_t join = grid < 2 * 148 ? grid : 2 * 148;
+    cfg.gridDim = dim3((unsigned)join);
+    return cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, (int)grid, (int)held, C::kDim, C::kRows);
 }
 // Tiles in the ring: as many as let two blocks share an SM, or, for wide heads, fill it for one.
 constexpr int stages_of(int steps, int cols)

@@ -18,9 +18,9 @@ __device__ __forceinline__ unsigned worth_of(const EvictArgs &a, float score, in
 }
 __device__ __forceinline__ unsigned worth_at(const EvictArgs &a, int s, int head, int slot, int seen, ull &bad)
 {
-    const int page = cache_page(a.c, s, slot, bad);
-    if (page < 0) return 0u;
-    const int64_t cell = cache_cell(a.c, page, slot, head);
+    const Spot o = cache_spot(a.c, s, slot, bad);
+    if (o.page < 0) return 0u;
+    const int64_t cell = cache_cell(a.c, o, head);
     return worth_of(a, __ldg(&a.c.scores[cell]), a.c.positions != nullptr ? __ldg(&a.c.positions[cell]) : slot, seen);
 }
 
@@ -112,16 +112,16 @@ __global__ void __launch_bounds__(kMoveThreads) k_cache_evict(const EvictArgs a)
         const g10_cache_move m = a.moves[(int64_t)item * a.budget + r];
         // (a source before the budget, or a target behind it, could be another move's)
         if (m.source < a.budget || m.source >= length || m.target < 0 || m.target >= a.budget) { bad |= G10_DEV_BAD_MOVE; continue; }
-        const int from_page = cache_page(a.c, s, m.source, bad), to_page = cache_page(a.c, s, m.target, bad);
-        if (from_page < 0 || to_page < 0) continue;
-        const int64_t from = 2 * cache_row(a.c, from_page, m.source, head), to = 2 * cache_row(a.c, to_page, m.target, head);
+        const Spot source = cache_spot(a.c, s, m.source, bad), target = cache_spot(a.c, s, m.target, bad);
+        if (source.page < 0 || target.page < 0) continue;
+        const int64_t from = 16 * (int64_t)cache_row(a.c, source, head), to = 16 * (int64_t)cache_row(a.c, target, head);
         for (int i = lane; i < 2 * chunks; i += 32) {
             const char *const rows = i < chunks ? a.c.k : a.c.v;
             const int at = 16 * (i < chunks ? i : i - chunks);
             *(uint4 *)(const_cast<char *>(rows) + to + at) = *(const uint4 *)(rows + from + at);
         }
         if (lane == 0) {
-            const int64_t x = cache_cell(a.c, from_page, m.source, head), y = cache_cell(a.c, to_page, m.target, head);
+            const int64_t x = cache_cell(a.c, source, head), y = cache_cell(a.c, target, head);
             if (a.c.scores != nullptr) a.c.scores[y] = a.c.scores[x];
             if (a.c.positions != nullptr) a.c.positions[y] = a.c.positions[x];
         }
