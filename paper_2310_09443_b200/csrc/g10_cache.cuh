@@ -91,6 +91,9 @@ struct Pair<__half> {
     static __device__ __forceinline__ float2 unpack(unsigned u) { return __half22float2(*(const __half2 *)&u); }
 };
 
+// Rows of the logits that are kept for a slot: those of a block of rows, rounded up for wide accesses.
+__host__ __device__ __forceinline__ int logit_rows(int kept) { return kept <= 2 ? kept : (kept + 3) & ~3; }
+
 // ---- launchers ----
 struct AppendArgs {
     CacheView c;
@@ -106,6 +109,13 @@ struct AppendArgs {
 };
 cudaError_t launch_cache_append(const AppendArgs &a, int dtype, cudaStream_t s);
 
+// What the booking kernel has to know of a tile.
+struct __align__(16) TileNote {
+    int s, head, slot, length;           // sequence, key-value head, first slot, the sequence's slots
+    int tiles;                           // of the item: from one block of rows to the next (0: another block of rows books the tile)
+    int unused[3];
+};
+static_assert(sizeof(TileNote) == 32, "read 16 bytes at a time");
 struct AttendArgs {
     CacheView c;
     const char *q;
@@ -120,11 +130,14 @@ struct AttendArgs {
     float2 *ml;                          // [block rows][pieces] running maximum and sum of every piece
     float *part;                         // [pieces][block rows][padded head_dim] its sums, not divided yet
     float *logits;                       // [tiles][64][rows of a block] scaled by log2 e (null: weights are not booked)
+    float *sums;                         // [items][block rows] lse of every row, to base 2
+    TileNote *notes;                     // [tiles]
+    int64_t *total;                      // number of tiles
 };
 // Sizes that the workspace goes by.
 struct AttendShape {
-    int row_blocks, block_rows, padded_dim;
-    int64_t pieces, tiles;               // upper bounds for the sequences' capacity
+    int row_blocks, block_rows, logit_rows, padded_dim;
+    int64_t items, pieces, tiles;        // upper bounds for the sequences' capacity
 };
 AttendShape attend_shape(const CacheView &c, int rows, int new_tokens, int window, int sinks);
 cudaError_t launch_cache_attend(const AttendArgs &a, int dtype, cudaStream_t s);

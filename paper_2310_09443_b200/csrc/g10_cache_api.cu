@@ -49,7 +49,7 @@ int32_t view_of(const g10_cache *c, bool rows, CacheView &o)
 int32_t status_of(cudaError_t e) { return e == cudaSuccess ? G10_OK : G10_ERR_CUDA; }
 
 struct AttendLayout {
-    size_t ml, part, logits, bytes;
+    size_t ml, part, logits, sums, notes, total, bytes;
 };
 AttendLayout attend_layout(const AttendShape &z, bool scores)
 {
@@ -57,7 +57,10 @@ AttendLayout attend_layout(const AttendShape &z, bool scores)
     l.ml = 0;
     l.part = align_up(l.ml + sizeof(float2) * (size_t)z.pieces * z.block_rows);
     l.logits = align_up(l.part + sizeof(float) * (size_t)z.pieces * z.block_rows * z.padded_dim);
-    l.bytes = align_up(l.logits + (scores ? sizeof(float) * (size_t)z.tiles * z.block_rows * 64 : 0));
+    l.sums = align_up(l.logits + (scores ? sizeof(float) * (size_t)z.tiles * z.logit_rows * 64 : 0));
+    l.notes = align_up(l.sums + (scores ? sizeof(float) * (size_t)z.items * z.block_rows : 0));
+    l.total = align_up(l.notes + (scores ? sizeof(TileNote) * (size_t)z.tiles : 0));
+    l.bytes = align_up(l.total + sizeof(int64_t));
     return l;
 }
 
@@ -139,6 +142,7 @@ int32_t g10_cache_attend(const g10_cache *cache, const g10_cache_queries *u, voi
     a.row_blocks = z.row_blocks; a.pieces = z.pieces;
     a.ml = (float2 *)((char *)ws + l.ml); a.part = (float *)((char *)ws + l.part);
     a.logits = u->add_scores ? (float *)((char *)ws + l.logits) : nullptr;
+    a.sums = (float *)((char *)ws + l.sums); a.notes = (TileNote *)((char *)ws + l.notes); a.total = (int64_t *)((char *)ws + l.total);
     return status_of(launch_cache_attend(a, cache->dtype, (cudaStream_t)stream));
 }
 

@@ -197,9 +197,6 @@ __device__ __forceinline__ unsigned turned8x8(unsigned x)
     return y;
 }
 
-// Rows of the logits that the first kernel leaves for a slot: those of a block of rows, rounded up for wide accesses.
-__host__ __device__ __forceinline__ int logit_rows(int kept) { return kept <= 2 ? kept : (kept + 3) & ~3; }
-
 constexpr int kParts = 4;                // warps of a block; each takes 16 slots of a tile
 constexpr int kThreads = 32 * kParts;
 constexpr float kSlack = 8.0f;           // see below
@@ -245,6 +242,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
     const int64_t begin = begin_of(share, blockIdx.x);
     const int n = (int)(begin_of(share, blockIdx.x + 1) - begin);
     if (bad != 0) raise_status(a.c.status, bad);
+    if (a.logits != nullptr && blockIdx.x == 0 && tid == 0) *a.total = share.total;
     if (n == 0) return;
     bad = 0;
     place_of(a, tally, begin, per, &s_place);
@@ -287,13 +285,19 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
         }
     };
     unsigned next_row = kNone;                           // of the tile to be issued next
+    {
+        unsigned rows[kStages];                          // (all on the way together: each is a miss)
 #pragma unroll
-    for (int i = 0; i < kStages; ++i) {
-        if (i > 0) {
-            if (i - 1 < n) issue(i - 1, next_row);
+        for (int i = 0; i < kStages; ++i) {
+            rows[i] = kNone;
+            if (i < n) { rows[i] = look_up(); cursor_next(a, ahead, per); }
+        }
+#pragma unroll
+        for (int i = 0; i < kStages - 1; ++i) {
+            if (i < n) issue(i, rows[i]);
             asm volatile("cp.async.commit_group;" ::: "memory");
         }
-        if (i < n) { next_row = look_up(); cursor_next(a, ahead, per); }
+        next_row = rows[kStages - 1];
     }
 
     float acc[kSteps][kCols][4], m[kCols][2], l[kCols][2];
@@ -395,6 +399,11 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
                 if (!whole && !sees(a, p[j][e & 1], slot0 + (lane >> 2) + (e >> 1) * 8)) x[j][e] = -INFINITY;
             }
         if (a.logits != nullptr) {
+            if (tid < 3) {                               // the tile's note (of the other blocks of rows: that it is none)
+                int2 *const note = (int2 *)&a.notes[begin + u];
+                const int first = first_slot(now.q, now.idx);
+                note[tid] = tid == 0 ? make_int2(now.s, now.head) : tid == 1 ? make_int2(first, now.q.length) : make_int2(now.block == 0 ? now.q.tiles : 0, 0);
+            }
             float *const to = a.logits + (begin + u) * (int64_t)(logit_pitch * kTile) + (part * 16 + (lane >> 2)) * logit_pitch;
 #pragma unroll
             for (int j = 0; j < kCols; ++j) {
@@ -541,7 +550,11 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
                         uint2 w = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
                         if (sum == 0.0f) w = make_uint2(0, 0);
                         *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
-                        if (a.lse != nullptr && d == 0) a.lse[at] = sum == 0.0f ? -INFINITY : (top + log2f(sum)) * 0.69314718055994531f;
+                        if (d == 0) {
+                            const float lse = top + log2f(sum);
+                            if (a.lse != nullptr) a.lse[at] = sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
+                            if (a.logits != nullptr) a.sums[item * C::kRows + r] = sum == 0.0f ? INFINITY : lse;
+                        }
                     }
                 }
             }
@@ -609,179 +622,136 @@ __device__ __forceinline__ Pieces pieces_of(int64_t item, int64_t first, int til
     return Pieces{item, owner_of(first, r), owner_of(first + tiles - 1, r)};
 }
 
-// What a block of the second kernel has to do, worked out by one warp.
-struct Segment {                         // a run of slots of one (sequence, head)
-    Cursor at;
-    int64_t before;                      // tiles of the sequences before, one block of rows
-    Pieces pieces;                       // of its first block of rows
-};
-__device__ __forceinline__ Pieces pieces_at(const AttendArgs &a, const Segment &g, int per, int block, const Share &share)
-{
-    const int64_t i = (int64_t)g.at.item * a.row_blocks + block;
-    return pieces_of((int64_t)g.at.s * per + i, g.before * a.row_blocks + i * g.at.q.tiles, g.at.q.tiles, share);
-}
-
 // The second kernel.  (1) An item that was cut into pieces is joined by the blocks whose turn its pieces' shares are, each taking a part of its rows
-// and dimensions; (2) rows of sequences without tiles are written; (3) weights are booked, the slots of all (sequence, head) shared out
-// anew.  What follows from the lengths alone is worked out while the first kernel still runs, by one warp each.
+// and dimensions; (2) rows of sequences without tiles are written.  What follows from the lengths alone is worked out while the first
+// kernel still runs.
 template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a, int first_grid, int held_blocks, int padded_dim, int block_rows)
+__global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a, int held_blocks, int padded_dim, int block_rows)
 {
-    __shared__ float s_lse[1024];
-    __shared__ Place s_place[3];
+    __shared__ Place s_place[2];
     __shared__ Cursor s_cut[2];
     __shared__ Pieces s_pieces[2];
-    __shared__ Segment s_segment;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = a.c.kv_heads * a.row_blocks;
     ull ignored = 0;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const Tally tally = tally_of<kJoinThreads>(a, ignored);
-    const Share share = share_of(tally.total, per, first_grid, held_blocks);       // the first kernel's
-    Share slots;                                         // of (3)
-    slots.total = a.logits != nullptr ? tally.total * a.c.kv_heads : 0; slots.blocks = gridDim.x;
-    const int64_t from = begin_of(slots, blockIdx.x), to = begin_of(slots, blockIdx.x + 1);
-    if (from < to) place_of(a, tally, from, a.c.kv_heads, &s_place[2]);
-    bool waited = false;
-    // ---- (1): the items of a share's first and last tile (those between are whole) ----
-    for (int b = blockIdx.x; b < share.blocks; b += gridDim.x) {
-        const int64_t begin = begin_of(share, b), end = begin_of(share, b + 1);
-        place_of(a, tally, begin, per, &s_place[0]); place_of(a, tally, end - 1, per, &s_place[1]);
-        __syncthreads();
-        if (warp < 2) {
-            const int64_t tile = warp == 0 ? begin : end - 1;
-            Cursor u;
-            cursor_at(a, u, s_place[warp], tile);
-            const Pieces p = pieces_of((int64_t)u.s * per + u.item, tile - u.idx, u.q.tiles, share);
-            if (lane == 0) { s_cut[warp] = u; s_pieces[warp] = p; }
-        } else if (warp == 2 && !waited && from < to) {
-            Segment g;
-            cursor_at(a, g.at, s_place[2], from);
-            g.before = s_place[2].before;
-            g.pieces = pieces_at(a, g, per, 0, share);
-            if (lane == 0) s_segment = g;
-        }
-        if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
-        waited = true;
-        __syncthreads();
-#pragma unroll 1
-        for (int side = 0; side < 2; ++side) {
-            const Pieces w = s_pieces[side];
-            const int pieces = w.b1 - w.b0 + 1;
-            if (pieces == 1 || (side == 1 && w.item == s_pieces[0].item)) continue;
-            const int s = s_cut[side].s, head = s_cut[side].head, first_row = s_cut[side].block * block_rows, rows = min(block_rows, a.rows - first_row);
-            const int lanes = lanes_for(pieces), teams = kJoinThreads / lanes;
-            const int quads = a.c.head_dim / 4, all = rows * quads;
-            const int e0 = all * (b - w.b0) / pieces, e1 = all * (b - w.b0 + 1) / pieces;        // (64 rows at most: 32 bits)
-            for (int e = e0 + warp * 32 / lanes; e < e1; e += teams) {             // (whole warps: all lanes take part in the shuffles)
-                const int mine = min(e + lane / lanes, e1 - 1), r = mine / quads, d = mine % quads * 4, row = first_row + r;
-                const Part p = part_join<true>(a, w.item, w.b0, w.b1, block_rows, r, padded_dim, d, lanes);
-                if (e + lane / lanes < e1 && (lane & (lanes - 1)) == 0) {
-                    const int64_t at = ((int64_t)s * a.new_tokens + row / a.group) * a.q_heads + head * a.group + row % a.group;
-                    const float inv = 1.0f / p.sum;
-                    uint2 o = make_uint2(Pair<T>::pack(p.o.x * inv, p.o.y * inv), Pair<T>::pack(p.o.z * inv, p.o.w * inv));
-                    if (p.sum == 0.0f) o = make_uint2(0, 0);
-                    *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = o;
-                    if (a.lse != nullptr && d == 0) a.lse[at] = p.sum == 0.0f ? -INFINITY : (p.top + log2f(p.sum)) * 0.69314718055994531f;
+    const Share share = share_of(tally.total, per, gridDim.x, held_blocks);        // the first kernel's
+    const int b = blockIdx.x;
+    const int64_t begin = begin_of(share, b), end = begin_of(share, b + 1);
+    if (begin < end) { place_of(a, tally, begin, per, &s_place[0]); place_of(a, tally, end - 1, per, &s_place[1]); }
+    __syncthreads();
+    if (warp < 2 && begin < end) {
+        const int64_t tile = warp == 0 ? begin : end - 1;
+        Cursor u;
+        cursor_at(a, u, s_place[warp], tile);
+        const Pieces p = pieces_of((int64_t)u.s * per + u.item, tile - u.idx, u.q.tiles, share);
+        if (lane == 0) { s_cut[warp] = u; s_pieces[warp] = p; }
+    }
+    __syncthreads();
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+
+    // ---- (1): the items of the share's first and last tile (those between are whole), half of the warps each ----
+    constexpr int kHalf = kJoinThreads / 64;
+    const int side = warp / kHalf;
+    const Pieces w = s_pieces[side];
+    const int pieces = w.b1 - w.b0 + 1;
+    if (begin < end && pieces > 1 && !(side == 1 && w.item == s_pieces[0].item)) {
+        const int s = s_cut[side].s, head = s_cut[side].head, first_row = s_cut[side].block * block_rows, rows = min(block_rows, a.rows - first_row);
+        const int lanes = lanes_for(pieces), teams = 32 / lanes;
+        const int quads = a.c.head_dim / 4, all = rows * quads;
+        const int e0 = all * (b - w.b0) / pieces, e1 = all * (b - w.b0 + 1) / pieces;            // (32 rows at most: 32 bits)
+        for (int e = e0 + warp % kHalf * teams; e < e1; e += kHalf * teams) {                    // (all lanes take part in the shuffles)
+            const int mine = min(e + lane / lanes, e1 - 1), r = mine / quads, d = mine % quads * 4, row = first_row + r;
+            const Part p = part_join<true>(a, w.item, w.b0, w.b1, block_rows, r, padded_dim, d, lanes);
+            if (e + lane / lanes < e1 && (lane & (lanes - 1)) == 0) {
+                const int64_t at = ((int64_t)s * a.new_tokens + row / a.group) * a.q_heads + head * a.group + row % a.group;
+                const float inv = 1.0f / p.sum;
+                uint2 o = make_uint2(Pair<T>::pack(p.o.x * inv, p.o.y * inv), Pair<T>::pack(p.o.z * inv, p.o.w * inv));
+                if (p.sum == 0.0f) o = make_uint2(0, 0);
+                *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = o;
+                if (d == 0) {
+                    const float lse = p.top + log2f(p.sum);
+                    if (a.lse != nullptr) a.lse[at] = p.sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
+                    if (a.logits != nullptr) a.sums[w.item * block_rows + r] = p.sum == 0.0f ? INFINITY : lse;
                 }
             }
         }
-        __syncthreads();
     }
-    if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
     // ---- (2) ----
-    for (int s = blockIdx.x; s < a.c.num_seqs; s += gridDim.x) {
+    for (int s = b; s < a.c.num_seqs; s += gridDim.x) {
         if (seq_of(a, s, ignored).tiles > 0) continue;
         const int64_t rows = (int64_t)a.new_tokens * a.q_heads, n = rows * (a.c.head_dim / 8);
         for (int64_t i = tid; i < n; i += kJoinThreads) ((uint4 *)(a.out + 2 * s * rows * a.c.head_dim))[i] = make_uint4(0, 0, 0, 0);
         if (a.lse != nullptr)
             for (int64_t i = tid; i < rows; i += kJoinThreads) a.lse[s * rows + i] = -INFINITY;
     }
-    if (from >= to) return;
+}
 
-    // ---- (3) ----
-    const int pitch = logit_rows(min(block_rows, a.rows)), all_rows = a.row_blocks > 1 ? a.row_blocks * block_rows : pitch;
-    ull bad = 0;
-    if (!waited || blockIdx.x >= share.blocks) {         // (a block without a share of its own)
-        __syncthreads();
-        if (warp == 0) {
-            Segment g;
-            cursor_at(a, g.at, s_place[2], from);
-            g.before = s_place[2].before;
-            g.pieces = pieces_at(a, g, per, 0, share);
-            if (lane == 0) s_segment = g;
+// The third kernel books the weights: a warp per tile, from the note that the first kernel has left for it, so that there is nothing to search for.  A
+// slot's rows lie side by side: as many neighbouring lanes as it has groups of four rows read them and add their weights up; a lane has the same
+// rows of every slot, and so its part of the lse in registers.  exp2(logit - lse) over all rows in order, and one addition to the score.
+template <int kTeam>
+__device__ __forceinline__ void book_tile(const AttendArgs &a, const TileNote &note, int64_t tile, int block_rows, int pitch, ull &bad)
+{
+    const int lane = threadIdx.x & 31, mate = lane & (kTeam - 1);
+    const int per = a.c.kv_heads * a.row_blocks;
+    const int64_t item = (int64_t)note.s * per + note.head * a.row_blocks;
+    constexpr int kPasses = 2 * kTeam, kAhead = kPasses < 8 ? kPasses : 8;
+#pragma unroll 1
+    for (int pass = 0; pass < kPasses; pass += kAhead) {
+        Spot spot[kAhead];
+        float w[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            const int slot = note.slot + (pass + i) * (32 / kTeam) + lane / kTeam;
+            spot[i] = slot < note.length ? cache_spot(a.c, note.s, slot, bad) : Spot{-1, 0};
+            w[i] = 0.0f;
         }
-    }
-    __syncthreads();
-    for (int64_t u = from; u < to;) {
-        const Segment g = s_segment;
-        const Cursor &now = g.at;
-        const int64_t before = g.before;
-        const int n = (int)min((int64_t)(now.q.tiles - now.idx), to - u);          // tiles of this (sequence, head)
-        for (int r = a.rows + tid; r < all_rows; r += kJoinThreads) s_lse[r] = INFINITY;         // (no such row: weight 0)
         for (int b = 0; b < a.row_blocks; ++b) {
-            const Pieces w = b == 0 ? g.pieces : pieces_at(a, g, per, b, share);
-            const int lanes = lanes_for(w.b1 - w.b0 + 1), teams = kJoinThreads / lanes;
-            const int rows = min(block_rows, a.rows - b * block_rows);
-            for (int r0 = warp * 32 / lanes; r0 < rows; r0 += teams) {             // (warps without a row have nothing to do)
-                const int r = min(r0 + lane / lanes, rows - 1);
-                const Part p = part_join<false>(a, w.item, w.b0, w.b1, block_rows, r, 0, 0, lanes);
-                if ((lane & (lanes - 1)) == 0) s_lse[b * block_rows + r] = p.sum == 0.0f ? INFINITY : p.top + log2f(p.sum);
-            }
-        }
-        __syncthreads();
-        if (warp == kJoinThreads / 32 - 1 && u + n < to) {                         // the next one, meanwhile
-            Segment h = g;
-            h.at.idx += n - 1;
-            cursor_next(a, h.at, a.c.kv_heads);
-            if (h.at.s != now.s) h.before += (int64_t)now.q.tiles * a.c.kv_heads;
-            h.pieces = pieces_at(a, h, per, 0, share);
-            if (lane == 0) s_segment = h;
-        }
-        // A slot's rows lie side by side: as many neighbouring lanes as it has groups of four rows (a power of two up to 8) read them together and
-        // add their weights up.  Four slots of each team at a time, so that their logits and pages are on the way together.
-        constexpr int kAhead = 4;
-        const int team = pitch <= 4 ? 1 : pitch <= 8 ? 2 : pitch <= 16 ? 4 : 8, mate = tid & (team - 1), teams = kJoinThreads / team;
-        const int64_t first_tile = before * a.row_blocks + (int64_t)now.item * a.row_blocks * now.q.tiles + now.idx;
-        for (int e0 = tid / team; e0 - tid / team < n * kTile; e0 += kAhead * teams) {           // (the same number of rounds for all)
-            Spot spot[kAhead];
-            float w[kAhead];
+            const float *const from = a.logits + ((tile + (int64_t)b * note.tiles) * kTile + pass * (32 / kTeam) + lane / kTeam) * pitch;
+            const int r = 4 * mate, rows = a.rows - b * block_rows;
+            const float *const lse = a.sums + (item + b) * block_rows + r;
+            if (pitch >= 4) {
+                float4 z = make_float4(INFINITY, INFINITY, INFINITY, INFINITY), x[kAhead];       // (no such row: weight 0)
+                if (r < pitch) {
+                    z = __ldcg((const float4 *)lse);
+                    if (r + 1 >= rows) z.y = INFINITY;
+                    if (r + 2 >= rows) z.z = INFINITY;
+                    if (r + 3 >= rows) z.w = INFINITY;
+                    if (r >= rows) z.x = INFINITY;
+                }
 #pragma unroll
-            for (int i = 0; i < kAhead; ++i) {
-                const int e = e0 + i * teams;
-                const int slot = e < n * kTile ? first_slot(now.q, now.idx + e / kTile) + e % kTile : 0x7fffffff;
-                spot[i] = slot < now.q.length ? cache_spot(a.c, now.s, slot, bad) : Spot{-1, 0};
-                w[i] = 0.0f;
-            }
-            for (int b = 0; b < a.row_blocks; ++b) {
-                const float *const logit = a.logits + (first_tile + (int64_t)b * now.q.tiles) * kTile * pitch, *const lse = s_lse + b * block_rows;
-                if (pitch >= 4) {
-                    for (int r = 4 * mate; r < pitch; r += 4 * team) {
-                        float4 x[kAhead];
+                for (int i = 0; i < kAhead; ++i) x[i] = r < pitch ? __ldcg((const float4 *)(from + i * (32 / kTeam) * pitch + r)) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
 #pragma unroll
-                        for (int i = 0; i < kAhead; ++i)
-                            if (spot[i].page >= 0) x[i] = __ldcg((const float4 *)(logit + (int64_t)(e0 + i * teams) * pitch + r));
+                for (int i = 0; i < kAhead; ++i) w[i] += (exp2_of(x[i].x - z.x) + exp2_of(x[i].y - z.y)) + (exp2_of(x[i].z - z.z) + exp2_of(x[i].w - z.w));
+            } else {
+                for (int q = 0; q < pitch; ++q) {
+                    const float z = __ldcg(lse + q);
 #pragma unroll
-                        for (int i = 0; i < kAhead; ++i)
-                            if (spot[i].page >= 0) w[i] += (exp2_of(x[i].x - lse[r]) + exp2_of(x[i].y - lse[r + 1])) + (exp2_of(x[i].z - lse[r + 2]) + exp2_of(x[i].w - lse[r + 3]));
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < kAhead; ++i)
-                        if (spot[i].page >= 0) {
-                            const float *const x = logit + (int64_t)(e0 + i * teams) * pitch;
-                            w[i] += exp2_of(__ldcg(x) - lse[0]);
-                            if (pitch == 2) w[i] += exp2_of(__ldcg(x + 1) - lse[1]);
-                        }
+                    for (int i = 0; i < kAhead; ++i) w[i] += exp2_of(__ldcg(from + i * 32 * pitch + q) - z);
                 }
             }
-            for (int o = team / 2; o > 0; o >>= 1)
-#pragma unroll
-                for (int i = 0; i < kAhead; ++i) w[i] += __shfl_xor_sync(0xffffffffu, w[i], o);
-#pragma unroll
-            for (int i = 0; i < kAhead; ++i)
-                if (mate == 0 && spot[i].page >= 0 && w[i] != 0.0f) atomicAdd(&a.c.scores[cache_cell(a.c, spot[i], now.item)], w[i]);
         }
-        u += n;
-        __syncthreads();
+#pragma unroll
+        for (int o = kTeam / 2; o > 0; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) w[i] += __shfl_xor_sync(0xffffffffu, w[i], o);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (mate == 0 && spot[i].page >= 0 && w[i] != 0.0f) atomicAdd(&a.c.scores[cache_cell(a.c, spot[i], note.head)], w[i]);
+    }
+}
+template <int kTeam>
+__global__ void __launch_bounds__(kJoinThreads) k_cache_book(const AttendArgs a, int block_rows)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int pitch = logit_rows(min(block_rows, a.rows));
+    const int64_t total = __ldcg(a.total);
+    ull bad = 0;
+    for (int64_t u = (int64_t)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5); u < total; u += (int64_t)gridDim.x * (kJoinThreads / 32)) {
+        const int4 x = __ldcg((const int4 *)&a.notes[u]);
+        const TileNote note{x.x, x.y, x.z, x.w, __ldcg(&a.notes[u].tiles), {0, 0, 0}};
+        if (note.tiles > 0) book_tile<kTeam>(a, note, u, block_rows, pitch, bad);
     }
     if (bad != 0) raise_status(a.c.status, bad);
 }
@@ -816,9 +786,12 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
-    const int64_t join = grid < 2 * 148 ? grid : 2 * 148;
-    cfg.gridDim = dim3((unsigned)join);
-    return cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, (int)grid, (int)held, C::kDim, C::kRows);
+    if ((e = cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, (int)held, C::kDim, C::kRows)) != cudaSuccess || a.logits == nullptr) return e;
+    const int64_t warps = kJoinThreads / 32, blocks = (z.tiles + warps - 1) / warps, most = 148 * 6;
+    cfg.gridDim = dim3((unsigned)(blocks < most ? blocks : most));
+    const int pitch = logit_rows(C::kRows < a.rows ? C::kRows : a.rows);
+    const auto book = pitch <= 4 ? k_cache_book<1> : pitch <= 8 ? k_cache_book<2> : pitch <= 16 ? k_cache_book<4> : k_cache_book<8>;
+    return cudaLaunchKernelEx(&cfg, book, a, C::kRows);
 }
 // Tiles in the ring: as many as let two blocks share an SM, or, for wide heads, fill it for one.
 constexpr int stages_of(int steps, int cols)

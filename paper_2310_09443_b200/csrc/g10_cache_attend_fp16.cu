@@ -18,7 +18,9 @@ AttendShape attend_shape(const CacheView &c, int rows, int new_tokens, int windo
         const int64_t seen = ((int64_t)sinks + attend::kTile - 1) / attend::kTile + ((int64_t)window + new_tokens + attend::kTile - 2) / attend::kTile + 1;
         tiles = seen < tiles ? seen : tiles;
     }
+    z.logit_rows = logit_rows(rows < z.block_rows ? rows : z.block_rows);
     const int64_t items = (int64_t)c.num_seqs * c.kv_heads * z.row_blocks;
+    z.items = items;
     z.tiles = items * tiles;
     z.pieces = items + attend::kMaxBlocks;
     return z;
