@@ -181,9 +181,16 @@ __device__ __forceinline__ void cursor_next(const AttendArgs &a, Cursor &u, int 
 
 __device__ __forceinline__ bool sees(const AttendArgs &a, int p, int slot) { return slot <= p && (a.window == 0 || slot < a.sinks || slot > p - a.window); }
 
-__device__ __forceinline__ void copy16(unsigned dst, const void *src)
+// (keys and values leave the L2 cache first: they are read once, and what is left there for the kernels behind is not)
+__device__ __forceinline__ uint64_t leaves_first()
 {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ void copy16(unsigned dst, const void *src, uint64_t policy)
+{
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
 }
 __device__ __forceinline__ void copy16_or_zeros(unsigned dst, const void *src, bool there)
 {
@@ -260,6 +267,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
         const Spot o = cache_spot(a.c, ahead.s, slot, bad);
         return o.page < 0 ? kNone : cache_row(a.c, o, ahead.head);
     };
+    const uint64_t policy = leaves_first();
     auto issue = [&](int stage, unsigned row_at) {
         constexpr int kChunks = 2 * kSteps;              // of 16 bytes in a row
         const unsigned to = ring + stage * C::kPartBytes;
@@ -269,8 +277,8 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
             for (int i = 0; i < 16 * kChunks / 32; ++i) {
                 const int c = i * 32 + lane, row = c / kChunks, chunk = c % kChunks;
                 const int64_t at = 16 * (int64_t)__shfl_sync(0xffffffffu, row_at, row);
-                copy16(to + row * C::kPitch + chunk * 16, a.c.k + 16 * chunk + at);
-                copy16(to + (16 + row) * C::kPitch + chunk * 16, a.c.v + 16 * chunk + at);
+                copy16(to + row * C::kPitch + chunk * 16, a.c.k + 16 * chunk + at, policy);
+                copy16(to + (16 + row) * C::kPitch + chunk * 16, a.c.v + 16 * chunk + at, policy);
             }
         } else {
 #pragma unroll 1
