@@ -7,76 +7,93 @@ namespace {
 constexpr int kAppendThreads = 128;
 
 // A row (one head of one token) is held by kLanes threads, 8 elements each.  Rows of a token: its query heads, its key heads, its
-// value heads.  Everything is read once and written once; the 8 values stay in registers between norm, rotation and rounding, and only
-// the partners of half-split pairs go through shared memory.
-template <typename T, int kLanes>
-__global__ void __launch_bounds__(kAppendThreads) k_cache_append(const AppendArgs a, int rows_each)
+// value heads; a team of kLanes threads takes kEach of them, every kTeams-th, and asks for all before it looks at the first.  Everything is read once and
+// written once; the 8 values stay in registers between norm, rotation and rounding, and only the partners of half-split pairs go
+// through shared memory.  The rotation's 8 cosines and sines are the same for all rows of a team: loaded once, 16 bytes at a time (kWide:
+// tables and rotary_dim allow it).  Bound by traffic for prompts, by the trip to memory for single tokens.
+template <typename T, int kLanes, int kEach, bool kWide>
+__global__ void __launch_bounds__(kAppendThreads) k_cache_append(const AppendArgs a, int shares)
 {
-    constexpr int kGroups = kAppendThreads / kLanes;
-    __shared__ float s_x[kAppendThreads * 8];
+    constexpr int kTeams = kAppendThreads / kLanes;
+    __shared__ __align__(16) float s_x[kAppendThreads * 8];
     const CacheView &c = a.c;
-    const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+    const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
     const int rows = a.q_heads + 2 * c.kv_heads;
-    const int shares = (rows + kGroups * rows_each - 1) / (kGroups * rows_each);
-    const int64_t item = blockIdx.x;
-    const int share = (int)(item % shares);
-    const int64_t token = item / shares;
-    const int s = (int)(token / a.new_tokens), t = (int)(token % a.new_tokens);
+    const unsigned token = blockIdx.x / (unsigned)shares;
+    const int share = (int)(blockIdx.x - token * (unsigned)shares);
+    const int s = (int)(token / (unsigned)a.new_tokens), t = (int)(token - (unsigned)s * (unsigned)a.new_tokens);
+    const int d0 = lane * 8, half = a.rotary / 2;
+    const bool mine = d0 < c.head_dim;
     ull bad = 0;
     const int length = cache_length(c, s, bad), count = cache_count(a.counts, s, a.new_tokens, length, bad);
     const bool counts = t < count;
-    const int slot = length - count + t;
+    if (!counts && share * kTeams * kEach >= a.q_heads) {          // (padding: only queries have something to write)
+        if (bad != 0 && threadIdx.x == 0) raise_status(c.status, bad);
+        return;
+    }
+    // the rows: all on the way
+    uint4 u[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int row = (share * kEach + i) * kTeams + team;
+        u[i] = make_uint4(0, 0, 0, 0);
+        const char *from = nullptr;
+        if (row < a.q_heads) from = a.q + 2 * (s * a.q_seq + t * a.q_token + row * a.q_head);
+        else if (row < a.q_heads + c.kv_heads) from = a.k + 2 * (s * a.k_seq + t * a.k_token + (row - a.q_heads) * a.k_head);
+        else if (row < rows) from = a.v + 2 * (s * a.v_seq + t * a.v_token + (row - a.q_heads - c.kv_heads) * a.v_head);
+        if (from != nullptr && counts && mine) u[i] = __ldg((const uint4 *)(from + 2 * d0));
+    }
     Spot spot{-1, 0};
     int64_t position = 0;
     if (counts) {
-        spot = cache_spot(c, s, slot, bad);
+        spot = cache_spot(c, s, length - count + t, bad);
         position = (int64_t)__ldg(&c.seen[s]) - count + t;
     }
-    const int d0 = lane * 8, half = a.rotary / 2;
-    const bool mine = d0 < c.head_dim;
-    // the rotation of this thread's 8 dimensions: the same for every head of the token
     float co[8], si[8];
     const bool turns = counts && a.rotary > 0 && position >= 0 && position < a.table_rows;
     if (counts && a.rotary > 0 && !turns) bad |= G10_DEV_BAD_POSITION;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        const int d = d0 + e;
-        co[e] = 1.0f; si[e] = 0.0f;
-        if (turns && d < a.rotary) {
-            const int64_t at = position * half + (a.interleaved ? d >> 1 : (d < half ? d : d - half));
-            co[e] = __ldg(&a.cos_table[at]); si[e] = __ldg(&a.sin_table[at]);
+    for (int e = 0; e < 8; ++e) { co[e] = 1.0f; si[e] = 0.0f; }
+    if (turns && d0 < a.rotary) {
+        const float *const cos_row = a.cos_table + position * half, *const sin_row = a.sin_table + position * half;
+        if (kWide) {
+            if (a.interleaved) {
+                const float4 x = __ldg((const float4 *)(cos_row + d0 / 2)), y = __ldg((const float4 *)(sin_row + d0 / 2));
+                co[0] = co[1] = x.x; co[2] = co[3] = x.y; co[4] = co[5] = x.z; co[6] = co[7] = x.w;
+                si[0] = si[1] = y.x; si[2] = si[3] = y.y; si[4] = si[5] = y.z; si[6] = si[7] = y.w;
+            } else {
+                const int j = d0 < half ? d0 : d0 - half;
+                *(float4 *)&co[0] = __ldg((const float4 *)(cos_row + j)); *(float4 *)&co[4] = __ldg((const float4 *)(cos_row + j + 4));
+                *(float4 *)&si[0] = __ldg((const float4 *)(sin_row + j)); *(float4 *)&si[4] = __ldg((const float4 *)(sin_row + j + 4));
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int d = d0 + e, j = a.interleaved ? d >> 1 : (d < half ? d : d - half);
+                if (d < a.rotary) { co[e] = __ldg(&cos_row[j]); si[e] = __ldg(&sin_row[j]); }
+            }
         }
     }
-    float *mate = s_x + group * kLanes * 8;
-    for (int i = 0; i < rows_each; ++i) {
-        const int row = (share * rows_each + i) * kGroups + group;
+    float *const mate = s_x + team * kLanes * 8;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+        const int row = (share * kEach + i) * kTeams + team;
         const bool is_q = row < a.q_heads, is_k = !is_q && row < a.q_heads + c.kv_heads, is_v = !is_q && !is_k && row < rows;
         const int head = is_q ? row : is_k ? row - a.q_heads : row - a.q_heads - c.kv_heads;
-        const char *from = nullptr;
-        char *to = nullptr;
-        if (is_q) {
-            from = a.q + 2 * (s * a.q_seq + t * a.q_token + head * a.q_head);
-            to = a.q_out + 2 * ((token * a.q_heads + head) * c.head_dim);
-        } else if (is_k || is_v) {
-            from = is_k ? a.k + 2 * (s * a.k_seq + t * a.k_token + head * a.k_head) : a.v + 2 * (s * a.v_seq + t * a.v_token + head * a.v_head);
-            if (spot.page >= 0) to = const_cast<char *>(is_k ? c.k : c.v) + 16 * (int64_t)cache_row(c, spot, head);
-        }
-        uint4 u = make_uint4(0, 0, 0, 0);
-        if (counts && from != nullptr && mine) u = *(const uint4 *)(from + 2 * d0);
-        if (__syncthreads_or(is_q || is_k)) {                  // (some row of the block has arithmetic to do)
+        unsigned *w = &u[i].x;
+        if (__any_sync(0xffffffffu, is_q || is_k)) {           // (some row of the warp has arithmetic to do)
             float x[8];
-            unsigned *w = &u.x;
 #pragma unroll
             for (int e = 0; e < 4; ++e) { const float2 p = Pair<T>::unpack(w[e]); x[2 * e] = p.x; x[2 * e + 1] = p.y; }
+            const char *weight = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
             float sum = 0.0f;
 #pragma unroll
             for (int e = 0; e < 8; ++e) sum = fmaf(x[e], x[e], sum);
 #pragma unroll
             for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-            const char *weight = is_q ? a.q_weight : is_k ? a.k_weight : nullptr;
             if (weight != nullptr) {
                 const float r = rsqrtf(sum / (float)c.head_dim + a.eps);
-                const uint4 g = mine ? *(const uint4 *)(weight + 2 * d0) : make_uint4(0, 0, 0, 0);
+                const uint4 g = mine ? __ldg((const uint4 *)(weight + 2 * d0)) : make_uint4(0, 0, 0, 0);
                 const unsigned *gw = &g.x;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -88,18 +105,26 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache_append(const AppendArg
                 float y[8];
                 if (a.interleaved) {
 #pragma unroll
-                    for (int e = 0; e < 8; e += 2) { y[e] = x[e] * co[e] - x[e + 1] * si[e]; y[e + 1] = x[e + 1] * co[e + 1] + x[e] * si[e + 1]; }
+                    for (int e = 0; e < 8; e += 2) {
+                        const bool turn = d0 + e < a.rotary;
+                        y[e] = turn ? x[e] * co[e] - x[e + 1] * si[e] : x[e]; y[e + 1] = turn ? x[e + 1] * co[e + 1] + x[e] * si[e + 1] : x[e + 1];
+                    }
                 } else {
                     __syncwarp();
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) mate[d0 + e] = x[e];
+                    *(float4 *)&mate[d0] = make_float4(x[0], x[1], x[2], x[3]); *(float4 *)&mate[d0 + 4] = make_float4(x[4], x[5], x[6], x[7]);
                     __syncwarp();
+                    float other[8];
+                    if (kWide) {
+                        const int at = d0 >= a.rotary ? d0 : d0 < half ? d0 + half : d0 - half;
+                        *(float4 *)&other[0] = *(const float4 *)&mate[at]; *(float4 *)&other[4] = *(const float4 *)&mate[at + 4];
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) { const int d = d0 + e; other[e] = d >= a.rotary ? 0.0f : mate[d < half ? d + half : d - half]; }
+                    }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const int d = d0 + e;
-                        const bool low = d < half;
-                        const float other = d < a.rotary ? mate[low ? d + half : d - half] : 0.0f;
-                        y[e] = low ? x[e] * co[e] - other * si[e] : x[e] * co[e] + other * si[e];
+                        y[e] = d >= a.rotary ? x[e] : d < half ? x[e] * co[e] - other[e] * si[e] : x[e] * co[e] + other[e] * si[e];
                     }
                 }
 #pragma unroll
@@ -110,31 +135,44 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache_append(const AppendArg
                 for (int e = 0; e < 4; ++e) w[e] = Pair<T>::pack(x[2 * e], x[2 * e + 1]);
             }
         }
-        if (to != nullptr && mine) {
-            if (!counts) u = make_uint4(0, 0, 0, 0);           // (a padding token's query: zero)
-            if (counts || is_q) *(uint4 *)(to + 2 * d0) = u;
+        if (is_q && mine) {
+            if (!counts) u[i] = make_uint4(0, 0, 0, 0);        // (a padding token's query: zero)
+            *(uint4 *)(a.q_out + 2 * (((int64_t)token * a.q_heads + head) * c.head_dim + d0)) = u[i];
         }
-        if (is_k && spot.page >= 0 && counts && lane == 0) {
-            const int64_t cell = cache_cell(c, spot, head);
-            if (c.scores != nullptr) c.scores[cell] = 0.0f;
-            if (c.positions != nullptr) c.positions[cell] = (int32_t)position;
+        if ((is_k || is_v) && spot.page >= 0) {
+            if (mine) *(uint4 *)(const_cast<char *>(is_k ? c.k : c.v) + 16 * (int64_t)cache_row(c, spot, head) + 2 * d0) = u[i];
+            if (is_k && lane == 0) {
+                const int64_t cell = cache_cell(c, spot, head);
+                if (c.scores != nullptr) c.scores[cell] = 0.0f;
+                if (c.positions != nullptr) c.positions[cell] = (int32_t)position;
+            }
         }
     }
     if (bad != 0 && threadIdx.x == 0) raise_status(c.status, bad);
 }
 
-template <typename T, int kLanes>
-cudaError_t launch(const AppendArgs &a, cudaStream_t s)
+template <typename T, int kLanes, int kEach>
+cudaError_t launch(const AppendArgs &a, int64_t tokens, int shares, cudaStream_t s)
 {
-    constexpr int kGroups = kAppendThreads / kLanes;
+    if (tokens * shares > 0x7fffffff) return cudaErrorInvalidValue;
+    const int half = a.rotary / 2;
+    const bool wide = (((uintptr_t)a.cos_table | (uintptr_t)a.sin_table) & 15u) == 0 && half % (a.interleaved ? 4 : 8) == 0;
+    if (wide) k_cache_append<T, kLanes, kEach, true><<<(unsigned)(tokens * shares), kAppendThreads, 0, s>>>(a, shares);
+    else k_cache_append<T, kLanes, kEach, false><<<(unsigned)(tokens * shares), kAppendThreads, 0, s>>>(a, shares);
+    count_launch();
+    return cudaGetLastError();
+}
+template <typename T, int kLanes>
+cudaError_t launch_lanes(const AppendArgs &a, cudaStream_t s)
+{
+    constexpr int kTeams = kAppendThreads / kLanes;
     const int rows = a.q_heads + 2 * a.c.kv_heads;
     const int64_t tokens = (int64_t)a.c.num_seqs * a.new_tokens;
-    int each = 1;
-    while (each < 8 && kGroups * each < rows && tokens * ((rows + 2 * kGroups * each - 1) / (2 * kGroups * each)) >= 148 * 16) each *= 2;
-    const int64_t blocks = tokens * ((rows + kGroups * each - 1) / (kGroups * each));
-    if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    k_cache_append<T, kLanes><<<(unsigned)blocks, kAppendThreads, 0, s>>>(a, each); count_launch();
-    return cudaGetLastError();
+    auto shares = [&](int each) { return (rows + kTeams * each - 1) / (kTeams * each); };
+    // (several rows a thread once there are blocks enough for all SMs all the same: fewer look-ups and rotations for each)
+    if (tokens * shares(4) >= 148 * 16 && rows > 2 * kTeams) return launch<T, kLanes, 4>(a, tokens, shares(4), s);
+    if (tokens * shares(2) >= 148 * 16 && rows > kTeams) return launch<T, kLanes, 2>(a, tokens, shares(2), s);
+    return launch<T, kLanes, 1>(a, tokens, shares(1), s);
 }
 
 }  // namespace
@@ -142,8 +180,8 @@ cudaError_t launch(const AppendArgs &a, cudaStream_t s)
 cudaError_t launch_cache_append(const AppendArgs &a, int dtype, cudaStream_t s)
 {
     const int lanes = (a.c.head_dim + 7) / 8;
-    if (dtype == G10_BF16) return lanes <= 8 ? launch<__nv_bfloat16, 8>(a, s) : lanes <= 16 ? launch<__nv_bfloat16, 16>(a, s) : launch<__nv_bfloat16, 32>(a, s);
-    return lanes <= 8 ? launch<__half, 8>(a, s) : lanes <= 16 ? launch<__half, 16>(a, s) : launch<__half, 32>(a, s);
+    if (dtype == G10_BF16) return lanes <= 8 ? launch_lanes<__nv_bfloat16, 8>(a, s) : lanes <= 16 ? launch_lanes<__nv_bfloat16, 16>(a, s) : launch_lanes<__nv_bfloat16, 32>(a, s);
+    return lanes <= 8 ? launch_lanes<__half, 8>(a, s) : lanes <= 16 ? launch_lanes<__half, 16>(a, s) : launch_lanes<__half, 32>(a, s);
 }
 
 }  // namespace g10
