@@ -102,7 +102,7 @@ struct AppendArgs {
     char *q_out;
     const int32_t *counts;
     const char *q_weight, *k_weight;
-    float eps;
+    float eps, inv_dim;                  // (1 / head_dim)
     const float *cos_table, *sin_table;
     int64_t table_rows;
     int new_tokens, q_heads, rotary, interleaved;

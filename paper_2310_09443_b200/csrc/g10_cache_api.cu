@@ -30,7 +30,7 @@ int32_t view_of(const g10_cache *c, bool rows, CacheView &o)
         if (c->page_stride < 0 || c->slot_stride < 0 || c->head_stride < 0) return G10_ERR_ARG;
         // (rows are found by numbers of 32 bits, in units of 16 bytes)
         const __int128 last = (__int128)(c->num_pages - 1) * c->page_stride + (__int128)(c->page_size - 1) * c->slot_stride + (__int128)(c->kv_heads - 1) * c->head_stride;
-        if (last / 8 >= 0xffffffffll) return G10_ERR_LIMIT;
+        if (last / 8 + 32 >= 0xffffffffll) return G10_ERR_LIMIT;
     }
     o.k = (const char *)c->k; o.v = (const char *)c->v;
     o.page_stride = c->page_stride / 8; o.slot_stride = c->slot_stride / 8; o.head_stride = c->head_stride / 8;
@@ -100,7 +100,7 @@ int32_t g10_cache_append(const g10_cache *cache, const g10_cache_tokens *t, void
     a.k_seq = t->k_seq_stride; a.k_token = t->k_token_stride; a.k_head = t->k_head_stride;
     a.v_seq = t->v_seq_stride; a.v_token = t->v_token_stride; a.v_head = t->v_head_stride;
     a.q_out = (char *)t->q_out; a.counts = t->counts;
-    a.q_weight = (const char *)t->q_weight; a.k_weight = (const char *)t->k_weight; a.eps = t->eps;
+    a.q_weight = (const char *)t->q_weight; a.k_weight = (const char *)t->k_weight; a.eps = t->eps; a.inv_dim = 1.0f / (float)a.c.head_dim;
     a.cos_table = t->cos_table; a.sin_table = t->sin_table; a.table_rows = t->table_rows;
     a.new_tokens = t->new_tokens; a.q_heads = t->q_heads; a.rotary = t->rotary_dim; a.interleaved = t->interleaved != 0;
     return status_of(launch_cache_append(a, cache->dtype, (cudaStream_t)stream));

@@ -4,9 +4,9 @@
 namespace g10 {
 namespace {
 
-constexpr int kPlanThreads = 512;
+constexpr int kPlanThreads = 1024;
 constexpr int kPlanWarps = kPlanThreads / 32;
-constexpr int kPlanCluster = 8;          // blocks that share one (sequence, head), at most
+constexpr int kPlanCluster = 8;          // blocks that share one (sequence, head), at most (16 find room for few at a time: 35 -> 55 us for 16 of 65 537 slots)
 constexpr int kMoveThreads = 256;
 constexpr int kMoves = 8;                // a warp takes at a time
 
@@ -42,6 +42,14 @@ __device__ __forceinline__ unsigned read_of(const unsigned *p, unsigned rank)
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
     return v;
 }
+
+// Sum of the words of the warps before this one (all of them, if `all`).
+__device__ __forceinline__ int sum_before(const unsigned *s_warp, bool all)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    return (int)__reduce_add_sync(0xffffffffu, all || lane < warp ? s_warp[lane] : 0u);
+}
+static_assert(kPlanWarps == 32, "a lane for each warp's word");
 
 // One cluster of blocks per (sequence, head); each has a run of the slots, and their numbers in shared memory (kKept; a run that is too long for it is
 // read again for every pass).  The budget-th largest number is found in three digits, from the top: counts over the slots that agree with what is known
@@ -112,7 +120,7 @@ __global__ void __launch_bounds__(kPlanThreads) k_cache_plan(const EvictArgs a, 
         for (int o = 1; o < 32; o <<= 1) { const unsigned v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
         if (lane == 31) s_warp[warp] = upto;
         __syncthreads();
-        for (int w = 0; w < warp; ++w) upto += s_warp[w];
+        upto += (unsigned)sum_before(s_warp, false);
         unsigned above = upto - mine;
         if (above < left && left <= upto) {
             int i = 0;
@@ -134,15 +142,12 @@ __global__ void __launch_bounds__(kPlanThreads) k_cache_plan(const EvictArgs a, 
     }
     if (lane == 0) s_warp[warp] = (unsigned)equals;
     __syncthreads();
-    int rank_before = 0;                                 // slots with the number before the warp's
-    {
-        int all = 0;
-        for (int w = 0; w < kPlanWarps; ++w) { const int v = (int)s_warp[w]; if (w < warp) rank_before += v; all += v; }
-        if (blocks > 1) {
-            if (tid == 0) s_mine[0] = (unsigned)all;
-            cluster_sync();
-            for (int r = 0; r < rank; ++r) rank_before += (int)read_of(&s_mine[0], (unsigned)r);
-        }
+    int rank_before = sum_before(s_warp, false);         // slots with the number before the warp's
+    if (blocks > 1) {
+        const int all = sum_before(s_warp, true);
+        if (tid == 0) s_mine[0] = (unsigned)all;
+        cluster_sync();
+        rank_before += (int)__reduce_add_sync(0xffffffffu, lane < rank ? read_of(&s_mine[0], (unsigned)lane) : 0u);
     }
     __syncthreads();
     auto each_slot = [&](auto &&visit) {                 // visit(slot, kept, votes) for the warp's slots, in order
@@ -164,22 +169,15 @@ __global__ void __launch_bounds__(kPlanThreads) k_cache_plan(const EvictArgs a, 
     });
     if (lane == 0) { s_warp[warp] = (unsigned)movers; s_warp2[warp] = (unsigned)holes; }
     __syncthreads();
-    int at_mover = 0, at_hole = 0, all_movers = 0, all_holes = 0;
-    for (int w = 0; w < kPlanWarps; ++w) {
-        const int x = (int)s_warp[w], y = (int)s_warp2[w];
-        if (w < warp) { at_mover += x; at_hole += y; }
-        all_movers += x; all_holes += y;
-    }
+    int at_mover = sum_before(s_warp, false), at_hole = sum_before(s_warp2, false), all_movers = sum_before(s_warp, true);
     if (blocks > 1) {
+        const int all_holes = sum_before(s_warp2, true);
         if (tid == 0) { s_mine[1] = (unsigned)all_movers; s_mine[2] = (unsigned)all_holes; }
         cluster_sync();
-        int total = 0;
-        for (int r = 0; r < blocks; ++r) {
-            const int x = (int)read_of(&s_mine[1], (unsigned)r);
-            if (r < rank) { at_mover += x; at_hole += (int)read_of(&s_mine[2], (unsigned)r); }
-            total += x;
-        }
-        all_movers = total;
+        const unsigned x = lane < blocks ? read_of(&s_mine[1], (unsigned)lane) : 0u, y = lane < rank ? read_of(&s_mine[2], (unsigned)lane) : 0u;
+        at_mover += (int)__reduce_add_sync(0xffffffffu, lane < rank ? x : 0u);
+        at_hole += (int)__reduce_add_sync(0xffffffffu, y);
+        all_movers = (int)__reduce_add_sync(0xffffffffu, x);
         cluster_sync();                                  // (nobody leaves while its memory may still be read)
     }
     g10_cache_move *const moves = a.moves + (int64_t)item * a.budget;
@@ -195,8 +193,8 @@ __global__ void __launch_bounds__(kPlanThreads) k_cache_plan(const EvictArgs a, 
 }
 
 // A warp takes kMoves moves at a time: a lane each looks source and target up and moves score and position, then the rows go, 16 bytes a lane, all
-// loads of up to 256 units under way before the first is stored.  Pure traffic: 4 * head_dim bytes read and written per move.
-__global__ void __launch_bounds__(kMoveThreads) k_cache_evict(const EvictArgs a, unsigned unit_mul)
+// 128 units under way before the first is stored.  Pure traffic: 4 * head_dim bytes read and written per move.
+__global__ void __launch_bounds__(kMoveThreads, 5) k_cache_evict(const EvictArgs a, unsigned unit_mul)
 {
     const int item = blockIdx.y, s = item / a.c.kv_heads, head = item % a.c.kv_heads;
     const int lane = threadIdx.x & 31;
@@ -222,23 +220,26 @@ __global__ void __launch_bounds__(kMoveThreads) k_cache_evict(const EvictArgs a,
             if (a.c.scores != nullptr) a.c.scores[to_cell] = a.c.scores[cell];
             if (a.c.positions != nullptr) a.c.positions[to_cell] = a.c.positions[cell];
         }
-        for (int u0 = 0; u0 < kMoves * units; u0 += 8 * 32) {
-            uint4 x[8];
-            char *to[8];
+        constexpr int kAhead = 4;
+#pragma unroll 1
+        for (int u0 = 0; u0 < kMoves * units; u0 += kAhead * 32) {
+            uint4 x[kAhead];
+            unsigned to[kAhead];                         // 16-byte units
+            bool key[kAhead];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < kAhead; ++i) {
                 const int u = u0 + i * 32 + lane, move = min((int)(((unsigned)u * unit_mul) >> 20), kMoves - 1), unit = u - move * units;
                 const unsigned source = __shfl_sync(0xffffffffu, row, move), target = __shfl_sync(0xffffffffu, row, kMoves + move);
-                to[i] = nullptr;
+                key[i] = unit < half;
+                const unsigned at = (unsigned)(key[i] ? unit : unit - half);
+                to[i] = 0xffffffffu;
                 if (u < kMoves * units && source != 0xffffffffu && target != 0xffffffffu) {
-                    const char *const rows = unit < half ? a.c.k : a.c.v;
-                    const int at = 16 * (unit < half ? unit : unit - half);
-                    x[i] = *(const uint4 *)(rows + 16 * (int64_t)source + at);
-                    to[i] = const_cast<char *>(rows) + 16 * (int64_t)target + at;
+                    x[i] = *(const uint4 *)((key[i] ? a.c.k : a.c.v) + 16 * ((int64_t)source + at));
+                    to[i] = target + at;
                 }
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) if (to[i] != nullptr) *(uint4 *)to[i] = x[i];
+            for (int i = 0; i < kAhead; ++i) if (to[i] != 0xffffffffu) *(uint4 *)(const_cast<char *>(key[i] ? a.c.k : a.c.v) + 16 * (int64_t)to[i]) = x[i];
         }
     }
     if (bad != 0) raise_status(a.c.status, bad);
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(kMoveThreads) k_cache_evict(const EvictArgs a,
 cudaError_t launch_cache_plan(const EvictArgs &a, cudaStream_t s)
 {
     const int64_t items = (int64_t)a.c.num_seqs * a.c.kv_heads;
-    // Blocks for one (sequence, head): one does for 2048 slots (each thread four), more as long as all find room on the device at once.
+    // Blocks for one (sequence, head): one does for 2048 slots (each thread two), more as long as all find room on the device at once.
     static int known[kMaxDevices], room[kMaxDevices];
     const void *const kernels[] = {(const void *)k_cache_plan<true>};
     const int most_bytes = dynamic_smem_room(kernels[0], room);
