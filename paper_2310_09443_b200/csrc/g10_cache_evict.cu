@@ -4,8 +4,6 @@
 namespace g10 {
 namespace {
 
-constexpr int kPlanThreads = 1024;
-constexpr int kPlanWarps = kPlanThreads / 32;
 constexpr int kPlanCluster = 8;          // blocks that share one (sequence, head), at most (16 find room for few at a time: 35 -> 55 us for 16 of 65 537 slots)
 constexpr int kMoveThreads = 256;
 constexpr int kMoves = 8;                // a warp takes at a time
@@ -43,84 +41,96 @@ __device__ __forceinline__ unsigned read_of(const unsigned *p, unsigned rank)
     return v;
 }
 
-// Sum of the words of the warps before this one (all of them, if `all`).
-__device__ __forceinline__ int sum_before(const unsigned *s_warp, bool all)
+__device__ __forceinline__ void add_to(unsigned *p, unsigned rank, unsigned v)
 {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    return (int)__reduce_add_sync(0xffffffffu, all || lane < warp ? s_warp[lane] : 0u);
+    unsigned at;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((unsigned)__cvta_generic_to_shared(p)), "r"(rank));
+    asm volatile("red.shared::cluster.add.u32 [%0], %1;" ::"r"(at), "r"(v) : "memory");
 }
-static_assert(kPlanWarps == 32, "a lane for each warp's word");
+
+// Of a run of slots: with the number that decides before and behind the budget, with a larger one before and behind it, slots before it.
+struct Census {
+    int even_before, even_behind, over_before, over_behind, before;
+};
+// What becomes of it when `rank` slots with the number come before the run and the first `left` of all are kept: the run's own are kept in order.
+__device__ __forceinline__ void settle(const Census &c, int rank, int left, int &movers, int &holes)
+{
+    const int kept = min(max(left - rank, 0), c.even_before + c.even_behind), kept_before = min(kept, c.even_before);
+    movers = c.over_behind + kept - kept_before;
+    holes = c.before - c.over_before - kept_before;
+}
 
 // One cluster of blocks per (sequence, head); each has a run of the slots, and their numbers in shared memory (kKept; a run that is too long for it is
 // read again for every pass).  The budget-th largest number is found in three digits, from the top: counts over the slots that agree with what is known
-// so far, added up over the cluster, and the digit at which they reach the budget.  The first digit has 11 bits, sign, exponent and two
-// more: with 8, nearly all scores of a head share a handful of counters.  Then every slot is known to be kept or not, and
-// movers and holes are numbered by counting: within a warp by votes, over warps and blocks by prefix sums.
-template <bool kKept>
-__global__ void __launch_bounds__(kPlanThreads) k_cache_plan(const EvictArgs a, int blocks)
+// so far, and the digit at which they reach the budget.  A block adds its counts that are not zero to those of all blocks of the cluster, so that one
+// meeting a digit does.  The first digit has 11 bits, sign, exponent and two more: with 8, nearly all scores of a head share a handful of
+// counters.  Then every slot is known to be kept or not; movers and holes are numbered from a census of each warp's slots (votes) and
+// prefix sums over warps and blocks.  A chain of short steps, bound by their meetings, not by the 8 bytes read per slot.
+template <bool kKept, int kThreads>
+__global__ void __launch_bounds__(kThreads) k_cache_plan(const EvictArgs a, int blocks)
 {
-    constexpr int kDigits = 2048;
-    __shared__ unsigned s_count[kDigits], s_sum[kDigits], s_warp[kPlanWarps], s_warp2[kPlanWarps], s_found[2], s_mine[3];
+    constexpr int kDigits = 2048, kWarps = kThreads / 32;
+    __shared__ unsigned s_count[kDigits], s_sum[3][kDigits], s_warp[kWarps], s_found[2];
+    __shared__ Census s_census[kWarps];
+    __shared__ int s_mine[5];
     extern __shared__ unsigned s_worth[];
     const int rank = (int)cluster_rank(), item = blockIdx.x / blocks, s = item / a.c.kv_heads, head = item % a.c.kv_heads;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     ull bad = 0;
     const int length = cache_length(a.c, s, bad);
+    const int seen = __ldg(&a.c.seen[s]);
     if (head == 0 && rank == 0 && tid == 0 && a.new_lengths != nullptr) a.new_lengths[s] = min(length, a.budget);
     if (length <= a.budget) {                            // (the whole cluster alike)
         if (rank == 0 && tid == 0) a.counts[item] = 0;
         if (bad != 0) raise_status(a.c.status, bad);
         return;
     }
-    const int seen = __ldg(&a.c.seen[s]);
     const int each = (length + blocks - 1) / blocks, from = min(length, rank * each), n = min(length, from + each) - from;
     auto worth = [&](int i) -> unsigned { return kKept ? s_worth[i] : worth_at(a, s, head, from + i, seen, bad); };
+    if (blocks > 1)
+        for (int i = tid; i < 3 * kDigits; i += kThreads) s_sum[0][i] = 0;
     if (kKept) {
-        for (int i0 = tid; i0 < n; i0 += 4 * kPlanThreads) {
-            unsigned w[4];
+        constexpr int kAhead = 8;
+        for (int i0 = tid; i0 < n; i0 += kAhead * kThreads) {
+            unsigned w[kAhead];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) w[q] = i0 + q * kPlanThreads < n ? worth_at(a, s, head, from + i0 + q * kPlanThreads, seen, bad) : 0u;
+            for (int q = 0; q < kAhead; ++q) w[q] = i0 + q * kThreads < n ? worth_at(a, s, head, from + i0 + q * kThreads, seen, bad) : 0u;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) if (i0 + q * kPlanThreads < n) s_worth[i0 + q * kPlanThreads] = w[q];
+            for (int q = 0; q < kAhead; ++q) if (i0 + q * kThreads < n) s_worth[i0 + q * kThreads] = w[q];
         }
     }
+    if (blocks > 1) cluster_sync();                      // (all have begun, and cleared their sums)
     unsigned known = 0, left = (unsigned)a.budget;       // the number's upper digits; how many of those that agree are kept
-#pragma unroll 1
+#pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, digits = 1 << bits;
-        for (int i = tid; i < digits; i += kPlanThreads) s_count[i] = 0;
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, digits = 1 << bits, few = digits / kThreads > 0 ? digits / kThreads : 1;
+        for (int i = tid; i < digits; i += kThreads) s_count[i] = 0;
         __syncthreads();
-        for (int i = tid; i < n; i += kPlanThreads) {
+        for (int i = tid; i < n; i += kThreads) {
             const unsigned w = worth(i);
             if (pass == 0 || w >> (shift + bits) == known >> (shift + bits)) atomicAdd(&s_count[(w >> shift) & (digits - 1)], 1u);
         }
-        // the cluster's counts: each block adds a part of the digits up, then all read all parts
-        const unsigned *counts = s_count;
         __syncthreads();
+        const unsigned *counts = s_count;
         if (blocks > 1) {
-            cluster_sync();
-            const int part = digits / blocks;
-            for (int i = tid; i < part; i += kPlanThreads) {
-                unsigned sum = 0;
-                for (int r = 0; r < blocks; ++r) sum += read_of(&s_count[rank * part + i], (unsigned)r);
-                s_sum[rank * part + i] = sum;
+            for (int i = tid; i < digits; i += kThreads) {
+                const unsigned v = s_count[i];
+                if (v != 0) for (int r = 0; r < blocks; ++r) add_to(&s_sum[pass][i], (unsigned)r, v);
             }
             cluster_sync();
-            for (int i = tid; i < digits; i += kPlanThreads)
-                if (i / part != rank) s_sum[i] = read_of(&s_sum[i], (unsigned)(i / part));
-            counts = s_sum;
-            __syncthreads();
+            counts = s_sum[pass];
         }
         // from the largest digit down: a few neighbours a thread
-        const int few = digits / kPlanThreads, top = digits - 1 - tid * few;
+        const int top = digits - 1 - tid * few;
         unsigned mine = 0;
+#pragma unroll
         for (int i = 0; i < few; ++i) mine += counts[top - i];
         unsigned upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const unsigned v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
         if (lane == 31) s_warp[warp] = upto;
         __syncthreads();
-        upto += (unsigned)sum_before(s_warp, false);
+        upto += __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[lane] : 0u);
         unsigned above = upto - mine;
         if (above < left && left <= upto) {
             int i = 0;
@@ -132,64 +142,71 @@ __global__ void __launch_bounds__(kPlanThreads) k_cache_plan(const EvictArgs a, 
     }
 
     // ---- who is kept: more than the number, and the first `left` of those that have it ----
-    const int run = (n + kPlanWarps - 1) / kPlanWarps, w0 = min(n, warp * run), w1 = min(n, w0 + run);      // the warp's slots
+    const int run = ((n + kWarps - 1) / kWarps + 31) & ~31, w0 = min(n, warp * run), w1 = min(n, w0 + run);        // the warp's slots
     const unsigned below = (1u << lane) - 1u;
-    int equals = 0;                                      // with the number, in the warp's run
+    Census c{0, 0, 0, 0, min(max(a.budget - from - w0, 0), w1 - w0)};
     for (int i0 = w0; i0 < w1; i0 += 32) {
         const int i = i0 + lane;
-        const unsigned w = i < w1 ? worth(i) : 0u;
-        equals += __popc(__ballot_sync(0xffffffffu, i < w1 && w == known));
+        const unsigned w = i < w1 ? worth(i) : 0u, front = __ballot_sync(0xffffffffu, from + i < a.budget);
+        const unsigned even = __ballot_sync(0xffffffffu, i < w1 && w == known), over = __ballot_sync(0xffffffffu, i < w1 && w > known);
+        c.even_before += __popc(even & front); c.even_behind += __popc(even & ~front);
+        c.over_before += __popc(over & front); c.over_behind += __popc(over & ~front);
     }
-    if (lane == 0) s_warp[warp] = (unsigned)equals;
+    if (lane == 0) s_census[warp] = c;
     __syncthreads();
-    int rank_before = sum_before(s_warp, false);         // slots with the number before the warp's
+    // (lane i looks after warp i, in every warp)
+    const Census of = lane < kWarps ? s_census[lane] : Census{0, 0, 0, 0, 0};
+    const int evens = of.even_before + of.even_behind;
+    int evens_upto = evens;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, evens_upto, o); if (lane >= o) evens_upto += v; }
+    int evens_before = 0, at_mover = 0, at_hole = 0, all_movers = 0;               // of the blocks before this one, and of all
     if (blocks > 1) {
-        const int all = sum_before(s_warp, true);
-        if (tid == 0) s_mine[0] = (unsigned)all;
-        cluster_sync();
-        rank_before += (int)__reduce_add_sync(0xffffffffu, lane < rank ? read_of(&s_mine[0], (unsigned)lane) : 0u);
-    }
-    __syncthreads();
-    auto each_slot = [&](auto &&visit) {                 // visit(slot, kept, votes) for the warp's slots, in order
-        int r = rank_before;
-        for (int i0 = w0; i0 < w1; i0 += 32) {
-            const int i = i0 + lane;
-            const unsigned w = i < w1 ? worth(i) : 0u;
-            const bool equal = i < w1 && w == known;
-            const unsigned votes = __ballot_sync(0xffffffffu, equal);
-            const bool kept = i < w1 && (w > known || (equal && r + __popc(votes & below) < (int)left));
-            r += __popc(votes);
-            visit(from + i, i < w1, kept);
+        const int sums[5] = {(int)__reduce_add_sync(0xffffffffu, of.even_before), (int)__reduce_add_sync(0xffffffffu, of.even_behind),
+                             (int)__reduce_add_sync(0xffffffffu, of.over_before), (int)__reduce_add_sync(0xffffffffu, of.over_behind),
+                             (int)__reduce_add_sync(0xffffffffu, of.before)};
+        if (tid == 0) {
+#pragma unroll
+            for (int q = 0; q < 5; ++q) s_mine[q] = sums[q];
         }
-    };
-    int movers = 0, holes = 0;
-    each_slot([&](int slot, bool real, bool kept) {
-        movers += __popc(__ballot_sync(0xffffffffu, kept && slot >= a.budget));
-        holes += __popc(__ballot_sync(0xffffffffu, real && !kept && slot < a.budget));
-    });
-    if (lane == 0) { s_warp[warp] = (unsigned)movers; s_warp2[warp] = (unsigned)holes; }
-    __syncthreads();
-    int at_mover = sum_before(s_warp, false), at_hole = sum_before(s_warp2, false), all_movers = sum_before(s_warp, true);
-    if (blocks > 1) {
-        const int all_holes = sum_before(s_warp2, true);
-        if (tid == 0) { s_mine[1] = (unsigned)all_movers; s_mine[2] = (unsigned)all_holes; }
         cluster_sync();
-        const unsigned x = lane < blocks ? read_of(&s_mine[1], (unsigned)lane) : 0u, y = lane < rank ? read_of(&s_mine[2], (unsigned)lane) : 0u;
-        at_mover += (int)__reduce_add_sync(0xffffffffu, lane < rank ? x : 0u);
-        at_hole += (int)__reduce_add_sync(0xffffffffu, y);
-        all_movers = (int)__reduce_add_sync(0xffffffffu, x);
-        cluster_sync();                                  // (nobody leaves while its memory may still be read)
+        Census x{0, 0, 0, 0, 0};
+        if (lane < blocks) {
+            x.even_before = (int)read_of((const unsigned *)&s_mine[0], (unsigned)lane); x.even_behind = (int)read_of((const unsigned *)&s_mine[1], (unsigned)lane);
+            x.over_before = (int)read_of((const unsigned *)&s_mine[2], (unsigned)lane); x.over_behind = (int)read_of((const unsigned *)&s_mine[3], (unsigned)lane);
+            x.before = (int)read_of((const unsigned *)&s_mine[4], (unsigned)lane);
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // (read: who waits for it, at the end, may leave)
+        int upto = x.even_before + x.even_behind, movers, holes;
+        const int own = upto;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) { const int v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
+        settle(x, upto - own, (int)left, movers, holes);
+        evens_before = (int)__reduce_add_sync(0xffffffffu, lane < rank ? own : 0);
+        at_mover = (int)__reduce_add_sync(0xffffffffu, lane < rank ? movers : 0);
+        at_hole = (int)__reduce_add_sync(0xffffffffu, lane < rank ? holes : 0);
+        all_movers = (int)__reduce_add_sync(0xffffffffu, movers);
     }
+    int movers, holes;
+    settle(of, evens_before + evens_upto - evens, (int)left, movers, holes);
+    at_mover += (int)__reduce_add_sync(0xffffffffu, lane < warp ? movers : 0);
+    at_hole += (int)__reduce_add_sync(0xffffffffu, lane < warp ? holes : 0);
+    if (blocks == 1) all_movers = (int)__reduce_add_sync(0xffffffffu, movers);
+    int even_rank = evens_before + (int)__reduce_add_sync(0xffffffffu, lane < warp ? evens : 0);
     g10_cache_move *const moves = a.moves + (int64_t)item * a.budget;
-    each_slot([&](int slot, bool real, bool kept) {
-        const bool mover = kept && slot >= a.budget, hole = real && !kept && slot < a.budget;
-        const unsigned mv = __ballot_sync(0xffffffffu, mover), ho = __ballot_sync(0xffffffffu, hole);
-        if (mover) moves[at_mover + __popc(mv & below)].source = slot;
-        if (hole) moves[at_hole + __popc(ho & below)].target = slot;
-        at_mover += __popc(mv); at_hole += __popc(ho);
-    });
+    for (int i0 = w0; i0 < w1; i0 += 32) {
+        const int i = i0 + lane, slot = from + i;
+        const unsigned w = i < w1 ? worth(i) : 0u, even = __ballot_sync(0xffffffffu, i < w1 && w == known);
+        const bool kept = i < w1 && (w > known || (w == known && even_rank + __popc(even & below) < (int)left));
+        const unsigned mv = __ballot_sync(0xffffffffu, kept && slot >= a.budget), ho = __ballot_sync(0xffffffffu, i < w1 && !kept && slot < a.budget);
+        // (in bounds whatever happens to the scores meanwhile)
+        if ((mv >> lane & 1u) && at_mover + __popc(mv & below) < a.budget) moves[at_mover + __popc(mv & below)].source = slot;
+        if ((ho >> lane & 1u) && at_hole + __popc(ho & below) < a.budget) moves[at_hole + __popc(ho & below)].target = slot;
+        even_rank += __popc(even); at_mover += __popc(mv); at_hole += __popc(ho);
+    }
     if (rank == 0 && tid == 0) a.counts[item] = all_movers;
     if (bad != 0) raise_status(a.c.status, bad);
+    if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 
 // A warp takes kMoves moves at a time: a lane each looks source and target up and moves score and position, then the rows go, 16 bytes a lane, all
@@ -250,26 +267,28 @@ __global__ void __launch_bounds__(kMoveThreads, 5) k_cache_evict(const EvictArgs
 cudaError_t launch_cache_plan(const EvictArgs &a, cudaStream_t s)
 {
     const int64_t items = (int64_t)a.c.num_seqs * a.c.kv_heads;
-    // Blocks for one (sequence, head): one does for 2048 slots (each thread two), more as long as all find room on the device at once.
+    // Blocks for one (sequence, head): one does for 2048 slots, more as long as all find room on the device at once.
     static int known[kMaxDevices], room[kMaxDevices];
-    const void *const kernels[] = {(const void *)k_cache_plan<true>};
+    const void *const kernels[] = {(const void *)k_cache_plan<true, 1024>};
     const int most_bytes = dynamic_smem_room(kernels[0], room);
     if (most_bytes <= 0) return cudaErrorInvalidDevice;
-    int most = largest_cluster(kernels, false, kPlanThreads, (size_t)most_bytes, known), blocks = 1;
+    int most = largest_cluster(kernels, false, 1024, (size_t)most_bytes, known), blocks = 1;
     most = most > kPlanCluster ? kPlanCluster : most;
     while (2 * blocks <= most && a.c.capacity > 2048 * blocks && items * 2 * blocks <= 2 * 148) blocks *= 2;
-    // (numbers that shared memory cannot take are worked out anew in each pass: some 50 000 slots a block)
+    // (numbers that shared memory cannot take are worked out anew in each pass: some 48 000 slots a block)
     while (2 * blocks <= most && ((int64_t)a.c.capacity + blocks - 1) / blocks * 4 > most_bytes) blocks *= 2;
-    const int64_t bytes = ((int64_t)a.c.capacity + blocks - 1) / blocks * 4;
+    const int64_t slots = ((int64_t)a.c.capacity + blocks - 1) / blocks, bytes = slots * 4;
     const bool kept = bytes <= most_bytes;
-    const auto kernel = kept ? k_cache_plan<true> : k_cache_plan<false>;
-    cudaError_t e = kept ? allow_launch((const void *)kernel, (size_t)most_bytes, blocks) : allow_launch((const void *)kernel, 0, blocks);
+    // (few threads meet sooner)
+    const bool small = slots <= 4096;
+    const auto kernel = !kept ? k_cache_plan<false, 1024> : small ? k_cache_plan<true, 256> : k_cache_plan<true, 1024>;
+    cudaError_t e = allow_launch((const void *)kernel, kept ? (size_t)most_bytes : 0, blocks);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = (unsigned)blocks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(items * blocks)); cfg.blockDim = dim3(kPlanThreads); cfg.dynamicSmemBytes = kept ? (size_t)bytes : 0; cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)(items * blocks)); cfg.blockDim = dim3(small ? 256u : 1024u); cfg.dynamicSmemBytes = kept ? (size_t)bytes : 0; cfg.stream = s;
     cfg.attrs = at; cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, a, blocks);
 }
