@@ -90,13 +90,31 @@ __global__ void __launch_bounds__(kThreads) k_cache_plan(const EvictArgs a, int 
     if (blocks > 1)
         for (int i = tid; i < 3 * kDigits; i += kThreads) s_sum[0][i] = 0;
     if (kKept) {
-        constexpr int kAhead = 8;
+        // (no branch between the loads of a round: all pages are on the way together, then all scores)
+        constexpr int kAhead = kThreads >= 512 ? 8 : 12;
+        const int32_t *const table = a.c.table + (int64_t)s * a.c.table_stride;
+        const bool any = a.c.num_pages > 0;
         for (int i0 = tid; i0 < n; i0 += kAhead * kThreads) {
-            unsigned w[kAhead];
+            Spot o[kAhead];
+            float score[kAhead];
+            int position[kAhead];
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) w[q] = i0 + q * kThreads < n ? worth_at(a, s, head, from + i0 + q * kThreads, seen, bad) : 0u;
+            for (int q = 0; q < kAhead; ++q) {
+                const int slot = from + min(i0 + q * kThreads, n - 1), at = (int)(((ull)(unsigned)slot * a.c.page_mul) >> a.c.page_shift);
+                o[q].page = __ldg(&table[at]); o[q].place = slot - at * a.c.page_size;
+                position[q] = slot;
+            }
 #pragma unroll
-            for (int q = 0; q < kAhead; ++q) if (i0 + q * kThreads < n) s_worth[i0 + q * kThreads] = w[q];
+            for (int q = 0; q < kAhead; ++q) {
+                const bool there = o[q].page >= 0 && o[q].page < (int)a.c.num_pages;
+                const int64_t cell = there ? cache_cell(a.c, o[q], head) : 0;
+                score[q] = any ? __ldg(&a.c.scores[cell]) : 0.0f;
+                if (a.c.positions != nullptr && any) position[q] = __ldg(&a.c.positions[cell]);
+                if (!there) { bad |= G10_DEV_BAD_PAGE; o[q].page = -1; }
+            }
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+                if (i0 + q * kThreads < n) s_worth[i0 + q * kThreads] = o[q].page < 0 ? 0u : worth_of(a, score[q], position[q], seen);
         }
     }
     if (blocks > 1) cluster_sync();                      // (all have begun, and cleared their sums)
@@ -269,10 +287,10 @@ cudaError_t launch_cache_plan(const EvictArgs &a, cudaStream_t s)
     const int64_t items = (int64_t)a.c.num_seqs * a.c.kv_heads;
     // Blocks for one (sequence, head): one does for 2048 slots, more as long as all find room on the device at once.
     static int known[kMaxDevices], room[kMaxDevices];
-    const void *const kernels[] = {(const void *)k_cache_plan<true, 1024>};
+    const void *const kernels[] = {(const void *)k_cache_plan<true, 512>};
     const int most_bytes = dynamic_smem_room(kernels[0], room);
     if (most_bytes <= 0) return cudaErrorInvalidDevice;
-    int most = largest_cluster(kernels, false, 1024, (size_t)most_bytes, known), blocks = 1;
+    int most = largest_cluster(kernels, false, 512, (size_t)most_bytes, known), blocks = 1;
     most = most > kPlanCluster ? kPlanCluster : most;
     while (2 * blocks <= most && a.c.capacity > 2048 * blocks && items * 2 * blocks <= 2 * 148) blocks *= 2;
     // (numbers that shared memory cannot take are worked out anew in each pass: some 48 000 slots a block)
@@ -281,14 +299,14 @@ cudaError_t launch_cache_plan(const EvictArgs &a, cudaStream_t s)
     const bool kept = bytes <= most_bytes;
     // (few threads meet sooner)
     const bool small = slots <= 4096;
-    const auto kernel = !kept ? k_cache_plan<false, 1024> : small ? k_cache_plan<true, 256> : k_cache_plan<true, 1024>;
+    const auto kernel = !kept ? k_cache_plan<false, 512> : small ? k_cache_plan<true, 256> : k_cache_plan<true, 512>;
     cudaError_t e = allow_launch((const void *)kernel, kept ? (size_t)most_bytes : 0, blocks);
     if (e != cudaSuccess) return e;
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = (unsigned)blocks; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)(items * blocks)); cfg.blockDim = dim3(small ? 256u : 1024u); cfg.dynamicSmemBytes = kept ? (size_t)bytes : 0; cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)(items * blocks)); cfg.blockDim = dim3(kept && small ? 256u : 512u); cfg.dynamicSmemBytes = kept ? (size_t)bytes : 0; cfg.stream = s;
     cfg.attrs = at; cfg.numAttrs = 1;
     return cudaLaunchKernelEx(&cfg, kernel, a, blocks);
 }
