@@ -9,11 +9,13 @@ constexpr int kAppendThreads = 128;
 // A row (one head of one token) is held by kLanes threads, 8 elements each.  Rows of a token: its query heads, its key heads, its
 // value heads; a team of kLanes threads takes kEach of them, every kTeams-th, and asks for all before it looks at the first.  Everything is read once and
 // written once; the 8 values stay in registers between norm, rotation and rounding, and only the partners of half-split pairs go
-// through shared memory.  The rotation's 8 cosines and sines are the same for all rows of a team: loaded once, 16 bytes at a time (kWide:
-// tables and rotary_dim allow it).  A block takes `run` tokens of a sequence, one after the other: what is the same for all of them (addresses,
+// through shared memory.  The rotation's 8 cosines and sines are the same for all rows of a team: loaded once, 16 bytes at a time where the
+// tables and rotary_dim allow it.  A block takes `run` tokens of a sequence, one after the other: what is the same for all of them (addresses,
 // lengths, weights) is worked out once, since for prompts the instructions, not the traffic, are what takes the time.
-template <typename T, int kLanes, int kEach, bool kWide>
-__global__ void __launch_bounds__(kAppendThreads) k_cache_append(const AppendArgs a, int shares, int runs, int run)
+enum { kNone, kSplit, kPairs, kAny };    // rotation: none, half-split or interleaved pairs in whole 16-byte units, whatever else
+
+template <typename T, int kLanes, int kEach, int kTurn>
+__global__ void __launch_bounds__(kAppendThreads, 6) k_cache_append(const AppendArgs a, int shares, int runs, int run)
 {
     constexpr int kTeams = kAppendThreads / kLanes;
     __shared__ __align__(16) float s_x[kAppendThreads * 8];
@@ -25,87 +27,79 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache_append(const AppendArg
     const int s = (int)(place / (unsigned)runs), t0 = (int)(place - (unsigned)s * (unsigned)runs) * run;
     const int d0 = lane * 8, half = a.rotary / 2;
     const bool mine = d0 < c.head_dim;
-    // the thread's rows: where they come from, token t0
+    const bool turned = kTurn != kNone && d0 < a.rotary;
+    // the thread's rows: where they come from and go to, token 0 of the sequence and slot 0 of page 0
     const char *from[kEach];
+    char *to[kEach];
     uint4 u[kEach];
+    const int64_t q_from = 2 * (s * a.q_seq + d0), k_from = 2 * (s * a.k_seq + d0), v_from = 2 * (s * a.v_seq + d0);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
         const int row = (share * kEach + i) * kTeams + team;
-        from[i] = nullptr;
-        if (row < a.q_heads) from[i] = a.q + 2 * (s * a.q_seq + t0 * a.q_token + row * a.q_head + d0);
-        else if (row < a.q_heads + c.kv_heads) from[i] = a.k + 2 * (s * a.k_seq + t0 * a.k_token + (row - a.q_heads) * a.k_head + d0);
-        else if (row < rows) from[i] = a.v + 2 * (s * a.v_seq + t0 * a.v_token + (row - a.q_heads - c.kv_heads) * a.v_head + d0);
-        if (!mine) from[i] = nullptr;
+        from[i] = nullptr; to[i] = nullptr;
+        u[i] = make_uint4(0, 0, 0, 0);
+        if (!mine || row >= rows) continue;
+        const bool is_q = row < a.q_heads, is_k = row < a.q_heads + c.kv_heads;
+        const int head = is_q ? row : is_k ? row - a.q_heads : row - a.q_heads - c.kv_heads;
+        from[i] = is_q ? a.q + q_from + 2 * head * a.q_head : is_k ? a.k + k_from + 2 * head * a.k_head : a.v + v_from + 2 * head * a.v_head;
+        to[i] = is_q ? a.q_out + 2 * (((int64_t)s * a.new_tokens * a.q_heads + head) * c.head_dim + d0)
+                     : const_cast<char *>(is_k ? c.k : c.v) + 16 * head * c.head_stride + 2 * d0;
         // (those of padding too: what they hold is not used)
-        u[i] = from[i] != nullptr ? __ldg((const uint4 *)from[i]) : make_uint4(0, 0, 0, 0);
+        u[i] = __ldg((const uint4 *)(from[i] + 2 * t0 * (is_q ? a.q_token : is_k ? a.k_token : a.v_token)));
     }
     ull bad = 0;
     const int seen = __ldg(&c.seen[s]);
     const int length = cache_length(c, s, bad), count = cache_count(a.counts, s, a.new_tokens, length, bad);
-    float qw[8], kw[8];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const char *const weight = h == 0 ? a.q_weight : a.k_weight;
-        float *const to = h == 0 ? qw : kw;
-        if (weight != nullptr && mine) {
-            const uint4 g = __ldg((const uint4 *)(weight + 2 * d0));
-            const unsigned gw[4] = {g.x, g.y, g.z, g.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) { const float2 p = Pair<T>::unpack(gw[e]); to[2 * e] = p.x; to[2 * e + 1] = p.y; }
-        } else {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) to[e] = 1.0f;
-        }
-    }
+    const uint4 qw = a.q_weight != nullptr && mine ? __ldg((const uint4 *)(a.q_weight + 2 * d0)) : make_uint4(0, 0, 0, 0);
+    const uint4 kw = a.k_weight != nullptr && mine ? __ldg((const uint4 *)(a.k_weight + 2 * d0)) : make_uint4(0, 0, 0, 0);
     float *const mate = s_x + team * kLanes * 8;
     const int t1 = min(a.new_tokens, t0 + run);
 #pragma unroll 1
     for (int t = t0; t < min(t1, count); ++t) {
         const int64_t position = (int64_t)seen - count + t;
         const Spot spot = cache_spot(c, s, length - count + t, bad);
+        const bool turns = turned && position >= 0 && position < a.table_rows;
+        if (kTurn != kNone && (position < 0 || position >= a.table_rows)) bad |= G10_DEV_BAD_POSITION;
         if (t > t0) {
 #pragma unroll
-            for (int i = 0; i < kEach; ++i)
-                if (from[i] != nullptr) {
-                    const int row = (share * kEach + i) * kTeams + team;
-                    from[i] += 2 * (row < a.q_heads ? a.q_token : row < a.q_heads + c.kv_heads ? a.k_token : a.v_token);
-                    u[i] = __ldg((const uint4 *)from[i]);
-                }
+            for (int i = 0; i < kEach; ++i) {
+                const int row = (share * kEach + i) * kTeams + team;
+                if (from[i] != nullptr) u[i] = __ldg((const uint4 *)(from[i] + 2 * t * (row < a.q_heads ? a.q_token : row < a.q_heads + c.kv_heads ? a.k_token : a.v_token)));
+            }
         }
-        float co[8], si[8];
-        const bool turns = a.rotary > 0 && position >= 0 && position < a.table_rows;
-        if (a.rotary > 0 && !turns) bad |= G10_DEV_BAD_POSITION;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) { co[e] = 1.0f; si[e] = 0.0f; }
-        if (turns && d0 < a.rotary) {
+        float co[8], si[8];                              // (the first of a pair takes its partner with a minus)
+        if (turns) {
             const float *const cos_row = a.cos_table + position * half, *const sin_row = a.sin_table + position * half;
-            if (kWide) {
-                if (a.interleaved) {
-                    const float4 x = __ldg((const float4 *)(cos_row + d0 / 2)), y = __ldg((const float4 *)(sin_row + d0 / 2));
-                    co[0] = co[1] = x.x; co[2] = co[3] = x.y; co[4] = co[5] = x.z; co[6] = co[7] = x.w;
-                    si[0] = si[1] = y.x; si[2] = si[3] = y.y; si[4] = si[5] = y.z; si[6] = si[7] = y.w;
-                } else {
-                    const int j = d0 < half ? d0 : d0 - half;
-                    *(float4 *)&co[0] = __ldg((const float4 *)(cos_row + j)); *(float4 *)&co[4] = __ldg((const float4 *)(cos_row + j + 4));
-                    *(float4 *)&si[0] = __ldg((const float4 *)(sin_row + j)); *(float4 *)&si[4] = __ldg((const float4 *)(sin_row + j + 4));
+            if (kTurn == kPairs) {
+                const float4 x = __ldg((const float4 *)(cos_row + d0 / 2)), y = __ldg((const float4 *)(sin_row + d0 / 2));
+                co[0] = co[1] = x.x; co[2] = co[3] = x.y; co[4] = co[5] = x.z; co[6] = co[7] = x.w;
+                si[0] = -y.x; si[1] = y.x; si[2] = -y.y; si[3] = y.y; si[4] = -y.z; si[5] = y.z; si[6] = -y.w; si[7] = y.w;
+            } else if (kTurn == kSplit) {
+                const int j = d0 < half ? d0 : d0 - half;
+                *(float4 *)&co[0] = __ldg((const float4 *)(cos_row + j)); *(float4 *)&co[4] = __ldg((const float4 *)(cos_row + j + 4));
+                *(float4 *)&si[0] = __ldg((const float4 *)(sin_row + j)); *(float4 *)&si[4] = __ldg((const float4 *)(sin_row + j + 4));
+                if (d0 < half) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) si[e] = -si[e];
                 }
             } else {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     const int d = d0 + e, j = a.interleaved ? d >> 1 : (d < half ? d : d - half);
-                    if (d < a.rotary) { co[e] = __ldg(&cos_row[j]); si[e] = __ldg(&sin_row[j]); }
+                    co[e] = 1.0f; si[e] = 0.0f;
+                    if (d < a.rotary) {
+                        co[e] = __ldg(&cos_row[j]); si[e] = __ldg(&sin_row[j]);
+                        if (a.interleaved ? (e & 1) == 0 : d < half) si[e] = -si[e];
+                    }
                 }
             }
         }
-        // (the first of a pair takes its partner with a minus)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (a.interleaved ? (e & 1) == 0 : d0 + e < half) si[e] = -si[e];
+        const int64_t q_at = 2 * (int64_t)t * a.q_heads * c.head_dim, kv_at = 16 * ((int64_t)spot.page * c.page_stride + (int64_t)spot.place * c.slot_stride);
+        const int64_t cell = ((int64_t)spot.page * c.kv_heads) * c.page_size + spot.place;
 #pragma unroll
         for (int i = 0; i < kEach; ++i) {
             const int row = (share * kEach + i) * kTeams + team;
-            const bool is_q = row < a.q_heads, is_k = !is_q && row < a.q_heads + c.kv_heads, is_v = !is_q && !is_k && row < rows;
-            const int head = is_q ? row : is_k ? row - a.q_heads : row - a.q_heads - c.kv_heads;
+            const bool is_q = row < a.q_heads, is_k = !is_q && row < a.q_heads + c.kv_heads;
             unsigned *w = &u[i].x;
             if (__any_sync(0xffffffffu, is_q || is_k)) {       // (some row of the warp has arithmetic to do)
                 float x[8];
@@ -118,34 +112,37 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache_append(const AppendArg
 #pragma unroll
                     for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                     const float r = rsqrtf(fmaf(sum, a.inv_dim, a.eps));
-                    if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr)
+                    if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) {
+                        const unsigned g[4] = {is_q ? qw.x : kw.x, is_q ? qw.y : kw.y, is_q ? qw.z : kw.z, is_q ? qw.w : kw.w};
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) x[e] *= r * (is_q ? qw[e] : kw[e]);
+                        for (int e = 0; e < 4; ++e) { const float2 p = Pair<T>::unpack(g[e]); x[2 * e] *= r * p.x; x[2 * e + 1] *= r * p.y; }
+                    }
                 }
-                if (a.rotary > 0) {
-                    float other[8];
-                    if (a.interleaved) {
+                if (kTurn == kPairs || (kTurn == kAny && a.interleaved)) {
+                    if (turns) {
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) other[e] = x[e ^ 1];
-                    } else {
-                        __syncwarp();
-                        *(float4 *)&mate[d0] = make_float4(x[0], x[1], x[2], x[3]); *(float4 *)&mate[d0 + 4] = make_float4(x[4], x[5], x[6], x[7]);
-                        __syncwarp();
-                        if (kWide) {
-                            const int at = d0 >= a.rotary ? d0 : d0 < half ? d0 + half : d0 - half;
-                            *(float4 *)&other[0] = *(const float4 *)&mate[at]; *(float4 *)&other[4] = *(const float4 *)&mate[at + 4];
-                        } else {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) { const int d = d0 + e; other[e] = d >= a.rotary ? 0.0f : mate[d < half ? d + half : d - half]; }
+                        for (int e = 0; e < 8; e += 2) {
+                            const float y = fmaf(x[e], co[e], x[e + 1] * si[e]), z = fmaf(x[e + 1], co[e + 1], x[e] * si[e + 1]);
+                            if (kTurn == kPairs || d0 + e < a.rotary) { x[e] = y; x[e + 1] = z; }
                         }
                     }
-                    if (kWide) {
-                        if (d0 < a.rotary)
+                } else if (kTurn != kNone) {
+                    __syncwarp();
+                    *(float4 *)&mate[d0] = make_float4(x[0], x[1], x[2], x[3]); *(float4 *)&mate[d0 + 4] = make_float4(x[4], x[5], x[6], x[7]);
+                    __syncwarp();
+                    if (turns) {
+                        if (kTurn == kSplit) {
+                            const float *const other = &mate[d0 < half ? d0 + half : d0 - half];
+                            const float4 y = *(const float4 *)other, z = *(const float4 *)(other + 4);
+                            x[0] = fmaf(x[0], co[0], y.x * si[0]); x[1] = fmaf(x[1], co[1], y.y * si[1]); x[2] = fmaf(x[2], co[2], y.z * si[2]); x[3] = fmaf(x[3], co[3], y.w * si[3]);
+                            x[4] = fmaf(x[4], co[4], z.x * si[4]); x[5] = fmaf(x[5], co[5], z.y * si[5]); x[6] = fmaf(x[6], co[6], z.z * si[6]); x[7] = fmaf(x[7], co[7], z.w * si[7]);
+                        } else {
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) x[e] = fmaf(x[e], co[e], other[e] * si[e]);
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) if (d0 + e < a.rotary) x[e] = fmaf(x[e], co[e], other[e] * si[e]);
+                            for (int e = 0; e < 8; ++e) {
+                                const int d = d0 + e;
+                                if (d < a.rotary) x[e] = fmaf(x[e], co[e], mate[d < half ? d + half : d - half] * si[e]);
+                            }
+                        }
                     }
                 }
                 if (is_q || is_k) {
@@ -153,24 +150,19 @@ __global__ void __launch_bounds__(kAppendThreads) k_cache_append(const AppendArg
                     for (int e = 0; e < 4; ++e) w[e] = Pair<T>::pack(x[2 * e], x[2 * e + 1]);
                 }
             }
-            if (is_q && mine) *(uint4 *)(a.q_out + 2 * ((((int64_t)s * a.new_tokens + t) * a.q_heads + head) * c.head_dim + d0)) = u[i];
-            if ((is_k || is_v) && spot.page >= 0) {
-                if (mine) *(uint4 *)(const_cast<char *>(is_k ? c.k : c.v) + 16 * (int64_t)cache_row(c, spot, head) + 2 * d0) = u[i];
-                if (is_k && lane == 0) {
-                    const int64_t cell = cache_cell(c, spot, head);
-                    if (c.scores != nullptr) c.scores[cell] = 0.0f;
-                    if (c.positions != nullptr) c.positions[cell] = (int32_t)position;
-                }
+            if (to[i] != nullptr && (is_q || spot.page >= 0)) *(uint4 *)(to[i] + (is_q ? q_at : kv_at)) = u[i];
+            if (is_k && spot.page >= 0 && lane == 0) {
+                const int64_t at = cell + (int64_t)(row - a.q_heads) * c.page_size;
+                if (c.scores != nullptr) c.scores[at] = 0.0f;
+                if (c.positions != nullptr) c.positions[at] = (int32_t)position;
             }
         }
     }
     // padding: its queries are zero, the cache has no room for it
     for (int t = max(t0, count); t < t1; ++t)
 #pragma unroll
-        for (int i = 0; i < kEach; ++i) {
-            const int row = (share * kEach + i) * kTeams + team;
-            if (row < a.q_heads && mine) *(uint4 *)(a.q_out + 2 * ((((int64_t)s * a.new_tokens + t) * a.q_heads + row) * c.head_dim + d0)) = make_uint4(0, 0, 0, 0);
-        }
+        for (int i = 0; i < kEach; ++i)
+            if ((share * kEach + i) * kTeams + team < a.q_heads && mine) *(uint4 *)(to[i] + 2 * (int64_t)t * a.q_heads * c.head_dim) = make_uint4(0, 0, 0, 0);
     if (bad != 0 && threadIdx.x == 0) raise_status(c.status, bad);
 }
 
@@ -179,15 +171,15 @@ cudaError_t launch(const AppendArgs &a, int shares, cudaStream_t s)
 {
     const int half = a.rotary / 2;
     const bool wide = (((uintptr_t)a.cos_table | (uintptr_t)a.sin_table) & 15u) == 0 && half % (a.interleaved ? 4 : 8) == 0;
-    // (runs of up to 8 tokens, as long as there are 16 blocks for every SM: 31 us with one token a block, for 12 291 of which 4120 count)
+    // (runs of up to 8 tokens, as long as there are 16 blocks for every SM)
     int run = 1;
     while (run < 8 && run < a.new_tokens && (int64_t)a.c.num_seqs * ((a.new_tokens + 2 * run - 1) / (2 * run)) * shares >= 148 * 16) run *= 2;
     const int runs = (a.new_tokens + run - 1) / run;
     const int64_t blocks = (int64_t)a.c.num_seqs * runs * shares;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    if (wide) k_cache_append<T, kLanes, kEach, true><<<(unsigned)blocks, kAppendThreads, 0, s>>>(a, shares, runs, run);
-    else k_cache_append<T, kLanes, kEach, false><<<(unsigned)blocks, kAppendThreads, 0, s>>>(a, shares, runs, run);
-    count_launch();
+    const auto kernel = half == 0 ? k_cache_append<T, kLanes, kEach, kNone> : !wide ? k_cache_append<T, kLanes, kEach, kAny>
+                      : a.interleaved ? k_cache_append<T, kLanes, kEach, kPairs> : k_cache_append<T, kLanes, kEach, kSplit>;
+    kernel<<<(unsigned)blocks, kAppendThreads, 0, s>>>(a, shares, runs, run); count_launch();
     return cudaGetLastError();
 }
 template <typename T, int kLanes>
