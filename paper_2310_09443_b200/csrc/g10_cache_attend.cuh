@@ -208,6 +208,19 @@ constexpr int kParts = 4;                // warps of a block; each takes 16 slot
 constexpr int kThreads = 32 * kParts;
 constexpr float kSlack = 8.0f;           // see below
 
+// Running maximum, sum and (four of) the accumulators of a row over some pieces.
+struct Part {
+    float top, sum;
+    float4 o;
+};
+__device__ __forceinline__ void part_add(Part &p, float top, float sum, const float4 &o)
+{
+    const float best = fmaxf(p.top, top), ref = best == -INFINITY ? 0.0f : best;
+    const float f = exp2_of(p.top - ref), g = exp2_of(top - ref);
+    p.top = best;
+    p.sum = p.sum * f + sum * g;
+    p.o = make_float4(p.o.x * f + o.x * g, p.o.y * f + o.y * g, p.o.z * f + o.z * g, p.o.w * f + o.w * g);
+}
 template <typename T, int kSteps, int kCols, int kStages>
 struct Config {
     static constexpr int kDim = 16 * kSteps;             // head_dim, padded with zeros
@@ -216,7 +229,10 @@ struct Config {
     static constexpr int kRows = 8 * kCols;
     static constexpr int kPartBytes = 2 * 16 * kPitch;   // a warp's part of a tile: 16 keys, 16 values
     static constexpr bool kHeld = kCols * kSteps <= 16;  // the queries stay in registers
-    static constexpr int kSmem = kParts * kStages * kPartBytes + (kHeld ? 0 : kRows * kPitch) + kParts * kRows * 8;
+    // what a cluster's blocks read of one another: sums, and maximum and sum of the weights, of every row (32 rows leave no room for it)
+    static constexpr bool kClusters = kCols <= 2;
+    static constexpr int kShared = kClusters ? kRows * kDim * 4 + kRows * 8 : 0;
+    static constexpr int kSmem = kParts * kStages * kPartBytes + (kHeld ? 0 : kRows * kPitch) + kParts * kRows * 8 + kShared;
     // joining the warps' sums: so many columns at a time fit the part of the ring that the warp has just left
     static constexpr int kMerge = kCols < 2 ? kCols : 2;
     static constexpr int kMergePitch = kDim + 4;         // floats (2 rows apart: 8 banks)
@@ -230,33 +246,67 @@ struct Config {
 //   S^T [16 slots x rows] = K Q^T,  W^T = exp2(S^T - ref),  O^T [dims x rows] += V^T W^T,
 // so that 8 rows (one key-value head's group of up to 8 query heads) fill the narrow side of the matrix instruction and keys and values
 // its wide one.  W^T reaches the layout that the second product wants through one 8 x 8 transposition in registers.
+// With `cluster` > 0, for few and short sequences, where the second kernel would take as long as the first: a cluster of so many blocks takes one
+// item, each an equal part of its tiles, and joins the parts itself, through one another's shared memory (16 heads of 517 slots: 10.2 -> 8.2 us).
+// The tiles of an item are then numbered from item * cap on.
 // ref is a maximum of the past: the weights are taken relative to it as long as no logit is more than kSlack above it (weights up to 2^8,
 // which either type holds), so that the sums are rescaled and the warp's lanes compared only when that fails, a few times per piece.
 template <typename T, int kSteps, int kCols, int kStages>
-__global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, int held_blocks)
+__global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, int held_blocks, int cluster, int cap)
 {
     typedef Config<T, kSteps, kCols, kStages> C;
     extern __shared__ __align__(128) char smem[];
-    char *const s_q = smem + kParts * kStages * C::kPartBytes;
+    float *const s_join = (float *)(smem + kParts * kStages * C::kPartBytes);          // [kRows][kDim], then [kRows] maximum and sum (kClusters)
+    float2 *const s_join_ml = (float2 *)(s_join + (C::kClusters ? C::kRows * C::kDim : 0));
+    char *const s_q = smem + kParts * kStages * C::kPartBytes + C::kShared;
     float2 *const s_ml = (float2 *)(s_q + (C::kHeld ? 0 : C::kRows * C::kPitch));      // [kParts][kRows]
     __shared__ Place s_place;
     const int tid = threadIdx.x, lane = tid & 31, part = tid >> 5;
     const int per = a.c.kv_heads * a.row_blocks;
     ull bad = 0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const Tally tally = tally_of<kThreads>(a, bad);
-    const Share share = share_of(tally.total, per, gridDim.x, held_blocks);
-    const int64_t begin = begin_of(share, blockIdx.x);
-    const int n = (int)(begin_of(share, blockIdx.x + 1) - begin);
-    if (bad != 0) raise_status(a.c.status, bad);
-    if (a.logits != nullptr && blockIdx.x == 0 && tid == 0) *a.total = share.total;
-    if (n == 0) return;
-    bad = 0;
-    place_of(a, tally, begin, per, &s_place);
-    __syncthreads();
-
     Cursor now, ahead;
-    cursor_at(a, now, s_place, begin);
+    int64_t begin;
+    int n, rank = 0, my_item = 0;                        // (clusters)
+    if (C::kClusters && cluster > 0) {
+        my_item = (int)blockIdx.x / cluster; rank = (int)blockIdx.x % cluster;
+        now.s = my_item / per; now.item = my_item % per;
+        now.head = now.item / a.row_blocks; now.block = now.item % a.row_blocks;
+        now.q = seq_of(a, now.s, bad);
+        if (bad != 0) raise_status(a.c.status, bad);
+        const int tiles = now.q.tiles;
+        now.idx = tiles * rank / cluster;
+        n = tiles * (rank + 1) / cluster - now.idx;
+        begin = (int64_t)my_item * cap + now.idx;
+        if (a.logits != nullptr && rank == 0) {          // (the numbers that the item does not use)
+            for (int i = tiles + tid; i < cap; i += kThreads) a.notes[(int64_t)my_item * cap + i].tiles = 0;
+            if (my_item == 0 && tid == 0) *a.total = (int64_t)a.c.num_seqs * per * cap;
+        }
+        if (tiles == 0) {                                // (the whole cluster alike)
+            const int chunks = a.c.head_dim / 8;
+            for (int i = rank * kThreads + tid; i < C::kRows * chunks; i += cluster * kThreads) {
+                const int r = i / chunks, row = now.block * C::kRows + r;
+                if (row >= a.rows) continue;
+                const int64_t at = ((int64_t)now.s * a.new_tokens + row / a.group) * a.q_heads + now.head * a.group + row % a.group;
+                *(uint4 *)(a.out + 2 * at * a.c.head_dim + 16 * (i - r * chunks)) = make_uint4(0, 0, 0, 0);
+                if (a.lse != nullptr && i == r * chunks) a.lse[at] = -INFINITY;
+            }
+            return;
+        }
+    } else {
+        const Tally tally = tally_of<kThreads>(a, bad);
+        const Share share = share_of(tally.total, per, gridDim.x, held_blocks);
+        begin = begin_of(share, blockIdx.x);
+        n = (int)(begin_of(share, blockIdx.x + 1) - begin);
+        if (bad != 0) raise_status(a.c.status, bad);
+        if (a.logits != nullptr && blockIdx.x == 0 && tid == 0) *a.total = share.total;
+        if (n == 0) return;
+        place_of(a, tally, begin, per, &s_place);
+        __syncthreads();
+        cursor_at(a, now, s_place, begin);
+    }
+    bad = 0;
+    const int my_s = now.s, my_head = now.head, my_block = now.block;
     ahead = now;
     const unsigned ring = smem_of(smem) + part * kStages * C::kPartBytes;
     // where the row of this lane's slot begins (lanes 16 .. 31: as lanes 0 .. 15), in the tile that `ahead` stands at
@@ -410,7 +460,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
             if (tid < 3) {                               // the tile's note (of the other blocks of rows: that it is none)
                 int2 *const note = (int2 *)&a.notes[begin + u];
                 const int first = first_slot(now.q, now.idx);
-                note[tid] = tid == 0 ? make_int2(now.s, now.head) : tid == 1 ? make_int2(first, now.q.length) : make_int2(now.block == 0 ? now.q.tiles : 0, 0);
+                note[tid] = tid == 0 ? make_int2(now.s, now.head) : tid == 1 ? make_int2(first, now.q.length) : make_int2(now.block == 0 ? (cluster > 0 ? cap : now.q.tiles) : 0, 0);
             }
             float *const to = a.logits + (begin + u) * (int64_t)(logit_pitch * kTile) + (part * 16 + (lane >> 2)) * logit_pitch;
 #pragma unroll
@@ -549,6 +599,11 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
                         sum = fmaf(ml.y, f, sum);
                         o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
                     }
+                    if (C::kClusters && cluster > 0) {
+                        if (d == 0) s_join_ml[r] = make_float2(top, sum);
+                        *(float4 *)(s_join + r * C::kDim + d) = o;
+                        continue;
+                    }
                     if (d == 0) a.ml[r * a.pieces + piece] = make_float2(top, sum);
                     if (!all) {
                         *(float4 *)(a.part + (piece * C::kRows + r) * C::kDim + d) = o;
@@ -574,21 +629,36 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (bad != 0) raise_status(a.c.status, bad);
+    if (C::kClusters && cluster > 0) {
+        // ---- the item's parts are joined: each block takes some of the elements of all ----
+        if (n == 0 && tid < C::kRows) s_join_ml[tid] = make_float2(-INFINITY, 0.0f);
+        cluster_sync();
+        const int quads = a.c.head_dim / 4, rows = min(C::kRows, a.rows - my_block * C::kRows);
+        for (int e = tid * cluster + rank; e < rows * quads; e += kThreads * cluster) {
+            const int r = e / quads, d = (e - r * quads) * 4, row = my_block * C::kRows + r;
+            Part p;
+            p.top = -INFINITY; p.sum = 0.0f; p.o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 4
+            for (int q = 0; q < cluster; ++q) {
+                const float2 ml = read_of(&s_join_ml[r], (unsigned)q);
+                const float4 o = read_of((const float4 *)(s_join + r * C::kDim + d), (unsigned)q);
+                if (ml.y != 0.0f) part_add(p, ml.x, ml.y, o);                      // (a part that saw nothing has no sums)
+            }
+            const int64_t at = ((int64_t)my_s * a.new_tokens + row / a.group) * a.q_heads + my_head * a.group + row % a.group;
+            const float inv = 1.0f / p.sum;
+            uint2 w = make_uint2(Pair<T>::pack(p.o.x * inv, p.o.y * inv), Pair<T>::pack(p.o.z * inv, p.o.w * inv));
+            if (p.sum == 0.0f) w = make_uint2(0, 0);
+            *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
+            if (d == 0) {
+                const float lse = p.top + log2f(p.sum);
+                if (a.lse != nullptr) a.lse[at] = p.sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
+                if (a.logits != nullptr) a.sums[(int64_t)my_item * C::kRows + r] = p.sum == 0.0f ? INFINITY : lse;
+            }
+        }
+        cluster_sync();                                  // (nobody leaves while its memory may still be read)
+    }
 }
 
-// Running maximum, sum and (four of) the accumulators of a row over some pieces.
-struct Part {
-    float top, sum;
-    float4 o;
-};
-__device__ __forceinline__ void part_add(Part &p, float top, float sum, const float4 &o)
-{
-    const float best = fmaxf(p.top, top), ref = best == -INFINITY ? 0.0f : best;
-    const float f = exp2_of(p.top - ref), g = exp2_of(top - ref);
-    p.top = best;
-    p.sum = p.sum * f + sum * g;
-    p.o = make_float4(p.o.x * f + o.x * g, p.o.y * f + o.y * g, p.o.z * f + o.z * g, p.o.w * f + o.w * g);
-}
 // The pieces of blocks b0 .. b1 joined by `lanes` neighbouring threads (a power of two up to 32); every one has the result.
 template <bool kSums>
 __device__ __forceinline__ Part part_join(const AttendArgs &a, int64_t item, int b0, int b1, int block_rows, int r, int padded_dim, int d, int lanes)
@@ -788,13 +858,31 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     const int64_t grid = z.tiles >= kLong * held && kCuts * held <= kMaxBlocks ? kCuts * held : held;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = s;
-    if ((e = cudaLaunchKernelEx(&cfg, kernel, a, (int)held)) != cudaSuccess) return e;
+    // Clusters: where every item has at most four tiles a block and all blocks run at a time.
+    const int64_t cap = z.items > 0 ? z.tiles / z.items : 0;
+    int cluster = 0;
+    if (C::kClusters && z.items <= room && cap >= 1) {
+        static int most_known[kMaxDevices];
+        const void *const kernels[] = {(const void *)kernel};
+        const int most = largest_cluster(kernels, false, kThreads, C::kSmem, most_known);
+        int n = 1;
+        while (2 * n <= 8 && 2 * n <= most && 2 * n <= cap && z.items * 2 * n <= room) n *= 2;
+        if (most >= 1 && cap <= 4 * n) cluster = n;
+    }
+    cudaLaunchAttribute own[1];
+    if (cluster > 0) {
+        own[0].id = cudaLaunchAttributeClusterDimension;
+        own[0].val.clusterDim.x = (unsigned)cluster; own[0].val.clusterDim.y = 1; own[0].val.clusterDim.z = 1;
+        cfg.gridDim = dim3((unsigned)(z.items * cluster)); cfg.attrs = own; cfg.numAttrs = 1;
+    }
+    if ((e = cudaLaunchKernelEx(&cfg, kernel, a, (int)held, cluster, (int)cap)) != cudaSuccess) return e;
     // (the second kernel is brought in, and does its sums over the lengths, while the first still runs)
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
-    if ((e = cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, (int)held, C::kDim, C::kRows)) != cudaSuccess || a.logits == nullptr) return e;
+    if (cluster == 0 && (e = cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, (int)held, C::kDim, C::kRows)) != cudaSuccess) return e;
+    if (a.logits == nullptr) return cudaSuccess;
     const int64_t warps = kJoinThreads / 32, blocks = (z.tiles + warps - 1) / warps, most = 148 * 6;
     cfg.gridDim = dim3((unsigned)(blocks < most ? blocks : most));
     const int pitch = logit_rows(C::kRows < a.rows ? C::kRows : a.rows);
@@ -804,7 +892,7 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
 // Tiles in the ring: as many as let two blocks share an SM, or, for wide heads, fill it for one.
 constexpr int stages_of(int steps, int cols)
 {
-    const int rest = (cols * steps <= 16 ? 0 : 8 * cols * (32 * steps + 16)) + kParts * 8 * cols * 8 + 1024;
+    const int rest = (cols * steps <= 16 ? 0 : 8 * cols * (32 * steps + 16)) + kParts * 8 * cols * 8 + (cols <= 2 ? 8 * cols * (64 * steps + 8) : 0) + 1024;
     const int n = ((steps <= 8 ? 113 : 226) * 1024 - rest) / (2 * kTile * (32 * steps + 16));
     return n > 6 ? 6 : n;
 }

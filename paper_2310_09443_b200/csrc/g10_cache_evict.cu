@@ -25,22 +25,6 @@ __device__ __forceinline__ unsigned worth_at(const EvictArgs &a, int s, int head
     return worth_of(a, __ldg(&a.c.scores[cell]), a.c.positions != nullptr ? __ldg(&a.c.positions[cell]) : slot, seen);
 }
 
-__device__ __forceinline__ unsigned cluster_rank()
-{
-    unsigned r;
-    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
-    return r;
-}
-__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// A word of another block's shared memory.
-__device__ __forceinline__ unsigned read_of(const unsigned *p, unsigned rank)
-{
-    unsigned at, v;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"((unsigned)__cvta_generic_to_shared(p)), "r"(rank));
-    asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-    return v;
-}
-
 __device__ __forceinline__ void add_to(unsigned *p, unsigned rank, unsigned v)
 {
     unsigned at;

@@ -111,6 +111,26 @@ def test_attend_window_and_sinks(g10, window, sinks, new, group):
     check_attend(g10, c, queries(c, new, group, sinks), window=window, sinks=sinks, book=True)
 
 
+@pytest.mark.parametrize("dim", [8, 64, 80, 96, 128, 192, 256])
+@pytest.mark.parametrize("group,new", [(1, 1), (4, 1), (7, 2), (16, 2), (3, 30)])
+def test_attend_with_room_in_the_table(g10, dim, group, new):
+    """Tables much longer than the sequences: what a block has to do is then not known before the lengths are read."""
+    lengths = [new + 1, new + 700, 0, 1, new + 64, 330]
+    for page, columns in ((16, 400), (64, 1000)):
+        c = O.make_cache(lengths, 2, dim, page, torch.bfloat16, dim + group, columns=columns)
+        check_attend(g10, c, queries(c, new, group, dim), book=True)
+        check_attend(g10, c, queries(c, new, group, dim + 1), window=150, sinks=70)
+
+
+@pytest.mark.parametrize("tiles", [1, 2, 3, 5, 8, 9, 16, 31, 32, 33])
+@pytest.mark.parametrize("group", [1, 12])
+def test_attend_lengths_about_what_a_cluster_takes(g10, tiles, group):
+    for lengths in ([64 * tiles], [64 * tiles - 63, 0, 1], [64 * tiles, 64, 65, 64 * tiles - 1]):
+        c = O.make_cache(lengths, 2, 128, 32, torch.float16, tiles)
+        check_attend(g10, c, queries(c, 1, group, tiles), book=True)
+        check_attend(g10, c, queries(c, 1, group, tiles), window=100, sinks=3)
+
+
 def test_attend_window_reads_nothing_outside(g10):
     """What stands between the first slots and the window may be anything."""
     c = O.make_cache([700], 2, 64, 16, torch.float16, 3)
