@@ -164,13 +164,14 @@ struct AttendArgs {
     float2 *ml;                          // [block rows][pieces] running maximum and sum of every piece
     float *part;                         // [pieces][block rows][padded head_dim] its sums, not divided yet
     float *logits;                       // [tiles][64][rows of a block] scaled by log2 e (null: weights are not booked)
+    bool books;
     float *sums;                         // [items][block rows] lse of every row, to base 2
     TileNote *notes;                     // [tiles]
     int64_t *total;                      // number of tiles
 };
 // Sizes that the workspace goes by.
 struct AttendShape {
-    int row_blocks, block_rows, logit_rows, padded_dim;
+    int row_blocks, block_rows, logit_rows, padded_dim;  // (logit_rows 0: the rows' kernels, which leave no logits)
     int64_t items, pieces, tiles;        // upper bounds for the sequences' capacity
 };
 AttendShape attend_shape(const CacheView &c, int rows, int new_tokens, int window, int sinks);

@@ -59,7 +59,7 @@ AttendLayout attend_layout(const AttendShape &z, bool scores)
     l.logits = align_up(l.part + sizeof(float) * (size_t)z.pieces * z.block_rows * z.padded_dim);
     l.sums = align_up(l.logits + (scores ? sizeof(float) * (size_t)z.tiles * z.logit_rows * 64 : 0));
     l.notes = align_up(l.sums + (scores ? sizeof(float) * (size_t)z.items * z.block_rows : 0));
-    l.total = align_up(l.notes + (scores ? sizeof(TileNote) * (size_t)z.tiles : 0));
+    l.total = align_up(l.notes + (scores && z.logit_rows > 0 ? sizeof(TileNote) * (size_t)z.tiles : 0));
     l.bytes = align_up(l.total + sizeof(int64_t));
     return l;
 }
@@ -141,7 +141,8 @@ int32_t g10_cache_attend(const g10_cache *cache, const g10_cache_queries *u, voi
     if (!ws || ((uintptr_t)ws & (kAlign - 1)) || ws_bytes < l.bytes) return G10_ERR_WORKSPACE;
     a.row_blocks = z.row_blocks; a.pieces = z.pieces;
     a.ml = (float2 *)((char *)ws + l.ml); a.part = (float *)((char *)ws + l.part);
-    a.logits = u->add_scores ? (float *)((char *)ws + l.logits) : nullptr;
+    a.books = u->add_scores != 0;
+    a.logits = a.books && z.logit_rows > 0 ? (float *)((char *)ws + l.logits) : nullptr;
     a.sums = (float *)((char *)ws + l.sums); a.notes = (TileNote *)((char *)ws + l.notes); a.total = (int64_t *)((char *)ws + l.total);
     return status_of(launch_cache_attend(a, cache->dtype, (cudaStream_t)stream));
 }

@@ -21,6 +21,7 @@ namespace attend {
 
 constexpr int kTile = 64;                // slots
 constexpr int kMaxBlocks = 148 * 8;      // of the grid; the workspace has room for their pieces
+constexpr int kMaxWideBlocks = 148 * 4;  // ... with 128 rows each
 constexpr int kJoinThreads = 256;
 
 __device__ __forceinline__ unsigned smem_of(const void *p) { return (unsigned)__cvta_generic_to_shared(p); }
@@ -83,7 +84,15 @@ struct Tally {
     int64_t start, sum;                  // tiles before them and of them (of one item of each sequence)
     int64_t total;
 };
-template <int kThreads>
+// (kUnit: tiles that count as one)
+template <int kUnit>
+__device__ __forceinline__ Seq units_of(const AttendArgs &a, int s, ull &bad)
+{
+    Seq q = seq_of(a, s, bad);
+    q.tiles = (q.tiles + kUnit - 1) / kUnit;
+    return q;
+}
+template <int kThreads, int kUnit = 1>
 __device__ __forceinline__ Tally tally_of(const AttendArgs &a, ull &bad)
 {
     __shared__ int64_t s_sum[kThreads / 32];
@@ -92,7 +101,7 @@ __device__ __forceinline__ Tally tally_of(const AttendArgs &a, ull &bad)
     Tally t;
     t.from = min(a.c.num_seqs, (int)threadIdx.x * each); t.to = min(a.c.num_seqs, t.from + each);
     long long sum = 0;
-    for (int s = t.from; s < t.to; ++s) sum += seq_of(a, s, bad).tiles;
+    for (int s = t.from; s < t.to; ++s) sum += units_of<kUnit>(a, s, bad).tiles;
     const long long upto = warp_inclusive_scan_i64(sum, lane);
     if (lane == 31) s_sum[warp] = upto;
     __syncthreads();
@@ -136,6 +145,7 @@ struct Place {
     int64_t before;
     int s;
 };
+template <int kUnit = 1>
 __device__ __forceinline__ void place_of(const AttendArgs &a, const Tally &t, int64_t u, int per, Place *to)
 {
     if (!(t.start * per <= u && u < (t.start + t.sum) * per)) return;
@@ -143,7 +153,7 @@ __device__ __forceinline__ void place_of(const AttendArgs &a, const Tally &t, in
     int s = t.from;
     for (;; ++s) {
         ull ignored = 0;
-        const int64_t n = (int64_t)seq_of(a, s, ignored).tiles * per;
+        const int64_t n = (int64_t)units_of<kUnit>(a, s, ignored).tiles * per;
         if (u < before + n) break;
         before += n;
     }
@@ -156,15 +166,17 @@ struct Cursor {
     int head, block;                     // key-value head and block of rows: item = head * row_blocks + block
     Seq q;
 };
+template <int kUnit = 1>
 __device__ __forceinline__ void cursor_at(const AttendArgs &a, Cursor &u, const Place &p, int64_t tile)
 {
     ull ignored = 0;
     u.s = p.s;
-    u.q = seq_of(a, p.s, ignored);
+    u.q = units_of<kUnit>(a, p.s, ignored);
     const int64_t in = tile - p.before;
     u.item = (int)divided(in, u.q.tiles); u.idx = (int)(in - (int64_t)u.item * u.q.tiles);
     u.head = u.item / a.row_blocks; u.block = u.item - u.head * a.row_blocks;
 }
+template <int kUnit = 1>
 __device__ __forceinline__ void cursor_next(const AttendArgs &a, Cursor &u, int per)
 {
     if (++u.idx < u.q.tiles) return;
@@ -175,7 +187,7 @@ __device__ __forceinline__ void cursor_next(const AttendArgs &a, Cursor &u, int 
     ull ignored = 0;
     do {
         if (++u.s >= a.c.num_seqs) { u.s = a.c.num_seqs; u.q.tiles = 0; return; }       // (behind the last: never used)
-        u.q = seq_of(a, u.s, ignored);
+        u.q = units_of<kUnit>(a, u.s, ignored);
     } while (u.q.tiles == 0);
 }
 
@@ -616,7 +628,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
                         if (d == 0) {
                             const float lse = top + log2f(sum);
                             if (a.lse != nullptr) a.lse[at] = sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
-                            if (a.logits != nullptr) a.sums[item * C::kRows + r] = sum == 0.0f ? INFINITY : lse;
+                            if (a.books) a.sums[item * C::kRows + r] = sum == 0.0f ? INFINITY : lse;
                         }
                     }
                 }
@@ -652,7 +664,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
             if (d == 0) {
                 const float lse = p.top + log2f(p.sum);
                 if (a.lse != nullptr) a.lse[at] = p.sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
-                if (a.logits != nullptr) a.sums[(int64_t)my_item * C::kRows + r] = p.sum == 0.0f ? INFINITY : lse;
+                if (a.books) a.sums[(int64_t)my_item * C::kRows + r] = p.sum == 0.0f ? INFINITY : lse;
             }
         }
         cluster_sync();                                  // (nobody leaves while its memory may still be read)
@@ -737,7 +749,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
         const int s = s_cut[side].s, head = s_cut[side].head, first_row = s_cut[side].block * block_rows, rows = min(block_rows, a.rows - first_row);
         const int lanes = lanes_for(pieces), teams = 32 / lanes;
         const int quads = a.c.head_dim / 4, all = rows * quads;
-        const int e0 = all * (b - w.b0) / pieces, e1 = all * (b - w.b0 + 1) / pieces;            // (32 rows at most: 32 bits)
+        const int parts = pieces * gridDim.y, nth = (b - w.b0) * gridDim.y + blockIdx.y;         // (128 rows at most: 32 bits)
+        const int e0 = all * nth / parts, e1 = all * (nth + 1) / parts;
         for (int e = e0 + warp % kHalf * teams; e < e1; e += kHalf * teams) {                    // (all lanes take part in the shuffles)
             const int mine = min(e + lane / lanes, e1 - 1), r = mine / quads, d = mine % quads * 4, row = first_row + r;
             const Part p = part_join<true>(a, w.item, w.b0, w.b1, block_rows, r, padded_dim, d, lanes);
@@ -750,13 +763,13 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
                 if (d == 0) {
                     const float lse = p.top + log2f(p.sum);
                     if (a.lse != nullptr) a.lse[at] = p.sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
-                    if (a.logits != nullptr) a.sums[w.item * block_rows + r] = p.sum == 0.0f ? INFINITY : lse;
+                    if (a.books) a.sums[w.item * block_rows + r] = p.sum == 0.0f ? INFINITY : lse;
                 }
             }
         }
     }
     // ---- (2) ----
-    for (int s = b; s < a.c.num_seqs; s += gridDim.x) {
+    for (int s = b; s < a.c.num_seqs && blockIdx.y == 0; s += gridDim.x) {
         if (seq_of(a, s, ignored).tiles > 0) continue;
         const int64_t rows = (int64_t)a.new_tokens * a.q_heads, n = rows * (a.c.head_dim / 8);
         for (int64_t i = tid; i < n; i += kJoinThreads) ((uint4 *)(a.out + 2 * s * rows * a.c.head_dim))[i] = make_uint4(0, 0, 0, 0);
@@ -899,10 +912,7 @@ constexpr int stages_of(int steps, int cols)
 template <typename T, int kSteps>
 cudaError_t launch_steps(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
 {
-    if (z.block_rows == 8) return launch<T, kSteps, 1, stages_of(kSteps, 1)>(a, z, s);
-    if (z.block_rows == 16) return launch<T, kSteps, 2, stages_of(kSteps, 2)>(a, z, s);
-    if constexpr (kSteps <= 8) return launch<T, kSteps, 4, stages_of(kSteps, 4)>(a, z, s);
-    return cudaErrorInvalidValue;                        // (wide heads: 16 rows at most)
+    return z.block_rows == 8 ? launch<T, kSteps, 1, stages_of(kSteps, 1)>(a, z, s) : launch<T, kSteps, 2, stages_of(kSteps, 2)>(a, z, s);
 }
 template <typename T>
 cudaError_t launch_type(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
@@ -921,5 +931,7 @@ cudaError_t launch_type(const AttendArgs &a, const AttendShape &z, cudaStream_t 
 
 cudaError_t launch_cache_attend_bf16(const AttendArgs &a, const AttendShape &z, cudaStream_t s);
 cudaError_t launch_cache_attend_fp16(const AttendArgs &a, const AttendShape &z, cudaStream_t s);
+cudaError_t launch_cache_rows_bf16(const AttendArgs &a, const AttendShape &z, cudaStream_t s);      // (g10_cache_rows_*.cu)
+cudaError_t launch_cache_rows_fp16(const AttendArgs &a, const AttendShape &z, cudaStream_t s);
 
 }  // namespace g10

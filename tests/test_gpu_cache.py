@@ -180,7 +180,23 @@ def test_attend_spreads_and_extremes(g10):
     check_attend(g10, c, queries(c, 1, 8, 2), scale=-0.2)
 
 
-@pytest.mark.parametrize("lengths,kv,group,dim", [([9001], 1, 8, 128), ([20000, 3, 4000, 0, 900], 2, 4, 64), ([5000] * 40, 4, 1, 64), ([2500] * 7, 8, 16, 128), ([3000, 1], 1, 1, 256)])
+@pytest.mark.parametrize("new,group", [(1, 8), (1, 12), (5, 5), (30, 4), (2, 80)])
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+def test_attend_where_later_slots_outweigh_all_before(g10, new, group, kind):
+    """Logits that rise along the sequence, by a little or by so much that each tile makes what was before it vanish; and that fall."""
+    c = O.make_cache([1000, 130 + new], 2, 64, 16, O.TYPES[kind], 31)
+    q = torch.ones(2, new, 2 * group, 64, dtype=c.dtype)
+    q[:, :, 1::2] = -1
+    for rise in (0.004, 0.05, 0.5):
+        for s, n in enumerate(c.lengths.tolist()):
+            pg, pl = O.places(c, s, n)
+            c.k[pg, pl] = (torch.arange(n)[:, None, None] * rise / 64 + 0.01 * torch.randn(n, 2, 64, generator=torch.Generator().manual_seed(s))).to(c.dtype)
+        for scale in (1.0, -1.0, 4.0, 0.0):
+            check_attend(g10, c, q, scale=scale, book=True)
+
+
+@pytest.mark.parametrize("lengths,kv,group,dim", [([9001], 1, 8, 128), ([20000, 3, 4000, 0, 900], 2, 4, 64), ([5000] * 40, 4, 1, 64), ([2500] * 7, 8, 16, 128), ([3000, 1], 1, 1, 256),
+                                                  ([6000, 1, 2000], 2, 24, 128), ([3000] * 9, 3, 40, 96), ([4000, 70], 1, 200, 256)])
 def test_attend_long(g10, lengths, kv, group, dim):
     c = O.make_cache(lengths, kv, dim, 64, torch.bfloat16, len(lengths))
     check_attend(g10, c, queries(c, 1, group, 3), book=True)
