@@ -39,14 +39,16 @@ __device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity)
     return ok != 0;
 }
 // Once a wait has run out anywhere in the block, none waits any more: the block goes through its tiles without them (every access stays where it
-// would be) and says so in the status word.
+// would be) and says so in the status word.  Whole warps wait, and leave the wait together: what follows mostly is an instruction that a warp
+// has to execute as one (a warp that had come apart in a wait read and wrote tensor memory piecemeal, which gave wrong sums and illegal instructions).
 __device__ __forceinline__ void bar_wait(unsigned bar, unsigned parity, volatile int *s_stop)
 {
-    if (bar_try(bar, parity)) return;
     for (unsigned i = 0; i < kWideSpins; ++i) {
-        if (bar_try(bar, parity) || *s_stop != 0) return;
+        const bool done = bar_try(bar, parity) || (i > 0 && *s_stop != 0);
+        if (__all_sync(0xffffffffu, done)) return;
     }
     *s_stop = 1;
+    __syncwarp();
 }
 
 // ---- tensor memory and products ----
@@ -55,15 +57,17 @@ __device__ __forceinline__ void after_sync() { asm volatile("tcgen05.fence::afte
 __device__ __forceinline__ void async_sees() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
 #define G10_R8(x, i) "=r"(x[i]), "=r"(x[i + 1]), "=r"(x[i + 2]), "=r"(x[i + 3]), "=r"(x[i + 4]), "=r"(x[i + 5]), "=r"(x[i + 6]), "=r"(x[i + 7])
 #define G10_W8(x, i) "r"(x[i]), "r"(x[i + 1]), "r"(x[i + 2]), "r"(x[i + 3]), "r"(x[i + 4]), "r"(x[i + 5]), "r"(x[i + 6]), "r"(x[i + 7])
-// 32 columns of the warp's lanes: a lane's row to its thread and back.
+// 32 columns of the warp's lanes: a lane's row to its thread and back.  (Executed by the warp as one: whatever came before may have parted it.)
 __device__ __forceinline__ void tmem_load(unsigned (&x)[32], unsigned at)
 {
+    __syncwarp();
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
                  "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
                  : G10_R8(x, 0), G10_R8(x, 8), G10_R8(x, 16), G10_R8(x, 24) : "r"(at) : "memory");
 }
 __device__ __forceinline__ void tmem_store(const unsigned (&x)[32], unsigned at)
 {
+    __syncwarp();
     asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
                  "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
                  ::G10_W8(x, 0), G10_W8(x, 8), G10_W8(x, 16), G10_W8(x, 24), "r"(at) : "memory");
@@ -98,11 +102,13 @@ __device__ __forceinline__ void tell_when_done(unsigned bar)
 }
 __device__ __forceinline__ void tmem_take(unsigned *to, unsigned columns)
 {
+    __syncwarp();
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_of(to)), "r"(columns) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tmem_give_back(unsigned at, unsigned columns)
 {
+    __syncwarp();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(at), "r"(columns) : "memory");
 }
 // Where 16-byte unit `unit` (of 8 dimensions) of a row lies: blocks of 64 dimensions `block` bytes apart.
@@ -122,14 +128,33 @@ __device__ __forceinline__ void rows_meet() { asm volatile("barrier.cta.sync 1, 
 __device__ __forceinline__ float2 fma2(float2 a, float2 b, float2 c)
 {
     float2 d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(*(uint64_t *)&d) : "l"(*(const uint64_t *)&a), "l"(*(const uint64_t *)&b), "l"(*(const uint64_t *)&c));
+    asm("{\n\t.reg .b64 x, y, z;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmov.b64 z, {%6, %7};\n\tfma.rn.f32x2 x, x, y, z;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y));
     return d;
 }
 __device__ __forceinline__ float2 add2(float2 a, float2 b)
 {
     float2 d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(*(uint64_t *)&d) : "l"(*(const uint64_t *)&a), "l"(*(const uint64_t *)&b));
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tadd.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
+}
+// 32 logits of the thread's row.
+__device__ __forceinline__ void logits_load(float2 *x, unsigned at)
+{
+    unsigned raw[32];
+    tmem_load(raw, at);
+    tmem_loaded();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) x[i] = make_float2(__uint_as_float(raw[2 * i]), __uint_as_float(raw[2 * i + 1]));
+}
+// One thread of the warp (all of it calls).
+__device__ __forceinline__ bool elected()
+{
+    unsigned one;
+    __syncwarp();
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
 }
 
 template <int kDims>                     // blocks of 64 dimensions
@@ -210,6 +235,8 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
         const int part = warp - 9;
         constexpr unsigned kNone = 0xffffffffu;
         const uint64_t policy = leaves_first();
+        int stage = 0, landed = 0;
+        unsigned round = 1;
         // (the page is loaded a tile ahead, and looked at when its turn comes)
         int page = -1, at_place = 0, head = 0;
         auto look_up = [&]() {
@@ -231,23 +258,30 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
             if (u >= C::kLag) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(C::kLag - 1) : "memory");
                 async_sees();
-                bar_arrive(full + 8 * ((u - C::kLag) % S));
+                bar_arrive(full + 8 * landed);
+                landed = landed == S - 1 ? 0 : landed + 1;
             }
             if (u < n) {
                 const unsigned mine = row_found();
                 if (u + 1 < n) { cursor_next(a, now, per); look_up(); }
-                bar_wait(free_ + 8 * (u % S), ((u / S) & 1) ^ 1, &s_stop);
-                const unsigned to = smem_of(s_ring) + (u % S) * C::kStageBytes;
+                bar_wait(free_ + 8 * stage, round, &s_stop);
+                const unsigned to = smem_of(s_ring) + stage * C::kStageBytes;
+                if (++stage == S) { stage = 0; round ^= 1; }
                 const bool all = __all_sync(0xffffffffu, mine != kNone) && a.c.head_dim == C::kDim && a.row_blocks == 1;
-#pragma unroll 8
-                for (int i = 0; i < C::kUnits; ++i) {
-                    const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
-                    const unsigned from = __shfl_sync(0xffffffffu, mine, row), at = swizzled(part * 32 + row, unit, kBlock);
-                    if (all) {
-                        const int64_t x = 16 * ((int64_t)from + unit);
-                        copy16(to + at, a.c.k + x, policy);
-                        copy16(to + kDims * kBlock + at, a.c.v + x, policy);
-                    } else {
+                if (all) {
+#pragma unroll
+                    for (int i = 0; i < C::kUnits; ++i) {
+                        const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
+                        const int64_t x = 16 * (int64_t)__shfl_sync(0xffffffffu, mine, row);
+                        const unsigned at = swizzled(part * 32 + row, unit, kBlock);
+                        copy16(to + at, a.c.k + 16 * unit + x, policy);
+                        copy16(to + kDims * kBlock + at, a.c.v + 16 * unit + x, policy);
+                    }
+                } else {
+#pragma unroll 2
+                    for (int i = 0; i < C::kUnits; ++i) {
+                        const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
+                        const unsigned from = __shfl_sync(0xffffffffu, mine, row), at = swizzled(part * 32 + row, unit, kBlock);
                         const bool there = from != kNone && unit * 8 < a.c.head_dim;
                         const int64_t x = there ? 16 * ((int64_t)from + unit) : 0;
                         copy16_or_zeros(to + at, a.c.k + x, there);
@@ -260,44 +294,58 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (bad != 0) raise_status(a.c.status, bad);
     } else if (warp == 8) {
-        // ---- the issuer ----
-        if (lane == 0) {
-            const unsigned keys = product_of<T, false>(kWideRows, kTile), values = product_of<T, true>(kWideRows, C::kDim);
-            const int steps = (a.c.head_dim + 15) / 16;
-            const unsigned q_at = smem_of(s_q), ring = smem_of(s_ring);
-            bool first = true;                           // of its piece
-            int pieces = 0, since = 0, since_before = 0; // tiles of the piece before tile u, before tile u - 1
-            auto take_values = [&](int v, bool starts) {
-                bar_wait(w_full + 8 * (v & 1), (v >> 1) & 1, &s_stop);
-                after_sync();
+        // ---- the issuer: the warp goes through the tiles together, one thread of it issues ----
+        const bool leads = elected();
+        const unsigned keys = product_of<T, false>(kWideRows, kTile), values = product_of<T, true>(kWideRows, C::kDim);
+        const unsigned ring = smem_of(s_ring);
+        // (descriptors: an address in units of 16 bytes in the lowest bits, so that the operands of later steps and stages are sums)
+        const uint64_t q_operand = operand(smem_of(s_q), 16, 1024), k_operand = operand(ring, 16, 1024), v_operand = operand(ring + kDims * kBlock, kBlock, 1024);
+        int stage = 0, stage_before = 0;
+        unsigned round = 0;
+        bool first = true;                               // of its piece
+        int pieces = 0, since = 0, since_before = 0;     // tiles of the piece before tile u, before tile u - 1
+        auto take_values = [&](int v, bool starts) {
+            bar_wait(w_full + 8 * (v & 1), (v >> 1) & 1, &s_stop);
+            __syncwarp();
+            after_sync();
+            if (leads) {
                 if (s_apart[v & 1] == 0) {
-                    const unsigned at = ring + (v % S) * C::kStageBytes + kDims * kBlock;
+                    const unsigned to = tmem + (C::kTeams == 2 ? (v & 1) * C::kDim : 0), from = tmem + C::kLogits + (v & 1) * kTile;
+                    const uint64_t at = v_operand + (unsigned)(stage_before * (C::kStageBytes >> 4));
 #pragma unroll
-                    for (int k = 0; k < kTile / 16; ++k)
-                        multiply_tmem(tmem + (C::kTeams == 2 ? (v & 1) * C::kDim : 0), tmem + C::kLogits + (v & 1) * kTile + 8 * k, operand(at + k * 16 * 128, kBlock, 1024), values, !(starts && k == 0));
+                    for (int k = 0; k < kTile / 16; ++k) multiply_tmem(to, from + 8 * k, at + (unsigned)(k * (16 * 128 >> 4)), values, !(starts && k == 0));
                 }
-                tell_when_done(free_ + 8 * (v % S));
+                tell_when_done(free_ + 8 * stage_before);
                 tell_when_done(v_done + 8 * (v & 1));
-            };
-            for (int u = 0; u < n; ++u) {
-                if (first) { bar_wait(q_full, pieces & 1, &s_stop); ++pieces; since = 0; }
-                bar_wait(full + 8 * (u % S), (u / S) & 1, &s_stop);
-                if (u >= 2) bar_wait(v_done + 8 * (u & 1), ((u >> 1) - 1) & 1, &s_stop);         // (the weights of tile u - 2 lie where its logits will)
-                after_sync();
-                const unsigned at = ring + (u % S) * C::kStageBytes;
-                for (int k = 0; k < steps; ++k)
-                    multiply(tmem + C::kLogits + (u & 1) * kTile, operand(q_at + (k >> 2) * kWideRows * 128 + (k & 3) * 32, 16, 1024),
-                             operand(at + (k >> 2) * kBlock + (k & 3) * 32, 16, 1024), keys, k > 0);
-                tell_when_done(s_full + 8 * (u & 1));
-                if (u > 0) take_values(u - 1, since_before < C::kTeams);
-                since_before = since++;
-                first = now.idx == now.q.tiles - 1;
-                cursor_next(a, now, per);
             }
-            take_values(n - 1, since_before < C::kTeams);
-            // (nothing is given back before the last product is done, stopped or not)
-            for (unsigned i = 0; i < kWideSpins && !bar_try(v_done + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1); ++i) {}
+            __syncwarp();
+        };
+        for (int u = 0; u < n; ++u) {
+            if (first) { bar_wait(q_full, pieces & 1, &s_stop); ++pieces; since = 0; }
+            bar_wait(full + 8 * stage, round, &s_stop);
+            if (u >= 2) bar_wait(v_done + 8 * (u & 1), ((u >> 1) - 1) & 1, &s_stop);     // (the weights of tile u - 2 lie where its logits will)
+            __syncwarp();
+            after_sync();
+            if (leads) {
+                const unsigned to = tmem + C::kLogits + (u & 1) * kTile;
+                const uint64_t at = k_operand + (unsigned)(stage * (C::kStageBytes >> 4));
+                // (dimensions behind head_dim are zeros on both sides)
+#pragma unroll
+                for (int k = 0; k < 4 * kDims; ++k)
+                    multiply(to, q_operand + (unsigned)(((k >> 2) * kWideRows * 128 + (k & 3) * 32) >> 4), at + (unsigned)(((k >> 2) * kBlock + (k & 3) * 32) >> 4), keys, k > 0);
+                tell_when_done(s_full + 8 * (u & 1));
+            }
+            __syncwarp();
+            if (u > 0) take_values(u - 1, since_before < C::kTeams);
+            since_before = since++;
+            stage_before = stage;
+            if (++stage == S) { stage = 0; round ^= 1; }
+            first = now.idx == now.q.tiles - 1;
+            cursor_next(a, now, per);
         }
+        take_values(n - 1, since_before < C::kTeams);
+        // (nothing is given back before the last product is done, stopped or not)
+        for (unsigned i = 0; i < kWideSpins && !bar_try(v_done + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1); ++i) {}
         __syncwarp();
     } else {
         // ---- rows: a thread of each team each ----
@@ -332,9 +380,8 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                 float2 x[kTile / 2];
                 if (busy) {
                     auto load = [&]() {
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) tmem_load(*(unsigned(*)[32])&x[16 * h], logits + 32 * h);
-                        tmem_loaded();
+                        logits_load(x, logits);
+                        logits_load(x + 16, logits + 32);
                     };
                     // Weights relative to the reference, and their sum.  Only if that gets near what the types hold (or there is no reference yet) is the largest
                     // logit looked for, and everything so far rescaled.
@@ -627,33 +674,38 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_book_wide(const AttendAr
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (bad != 0) raise_status(a.c.status, bad);
     } else if (warp == 8) {
-        if (lane == 0) {
-            const int steps = (a.c.head_dim + 15) / 16;
-            const unsigned q_at = smem_of(s_q), ring = smem_of(s_ring);
-            int given = 0;                               // times that queries were brought
-            bool fresh = true;
-            for (int u = 0, d = 0; u < n; ++u) {
-                bar_wait(full + 8 * (u % S), (u / S) & 1, &s_stop);
-                for (int b = 0; b < blocks; ++b, ++d) {
-                    if (fresh || blocks > 1) { bar_wait(q_full, given & 1, &s_stop); ++given; }          // (brought for every run)
-                    fresh = false;
-                    if (d >= 2) bar_wait(d_free + 8 * (d & 1), ((d >> 1) - 1) & 1, &s_stop);
-                    after_sync();
+        const bool leads = elected();
+        const uint64_t q_operand = operand(smem_of(s_q), 16, 1024), k_operand = operand(smem_of(s_ring), 16, 1024);
+        int given = 0;                                   // times that queries were brought
+        bool fresh = true;
+        int stage = 0;
+        unsigned round = 0;
+        for (int u = 0, d = 0; u < n; ++u) {
+            bar_wait(full + 8 * stage, round, &s_stop);
+            for (int b = 0; b < blocks; ++b, ++d) {
+                if (fresh || blocks > 1) { bar_wait(q_full, given & 1, &s_stop); ++given; }      // (brought for every run)
+                fresh = false;
+                if (d >= 2) bar_wait(d_free + 8 * (d & 1), ((d >> 1) - 1) & 1, &s_stop);
+                __syncwarp();
+                after_sync();
+                if (leads) {
                     const int rows = min(kWideRows, a.rows - b * kWideRows);
-                    const unsigned what = product_of<T, false>(128, (rows + 15) & ~15);
-                    const unsigned at = ring + (u % S) * C::kStageBytes;
-                    for (int k = 0; k < steps; ++k)
-                        multiply(tmem + (d & 1) * 128, operand(at + (k >> 2) * 128 * 128 + (k & 3) * 32, 16, 1024),
-                                 operand(q_at + (k >> 2) * kWideRows * 128 + (k & 3) * 32, 16, 1024), what, k > 0);
-                    if (b == blocks - 1) tell_when_done(free_ + 8 * (u % S));
+                    const unsigned what = product_of<T, false>(128, (rows + 15) & ~15), to = tmem + (d & 1) * 128;
+                    const uint64_t at = k_operand + (unsigned)(stage * (C::kStageBytes >> 4));
+#pragma unroll
+                    for (int k = 0; k < 4 * kDims; ++k)
+                        multiply(to, at + (unsigned)(((k >> 2) * 128 * 128 + (k & 3) * 32) >> 4), q_operand + (unsigned)(((k >> 2) * kWideRows * 128 + (k & 3) * 32) >> 4), what, k > 0);
+                    if (b == blocks - 1) tell_when_done(free_ + 8 * stage);
                     tell_when_done(d_full + 8 * (d & 1));
                 }
-                fresh = now.idx == now.q.tiles - 1;
-                cursor_next<2>(one, now, heads);
+                __syncwarp();
             }
-            const int last = n * blocks - 1;
-            for (unsigned i = 0; i < kWideSpins && !bar_try(d_full + 8 * (last & 1), (last >> 1) & 1); ++i) {}
+            if (++stage == S) { stage = 0; round ^= 1; }
+            fresh = now.idx == now.q.tiles - 1;
+            cursor_next<2>(one, now, heads);
         }
+        const int last = n * blocks - 1;
+        for (unsigned i = 0; i < kWideSpins && !bar_try(d_full + 8 * (last & 1), (last >> 1) & 1); ++i) {}
         __syncwarp();
     } else {
         // ---- slots: a thread each; the two teams take the pairs of tiles in turn ----
@@ -695,8 +747,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_book_wide(const AttendAr
 #pragma unroll 1
                     for (int c = 0; c < rows; c += 32) {
                         float2 x[16];
-                        tmem_load(*(unsigned(*)[32])&x[0], mine + (d & 1) * 128 + c);
-                        tmem_loaded();
+                        logits_load(x, mine + (d & 1) * 128 + c);
                         if (whole && c + 32 <= rows) {
 #pragma unroll
                             for (int i = 0; i < 16; i += 2) {
