@@ -26,6 +26,7 @@ namespace attend {
 
 constexpr int kWideRows = 128;           // of a block
 constexpr int kRowThreads = 256, kLoadThreads = 64, kWideThreads = kRowThreads + 32 + kLoadThreads;      // 8 warps of rows, 1 that issues, 2 that load
+constexpr int kBookThreads = kRowThreads + 32 + 128;
 constexpr unsigned kWideSpins = 1u << 22;
 constexpr int kBlock = kTile * 128;      // bytes of 64 dimensions of a tile's keys or values
 
@@ -165,9 +166,16 @@ struct Wide {
     static constexpr int kSmem = 1024 + kQBytes + kStages * kStageBytes;
     static constexpr int kTeams = 2 * kDim + 2 * kTile <= 512 ? 2 : 1;
     static constexpr int kLogits = kTeams * kDim;        // first column of tensor memory behind each team's O: S twice (W over its S)
-    static constexpr unsigned kColumns = kLogits + 2 * kTile <= 256 ? 256 : 512;
+    // W has columns of its own where there is room; else it lies over its S, which then is not free before W has been used
+    static constexpr bool kOwnWeights = kLogits + 2 * kTile + kTile <= 512;
+    static constexpr int kWeights = kLogits + (kOwnWeights ? 2 * kTile : 0), kWeightsApart = kOwnWeights ? kTile / 2 : kTile;
+    static constexpr int kUsed = kLogits + 2 * kTile + (kOwnWeights ? kTile : 0);
+    static constexpr unsigned kColumns = kUsed <= 256 ? 256 : 512;
     static constexpr int kLag = kStages > 3 ? 3 : kStages - 1;       // tiles on their way before the first of them is waited for
-    static_assert(kStages >= 2, "two tiles");
+    // Tiles whose product with the queries is issued before the product of a tile with its values.  (A tile is told full kLag tiles after its
+    // copies were issued, which wait for a stage: kLag + kBehind stages at least, or the two wait for each other.)
+    static constexpr int kBehind = kStages - kLag >= 2 && kTeams == 2 ? 2 : 1;
+    static_assert(kStages >= 2 && kLag + kBehind <= kStages, "stages");
 };
 
 // A row's queries, from global memory to their exchanged places (with the sign of the scale, so that the largest product is the largest logit).
@@ -195,7 +203,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
     typedef Wide<kDims> C;
     constexpr int S = C::kStages;
     extern __shared__ char smem_raw[];
-    __shared__ __align__(8) uint64_t s_bar[2 * S + 7];
+    __shared__ __align__(8) uint64_t s_bar[2 * S + 9];
     __shared__ Place s_place;
     __shared__ int s_stop, s_apart[2];
     __shared__ float2 s_ml[2][kWideRows];
@@ -212,11 +220,11 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
     if (n == 0) return;
     bad = 0;
     place_of(a, tally, begin, per, &s_place);
-    const unsigned full = smem_of(s_bar), free_ = full + 8 * S, s_full = free_ + 8 * S, w_full = s_full + 16, q_full = w_full + 16, v_done = q_full + 8;
+    const unsigned full = smem_of(s_bar), free_ = full + 8 * S, s_full = free_ + 8 * S, w_full = s_full + 16, q_full = w_full + 16, v_done = q_full + 8, s_free = v_done + 16;
     if (tid == 0) {
         s_stop = 0;
         for (int i = 0; i < S; ++i) { bar_init(full + 8 * i, kLoadThreads); bar_init(free_ + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(w_full + 8 * i, 128); bar_init(v_done + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(w_full + 8 * i, 128); bar_init(v_done + 8 * i, 1); bar_init(s_free + 8 * i, 128); }
         bar_init(q_full, kRowThreads);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -300,31 +308,38 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
         const unsigned ring = smem_of(s_ring);
         // (descriptors: an address in units of 16 bytes in the lowest bits, so that the operands of later steps and stages are sums)
         const uint64_t q_operand = operand(smem_of(s_q), 16, 1024), k_operand = operand(ring, 16, 1024), v_operand = operand(ring + kDims * kBlock, kBlock, 1024);
-        int stage = 0, stage_before = 0;
+        int stage = 0, taken = 0, taken_stage = 0, start = 0;      // ... of tile u; tiles whose values have been taken, and the next one's stage; the piece's first tile
         unsigned round = 0;
         bool first = true;                               // of its piece
-        int pieces = 0, since = 0, since_before = 0;     // tiles of the piece before tile u, before tile u - 1
-        auto take_values = [&](int v, bool starts) {
+        int pieces = 0;
+        auto take_values = [&]() {
+            const int v = taken;
             bar_wait(w_full + 8 * (v & 1), (v >> 1) & 1, &s_stop);
-            __syncwarp();
             after_sync();
             if (leads) {
                 if (s_apart[v & 1] == 0) {
-                    const unsigned to = tmem + (C::kTeams == 2 ? (v & 1) * C::kDim : 0), from = tmem + C::kLogits + (v & 1) * kTile;
-                    const uint64_t at = v_operand + (unsigned)(stage_before * (C::kStageBytes >> 4));
+                    const unsigned to = tmem + (C::kTeams == 2 ? (v & 1) * C::kDim : 0), from = tmem + C::kWeights + (v & 1) * C::kWeightsApart;
+                    const uint64_t at = v_operand + (unsigned)(taken_stage * (C::kStageBytes >> 4));
+                    const bool starts = v - start < C::kTeams;
 #pragma unroll
                     for (int k = 0; k < kTile / 16; ++k) multiply_tmem(to, from + 8 * k, at + (unsigned)(k * (16 * 128 >> 4)), values, !(starts && k == 0));
                 }
-                tell_when_done(free_ + 8 * stage_before);
+                tell_when_done(free_ + 8 * taken_stage);
                 tell_when_done(v_done + 8 * (v & 1));
             }
             __syncwarp();
+            ++taken;
+            taken_stage = taken_stage == S - 1 ? 0 : taken_stage + 1;
         };
         for (int u = 0; u < n; ++u) {
-            if (first) { bar_wait(q_full, pieces & 1, &s_stop); ++pieces; since = 0; }
+            if (first) {                                 // (the rows bring new queries once they have seen all of the piece before, and wait for its products)
+                while (taken < u) take_values();
+                bar_wait(q_full, pieces & 1, &s_stop);
+                ++pieces;
+                start = u;
+            }
             bar_wait(full + 8 * stage, round, &s_stop);
-            if (u >= 2) bar_wait(v_done + 8 * (u & 1), ((u >> 1) - 1) & 1, &s_stop);     // (the weights of tile u - 2 lie where its logits will)
-            __syncwarp();
+            if (u >= 2) bar_wait((C::kOwnWeights ? s_free : v_done) + 8 * (u & 1), ((u >> 1) - 1) & 1, &s_stop);
             after_sync();
             if (leads) {
                 const unsigned to = tmem + C::kLogits + (u & 1) * kTile;
@@ -336,14 +351,12 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                 tell_when_done(s_full + 8 * (u & 1));
             }
             __syncwarp();
-            if (u > 0) take_values(u - 1, since_before < C::kTeams);
-            since_before = since++;
-            stage_before = stage;
+            while (taken <= u - C::kBehind) take_values();
             if (++stage == S) { stage = 0; round ^= 1; }
             first = now.idx == now.q.tiles - 1;
             cursor_next(a, now, per);
         }
-        take_values(n - 1, since_before < C::kTeams);
+        while (taken < n) take_values();
         // (nothing is given back before the last product is done, stopped or not)
         for (unsigned i = 0; i < kWideSpins && !bar_try(v_done + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1); ++i) {}
         __syncwarp();
@@ -352,7 +365,6 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
         const int r = tid & (kWideRows - 1), team = tid >> 7;
         const unsigned mine = tmem + ((unsigned)((warp & 3) * 32) << 16), own = mine + (C::kTeams == 2 ? team * C::kDim : 0);
         const float scale = fabsf(a.scale_log2);
-        constexpr float kMost = 16384.0f;                // (fp16 ends at 65504)
         constexpr int kHalf = C::kDim / 2;               // columns that this thread joins
         bring_queries<kDims>(a, now, now.block * kWideRows, r, team, s_q);
         async_sees();
@@ -383,41 +395,24 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                         logits_load(x, logits);
                         logits_load(x + 16, logits + 32);
                     };
-                    // Weights relative to the reference, and their sum.  Only if that gets near what the types hold (or there is no reference yet) is the largest
-                    // logit looked for, and everything so far rescaled.
-                    auto weigh = [&]() -> float {
-                        const float ref = m == -INFINITY ? 0.0f : m;
-                        const float2 by = make_float2(scale, scale), off = make_float2(-ref, -ref);
-                        float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-                        if (whole) {
-#pragma unroll
-                            for (int j = 0; j < kTile / 2; ++j) {
-                                const float2 y = fma2(x[j], by, off);
-                                x[j] = make_float2(exp2_of(y.x), exp2_of(y.y));
-                                part[j & 1] = add2(part[j & 1], x[j]);
-                            }
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < kTile / 2; ++j) {
-                                const float2 y = fma2(x[j], by, off);
-                                x[j] = make_float2(sees(a, p, slot0 + 2 * j) ? exp2_of(y.x) : 0.0f, sees(a, p, slot0 + 2 * j + 1) ? exp2_of(y.y) : 0.0f);
-                                part[j & 1] = add2(part[j & 1], x[j]);
-                            }
-                        }
-                        const float2 sum = add2(part[0], part[1]);
-                        return sum.x + sum.y;
-                    };
                     load();
-                    float sum = first ? INFINITY : weigh();
-                    if (__any_sync(0xffffffffu, sum > kMost)) {
-                        if (!first) load();              // (the logits once more)
-                        float top = -INFINITY;
+                    if (C::kOwnWeights) { before_sync(); bar_arrive(s_free + 8 * b); }
+                    float2 best[2] = {make_float2(-INFINITY, -INFINITY), make_float2(-INFINITY, -INFINITY)};
+                    if (whole) {
+#pragma unroll
+                        for (int j = 0; j < kTile / 2; ++j) { best[j & 1].x = fmaxf(best[j & 1].x, x[j].x); best[j & 1].y = fmaxf(best[j & 1].y, x[j].y); }
+                    } else {
 #pragma unroll
                         for (int j = 0; j < kTile / 2; ++j) {
-                            if (whole || sees(a, p, slot0 + 2 * j)) top = fmaxf(top, x[j].x);
-                            if (whole || sees(a, p, slot0 + 2 * j + 1)) top = fmaxf(top, x[j].y);
+                            if (sees(a, p, slot0 + 2 * j)) best[j & 1].x = fmaxf(best[j & 1].x, x[j].x);
+                            if (sees(a, p, slot0 + 2 * j + 1)) best[j & 1].y = fmaxf(best[j & 1].y, x[j].y);
                         }
-                        top = fmaxf(top == -INFINITY ? top : top * scale, m);
+                    }
+                    float top = fmaxf(fmaxf(best[0].x, best[1].x), fmaxf(best[0].y, best[1].y));
+                    top = top == -INFINITY ? top : top * scale;
+                    // (rescaled only where a logit is more than kSlack above the reference)
+                    if (__any_sync(0xffffffffu, top > m + kSlack)) {
+                        top = fmaxf(top, m);
                         const float by = exp2_of(m - (top == -INFINITY ? 0.0f : top));
                         m = top; l *= by;
                         if (!first) {
@@ -433,9 +428,29 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                             }
                             tmem_stored();
                         }
-                        sum = weigh();
                     }
-                    l += sum;
+                    const float ref = m == -INFINITY ? 0.0f : m;
+                    const float2 by = make_float2(scale, scale), off = make_float2(-ref, -ref);
+                    float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+                    if (whole) {
+#pragma unroll
+                        for (int j = 0; j < kTile / 2; ++j) {
+                            const float2 y = fma2(x[j], by, off);
+                            x[j] = make_float2(exp2_of(y.x), exp2_of(y.y));
+                            part[j & 1] = add2(part[j & 1], x[j]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < kTile / 2; ++j) {
+                            const float2 y = fma2(x[j], by, off);
+                            x[j] = make_float2(sees(a, p, slot0 + 2 * j) ? exp2_of(y.x) : 0.0f, sees(a, p, slot0 + 2 * j + 1) ? exp2_of(y.y) : 0.0f);
+                            part[j & 1] = add2(part[j & 1], x[j]);
+                        }
+                    }
+                    part[0] = add2(part[0], part[1]);
+                    l += part[0].x + part[0].y;
+                } else if (C::kOwnWeights) {
+                    bar_arrive(s_free + 8 * b);
                 }
                 bool apart = false;
                 if (!whole && now.q.count > 1) {
@@ -480,11 +495,15 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                         tmem_stored();
                     }
                 }
+                if (C::kOwnWeights && u >= 2) {          // (the columns that W goes to: the product with W of tile u - 2 is done)
+                    bar_wait(v_done + 8 * b, ((u >> 1) - 1) & 1, &s_stop);
+                    after_sync();
+                }
                 if (!apart && busy) {
                     unsigned w[kTile / 2];
 #pragma unroll
                     for (int j = 0; j < kTile / 2; ++j) w[j] = Pair<T>::pack(x[j].x, x[j].y);
-                    tmem_store(w, logits);
+                    tmem_store(w, mine + C::kWeights + b * C::kWeightsApart);
                     tmem_stored();
                 }
                 if (r == 0) s_apart[b] = apart ? 1 : 0;
@@ -584,7 +603,7 @@ struct Book {
     static_assert(kStages >= 2, "two tiles");
 };
 template <typename T, int kDims>
-__global__ void __launch_bounds__(kWideThreads) k_cache_book_wide(const AttendArgs a)
+__global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendArgs a)
 {
     typedef Book<kDims> C;
     constexpr int S = C::kStages;
@@ -599,7 +618,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_book_wide(const AttendAr
     ull bad = 0;
     AttendArgs one = a;                                  // (slots are shared out by head, whatever the blocks of rows)
     one.row_blocks = 1;
-    const Tally tally = tally_of<kWideThreads, 2>(one, bad);
+    const Tally tally = tally_of<kBookThreads, 2>(one, bad);
     Share share;
     share.total = tally.total * heads; share.blocks = gridDim.x;
     const int64_t begin = begin_of(share, blockIdx.x);
@@ -610,7 +629,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_book_wide(const AttendAr
     const unsigned full = smem_of(s_bar), free_ = full + 8 * S, d_full = free_ + 8 * S, d_free = d_full + 16, q_full = d_free + 16;
     if (tid == 0) {
         s_stop = 0;
-        for (int i = 0; i < S; ++i) { bar_init(full + 8 * i, kLoadThreads); bar_init(free_ + 8 * i, 1); }
+        for (int i = 0; i < S; ++i) { bar_init(full + 8 * i, 128); bar_init(free_ + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { bar_init(d_full + 8 * i, 1); bar_init(d_free + 8 * i, 128); }
         bar_init(q_full, kRowThreads);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -628,46 +647,54 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_book_wide(const AttendAr
     if (warp >= 9) {
         const int part = warp - 9;
         constexpr unsigned kNone = 0xffffffffu;
-        int page[2], at_place[2], head = 0;              // (two slots a lane: one tile of the pair a warp)
+        const uint64_t policy = leaves_first();
+        int page = -1, at_place = 0, head = 0, stage = 0, landed = 0;
+        unsigned round = 1;
         auto look_up = [&]() {
-            head = now.head;
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int slot = first_slot(now.q, 2 * now.idx + part) + h * 32 + lane;
-                page[h] = -1; at_place[h] = 0;
-                if (slot >= now.q.length || !(a.window == 0 || slot < a.sinks || slot > now.q.length - now.q.count - a.window)) continue;
-                const int at = (int)(((ull)(unsigned)slot * a.c.page_mul) >> a.c.page_shift);
-                at_place[h] = slot - at * a.c.page_size;
-                page[h] = __ldg(&a.c.table[(int64_t)now.s * a.c.table_stride + at]);
-                if (page[h] == -1) page[h] = -2;
-            }
+            const int slot = first_slot(now.q, 2 * now.idx + part / 2) + (part & 1) * 32 + lane;
+            page = -1; head = now.head;
+            if (slot >= now.q.length || !(a.window == 0 || slot < a.sinks || slot > now.q.length - now.q.count - a.window)) return;
+            const int at = (int)(((ull)(unsigned)slot * a.c.page_mul) >> a.c.page_shift);
+            at_place = slot - at * a.c.page_size;
+            page = __ldg(&a.c.table[(int64_t)now.s * a.c.table_stride + at]);
+            if (page == -1) page = -2;
         };
-        auto row_found = [&](int h) -> unsigned {
-            if (page[h] == -1) return kNone;
-            if (page[h] < 0 || page[h] >= (int)a.c.num_pages) { bad |= G10_DEV_BAD_PAGE; return kNone; }
-            return cache_row(a.c, Spot{page[h], at_place[h]}, head);
+        auto row_found = [&]() -> unsigned {
+            if (page == -1) return kNone;
+            if (page < 0 || page >= (int)a.c.num_pages) { bad |= G10_DEV_BAD_PAGE; return kNone; }
+            return cache_row(a.c, Spot{page, at_place}, head);
         };
         look_up();
         for (int u = 0; u < n + C::kLag; ++u) {
             if (u >= C::kLag) {
                 asm volatile("cp.async.wait_group %0;" ::"n"(C::kLag - 1) : "memory");
                 async_sees();
-                bar_arrive(full + 8 * ((u - C::kLag) % S));
+                bar_arrive(full + 8 * landed);
+                landed = landed == S - 1 ? 0 : landed + 1;
             }
             if (u < n) {
-                const unsigned found[2] = {row_found(0), row_found(1)};
+                const unsigned mine = row_found();
                 if (u + 1 < n) { cursor_next<2>(one, now, heads); look_up(); }
-                bar_wait(free_ + 8 * (u % S), ((u / S) & 1) ^ 1, &s_stop);
-                const unsigned to = smem_of(s_ring) + (u % S) * C::kStageBytes;
+                bar_wait(free_ + 8 * stage, round, &s_stop);
+                const unsigned to = smem_of(s_ring) + stage * C::kStageBytes;
+                if (++stage == S) { stage = 0; round ^= 1; }
+                const bool all = __all_sync(0xffffffffu, mine != kNone) && a.c.head_dim == C::kDim;
+                if (all) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll 8
                     for (int i = 0; i < C::kUnits; ++i) {
                         const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
-                        const unsigned from = __shfl_sync(0xffffffffu, found[h], row);
-                        const bool there = from != kNone && unit * 8 < a.c.head_dim;
-                        copy16_or_zeros(to + swizzled(part * 64 + h * 32 + row, unit, 128 * 128), a.c.k + (there ? 16 * ((int64_t)from + unit) : 0), there);
+                        const int64_t x = 16 * (int64_t)__shfl_sync(0xffffffffu, mine, row);
+                        copy16(to + swizzled(part * 32 + row, unit, 128 * 128), a.c.k + 16 * unit + x, policy);
                     }
+                } else {
+#pragma unroll 2
+                    for (int i = 0; i < C::kUnits; ++i) {
+                        const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
+                        const unsigned from = __shfl_sync(0xffffffffu, mine, row);
+                        const bool there = from != kNone && unit * 8 < a.c.head_dim;
+                        copy16_or_zeros(to + swizzled(part * 32 + row, unit, 128 * 128), a.c.k + (there ? 16 * ((int64_t)from + unit) : 0), there);
+                    }
+                }
             }
             asm volatile("cp.async.commit_group;" ::: "memory");
         }
@@ -810,7 +837,7 @@ cudaError_t launch_wide(const AttendArgs &a, const AttendShape &z, cudaStream_t 
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
     cfg.gridDim = dim3((unsigned)grid, 4);               // (of the many elements of a piece each takes a part)
     if ((e = cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, (int)held, C::kDim, kWideRows)) != cudaSuccess || !a.books) return e;
-    cfg.blockDim = dim3(kWideThreads); cfg.dynamicSmemBytes = Book<kDims>::kSmem;
+    cfg.blockDim = dim3(kBookThreads); cfg.dynamicSmemBytes = Book<kDims>::kSmem;
     cfg.gridDim = dim3((unsigned)held);
     return cudaLaunchKernelEx(&cfg, book, a);
 }
