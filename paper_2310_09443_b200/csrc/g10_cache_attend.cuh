@@ -518,6 +518,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
                 l[j][h] += x[j][h] + x[j][h + 2];
             }
         // ---- O^T ----
+        __syncwarp();                                    // (a warp executes what follows as one)
         bool apart = false;
         if (!whole && now.q.count > 1) {
             // Slots that only some rows see: a weight of zero times an infinite or undefined value is not zero.

@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_plan(const EvictArgs a, int 
             x.over_before = (int)read_of((const unsigned *)&s_mine[2], (unsigned)lane); x.over_behind = (int)read_of((const unsigned *)&s_mine[3], (unsigned)lane);
             x.before = (int)read_of((const unsigned *)&s_mine[4], (unsigned)lane);
         }
-        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");      // (read: who waits for it, at the end, may leave)
+        cluster_arrive();                                // (read: who waits for it, at the end, may leave)
         int upto = x.even_before + x.even_behind, movers, holes;
         const int own = upto;
 #pragma unroll
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_plan(const EvictArgs a, int 
     }
     if (rank == 0 && tid == 0) a.counts[item] = all_movers;
     if (bad != 0) raise_status(a.c.status, bad);
-    if (blocks > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (blocks > 1) cluster_wait();
 }
 
 // A warp takes kMoves moves at a time: a lane each looks source and target up and moves score and position, then the rows go, 16 bytes a lane, all

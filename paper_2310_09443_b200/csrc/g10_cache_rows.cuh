@@ -3,7 +3,7 @@
 //
 // The mathematics and the way the work is shared out are those of g10_cache_attend.cuh.  With R rows a tile of 64 slots takes 4 * 64 * R * head_dim
 // operations for 256 * head_dim bytes: up to some hundred rows memory still is the bound, but the older matrix instructions, fed from registers,
-// cannot keep up (32 rows a block, the cache read twice for 64 rows: CASE_OLD us for 6 sequences of 9001 slots and 16 new tokens of 4 heads).  So up to
+// cannot keep up (32 rows a block, the cache read twice for 64 rows: 127 us for 6 sequences of 9001 slots and 16 new tokens of 4 heads, 86 this way).  So up to
 // 128 rows of an item form one operand, [128 rows x dims], and
 //   S [128 x 64] = Q K^T,    W = exp2(S - ref),    O [128 x dims] += W V
 // are tcgen05 products with S, W and O in tensor memory.  A row is a lane of tensor memory and belongs to one thread, which sees all of its 64 logits:
@@ -171,7 +171,7 @@ struct Wide {
     static constexpr int kWeights = kLogits + (kOwnWeights ? 2 * kTile : 0), kWeightsApart = kOwnWeights ? kTile / 2 : kTile;
     static constexpr int kUsed = kLogits + 2 * kTile + (kOwnWeights ? kTile : 0);
     static constexpr unsigned kColumns = kUsed <= 256 ? 256 : 512;
-    static constexpr int kLag = kStages > 3 ? 3 : kStages - 1;       // tiles on their way before the first of them is waited for
+    static constexpr int kLag = kStages > 2 ? 2 : 1;     // tiles on their way before the first of them is waited for
     // Tiles whose product with the queries is issued before the product of a tile with its values.  (A tile is told full kLag tiles after its
     // copies were issued, which wait for a stage: kLag + kBehind stages at least, or the two wait for each other.)
     static constexpr int kBehind = kStages - kLag >= 2 && kTeams == 2 ? 2 : 1;
@@ -599,7 +599,7 @@ struct Book {
     static constexpr int kFit = (226 * 1024 - 4096 - kQBytes) / kStageBytes, kStages = kFit > 6 ? 6 : kFit;
     static constexpr int kSmem = 1024 + kQBytes + kStages * kStageBytes;
     static constexpr unsigned kColumns = 256;            // of tensor memory: S^T twice
-    static constexpr int kLag = kStages > 3 ? 3 : kStages - 1;       // tiles on their way before the first of them is waited for
+    static constexpr int kLag = kStages > 2 ? 2 : 1;     // tiles on their way before the first of them is waited for
     static_assert(kStages >= 2, "two tiles");
 };
 template <typename T, int kDims>
@@ -782,6 +782,12 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
                                 const float2 y = fma2(x[i], by, make_float2(off.x, off.y)), z = fma2(x[i + 1], by, make_float2(off.z, off.w));
                                 part[0] = add2(part[0], make_float2(exp2_of(y.x), exp2_of(y.y)));
                                 part[1] = add2(part[1], make_float2(exp2_of(z.x), exp2_of(z.y)));
+                            }
+                        } else if (whole) {
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) {
+                                const float2 y = fma2(x[i], by, *(const float2 *)&s_off[c + 2 * i]);
+                                part[i & 1] = add2(part[i & 1], make_float2(c + 2 * i < rows ? exp2_of(y.x) : 0.0f, c + 2 * i + 1 < rows ? exp2_of(y.y) : 0.0f));
                             }
                         } else {
 #pragma unroll
