@@ -672,26 +672,34 @@ __global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, i
     }
 }
 
-// The pieces of blocks b0 .. b1 joined by `lanes` neighbouring threads (a power of two up to 32); every one has the result.
-template <bool kSums>
+// The pieces of blocks b0 .. b1 joined by `lanes` neighbouring threads (a power of two up to 32), each with four pieces on their way at a time; every
+// one has the result.
+constexpr int kPiecesEach = 4;
 __device__ __forceinline__ Part part_join(const AttendArgs &a, int64_t item, int b0, int b1, int block_rows, int r, int padded_dim, int d, int lanes)
 {
     const int lane = threadIdx.x & (lanes - 1);
     Part p;
     p.top = -INFINITY; p.sum = 0.0f; p.o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 4
-    for (int b = b0 + lane; b <= b1; b += lanes) {
-        const float2 ml = __ldcg(&a.ml[r * a.pieces + item + b]);
-        float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (kSums) o = __ldcg((const float4 *)(a.part + ((item + b) * block_rows + r) * padded_dim + d));
-        part_add(p, ml.x, ml.y, o);
+#pragma unroll 1
+    for (int b = b0 + lane; b <= b1; b += kPiecesEach * lanes) {
+        float2 ml[kPiecesEach];
+        float4 o[kPiecesEach];
+#pragma unroll
+        for (int i = 0; i < kPiecesEach; ++i) {
+            const int64_t piece = item + b + i * lanes;
+            ml[i] = make_float2(-INFINITY, 0.0f); o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (b + i * lanes <= b1) {
+                ml[i] = __ldcg(&a.ml[r * a.pieces + piece]);
+                o[i] = __ldcg((const float4 *)(a.part + (piece * block_rows + r) * padded_dim + d));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kPiecesEach; ++i) part_add(p, ml[i].x, ml[i].y, o[i]);
     }
     for (int o = lanes / 2; o > 0; o >>= 1) {
         const float top = __shfl_xor_sync(0xffffffffu, p.top, o), sum = __shfl_xor_sync(0xffffffffu, p.sum, o);
-        float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        if (kSums)
-            x = make_float4(__shfl_xor_sync(0xffffffffu, p.o.x, o), __shfl_xor_sync(0xffffffffu, p.o.y, o), __shfl_xor_sync(0xffffffffu, p.o.z, o),
-                            __shfl_xor_sync(0xffffffffu, p.o.w, o));
+        const float4 x = make_float4(__shfl_xor_sync(0xffffffffu, p.o.x, o), __shfl_xor_sync(0xffffffffu, p.o.y, o), __shfl_xor_sync(0xffffffffu, p.o.z, o),
+                                     __shfl_xor_sync(0xffffffffu, p.o.w, o));
         part_add(p, top, sum, x);
     }
     return p;
@@ -699,7 +707,7 @@ __device__ __forceinline__ Part part_join(const AttendArgs &a, int64_t item, int
 __device__ __forceinline__ int lanes_for(int pieces)
 {
     int n = 1;
-    while (n < pieces && n < 32) n *= 2;
+    while (n * kPiecesEach < pieces && n < 32) n *= 2;
     return n;
 }
 
@@ -754,7 +762,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
         const int e0 = all * nth / parts, e1 = all * (nth + 1) / parts;
         for (int e = e0 + warp % kHalf * teams; e < e1; e += kHalf * teams) {                    // (all lanes take part in the shuffles)
             const int mine = min(e + lane / lanes, e1 - 1), r = mine / quads, d = mine % quads * 4, row = first_row + r;
-            const Part p = part_join<true>(a, w.item, w.b0, w.b1, block_rows, r, padded_dim, d, lanes);
+            const Part p = part_join(a, w.item, w.b0, w.b1, block_rows, r, padded_dim, d, lanes);
             if (e + lane / lanes < e1 && (lane & (lanes - 1)) == 0) {
                 const int64_t at = ((int64_t)s * a.new_tokens + row / a.group) * a.q_heads + head * a.group + row % a.group;
                 const float inv = 1.0f / p.sum;

@@ -246,18 +246,19 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
         int stage = 0, landed = 0;
         unsigned round = 1;
         // (the page is loaded a tile ahead, and looked at when its turn comes)
-        int page = -1, at_place = 0, head = 0;
+        int page = 0, at_place = 0, head = 0;
+        bool there = false;                              // (a slot that somebody sees)
         auto look_up = [&]() {
             const int slot = first_slot(now.q, now.idx) + part * 32 + lane;
-            page = -1; head = now.head;
+            there = false; head = now.head;
             if (slot >= now.q.length || !(a.window == 0 || slot < a.sinks || slot > now.q.length - now.q.count - a.window)) return;
             const int at = (int)(((ull)(unsigned)slot * a.c.page_mul) >> a.c.page_shift);
             at_place = slot - at * a.c.page_size;
             page = __ldg(&a.c.table[(int64_t)now.s * a.c.table_stride + at]);
-            if (page == -1) page = -2;                   // (an entry that names no page, not a slot that nobody sees)
+            there = true;
         };
         auto row_found = [&]() -> unsigned {
-            if (page == -1) return kNone;
+            if (!there) return kNone;
             if (page < 0 || page >= (int)a.c.num_pages) { bad |= G10_DEV_BAD_PAGE; return kNone; }
             return cache_row(a.c, Spot{page, at_place}, head);
         };
@@ -290,10 +291,10 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                     for (int i = 0; i < C::kUnits; ++i) {
                         const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
                         const unsigned from = __shfl_sync(0xffffffffu, mine, row), at = swizzled(part * 32 + row, unit, kBlock);
-                        const bool there = from != kNone && unit * 8 < a.c.head_dim;
-                        const int64_t x = there ? 16 * ((int64_t)from + unit) : 0;
-                        copy16_or_zeros(to + at, a.c.k + x, there);
-                        copy16_or_zeros(to + kDims * kBlock + at, a.c.v + x, there);
+                        const bool real = from != kNone && unit * 8 < a.c.head_dim;
+                        const int64_t x = real ? 16 * ((int64_t)from + unit) : 0;
+                        copy16_or_zeros(to + at, a.c.k + x, real);
+                        copy16_or_zeros(to + kDims * kBlock + at, a.c.v + x, real);
                     }
                 }
             }
@@ -634,6 +635,11 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
         bar_init(q_full, kRowThreads);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    __syncthreads();
+    Cursor now;
+    cursor_at<2>(one, now, s_place, begin);
+    // (in all warps: none spends its limited waits on the kernels before, and none holds tensor memory that they may wait for)
+    asm volatile("griddepcontrol.wait;" ::: "memory");
     if (warp == 8) tmem_take(&s_tmem, C::kColumns);
     before_sync();
     __syncthreads();
@@ -641,26 +647,24 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
     const unsigned tmem = s_tmem;
     char *const s_q = (char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     char *const s_ring = s_q + C::kQBytes;
-    Cursor now;
-    cursor_at<2>(one, now, s_place, begin);
-    asm volatile("griddepcontrol.wait;" ::: "memory");       // (in all warps: none spends its limited waits on the kernels before)
     if (warp >= 9) {
         const int part = warp - 9;
         constexpr unsigned kNone = 0xffffffffu;
         const uint64_t policy = leaves_first();
-        int page = -1, at_place = 0, head = 0, stage = 0, landed = 0;
+        int page = 0, at_place = 0, head = 0, stage = 0, landed = 0;
+        bool there = false;
         unsigned round = 1;
         auto look_up = [&]() {
             const int slot = first_slot(now.q, 2 * now.idx + part / 2) + (part & 1) * 32 + lane;
-            page = -1; head = now.head;
+            there = false; head = now.head;
             if (slot >= now.q.length || !(a.window == 0 || slot < a.sinks || slot > now.q.length - now.q.count - a.window)) return;
             const int at = (int)(((ull)(unsigned)slot * a.c.page_mul) >> a.c.page_shift);
             at_place = slot - at * a.c.page_size;
             page = __ldg(&a.c.table[(int64_t)now.s * a.c.table_stride + at]);
-            if (page == -1) page = -2;
+            there = true;
         };
         auto row_found = [&]() -> unsigned {
-            if (page == -1) return kNone;
+            if (!there) return kNone;
             if (page < 0 || page >= (int)a.c.num_pages) { bad |= G10_DEV_BAD_PAGE; return kNone; }
             return cache_row(a.c, Spot{page, at_place}, head);
         };
@@ -691,8 +695,8 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
                     for (int i = 0; i < C::kUnits; ++i) {
                         const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
                         const unsigned from = __shfl_sync(0xffffffffu, mine, row);
-                        const bool there = from != kNone && unit * 8 < a.c.head_dim;
-                        copy16_or_zeros(to + swizzled(part * 32 + row, unit, 128 * 128), a.c.k + (there ? 16 * ((int64_t)from + unit) : 0), there);
+                        const bool real = from != kNone && unit * 8 < a.c.head_dim;
+                        copy16_or_zeros(to + swizzled(part * 32 + row, unit, 128 * 128), a.c.k + (real ? 16 * ((int64_t)from + unit) : 0), real);
                     }
                 }
             }
