@@ -732,7 +732,6 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
     __shared__ Pieces s_pieces[2];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = a.c.kv_heads * a.row_blocks;
     ull ignored = 0;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const Tally tally = tally_of<kJoinThreads>(a, ignored);
     const Share share = share_of(tally.total, per, gridDim.x, held_blocks);        // the first kernel's
     const int b = blockIdx.x;
@@ -748,6 +747,8 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
     }
     __syncthreads();
     asm volatile("griddepcontrol.wait;" ::: "memory");
+    // (only now: a kernel behind this one finds all that the first has written)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
 
     // ---- (1): the items of the share's first and last tile (those between are whole), half of the warps each ----
     constexpr int kHalf = kJoinThreads / 64;
@@ -791,8 +792,12 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
 // slot's rows lie side by side: as many neighbouring lanes as it has groups of four rows read them and add their weights up; a lane has the same
 // rows of every slot, and so its part of the lse in registers.  exp2(logit - lse) over all rows in order, and one addition to the score.
 template <int kTeam>
-__device__ __forceinline__ void book_tile(const AttendArgs &a, const TileNote &note, int64_t tile, int block_rows, int pitch, ull &bad)
+__device__ __forceinline__ void book_tile(const AttendArgs &a, const TileNote &note, int64_t tile, int block_rows, int pitch, bool &waited, ull &bad)
 {
+    auto joined = [&]() {                                // (what the second kernel writes: each lse)
+        if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
+        waited = true;
+    };
     const int lane = threadIdx.x & 31, mate = lane & (kTeam - 1);
     const int per = a.c.kv_heads * a.row_blocks;
     const int64_t item = (int64_t)note.s * per + note.head * a.row_blocks;
@@ -813,6 +818,9 @@ __device__ __forceinline__ void book_tile(const AttendArgs &a, const TileNote &n
             const float *const lse = a.sums + (item + b) * block_rows + r;
             if (pitch >= 4) {
                 float4 z = make_float4(INFINITY, INFINITY, INFINITY, INFINITY), x[kAhead];       // (no such row: weight 0)
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) x[i] = r < pitch ? __ldcg((const float4 *)(from + i * (32 / kTeam) * pitch + r)) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+                joined();
                 if (r < pitch) {
                     z = __ldcg((const float4 *)lse);
                     if (r + 1 >= rows) z.y = INFINITY;
@@ -821,14 +829,16 @@ __device__ __forceinline__ void book_tile(const AttendArgs &a, const TileNote &n
                     if (r >= rows) z.x = INFINITY;
                 }
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) x[i] = r < pitch ? __ldcg((const float4 *)(from + i * (32 / kTeam) * pitch + r)) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-#pragma unroll
                 for (int i = 0; i < kAhead; ++i) w[i] += (exp2_of(x[i].x - z.x) + exp2_of(x[i].y - z.y)) + (exp2_of(x[i].z - z.z) + exp2_of(x[i].w - z.w));
             } else {
                 for (int q = 0; q < pitch; ++q) {
+                    float x[kAhead];
+#pragma unroll
+                    for (int i = 0; i < kAhead; ++i) x[i] = __ldcg(from + i * 32 * pitch + q);
+                    joined();
                     const float z = __ldcg(lse + q);
 #pragma unroll
-                    for (int i = 0; i < kAhead; ++i) w[i] += exp2_of(__ldcg(from + i * 32 * pitch + q) - z);
+                    for (int i = 0; i < kAhead; ++i) w[i] += exp2_of(x[i] - z);
                 }
             }
         }
@@ -842,17 +852,26 @@ __device__ __forceinline__ void book_tile(const AttendArgs &a, const TileNote &n
     }
 }
 template <int kTeam>
-__global__ void __launch_bounds__(kJoinThreads) k_cache_book(const AttendArgs a, int block_rows)
+__global__ void __launch_bounds__(kJoinThreads) k_cache_book(const AttendArgs a, int block_rows, bool behind_join)
 {
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // Behind the second kernel, which lets this one begin once the first is done: its notes and logits may be read at once.
+    bool waited = !behind_join;
+    if (waited) asm volatile("griddepcontrol.wait;" ::: "memory");
     const int pitch = logit_rows(min(block_rows, a.rows));
-    const int64_t total = __ldcg(a.total);
+    const int64_t total = __ldcg(a.total), step = (int64_t)gridDim.x * (kJoinThreads / 32);
     ull bad = 0;
-    for (int64_t u = (int64_t)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5); u < total; u += (int64_t)gridDim.x * (kJoinThreads / 32)) {
-        const int4 x = __ldcg((const int4 *)&a.notes[u]);
-        const TileNote note{x.x, x.y, x.z, x.w, __ldcg(&a.notes[u].tiles), {0, 0, 0}};
-        if (note.tiles > 0) book_tile<kTeam>(a, note, u, block_rows, pitch, bad);
+    int64_t u = (int64_t)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
+    int4 x = make_int4(0, 0, 0, 0);
+    int tiles = 0;
+    if (u < total) { x = __ldcg((const int4 *)&a.notes[u]); tiles = __ldcg(&a.notes[u].tiles); }
+    while (u < total) {
+        const TileNote note{x.x, x.y, x.z, x.w, tiles, {0, 0, 0}};
+        const int64_t now = u;
+        u += step;
+        if (u < total) { x = __ldcg((const int4 *)&a.notes[u]); tiles = __ldcg(&a.notes[u].tiles); }
+        if (note.tiles > 0) book_tile<kTeam>(a, note, now, block_rows, pitch, waited, bad);
     }
+    if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");      // (this kernel's end says that the second has ended)
     if (bad != 0) raise_status(a.c.status, bad);
 }
 
@@ -909,7 +928,7 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     cfg.gridDim = dim3((unsigned)(blocks < most ? blocks : most));
     const int pitch = logit_rows(C::kRows < a.rows ? C::kRows : a.rows);
     const auto book = pitch <= 4 ? k_cache_book<1> : pitch <= 8 ? k_cache_book<2> : pitch <= 16 ? k_cache_book<4> : k_cache_book<8>;
-    return cudaLaunchKernelEx(&cfg, book, a, C::kRows);
+    return cudaLaunchKernelEx(&cfg, book, a, C::kRows, cluster == 0);
 }
 // Tiles in the ring: as many as let two blocks share an SM, or, for wide heads, fill it for one.
 constexpr int stages_of(int steps, int cols)

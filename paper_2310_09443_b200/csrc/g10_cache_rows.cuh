@@ -624,7 +624,10 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
     share.total = tally.total * heads; share.blocks = gridDim.x;
     const int64_t begin = begin_of(share, blockIdx.x);
     const int n = (int)(begin_of(share, blockIdx.x + 1) - begin);
-    if (n == 0) return;
+    if (n == 0) {                                        // (this kernel's end says that those before have ended)
+        asm volatile("griddepcontrol.wait;" ::: "memory");
+        return;
+    }
     bad = 0;
     place_of<2>(one, tally, begin, heads, &s_place);
     const unsigned full = smem_of(s_bar), free_ = full + 8 * S, d_full = free_ + 8 * S, d_free = d_full + 16, q_full = d_free + 16;
@@ -635,11 +638,7 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
         bar_init(q_full, kRowThreads);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    __syncthreads();
-    Cursor now;
-    cursor_at<2>(one, now, s_place, begin);
-    // (in all warps: none spends its limited waits on the kernels before, and none holds tensor memory that they may wait for)
-    asm volatile("griddepcontrol.wait;" ::: "memory");
+    // (the kernel before lets this one begin once it has nothing but its last, short part left: tensor memory may be taken, and limited waits begun)
     if (warp == 8) tmem_take(&s_tmem, C::kColumns);
     before_sync();
     __syncthreads();
@@ -647,6 +646,8 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
     const unsigned tmem = s_tmem;
     char *const s_q = (char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     char *const s_ring = s_q + C::kQBytes;
+    Cursor now;
+    cursor_at<2>(one, now, s_place, begin);
     if (warp >= 9) {
         const int part = warp - 9;
         constexpr unsigned kNone = 0xffffffffu;
@@ -743,6 +744,7 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
         const int r = tid & 127, team = tid >> 7;
         const unsigned mine = tmem + ((unsigned)((warp & 3) * 32) << 16);
         const float scale = fabsf(a.scale_log2);
+        asm volatile("griddepcontrol.wait;" ::: "memory");       // (for each lse; the keys are on their way meanwhile)
         auto bring = [&](int b) {                        // queries, lse and places of block b's rows
             const int row = b * kWideRows + r, t = row / a.group;
             bring_queries<kDims>(a, now, b * kWideRows, r, team, s_q);
