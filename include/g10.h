@@ -404,8 +404,9 @@ int32_t g10_pressure_timeline_static(const g10_trace *trace, g10_timeline_out *o
    Errors that depend on the data are OR-ed into *status (one word, never cleared by the library: a program clears it and
    looks at it when it likes): G10_DEV_BAD_LENGTH (a length outside 0 .. max_pages * page_size or a count outside 0 .. new_tokens; the
    call goes on with the nearest valid value), G10_DEV_BAD_PAGE (a page outside 0 .. num_pages - 1: a slot there is not
-   written and read as zeros), G10_DEV_BAD_POSITION (a position outside the rotation tables: not rotated), G10_DEV_BAD_MOVE.  Every access stays in
-   bounds.
+   written and read as zeros), G10_DEV_BAD_POSITION (a position outside the rotation tables: not rotated), G10_DEV_BAD_MOVE, and
+   G10_DEV_TIMEOUT (attend for more than 16 rows a head: a wait inside a thread block ran out; that call's results are void).  Every access
+   stays in bounds.  Arrays that a call writes overlap none that it reads, except where its description says that it moves them.
    A page may be shared by sequences that only attend; append, evict and booked weights want a page to belong to one sequence
    and to stand once in its table (booked weights of a shared page are added up, in any order; the other two leave it unspecified). */
 #define G10_BF16 0
@@ -471,9 +472,9 @@ int32_t g10_cache_append(const g10_cache *cache, const g10_cache_tokens *tokens,
    empty sequence) gives out = 0, lse = -inf.  What stands in slots that a row does not see has no influence on it, not even
    as infinity or NaN.  With add_scores, scores of each slot grows by the sum of its w_j over the queries and the heads of its group.
    Products take their operands as they are stored and are added up in 32 bits; the weights are rounded to the cache's type before they
-   multiply the values (relative 2^-9 / 2^-12 each), the booked ones are not.  The result does not depend on the timing of the
+   multiply the values (relative 2^-8 / 2^-11 each), the booked ones are not.  The result does not depend on the timing of the
    blocks; the way the work is split, and with it the rounding, depends on all lengths of the batch.
-   Limit: new_tokens * q_heads / kv_heads <= 1024. */
+   Limit: new_tokens * q_heads / kv_heads <= 1024; scale / log 2 is finite. */
 typedef struct g10_cache_queries {
     int32_t new_tokens, q_heads;
     const void *q;                  /* strides as above                                             */

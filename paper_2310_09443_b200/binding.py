@@ -556,7 +556,8 @@ class CacheBuffers:
     k, v: bf16 or fp16 [pages, page_size, kv_heads, head_dim], any strides (the same for both, multiples of 8, the last one 1): a view of
     [pages, kv_heads, page_size, head_dim] will do.  page_table: int32 [seqs, columns]; lengths, seen: int32 [seqs] (shared by all layers; no
     call changes them).  scores: float32, positions: int32, both [pages, kv_heads, page_size].  status: int64 [1], made here unless given:
-    data-dependent errors are OR-ed into it.  k and v may be None for a cache that is only planned on (then page_size and kv_heads say
+    data-dependent errors are OR-ed into it.  The calls run on `stream`, or the current stream of the cache's device; what they allocate belongs to
+    the stream that they run on.  No gradients flow through them.  k and v may be None for a cache that is only planned on (then page_size and kv_heads say
     the sizes)."""
 
     def __init__(self, k, v, page_table, lengths, seen=None, scores=None, positions=None, status=None, page_size=None, kv_heads=None):
@@ -608,6 +609,8 @@ _CACHE_TYPES = {torch.bfloat16: 0, torch.float16: 1}
 
 def _cache_call(call, cache, args, stream):
     """call(cache, *args, stream) with the cache's device current."""
+    if stream is not None and stream.device_index != cache.index:
+        raise G10Error("stream has to belong to %s" % cache.device)
     if torch._C._cuda_getDevice() == cache.index:
         rc = call(cache.ref, *args, torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream)
     else:
@@ -615,6 +618,14 @@ def _cache_call(call, cache, args, stream):
             rc = call(cache.ref, *args, torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream)
     if rc != 0:
         _check(rc)
+
+
+def _cache_empty(cache, shape, dtype, stream):
+    """Memory for a call on `stream`: from that stream's own pool, since that of the current stream may still be in use there."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=cache.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=cache.device)
 
 
 def g10_cache_append(cache: CacheBuffers, k, v, q=None, q_weight=None, k_weight=None, eps=1e-6, cos=None, sin=None, interleaved=False, counts=None,
@@ -632,7 +643,7 @@ def g10_cache_append(cache: CacheBuffers, k, v, q=None, q_weight=None, k_weight=
         q_shape, qs = _rows("q", q, cache)
         heads = q_shape[2]
         if q_out is None:
-            q_out = torch.empty(q_shape, dtype=q.dtype, device=q.device)
+            q_out = _cache_empty(cache, q_shape, q.dtype, stream)
         else:
             _typed("q_out", q_out, cache.dtype, q_shape, dev)
     if v_shape[1] != new or (heads and q_shape[1] != new):
@@ -672,7 +683,7 @@ def g10_cache_attend(cache: CacheBuffers, q, scale=None, window=0, sinks=0, coun
     shape, qs = _rows("q", q, cache)
     dev, new, heads = cache.index, shape[1], shape[2]
     if out is None:
-        out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        out = _cache_empty(cache, shape, q.dtype, stream)
     else:
         _typed("out", out, cache.dtype, shape, dev)
     if lse is not None:
@@ -680,9 +691,7 @@ def g10_cache_attend(cache: CacheBuffers, q, scale=None, window=0, sinks=0, coun
     if counts is not None:
         _typed("counts", counts, torch.int32, (cache.num_seqs,), dev)
     if ws is None:
-        ws = torch.empty(max(256, g10_cache_workspace_bytes(cache, new, heads, window, sinks, add_scores)), dtype=torch.uint8, device=cache.device)
-        if stream is not None:
-            ws.record_stream(stream)
+        ws = _cache_empty(cache, max(256, g10_cache_workspace_bytes(cache, new, heads, window, sinks, add_scores)), torch.uint8, stream)
     elif ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
         raise G10Error("ws has to be contiguous uint8 on %s" % cache.device)
     u = _CacheQueries(new, heads, q.data_ptr(), qs[0], qs[1], qs[2], _ptr(counts), out.data_ptr(), _ptr(lse), cache.head_dim ** -0.5 if scale is None else scale,
@@ -704,13 +713,12 @@ def g10_cache_plan_evictions(cache: CacheBuffers, budget, sinks=0, recent=0, mov
     """Plans which `budget` slots of each (sequence, key-value head) stay: positions below `sinks` and the last `recent` first, then the largest
     scores.  Returns moves int32 [seqs, kv_heads, budget, 2] (source, target slot; valid up to the count), counts int32 [seqs, kv_heads] and
     new_lengths int32 [seqs]; changes nothing else."""
-    dev = cache.device
     if moves is None:
-        moves = torch.empty((cache.num_seqs, cache.kv_heads, max(budget, 0), 2), dtype=torch.int32, device=dev)
+        moves = _cache_empty(cache, (cache.num_seqs, cache.kv_heads, max(budget, 0), 2), torch.int32, stream)
     if counts is None:
-        counts = torch.empty((cache.num_seqs, cache.kv_heads), dtype=torch.int32, device=dev)
+        counts = _cache_empty(cache, (cache.num_seqs, cache.kv_heads), torch.int32, stream)
     if new_lengths is None:
-        new_lengths = torch.empty(cache.num_seqs, dtype=torch.int32, device=dev)
+        new_lengths = _cache_empty(cache, (cache.num_seqs,), torch.int32, stream)
     p = _cache_plan(cache, budget, sinks, recent, moves, counts, new_lengths)
     _cache_call(load_library().g10_cache_plan_evictions, cache, (p,), stream)
     return SimpleNamespace(moves=moves, counts=counts, new_lengths=new_lengths)

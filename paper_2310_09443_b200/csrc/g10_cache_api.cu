@@ -8,6 +8,7 @@ namespace g10 {
 namespace {
 
 constexpr int64_t kCacheLimit = 0x7fffffff - 64;
+constexpr float kLog2E = 1.4426950408889634f;
 
 bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
 // (strides of a dimension of one entry are never used, but are asked for all the same: they are the caller's arithmetic)
@@ -126,14 +127,14 @@ int32_t g10_cache_attend(const g10_cache *cache, const g10_cache_queries *u, voi
     if (!u) return G10_ERR_ARG;
     rc = check_heads(a.c, u->new_tokens, u->q_heads, u->window, u->sinks);
     if (rc != G10_OK) return rc;
-    if ((u->window > 0 && cache->positions) || (u->add_scores && !cache->scores) || !std::isfinite(u->scale)) return G10_ERR_ARG;
+    if ((u->window > 0 && cache->positions) || (u->add_scores && !cache->scores) || !std::isfinite(u->scale * kLog2E)) return G10_ERR_ARG;
     if (a.c.num_seqs == 0) return G10_OK;
     if (!u->q || !u->out || !aligned16(u->q) || !aligned16(u->out) || !row_stride(u->q_seq_stride) || !row_stride(u->q_token_stride) ||
         !row_stride(u->q_head_stride))
         return G10_ERR_ARG;
     a.q = (const char *)u->q; a.q_seq = u->q_seq_stride; a.q_token = u->q_token_stride; a.q_head = u->q_head_stride;
     a.counts = u->counts; a.out = (char *)u->out; a.lse = u->lse;
-    a.scale_log2 = u->scale * 1.4426950408889634f;
+    a.scale_log2 = u->scale * kLog2E;
     a.new_tokens = u->new_tokens; a.q_heads = u->q_heads; a.group = u->q_heads / a.c.kv_heads; a.rows = u->new_tokens * a.group;
     a.window = u->window; a.sinks = u->window > 0 ? u->sinks : 0;
     const AttendShape z = attend_shape(a.c, a.rows, a.new_tokens, a.window, a.sinks);

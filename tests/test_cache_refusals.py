@@ -70,7 +70,7 @@ def test_rows(lib, change):
 @pytest.mark.parametrize("change,code", [(dict(new_tokens=0), -1), (dict(q_heads=0), -1), (dict(q_heads=6), -1), (dict(new_tokens=513), -2), (dict(q=None), -1),
                                          (dict(out=None), -1), (dict(q=FAKE + 4), -1), (dict(out=FAKE + 4), -1), (dict(q_seq_stride=4), -1),
                                          (dict(q_token_stride=4), -1), (dict(q_head_stride=4), -1), (dict(window=-1), -1), (dict(sinks=-1), -1),
-                                         (dict(scale=float("inf")), -1), (dict(scale=float("nan")), -1)])
+                                         (dict(scale=float("inf")), -1), (dict(scale=float("nan")), -1), (dict(scale=3e38), -1), (dict(scale=-3e38), -1)])
 def test_queries(lib, change, code):
     assert lib.g10_cache_attend(cache(), queries(**change), FAKE, 1 << 40, None) == code
 

@@ -525,6 +525,135 @@ def test_graphs_streams_and_workspaces(g10):
     assert same(cache.k, c.k) and same(cache.v, c.v) and same(cache.scores, c.scores)
 
 
+@pytest.mark.parametrize("new,group", [(1, 4), (3, 4), (8, 7)])
+def test_captured_booking(g10, new, group):
+    """A captured call that books, replayed after the lengths have moved, three times in a row with nothing between."""
+    c = O.make_cache([700, 90, 1500, 64], 2, 128, 16, torch.bfloat16, 21)
+    q = queries(c, new, group, 3)
+    cache, dq = O.upload(g10, c), q.to(DEV)
+    out = torch.empty_like(dq)
+    ws = torch.empty(g10.g10_cache_workspace_bytes(cache, new, 2 * group, add_scores=True), dtype=torch.uint8, device=DEV)
+    g10.g10_cache_attend(cache, dq, out=out, ws=ws, add_scores=True)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        g10.g10_cache_attend(cache, dq, out=out, ws=ws, add_scores=True)
+    c.lengths = c.lengths - 40
+    cache.lengths.copy_(c.lengths)
+    cache.scores.zero_()
+    for _ in range(3):
+        g.replay()
+    torch.cuda.synchronize()
+    assert int(cache.status.item()) == 0
+    r = O.attend(c, q, 128 ** -0.5)
+    bound, _, rel = O.attend_bounds(c, r)
+    assert ((out.cpu().double() - r.out).abs() <= bound).all()
+    got = cache.scores.cpu().double()
+    for (s, h), w in r.booked.items():
+        pg, pl = O.places(c, s, len(w))
+        # (three additions to a score, each rounded)
+        assert ((got[pg, h, pl] - 3 * w).abs() <= 3 * w * (float(rel[s].max()) * 1.01 + 2.0 ** -23) + 1e-30).all()
+
+
+def test_what_a_call_allocates_on_another_stream_is_its_own(g10):
+    """Memory that the current stream has given back may still have work ahead of it there: a call on another stream does not get it."""
+    c = O.make_cache([300, 90], 2, 64, 16, torch.bfloat16, 5)
+    q = queries(c, 1, 4, 5)
+    cache, dq = O.upload(g10, c), q.to(DEV)
+    side = torch.cuda.Stream()
+    r = O.attend(c, q, 64 ** -0.5)
+    bound = O.attend_bounds(c, r)[0]
+    size = g10.g10_cache_workspace_bytes(cache, 1, 8)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(20_000_000)
+    for given in (dq.numel() * 2, size):
+        x = torch.empty(given, dtype=torch.uint8, device=DEV)
+        x.fill_(255)
+        del x
+    out = g10.g10_cache_attend(cache, dq, stream=side)
+    torch.cuda.synchronize()
+    assert ((out.cpu().double() - r.out).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("new", [1, 9])
+def test_largest_windows(g10, new):
+    most = 2 ** 31 - 1
+    c = O.make_cache([300, 0, 65], 2, 64, 16, torch.float16, 8)
+    q = queries(c, new, 4, 2)
+    for window, sinks in ((most, 0), (most, most), (1, most), (70, most)):
+        check_attend(g10, c, q, window=window, sinks=sinks, book=True)
+
+
+def test_calls_of_two_threads(g10):
+    import threading
+    c = O.make_cache([900, 33, 400], 2, 128, 16, torch.bfloat16, 31)
+    cases = [(1, 4), (8, 6)]
+    wrong = []
+
+    def work(new, group):
+        with torch.cuda.device(0), torch.cuda.stream(torch.cuda.Stream()):
+            q = queries(c, new, group, new)
+            cache, dq = O.upload(g10, c), q.to(DEV)
+            outs = [g10.g10_cache_attend(cache, dq) for _ in range(30)]
+            torch.cuda.current_stream().synchronize()
+            r = O.attend(c, q, 128 ** -0.5)
+            bound = O.attend_bounds(c, r)[0]
+            wrong.extend(1 for out in outs if not ((out.cpu().double() - r.out).abs() <= bound).all())
+            wrong.extend(1 for _ in range(int(cache.status.item() != 0)))
+
+    threads = [threading.Thread(target=work, args=x) for x in cases * 2]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
+def test_shared_rows_and_pages_of_sequences_that_attend(g10):
+    """The same pages in two tables, and one query for all sequences, by a stride of zero."""
+    c = O.make_cache([200, 200, 130], 2, 64, 16, torch.bfloat16, 17)
+    c.table[1] = c.table[0]
+    q = queries(c, 1, 4, 6)[:1].expand(3, -1, -1, -1)
+    cache = O.upload(g10, c)
+    out = g10.g10_cache_attend(cache, q[:1].to(DEV).expand(3, -1, -1, -1))
+    r = O.attend(c, q, 64 ** -0.5)
+    assert ((out.cpu().double() - r.out).abs() <= O.attend_bounds(c, r)[0]).all()
+
+
+def test_binding_refusals(g10):
+    c = O.make_cache([40, 20], 2, 64, 16, torch.bfloat16, 1, positions=True)
+    cache = O.upload(g10, c)
+    q = torch.zeros(2, 1, 8, 64, dtype=torch.bfloat16, device=DEV)
+    kv = torch.zeros(2, 1, 2, 64, dtype=torch.bfloat16, device=DEV)
+    table = torch.zeros(50, 32, device=DEV)
+    ints = torch.zeros(2, dtype=torch.int32, device=DEV)
+    plan = g10.g10_cache_plan_evictions(cache, 8)
+    state = [x.clone() for x in (cache.k, cache.v, cache.scores)]
+    attend = [(q.float(), {}), (q.half(), {}), (q.cpu(), {}), (q[:1], {}), (q[..., :32], {}), (q[0], {}), (q.transpose(2, 3).contiguous().transpose(2, 3), {}),
+              (q[:, :, :7], {}), (q, dict(out=q.float())), (q, dict(out=torch.empty(2, 1, 8, 128, dtype=q.dtype, device=DEV)[..., ::2])), (q, dict(lse=ints)),
+              (q, dict(counts=ints.long())), (q, dict(counts=ints[:1])), (q, dict(ws=torch.empty(64, dtype=torch.uint8, device=DEV))), (q, dict(ws=ints)),
+              (q, dict(window=5)), (q, dict(scale=math.inf)), (q[:, :0], {}), (torch.zeros(2, 300, 8, 64, dtype=q.dtype, device=DEV), {})]
+    for x, kw in attend:
+        with pytest.raises(g10.G10Error):
+            g10.g10_cache_attend(cache, x, **kw)
+    append = [((kv.float(), kv), {}), ((kv, kv.cpu()), {}), ((kv[:, :, :1], kv), {}), ((kv, kv.expand(2, 1, 2, 64)[:, :, :, :32]), {}), ((kv, kv), dict(cos=table)),
+              ((kv, kv), dict(cos=table, sin=table[:, :16])), ((kv, kv), dict(cos=table.double(), sin=table.double())), ((kv, kv), dict(k_weight=table[0])),
+              ((kv, kv), dict(q=q[:1])), ((kv, kv), dict(q=q, q_out=q[:, :, :4])), ((kv, kv), dict(counts=ints.long())),
+              ((kv, kv), dict(cos=torch.zeros(9, 40, device=DEV), sin=torch.zeros(9, 40, device=DEV)))]
+    for x, kw in append:
+        with pytest.raises(g10.G10Error):
+            g10.g10_cache_append(cache, *x, **kw)
+    for moves, counts in [(plan.moves.long(), plan.counts), (plan.moves[:1], plan.counts), (plan.moves, plan.counts[:, :1]), (plan.moves.cpu(), plan.counts), (plan.moves[0], plan.counts)]:
+        with pytest.raises(g10.G10Error):
+            g10.g10_cache_evict(cache, moves, counts)
+    for kw in (dict(budget=0), dict(budget=8, sinks=5, recent=4), dict(budget=8, counts=ints)):
+        with pytest.raises(g10.G10Error):
+            g10.g10_cache_plan_evictions(cache, **kw)
+    torch.cuda.synchronize()
+    assert int(cache.status.item()) == 0
+    assert all(same(a, b) for a, b in zip(state, (cache.k, cache.v, cache.scores)))
+
+
 def test_a_conversation_within_a_budget(g10):
     """Prompts of different lengths, their last tokens looked at, eviction, then token after token with an eviction every few: two layers
     that share lengths.  Each step is compared with the definitions applied to the device's state before it."""
