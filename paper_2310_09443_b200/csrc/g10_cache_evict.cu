@@ -53,8 +53,9 @@ __device__ __forceinline__ void settle(const Census &c, int rank, int left, int 
 template <bool kKept, int kThreads>
 __global__ void __launch_bounds__(kThreads) k_cache_plan(const EvictArgs a, int blocks)
 {
-    constexpr int kDigits = 2048, kWarps = kThreads / 32;
-    __shared__ unsigned s_count[kDigits], s_sum[3][kDigits], s_warp[kWarps], s_found[2];
+    constexpr int kDigits = 2048, kCounts = 2 * kDigits + kDigits / 2, kWarps = kThreads / 32;
+    __shared__ __align__(16) unsigned s_count[kCounts], s_sum[kCounts];            // of the three digits; the block's, the cluster's
+    __shared__ unsigned s_warp[kWarps], s_found[2];
     __shared__ Census s_census[kWarps];
     __shared__ int s_mine[5];
     extern __shared__ unsigned s_worth[];
@@ -71,8 +72,10 @@ __global__ void __launch_bounds__(kThreads) k_cache_plan(const EvictArgs a, int 
     }
     const int each = (length + blocks - 1) / blocks, from = min(length, rank * each), n = min(length, from + each) - from;
     auto worth = [&](int i) -> unsigned { return kKept ? s_worth[i] : worth_at(a, s, head, from + i, seen, bad); };
-    if (blocks > 1)
-        for (int i = tid; i < 3 * kDigits; i += kThreads) s_sum[0][i] = 0;
+    for (int i = tid; i < kCounts / 4; i += kThreads) {
+        ((uint4 *)s_count)[i] = make_uint4(0, 0, 0, 0);
+        if (blocks > 1) ((uint4 *)s_sum)[i] = make_uint4(0, 0, 0, 0);
+    }
     if (kKept) {
         // (no branch between the loads of a round: all pages are on the way together, then all scores)
         constexpr int kAhead = kThreads >= 512 ? 8 : 12;
@@ -102,31 +105,31 @@ __global__ void __launch_bounds__(kThreads) k_cache_plan(const EvictArgs a, int 
         }
     }
     if (blocks > 1) cluster_sync();                      // (all have begun, and cleared their sums)
+    else __syncthreads();
     unsigned known = 0, left = (unsigned)a.budget;       // the number's upper digits; how many of those that agree are kept
 #pragma unroll
     for (int pass = 0; pass < 3; ++pass) {
-        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, digits = 1 << bits, few = digits / kThreads > 0 ? digits / kThreads : 1;
-        for (int i = tid; i < digits; i += kThreads) s_count[i] = 0;
-        __syncthreads();
+        const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, digits = 1 << bits, few = digits / kThreads;
+        unsigned *const count = s_count + pass * kDigits;
         for (int i = tid; i < n; i += kThreads) {
             const unsigned w = worth(i);
-            if (pass == 0 || w >> (shift + bits) == known >> (shift + bits)) atomicAdd(&s_count[(w >> shift) & (digits - 1)], 1u);
+            if (pass == 0 || w >> (shift + bits) == known >> (shift + bits)) atomicAdd(&count[(w >> shift) & (digits - 1)], 1u);
         }
         __syncthreads();
-        const unsigned *counts = s_count;
+        const unsigned *counts = count;
         if (blocks > 1) {
             for (int i = tid; i < digits; i += kThreads) {
-                const unsigned v = s_count[i];
-                if (v != 0) for (int r = 0; r < blocks; ++r) add_to(&s_sum[pass][i], (unsigned)r, v);
+                const unsigned v = count[i];
+                if (v != 0) for (int r = 0; r < blocks; ++r) add_to(&s_sum[pass * kDigits + i], (unsigned)r, v);
             }
             cluster_sync();
-            counts = s_sum[pass];
+            counts = s_sum + pass * kDigits;
         }
-        // from the largest digit down: a few neighbours a thread
-        const int top = digits - 1 - tid * few;
-        unsigned mine = 0;
+        // from the largest digit down: a few neighbours a thread (2, 4 or 8)
+        const int lowest = digits - (tid + 1) * few;
+        unsigned of_digit[8], mine = 0;
 #pragma unroll
-        for (int i = 0; i < few; ++i) mine += counts[top - i];
+        for (int i = 0; i < few; i += 2) { const uint2 v = *(const uint2 *)&counts[lowest + i]; of_digit[i] = v.x; of_digit[i + 1] = v.y; mine += v.x + v.y; }
         unsigned upto = mine;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) { const unsigned v = __shfl_up_sync(0xffffffffu, upto, o); if (lane >= o) upto += v; }
@@ -135,9 +138,15 @@ __global__ void __launch_bounds__(kThreads) k_cache_plan(const EvictArgs a, int 
         upto += __reduce_add_sync(0xffffffffu, lane < warp ? s_warp[lane] : 0u);
         unsigned above = upto - mine;
         if (above < left && left <= upto) {
-            int i = 0;
-            while (above + counts[top - i] < left) { above += counts[top - i]; ++i; }
-            s_found[0] = known | (unsigned)(top - i) << shift; s_found[1] = left - above;
+            bool found = false;
+#pragma unroll
+            for (int i = few - 1; i >= 0; --i) {
+                if (!found && above + of_digit[i] >= left) {
+                    found = true;
+                    s_found[0] = known | (unsigned)(lowest + i) << shift; s_found[1] = left - above;
+                }
+                above += of_digit[i];
+            }
         }
         __syncthreads();
         known = s_found[0]; left = s_found[1];
