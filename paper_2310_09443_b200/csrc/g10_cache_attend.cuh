@@ -120,8 +120,9 @@ struct Share {
     int blocks;                          // that share them
 };
 // `held` blocks run at a time, and each takes one share, of equal length.  Equal shares do not take equally long (with one share each, the first block of
-// 64 sequences of 16 000 slots ended after 75 % of the time): where they are long they are cut into kCuts, and the blocks that wait for a place even
-// it out (424 -> 412 us there).  Shorter ones are not: 320 blocks of 24 tiles, where 296 run at a time, take two rounds (49 -> 71 us).
+// 64 sequences of 16 000 slots ended after 75 % of the time): where they are long and not more than two blocks share an SM they are cut into kCuts, and the
+// blocks that wait for a place even it out (424 -> 412 us there, with two blocks an SM; with three it no longer tells).  Shorter ones are not: 320
+// blocks of 24 tiles, where 296 run at a time, take two rounds (49 -> 71 us).
 constexpr int kLong = 128, kCuts = 4;    // tiles
 __device__ __forceinline__ Share share_of(int64_t tiles, int per, int grid, int held)
 {
@@ -233,8 +234,23 @@ __device__ __forceinline__ void part_add(Part &p, float top, float sum, const fl
     p.sum = p.sum * f + sum * g;
     p.o = make_float4(p.o.x * f + o.x * g, p.o.y * f + o.y * g, p.o.z * f + o.z * g, p.o.w * f + o.w * g);
 }
-template <typename T, int kSteps, int kCols, int kStages>
+// Blocks that share an SM, and tiles in a block's ring.  What a warp does for a tile is a chain that two warps a scheduler do not fill, so there are as many
+// blocks as leave each a ring of two tiles and the registers it needs: four up to 64 dims (24 sequences of 4100 slots against two: 50 -> 39 us, 64 of
+// 16 000: 280 -> 238), three above (128 dims: 57.6 -> 55.7, 428 -> 421).  Not so for rows of about 160 bytes, no whole number of the memory's 64: they are
+// bound by it, and the more places are read from at a time the worse (a window over 80 dims 46 -> 52 us with three, 64 sequences 407 -> 420).  Wide
+// heads: one block.
+template <int kSteps, int kCols>
+struct Ring {
+    static constexpr int kOther = (kCols * kSteps <= 16 ? 0 : 8 * kCols * (32 * kSteps + 16)) + kParts * 8 * kCols * 8 + (kCols <= 2 ? 8 * kCols * (64 * kSteps + 8) : 0) + 1024;
+    static constexpr int kTileBytes = 2 * kTile * (32 * kSteps + 16);
+    static constexpr int fits(int blocks) { return (226 * 1024 / blocks - kOther) / kTileBytes; }
+    static constexpr int kBlocks = kSteps > 8 ? 1 : kSteps <= 4 && fits(4) >= 2 ? 4 : kSteps != 5 && fits(3) >= 2 ? 3 : 2;
+    static constexpr int kStages = fits(kBlocks) > 6 ? 6 : fits(kBlocks);
+    static_assert(kStages >= 2, "a tile in use, and one on its way");
+};
+template <typename T, int kSteps, int kCols>
 struct Config {
+    static constexpr int kStages = Ring<kSteps, kCols>::kStages;
     static constexpr int kDim = 16 * kSteps;             // head_dim, padded with zeros
     // bytes of a row in shared memory: an odd number of 16-byte units, so that the 8 rows of a matrix lie in different banks
     static constexpr int kPitch = 2 * kDim + 16;
@@ -263,10 +279,11 @@ struct Config {
 // The tiles of an item are then numbered from item * cap on.
 // ref is a maximum of the past: the weights are taken relative to it as long as no logit is more than kSlack above it (weights up to 2^8,
 // which either type holds), so that the sums are rescaled and the warp's lanes compared only when that fails, a few times per piece.
-template <typename T, int kSteps, int kCols, int kStages>
-__global__ void __launch_bounds__(kThreads) k_cache_attend(const AttendArgs a, int held_blocks, int cluster, int cap)
+template <typename T, int kSteps, int kCols>
+__global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cache_attend(const AttendArgs a, int held_blocks, int cluster, int cap)
 {
-    typedef Config<T, kSteps, kCols, kStages> C;
+    typedef Config<T, kSteps, kCols> C;
+    constexpr int kStages = C::kStages;
     extern __shared__ __align__(128) char smem[];
     float *const s_join = (float *)(smem + kParts * kStages * C::kPartBytes);          // [kRows][kDim], then [kRows] maximum and sum (kClusters)
     float2 *const s_join_ml = (float2 *)(s_join + (C::kClusters ? C::kRows * C::kDim : 0));
@@ -876,11 +893,11 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_book(const AttendArgs a,
 }
 
 // ---- host ----
-template <typename T, int kSteps, int kCols, int kStages>
+template <typename T, int kSteps, int kCols>
 cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
 {
-    typedef Config<T, kSteps, kCols, kStages> C;
-    const auto kernel = k_cache_attend<T, kSteps, kCols, kStages>;
+    typedef Config<T, kSteps, kCols> C;
+    const auto kernel = k_cache_attend<T, kSteps, kCols>;
     static int known[kMaxDevices];                       // blocks that the device holds at a time
     int dev = 0, room = 0;
     cudaError_t e = cudaGetDevice(&dev);
@@ -930,17 +947,10 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     const auto book = pitch <= 4 ? k_cache_book<1> : pitch <= 8 ? k_cache_book<2> : pitch <= 16 ? k_cache_book<4> : k_cache_book<8>;
     return cudaLaunchKernelEx(&cfg, book, a, C::kRows, cluster == 0);
 }
-// Tiles in the ring: as many as let two blocks share an SM, or, for wide heads, fill it for one.
-constexpr int stages_of(int steps, int cols)
-{
-    const int rest = (cols * steps <= 16 ? 0 : 8 * cols * (32 * steps + 16)) + kParts * 8 * cols * 8 + (cols <= 2 ? 8 * cols * (64 * steps + 8) : 0) + 1024;
-    const int n = ((steps <= 8 ? 113 : 226) * 1024 - rest) / (2 * kTile * (32 * steps + 16));
-    return n > 6 ? 6 : n;
-}
 template <typename T, int kSteps>
 cudaError_t launch_steps(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
 {
-    return z.block_rows == 8 ? launch<T, kSteps, 1, stages_of(kSteps, 1)>(a, z, s) : launch<T, kSteps, 2, stages_of(kSteps, 2)>(a, z, s);
+    return z.block_rows == 8 ? launch<T, kSteps, 1>(a, z, s) : launch<T, kSteps, 2>(a, z, s);
 }
 template <typename T>
 cudaError_t launch_type(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
