@@ -3,7 +3,7 @@
 //
 // The mathematics and the way the work is shared out are those of g10_cache_attend.cuh.  With R rows a tile of 64 slots takes 4 * 64 * R * head_dim
 // operations for 256 * head_dim bytes: up to some hundred rows memory still is the bound, but the older matrix instructions, fed from registers,
-// cannot keep up (32 rows a block, the cache read twice for 64 rows: 127 us for 6 sequences of 9001 slots and 16 new tokens of 4 heads, 86 this way).  So up to
+// cannot keep up (32 rows a block, the cache read twice for 64 rows: 127 us for 6 sequences of 9001 slots and 16 new tokens of 4 heads, 73 this way).  So up to
 // 128 rows of an item form one operand, [128 rows x dims], and
 //   S [128 x 64] = Q K^T,    W = exp2(S - ref),    O [128 x dims] += W V
 // are tcgen05 products with S, W and O in tensor memory.  A row is a lane of tensor memory and belongs to one thread, which sees all of its 64 logits:
@@ -33,6 +33,9 @@ constexpr int kBlock = kTile * 128;      // bytes of 64 dimensions of a tile's k
 // ---- barriers in shared memory; every wait has a limit ----
 __device__ __forceinline__ void bar_init(unsigned bar, int arrivals) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(arrivals) : "memory"); }
 __device__ __forceinline__ void bar_arrive(unsigned bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// The thread's arrival once all copies that it has asked for so far have landed.  (Who waits for it and issues products calls async_sees() first: the
+// copies wrote through another path than the one by which products read.)
+__device__ __forceinline__ void bar_arrive_landed(unsigned bar) { asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity)
 {
     unsigned ok;
@@ -171,11 +174,9 @@ struct Wide {
     static constexpr int kWeights = kLogits + (kOwnWeights ? 2 * kTile : 0), kWeightsApart = kOwnWeights ? kTile / 2 : kTile;
     static constexpr int kUsed = kLogits + 2 * kTile + (kOwnWeights ? kTile : 0);
     static constexpr unsigned kColumns = kUsed <= 256 ? 256 : 512;
-    static constexpr int kLag = kStages > 2 ? 2 : 1;     // tiles on their way before the first of them is waited for
-    // Tiles whose product with the queries is issued before the product of a tile with its values.  (A tile is told full kLag tiles after its
-    // copies were issued, which wait for a stage: kLag + kBehind stages at least, or the two wait for each other.)
-    static constexpr int kBehind = kStages - kLag >= 2 && kTeams == 2 ? 2 : 1;
-    static_assert(kStages >= 2 && kLag + kBehind <= kStages, "stages");
+    // Tiles whose product with the queries is issued before the product of a tile with its values.
+    static constexpr int kBehind = kStages >= 4 && kTeams == 2 ? 2 : 1;
+    static_assert(kBehind < kStages, "stages");
 };
 
 // A row's queries, from global memory to their exchanged places (with the sign of the scale, so that the largest product is the largest logit).
@@ -239,11 +240,11 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
     cursor_at(a, now, s_place, begin);
 
     if (warp >= 9) {
-        // ---- the loaders: 32 slots each, one a lane; a tile is told full once it has landed, some tiles later ----
+        // ---- the loaders: 32 slots each, one a lane; a tile is told full as its copies land ----
         const int part = warp - 9;
         constexpr unsigned kNone = 0xffffffffu;
         const uint64_t policy = leaves_first();
-        int stage = 0, landed = 0;
+        int stage = 0;
         unsigned round = 1;
         // (the page is loaded a tile ahead, and looked at when its turn comes)
         int page = 0, at_place = 0, head = 0;
@@ -263,42 +264,34 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
             return cache_row(a.c, Spot{page, at_place}, head);
         };
         look_up();
-        for (int u = 0; u < n + C::kLag; ++u) {
-            if (u >= C::kLag) {
-                asm volatile("cp.async.wait_group %0;" ::"n"(C::kLag - 1) : "memory");
-                async_sees();
-                bar_arrive(full + 8 * landed);
-                landed = landed == S - 1 ? 0 : landed + 1;
-            }
-            if (u < n) {
-                const unsigned mine = row_found();
-                if (u + 1 < n) { cursor_next(a, now, per); look_up(); }
-                bar_wait(free_ + 8 * stage, round, &s_stop);
-                const unsigned to = smem_of(s_ring) + stage * C::kStageBytes;
-                if (++stage == S) { stage = 0; round ^= 1; }
-                const bool all = __all_sync(0xffffffffu, mine != kNone) && a.c.head_dim == C::kDim && a.row_blocks == 1;
-                if (all) {
+        for (int u = 0; u < n; ++u) {
+            const unsigned mine = row_found();
+            if (u + 1 < n) { cursor_next(a, now, per); look_up(); }
+            bar_wait(free_ + 8 * stage, round, &s_stop);
+            const unsigned told = full + 8 * stage, to = smem_of(s_ring) + stage * C::kStageBytes;
+            if (++stage == S) { stage = 0; round ^= 1; }
+            const bool all = __all_sync(0xffffffffu, mine != kNone) && a.c.head_dim == C::kDim && a.row_blocks == 1;
+            if (all) {
 #pragma unroll
-                    for (int i = 0; i < C::kUnits; ++i) {
-                        const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
-                        const int64_t x = 16 * (int64_t)__shfl_sync(0xffffffffu, mine, row);
-                        const unsigned at = swizzled(part * 32 + row, unit, kBlock);
-                        copy16(to + at, a.c.k + 16 * unit + x, policy);
-                        copy16(to + kDims * kBlock + at, a.c.v + 16 * unit + x, policy);
-                    }
-                } else {
+                for (int i = 0; i < C::kUnits; ++i) {
+                    const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
+                    const int64_t x = 16 * (int64_t)__shfl_sync(0xffffffffu, mine, row);
+                    const unsigned at = swizzled(part * 32 + row, unit, kBlock);
+                    copy16(to + at, a.c.k + 16 * unit + x, policy);
+                    copy16(to + kDims * kBlock + at, a.c.v + 16 * unit + x, policy);
+                }
+            } else {
 #pragma unroll 2
-                    for (int i = 0; i < C::kUnits; ++i) {
-                        const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
-                        const unsigned from = __shfl_sync(0xffffffffu, mine, row), at = swizzled(part * 32 + row, unit, kBlock);
-                        const bool real = from != kNone && unit * 8 < a.c.head_dim;
-                        const int64_t x = real ? 16 * ((int64_t)from + unit) : 0;
-                        copy16_or_zeros(to + at, a.c.k + x, real);
-                        copy16_or_zeros(to + kDims * kBlock + at, a.c.v + x, real);
-                    }
+                for (int i = 0; i < C::kUnits; ++i) {
+                    const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
+                    const unsigned from = __shfl_sync(0xffffffffu, mine, row), at = swizzled(part * 32 + row, unit, kBlock);
+                    const bool real = from != kNone && unit * 8 < a.c.head_dim;
+                    const int64_t x = real ? 16 * ((int64_t)from + unit) : 0;
+                    copy16_or_zeros(to + at, a.c.k + x, real);
+                    copy16_or_zeros(to + kDims * kBlock + at, a.c.v + x, real);
                 }
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
+            bar_arrive_landed(told);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (bad != 0) raise_status(a.c.status, bad);
@@ -340,6 +333,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                 start = u;
             }
             bar_wait(full + 8 * stage, round, &s_stop);
+            async_sees();
             if (u >= 2) bar_wait((C::kOwnWeights ? s_free : v_done) + 8 * (u & 1), ((u >> 1) - 1) & 1, &s_stop);
             after_sync();
             if (leads) {
@@ -600,7 +594,6 @@ struct Book {
     static constexpr int kFit = (226 * 1024 - 4096 - kQBytes) / kStageBytes, kStages = kFit > 6 ? 6 : kFit;
     static constexpr int kSmem = 1024 + kQBytes + kStages * kStageBytes;
     static constexpr unsigned kColumns = 256;            // of tensor memory: S^T twice
-    static constexpr int kLag = kStages > 2 ? 2 : 1;     // tiles on their way before the first of them is waited for
     static_assert(kStages >= 2, "two tiles");
 };
 template <typename T, int kDims>
@@ -652,7 +645,7 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
         const int part = warp - 9;
         constexpr unsigned kNone = 0xffffffffu;
         const uint64_t policy = leaves_first();
-        int page = 0, at_place = 0, head = 0, stage = 0, landed = 0;
+        int page = 0, at_place = 0, head = 0, stage = 0;
         bool there = false;
         unsigned round = 1;
         auto look_up = [&]() {
@@ -670,38 +663,30 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
             return cache_row(a.c, Spot{page, at_place}, head);
         };
         look_up();
-        for (int u = 0; u < n + C::kLag; ++u) {
-            if (u >= C::kLag) {
-                asm volatile("cp.async.wait_group %0;" ::"n"(C::kLag - 1) : "memory");
-                async_sees();
-                bar_arrive(full + 8 * landed);
-                landed = landed == S - 1 ? 0 : landed + 1;
-            }
-            if (u < n) {
-                const unsigned mine = row_found();
-                if (u + 1 < n) { cursor_next<2>(one, now, heads); look_up(); }
-                bar_wait(free_ + 8 * stage, round, &s_stop);
-                const unsigned to = smem_of(s_ring) + stage * C::kStageBytes;
-                if (++stage == S) { stage = 0; round ^= 1; }
-                const bool all = __all_sync(0xffffffffu, mine != kNone) && a.c.head_dim == C::kDim;
-                if (all) {
+        for (int u = 0; u < n; ++u) {
+            const unsigned mine = row_found();
+            if (u + 1 < n) { cursor_next<2>(one, now, heads); look_up(); }
+            bar_wait(free_ + 8 * stage, round, &s_stop);
+            const unsigned told = full + 8 * stage, to = smem_of(s_ring) + stage * C::kStageBytes;
+            if (++stage == S) { stage = 0; round ^= 1; }
+            const bool all = __all_sync(0xffffffffu, mine != kNone) && a.c.head_dim == C::kDim;
+            if (all) {
 #pragma unroll
-                    for (int i = 0; i < C::kUnits; ++i) {
-                        const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
-                        const int64_t x = 16 * (int64_t)__shfl_sync(0xffffffffu, mine, row);
-                        copy16(to + swizzled(part * 32 + row, unit, 128 * 128), a.c.k + 16 * unit + x, policy);
-                    }
-                } else {
+                for (int i = 0; i < C::kUnits; ++i) {
+                    const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
+                    const int64_t x = 16 * (int64_t)__shfl_sync(0xffffffffu, mine, row);
+                    copy16(to + swizzled(part * 32 + row, unit, 128 * 128), a.c.k + 16 * unit + x, policy);
+                }
+            } else {
 #pragma unroll 2
-                    for (int i = 0; i < C::kUnits; ++i) {
-                        const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
-                        const unsigned from = __shfl_sync(0xffffffffu, mine, row);
-                        const bool real = from != kNone && unit * 8 < a.c.head_dim;
-                        copy16_or_zeros(to + swizzled(part * 32 + row, unit, 128 * 128), a.c.k + (real ? 16 * ((int64_t)from + unit) : 0), real);
-                    }
+                for (int i = 0; i < C::kUnits; ++i) {
+                    const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
+                    const unsigned from = __shfl_sync(0xffffffffu, mine, row);
+                    const bool real = from != kNone && unit * 8 < a.c.head_dim;
+                    copy16_or_zeros(to + swizzled(part * 32 + row, unit, 128 * 128), a.c.k + (real ? 16 * ((int64_t)from + unit) : 0), real);
                 }
             }
-            asm volatile("cp.async.commit_group;" ::: "memory");
+            bar_arrive_landed(told);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
         if (bad != 0) raise_status(a.c.status, bad);
@@ -714,6 +699,7 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
         unsigned round = 0;
         for (int u = 0, d = 0; u < n; ++u) {
             bar_wait(full + 8 * stage, round, &s_stop);
+            async_sees();
             for (int b = 0; b < blocks; ++b, ++d) {
                 if (fresh || blocks > 1) { bar_wait(q_full, given & 1, &s_stop); ++given; }      // (brought for every run)
                 fresh = false;
