@@ -15,7 +15,7 @@
 // Warps: 0 - 7 weights and results (a lane per row), 8 issues the products (one thread), 9 and 10 bring the tiles.  Keys and values lie in
 // shared memory as the products want them, 128-byte rows of 64 dimensions with their 16-byte units exchanged by the row's number (the 128-byte swizzle);
 // pages are no whole tiles, so rows are copied one by one, 16 bytes at a time, to their exchanged places.  The product of tile u with the queries is
-// issued before that of tile u - 1 with the values, so that it runs while the weights are worked out.
+// issued before those of the one or two tiles before it with the values, so that it runs while the weights are worked out.
 #pragma once
 #include <type_traits>
 
