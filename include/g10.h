@@ -472,7 +472,7 @@ int32_t g10_cache_append(const g10_cache *cache, const g10_cache_tokens *tokens,
    empty sequence) gives out = 0, lse = -inf.  What stands in slots that a row does not see has no influence on it, not even
    as infinity or NaN.  With add_scores, scores of each slot grows by the sum of its w_j over the queries and the heads of its group.
    Products take their operands as they are stored and are added up in 32 bits; the weights are rounded to the cache's type before they
-   multiply the values (relative 2^-8 / 2^-11 each), the booked ones are not.  The result does not depend on the timing of the
+   multiply the values (relative 2^-8 / 2^-11 each; for fp16 those below 2^-24 of the row's largest by up to 2^-35 of that one), the booked ones are not.  The result does not depend on the timing of the
    blocks; the way the work is split, and with it the rounding, depends on all lengths of the batch.
    Limit: new_tokens * q_heads / kv_heads <= 1024; scale / log 2 is finite. */
 typedef struct g10_cache_queries {

@@ -219,7 +219,20 @@ __device__ __forceinline__ unsigned turned8x8(unsigned x)
 
 constexpr int kParts = 4;                // warps of a block; each takes 16 slots of a tile
 constexpr int kThreads = 32 * kParts;
-constexpr float kSlack = 8.0f;           // see below
+
+// Weights are taken relative to ref, a maximum of the past, as long as no logit is more than kSlack above it, and multiply the values rounded to the
+// cache's type (the second product's operands have to be of one type; a weight in two halves would double it).  bf16 reaches as far down as 32 bits do.
+// fp16 is whole down to 2^-14 and ends at 2^-24: of thousands of slots that far below one, whose weights are all rounded alike, too much or nothing
+// would be left.  So fp16 weights are 2^kLift times too large, in sums and results alike: up to 2^15, whole down to 2^-24 of the largest, and off
+// by 2^-35 of it at most below that.  (16 new tokens of 4 heads, fp16: 70.3 us with a slack of 8, 70.9 with 5, 72.0 with 3; few rows: no difference.)
+template <typename T>
+struct Weights {
+    static constexpr float kSlack = 8.0f, kLift = 0.0f, kUnlift = 1.0f;
+};
+template <>
+struct Weights<__half> {
+    static constexpr float kSlack = 5.0f, kLift = 10.0f, kUnlift = 1.0f / 1024.0f;       // (kSlack + kLift: 2^15, below 65504)
+};
 
 // Running maximum, sum and (four of) the accumulators of a row over some pieces.
 struct Part {
@@ -277,8 +290,8 @@ struct Config {
 // With `cluster` > 0, for few and short sequences, where the second kernel would take as long as the first: a cluster of so many blocks takes one
 // item, each an equal part of its tiles, and joins the parts itself, through one another's shared memory (16 heads of 517 slots: 10.2 -> 8.2 us).
 // The tiles of an item are then numbered from item * cap on.
-// ref is a maximum of the past: the weights are taken relative to it as long as no logit is more than kSlack above it (weights up to 2^8,
-// which either type holds), so that the sums are rescaled and the warp's lanes compared only when that fails, a few times per piece.
+// ref is a maximum of the past (see Weights), so that the sums are rescaled and the warp's lanes compared only when a logit is far above it, a few times per
+// piece.
 template <typename T, int kSteps, int kCols>
 __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cache_attend(const AttendArgs a, int held_blocks, int cluster, int cap)
 {
@@ -509,7 +522,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
 #pragma unroll
         for (int j = 0; j < kCols; ++j)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) over |= fmaxf(x[j][h], x[j][h + 2]) > m[j][h] + kSlack;
+            for (int h = 0; h < 2; ++h) over |= fmaxf(x[j][h], x[j][h + 2]) > m[j][h] + Weights<T>::kSlack;
         if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
             for (int j = 0; j < kCols; ++j)
@@ -530,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
         for (int j = 0; j < kCols; ++j)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float ref = m[j][h] == -INFINITY ? 0.0f : m[j][h];
+                const float ref = (m[j][h] == -INFINITY ? 0.0f : m[j][h]) - Weights<T>::kLift;
                 x[j][h] = exp2_of(x[j][h] - ref); x[j][h + 2] = exp2_of(x[j][h + 2] - ref);
                 l[j][h] += x[j][h] + x[j][h + 2];
             }
@@ -644,7 +657,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
                         if (sum == 0.0f) w = make_uint2(0, 0);
                         *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
                         if (d == 0) {
-                            const float lse = top + log2f(sum);
+                            const float lse = top + log2f(sum * Weights<T>::kUnlift);
                             if (a.lse != nullptr) a.lse[at] = sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
                             if (a.books) a.sums[item * C::kRows + r] = sum == 0.0f ? INFINITY : lse;
                         }
@@ -680,7 +693,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
             if (p.sum == 0.0f) w = make_uint2(0, 0);
             *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
             if (d == 0) {
-                const float lse = p.top + log2f(p.sum);
+                const float lse = p.top + log2f(p.sum * Weights<T>::kUnlift);
                 if (a.lse != nullptr) a.lse[at] = p.sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
                 if (a.books) a.sums[(int64_t)my_item * C::kRows + r] = p.sum == 0.0f ? INFINITY : lse;
             }
@@ -788,7 +801,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
                 if (p.sum == 0.0f) o = make_uint2(0, 0);
                 *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = o;
                 if (d == 0) {
-                    const float lse = p.top + log2f(p.sum);
+                    const float lse = p.top + log2f(p.sum * Weights<T>::kUnlift);
                     if (a.lse != nullptr) a.lse[at] = p.sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
                     if (a.books) a.sums[w.item * block_rows + r] = p.sum == 0.0f ? INFINITY : lse;
                 }

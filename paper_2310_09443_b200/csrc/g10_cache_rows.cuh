@@ -405,8 +405,8 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                     }
                     float top = fmaxf(fmaxf(best[0].x, best[1].x), fmaxf(best[0].y, best[1].y));
                     top = top == -INFINITY ? top : top * scale;
-                    // (rescaled only where a logit is more than kSlack above the reference)
-                    if (__any_sync(0xffffffffu, top > m + kSlack)) {
+                    // (rescaled only where a logit is far above the reference)
+                    if (__any_sync(0xffffffffu, top > m + Weights<T>::kSlack)) {
                         top = fmaxf(top, m);
                         const float by = exp2_of(m - (top == -INFINITY ? 0.0f : top));
                         m = top; l *= by;
@@ -425,7 +425,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                         }
                     }
                     const float ref = m == -INFINITY ? 0.0f : m;
-                    const float2 by = make_float2(scale, scale), off = make_float2(-ref, -ref);
+                    const float2 by = make_float2(scale, scale), off = make_float2(Weights<T>::kLift - ref, Weights<T>::kLift - ref);
                     float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
                     if (whole) {
 #pragma unroll
@@ -528,7 +528,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
             if (real && team == 0) {
                 a.ml[r * a.pieces + piece] = make_float2(p < 0 ? -INFINITY : top, sum);
                 if (all) {
-                    const float lse = top + log2f(sum);
+                    const float lse = top + log2f(sum * Weights<T>::kUnlift);
                     if (a.lse != nullptr) a.lse[at] = sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
                     if (a.books) a.sums[item * kWideRows + r] = sum == 0.0f ? INFINITY : lse;
                 }

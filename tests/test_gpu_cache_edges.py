@@ -1,0 +1,59 @@
+"""The key-value cache on the device at the edges of what its calls allow, against the definitions in 64 bits (cache_oracle.py)."""
+import math
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+import cache_oracle as O
+from test_gpu_cache import DEV, check_attend, g10, queries, same  # noqa: F401 (g10 is the fixture)
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- weights far below the largest -------------------------------------------------------------------------------------
+@pytest.mark.parametrize("below", [10.0, 16.0, 17.5, 21.0])
+@pytest.mark.parametrize("where", [0, 6_000, 12_002])
+@pytest.mark.parametrize("group", [4, 20])
+def test_many_weights_far_below_one(g10, below, where, group):
+    """One slot with a value of zero outweighs each of 12 002 equal ones with a value of one by e^below: the answer is what these add up to.  So many
+    heads that a block goes through whole sequences, and has that slot and thousands of the others under one maximum.
+
+    The bound is that of attend_bounds with 2^-35 of the row's largest weight in place of half the smallest fp16 subnormal: fp16 weights are kept
+    2^10 times too large (a weight of 1 then is 2^10, so half a subnormal step, 2^-25, is 2^-35 of the largest)."""
+    n, kv = 12_003, 640
+    c = O.make_cache([n], kv, 8, 64, torch.float16, 1, scores=False)
+    pg, pl = O.places(c, 0, n)
+    c.k[pg, pl], c.v[pg, pl] = 0.0, 1.0
+    c.k[pg[where], pl[where], :, 0] = below
+    c.v[pg[where], pl[where]] = 0.0
+    q = torch.zeros(1, 1, kv * group, 8, dtype=torch.float16)
+    q[..., 0] = 1.0
+    lse = torch.empty(q.shape[:3], device=DEV)
+    cache = O.upload(g10, c)
+    out = g10.g10_cache_attend(cache, q.to(DEV), scale=1.0, lse=lse).cpu().double()
+    assert int(cache.status.item()) == 0
+    one = SimpleNamespace(**{**vars(c), "k": c.k[:, :, :1], "v": c.v[:, :, :1], "kv_heads": 1})        # (all heads are alike)
+    r = O.attend(one, q[:, :, :1], 1.0)
+    b_out, b_lse, _ = O.attend_bounds(one, r)
+    b_out = b_out - (2.0 ** -25 - 2.0 ** -35) * r.all_v
+    off = (out - r.out).abs() - b_out
+    assert (off <= 0).all(), "%g instead of %g, off by %g over the bound" % (out.flatten()[off.argmax()], r.out.flatten()[0], off.max())
+    assert ((lse.cpu().double() - r.lse).abs() <= b_lse).all()
+
+
+@pytest.mark.parametrize("new,group", [(1, 4), (1, 12), (30, 4)])
+def test_large_fp16_values_under_lifted_weights(g10, new, group):
+    """Values at the type's end, the largest weights as large as they get: nothing overflows on the way to sums that are in range."""
+    c = O.make_cache([2000, new + 3], 2, 64, 16, torch.float16, 4)
+    own = torch.isfinite(c.v)
+    c.v[own] = torch.where(c.v[own] > 0, 65504.0, 65000.0).half()
+    q = queries(c, new, group, 2)
+    # (k along q's first element rises a little less than the reference's slack from tile to tile)
+    for s, n in enumerate(c.lengths.tolist()):
+        pg, pl = O.places(c, s, n)
+        c.k[pg, pl] = 0.0
+        c.k[pg, pl, :, 0] = (torch.arange(n)[:, None] * 0.02).half()
+    q[:] = 0.0
+    q[..., 0] = 1.0
+    check_attend(g10, c, q, scale=1.0, book=True)
