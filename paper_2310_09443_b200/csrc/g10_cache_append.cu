@@ -45,7 +45,7 @@ __global__ void __launch_bounds__(kAppendThreads, 6) k_cache_append(const Append
         to[i] = is_q ? a.q_out + 2 * (((int64_t)s * a.new_tokens * a.q_heads + head) * c.head_dim + d0)
                      : const_cast<char *>(is_k ? c.k : c.v) + 16 * head * c.head_stride + 2 * d0;
         // (those of padding too: what they hold is not used)
-        u[i] = __ldg((const uint4 *)(from[i] + 2 * t0 * (is_q ? a.q_token : is_k ? a.k_token : a.v_token)));
+        u[i] = __ldg((const uint4 *)(from[i] + 2 * (int64_t)t0 * (is_q ? a.q_token : is_k ? a.k_token : a.v_token)));
     }
     ull bad = 0;
     const int seen = __ldg(&c.seen[s]);
@@ -64,7 +64,7 @@ __global__ void __launch_bounds__(kAppendThreads, 6) k_cache_append(const Append
 #pragma unroll
             for (int i = 0; i < kEach; ++i) {
                 const int row = (share * kEach + i) * kTeams + team;
-                if (from[i] != nullptr) u[i] = __ldg((const uint4 *)(from[i] + 2 * t * (row < a.q_heads ? a.q_token : row < a.q_heads + c.kv_heads ? a.k_token : a.v_token)));
+                if (from[i] != nullptr) u[i] = __ldg((const uint4 *)(from[i] + 2 * (int64_t)t * (row < a.q_heads ? a.q_token : row < a.q_heads + c.kv_heads ? a.k_token : a.v_token)));
             }
         }
         float co[8], si[8];                              // (the first of a pair takes its partner with a minus)

@@ -57,3 +57,36 @@ def test_large_fp16_values_under_lifted_weights(g10, new, group):
     q[:] = 0.0
     q[..., 0] = 1.0
     check_attend(g10, c, q, scale=1.0, book=True)
+
+
+# ---- append ------------------------------------------------------------------------------------------------------------
+def test_append_of_more_than_2_to_the_30_tokens(g10):
+    """Offsets in 64 bits from the token's number on: 2^30 + 9 tokens of one head of 8 dims (16 GiB of keys), the values one row by a stride of zero."""
+    n, page = (1 << 30) + 9, 65536
+    pages = -(-n // page)
+    torch.cuda.empty_cache()
+    k = torch.zeros(1, n, 1, 8, dtype=torch.bfloat16, device=DEV)
+    there = [0, 1, 7, 8, 12345, n // 2, n - 18, n - 17, n - 10, n - 9, n - 8, n - 2, n - 1]
+    for t in there:
+        k[0, t] = torch.randn(8, dtype=torch.bfloat16, device=DEV)
+    v = torch.randn(1, 1, 1, 8, dtype=torch.bfloat16, device=DEV).expand(1, n, 1, 8)
+    pool_k, pool_v = (torch.zeros(pages, page, 1, 8, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    cache = g10.CacheBuffers(pool_k, pool_v, torch.arange(pages, dtype=torch.int32, device=DEV)[None], torch.tensor([n], dtype=torch.int32, device=DEV))
+    g10.g10_cache_append(cache, k, v)
+    torch.cuda.synchronize()
+    assert int(cache.status.item()) == 0
+    rows_k, rows_v = pool_k.view(-1, 8), pool_v.view(-1, 8)
+    assert all(same(rows_k[t], k[0, t, 0]) and same(rows_v[t], v[0, 0, 0]) for t in there)
+    step = 1 << 26
+    for t in range(0, n, step):
+        m = min(step, n - t)
+        assert torch.equal(rows_k[t:t + m], k[0, t:t + m, 0]) and bool((rows_v[t:t + m] == v[0, 0, 0]).all())
+    assert not rows_k[n:].any() and not rows_v[n:].any()
+    # padding that far behind the tokens that count
+    pool_k.zero_()
+    g10.g10_cache_append(cache, k, v, counts=torch.tensor([3], dtype=torch.int32, device=DEV))
+    torch.cuda.synchronize()
+    assert int(cache.status.item()) == 0
+    assert same(rows_k[n - 3:n], k[0, :3, 0]) and not rows_k[:1 << 20].any()
+    del k, v, pool_k, pool_v, rows_k, rows_v, cache
+    torch.cuda.empty_cache()
