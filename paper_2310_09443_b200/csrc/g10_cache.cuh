@@ -179,6 +179,9 @@ struct AttendArgs {
     float *sums;                         // [items][block rows] lse of every row, to base 2
     TileNote *notes;                     // [tiles]
     int64_t *total;                      // number of tiles
+#ifdef G10_TEST_HOOKS
+    int mute;                            // which arrival the first block of the kernels for many rows keeps to itself (0: none)
+#endif
 };
 // Sizes that the workspace goes by.
 struct AttendShape {

@@ -1,5 +1,6 @@
 // The C entry points of the key-value cache: argument checks, workspace layout, launches.
 #include <cmath>
+#include <cstdlib>
 #include <cstring>
 
 #include "g10_cache.cuh"
@@ -145,6 +146,11 @@ int32_t g10_cache_attend(const g10_cache *cache, const g10_cache_queries *u, voi
     a.books = u->add_scores != 0;
     a.logits = a.books && z.logit_rows > 0 ? (float *)((char *)ws + l.logits) : nullptr;
     a.sums = (float *)((char *)ws + l.sums); a.notes = (TileNote *)((char *)ws + l.notes); a.total = (int64_t *)((char *)ws + l.total);
+#ifdef G10_TEST_HOOKS
+    // test build: an arrival that never comes
+    const char *const mute = getenv("G10_TEST_CACHE_MUTE");
+    a.mute = mute ? atoi(mute) : 0;
+#endif
     return status_of(launch_cache_attend(a, cache->dtype, (cudaStream_t)stream));
 }
 

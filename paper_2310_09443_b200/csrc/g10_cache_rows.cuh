@@ -27,7 +27,7 @@ namespace attend {
 constexpr int kWideRows = 128;           // of a block
 constexpr int kRowThreads = 256, kLoadThreads = 64, kWideThreads = kRowThreads + 32 + kLoadThreads;      // 8 warps of rows, 1 that issues, 2 that load
 constexpr int kBookThreads = kRowThreads + 32 + 128;
-constexpr unsigned kWideSpins = 1u << 22;
+constexpr unsigned kWideSpins = 1u << 20;             // polls before a wait gives up (a poll that waits takes 4 us: 4 s)
 constexpr int kBlock = kTile * 128;      // bytes of 64 dimensions of a tile's keys or values
 
 // ---- barriers in shared memory; every wait has a limit ----
@@ -42,17 +42,35 @@ __device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity)
     asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Once a wait has run out anywhere in the block, none waits any more: the block goes through its tiles without them (every access stays where it
-// would be) and says so in the status word.  Whole warps wait, and leave the wait together: what follows mostly is an instruction that a warp
-// has to execute as one (a warp that had come apart in a wait read and wrote tensor memory piecemeal, which gave wrong sums and illegal instructions).
-__device__ __forceinline__ void bar_wait(unsigned bar, unsigned parity, volatile int *s_stop)
+// Waits until the barrier's phase is done; false once a wait has run out anywhere in the block.  Who is told so issues nothing more, neither products nor
+// copies nor accesses of tensor memory (what those would meet is no longer ordered), and arrives nowhere: loaders and issuer leave their loops, the row
+// threads, which meet one another, go through theirs without.  The block ends when all that it has under way is done, and says so in the status word.
+// Whole warps wait, and leave the wait together with one answer: what follows mostly is an instruction that a warp has to execute as one (a warp that had
+// come apart in a wait read and wrote tensor memory piecemeal, which gave wrong sums and illegal instructions).
+__device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity, volatile int *s_stop, unsigned limit)
 {
-    for (unsigned i = 0; i < kWideSpins; ++i) {
-        const bool done = bar_try(bar, parity) || (i > 0 && *s_stop != 0);
-        if (__all_sync(0xffffffffu, done)) return;
+    for (unsigned i = 0; i < limit; ++i) {
+        if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
+        if (__any_sync(0xffffffffu, *s_stop != 0)) return false;
     }
     *s_stop = 1;
     __syncwarp();
+    return false;
+}
+// The limit, in polls.  (Test build: the first block keeps one of its arrivals to itself, and its waits are short.)
+__device__ __forceinline__ unsigned wait_limit(const AttendArgs &a)
+{
+#ifdef G10_TEST_HOOKS
+    if (a.mute != 0 && blockIdx.x == 0) return 1u << 10;
+#endif
+    return kWideSpins;
+}
+__device__ __forceinline__ bool muted(const AttendArgs &a, int what, int tile)
+{
+#ifdef G10_TEST_HOOKS
+    return a.mute == what && blockIdx.x == 0 && tile == 1;
+#endif
+    return false;
 }
 
 // ---- tensor memory and products ----
@@ -204,7 +222,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
     typedef Wide<kDims> C;
     constexpr int S = C::kStages;
     extern __shared__ char smem_raw[];
-    __shared__ __align__(8) uint64_t s_bar[2 * S + 9];
+    __shared__ __align__(8) uint64_t s_bar[2 * S + 10];
     __shared__ Place s_place;
     __shared__ int s_stop, s_apart[2];
     __shared__ float2 s_ml[2][kWideRows];
@@ -221,19 +239,21 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
     if (n == 0) return;
     bad = 0;
     place_of(a, tally, begin, per, &s_place);
-    const unsigned full = smem_of(s_bar), free_ = full + 8 * S, s_full = free_ + 8 * S, w_full = s_full + 16, q_full = w_full + 16, v_done = q_full + 8, s_free = v_done + 16;
+    const unsigned full = smem_of(s_bar), free_ = full + 8 * S, s_full = free_ + 8 * S, w_full = s_full + 16, q_full = w_full + 16, v_done = q_full + 8, s_free = v_done + 16, at_end = s_free + 16;
     if (tid == 0) {
         s_stop = 0;
         for (int i = 0; i < S; ++i) { bar_init(full + 8 * i, kLoadThreads); bar_init(free_ + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(w_full + 8 * i, 128); bar_init(v_done + 8 * i, 1); bar_init(s_free + 8 * i, 128); }
         bar_init(q_full, kRowThreads);
+        bar_init(at_end, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 8) tmem_take(&s_tmem, C::kColumns);
     before_sync();
     __syncthreads();
     after_sync();
-    const unsigned tmem = s_tmem;
+    const unsigned tmem = s_tmem, limit = wait_limit(a);
+    auto wait = [&](unsigned bar, unsigned parity) -> bool { return bar_wait(bar, parity, &s_stop, limit); };
     char *const s_q = (char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     char *const s_ring = s_q + C::kQBytes;
     Cursor now;
@@ -267,7 +287,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
         for (int u = 0; u < n; ++u) {
             const unsigned mine = row_found();
             if (u + 1 < n) { cursor_next(a, now, per); look_up(); }
-            bar_wait(free_ + 8 * stage, round, &s_stop);
+            if (!wait(free_ + 8 * stage, round)) break;
             const unsigned told = full + 8 * stage, to = smem_of(s_ring) + stage * C::kStageBytes;
             if (++stage == S) { stage = 0; round ^= 1; }
             const bool all = __all_sync(0xffffffffu, mine != kNone) && a.c.head_dim == C::kDim && a.row_blocks == 1;
@@ -291,9 +311,10 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                     copy16_or_zeros(to + kDims * kBlock + at, a.c.v + x, real);
                 }
             }
-            bar_arrive_landed(told);
+            if (!muted(a, 1, u)) bar_arrive_landed(told);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
+        if (s_stop != 0) __nanosleep(10000);             // (for the arrivals that the copies bring about, which nobody waits for then)
         if (bad != 0) raise_status(a.c.status, bad);
     } else if (warp == 8) {
         // ---- the issuer: the warp goes through the tiles together, one thread of it issues ----
@@ -306,9 +327,9 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
         unsigned round = 0;
         bool first = true;                               // of its piece
         int pieces = 0;
-        auto take_values = [&]() {
+        auto take_values = [&]() -> bool {
             const int v = taken;
-            bar_wait(w_full + 8 * (v & 1), (v >> 1) & 1, &s_stop);
+            if (!wait(w_full + 8 * (v & 1), (v >> 1) & 1)) return false;
             after_sync();
             if (leads) {
                 if (s_apart[v & 1] == 0) {
@@ -324,17 +345,19 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
             __syncwarp();
             ++taken;
             taken_stage = taken_stage == S - 1 ? 0 : taken_stage + 1;
+            return true;
         };
+        bool going = true;
         for (int u = 0; u < n; ++u) {
             if (first) {                                 // (the rows bring new queries once they have seen all of the piece before, and wait for its products)
-                while (taken < u) take_values();
-                bar_wait(q_full, pieces & 1, &s_stop);
+                while (going && taken < u) going = take_values();
+                if (!going || !wait(q_full, pieces & 1)) { going = false; break; }
                 ++pieces;
                 start = u;
             }
-            bar_wait(full + 8 * stage, round, &s_stop);
+            if (!wait(full + 8 * stage, round)) { going = false; break; }
             async_sees();
-            if (u >= 2) bar_wait((C::kOwnWeights ? s_free : v_done) + 8 * (u & 1), ((u >> 1) - 1) & 1, &s_stop);
+            if (u >= 2 && !wait((C::kOwnWeights ? s_free : v_done) + 8 * (u & 1), ((u >> 1) - 1) & 1)) { going = false; break; }
             after_sync();
             if (leads) {
                 const unsigned to = tmem + C::kLogits + (u & 1) * kTile;
@@ -343,17 +366,21 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
 #pragma unroll
                 for (int k = 0; k < 4 * kDims; ++k)
                     multiply(to, q_operand + (unsigned)(((k >> 2) * kWideRows * 128 + (k & 3) * 32) >> 4), at + (unsigned)(((k >> 2) * kBlock + (k & 3) * 32) >> 4), keys, k > 0);
-                tell_when_done(s_full + 8 * (u & 1));
+                if (!muted(a, 3, u)) tell_when_done(s_full + 8 * (u & 1));
             }
             __syncwarp();
-            while (taken <= u - C::kBehind) take_values();
+            while (going && taken <= u - C::kBehind) going = take_values();
+            if (!going) break;
             if (++stage == S) { stage = 0; round ^= 1; }
             first = now.idx == now.q.tiles - 1;
             cursor_next(a, now, per);
         }
-        while (taken < n) take_values();
-        // (nothing is given back before the last product is done, stopped or not)
-        for (unsigned i = 0; i < kWideSpins && !bar_try(v_done + 8 * ((n - 1) & 1), ((n - 1) >> 1) & 1); ++i) {}
+        while (going && taken < n) going = take_values();
+        // (nothing is given back before the last product is done, stopped or not; a barrier that is used once, since who has not waited for all phases of
+        // another cannot tell them apart)
+        if (leads) tell_when_done(at_end);
+        __syncwarp();
+        for (unsigned i = 0; i < kWideSpins && !bar_try(at_end, 0); ++i) {}
         __syncwarp();
     } else {
         // ---- rows: a thread of each team each ----
@@ -361,9 +388,10 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
         const unsigned mine = tmem + ((unsigned)((warp & 3) * 32) << 16), own = mine + (C::kTeams == 2 ? team * C::kDim : 0);
         const float scale = fabsf(a.scale_log2);
         constexpr int kHalf = C::kDim / 2;               // columns that this thread joins
+        bool going = true;                               // (the warp alike)
         bring_queries<kDims>(a, now, now.block * kWideRows, r, team, s_q);
         async_sees();
-        bar_arrive(q_full);
+        if (!(muted(a, 6, 1) && tid == 0)) bar_arrive(q_full);
         for (int u0 = 0; u0 < n;) {
             // ---- a piece: tiles u0 .. u1 - 1 ----
             const int u1 = u0 + min(now.q.tiles - now.idx, n - u0);
@@ -379,13 +407,14 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                 const unsigned logits = mine + C::kLogits + b * kTile;
                 auto products_so_far = [&]() {           // (those of this team)
                     const int v = u - C::kTeams;
-                    bar_wait(v_done + 8 * (v & 1), (v >> 1) & 1, &s_stop);
+                    going = going && wait(v_done + 8 * (v & 1), (v >> 1) & 1);
                     after_sync();
                 };
-                bar_wait(s_full + 8 * b, (u >> 1) & 1, &s_stop);
+                going = going && wait(s_full + 8 * b, (u >> 1) & 1);
                 after_sync();
                 float2 x[kTile / 2];
-                if (busy) {
+                if (!going) {
+                } else if (busy) {
                     auto load = [&]() {
                         logits_load(x, logits);
                         logits_load(x + 16, logits + 32);
@@ -413,7 +442,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                         if (!first) {
                             products_so_far();
 #pragma unroll 1
-                            for (int c = 0; c < C::kDim; c += 32) {
+                            for (int c = 0; c < C::kDim && going; c += 32) {
                                 unsigned o[32];
                                 tmem_load(o, own + c);
                                 tmem_loaded();
@@ -421,7 +450,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                                 for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * by);
                                 tmem_store(o, own + c);
                             }
-                            tmem_stored();
+                            if (going) tmem_stored();
                         }
                     }
                     const float ref = m == -INFINITY ? 0.0f : m;
@@ -450,20 +479,20 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                 bool apart = false;
                 if (!whole && now.q.count > 1) {
                     // Slots that only some rows see: a weight of zero times an infinite or undefined value is not zero.
-                    bar_wait(full + 8 * (u % S), (u / S) & 1, &s_stop);
+                    going = going && wait(full + 8 * (u % S), (u / S) & 1);
                     const char *const values = s_ring + (u % S) * C::kStageBytes + kDims * kBlock;
                     for (int i = r; i < kDims * kBlock / 4; i += 128) {
                         const float2 f = Pair<T>::unpack(*(const unsigned *)(values + 4 * i));
                         apart |= !(fabsf(f.x) <= 3.4028235e38f) || !(fabsf(f.y) <= 3.4028235e38f);
                     }
                     apart = any_of_team(team, apart);
-                    if (apart && busy) {                 // the tile's products one by one, of what each row sees
+                    if (apart && busy && going) {        // the tile's products one by one, of what each row sees
                         float weight[kTile];
 #pragma unroll
                         for (int j = 0; j < kTile / 2; ++j) { weight[2 * j] = x[j].x; weight[2 * j + 1] = x[j].y; }
                         if (!first) products_so_far();
 #pragma unroll 1
-                        for (int c = 0; c < C::kDim; c += 32) {
+                        for (int c = 0; c < C::kDim && going; c += 32) {
                             unsigned o[32];
 #pragma unroll
                             for (int i = 0; i < 32; ++i) o[i] = 0u;
@@ -487,14 +516,14 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                             }
                             tmem_store(o, own + c);
                         }
-                        tmem_stored();
+                        if (going) tmem_stored();
                     }
                 }
                 if (C::kOwnWeights && u >= 2) {          // (the columns that W goes to: the product with W of tile u - 2 is done)
-                    bar_wait(v_done + 8 * b, ((u >> 1) - 1) & 1, &s_stop);
+                    going = going && wait(v_done + 8 * b, ((u >> 1) - 1) & 1);
                     after_sync();
                 }
-                if (!apart && busy) {
+                if (!apart && busy && going) {
                     unsigned w[kTile / 2];
 #pragma unroll
                     for (int j = 0; j < kTile / 2; ++j) w[j] = Pair<T>::pack(x[j].x, x[j].y);
@@ -503,7 +532,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                 }
                 if (r == 0) s_apart[b] = apart ? 1 : 0;
                 before_sync();
-                bar_arrive(w_full + 8 * b);
+                if (going && !(muted(a, 2, u) && r == 0)) bar_arrive(w_full + 8 * b);
                 first = false;
             }
             // ---- the piece's end: the teams' parts are joined, half of the columns by each ----
@@ -515,11 +544,13 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
             if (u1 < n) {                                // (a piece that is not the last ends with its item)
                 now.idx = now.q.tiles - 1;
                 cursor_next(a, now, per);
-                bring_queries<kDims>(a, now, now.block * kWideRows, r, team, s_q);
-                async_sees();
-                bar_arrive(q_full);
+                if (going) {
+                    bring_queries<kDims>(a, now, now.block * kWideRows, r, team, s_q);
+                    async_sees();
+                    bar_arrive(q_full);
+                }
             }
-            for (int v = max(u0, u1 - 2); v < u1; ++v) bar_wait(v_done + 8 * (v & 1), (v >> 1) & 1, &s_stop);
+            for (int v = max(u0, u1 - 2); v < u1; ++v) going = going && wait(v_done + 8 * (v & 1), (v >> 1) & 1);
             after_sync();
             const float2 one = s_ml[0][r], two = s_ml[1][r];
             const float top = fmaxf(one.x, two.x), ref = top == -INFINITY ? 0.0f : top;
@@ -533,7 +564,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                     if (a.books) a.sums[item * kWideRows + r] = sum == 0.0f ? INFINITY : lse;
                 }
             }
-            if (busy) {
+            if (busy && going) {
 #pragma unroll 1
                 for (int c = team * kHalf; c < (team + 1) * kHalf; c += 32) {
                     unsigned o[32];
@@ -602,7 +633,7 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
     typedef Book<kDims> C;
     constexpr int S = C::kStages;
     extern __shared__ char smem_raw[];
-    __shared__ __align__(8) uint64_t s_bar[2 * S + 5];
+    __shared__ __align__(8) uint64_t s_bar[2 * S + 6];
     __shared__ Place s_place;
     __shared__ int s_stop, s_p[kWideRows];
     __shared__ __align__(16) float s_off[kWideRows];     // - lse of each row, to base 2
@@ -623,12 +654,13 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
     }
     bad = 0;
     place_of<2>(one, tally, begin, heads, &s_place);
-    const unsigned full = smem_of(s_bar), free_ = full + 8 * S, d_full = free_ + 8 * S, d_free = d_full + 16, q_full = d_free + 16;
+    const unsigned full = smem_of(s_bar), free_ = full + 8 * S, d_full = free_ + 8 * S, d_free = d_full + 16, q_full = d_free + 16, at_end = q_full + 8;
     if (tid == 0) {
         s_stop = 0;
         for (int i = 0; i < S; ++i) { bar_init(full + 8 * i, 128); bar_init(free_ + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { bar_init(d_full + 8 * i, 1); bar_init(d_free + 8 * i, 128); }
         bar_init(q_full, kRowThreads);
+        bar_init(at_end, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     // (the kernel before lets this one begin once it has nothing but its last, short part left: tensor memory may be taken, and limited waits begun)
@@ -636,7 +668,8 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
     before_sync();
     __syncthreads();
     after_sync();
-    const unsigned tmem = s_tmem;
+    const unsigned tmem = s_tmem, limit = wait_limit(a);
+    auto wait = [&](unsigned bar, unsigned parity) -> bool { return bar_wait(bar, parity, &s_stop, limit); };
     char *const s_q = (char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
     char *const s_ring = s_q + C::kQBytes;
     Cursor now;
@@ -666,7 +699,7 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
         for (int u = 0; u < n; ++u) {
             const unsigned mine = row_found();
             if (u + 1 < n) { cursor_next<2>(one, now, heads); look_up(); }
-            bar_wait(free_ + 8 * stage, round, &s_stop);
+            if (!wait(free_ + 8 * stage, round)) break;
             const unsigned told = full + 8 * stage, to = smem_of(s_ring) + stage * C::kStageBytes;
             if (++stage == S) { stage = 0; round ^= 1; }
             const bool all = __all_sync(0xffffffffu, mine != kNone) && a.c.head_dim == C::kDim;
@@ -686,9 +719,10 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
                     copy16_or_zeros(to + swizzled(part * 32 + row, unit, 128 * 128), a.c.k + (real ? 16 * ((int64_t)from + unit) : 0), real);
                 }
             }
-            bar_arrive_landed(told);
+            if (!muted(a, 4, u)) bar_arrive_landed(told);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
+        if (s_stop != 0) __nanosleep(10000);             // (for the arrivals that the copies bring about, which nobody waits for then)
         if (bad != 0) raise_status(a.c.status, bad);
     } else if (warp == 8) {
         const bool leads = elected();
@@ -697,14 +731,15 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
         bool fresh = true;
         int stage = 0;
         unsigned round = 0;
-        for (int u = 0, d = 0; u < n; ++u) {
-            bar_wait(full + 8 * stage, round, &s_stop);
+        bool going = true;
+        for (int u = 0, d = 0; u < n && going; ++u) {
+            going = wait(full + 8 * stage, round);
             async_sees();
-            for (int b = 0; b < blocks; ++b, ++d) {
-                if (fresh || blocks > 1) { bar_wait(q_full, given & 1, &s_stop); ++given; }      // (brought for every run)
+            for (int b = 0; b < blocks && going; ++b, ++d) {
+                if (fresh || blocks > 1) { going = wait(q_full, given & 1); ++given; }           // (brought for every run)
                 fresh = false;
-                if (d >= 2) bar_wait(d_free + 8 * (d & 1), ((d >> 1) - 1) & 1, &s_stop);
-                __syncwarp();
+                if (d >= 2) going = going && wait(d_free + 8 * (d & 1), ((d >> 1) - 1) & 1);
+                if (!going) break;
                 after_sync();
                 if (leads) {
                     const int rows = min(kWideRows, a.rows - b * kWideRows);
@@ -722,8 +757,9 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
             fresh = now.idx == now.q.tiles - 1;
             cursor_next<2>(one, now, heads);
         }
-        const int last = n * blocks - 1;
-        for (unsigned i = 0; i < kWideSpins && !bar_try(d_full + 8 * (last & 1), (last >> 1) & 1); ++i) {}
+        if (leads) tell_when_done(at_end);               // (as above)
+        __syncwarp();
+        for (unsigned i = 0; i < kWideSpins && !bar_try(at_end, 0); ++i) {}
         __syncwarp();
     } else {
         // ---- slots: a thread each; the two teams take the pairs of tiles in turn ----
@@ -731,14 +767,17 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
         const unsigned mine = tmem + ((unsigned)((warp & 3) * 32) << 16);
         const float scale = fabsf(a.scale_log2);
         asm volatile("griddepcontrol.wait;" ::: "memory");       // (for each lse; the keys are on their way meanwhile)
+        bool going = true;                               // (the warp alike)
         auto bring = [&](int b) {                        // queries, lse and places of block b's rows
             const int row = b * kWideRows + r, t = row / a.group;
-            bring_queries<kDims>(a, now, b * kWideRows, r, team, s_q);
-            const bool real = row < a.rows && t < now.q.count;
-            if (team == 0) s_p[r] = real ? now.q.length - now.q.count + t : -1;
-            else s_off[r] = real ? -__ldcg(&a.sums[((int64_t)now.s * heads * blocks + now.head * blocks + b) * kWideRows + r]) : -INFINITY;
-            async_sees();
-            bar_arrive(q_full);
+            if (going) {
+                bring_queries<kDims>(a, now, b * kWideRows, r, team, s_q);
+                const bool real = row < a.rows && t < now.q.count;
+                if (team == 0) s_p[r] = real ? now.q.length - now.q.count + t : -1;
+                else s_off[r] = real ? -__ldcg(&a.sums[((int64_t)now.s * heads * blocks + now.head * blocks + b) * kWideRows + r]) : -INFINITY;
+                async_sees();
+                bar_arrive(q_full);
+            }
             rows_meet();
         };
         for (int u = 0, d = 0; u < n;) {
@@ -759,7 +798,8 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
                         spot = slot < now.q.length ? cache_spot(a.c, now.s, slot, bad) : Spot{-1, 0};
                         sum = 0.0f;
                     }
-                    bar_wait(d_full + 8 * (d & 1), (d >> 1) & 1, &s_stop);
+                    going = going && wait(d_full + 8 * (d & 1), (d >> 1) & 1);
+                    if (!going) continue;
                     after_sync();
                     float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
                     const float2 by = make_float2(scale, scale);
@@ -791,7 +831,7 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
                         }
                     }
                     before_sync();
-                    bar_arrive(d_free + 8 * (d & 1));
+                    if (!(muted(a, 5, d) && r == 0)) bar_arrive(d_free + 8 * (d & 1));
                     part[0] = add2(part[0], part[1]);
                     sum += part[0].x + part[0].y;
                     if (b == blocks - 1 && spot.page >= 0 && sum != 0.0f) atomicAdd(&a.c.scores[cache_cell(a.c, spot, now.head)], sum);

@@ -1,5 +1,6 @@
 """The key-value cache on the device at the edges of what its calls allow, against the definitions in 64 bits (cache_oracle.py)."""
 import math
+import time
 from types import SimpleNamespace
 
 import pytest
@@ -90,3 +91,50 @@ def test_append_of_more_than_2_to_the_30_tokens(g10):
     assert same(rows_k[n - 3:n], k[0, :3, 0]) and not rows_k[:1 << 20].any()
     del k, v, pool_k, pool_v, rows_k, rows_v, cache
     torch.cuda.empty_cache()
+
+
+# ---- waits that run out ------------------------------------------------------------------------------------------------
+@pytest.fixture
+def hooks(monkeypatch):
+    """The test build of the library (-DG10_TEST_HOOKS), in which an environment variable names an arrival that the first block of the kernels for many rows
+    keeps to itself; that block's waits are short."""
+    from paper_2310_09443_b200 import binding, build
+    monkeypatch.setattr(binding, "LIB_PATH", build.build(hooks=True))
+    monkeypatch.setattr(binding, "_lib", None)
+    monkeypatch.delenv("G10_TEST_CACHE_MUTE", raising=False)
+    binding.load_library()
+    return binding
+
+
+@pytest.mark.parametrize("dim", [64, 128, 192, 256])
+@pytest.mark.parametrize("new,group", [(1, 20), (20, 8)])
+def test_a_wait_that_runs_out(hooks, monkeypatch, dim, new, group):
+    """A tile that is never told full, weights, logits, queries or room for logits that are never told of, in either kernel: the block gives up, the call
+    returns with the timeout bit, nothing is written out of place, and the next call is right.  Nothing traps, faults or spins on."""
+    c = O.make_cache([9000, 700, 2500 + new], 8, dim, 64, torch.bfloat16, dim + group)
+    q = queries(c, new, group, 3)
+    dq = q.to(DEV)
+    r = O.attend(c, q, dim ** -0.5)
+    bound, _, rel = O.attend_bounds(c, r)
+    around = torch.full((2 * dq.numel(),), 7.0, dtype=dq.dtype, device=DEV)
+    out = around[dq.numel() // 2:][:dq.numel()].view(dq.shape)
+    size = hooks.g10_cache_workspace_bytes(O.upload(hooks, c), new, 8 * group, add_scores=True)
+    ws = torch.zeros(size + 1024, dtype=torch.uint8, device=DEV)
+    for mute in (0, 1, 2, 3, 4, 5, 6, 0):
+        monkeypatch.setenv("G10_TEST_CACHE_MUTE", str(mute))
+        cache = O.upload(hooks, c)
+        t0 = time.perf_counter()
+        hooks.g10_cache_attend(cache, dq, out=out, ws=ws[:size], add_scores=True)
+        torch.cuda.synchronize()
+        took = time.perf_counter() - t0
+        assert int(cache.status.item()) == (0 if mute == 0 else 0x80), mute
+        assert took < 1.0, (mute, took)
+        assert (around[:dq.numel() // 2] == 7).all() and (around[dq.numel() // 2 + dq.numel():] == 7).all() and not ws[size:].any()
+        assert same(cache.k, c.k) and same(cache.v, c.v)
+        if mute == 0:
+            assert ((out.cpu().double() - r.out).abs() <= bound).all()
+            got = cache.scores.cpu()
+            for (s, h), w in r.booked.items():
+                pg, pl = O.places(c, s, len(w))
+                was = c.scores[pg, h, pl].double()
+                assert ((got[pg, h, pl].double() - was - w).abs() <= w * float(rel[s].max()) * 1.01 + 2.0 ** -23 * (was + w)).all()
