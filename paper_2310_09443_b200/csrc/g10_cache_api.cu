@@ -35,6 +35,8 @@ int32_t view_of(const g10_cache *c, bool rows, CacheView &o)
         if (last / 8 + 32 >= 0xffffffffll) return G10_ERR_LIMIT;
     }
     o.k = (const char *)c->k; o.v = (const char *)c->v;
+    // (copies of no bytes, for slots whose page is none, are asked for from there all the same: an address that exists)
+    if (c->num_pages == 0) o.k = o.v = (const char *)((uintptr_t)c->status & ~(uintptr_t)15);
     o.page_stride = c->page_stride / 8; o.slot_stride = c->slot_stride / 8; o.head_stride = c->head_stride / 8;
     int l = 0;
     while ((1 << l) < c->page_size) ++l;
@@ -128,7 +130,7 @@ int32_t g10_cache_attend(const g10_cache *cache, const g10_cache_queries *u, voi
     if (!u) return G10_ERR_ARG;
     rc = check_heads(a.c, u->new_tokens, u->q_heads, u->window, u->sinks);
     if (rc != G10_OK) return rc;
-    if ((u->window > 0 && cache->positions) || (u->add_scores && !cache->scores) || !std::isfinite(u->scale * kLog2E)) return G10_ERR_ARG;
+    if ((u->window > 0 && cache->positions) || (u->add_scores && cache->num_pages > 0 && !cache->scores) || !std::isfinite(u->scale * kLog2E)) return G10_ERR_ARG;
     if (a.c.num_seqs == 0) return G10_OK;
     if (!u->q || !u->out || !aligned16(u->q) || !aligned16(u->out) || !row_stride(u->q_seq_stride) || !row_stride(u->q_token_stride) ||
         !row_stride(u->q_head_stride))

@@ -955,7 +955,7 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     if (cluster == 0 && (e = cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, (int)held, C::kDim, C::kRows)) != cudaSuccess) return e;
     if (a.logits == nullptr) return cudaSuccess;
     const int64_t warps = kJoinThreads / 32, blocks = (z.tiles + warps - 1) / warps, most = 148 * 6;
-    cfg.gridDim = dim3((unsigned)(blocks < most ? blocks : most));
+    cfg.gridDim = dim3((unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most));      // (a table without columns: no tile)
     const int pitch = logit_rows(C::kRows < a.rows ? C::kRows : a.rows);
     const auto book = pitch <= 4 ? k_cache_book<1> : pitch <= 8 ? k_cache_book<2> : pitch <= 16 ? k_cache_book<4> : k_cache_book<8>;
     return cudaLaunchKernelEx(&cfg, book, a, C::kRows, cluster == 0);

@@ -93,6 +93,39 @@ def test_append_of_more_than_2_to_the_30_tokens(g10):
     torch.cuda.empty_cache()
 
 
+# ---- tables without columns, pools without pages ----------------------------------------------------------------------
+@pytest.mark.parametrize("new,group", [(1, 2), (1, 12), (4, 6)])
+@pytest.mark.parametrize("pages", [0, 3])
+@pytest.mark.parametrize("columns", [0, 2])
+def test_nothing_to_look_at(g10, new, group, pages, columns):
+    """Before the first page is given out.  Lengths of zero; or, where there are columns, lengths whose pages are none: read as zeros."""
+    on = dict(device=DEV)
+    k = torch.randn(pages, 16, 2, 64, **on).to(torch.bfloat16)
+    cells = (pages, 2, 16)
+    scores, positions = torch.rand(cells, **on), torch.zeros(cells, dtype=torch.int32, **on)
+    before = [x.clone() for x in (k, scores)]
+    table = torch.full((3, columns), -1, dtype=torch.int32, **on)
+    for lengths in ([0, 0, 0],) if columns == 0 else ([0, 0, 0], [0, 5, 32]):
+        cache = g10.CacheBuffers(k, k.clone(), table, torch.tensor(lengths, dtype=torch.int32, **on), scores=scores, positions=positions)
+        q = torch.randn(3, new, 2 * group, 64, **on).to(torch.bfloat16)
+        out, lse = torch.full_like(q, 9.0), torch.full(q.shape[:3], 9.0, **on)
+        g10.g10_cache_attend(cache, q, add_scores=True, out=out, lse=lse)
+        rows = torch.randn(3, new, 2, 64, **on).to(torch.bfloat16)
+        q_out = g10.g10_cache_append(cache, rows, rows, q)
+        p = g10.g10_cache_plan_evictions(cache, 4, 1, 1)
+        g10.g10_cache_evict(cache, p.moves, p.counts)
+        torch.cuda.synchronize()
+        assert int(cache.status.item()) == (0x400 if any(lengths) else 0)
+        assert not out.any() and p.new_lengths.tolist() == [min(n, 4) for n in lengths]
+        for s, n in enumerate(lengths):
+            count = min(n, new)
+            assert not q_out[s, count:].any() and same(q_out[s, :count], q[s, :count])
+            for t in range(new):
+                want = math.log(n - count + t + 1) if t < count else -math.inf
+                assert torch.allclose(lse[s, t].double().cpu(), torch.tensor(want, dtype=torch.float64), rtol=2.0 ** -20, atol=2.0 ** -20)
+        assert same(k, before[0]) and same(scores, before[1])
+
+
 # ---- waits that run out ------------------------------------------------------------------------------------------------
 @pytest.fixture
 def hooks(monkeypatch):
