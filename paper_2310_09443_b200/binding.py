@@ -566,8 +566,13 @@ class CacheBuffers:
         self.device = lengths.device
         if not lengths.is_cuda:
             raise G10Error("the cache has to be on a CUDA device")
-        self.status = torch.zeros(1, dtype=torch.int64, device=self.device) if status is None else status
         self.index = index = self.device.index
+        self.status = status
+        if status is None:
+            with torch.cuda.device(index):
+                self.status = torch.zeros(1, dtype=torch.int64, device=self.device)
+                if not torch.cuda.is_current_stream_capturing():   # (a first call on another stream finds it cleared)
+                    torch.cuda.current_stream().synchronize()
         for t in (k, v, page_table):
             if t is not None and t.get_device() != index:
                 raise G10Error("all tensors of the cache have to be on %s: got one on %s" % (self.device, t.device))

@@ -126,6 +126,26 @@ def test_nothing_to_look_at(g10, new, group, pages, columns):
         assert same(k, before[0]) and same(scores, before[1])
 
 
+# ---- the status word -----------------------------------------------------------------------------------------------------
+def test_a_status_word_made_here_is_cleared_before_the_first_call(g10):
+    """Work that waits on the current stream does not clear it after a call on another stream has written to it."""
+    c = O.make_cache([40, 40], 2, 64, 16, torch.bfloat16, 3, scores=False)
+    k, v, table = c.k.to(DEV), c.v.to(DEV), c.table.to(DEV)
+    lengths = torch.tensor([40, 49], dtype=torch.int32, device=DEV)          # (49: more than the table has room for)
+    q = queries(c, 1, 2, 1).to(DEV)
+    side = torch.cuda.Stream()
+    out, lse = torch.empty_like(q), torch.empty(q.shape[:3], device=DEV)
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device=DEV)
+    word = torch.zeros(1, dtype=torch.int64, device=DEV)
+    g10.g10_cache_attend(g10.CacheBuffers(k, v, table, lengths, status=word), q, out=out, lse=lse, ws=ws, stream=side)      # (all is loaded)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(40_000_000)
+    cache = g10.CacheBuffers(k, v, table, lengths)
+    g10.g10_cache_attend(cache, q, out=out, lse=lse, ws=ws, stream=side)
+    torch.cuda.synchronize()
+    assert int(cache.status.item()) == 0x800
+
+
 # ---- waits that run out ------------------------------------------------------------------------------------------------
 @pytest.fixture
 def hooks(monkeypatch):
