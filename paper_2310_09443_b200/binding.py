@@ -540,6 +540,16 @@ def _typed(name, t, dtype, shape, device):
             name, dtype, tuple(shape), device, t.dtype, tuple(t.shape), t.stride(), t.device))
 
 
+_MOST = 0x7fffffff
+
+
+def _fits(**numbers):
+    """Numbers that the C structs hold in 32 bits (ctypes would cut longer ones down without a word)."""
+    for name, n in numbers.items():
+        if not -_MOST <= n <= _MOST:
+            raise G10Error("%s does not fit 32 bits: %d" % (name, n))
+
+
 def _rows(name, t, cache, heads=None):
     """Shape and strides of a tensor [seqs, new_tokens, heads, head_dim] of the cache's type, the last stride 1."""
     shape, strides = t.shape, t.stride()
@@ -602,6 +612,7 @@ class CacheBuffers:
             _typed("scores", scores, torch.float32, cells, index)
         if positions is not None:
             _typed("positions", positions, torch.int32, cells, index)
+        _fits(sequences=self.num_seqs, columns=int(page_table.shape[1]), page_size=self.page_size, kv_heads=self.kv_heads, head_dim=self.head_dim)
         strides = k.stride() if k is not None else (0, 0, 0, 1)
         self.c_struct = _Cache(_CACHE_TYPES[self.dtype], self.num_seqs, self.kv_heads, self.head_dim, self.page_size, int(page_table.shape[1]),
                                self.num_pages, _ptr(k), _ptr(v), strides[0], strides[1], strides[2], _ptr(page_table), int(page_table.stride(0)),
@@ -653,6 +664,8 @@ def g10_cache_append(cache: CacheBuffers, k, v, q=None, q_weight=None, k_weight=
             _typed("q_out", q_out, cache.dtype, q_shape, dev)
     if v_shape[1] != new or (heads and q_shape[1] != new):
         raise G10Error("q, k and v have to hold as many tokens")
+    if new > _MOST or heads > _MOST:
+        _fits(new_tokens=new, q_heads=heads)
     if q_weight is not None:
         _typed("q_weight", q_weight, cache.dtype, (cache.head_dim,), dev)
     if k_weight is not None:
@@ -662,6 +675,8 @@ def g10_cache_append(cache: CacheBuffers, k, v, q=None, q_weight=None, k_weight=
         if cos is None or sin is None or cos.dim() != 2:
             raise G10Error("cos and sin come together, float32 [positions, rotary_dim / 2]")
         rows, half = cos.shape
+        if 2 * half > _MOST:
+            _fits(rotary_dim=2 * half)
         _typed("cos", cos, torch.float32, (rows, half), dev)
         _typed("sin", sin, torch.float32, (rows, half), dev)
     if counts is not None:
@@ -674,6 +689,7 @@ def g10_cache_append(cache: CacheBuffers, k, v, q=None, q_weight=None, k_weight=
 
 def g10_cache_workspace_bytes(cache: CacheBuffers, new_tokens, q_heads, window=0, sinks=0, add_scores=False) -> int:
     """Bytes of workspace that g10_cache_attend needs."""
+    _fits(new_tokens=new_tokens, q_heads=q_heads, window=window, sinks=sinks)
     out = C.c_size_t(0)
     _check(load_library().g10_cache_workspace_bytes(cache.ref, new_tokens, q_heads, window, sinks, 1 if add_scores else 0, C.byref(out)))
     return int(out.value)
@@ -687,6 +703,8 @@ def g10_cache_attend(cache: CacheBuffers, q, scale=None, window=0, sinks=0, coun
     captured graphs among them, need one each."""
     shape, qs = _rows("q", q, cache)
     dev, new, heads = cache.index, shape[1], shape[2]
+    if max(new, heads, window, sinks) > _MOST or min(window, sinks) < 0:
+        _fits(new_tokens=new, q_heads=heads, window=window, sinks=sinks)
     if out is None:
         out = _cache_empty(cache, shape, q.dtype, stream)
     else:
@@ -718,6 +736,8 @@ def g10_cache_plan_evictions(cache: CacheBuffers, budget, sinks=0, recent=0, mov
     """Plans which `budget` slots of each (sequence, key-value head) stay: positions below `sinks` and the last `recent` first, then the largest
     scores.  Returns moves int32 [seqs, kv_heads, budget, 2] (source, target slot; valid up to the count), counts int32 [seqs, kv_heads] and
     new_lengths int32 [seqs]; changes nothing else."""
+    if max(budget, sinks, recent) > _MOST or min(budget, sinks, recent) < 0:
+        _fits(budget=budget, sinks=sinks, recent=recent)
     if moves is None:
         moves = _cache_empty(cache, (cache.num_seqs, cache.kv_heads, max(budget, 0), 2), torch.int32, stream)
     if counts is None:
@@ -732,7 +752,10 @@ def g10_cache_plan_evictions(cache: CacheBuffers, budget, sinks=0, recent=0, mov
 def g10_cache_evict(cache: CacheBuffers, moves, counts, stream=None):
     """Carries the moves of a plan out (rows of k and v, scores, positions).  cache.lengths still are those that the plan was made for; the
     program takes new_lengths over once every layer has been evicted."""
-    p = _cache_plan(cache, int(moves.shape[2]) if moves.dim() == 4 else 0, 0, 0, moves, counts, None)
+    budget = int(moves.shape[2]) if moves.dim() == 4 else 0
+    if budget > _MOST:
+        _fits(budget=budget)
+    p = _cache_plan(cache, budget, 0, 0, moves, counts, None)
     _cache_call(load_library().g10_cache_evict, cache, (p,), stream)
 
 

@@ -146,6 +146,28 @@ def test_a_status_word_made_here_is_cleared_before_the_first_call(g10):
     assert int(cache.status.item()) == 0x800
 
 
+# ---- numbers of more than 32 bits ------------------------------------------------------------------------------------------
+def test_numbers_that_do_not_fit_are_refused(g10):
+    """A window of 2^32 + 5 is not one of 5."""
+    c = O.make_cache([40], 1, 64, 16, torch.bfloat16, 3)
+    cache = O.upload(g10, c)
+    big = 2 ** 32 + 5
+    q = torch.zeros(1, 1, 2, 64, dtype=torch.bfloat16, device=DEV)
+    kv = torch.zeros(1, 1, 1, 64, dtype=torch.bfloat16, device=DEV)
+    many = kv.expand(1, big, 1, 64)
+    before = [x.clone() for x in (cache.k, cache.v, cache.scores)]
+    calls = [lambda: g10.g10_cache_attend(cache, q, window=big), lambda: g10.g10_cache_attend(cache, q, window=4, sinks=big),
+             lambda: g10.g10_cache_attend(cache, q, window=-2 ** 32 + 5), lambda: g10.g10_cache_workspace_bytes(cache, 1, 2, window=big),
+             lambda: g10.g10_cache_workspace_bytes(cache, big, 2), lambda: g10.g10_cache_append(cache, many, many),
+             lambda: g10.g10_cache_plan_evictions(cache, 8, recent=2 ** 32), lambda: g10.g10_cache_plan_evictions(cache, 8, sinks=2 ** 32),
+             lambda: g10.g10_cache_plan_evictions(cache, big)]
+    for i, call in enumerate(calls):
+        with pytest.raises(g10.G10Error, match="32 bits"):
+            call()
+            raise AssertionError("call %d was taken" % i)
+    assert all(same(a, b) for a, b in zip(before, (cache.k, cache.v, cache.scores)))
+
+
 # ---- waits that run out ------------------------------------------------------------------------------------------------
 @pytest.fixture
 def hooks(monkeypatch):
