@@ -568,7 +568,15 @@ class CacheBuffers:
     call changes them).  scores: float32, positions: int32, both [pages, kv_heads, page_size].  status: int64 [1], made here unless given:
     data-dependent errors are OR-ed into it.  The calls run on `stream`, or the current stream of the cache's device; what they allocate belongs to
     the stream that they run on.  No gradients flow through them.  k and v may be None for a cache that is only planned on (then page_size and kv_heads say
-    the sizes)."""
+    the sizes).  The tensors are fixed once it is made (what they hold is not: a program writes to them); another tensor wants another CacheBuffers."""
+
+    _FIXED = frozenset(("k", "v", "page_table", "lengths", "seen", "scores", "positions", "status"))
+
+    def __setattr__(self, name, value):
+        # (the calls have the addresses of the old one, which would be given back)
+        if name in self._FIXED and "ref" in self.__dict__ and value is not self.__dict__[name]:       # (not so: cache.lengths += 1)
+            raise G10Error("%s of a CacheBuffers is fixed: write to it, or make another" % name)
+        object.__setattr__(self, name, value)
 
     def __init__(self, k, v, page_table, lengths, seen=None, scores=None, positions=None, status=None, page_size=None, kv_heads=None):
         self.k, self.v, self.page_table, self.lengths, self.seen = k, v, page_table, lengths, seen

@@ -146,6 +146,22 @@ def test_a_status_word_made_here_is_cleared_before_the_first_call(g10):
     assert int(cache.status.item()) == 0x800
 
 
+def test_the_tensors_of_a_cache_are_fixed(g10):
+    """An assignment would leave the calls with the old tensor's address: it is refused; writing into the tensor is what counts."""
+    c = O.make_cache([40, 30], 1, 64, 16, torch.bfloat16, 3, positions=True)
+    cache = O.upload(g10, c)
+    for name in ("k", "v", "page_table", "lengths", "seen", "scores", "positions", "status"):
+        old = getattr(cache, name)
+        with pytest.raises(g10.G10Error, match=name):
+            setattr(cache, name, torch.zeros(2, dtype=torch.int32, device=DEV))
+        assert getattr(cache, name) is old
+    lengths = cache.lengths
+    lengths -= 10
+    cache.lengths -= 1
+    assert g10.g10_cache_plan_evictions(cache, 25).new_lengths.tolist() == [25, 19]
+    cache.layer = 7                                      # (whatever else a program keeps there)
+
+
 # ---- numbers of more than 32 bits ------------------------------------------------------------------------------------------
 def test_numbers_that_do_not_fit_are_refused(g10):
     """A window of 2^32 + 5 is not one of 5."""
