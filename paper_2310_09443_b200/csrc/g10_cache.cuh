@@ -117,7 +117,6 @@ template <typename T>
 struct Pair;
 template <>
 struct Pair<__nv_bfloat16> {
-    typedef __nv_bfloat162 type;
     static __device__ __forceinline__ unsigned pack(float a, float b)
     {
         const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
@@ -127,7 +126,6 @@ struct Pair<__nv_bfloat16> {
 };
 template <>
 struct Pair<__half> {
-    typedef __half2 type;
     static __device__ __forceinline__ unsigned pack(float a, float b)
     {
         const __half2 p = __floats2half2_rn(a, b);
@@ -136,8 +134,8 @@ struct Pair<__half> {
     static __device__ __forceinline__ float2 unpack(unsigned u) { return __half22float2(*(const __half2 *)&u); }
 };
 
-// Rows of the logits that are kept for a slot: those of a block of rows, rounded up for wide accesses.
-__host__ __device__ __forceinline__ int logit_rows(int kept) { return kept <= 2 ? kept : (kept + 3) & ~3; }
+// Rows of the logits that are kept for a slot (up to 16), rounded up for wide accesses.
+__host__ __device__ __forceinline__ int logit_rows(int rows) { return rows <= 2 ? rows : (rows + 3) & ~3; }
 
 // ---- launchers ----
 struct AppendArgs {
@@ -156,11 +154,9 @@ cudaError_t launch_cache_append(const AppendArgs &a, int dtype, cudaStream_t s);
 
 // What the booking kernel has to know of a tile.
 struct __align__(16) TileNote {
-    int s, head, slot, length;           // sequence, key-value head, first slot, the sequence's slots
-    int tiles;                           // of the item: from one block of rows to the next (0: another block of rows books the tile)
-    int unused[3];
+    int s, head, slot, length;           // sequence, key-value head, first slot, the sequence's slots (0: no tile has this number)
 };
-static_assert(sizeof(TileNote) == 32, "read 16 bytes at a time");
+static_assert(sizeof(TileNote) == 16, "read at a time");
 struct AttendArgs {
     CacheView c;
     const char *q;
@@ -174,7 +170,7 @@ struct AttendArgs {
     int64_t pieces;                      // (room for so many)
     float2 *ml;                          // [block rows][pieces] running maximum and sum of every piece
     float *part;                         // [pieces][block rows][padded head_dim] its sums, not divided yet
-    float *logits;                       // [tiles][64][rows of a block] scaled by log2 e (null: weights are not booked)
+    float *logits;                       // [tiles][64][logit_rows] scaled by log2 e (null: weights are not booked, or for more than 16 rows)
     bool books;
     float *sums;                         // [items][block rows] lse of every row, to base 2
     TileNote *notes;                     // [tiles]

@@ -11,8 +11,11 @@
 // always grows.  A piece that is a whole item gives the answer; of the others (m, l, o) are joined by the second kernel.
 //
 // The weights w_j = exp(s_j - lse) that the cache books need lse, which nobody knows before the last piece is done.  So the first kernel
-// leaves s_j (4 bytes a row, beside 4 * head_dim bytes of key and value), and the second adds the weights up.  Each slot's sum is made by one
-// thread over its rows in order and added once: the same every time.
+// leaves s_j (4 bytes a row, beside 4 * head_dim bytes of key and value), and the third adds the weights up: up to four lanes a slot, each over four rows,
+// joined in a fixed order and added to the score once, the same every time.
+//
+// This file is for up to 16 rows per key-value head (new tokens times heads of the group), one block of rows each; more are g10_cache_rows.cuh's, which has the
+// sharing out of tiles and the second kernel from here.
 #pragma once
 #include "g10_cache.cuh"
 
@@ -254,7 +257,8 @@ __device__ __forceinline__ void part_add(Part &p, float top, float sum, const fl
 // heads: one block.
 template <int kSteps, int kCols>
 struct Ring {
-    static constexpr int kOther = (kCols * kSteps <= 16 ? 0 : 8 * kCols * (32 * kSteps + 16)) + kParts * 8 * kCols * 8 + (kCols <= 2 ? 8 * kCols * (64 * kSteps + 8) : 0) + 1024;
+    static_assert(kCols == 1 || kCols == 2, "8 or 16 rows");
+    static constexpr int kOther = (kCols * kSteps <= 16 ? 0 : 8 * kCols * (32 * kSteps + 16)) + kParts * 8 * kCols * 8 + 8 * kCols * (64 * kSteps + 8) + 1024;
     static constexpr int kTileBytes = 2 * kTile * (32 * kSteps + 16);
     static constexpr int fits(int blocks) { return (226 * 1024 / blocks - kOther) / kTileBytes; }
     static constexpr int kBlocks = kSteps > 8 ? 1 : kSteps <= 4 && fits(4) >= 2 ? 4 : kSteps != 5 && fits(3) >= 2 ? 3 : 2;
@@ -270,14 +274,12 @@ struct Config {
     static constexpr int kRows = 8 * kCols;
     static constexpr int kPartBytes = 2 * 16 * kPitch;   // a warp's part of a tile: 16 keys, 16 values
     static constexpr bool kHeld = kCols * kSteps <= 16;  // the queries stay in registers
-    // what a cluster's blocks read of one another: sums, and maximum and sum of the weights, of every row (32 rows leave no room for it)
-    static constexpr bool kClusters = kCols <= 2;
-    static constexpr int kShared = kClusters ? kRows * kDim * 4 + kRows * 8 : 0;
+    // what a cluster's blocks read of one another: sums, and maximum and sum of the weights, of every row
+    static constexpr int kShared = kRows * kDim * 4 + kRows * 8;
     static constexpr int kSmem = kParts * kStages * kPartBytes + (kHeld ? 0 : kRows * kPitch) + kParts * kRows * 8 + kShared;
-    // joining the warps' sums: so many columns at a time fit the part of the ring that the warp has just left
-    static constexpr int kMerge = kCols < 2 ? kCols : 2;
+    // joining the warps' sums: they fit the part of the ring that the warp has just left
     static constexpr int kMergePitch = kDim + 4;         // floats (2 rows apart: 8 banks)
-    static_assert(8 * kMerge * kMergePitch * 4 <= kPartBytes && kCols % kMerge == 0, "a warp's sums fit");
+    static_assert(kRows * kMergePitch * 4 <= kPartBytes, "a warp's sums fit");
 };
 
 // The block's four warps go through its tiles side by side, warp p at the 16 slots p of each, with maxima, sums and accumulators of their
@@ -298,22 +300,21 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
     typedef Config<T, kSteps, kCols> C;
     constexpr int kStages = C::kStages;
     extern __shared__ __align__(128) char smem[];
-    float *const s_join = (float *)(smem + kParts * kStages * C::kPartBytes);          // [kRows][kDim], then [kRows] maximum and sum (kClusters)
-    float2 *const s_join_ml = (float2 *)(s_join + (C::kClusters ? C::kRows * C::kDim : 0));
+    float *const s_join = (float *)(smem + kParts * kStages * C::kPartBytes);          // [kRows][kDim], then [kRows] maximum and sum
+    float2 *const s_join_ml = (float2 *)(s_join + C::kRows * C::kDim);
     char *const s_q = smem + kParts * kStages * C::kPartBytes + C::kShared;
     float2 *const s_ml = (float2 *)(s_q + (C::kHeld ? 0 : C::kRows * C::kPitch));      // [kParts][kRows]
     __shared__ Place s_place;
     const int tid = threadIdx.x, lane = tid & 31, part = tid >> 5;
-    const int per = a.c.kv_heads * a.row_blocks;
+    const int per = a.c.kv_heads;                        // (one block of rows a head)
     ull bad = 0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     Cursor now, ahead;
     int64_t begin;
     int n, rank = 0, my_item = 0;                        // (clusters)
-    if (C::kClusters && cluster > 0) {
+    if (cluster > 0) {
         my_item = (int)blockIdx.x / cluster; rank = (int)blockIdx.x % cluster;
-        now.s = my_item / per; now.item = my_item % per;
-        now.head = now.item / a.row_blocks; now.block = now.item % a.row_blocks;
+        now.s = my_item / per; now.item = now.head = my_item % per; now.block = 0;
         now.q = seq_of(a, now.s, bad);
         if (bad != 0) raise_status(a.c.status, bad);
         const int tiles = now.q.tiles;
@@ -321,17 +322,17 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
         n = tiles * (rank + 1) / cluster - now.idx;
         begin = (int64_t)my_item * cap + now.idx;
         if (a.logits != nullptr && rank == 0) {          // (the numbers that the item does not use)
-            for (int i = tiles + tid; i < cap; i += kThreads) a.notes[(int64_t)my_item * cap + i].tiles = 0;
+            for (int i = tiles + tid; i < cap; i += kThreads) a.notes[(int64_t)my_item * cap + i].length = 0;
             if (my_item == 0 && tid == 0) *a.total = (int64_t)a.c.num_seqs * per * cap;
         }
         if (tiles == 0) {                                // (the whole cluster alike)
             const int chunks = a.c.head_dim / 8;
             for (int i = rank * kThreads + tid; i < C::kRows * chunks; i += cluster * kThreads) {
-                const int r = i / chunks, row = now.block * C::kRows + r;
+                const int row = i / chunks;
                 if (row >= a.rows) continue;
                 const int64_t at = ((int64_t)now.s * a.new_tokens + row / a.group) * a.q_heads + now.head * a.group + row % a.group;
-                *(uint4 *)(a.out + 2 * at * a.c.head_dim + 16 * (i - r * chunks)) = make_uint4(0, 0, 0, 0);
-                if (a.lse != nullptr && i == r * chunks) a.lse[at] = -INFINITY;
+                *(uint4 *)(a.out + 2 * at * a.c.head_dim + 16 * (i - row * chunks)) = make_uint4(0, 0, 0, 0);
+                if (a.lse != nullptr && i == row * chunks) a.lse[at] = -INFINITY;
             }
             return;
         }
@@ -348,7 +349,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
         cursor_at(a, now, s_place, begin);
     }
     bad = 0;
-    const int my_s = now.s, my_head = now.head, my_block = now.block;
+    const int my_s = now.s, my_head = now.head;
     ahead = now;
     const unsigned ring = smem_of(smem) + part * kStages * C::kPartBytes;
     // where the row of this lane's slot begins (lanes 16 .. 31: as lanes 0 .. 15), in the tile that `ahead` stands at
@@ -405,16 +406,15 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
     int p[kCols][2];                                     // slot at which a row's token stands, -1: no row
     bool fresh = true;
     int64_t item = 0;
-    int first_row = 0, stage = 0;
-    const int kept = min(C::kRows, a.rows), logit_pitch = logit_rows(kept);
+    int stage = 0;
+    const int logit_pitch = logit_rows(a.rows);
     for (int u = 0; u < n; ++u) {
         if (fresh) {                                     // a new item: its queries
             fresh = false;
             item = (int64_t)now.s * per + now.item;
-            first_row = now.block * C::kRows;
             const int head = now.head;
-            auto row_of = [&](int r) -> const char * {   // (null: no such row)
-                const int row = first_row + r, t = row / a.group;
+            auto row_of = [&](int row) -> const char * { // (null: no such row)
+                const int t = row / a.group;
                 if (row >= a.rows || t >= now.q.count) return nullptr;
                 return a.q + 2 * (now.s * a.q_seq + t * a.q_token + (head * a.group + row % a.group) * a.q_head);
             };
@@ -446,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     m[j][h] = -INFINITY; l[j][h] = 0.0f;
-                    const int row = first_row + j * 8 + (lane & 3) * 2 + h, t = row / a.group;
+                    const int row = j * 8 + (lane & 3) * 2 + h, t = row / a.group;
                     p[j][h] = row < a.rows && t < now.q.count ? now.q.length - now.q.count + t : -1;
                 }
             }
@@ -474,18 +474,15 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
                 for (int j = 0; j < kCols; ++j) mma<T>(x[j], ka, held[j * 2 * kSteps + 2 * k], held[j * 2 * kSteps + 2 * k + 1]);
             }
         } else {
-            const unsigned q_at = smem_of(s_q) + ((lane & 7) + (kCols > 1 ? (lane >> 4) * 8 : 0)) * C::kPitch + ((lane >> 3) & 1) * 16;
+            // (16 rows of wide heads)
+            const unsigned q_at = smem_of(s_q) + ((lane & 7) + (lane >> 4) * 8) * C::kPitch + ((lane >> 3) & 1) * 16;
 #pragma unroll
             for (int k = 0; k < kSteps; ++k) {
-                unsigned ka[4];
+                unsigned ka[4], qb[4];
                 ldsm4(ka, k_at + k * 32);
-#pragma unroll
-                for (int j = 0; j < kCols; j += 2) {
-                    unsigned qb[4];
-                    ldsm4(qb, q_at + j * 8 * C::kPitch + k * 32);
-                    mma<T>(x[j], ka, qb[0], qb[1]);
-                    if (j + 1 < kCols) mma<T>(x[j + 1], ka, qb[2], qb[3]);
-                }
+                ldsm4(qb, q_at + k * 32);
+                mma<T>(x[0], ka, qb[0], qb[1]);
+                mma<T>(x[kCols - 1], ka, qb[2], qb[3]);
             }
         }
         // ---- what each row sees ----
@@ -499,11 +496,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
                 if (!whole && !sees(a, p[j][e & 1], slot0 + (lane >> 2) + (e >> 1) * 8)) x[j][e] = -INFINITY;
             }
         if (a.logits != nullptr) {
-            if (tid < 3) {                               // the tile's note (of the other blocks of rows: that it is none)
-                int2 *const note = (int2 *)&a.notes[begin + u];
-                const int first = first_slot(now.q, now.idx);
-                note[tid] = tid == 0 ? make_int2(now.s, now.head) : tid == 1 ? make_int2(first, now.q.length) : make_int2(now.block == 0 ? (cluster > 0 ? cap : now.q.tiles) : 0, 0);
-            }
+            if (tid == 0) *(int4 *)&a.notes[begin + u] = make_int4(now.s, now.head, first_slot(now.q, now.idx), now.q.length);
             float *const to = a.logits + (begin + u) * (int64_t)(logit_pitch * kTile) + (part * 16 + (lane >> 2)) * logit_pitch;
 #pragma unroll
             for (int j = 0; j < kCols; ++j) {
@@ -614,53 +607,47 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
             const bool all = u >= now.idx && now.idx == now.q.tiles - 1;
             const int64_t piece = item + blockIdx.x;
 #pragma unroll
-            for (int j0 = 0; j0 < kCols; j0 += C::kMerge) {
-                if (j0 > 0) __syncthreads();
-                constexpr int kSome = 8 * C::kMerge;     // rows in this step
+            for (int j = 0; j < kCols; ++j)
 #pragma unroll
-                for (int j = j0; j < j0 + C::kMerge; ++j)
+                for (int k = 0; k < kSteps; ++k)
 #pragma unroll
-                    for (int k = 0; k < kSteps; ++k)
+                    for (int e = 0; e < 4; ++e)
+                        room[part * kApart + (j * 8 + (lane & 3) * 2 + (e & 1)) * C::kMergePitch + k * 16 + (e >> 1) * 8 + (lane >> 2)] = acc[k][j][e];
+            __syncthreads();
+            for (int i = tid; i < C::kRows * (C::kDim / 4); i += kThreads) {
+                const int row = i / (C::kDim / 4), d = i % (C::kDim / 4) * 4;
+                if (row >= a.rows) continue;
+                float top = -INFINITY, sum = 0.0f;
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            room[part * kApart + ((j - j0) * 8 + (lane & 3) * 2 + (e & 1)) * C::kMergePitch + k * 16 + (e >> 1) * 8 + (lane >> 2)] = acc[k][j][e];
-                __syncthreads();
-                for (int i = tid; i < kSome * (C::kDim / 4); i += kThreads) {
-                    const int some = i / (C::kDim / 4), d = i % (C::kDim / 4) * 4;
-                    const int r = j0 * 8 + some, row = first_row + r;
-                    if (row >= a.rows) continue;
-                    float top = -INFINITY, sum = 0.0f;
+                for (int q = 0; q < kParts; ++q) top = fmaxf(top, s_ml[q * C::kRows + row].x);
+                const float ref = top == -INFINITY ? 0.0f : top;
+                float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-                    for (int q = 0; q < kParts; ++q) top = fmaxf(top, s_ml[q * C::kRows + r].x);
-                    const float ref = top == -INFINITY ? 0.0f : top;
-                    float4 o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-                    for (int q = 0; q < kParts; ++q) {
-                        const float2 ml = s_ml[q * C::kRows + r];
-                        const float f = exp2_of(ml.x - ref);
-                        const float4 v = *(const float4 *)&room[q * kApart + some * C::kMergePitch + d];
-                        sum = fmaf(ml.y, f, sum);
-                        o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
-                    }
-                    if (C::kClusters && cluster > 0) {
-                        if (d == 0) s_join_ml[r] = make_float2(top, sum);
-                        *(float4 *)(s_join + r * C::kDim + d) = o;
-                        continue;
-                    }
-                    if (d == 0) a.ml[r * a.pieces + piece] = make_float2(top, sum);
-                    if (!all) {
-                        *(float4 *)(a.part + (piece * C::kRows + r) * C::kDim + d) = o;
-                    } else if (d < a.c.head_dim) {
-                        const int64_t at = ((int64_t)now.s * a.new_tokens + row / a.group) * a.q_heads + now.head * a.group + row % a.group;
-                        const float inv = 1.0f / sum;    // (sees nothing: zero, whatever the sums hold)
-                        uint2 w = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
-                        if (sum == 0.0f) w = make_uint2(0, 0);
-                        *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
-                        if (d == 0) {
-                            const float lse = top + log2f(sum * Weights<T>::kUnlift);
-                            if (a.lse != nullptr) a.lse[at] = sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
-                            if (a.books) a.sums[item * C::kRows + r] = sum == 0.0f ? INFINITY : lse;
-                        }
+                for (int q = 0; q < kParts; ++q) {
+                    const float2 ml = s_ml[q * C::kRows + row];
+                    const float f = exp2_of(ml.x - ref);
+                    const float4 v = *(const float4 *)&room[q * kApart + row * C::kMergePitch + d];
+                    sum = fmaf(ml.y, f, sum);
+                    o.x = fmaf(v.x, f, o.x); o.y = fmaf(v.y, f, o.y); o.z = fmaf(v.z, f, o.z); o.w = fmaf(v.w, f, o.w);
+                }
+                if (cluster > 0) {
+                    if (d == 0) s_join_ml[row] = make_float2(top, sum);
+                    *(float4 *)(s_join + row * C::kDim + d) = o;
+                    continue;
+                }
+                if (d == 0) a.ml[row * a.pieces + piece] = make_float2(top, sum);
+                if (!all) {
+                    *(float4 *)(a.part + (piece * C::kRows + row) * C::kDim + d) = o;
+                } else if (d < a.c.head_dim) {
+                    const int64_t at = ((int64_t)now.s * a.new_tokens + row / a.group) * a.q_heads + now.head * a.group + row % a.group;
+                    const float inv = 1.0f / sum;        // (sees nothing: zero, whatever the sums hold)
+                    uint2 w = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
+                    if (sum == 0.0f) w = make_uint2(0, 0);
+                    *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
+                    if (d == 0) {
+                        const float lse = top + log2f(sum * Weights<T>::kUnlift);
+                        if (a.lse != nullptr) a.lse[at] = sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
+                        if (a.books) a.sums[item * C::kRows + row] = sum == 0.0f ? INFINITY : lse;
                     }
                 }
             }
@@ -672,19 +659,19 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (bad != 0) raise_status(a.c.status, bad);
-    if (C::kClusters && cluster > 0) {
+    if (cluster > 0) {
         // ---- the item's parts are joined: each block takes some of the elements of all ----
         if (n == 0 && tid < C::kRows) s_join_ml[tid] = make_float2(-INFINITY, 0.0f);
         cluster_sync();
-        const int quads = a.c.head_dim / 4, rows = min(C::kRows, a.rows - my_block * C::kRows);
-        for (int e = tid * cluster + rank; e < rows * quads; e += kThreads * cluster) {
-            const int r = e / quads, d = (e - r * quads) * 4, row = my_block * C::kRows + r;
+        const int quads = a.c.head_dim / 4;
+        for (int e = tid * cluster + rank; e < a.rows * quads; e += kThreads * cluster) {
+            const int row = e / quads, d = (e - row * quads) * 4;
             Part p;
             p.top = -INFINITY; p.sum = 0.0f; p.o = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll 4
             for (int q = 0; q < cluster; ++q) {
-                const float2 ml = read_of(&s_join_ml[r], (unsigned)q);
-                const float4 o = read_of((const float4 *)(s_join + r * C::kDim + d), (unsigned)q);
+                const float2 ml = read_of(&s_join_ml[row], (unsigned)q);
+                const float4 o = read_of((const float4 *)(s_join + row * C::kDim + d), (unsigned)q);
                 if (ml.y != 0.0f) part_add(p, ml.x, ml.y, o);                      // (a part that saw nothing has no sums)
             }
             const int64_t at = ((int64_t)my_s * a.new_tokens + row / a.group) * a.q_heads + my_head * a.group + row % a.group;
@@ -695,7 +682,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
             if (d == 0) {
                 const float lse = p.top + log2f(p.sum * Weights<T>::kUnlift);
                 if (a.lse != nullptr) a.lse[at] = p.sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
-                if (a.books) a.sums[(int64_t)my_item * C::kRows + r] = p.sum == 0.0f ? INFINITY : lse;
+                if (a.books) a.sums[(int64_t)my_item * C::kRows + row] = p.sum == 0.0f ? INFINITY : lse;
             }
         }
         cluster_sync();                                  // (nobody leaves while its memory may still be read)
@@ -819,8 +806,9 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
 }
 
 // The third kernel books the weights: a warp per tile, from the note that the first kernel has left for it, so that there is nothing to search for.  A
-// slot's rows lie side by side: as many neighbouring lanes as it has groups of four rows read them and add their weights up; a lane has the same
-// rows of every slot, and so its part of the lse in registers.  exp2(logit - lse) over all rows in order, and one addition to the score.
+// slot's rows lie side by side: as many neighbouring lanes as it has groups of four rows read them, add their weights exp2(logit - lse) up and join
+// them, always in the same order; the first makes the one addition to the score.  A lane has the same rows of every slot, and so its part of the
+// lse in registers.
 template <int kTeam>
 __device__ __forceinline__ void book_tile(const AttendArgs &a, const TileNote &note, int64_t tile, int block_rows, int pitch, bool &waited, ull &bad)
 {
@@ -828,9 +816,8 @@ __device__ __forceinline__ void book_tile(const AttendArgs &a, const TileNote &n
         if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");
         waited = true;
     };
-    const int lane = threadIdx.x & 31, mate = lane & (kTeam - 1);
-    const int per = a.c.kv_heads * a.row_blocks;
-    const int64_t item = (int64_t)note.s * per + note.head * a.row_blocks;
+    const int lane = threadIdx.x & 31, mate = lane & (kTeam - 1), r = 4 * mate;
+    const float *const lse = a.sums + ((int64_t)note.s * a.c.kv_heads + note.head) * block_rows + r;
     constexpr int kPasses = 2 * kTeam, kAhead = kPasses < 8 ? kPasses : 8;
 #pragma unroll 1
     for (int pass = 0; pass < kPasses; pass += kAhead) {
@@ -842,34 +829,30 @@ __device__ __forceinline__ void book_tile(const AttendArgs &a, const TileNote &n
             spot[i] = slot < note.length ? cache_spot(a.c, note.s, slot, bad) : Spot{-1, 0};
             w[i] = 0.0f;
         }
-        for (int b = 0; b < a.row_blocks; ++b) {
-            const float *const from = a.logits + ((tile + (int64_t)b * note.tiles) * kTile + pass * (32 / kTeam) + lane / kTeam) * pitch;
-            const int r = 4 * mate, rows = a.rows - b * block_rows;
-            const float *const lse = a.sums + (item + b) * block_rows + r;
-            if (pitch >= 4) {
-                float4 z = make_float4(INFINITY, INFINITY, INFINITY, INFINITY), x[kAhead];       // (no such row: weight 0)
+        const float *const from = a.logits + (tile * kTile + pass * (32 / kTeam) + lane / kTeam) * pitch;
+        if (pitch >= 4) {
+            float4 z = make_float4(INFINITY, INFINITY, INFINITY, INFINITY), x[kAhead];           // (no such row: weight 0)
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) x[i] = r < pitch ? __ldcg((const float4 *)(from + i * (32 / kTeam) * pitch + r)) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            for (int i = 0; i < kAhead; ++i) x[i] = r < pitch ? __ldcg((const float4 *)(from + i * (32 / kTeam) * pitch + r)) : make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+            joined();
+            if (r < pitch) {
+                z = __ldcg((const float4 *)lse);
+                if (r + 1 >= a.rows) z.y = INFINITY;
+                if (r + 2 >= a.rows) z.z = INFINITY;
+                if (r + 3 >= a.rows) z.w = INFINITY;
+                if (r >= a.rows) z.x = INFINITY;
+            }
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i) w[i] += (exp2_of(x[i].x - z.x) + exp2_of(x[i].y - z.y)) + (exp2_of(x[i].z - z.z) + exp2_of(x[i].w - z.w));
+        } else {
+            for (int q = 0; q < pitch; ++q) {
+                float x[kAhead];
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i) x[i] = __ldcg(from + i * 32 * pitch + q);
                 joined();
-                if (r < pitch) {
-                    z = __ldcg((const float4 *)lse);
-                    if (r + 1 >= rows) z.y = INFINITY;
-                    if (r + 2 >= rows) z.z = INFINITY;
-                    if (r + 3 >= rows) z.w = INFINITY;
-                    if (r >= rows) z.x = INFINITY;
-                }
+                const float z = __ldcg(lse + q);
 #pragma unroll
-                for (int i = 0; i < kAhead; ++i) w[i] += (exp2_of(x[i].x - z.x) + exp2_of(x[i].y - z.y)) + (exp2_of(x[i].z - z.z) + exp2_of(x[i].w - z.w));
-            } else {
-                for (int q = 0; q < pitch; ++q) {
-                    float x[kAhead];
-#pragma unroll
-                    for (int i = 0; i < kAhead; ++i) x[i] = __ldcg(from + i * 32 * pitch + q);
-                    joined();
-                    const float z = __ldcg(lse + q);
-#pragma unroll
-                    for (int i = 0; i < kAhead; ++i) w[i] += exp2_of(x[i] - z);
-                }
+                for (int i = 0; i < kAhead; ++i) w[i] += exp2_of(x[i] - z);
             }
         }
 #pragma unroll
@@ -887,19 +870,18 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_book(const AttendArgs a,
     // Behind the second kernel, which lets this one begin once the first is done: its notes and logits may be read at once.
     bool waited = !behind_join;
     if (waited) asm volatile("griddepcontrol.wait;" ::: "memory");
-    const int pitch = logit_rows(min(block_rows, a.rows));
+    const int pitch = logit_rows(a.rows);
     const int64_t total = __ldcg(a.total), step = (int64_t)gridDim.x * (kJoinThreads / 32);
     ull bad = 0;
     int64_t u = (int64_t)blockIdx.x * (kJoinThreads / 32) + (threadIdx.x >> 5);
     int4 x = make_int4(0, 0, 0, 0);
-    int tiles = 0;
-    if (u < total) { x = __ldcg((const int4 *)&a.notes[u]); tiles = __ldcg(&a.notes[u].tiles); }
+    if (u < total) x = __ldcg((const int4 *)&a.notes[u]);
     while (u < total) {
-        const TileNote note{x.x, x.y, x.z, x.w, tiles, {0, 0, 0}};
+        const TileNote note{x.x, x.y, x.z, x.w};
         const int64_t now = u;
         u += step;
-        if (u < total) { x = __ldcg((const int4 *)&a.notes[u]); tiles = __ldcg(&a.notes[u].tiles); }
-        if (note.tiles > 0) book_tile<kTeam>(a, note, now, block_rows, pitch, waited, bad);
+        if (u < total) x = __ldcg((const int4 *)&a.notes[u]);
+        if (note.length > 0) book_tile<kTeam>(a, note, now, block_rows, pitch, waited, bad);
     }
     if (!waited) asm volatile("griddepcontrol.wait;" ::: "memory");      // (this kernel's end says that the second has ended)
     if (bad != 0) raise_status(a.c.status, bad);
@@ -932,7 +914,7 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     // Clusters: where every item has at most four tiles a block and all blocks run at a time.
     const int64_t cap = z.items > 0 ? z.tiles / z.items : 0;
     int cluster = 0;
-    if (C::kClusters && z.items <= room && cap >= 1) {
+    if (z.items <= room && cap >= 1) {
         static int most_known[kMaxDevices];
         const void *const kernels[] = {(const void *)kernel};
         const int most = largest_cluster(kernels, false, kThreads, C::kSmem, most_known);
@@ -956,8 +938,7 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     if (a.logits == nullptr) return cudaSuccess;
     const int64_t warps = kJoinThreads / 32, blocks = (z.tiles + warps - 1) / warps, most = 148 * 6;
     cfg.gridDim = dim3((unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most));      // (a table without columns: no tile)
-    const int pitch = logit_rows(C::kRows < a.rows ? C::kRows : a.rows);
-    const auto book = pitch <= 4 ? k_cache_book<1> : pitch <= 8 ? k_cache_book<2> : pitch <= 16 ? k_cache_book<4> : k_cache_book<8>;
+    const auto book = a.rows <= 4 ? k_cache_book<1> : a.rows <= 8 ? k_cache_book<2> : k_cache_book<4>;
     return cudaLaunchKernelEx(&cfg, book, a, C::kRows, cluster == 0);
 }
 template <typename T, int kSteps>
