@@ -7,7 +7,7 @@ import pytest
 import torch
 
 import cache_oracle as O
-from test_gpu_cache import DEV, check_attend, g10, queries, same  # noqa: F401 (g10 is the fixture)
+from test_gpu_cache import DEV, check_attend, check_plan_and_evict, g10, queries, same, shuffle_positions  # noqa: F401 (g10 is the fixture)
 
 pytestmark = pytest.mark.gpu
 
@@ -182,6 +182,105 @@ def test_numbers_that_do_not_fit_are_refused(g10):
             call()
             raise AssertionError("call %d was taken" % i)
     assert all(same(a, b) for a, b in zip(before, (cache.k, cache.v, cache.scores)))
+
+
+# ---- forms that only large sizes take --------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("lengths,columns,budget", [([3000, 70, 500, 0], 8000, 200), ([3000, 70, 500, 0], 8000, 2999), ([410_001, 9], None, 4000)])
+def test_plan_where_shared_memory_holds_no_scores(g10, lengths, columns, budget):
+    """Some 48 000 slots a block is what it takes: tables of half a million slots, long sequences and short ones."""
+    c = O.make_cache(lengths, 2, 8, 64, torch.bfloat16, 7, columns=columns, positions=True)
+    shuffle_positions(c, 3)
+    check_plan_and_evict(g10, c, budget, 4, budget // 8)
+
+
+@pytest.mark.parametrize("seqs,kv,dim,group,new", [(32, 16, 192, 2, 1), (32, 16, 256, 6, 2), (64, 16, 80, 1, 1), (128, 4, 64, 20, 1), (128, 4, 256, 9, 2)])
+def test_shares_that_are_cut(g10, seqs, kv, dim, group, new):
+    """At least 128 tiles for each block that runs at a time: four shares for each.  The sequences have the same pages, so that it takes little memory;
+    what is booked adds up."""
+    lengths = [2560 - i for i in range(seqs)]
+    c = O.make_cache(lengths[:1], kv, dim, 64, torch.bfloat16, dim)
+    c.lengths = torch.tensor(lengths, dtype=torch.int32)
+    c.table = c.table.expand(seqs, -1).contiguous()
+    c.scores.zero_()
+    q = queries(c, new, group, 4)
+    cache = O.upload(g10, c)
+    lse = torch.empty(q.shape[:3], device=DEV)
+    out = g10.g10_cache_attend(cache, q.to(DEV), add_scores=True, lse=lse).cpu().double()
+    assert int(cache.status.item()) == 0
+    r = O.attend(c, q, dim ** -0.5)
+    b_out, b_lse, rel = O.attend_bounds(c, r)
+    assert ((out - r.out).abs() <= b_out).all() and ((lse.cpu().double() - r.lse).abs() <= b_lse).all()
+    got, want = cache.scores.cpu().double(), torch.zeros(c.scores.shape, dtype=torch.float64)
+    for (s, h), w in r.booked.items():
+        pg, pl = O.places(c, s, len(w))
+        want[pg, h, pl] += w
+    # (one rounded addition for each sequence)
+    assert ((got - want).abs() <= want * (float(rel.max()) * 1.01 + seqs * 2.0 ** -24)).all()
+
+
+def test_evict_of_more_heads_than_one_launch_takes(g10):
+    """1100 sequences of 64 heads: 70 400 pairs, 65 472 in the first launch."""
+    lengths = [6 + i % 3 if i % 2 == 0 or i > 1000 else i % 5 for i in range(1100)]
+    c = O.make_cache(lengths, 64, 8, 4, torch.float16, 2, positions=True)
+    check_plan_and_evict(g10, c, 5, 1, 1)
+
+
+# ---- what is wrong in the data, for many rows ------------------------------------------------------------------------------------
+@pytest.mark.parametrize("new,group", [(1, 20), (20, 7)])
+@pytest.mark.parametrize("book", [False, True])
+def test_bad_pages_and_lengths_for_many_rows(g10, new, group, book):
+    """Reported; a slot without a page is read as zeros and not written, a length is taken as the nearest that is possible."""
+    c = O.make_cache([200, 190], 2, 64, 16, torch.bfloat16, 3)
+    c.table = torch.cat([c.table, c.table[:, :1]], 1).contiguous()           # (room for more slots than there are)
+    c.table[:, -1] = c.table[0, 0]
+    q = queries(c, new, group, 1)
+    dq = q.to(DEV)
+    good = c.table.clone()
+    capacity = 16 * c.table.shape[1]
+
+    def call(counts=None):
+        cache = O.upload(g10, c)
+        out = g10.g10_cache_attend(cache, dq, scale=0.1, add_scores=book, counts=counts)
+        torch.cuda.synchronize()
+        assert same(cache.k, c.k) and same(cache.v, c.v)
+        return cache, out.cpu().double()
+
+    for page in (-1, -2 ** 31, c.k.shape[0], 2 ** 31 - 1):
+        c.table[1, 2] = page
+        cache, out = call()
+        assert int(cache.status.item()) == 0x400
+        # the same with a page of zeros there: the one that nobody has
+        spare = next(i for i in range(c.k.shape[0]) if i not in good.flatten().tolist())
+        c.table[1, 2] = spare
+        kept = c.k[spare].clone(), c.v[spare].clone(), c.scores[spare].clone()
+        c.k[spare], c.v[spare] = 0.0, 0.0
+        r = O.attend(c, q, 0.1)
+        bound = O.attend_bounds(c, r)[0]
+        assert ((out - r.out).abs() <= bound).all()
+        if book:
+            got = cache.scores.cpu()
+            assert same(got[spare], kept[2])
+            pg, pl = O.places(c, 1, 190)
+            for h in range(2):
+                want = c.scores[pg, h, pl].double() + r.booked[1, h]
+                there = pg != spare
+                assert ((got[pg, h, pl].double() - want).abs() <= want * 0.001)[there].all()
+        c.k[spare], c.v[spare] = kept[0], kept[1]
+        c.table[1, 2] = good[1, 2]
+    for length, nearest in ((-1, 0), (-2 ** 31, 0), (capacity + 1, capacity), (2 ** 31 - 1, capacity)):
+        c.lengths[1] = length
+        cache, out = call()
+        c.lengths[1] = nearest
+        again, want = call()
+        # (all that the table has room for: one entry of this sequence's names no page)
+        assert int(again.status.item()) == (0x400 if nearest else 0) and int(cache.status.item()) == int(again.status.item()) | 0x800
+        assert same(out.float(), want.float())
+    c.lengths[1] = 190
+    for count, nearest in ((-1, 0), (new + 1, new), (2 ** 31 - 1, new)):
+        cache, out = call(torch.tensor([new, count], dtype=torch.int32, device=DEV))
+        assert int(cache.status.item()) == 0x800
+        again, want = call(torch.tensor([new, nearest], dtype=torch.int32, device=DEV))
+        assert int(again.status.item()) == 0 and same(out.float(), want.float())
 
 
 # ---- waits that run out ------------------------------------------------------------------------------------------------
