@@ -474,7 +474,8 @@ int32_t g10_cache_append(const g10_cache *cache, const g10_cache_tokens *tokens,
    Products take their operands as they are stored and are added up in 32 bits; the weights are rounded to the cache's type before they
    multiply the values (relative 2^-8 / 2^-11 each; for fp16 those below 2^-24 of the row's largest by up to 2^-35 of that one), the booked ones are not.  The result does not depend on the timing of the
    blocks; the way the work is split, and with it the rounding, depends on all lengths of the batch.
-   Limit: new_tokens * q_heads / kv_heads <= 1024; scale / log 2 is finite. */
+   Limit: new_tokens * q_heads / kv_heads <= 1024; scale / log 2 is finite.  A longer prompt is looked at in parts, each with `lengths` that end at the
+   part's last token (an array of their own: the cache's other calls go on with theirs). */
 typedef struct g10_cache_queries {
     int32_t new_tokens, q_heads;
     const void *q;                  /* strides as above                                             */
@@ -487,7 +488,10 @@ typedef struct g10_cache_queries {
     int32_t add_scores;
 } g10_cache_queries;
 int32_t g10_cache_attend(const g10_cache *cache, const g10_cache_queries *queries, void *ws, size_t ws_bytes, void *stream);
-/* Workspace of g10_cache_attend (its contents are scratch). */
+/* Workspace of g10_cache_attend (its contents are scratch).  Lengths are not known to the host, so its size goes by the table's capacity, C = max_pages *
+   page_size slots (with a window, by the window if that is less): with add_scores and up to 16 rows a key-value head 4 C bytes for each row (rounded up to 1, 2 or a
+   multiple of 4) and key-value head of every sequence, 16 bytes for each 64 slots of it, and some MB; otherwise some MB.  64 sequences of 8 heads of 8 rows over 131 072 slots take 2.2 GB.
+   Launch shapes go by C, too, of attend and of plan_evictions: a table much wider than the sequences costs time, of a plan above all. */
 int32_t g10_cache_workspace_bytes(const g10_cache *cache, int32_t new_tokens, int32_t q_heads, int32_t window, int32_t sinks,
                                   int32_t add_scores, size_t *out_bytes);
 

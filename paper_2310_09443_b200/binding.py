@@ -707,7 +707,8 @@ def g10_cache_attend(cache: CacheBuffers, q, scale=None, window=0, sinks=0, coun
     """Attention of the new tokens' queries q [seqs, new_tokens, q_heads, head_dim] over the cache (scale: 1 / sqrt(head_dim) if None); returns
     `out` (made here if None).  lse: float32 [seqs, new_tokens, q_heads] to write the logarithms of the sums to, or None.  window, sinks: only the
     last `window` slots and the first `sinks` are visible (0: all).  add_scores: cache.scores grows by the weights that each slot received.
-    ws: a uint8 device tensor of at least g10_cache_workspace_bytes(...) bytes (allocated here when None); calls that may overlap on the GPU, those of
+    ws: a uint8 device tensor of at least g10_cache_workspace_bytes(...) bytes (allocated here when None, at every call: with add_scores its size goes by
+    what the page table has room for, which may be GBs); calls that may overlap on the GPU, those of
     captured graphs among them, need one each."""
     shape, qs = _rows("q", q, cache)
     dev, new, heads = cache.index, shape[1], shape[2]

@@ -225,6 +225,37 @@ def test_evict_of_more_heads_than_one_launch_takes(g10):
     check_plan_and_evict(g10, c, 5, 1, 1)
 
 
+def test_a_prompt_in_parts(g10):
+    """More tokens than one call takes: parts with lengths of their own give what the definitions give for the whole, booked weights too."""
+    prompts, group, part = [700, 333], 4, 256
+    c = O.make_cache([n + 50 for n in prompts], 2, 64, 16, torch.bfloat16, 9)
+    q = queries(c, 700, group, 5)
+    counts = torch.tensor(prompts, dtype=torch.int32)
+    r = O.attend(c, q, 0.125, counts=counts)
+    cache = O.upload(g10, c)
+    dq, lengths = q.to(DEV), cache.lengths
+    with pytest.raises(g10.G10Error):
+        g10.g10_cache_attend(cache, dq, counts=counts.to(DEV))
+    ends = lengths.clone()
+    view = g10.CacheBuffers(cache.k, cache.v, cache.page_table, ends, scores=cache.scores, status=cache.status)
+    done = counts.to(DEV)
+    outs = []
+    for t in range(0, 700, part):
+        mine = (done - t).clamp(0, part).int()
+        ends.copy_(lengths - done + (done.clamp(max=t + part)))
+        outs.append(g10.g10_cache_attend(view, dq[:, t:t + part], scale=0.125, counts=mine, add_scores=True))
+    out = torch.cat(outs, 1).cpu().double()
+    assert int(cache.status.item()) == 0
+    bound, _, rel = O.attend_bounds(c, r)
+    assert ((out - r.out).abs() <= bound).all()
+    got = cache.scores.cpu().double()
+    for (s, h), w in r.booked.items():
+        pg, pl = O.places(c, s, len(w))
+        was = c.scores[pg, h, pl].double()
+        # (three additions to a score, each rounded)
+        assert ((got[pg, h, pl] - was - w).abs() <= w * float(rel[s].max()) * 1.01 + 3 * 2.0 ** -24 * (was + w)).all()
+
+
 # ---- what is wrong in the data, for many rows ------------------------------------------------------------------------------------
 @pytest.mark.parametrize("new,group", [(1, 20), (20, 7)])
 @pytest.mark.parametrize("book", [False, True])
