@@ -519,6 +519,47 @@ int32_t g10_cache_plan_evictions(const g10_cache *cache, const g10_cache_plan *p
    plan, budget, moves and counts are used. */
 int32_t g10_cache_evict(const g10_cache *cache, const g10_cache_plan *plan, void *stream);
 
+/* ---- The same cache in 8 bits ------------------------------------------------------------------------------------------------
+   Within the same budget of bytes a cache holds nearly twice the tokens when its rows are kept in 8 bits.  A row (key or value of one token and head, x after norm
+   and rotation, in 32 bits) is kept as a scale of its own and one code an element, Q = 127 (G10_INT8) or 448 (G10_E4M3):
+     scale = max |x_i| / Q,   code_i = x_i * (Q / max |x_i|), rounded to the nearest code, ties to even;   value_i = code_i * scale
+   A row whose largest element is below 2^-100 has scale 0 and codes 0; one that holds an infinity or NaN has scale NaN and codes 0: all its values are
+   NaN.  Scales are not negative.  The four calls take the description below; a plan of evictions is g10_cache_plan_evictions' of its `cache` (which reads
+   neither k nor v).  What is said above of lengths, status, streams, graphs, shared pages and memory holds here, too. */
+#define G10_INT8 0
+#define G10_E4M3 1
+typedef struct g10_packed {
+    g10_cache cache;                /* dtype: of new tokens, queries, norm weights, outputs.  k and v: one byte an element, 16-byte aligned; the three strides are in
+                                       bytes, multiples of 16, all offsets below 2^36; head_dim a multiple of 16 */
+    int32_t code;                   /* G10_INT8 (two's complement) or G10_E4M3                     */
+    float *scales;                  /* [num_pages][kv_heads][page_size][2]: of the key and of the value row; 8-byte aligned */
+} g10_packed;
+
+/* g10_cache_append with rows written as codes and scales (queries as there). */
+int32_t g10_packed_append(const g10_packed *packed, const g10_cache_tokens *tokens, void *stream);
+
+/* Reads rows back: k and v [num_seqs][tokens][kv_heads][head_dim] of the cache's dtype receive the values of slots starts[s] .. starts[s] + tokens - 1 (starts NULL: 0),
+   rounded once; slots before 0, or at or behind the sequence's length, read as zeros.  Either of k and v may be NULL.  The output, whole pages of it, is
+   what g10_cache_attend takes as a cache, for one. */
+typedef struct g10_packed_rows {
+    int32_t tokens;
+    const int32_t *starts;          /* [num_seqs] or NULL                                           */
+    void *k, *v;                    /* strides in elements, as g10_cache_tokens'                    */
+    int64_t k_seq_stride, k_token_stride, k_head_stride;
+    int64_t v_seq_stride, v_token_stride, v_head_stride;
+} g10_packed_rows;
+int32_t g10_packed_read(const g10_packed *packed, const g10_packed_rows *rows, void *stream);
+
+/* g10_cache_attend over the packed rows: the same arguments, outputs and booking, for up to 16 rows a key-value head (new_tokens * q_heads / kv_heads).  The codes
+   themselves are multiplied, with the queries (bf16 queries as fp16 after a power of two for each row, exact but for elements 2^-30 of the row's largest) and with
+   the weights times the value's scale, rounded to 11 bits (those below 2^-24 of the row's largest by up to 2^-35 of that one); sums are in 32 bits. */
+int32_t g10_packed_attend(const g10_packed *packed, const g10_cache_queries *queries, void *ws, size_t ws_bytes, void *stream);
+int32_t g10_packed_workspace_bytes(const g10_packed *packed, int32_t new_tokens, int32_t q_heads, int32_t window, int32_t sinks, int32_t add_scores,
+                                   size_t *out_bytes);
+
+/* g10_cache_evict: codes, scales, scores and positions of every move's source go to its target. */
+int32_t g10_packed_evict(const g10_packed *packed, const g10_cache_plan *plan, void *stream);
+
 /* Bytes of device workspace the call `which` (G10_WS_*) needs for a trace of K kernels, N tensors,
    E events whose arrays live in `mem`. */
 int32_t g10_workspace_bytes(int32_t which, int64_t num_kernels, int64_t num_tensors, int64_t num_events,

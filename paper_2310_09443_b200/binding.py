@@ -27,7 +27,8 @@ FLAG_SPREAD_STATE = 8
 STATUS = {0: "ALREADY_FITS", 1: "FIT", 2: "EXHAUSTED", 3: "ITERATION_LIMIT"}
 EXPORTS = ("g10_vitality", "g10_pressure_timeline", "g10_candidate_geometry", "g10_plan_migrations",
            "g10_workspace_bytes", "g10_strerror", "g10_version", "g10_pressure_timeline_static", "g10_schedule_prefetch", "g10_emit_instructions", "g10_characterize", "g10_plan_batch", "g10_plan_cyclic", "g10_launch_count",
-           "g10_cache_append", "g10_cache_attend", "g10_cache_plan_evictions", "g10_cache_evict", "g10_cache_workspace_bytes")
+           "g10_cache_append", "g10_cache_attend", "g10_cache_plan_evictions", "g10_cache_evict", "g10_cache_workspace_bytes",
+           "g10_packed_append", "g10_packed_read", "g10_packed_attend", "g10_packed_workspace_bytes", "g10_packed_evict")
 STATIC_MAX_KERNELS, STATIC_MAX_TENSORS = 32768, 131072
 
 INSTRUCTION_DTYPE = np.dtype([("opcode", "<i4"), ("tensor", "<i4"), ("target", "<i4"), ("record", "<i4"),
@@ -105,6 +106,16 @@ class _Cache(C.Structure):
                 ("lengths", C.c_void_p), ("seen", C.c_void_p), ("scores", C.c_void_p), ("positions", C.c_void_p), ("status", C.c_void_p)]
 
 
+class _Packed(C.Structure):
+    _fields_ = [("cache", _Cache), ("code", C.c_int32), ("scales", C.c_void_p)]
+
+
+class _PackedRows(C.Structure):
+    _fields_ = [("tokens", C.c_int32), ("starts", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("k_seq_stride", C.c_int64), ("k_token_stride", C.c_int64), ("k_head_stride", C.c_int64),
+                ("v_seq_stride", C.c_int64), ("v_token_stride", C.c_int64), ("v_head_stride", C.c_int64)]
+
+
 class _CacheTokens(C.Structure):
     _fields_ = [("new_tokens", C.c_int32), ("q_heads", C.c_int32), ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
                 ("q_seq_stride", C.c_int64), ("q_token_stride", C.c_int64), ("q_head_stride", C.c_int64),
@@ -180,6 +191,16 @@ def load_library():
         lib.g10_cache_evict.argtypes = [C.POINTER(_Cache), C.POINTER(_CachePlan), C.c_void_p]
         lib.g10_cache_workspace_bytes.restype = C.c_int32
         lib.g10_cache_workspace_bytes.argtypes = [C.POINTER(_Cache), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        lib.g10_packed_append.restype = C.c_int32
+        lib.g10_packed_append.argtypes = [C.POINTER(_Packed), C.POINTER(_CacheTokens), C.c_void_p]
+        lib.g10_packed_read.restype = C.c_int32
+        lib.g10_packed_read.argtypes = [C.POINTER(_Packed), C.POINTER(_PackedRows), C.c_void_p]
+        lib.g10_packed_attend.restype = C.c_int32
+        lib.g10_packed_attend.argtypes = [C.POINTER(_Packed), C.POINTER(_CacheQueries), C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.g10_packed_workspace_bytes.restype = C.c_int32
+        lib.g10_packed_workspace_bytes.argtypes = [C.POINTER(_Packed), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        lib.g10_packed_evict.restype = C.c_int32
+        lib.g10_packed_evict.argtypes = [C.POINTER(_Packed), C.POINTER(_CachePlan), C.c_void_p]
         _lib = lib
     return _lib
 
@@ -560,25 +581,18 @@ def _rows(name, t, cache, heads=None):
     return shape, strides
 
 
-class CacheBuffers:
-    """One layer of a paged key-value cache, as the g10_cache_* calls take it (device tensors, kept alive here).
+class _Buffers:
+    """What the two kinds of caches have in common: whose slots lie where."""
 
-    k, v: bf16 or fp16 [pages, page_size, kv_heads, head_dim], any strides (the same for both, multiples of 8, the last one 1): a view of
-    [pages, kv_heads, page_size, head_dim] will do.  page_table: int32 [seqs, columns]; lengths, seen: int32 [seqs] (shared by all layers; no
-    call changes them).  scores: float32, positions: int32, both [pages, kv_heads, page_size].  status: int64 [1], made here unless given:
-    data-dependent errors are OR-ed into it.  The calls run on `stream`, or the current stream of the cache's device; what they allocate belongs to
-    the stream that they run on.  No gradients flow through them.  k and v may be None for a cache that is only planned on (then page_size and kv_heads say
-    the sizes).  The tensors are fixed once it is made (what they hold is not: a program writes to them); another tensor wants another CacheBuffers."""
-
-    _FIXED = frozenset(("k", "v", "page_table", "lengths", "seen", "scores", "positions", "status"))
+    _FIXED = frozenset(("k", "v", "scales", "page_table", "lengths", "seen", "scores", "positions", "status"))
 
     def __setattr__(self, name, value):
         # (the calls have the addresses of the old one, which would be given back)
         if name in self._FIXED and "ref" in self.__dict__ and value is not self.__dict__[name]:       # (not so: cache.lengths += 1)
-            raise G10Error("%s of a CacheBuffers is fixed: write to it, or make another" % name)
+            raise G10Error("%s of a %s is fixed: write to it, or make another" % (name, type(self).__name__))
         object.__setattr__(self, name, value)
 
-    def __init__(self, k, v, page_table, lengths, seen=None, scores=None, positions=None, status=None, page_size=None, kv_heads=None):
+    def _begin(self, k, v, page_table, lengths, seen, scores, positions, status):
         self.k, self.v, self.page_table, self.lengths, self.seen = k, v, page_table, lengths, seen
         self.scores, self.positions = scores, positions
         self.device = lengths.device
@@ -603,6 +617,33 @@ class CacheBuffers:
             _typed("seen", seen, torch.int32, (self.num_seqs,), index)
         if (k is None) != (v is None):
             raise G10Error("k and v come together")
+
+    def _end(self):
+        """The C struct; self has sizes and types."""
+        cells = (self.num_pages, self.kv_heads, self.page_size)
+        if self.scores is not None:
+            _typed("scores", self.scores, torch.float32, cells, self.index)
+        if self.positions is not None:
+            _typed("positions", self.positions, torch.int32, cells, self.index)
+        _fits(sequences=self.num_seqs, columns=int(self.page_table.shape[1]), page_size=self.page_size, kv_heads=self.kv_heads, head_dim=self.head_dim)
+        strides = self.k.stride() if self.k is not None else (0, 0, 0, 1)
+        return _Cache(_CACHE_TYPES[self.dtype], self.num_seqs, self.kv_heads, self.head_dim, self.page_size, int(self.page_table.shape[1]),
+                      self.num_pages, _ptr(self.k), _ptr(self.v), strides[0], strides[1], strides[2], _ptr(self.page_table), int(self.page_table.stride(0)),
+                      _ptr(self.lengths), _ptr(self.seen), _ptr(self.scores), _ptr(self.positions), _ptr(self.status))
+
+
+class CacheBuffers(_Buffers):
+    """One layer of a paged key-value cache, as the g10_cache_* calls take it (device tensors, kept alive here).
+
+    k, v: bf16 or fp16 [pages, page_size, kv_heads, head_dim], any strides (the same for both, multiples of 8, the last one 1): a view of
+    [pages, kv_heads, page_size, head_dim] will do.  page_table: int32 [seqs, columns]; lengths, seen: int32 [seqs] (shared by all layers; no
+    call changes them).  scores: float32, positions: int32, both [pages, kv_heads, page_size].  status: int64 [1], made here unless given:
+    data-dependent errors are OR-ed into it.  The calls run on `stream`, or the current stream of the cache's device; what they allocate belongs to
+    the stream that they run on.  No gradients flow through them.  k and v may be None for a cache that is only planned on (then page_size and kv_heads say
+    the sizes).  The tensors are fixed once it is made (what they hold is not: a program writes to them); another tensor wants another CacheBuffers."""
+
+    def __init__(self, k, v, page_table, lengths, seen=None, scores=None, positions=None, status=None, page_size=None, kv_heads=None):
+        self._begin(k, v, page_table, lengths, seen, scores, positions, status)
         if k is not None:
             if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dtype not in _CACHE_TYPES or k.stride(3) != 1:
                 raise G10Error("k and v have to be bf16 or fp16 [pages, page_size, kv_heads, head_dim] of the same strides, the last one 1")
@@ -615,31 +656,49 @@ class CacheBuffers:
                 raise G10Error("without k and v, page_size, kv_heads and scores are wanted")
             self.num_pages, self.page_size, self.kv_heads, self.head_dim = int(scores.shape[0]), page_size, kv_heads, 8
             self.dtype = torch.bfloat16
-        cells = (self.num_pages, self.kv_heads, self.page_size)
-        if scores is not None:
-            _typed("scores", scores, torch.float32, cells, index)
-        if positions is not None:
-            _typed("positions", positions, torch.int32, cells, index)
-        _fits(sequences=self.num_seqs, columns=int(page_table.shape[1]), page_size=self.page_size, kv_heads=self.kv_heads, head_dim=self.head_dim)
-        strides = k.stride() if k is not None else (0, 0, 0, 1)
-        self.c_struct = _Cache(_CACHE_TYPES[self.dtype], self.num_seqs, self.kv_heads, self.head_dim, self.page_size, int(page_table.shape[1]),
-                               self.num_pages, _ptr(k), _ptr(v), strides[0], strides[1], strides[2], _ptr(page_table), int(page_table.stride(0)),
-                               _ptr(lengths), _ptr(seen), _ptr(scores), _ptr(positions), _ptr(self.status))
+        self.c_struct = self._end()
+        self.ref = self.plan_ref = C.byref(self.c_struct)
+
+
+class PackedBuffers(_Buffers):
+    """One layer of a paged key-value cache whose rows are kept in 8 bits, as the g10_packed_* calls take it; g10_cache_plan_evictions takes it, too.
+
+    k, v: int8 or float8_e4m3fn [pages, page_size, kv_heads, head_dim], head_dim a multiple of 16, any strides (the same for both, multiples of 16,
+    the last one 1).  scales: float32 [pages, kv_heads, page_size, 2], of each key and value row.  dtype: of new tokens, queries and outputs (bf16 or fp16).
+    Everything else as CacheBuffers'."""
+
+    def __init__(self, k, v, scales, page_table, lengths, dtype=torch.bfloat16, seen=None, scores=None, positions=None, status=None):
+        if k is None or v is None:
+            raise G10Error("k and v are wanted")
+        self._begin(k, v, page_table, lengths, seen, scores, positions, status)
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.dtype not in _PACKED_CODES or k.stride(3) != 1:
+            raise G10Error("k and v have to be int8 or float8_e4m3fn [pages, page_size, kv_heads, head_dim] of the same strides, the last one 1")
+        if dtype not in _CACHE_TYPES:
+            raise G10Error("dtype has to be bf16 or fp16: got %s" % dtype)
+        self.num_pages, self.page_size, self.kv_heads, self.head_dim = (int(n) for n in k.shape)
+        self.dtype, self.scales = dtype, scales
+        _typed("scales", scales, torch.float32, (self.num_pages, self.kv_heads, self.page_size, 2), self.index)
+        self.c_struct = _Packed(self._end(), _PACKED_CODES[k.dtype], _ptr(scales))
+        self.plan_ref = C.byref(self.c_struct.cache)
         self.ref = C.byref(self.c_struct)
 
 
 _CACHE_TYPES = {torch.bfloat16: 0, torch.float16: 1}
+_PACKED_CODES = {torch.int8: 0, torch.float8_e4m3fn: 1}
 
 
-def _cache_call(call, cache, args, stream):
-    """call(cache, *args, stream) with the cache's device current."""
+def _cache_call(call, cache, kind, args, stream):
+    """call(cache, *args, stream) with the cache's device current; kind: what the cache has to be (None: either)."""
+    if type(cache) is not kind and kind is not None and not isinstance(cache, kind):
+        raise G10Error("this call takes a %s: got a %s" % (kind.__name__, type(cache).__name__))
+    ref = cache.plan_ref if kind is None else cache.ref
     if stream is not None and stream.device_index != cache.index:
         raise G10Error("stream has to belong to %s" % cache.device)
     if torch._C._cuda_getDevice() == cache.index:
-        rc = call(cache.ref, *args, torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream)
+        rc = call(ref, *args, torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream)
     else:
         with torch.cuda.device(cache.index):
-            rc = call(cache.ref, *args, torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream)
+            rc = call(ref, *args, torch._C._cuda_getCurrentRawStream(cache.index) if stream is None else stream.cuda_stream)
     if rc != 0:
         _check(rc)
 
@@ -652,84 +711,133 @@ def _cache_empty(cache, shape, dtype, stream):
         return torch.empty(shape, dtype=dtype, device=cache.device)
 
 
-def g10_cache_append(cache: CacheBuffers, k, v, q=None, q_weight=None, k_weight=None, eps=1e-6, cos=None, sin=None, interleaved=False, counts=None,
-                     q_out=None, stream=None):
-    """Norm of queries and keys per head, position rotation and write to the cache's pages, in one pass.  k, v [seqs, new_tokens, kv_heads,
+def _append_call(name, kind, doc):
+    def call(cache, k, v, q=None, q_weight=None, k_weight=None, eps=1e-6, cos=None, sin=None, interleaved=False, counts=None,
+                 q_out=None, stream=None):
+        dev, heads = cache.index, 0
+        shape, ks = _rows("k", k, cache, cache.kv_heads)
+        v_shape, vs = _rows("v", v, cache, cache.kv_heads)
+        new = shape[1]
+        qs = (0, 0, 0)
+        if q is not None:
+            q_shape, qs = _rows("q", q, cache)
+            heads = q_shape[2]
+            if q_out is None:
+                q_out = _cache_empty(cache, q_shape, q.dtype, stream)
+            else:
+                _typed("q_out", q_out, cache.dtype, q_shape, dev)
+        if v_shape[1] != new or (heads and q_shape[1] != new):
+            raise G10Error("q, k and v have to hold as many tokens")
+        if new > _MOST or heads > _MOST:
+            _fits(new_tokens=new, q_heads=heads)
+        if q_weight is not None:
+            _typed("q_weight", q_weight, cache.dtype, (cache.head_dim,), dev)
+        if k_weight is not None:
+            _typed("k_weight", k_weight, cache.dtype, (cache.head_dim,), dev)
+        half = rows = 0
+        if cos is not None or sin is not None:
+            if cos is None or sin is None or cos.dim() != 2:
+                raise G10Error("cos and sin come together, float32 [positions, rotary_dim / 2]")
+            rows, half = cos.shape
+            if 2 * half > _MOST:
+                _fits(rotary_dim=2 * half)
+            _typed("cos", cos, torch.float32, (rows, half), dev)
+            _typed("sin", sin, torch.float32, (rows, half), dev)
+        if counts is not None:
+            _typed("counts", counts, torch.int32, (cache.num_seqs,), dev)
+        t = _CacheTokens(new, heads, _ptr(q), k.data_ptr(), v.data_ptr(), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], _ptr(q_out) if heads else None,
+                         _ptr(counts), _ptr(q_weight), _ptr(k_weight), eps, _ptr(cos), _ptr(sin), rows, 2 * half, 1 if interleaved else 0)
+        _cache_call(getattr(load_library(), name), cache, kind, (t,), stream)
+        return q_out if heads else None
+
+    call.__name__ = call.__qualname__ = name
+    call.__doc__ = doc
+    return call
+
+
+g10_cache_append = _append_call("g10_cache_append", CacheBuffers, """Norm of queries and keys per head, position rotation and write to the cache's pages, in one pass.  k, v [seqs, new_tokens, kv_heads,
     head_dim], q [seqs, new_tokens, q_heads, head_dim] (strided views, as of one projection's output); q_weight, k_weight [head_dim]; cos, sin
     float32 [positions, rotary_dim / 2]; counts int32 [seqs]: tokens of each sequence that count (None: all).  cache.lengths (and seen) count the
-    new tokens in.  Returns the queries (q_out, made here if None), or None without q."""
-    dev, heads = cache.index, 0
-    shape, ks = _rows("k", k, cache, cache.kv_heads)
-    v_shape, vs = _rows("v", v, cache, cache.kv_heads)
-    new = shape[1]
-    qs = (0, 0, 0)
-    if q is not None:
-        q_shape, qs = _rows("q", q, cache)
-        heads = q_shape[2]
-        if q_out is None:
-            q_out = _cache_empty(cache, q_shape, q.dtype, stream)
-        else:
-            _typed("q_out", q_out, cache.dtype, q_shape, dev)
-    if v_shape[1] != new or (heads and q_shape[1] != new):
-        raise G10Error("q, k and v have to hold as many tokens")
-    if new > _MOST or heads > _MOST:
-        _fits(new_tokens=new, q_heads=heads)
-    if q_weight is not None:
-        _typed("q_weight", q_weight, cache.dtype, (cache.head_dim,), dev)
-    if k_weight is not None:
-        _typed("k_weight", k_weight, cache.dtype, (cache.head_dim,), dev)
-    half = rows = 0
-    if cos is not None or sin is not None:
-        if cos is None or sin is None or cos.dim() != 2:
-            raise G10Error("cos and sin come together, float32 [positions, rotary_dim / 2]")
-        rows, half = cos.shape
-        if 2 * half > _MOST:
-            _fits(rotary_dim=2 * half)
-        _typed("cos", cos, torch.float32, (rows, half), dev)
-        _typed("sin", sin, torch.float32, (rows, half), dev)
-    if counts is not None:
-        _typed("counts", counts, torch.int32, (cache.num_seqs,), dev)
-    t = _CacheTokens(new, heads, _ptr(q), k.data_ptr(), v.data_ptr(), qs[0], qs[1], qs[2], ks[0], ks[1], ks[2], vs[0], vs[1], vs[2], _ptr(q_out) if heads else None,
-                     _ptr(counts), _ptr(q_weight), _ptr(k_weight), eps, _ptr(cos), _ptr(sin), rows, 2 * half, 1 if interleaved else 0)
-    _cache_call(load_library().g10_cache_append, cache, (t,), stream)
-    return q_out if heads else None
+    new tokens in.  Returns the queries (q_out, made here if None), or None without q.""")
+g10_packed_append = _append_call("g10_packed_append", PackedBuffers, """g10_cache_append into a cache of 8-bit rows (a PackedBuffers): keys, after norm and rotation, and values are
+written as codes and scales.  Queries are not packed.""")
+
+
+def _workspace_bytes(name, kind, cache, new_tokens, q_heads, window, sinks, add_scores):
+    if not isinstance(cache, kind):
+        raise G10Error("this call takes a %s: got a %s" % (kind.__name__, type(cache).__name__))
+    _fits(new_tokens=new_tokens, q_heads=q_heads, window=window, sinks=sinks)
+    out = C.c_size_t(0)
+    _check(getattr(load_library(), name)(cache.ref, new_tokens, q_heads, window, sinks, 1 if add_scores else 0, C.byref(out)))
+    return int(out.value)
 
 
 def g10_cache_workspace_bytes(cache: CacheBuffers, new_tokens, q_heads, window=0, sinks=0, add_scores=False) -> int:
     """Bytes of workspace that g10_cache_attend needs."""
-    _fits(new_tokens=new_tokens, q_heads=q_heads, window=window, sinks=sinks)
-    out = C.c_size_t(0)
-    _check(load_library().g10_cache_workspace_bytes(cache.ref, new_tokens, q_heads, window, sinks, 1 if add_scores else 0, C.byref(out)))
-    return int(out.value)
+    return _workspace_bytes("g10_cache_workspace_bytes", CacheBuffers, cache, new_tokens, q_heads, window, sinks, add_scores)
 
 
-def g10_cache_attend(cache: CacheBuffers, q, scale=None, window=0, sinks=0, counts=None, add_scores=False, out=None, lse=None, ws=None, stream=None):
-    """Attention of the new tokens' queries q [seqs, new_tokens, q_heads, head_dim] over the cache (scale: 1 / sqrt(head_dim) if None); returns
+def g10_packed_workspace_bytes(cache: PackedBuffers, new_tokens, q_heads, window=0, sinks=0, add_scores=False) -> int:
+    """Bytes of workspace that g10_packed_attend needs."""
+    return _workspace_bytes("g10_packed_workspace_bytes", PackedBuffers, cache, new_tokens, q_heads, window, sinks, add_scores)
+
+
+def _attend_call(name, kind, workspace_bytes, doc):
+    def call(cache, q, scale=None, window=0, sinks=0, counts=None, add_scores=False, out=None, lse=None, ws=None, stream=None):
+        shape, qs = _rows("q", q, cache)
+        dev, new, heads = cache.index, shape[1], shape[2]
+        if max(new, heads, window, sinks) > _MOST or min(window, sinks) < 0:
+            _fits(new_tokens=new, q_heads=heads, window=window, sinks=sinks)
+        if out is None:
+            out = _cache_empty(cache, shape, q.dtype, stream)
+        else:
+            _typed("out", out, cache.dtype, shape, dev)
+        if lse is not None:
+            _typed("lse", lse, torch.float32, shape[:3], dev)
+        if counts is not None:
+            _typed("counts", counts, torch.int32, (cache.num_seqs,), dev)
+        if ws is None:
+            ws = _cache_empty(cache, max(256, workspace_bytes(cache, new, heads, window, sinks, add_scores)), torch.uint8, stream)
+        elif ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
+            raise G10Error("ws has to be contiguous uint8 on %s" % cache.device)
+        u = _CacheQueries(new, heads, q.data_ptr(), qs[0], qs[1], qs[2], _ptr(counts), out.data_ptr(), _ptr(lse), cache.head_dim ** -0.5 if scale is None else scale,
+                          window, sinks, 1 if add_scores else 0)
+        _cache_call(getattr(load_library(), name), cache, kind, (u, ws.data_ptr(), ws.numel()), stream)
+        return out
+
+    call.__name__ = call.__qualname__ = name
+    call.__doc__ = doc
+    return call
+
+
+g10_cache_attend = _attend_call("g10_cache_attend", CacheBuffers, g10_cache_workspace_bytes, """Attention of the new tokens' queries q [seqs, new_tokens, q_heads, head_dim] over the cache (scale: 1 / sqrt(head_dim) if None); returns
     `out` (made here if None).  lse: float32 [seqs, new_tokens, q_heads] to write the logarithms of the sums to, or None.  window, sinks: only the
     last `window` slots and the first `sinks` are visible (0: all).  add_scores: cache.scores grows by the weights that each slot received.
     ws: a uint8 device tensor of at least g10_cache_workspace_bytes(...) bytes (allocated here when None, at every call: with add_scores its size goes by
     what the page table has room for, which may be GBs); calls that may overlap on the GPU, those of
-    captured graphs among them, need one each."""
-    shape, qs = _rows("q", q, cache)
-    dev, new, heads = cache.index, shape[1], shape[2]
-    if max(new, heads, window, sinks) > _MOST or min(window, sinks) < 0:
-        _fits(new_tokens=new, q_heads=heads, window=window, sinks=sinks)
-    if out is None:
-        out = _cache_empty(cache, shape, q.dtype, stream)
-    else:
-        _typed("out", out, cache.dtype, shape, dev)
-    if lse is not None:
-        _typed("lse", lse, torch.float32, shape[:3], dev)
-    if counts is not None:
-        _typed("counts", counts, torch.int32, (cache.num_seqs,), dev)
-    if ws is None:
-        ws = _cache_empty(cache, max(256, g10_cache_workspace_bytes(cache, new, heads, window, sinks, add_scores)), torch.uint8, stream)
-    elif ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
-        raise G10Error("ws has to be contiguous uint8 on %s" % cache.device)
-    u = _CacheQueries(new, heads, q.data_ptr(), qs[0], qs[1], qs[2], _ptr(counts), out.data_ptr(), _ptr(lse), cache.head_dim ** -0.5 if scale is None else scale,
-                      window, sinks, 1 if add_scores else 0)
-    _cache_call(load_library().g10_cache_attend, cache, (u, ws.data_ptr(), ws.numel()), stream)
-    return out
+    captured graphs among them, need one each.""")
+g10_packed_attend = _attend_call("g10_packed_attend", PackedBuffers, g10_packed_workspace_bytes, """g10_cache_attend over a cache of 8-bit rows (a PackedBuffers): the same
+arguments; workspace of g10_packed_workspace_bytes(...) bytes.""")
+
+
+def g10_packed_read(cache: PackedBuffers, tokens, starts=None, k=None, v=None, stream=None):
+    """Reads rows of a packed cache back: k and v [seqs, tokens, kv_heads, head_dim] of the cache's dtype (any strides, multiples of 8, the last one 1; made here
+    if both are None; of one alone, only that is read) receive slots starts[s] .. starts[s] + tokens - 1 of each sequence (starts: int32 [seqs], None: 0), zeros
+    where the sequence has no slot.  Returns (k, v)."""
+    if not 0 <= tokens <= _MOST:
+        raise G10Error("tokens has to be 0 .. %d: got %s" % (_MOST, tokens))
+    if starts is not None:
+        _typed("starts", starts, torch.int32, (cache.num_seqs,), cache.index)
+    if k is None and v is None:
+        k, v = (_cache_empty(cache, (cache.num_seqs, tokens, cache.kv_heads, cache.head_dim), cache.dtype, stream) for _ in range(2))
+    strides = []
+    for name, t in (("k", k), ("v", v)):
+        strides += (0, 0, 0) if t is None else _rows(name, t, cache, cache.kv_heads)[1][:3]
+        if t is not None and t.shape[1] != tokens:
+            raise G10Error("%s has to hold %d tokens of each sequence: it holds %d" % (name, tokens, t.shape[1]))
+    r = _PackedRows(tokens, _ptr(starts), _ptr(k), _ptr(v), *strides)
+    _cache_call(load_library().g10_packed_read, cache, PackedBuffers, (r,), stream)
+    return k, v
 
 
 def _cache_plan(cache, budget, sinks, recent, moves, counts, new_lengths):
@@ -754,18 +862,27 @@ def g10_cache_plan_evictions(cache: CacheBuffers, budget, sinks=0, recent=0, mov
     if new_lengths is None:
         new_lengths = _cache_empty(cache, (cache.num_seqs,), torch.int32, stream)
     p = _cache_plan(cache, budget, sinks, recent, moves, counts, new_lengths)
-    _cache_call(load_library().g10_cache_plan_evictions, cache, (p,), stream)
+    _cache_call(load_library().g10_cache_plan_evictions, cache, None, (p,), stream)
     return SimpleNamespace(moves=moves, counts=counts, new_lengths=new_lengths)
+
+
+def _evict(call, cache, kind, moves, counts, stream):
+    budget = int(moves.shape[2]) if moves.dim() == 4 else 0
+    if budget > _MOST:
+        _fits(budget=budget)
+    p = _cache_plan(cache, budget, 0, 0, moves, counts, None)
+    _cache_call(call, cache, kind, (p,), stream)
 
 
 def g10_cache_evict(cache: CacheBuffers, moves, counts, stream=None):
     """Carries the moves of a plan out (rows of k and v, scores, positions).  cache.lengths still are those that the plan was made for; the
     program takes new_lengths over once every layer has been evicted."""
-    budget = int(moves.shape[2]) if moves.dim() == 4 else 0
-    if budget > _MOST:
-        _fits(budget=budget)
-    p = _cache_plan(cache, budget, 0, 0, moves, counts, None)
-    _cache_call(load_library().g10_cache_evict, cache, (p,), stream)
+    _evict(load_library().g10_cache_evict, cache, CacheBuffers, moves, counts, stream)
+
+
+def g10_packed_evict(cache: PackedBuffers, moves, counts, stream=None):
+    """g10_cache_evict on a cache of 8-bit rows: codes, scales, scores and positions move."""
+    _evict(load_library().g10_packed_evict, cache, PackedBuffers, moves, counts, stream)
 
 
 def instructions_numpy(em) -> np.ndarray:

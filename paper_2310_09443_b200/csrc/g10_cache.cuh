@@ -149,8 +149,10 @@ struct AppendArgs {
     const float *cos_table, *sin_table;
     int64_t table_rows;
     int new_tokens, q_heads, rotary, interleaved;
+    float *scales;                       // (rows of codes)
 };
 cudaError_t launch_cache_append(const AppendArgs &a, int dtype, cudaStream_t s);
+cudaError_t launch_packed_append(const AppendArgs &a, int dtype, int code, cudaStream_t s);
 
 // What the booking kernel has to know of a tile.
 struct __align__(16) TileNote {
@@ -192,8 +194,23 @@ struct EvictArgs {
     int budget, sinks, recent;
     g10_cache_move *moves;
     int32_t *counts, *new_lengths;
+    int row_units;                       // 16-byte units of a row
+    float2 *scales;                      // of rows of codes, or null
 };
 cudaError_t launch_cache_plan(const EvictArgs &a, cudaStream_t s);
 cudaError_t launch_cache_evict(const EvictArgs &a, cudaStream_t s);
+
+// ---- rows of 8-bit codes (the view's row strides and addresses as those of the other cache, in units of 16 bytes) ----
+struct ReadArgs {
+    CacheView c;
+    const float2 *scales;
+    char *k, *v;
+    int64_t k_seq, k_token, k_head, v_seq, v_token, v_head;
+    const int32_t *starts;
+    int tokens;
+};
+cudaError_t launch_packed_read(const ReadArgs &a, int dtype, int code, cudaStream_t s);
+AttendShape packed_shape(const CacheView &c, int rows, int new_tokens, int window, int sinks);
+cudaError_t launch_packed_attend(const AttendArgs &a, const float2 *scales, int dtype, int code, cudaStream_t s);
 
 }  // namespace g10

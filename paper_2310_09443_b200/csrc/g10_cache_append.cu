@@ -1,5 +1,8 @@
-// Writing new tokens to the key-value cache: norm of queries and keys per head, position rotation, write to the pages, one pass.
-#include "g10_cache.cuh"
+// Writing new tokens to the key-value cache: norm of queries and keys per head, position rotation, write to the pages (as they are, or in 8 bits), one
+// pass.
+#include <type_traits>
+
+#include "g10_packed.cuh"
 
 namespace g10 {
 namespace {
@@ -12,12 +15,14 @@ constexpr int kAppendThreads = 128;
 // through shared memory.  The rotation's 8 cosines and sines are the same for all rows of a team: loaded once, 16 bytes at a time where the
 // tables and rotary_dim allow it.  A block takes `run` tokens of a sequence, one after the other: what is the same for all of them (addresses,
 // lengths, weights) is worked out once, since for prompts the instructions, not the traffic, are what takes the time.
+// With a Code, rows of keys and values go out as 8-bit codes: the row's threads find its largest element while it is still in their registers.
 enum { kNone, kSplit, kPairs, kAny };    // rotation: none, half-split or interleaved pairs in whole 16-byte units, whatever else
 
-template <typename T, int kLanes, int kEach, int kTurn>
+template <typename T, typename Code, int kLanes, int kEach, int kTurn>
 __global__ void __launch_bounds__(kAppendThreads, 6) k_cache_append(const AppendArgs a, int shares, int runs, int run)
 {
     constexpr int kTeams = kAppendThreads / kLanes;
+    constexpr bool kPacked = !std::is_void<Code>::value;
     __shared__ __align__(16) float s_x[kAppendThreads * 8];
     const CacheView &c = a.c;
     const int lane = threadIdx.x % kLanes, team = threadIdx.x / kLanes;
@@ -43,7 +48,7 @@ __global__ void __launch_bounds__(kAppendThreads, 6) k_cache_append(const Append
         const int head = is_q ? row : is_k ? row - a.q_heads : row - a.q_heads - c.kv_heads;
         from[i] = is_q ? a.q + q_from + 2 * head * a.q_head : is_k ? a.k + k_from + 2 * head * a.k_head : a.v + v_from + 2 * head * a.v_head;
         to[i] = is_q ? a.q_out + 2 * (((int64_t)s * a.new_tokens * a.q_heads + head) * c.head_dim + d0)
-                     : const_cast<char *>(is_k ? c.k : c.v) + 16 * head * c.head_stride + 2 * d0;
+                     : const_cast<char *>(is_k ? c.k : c.v) + 16 * head * c.head_stride + (kPacked ? 1 : 2) * d0;
         // (those of padding too: what they hold is not used)
         u[i] = __ldg((const uint4 *)(from[i] + 2 * (int64_t)t0 * (is_q ? a.q_token : is_k ? a.k_token : a.v_token)));
     }
@@ -101,8 +106,8 @@ __global__ void __launch_bounds__(kAppendThreads, 6) k_cache_append(const Append
             const int row = (share * kEach + i) * kTeams + team;
             const bool is_q = row < a.q_heads, is_k = !is_q && row < a.q_heads + c.kv_heads;
             unsigned *w = &u[i].x;
-            if (__any_sync(0xffffffffu, is_q || is_k)) {       // (some row of the warp has arithmetic to do)
-                float x[8];
+            float x[8];
+            if (kPacked || __any_sync(0xffffffffu, is_q || is_k)) {      // (some row of the warp has arithmetic to do)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) { const float2 p = Pair<T>::unpack(w[e]); x[2 * e] = p.x; x[2 * e + 1] = p.y; }
                 if (a.q_weight != nullptr || a.k_weight != nullptr) {
@@ -112,14 +117,14 @@ __global__ void __launch_bounds__(kAppendThreads, 6) k_cache_append(const Append
 #pragma unroll
                     for (int o = kLanes / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
                     const float r = rsqrtf(fmaf(sum, a.inv_dim, a.eps));
-                    if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr) {
+                    if (is_q ? a.q_weight != nullptr : a.k_weight != nullptr && (!kPacked || is_k)) {
                         const unsigned g[4] = {is_q ? qw.x : kw.x, is_q ? qw.y : kw.y, is_q ? qw.z : kw.z, is_q ? qw.w : kw.w};
 #pragma unroll
                         for (int e = 0; e < 4; ++e) { const float2 p = Pair<T>::unpack(g[e]); x[2 * e] *= r * p.x; x[2 * e + 1] *= r * p.y; }
                     }
                 }
                 if (kTurn == kPairs || (kTurn == kAny && a.interleaved)) {
-                    if (turns) {
+                    if (turns && (!kPacked || is_q || is_k)) {
 #pragma unroll
                         for (int e = 0; e < 8; e += 2) {
                             const float y = fmaf(x[e], co[e], x[e + 1] * si[e]), z = fmaf(x[e + 1], co[e + 1], x[e] * si[e + 1]);
@@ -130,7 +135,7 @@ __global__ void __launch_bounds__(kAppendThreads, 6) k_cache_append(const Append
                     __syncwarp();
                     *(float4 *)&mate[d0] = make_float4(x[0], x[1], x[2], x[3]); *(float4 *)&mate[d0 + 4] = make_float4(x[4], x[5], x[6], x[7]);
                     __syncwarp();
-                    if (turns) {
+                    if (turns && (!kPacked || is_q || is_k)) {
                         if (kTurn == kSplit) {
                             const float *const other = &mate[d0 < half ? d0 + half : d0 - half];
                             const float4 y = *(const float4 *)other, z = *(const float4 *)(other + 4);
@@ -145,12 +150,29 @@ __global__ void __launch_bounds__(kAppendThreads, 6) k_cache_append(const Append
                         }
                     }
                 }
-                if (is_q || is_k) {
+                if (kPacked ? is_q : is_q || is_k) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[e] = Pair<T>::pack(x[2 * e], x[2 * e + 1]);
                 }
             }
-            if (to[i] != nullptr && (is_q || spot.page >= 0)) *(uint4 *)(to[i] + (is_q ? q_at : kv_at)) = u[i];
+            if constexpr (kPacked) {
+                // (as unsigned numbers the magnitudes are in order, infinities and NaN above all others)
+                unsigned top = 0;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+#pragma unroll
+                for (int o = kLanes / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+                if (!is_q && to[i] != nullptr && spot.page >= 0) {
+                    float scale;
+                    *(uint2 *)(to[i] + kv_at) = packed_row<Code>(x, top, scale);
+                    if (lane == 0) {
+                        const int head = row - a.q_heads - (is_k ? 0 : c.kv_heads);
+                        a.scales[2 * (cell + (int64_t)head * c.page_size) + (is_k ? 0 : 1)] = scale;
+                    }
+                }
+            }
+            if (kPacked && !is_q) {
+            } else if (to[i] != nullptr && (is_q || spot.page >= 0)) *(uint4 *)(to[i] + (is_q ? q_at : kv_at)) = u[i];
             if (is_k && spot.page >= 0 && lane == 0) {
                 const int64_t at = cell + (int64_t)(row - a.q_heads) * c.page_size;
                 if (c.scores != nullptr) c.scores[at] = 0.0f;
@@ -166,7 +188,7 @@ __global__ void __launch_bounds__(kAppendThreads, 6) k_cache_append(const Append
     if (bad != 0 && threadIdx.x == 0) raise_status(c.status, bad);
 }
 
-template <typename T, int kLanes, int kEach>
+template <typename T, typename Code, int kLanes, int kEach>
 cudaError_t launch(const AppendArgs &a, int shares, cudaStream_t s)
 {
     const int half = a.rotary / 2;
@@ -177,12 +199,12 @@ cudaError_t launch(const AppendArgs &a, int shares, cudaStream_t s)
     const int runs = (a.new_tokens + run - 1) / run;
     const int64_t blocks = (int64_t)a.c.num_seqs * runs * shares;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    const auto kernel = half == 0 ? k_cache_append<T, kLanes, kEach, kNone> : !wide ? k_cache_append<T, kLanes, kEach, kAny>
-                      : a.interleaved ? k_cache_append<T, kLanes, kEach, kPairs> : k_cache_append<T, kLanes, kEach, kSplit>;
+    const auto kernel = half == 0 ? k_cache_append<T, Code, kLanes, kEach, kNone> : !wide ? k_cache_append<T, Code, kLanes, kEach, kAny>
+                      : a.interleaved ? k_cache_append<T, Code, kLanes, kEach, kPairs> : k_cache_append<T, Code, kLanes, kEach, kSplit>;
     kernel<<<(unsigned)blocks, kAppendThreads, 0, s>>>(a, shares, runs, run); count_launch();
     return cudaGetLastError();
 }
-template <typename T, int kLanes>
+template <typename T, typename Code, int kLanes>
 cudaError_t launch_lanes(const AppendArgs &a, cudaStream_t s)
 {
     constexpr int kTeams = kAppendThreads / kLanes;
@@ -190,18 +212,28 @@ cudaError_t launch_lanes(const AppendArgs &a, cudaStream_t s)
     const int64_t tokens = (int64_t)a.c.num_seqs * a.new_tokens;
     auto shares = [&](int each) { return (rows + kTeams * each - 1) / (kTeams * each); };
     // (several rows a thread once there are blocks enough for all SMs all the same: fewer look-ups and rotations for each)
-    if (tokens * shares(4) >= 148 * 16 && rows > 2 * kTeams) return launch<T, kLanes, 4>(a, shares(4), s);
-    if (tokens * shares(2) >= 148 * 16 && rows > kTeams) return launch<T, kLanes, 2>(a, shares(2), s);
-    return launch<T, kLanes, 1>(a, shares(1), s);
+    if (tokens * shares(4) >= 148 * 16 && rows > 2 * kTeams) return launch<T, Code, kLanes, 4>(a, shares(4), s);
+    if (tokens * shares(2) >= 148 * 16 && rows > kTeams) return launch<T, Code, kLanes, 2>(a, shares(2), s);
+    return launch<T, Code, kLanes, 1>(a, shares(1), s);
+}
+
+template <typename T, typename Code>
+cudaError_t launch_type(const AppendArgs &a, cudaStream_t s)
+{
+    const int lanes = (a.c.head_dim + 7) / 8;
+    return lanes <= 8 ? launch_lanes<T, Code, 8>(a, s) : lanes <= 16 ? launch_lanes<T, Code, 16>(a, s) : launch_lanes<T, Code, 32>(a, s);
 }
 
 }  // namespace
 
 cudaError_t launch_cache_append(const AppendArgs &a, int dtype, cudaStream_t s)
 {
-    const int lanes = (a.c.head_dim + 7) / 8;
-    if (dtype == G10_BF16) return lanes <= 8 ? launch_lanes<__nv_bfloat16, 8>(a, s) : lanes <= 16 ? launch_lanes<__nv_bfloat16, 16>(a, s) : launch_lanes<__nv_bfloat16, 32>(a, s);
-    return lanes <= 8 ? launch_lanes<__half, 8>(a, s) : lanes <= 16 ? launch_lanes<__half, 16>(a, s) : launch_lanes<__half, 32>(a, s);
+    return dtype == G10_BF16 ? launch_type<__nv_bfloat16, void>(a, s) : launch_type<__half, void>(a, s);
+}
+cudaError_t launch_packed_append(const AppendArgs &a, int dtype, int code, cudaStream_t s)
+{
+    if (code == G10_INT8) return dtype == G10_BF16 ? launch_type<__nv_bfloat16, Int8>(a, s) : launch_type<__half, Int8>(a, s);
+    return dtype == G10_BF16 ? launch_type<__nv_bfloat16, E4m3>(a, s) : launch_type<__half, E4m3>(a, s);
 }
 
 }  // namespace g10

@@ -888,20 +888,18 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_book(const AttendArgs a,
 }
 
 // ---- host ----
-template <typename T, int kSteps, int kCols>
-cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
+// The three kernels for up to 16 rows.  `kernel`: the first, kRows rows of kDim dims, `smem` bytes of shared memory; known, most_known: what the device holds of it.
+template <typename T, int kRows, int kDim, typename Args>
+cudaError_t launch_few(void (*kernel)(const Args, int, int, int), size_t smem, int *known, int *most_known, const Args &a, const AttendShape &z, cudaStream_t s)
 {
-    typedef Config<T, kSteps, kCols> C;
-    const auto kernel = k_cache_attend<T, kSteps, kCols>;
-    static int known[kMaxDevices];                       // blocks that the device holds at a time
     int dev = 0, room = 0;
     cudaError_t e = cudaGetDevice(&dev);
     if (e != cudaSuccess) return e;
-    if ((e = allow_launch((const void *)kernel, C::kSmem, 1)) != cudaSuccess) return e;
+    if ((e = allow_launch((const void *)kernel, smem, 1)) != cudaSuccess) return e;
     if (dev < kMaxDevices) room = __atomic_load_n(&known[dev], __ATOMIC_ACQUIRE);
     if (room == 0) {
         int each = 0;
-        if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, kThreads, C::kSmem)) != cudaSuccess) return e;
+        if ((e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&each, kernel, kThreads, smem)) != cudaSuccess) return e;
         room = each * current_sm_count();
         if (room < 1) return cudaErrorInvalidDevice;
         if (dev < kMaxDevices) __atomic_store_n(&known[dev], room, __ATOMIC_RELEASE);
@@ -910,14 +908,13 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     held = held < 1 ? 1 : held > kMaxBlocks ? kMaxBlocks : held;
     const int64_t grid = z.tiles >= kLong * held && kCuts * held <= kMaxBlocks ? kCuts * held : held;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = s;
+    cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
     // Clusters: where every item has at most four tiles a block and all blocks run at a time.
     const int64_t cap = z.items > 0 ? z.tiles / z.items : 0;
     int cluster = 0;
     if (z.items <= room && cap >= 1) {
-        static int most_known[kMaxDevices];
         const void *const kernels[] = {(const void *)kernel};
-        const int most = largest_cluster(kernels, false, kThreads, C::kSmem, most_known);
+        const int most = largest_cluster(kernels, false, kThreads, smem, most_known);
         int n = 1;
         while (2 * n <= 8 && 2 * n <= most && 2 * n <= cap && z.items * 2 * n <= room) n *= 2;
         if (most >= 1 && cap <= 4 * n) cluster = n;
@@ -934,12 +931,20 @@ cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
-    if (cluster == 0 && (e = cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, (int)held, C::kDim, C::kRows)) != cudaSuccess) return e;
+    const AttendArgs &b = a;
+    if (cluster == 0 && (e = cudaLaunchKernelEx(&cfg, k_cache_join<T>, b, (int)held, kDim, kRows)) != cudaSuccess) return e;
     if (a.logits == nullptr) return cudaSuccess;
     const int64_t warps = kJoinThreads / 32, blocks = (z.tiles + warps - 1) / warps, most = 148 * 6;
     cfg.gridDim = dim3((unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most));      // (a table without columns: no tile)
     const auto book = a.rows <= 4 ? k_cache_book<1> : a.rows <= 8 ? k_cache_book<2> : k_cache_book<4>;
-    return cudaLaunchKernelEx(&cfg, book, a, C::kRows, cluster == 0);
+    return cudaLaunchKernelEx(&cfg, book, b, kRows, cluster == 0);
+}
+template <typename T, int kSteps, int kCols>
+cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
+{
+    typedef Config<T, kSteps, kCols> C;
+    static int known[kMaxDevices], most_known[kMaxDevices];
+    return launch_few<T, C::kRows, C::kDim>(k_cache_attend<T, kSteps, kCols>, C::kSmem, known, most_known, a, z, s);
 }
 template <typename T, int kSteps>
 cudaError_t launch_steps(const AttendArgs &a, const AttendShape &z, cudaStream_t s)

@@ -221,7 +221,7 @@ __global__ void __launch_bounds__(kThreads) k_cache_plan(const EvictArgs a, int 
 }
 
 // A warp takes kMoves moves at a time: a lane each looks source and target up and moves score and position, then the rows go, 16 bytes a lane, all
-// 128 units under way before the first is stored.  Pure traffic: 4 * head_dim bytes read and written per move.
+// 128 units under way before the first is stored.  Pure traffic: key and value row (4 * head_dim bytes, or 2 * head_dim of codes) read and written per move.
 __global__ void __launch_bounds__(kMoveThreads, 5) k_cache_evict(const EvictArgs a, unsigned unit_mul)
 {
     const int item = blockIdx.y, s = item / a.c.kv_heads, head = item % a.c.kv_heads;
@@ -230,7 +230,7 @@ __global__ void __launch_bounds__(kMoveThreads, 5) k_cache_evict(const EvictArgs
     const int length = cache_length(a.c, s, bad);
     int n = __ldg(&a.counts[item]);
     if (n < 0 || n > a.budget) { bad |= G10_DEV_BAD_MOVE; n = 0; }
-    const int units = a.c.head_dim / 4, half = units / 2;                          // 16-byte units of a move: half of k, half of v
+    const int half = a.row_units, units = 2 * half;                                // 16-byte units of a move: half of k, half of v
     for (int r0 = (blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5)) * kMoves; r0 < n; r0 += gridDim.x * (kMoveThreads / 32) * kMoves) {
         unsigned row = 0xffffffffu;                      // lanes 0 .. 7: sources, 8 .. 15: targets
         int64_t cell = -1;
@@ -247,6 +247,7 @@ __global__ void __launch_bounds__(kMoveThreads, 5) k_cache_evict(const EvictArgs
         if (lane < kMoves && cell >= 0 && to_cell >= 0) {
             if (a.c.scores != nullptr) a.c.scores[to_cell] = a.c.scores[cell];
             if (a.c.positions != nullptr) a.c.positions[to_cell] = a.c.positions[cell];
+            if (a.scales != nullptr) a.scales[to_cell] = a.scales[cell];
         }
         constexpr int kAhead = 4;
 #pragma unroll 1
@@ -308,7 +309,7 @@ cudaError_t launch_cache_evict(const EvictArgs &a, cudaStream_t s)
 {
     const int64_t items = (int64_t)a.c.num_seqs * a.c.kv_heads, step = 65535 / a.c.kv_heads * a.c.kv_heads;      // (gridDim.y ends at 65 535)
     const int64_t each = kMoveThreads / 32 * kMoves, most = (a.budget + each - 1) / each, want = (148 * 8 + items - 1) / items;
-    const unsigned units = (unsigned)a.c.head_dim / 4, unit_mul = ((1u << 20) + units - 1) / units;              // (u / units, u < 512, is exact)
+    const unsigned units = 2 * (unsigned)a.row_units, unit_mul = ((1u << 20) + units - 1) / units;              // (u / units, u < 512, is exact)
     for (int64_t i = 0; i < items; i += step) {
         const int64_t n = items - i < step ? items - i : step, seq = i / a.c.kv_heads;
         EvictArgs b = a;
