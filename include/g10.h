@@ -495,6 +495,16 @@ int32_t g10_cache_attend(const g10_cache *cache, const g10_cache_queries *querie
 int32_t g10_cache_workspace_bytes(const g10_cache *cache, int32_t new_tokens, int32_t q_heads, int32_t window, int32_t sinks,
                                   int32_t add_scores, size_t *out_bytes);
 
+/* g10_cache_attend for a batch whose sequences begin alike: the first *shared slots of every sequence stand where sequence 0's row of the page table says (many answers to one
+   question, questions about one document).  The same result, up to rounding; keys and values of the beginning are read once for all sequences.  *shared (one word on
+   the device) is at most lengths[s] - c_s for every sequence with c_s > 0 (else G10_DEV_BAD_LENGTH, and as many slots are taken as shared as can be); sequence 0's
+   row holds the beginning's pages even where that sequence has no new tokens.  Whole tiles of 64 slots are read once, what is left of the beginning for each sequence.
+   No window, no add_scores: a page that sequences share does not belong to one that could evict from it. */
+int32_t g10_cache_attend_shared(const g10_cache *cache, const g10_cache_queries *queries, const int32_t *shared, void *ws, size_t ws_bytes, void *stream);
+/* Its workspace: 4 head_dim + 8 bytes for each query head of a new token, and room for the parts that are joined (4 head_dim + 8 bytes a row of some thousand blocks of
+   rows, and of all that the beginning has). */
+int32_t g10_cache_shared_workspace_bytes(const g10_cache *cache, int32_t new_tokens, int32_t q_heads, size_t *out_bytes);
+
 /* Which tokens leave: for each sequence with more than `budget` slots, and each key-value head on its own, `budget` slots are kept:
    first those whose position is below `sinks` or at least seen[s] - recent, then by score, the largest first (NaN counts as the
    lowest); among equals the lower slot.  The r-th kept slot at or behind `budget`, counted in slot order, moves to the r-th slot

@@ -28,7 +28,7 @@ STATUS = {0: "ALREADY_FITS", 1: "FIT", 2: "EXHAUSTED", 3: "ITERATION_LIMIT"}
 EXPORTS = ("g10_vitality", "g10_pressure_timeline", "g10_candidate_geometry", "g10_plan_migrations",
            "g10_workspace_bytes", "g10_strerror", "g10_version", "g10_pressure_timeline_static", "g10_schedule_prefetch", "g10_emit_instructions", "g10_characterize", "g10_plan_batch", "g10_plan_cyclic", "g10_launch_count",
            "g10_cache_append", "g10_cache_attend", "g10_cache_plan_evictions", "g10_cache_evict", "g10_cache_workspace_bytes",
-           "g10_packed_append", "g10_packed_read", "g10_packed_attend", "g10_packed_workspace_bytes", "g10_packed_evict")
+           "g10_cache_attend_shared", "g10_cache_shared_workspace_bytes", "g10_packed_append", "g10_packed_read", "g10_packed_attend", "g10_packed_workspace_bytes", "g10_packed_evict")
 STATIC_MAX_KERNELS, STATIC_MAX_TENSORS = 32768, 131072
 
 INSTRUCTION_DTYPE = np.dtype([("opcode", "<i4"), ("tensor", "<i4"), ("target", "<i4"), ("record", "<i4"),
@@ -191,6 +191,10 @@ def load_library():
         lib.g10_cache_evict.argtypes = [C.POINTER(_Cache), C.POINTER(_CachePlan), C.c_void_p]
         lib.g10_cache_workspace_bytes.restype = C.c_int32
         lib.g10_cache_workspace_bytes.argtypes = [C.POINTER(_Cache), C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
+        lib.g10_cache_attend_shared.restype = C.c_int32
+        lib.g10_cache_attend_shared.argtypes = [C.POINTER(_Cache), C.POINTER(_CacheQueries), C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        lib.g10_cache_shared_workspace_bytes.restype = C.c_int32
+        lib.g10_cache_shared_workspace_bytes.argtypes = [C.POINTER(_Cache), C.c_int32, C.c_int32, C.POINTER(C.c_size_t)]
         lib.g10_packed_append.restype = C.c_int32
         lib.g10_packed_append.argtypes = [C.POINTER(_Packed), C.POINTER(_CacheTokens), C.c_void_p]
         lib.g10_packed_read.restype = C.c_int32
@@ -818,6 +822,42 @@ g10_cache_attend = _attend_call("g10_cache_attend", CacheBuffers, g10_cache_work
     captured graphs among them, need one each.""")
 g10_packed_attend = _attend_call("g10_packed_attend", PackedBuffers, g10_packed_workspace_bytes, """g10_cache_attend over a cache of 8-bit rows (a PackedBuffers): the same
 arguments; workspace of g10_packed_workspace_bytes(...) bytes.""")
+
+
+def g10_cache_shared_workspace_bytes(cache: CacheBuffers, new_tokens, q_heads) -> int:
+    """Bytes of workspace that g10_cache_attend_shared needs."""
+    if not isinstance(cache, CacheBuffers):
+        raise G10Error("this call takes a CacheBuffers: got a %s" % type(cache).__name__)
+    _fits(new_tokens=new_tokens, q_heads=q_heads)
+    out = C.c_size_t(0)
+    _check(load_library().g10_cache_shared_workspace_bytes(cache.ref, new_tokens, q_heads, C.byref(out)))
+    return int(out.value)
+
+
+def g10_cache_attend_shared(cache: CacheBuffers, q, shared, scale=None, counts=None, out=None, lse=None, ws=None, stream=None):
+    """g10_cache_attend for a batch whose sequences begin alike: the first `shared` slots (int32 [1] on the cache's device) of every sequence stand where the
+    first row of the page table says, and are read once for all.  q, scale, counts, out, lse as there; ws: g10_cache_shared_workspace_bytes(...) bytes, allocated
+    here when None; calls that may overlap on the GPU need one each."""
+    shape, qs = _rows("q", q, cache)
+    dev, new, heads = cache.index, shape[1], shape[2]
+    if max(new, heads) > _MOST:
+        _fits(new_tokens=new, q_heads=heads)
+    _typed("shared", shared, torch.int32, (1,), dev)
+    if out is None:
+        out = _cache_empty(cache, shape, q.dtype, stream)
+    else:
+        _typed("out", out, cache.dtype, shape, dev)
+    if lse is not None:
+        _typed("lse", lse, torch.float32, shape[:3], dev)
+    if counts is not None:
+        _typed("counts", counts, torch.int32, (cache.num_seqs,), dev)
+    if ws is None:
+        ws = _cache_empty(cache, max(256, g10_cache_shared_workspace_bytes(cache, new, heads)), torch.uint8, stream)
+    elif ws.dtype is not torch.uint8 or ws.get_device() != dev or not ws.is_contiguous():
+        raise G10Error("ws has to be contiguous uint8 on %s" % cache.device)
+    u = _CacheQueries(new, heads, q.data_ptr(), qs[0], qs[1], qs[2], _ptr(counts), out.data_ptr(), _ptr(lse), cache.head_dim ** -0.5 if scale is None else scale, 0, 0, 0)
+    _cache_call(load_library().g10_cache_attend_shared, cache, CacheBuffers, (u, shared.data_ptr(), ws.data_ptr(), ws.numel()), stream)
+    return out
 
 
 def g10_packed_read(cache: PackedBuffers, tokens, starts=None, k=None, v=None, stream=None):

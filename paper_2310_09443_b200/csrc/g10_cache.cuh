@@ -181,6 +181,15 @@ struct AttendArgs {
     int mute;                            // which arrival the first block of the kernels for many rows keeps to itself (0: none)
 #endif
 };
+// Attention of a batch behind a shared beginning, in two parts.
+struct SharedArgs : AttendArgs {
+    int32_t *shared;                     // [1] slots that are shared: whole tiles, checked
+    int each;                            // new tokens of a sequence
+    float2 *begin_ml;                    // [sequences][new tokens][query heads] maximum and sum over the beginning
+    float *begin_o;                      // ... [head_dim] its sums, not divided
+};
+struct BeginArgs : SharedArgs {};        // the beginning: one sequence, whose tokens are all sequences'
+struct RestArgs : SharedArgs {};         // what each sequence has behind it
 // Sizes that the workspace goes by.
 struct AttendShape {
     int row_blocks, block_rows, logit_rows, padded_dim;  // (logit_rows 0: the rows' kernels, which leave no logits)
@@ -188,6 +197,8 @@ struct AttendShape {
 };
 AttendShape attend_shape(const CacheView &c, int rows, int new_tokens, int window, int sinks);
 cudaError_t launch_cache_attend(const AttendArgs &a, int dtype, cudaStream_t s);
+// `begin` has its own room (shape: attend_shape of its sequence); shared: as the caller has it.
+cudaError_t launch_cache_shared(const BeginArgs &begin, const RestArgs &rest, const int32_t *shared, int dtype, cudaStream_t s);
 
 struct EvictArgs {
     CacheView c;

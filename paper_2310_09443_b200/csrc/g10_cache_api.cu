@@ -150,6 +150,35 @@ int32_t attend_places(const AttendShape &z, void *ws, size_t ws_bytes, AttendArg
     return G10_OK;
 }
 
+// Behind a shared beginning: what the beginning leaves, and room for either part in turn.
+struct SharedLayout {
+    size_t shared, ml, o, room, bytes;
+};
+SharedLayout shared_layout(const AttendShape &begin, const AttendShape &rest, int64_t rows, int head_dim)
+{
+    SharedLayout l;
+    l.shared = 0;
+    l.ml = align_up(l.shared + sizeof(int32_t));
+    l.o = align_up(l.ml + sizeof(float2) * (size_t)rows);
+    l.room = align_up(l.o + sizeof(float) * (size_t)rows * head_dim);
+    const size_t x = attend_layout(begin, false).bytes, y = attend_layout(rest, false).bytes;
+    l.bytes = l.room + (x > y ? x : y);
+    return l;
+}
+// The beginning as one sequence with all sequences' new tokens.
+CacheView begin_view(const CacheView &c)
+{
+    CacheView v = c;
+    v.num_seqs = 1;
+    return v;
+}
+int32_t check_shared(const CacheView &c, int32_t new_tokens, int32_t q_heads)
+{
+    const int32_t rc = check_heads(c, new_tokens, q_heads, 0, 0);
+    if (rc != G10_OK) return rc;
+    return (int64_t)c.num_seqs * new_tokens * (q_heads / c.kv_heads) > kCacheLimit ? G10_ERR_LIMIT : G10_OK;
+}
+
 int32_t evict_args(const g10_cache_plan *p, EvictArgs &a, bool &nothing)
 {
     nothing = false;
@@ -200,6 +229,43 @@ int32_t g10_cache_attend(const g10_cache *cache, const g10_cache_queries *u, voi
     if (rc != G10_OK || nothing) return rc;
     rc = attend_places(attend_shape(a.c, a.rows, a.new_tokens, a.window, a.sinks), ws, ws_bytes, a);
     return rc != G10_OK ? rc : status_of(launch_cache_attend(a, cache->dtype, (cudaStream_t)stream));
+}
+
+int32_t g10_cache_shared_workspace_bytes(const g10_cache *cache, int32_t new_tokens, int32_t q_heads, size_t *out_bytes)
+{
+    CacheView c;
+    int32_t rc = view_of(cache, false, c);
+    if (rc == G10_OK && !out_bytes) rc = G10_ERR_ARG;
+    if (rc == G10_OK) rc = check_shared(c, new_tokens, q_heads);
+    if (rc != G10_OK) return rc;
+    const int tokens = c.num_seqs * new_tokens, group = q_heads / c.kv_heads;
+    *out_bytes = shared_layout(attend_shape(begin_view(c), tokens * group, tokens, 0, 0), attend_shape(c, new_tokens * group, new_tokens, 0, 0),
+                               (int64_t)tokens * q_heads, c.head_dim).bytes;
+    return G10_OK;
+}
+
+int32_t g10_cache_attend_shared(const g10_cache *cache, const g10_cache_queries *u, const int32_t *shared, void *ws, size_t ws_bytes, void *stream)
+{
+    RestArgs a;
+    bool nothing;
+    int32_t rc = view_of(cache, true, a.c);
+    if (rc == G10_OK) rc = attend_args(cache, u, a, nothing);
+    if (rc != G10_OK) return rc;
+    if (!shared || u->window > 0 || u->add_scores) return G10_ERR_ARG;
+    if (nothing) return G10_OK;
+    if ((rc = check_shared(a.c, u->new_tokens, u->q_heads)) != G10_OK) return rc;
+    a.each = a.new_tokens;
+    BeginArgs b;
+    static_cast<SharedArgs &>(b) = a;
+    b.c = begin_view(a.c);
+    b.new_tokens = a.c.num_seqs * a.new_tokens; b.rows = b.new_tokens * b.group; b.counts = nullptr;
+    const AttendShape y = attend_shape(b.c, b.rows, b.new_tokens, 0, 0), z = attend_shape(a.c, a.rows, a.new_tokens, 0, 0);
+    const SharedLayout l = shared_layout(y, z, (int64_t)b.new_tokens * a.q_heads, a.c.head_dim);
+    if (!ws || ((uintptr_t)ws & (kAlign - 1)) || ws_bytes < l.bytes) return G10_ERR_WORKSPACE;
+    a.shared = b.shared = (int32_t *)((char *)ws + l.shared);
+    a.begin_ml = b.begin_ml = (float2 *)((char *)ws + l.ml); a.begin_o = b.begin_o = (float *)((char *)ws + l.o);
+    if ((rc = attend_places(y, (char *)ws + l.room, l.bytes - l.room, b)) != G10_OK || (rc = attend_places(z, (char *)ws + l.room, l.bytes - l.room, a)) != G10_OK) return rc;
+    return status_of(launch_cache_shared(b, a, shared, cache->dtype, (cudaStream_t)stream));
 }
 
 int32_t g10_cache_plan_evictions(const g10_cache *cache, const g10_cache_plan *p, void *stream)

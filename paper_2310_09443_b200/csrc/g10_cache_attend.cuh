@@ -17,6 +17,8 @@
 // This file is for up to 16 rows per key-value head (new tokens times heads of the group), one block of rows each; more are g10_cache_rows.cuh's, which has the
 // sharing out of tiles and the second kernel from here.
 #pragma once
+#include <type_traits>
+
 #include "g10_cache.cuh"
 
 namespace g10 {
@@ -79,6 +81,36 @@ __device__ __forceinline__ Seq seq_of(const AttendArgs &a, int s, ull &bad)
     if (q.count == 0) q.tiles = 0;
     return q;
 }
+// Behind a shared beginning (whole tiles of it, and less than a sequence with new tokens holds without them).
+__device__ __forceinline__ Seq seq_of(const BeginArgs &a, int, ull &)
+{
+    Seq q;
+    q.length = __ldcg(a.shared); q.count = a.new_tokens;
+    q.tiles = q.length / kTile; q.head_tiles = 0; q.skipped = 0;
+    return q;
+}
+__device__ __forceinline__ Seq seq_of(const RestArgs &a, int s, ull &bad)
+{
+    Seq q;
+    q.length = cache_length(a.c, s, bad);
+    q.count = cache_count(a.counts, s, a.new_tokens, q.length, bad);
+    q.head_tiles = 0; q.skipped = __ldcg(a.shared) / kTile;
+    q.tiles = q.count == 0 ? 0 : (q.length + kTile - 1) / kTile - q.skipped;
+    return q;
+}
+// The queries of a sequence's token t, head 0.
+__device__ __forceinline__ const char *queries_of(const AttendArgs &a, int s, int t) { return a.q + 2 * (s * a.q_seq + t * a.q_token); }
+__device__ __forceinline__ const char *queries_of(const BeginArgs &a, int, int t)
+{
+    const int s = t / a.each;
+    return a.q + 2 * (s * a.q_seq + (t - s * a.each) * a.q_token);
+}
+// Last slot that token t sees.
+template <typename Args>
+__device__ __forceinline__ int stands_at(const Args &, const Seq &q, int t) { return std::is_same<Args, BeginArgs>::value ? q.length - 1 : q.length - q.count + t; }
+// Slots from here on are not seen by the first token.
+template <typename Args>
+__device__ __forceinline__ int seen_by_all(const Args &a, const Seq &q) { return stands_at(a, q, 0); }
 __device__ __forceinline__ int first_slot(const Seq &q, int idx) { return (idx < q.head_tiles ? idx : idx + q.skipped) * kTile; }
 
 // The tiles of all sequences, added up: every thread of the block has a run of sequences of its own.
@@ -88,15 +120,15 @@ struct Tally {
     int64_t total;
 };
 // (kUnit: tiles that count as one)
-template <int kUnit>
-__device__ __forceinline__ Seq units_of(const AttendArgs &a, int s, ull &bad)
+template <int kUnit, typename Args>
+__device__ __forceinline__ Seq units_of(const Args &a, int s, ull &bad)
 {
     Seq q = seq_of(a, s, bad);
     q.tiles = (q.tiles + kUnit - 1) / kUnit;
     return q;
 }
-template <int kThreads, int kUnit = 1>
-__device__ __forceinline__ Tally tally_of(const AttendArgs &a, ull &bad)
+template <int kThreads, int kUnit = 1, typename Args>
+__device__ __forceinline__ Tally tally_of(const Args &a, ull &bad)
 {
     __shared__ int64_t s_sum[kThreads / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
@@ -149,8 +181,8 @@ struct Place {
     int64_t before;
     int s;
 };
-template <int kUnit = 1>
-__device__ __forceinline__ void place_of(const AttendArgs &a, const Tally &t, int64_t u, int per, Place *to)
+template <int kUnit = 1, typename Args>
+__device__ __forceinline__ void place_of(const Args &a, const Tally &t, int64_t u, int per, Place *to)
 {
     if (!(t.start * per <= u && u < (t.start + t.sum) * per)) return;
     int64_t before = t.start * per;
@@ -170,8 +202,8 @@ struct Cursor {
     int head, block;                     // key-value head and block of rows: item = head * row_blocks + block
     Seq q;
 };
-template <int kUnit = 1>
-__device__ __forceinline__ void cursor_at(const AttendArgs &a, Cursor &u, const Place &p, int64_t tile)
+template <int kUnit = 1, typename Args>
+__device__ __forceinline__ void cursor_at(const Args &a, Cursor &u, const Place &p, int64_t tile)
 {
     ull ignored = 0;
     u.s = p.s;
@@ -180,8 +212,8 @@ __device__ __forceinline__ void cursor_at(const AttendArgs &a, Cursor &u, const 
     u.item = (int)divided(in, u.q.tiles); u.idx = (int)(in - (int64_t)u.item * u.q.tiles);
     u.head = u.item / a.row_blocks; u.block = u.item - u.head * a.row_blocks;
 }
-template <int kUnit = 1>
-__device__ __forceinline__ void cursor_next(const AttendArgs &a, Cursor &u, int per)
+template <int kUnit = 1, typename Args>
+__device__ __forceinline__ void cursor_next(const Args &a, Cursor &u, int per)
 {
     if (++u.idx < u.q.tiles) return;
     u.idx = 0;
@@ -202,6 +234,12 @@ __device__ __forceinline__ uint64_t leaves_first()
 {
     uint64_t p;
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(p));
+    return p;
+}
+__device__ __forceinline__ uint64_t stays()
+{
+    uint64_t p;
+    asm volatile("createpolicy.fractional.L2::evict_normal.b64 %0, 1.0;" : "=l"(p));
     return p;
 }
 __device__ __forceinline__ void copy16(unsigned dst, const void *src, uint64_t policy)
@@ -250,6 +288,34 @@ __device__ __forceinline__ void part_add(Part &p, float top, float sum, const fl
     p.sum = p.sum * f + sum * g;
     p.o = make_float4(p.o.x * f + o.x * g, p.o.y * f + o.y * g, p.o.z * f + o.z * g, p.o.w * f + o.w * g);
 }
+// A row's result, four of its elements: maximum, sum of the weights and sums over all slots.  `at`: number of the row among [sequences][new tokens][query heads]; real: it has a
+// token; sums: where the booking kernel looks for its lse.
+template <typename T, typename Args>
+__device__ __forceinline__ void give(const Args &a, int64_t at, int d, bool real, float top, float sum, float4 o, int64_t sums)
+{
+    if constexpr (std::is_same<Args, BeginArgs>::value) {
+        if (d == 0) a.begin_ml[at] = make_float2(top, sum);
+        *(float4 *)(a.begin_o + at * a.c.head_dim + d) = o;
+        return;
+    }
+    if constexpr (std::is_same<Args, RestArgs>::value) {
+        if (real && __ldcg(a.shared) > 0) {
+            const float2 ml = __ldcg(&a.begin_ml[at]);
+            Part p{top, sum, o};
+            part_add(p, ml.x, ml.y, __ldcg((const float4 *)(a.begin_o + at * a.c.head_dim + d)));
+            top = p.top; sum = p.sum; o = p.o;
+        }
+    }
+    const float inv = 1.0f / sum;                        // (sees nothing: zero, whatever the sums hold)
+    uint2 w = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
+    if (sum == 0.0f) w = make_uint2(0, 0);
+    *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
+    if (d == 0) {
+        const float lse = top + log2f(sum * Weights<T>::kUnlift);
+        if (a.lse != nullptr) a.lse[at] = sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
+        if (a.books) a.sums[sums] = sum == 0.0f ? INFINITY : lse;
+    }
+}
 // Blocks that share an SM, and tiles in a block's ring.  What a warp does for a tile is a chain that two warps a scheduler do not fill, so there are as many
 // blocks as leave each a ring of two tiles and the registers it needs: four up to 64 dims (24 sequences of 4100 slots against two: 50 -> 39 us, 64 of
 // 16 000: 280 -> 238), three above (128 dims: 57.6 -> 55.7, 428 -> 421).  Not so for rows of about 160 bytes, no whole number of the memory's 64: they are
@@ -294,8 +360,8 @@ struct Config {
 // The tiles of an item are then numbered from item * cap on.
 // ref is a maximum of the past (see Weights), so that the sums are rescaled and the warp's lanes compared only when a logit is far above it, a few times per
 // piece.
-template <typename T, int kSteps, int kCols>
-__global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cache_attend(const AttendArgs a, int held_blocks, int cluster, int cap)
+template <typename T, int kSteps, int kCols, typename Args>
+__global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cache_attend(const Args a, int held_blocks, int cluster, int cap)
 {
     typedef Config<T, kSteps, kCols> C;
     constexpr int kStages = C::kStages;
@@ -326,6 +392,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
             if (my_item == 0 && tid == 0) *a.total = (int64_t)a.c.num_seqs * per * cap;
         }
         if (tiles == 0) {                                // (the whole cluster alike)
+            if (std::is_same<Args, BeginArgs>::value) return;
             const int chunks = a.c.head_dim / 8;
             for (int i = rank * kThreads + tid; i < C::kRows * chunks; i += cluster * kThreads) {
                 const int row = i / chunks;
@@ -349,7 +416,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
         cursor_at(a, now, s_place, begin);
     }
     bad = 0;
-    const int my_s = now.s, my_head = now.head;
+    const int my_s = now.s, my_head = now.head, my_count = now.q.count;
     ahead = now;
     const unsigned ring = smem_of(smem) + part * kStages * C::kPartBytes;
     // where the row of this lane's slot begins (lanes 16 .. 31: as lanes 0 .. 15), in the tile that `ahead` stands at
@@ -416,7 +483,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
             auto row_of = [&](int row) -> const char * { // (null: no such row)
                 const int t = row / a.group;
                 if (row >= a.rows || t >= now.q.count) return nullptr;
-                return a.q + 2 * (now.s * a.q_seq + t * a.q_token + (head * a.group + row % a.group) * a.q_head);
+                return queries_of(a, now.s, t) + 2 * (head * a.group + row % a.group) * a.q_head;
             };
             if (C::kHeld) {
 #pragma unroll
@@ -447,7 +514,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
                 for (int h = 0; h < 2; ++h) {
                     m[j][h] = -INFINITY; l[j][h] = 0.0f;
                     const int row = j * 8 + (lane & 3) * 2 + h, t = row / a.group;
-                    p[j][h] = row < a.rows && t < now.q.count ? now.q.length - now.q.count + t : -1;
+                    p[j][h] = row < a.rows && t < now.q.count ? stands_at(a, now.q, t) : -1;
                 }
             }
         }
@@ -486,7 +553,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
             }
         }
         // ---- what each row sees ----
-        const int slot0 = first_slot(now.q, now.idx) + part * 16, seen0 = now.q.length - now.q.count;
+        const int slot0 = first_slot(now.q, now.idx) + part * 16, seen0 = seen_by_all(a, now.q);
         const bool whole = slot0 + 15 <= seen0 && (a.window == 0 || slot0 > now.q.length - 1 - a.window);
 #pragma unroll
         for (int j = 0; j < kCols; ++j)
@@ -640,15 +707,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
                     *(float4 *)(a.part + (piece * C::kRows + row) * C::kDim + d) = o;
                 } else if (d < a.c.head_dim) {
                     const int64_t at = ((int64_t)now.s * a.new_tokens + row / a.group) * a.q_heads + now.head * a.group + row % a.group;
-                    const float inv = 1.0f / sum;        // (sees nothing: zero, whatever the sums hold)
-                    uint2 w = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
-                    if (sum == 0.0f) w = make_uint2(0, 0);
-                    *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
-                    if (d == 0) {
-                        const float lse = top + log2f(sum * Weights<T>::kUnlift);
-                        if (a.lse != nullptr) a.lse[at] = sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
-                        if (a.books) a.sums[item * C::kRows + row] = sum == 0.0f ? INFINITY : lse;
-                    }
+                    give<T>(a, at, d, row / a.group < now.q.count, top, sum, o, item * C::kRows + row);
                 }
             }
             fresh = true;
@@ -675,15 +734,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
                 if (ml.y != 0.0f) part_add(p, ml.x, ml.y, o);                      // (a part that saw nothing has no sums)
             }
             const int64_t at = ((int64_t)my_s * a.new_tokens + row / a.group) * a.q_heads + my_head * a.group + row % a.group;
-            const float inv = 1.0f / p.sum;
-            uint2 w = make_uint2(Pair<T>::pack(p.o.x * inv, p.o.y * inv), Pair<T>::pack(p.o.z * inv, p.o.w * inv));
-            if (p.sum == 0.0f) w = make_uint2(0, 0);
-            *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
-            if (d == 0) {
-                const float lse = p.top + log2f(p.sum * Weights<T>::kUnlift);
-                if (a.lse != nullptr) a.lse[at] = p.sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
-                if (a.books) a.sums[(int64_t)my_item * C::kRows + row] = p.sum == 0.0f ? INFINITY : lse;
-            }
+            give<T>(a, at, d, row / a.group < my_count, p.top, p.sum, p.o, (int64_t)my_item * C::kRows + row);
         }
         cluster_sync();                                  // (nobody leaves while its memory may still be read)
     }
@@ -741,8 +792,8 @@ __device__ __forceinline__ Pieces pieces_of(int64_t item, int64_t first, int til
 // The second kernel.  (1) An item that was cut into pieces is joined by the blocks whose turn its pieces' shares are, each taking a part of its rows
 // and dimensions; (2) rows of sequences without tiles are written.  What follows from the lengths alone is worked out while the first
 // kernel still runs.
-template <typename T>
-__global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a, int held_blocks, int padded_dim, int block_rows)
+template <typename T, typename Args>
+__global__ void __launch_bounds__(kJoinThreads) k_cache_join(const Args a, int held_blocks, int padded_dim, int block_rows)
 {
     __shared__ Place s_place[2];
     __shared__ Cursor s_cut[2];
@@ -783,20 +834,12 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const AttendArgs a,
             const Part p = part_join(a, w.item, w.b0, w.b1, block_rows, r, padded_dim, d, lanes);
             if (e + lane / lanes < e1 && (lane & (lanes - 1)) == 0) {
                 const int64_t at = ((int64_t)s * a.new_tokens + row / a.group) * a.q_heads + head * a.group + row % a.group;
-                const float inv = 1.0f / p.sum;
-                uint2 o = make_uint2(Pair<T>::pack(p.o.x * inv, p.o.y * inv), Pair<T>::pack(p.o.z * inv, p.o.w * inv));
-                if (p.sum == 0.0f) o = make_uint2(0, 0);
-                *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = o;
-                if (d == 0) {
-                    const float lse = p.top + log2f(p.sum * Weights<T>::kUnlift);
-                    if (a.lse != nullptr) a.lse[at] = p.sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
-                    if (a.books) a.sums[w.item * block_rows + r] = p.sum == 0.0f ? INFINITY : lse;
-                }
+                give<T>(a, at, d, row / a.group < s_cut[side].q.count, p.top, p.sum, p.o, w.item * block_rows + r);
             }
         }
     }
     // ---- (2) ----
-    for (int s = b; s < a.c.num_seqs && blockIdx.y == 0; s += gridDim.x) {
+    for (int s = b; s < a.c.num_seqs && blockIdx.y == 0 && !std::is_same<Args, BeginArgs>::value; s += gridDim.x) {
         if (seq_of(a, s, ignored).tiles > 0) continue;
         const int64_t rows = (int64_t)a.new_tokens * a.q_heads, n = rows * (a.c.head_dim / 8);
         for (int64_t i = tid; i < n; i += kJoinThreads) ((uint4 *)(a.out + 2 * s * rows * a.c.head_dim))[i] = make_uint4(0, 0, 0, 0);
@@ -889,7 +932,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_book(const AttendArgs a,
 
 // ---- host ----
 // The three kernels for up to 16 rows.  `kernel`: the first, kRows rows of kDim dims, `smem` bytes of shared memory; known, most_known: what the device holds of it.
-template <typename T, int kRows, int kDim, typename Args>
+template <typename T, int kRows, int kDim, typename JoinArgs, typename Args>
 cudaError_t launch_few(void (*kernel)(const Args, int, int, int), size_t smem, int *known, int *most_known, const Args &a, const AttendShape &z, cudaStream_t s)
 {
     int dev = 0, room = 0;
@@ -931,28 +974,28 @@ cudaError_t launch_few(void (*kernel)(const Args, int, int, int), size_t smem, i
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
-    const AttendArgs &b = a;
-    if (cluster == 0 && (e = cudaLaunchKernelEx(&cfg, k_cache_join<T>, b, (int)held, kDim, kRows)) != cudaSuccess) return e;
+    const JoinArgs &b = a;
+    if (cluster == 0 && (e = cudaLaunchKernelEx(&cfg, k_cache_join<T, JoinArgs>, b, (int)held, kDim, kRows)) != cudaSuccess) return e;
     if (a.logits == nullptr) return cudaSuccess;
     const int64_t warps = kJoinThreads / 32, blocks = (z.tiles + warps - 1) / warps, most = 148 * 6;
     cfg.gridDim = dim3((unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most));      // (a table without columns: no tile)
     const auto book = a.rows <= 4 ? k_cache_book<1> : a.rows <= 8 ? k_cache_book<2> : k_cache_book<4>;
     return cudaLaunchKernelEx(&cfg, book, b, kRows, cluster == 0);
 }
-template <typename T, int kSteps, int kCols>
-cudaError_t launch(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
+template <typename T, int kSteps, int kCols, typename Args>
+cudaError_t launch(const Args &a, const AttendShape &z, cudaStream_t s)
 {
     typedef Config<T, kSteps, kCols> C;
     static int known[kMaxDevices], most_known[kMaxDevices];
-    return launch_few<T, C::kRows, C::kDim>(k_cache_attend<T, kSteps, kCols>, C::kSmem, known, most_known, a, z, s);
+    return launch_few<T, C::kRows, C::kDim, Args>(k_cache_attend<T, kSteps, kCols, Args>, C::kSmem, known, most_known, a, z, s);
 }
-template <typename T, int kSteps>
-cudaError_t launch_steps(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
+template <typename T, int kSteps, typename Args>
+cudaError_t launch_steps(const Args &a, const AttendShape &z, cudaStream_t s)
 {
     return z.block_rows == 8 ? launch<T, kSteps, 1>(a, z, s) : launch<T, kSteps, 2>(a, z, s);
 }
-template <typename T>
-cudaError_t launch_type(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
+template <typename T, typename Args>
+cudaError_t launch_type(const Args &a, const AttendShape &z, cudaStream_t s)
 {
     switch (z.padded_dim / 16) {
     case 4: return launch_steps<T, 4>(a, z, s);

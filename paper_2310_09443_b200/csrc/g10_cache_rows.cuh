@@ -199,13 +199,13 @@ struct Wide {
 
 // A row's queries, from global memory to their exchanged places (with the sign of the scale, so that the largest product is the largest logit).
 // Half `part` of its units.
-template <int kDims>
-__device__ __forceinline__ void bring_queries(const AttendArgs &a, const Cursor &u, int first_row, int r, int part, char *s_q)
+template <int kDims, typename Args>
+__device__ __forceinline__ void bring_queries(const Args &a, const Cursor &u, int first_row, int r, int part, char *s_q)
 {
     constexpr int kUnits = 4 * kDims;
     const int row = first_row + r, t = row / a.group;
     const bool real = row < a.rows && t < u.q.count;
-    const char *from = a.q + 2 * (u.s * a.q_seq + t * a.q_token + (u.head * a.group + row % a.group) * a.q_head);
+    const char *from = (real ? queries_of(a, u.s, t) : a.q) + 2 * (u.head * a.group + row % a.group) * a.q_head;
     const unsigned flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
 #pragma unroll 8
     for (int j = 0; j < kUnits; ++j) {
@@ -216,11 +216,12 @@ __device__ __forceinline__ void bring_queries(const AttendArgs &a, const Cursor 
     }
 }
 
-template <typename T, int kDims>
-__global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const AttendArgs a, int held_blocks)
+template <typename T, int kDims, typename Args>
+__global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a, int held_blocks)
 {
     typedef Wide<kDims> C;
     constexpr int S = C::kStages;
+    constexpr bool kBegin = std::is_same<Args, BeginArgs>::value, kRest = std::is_same<Args, RestArgs>::value;
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t s_bar[2 * S + 10];
     __shared__ Place s_place;
@@ -263,7 +264,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
         // ---- the loaders: 32 slots each, one a lane; a tile is told full as its copies land ----
         const int part = warp - 9;
         constexpr unsigned kNone = 0xffffffffu;
-        const uint64_t policy = leaves_first();
+        const uint64_t policy = kBegin && a.row_blocks > 1 ? stays() : leaves_first();
         int stage = 0;
         unsigned round = 1;
         // (the page is loaded a tile ahead, and looked at when its turn comes)
@@ -290,7 +291,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
             if (!wait(free_ + 8 * stage, round)) break;
             const unsigned told = full + 8 * stage, to = smem_of(s_ring) + stage * C::kStageBytes;
             if (++stage == S) { stage = 0; round ^= 1; }
-            const bool all = __all_sync(0xffffffffu, mine != kNone) && a.c.head_dim == C::kDim && a.row_blocks == 1;
+            const bool all = __all_sync(0xffffffffu, mine != kNone) && a.c.head_dim == C::kDim && (kBegin || a.row_blocks == 1);
             if (all) {
 #pragma unroll
                 for (int i = 0; i < C::kUnits; ++i) {
@@ -395,8 +396,8 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
         for (int u0 = 0; u0 < n;) {
             // ---- a piece: tiles u0 .. u1 - 1 ----
             const int u1 = u0 + min(now.q.tiles - now.idx, n - u0);
-            const int row = now.block * kWideRows + r, t = row / a.group, seen0 = now.q.length - now.q.count;
-            const int p = row < a.rows && t < now.q.count ? seen0 + t : -1;
+            const int row = now.block * kWideRows + r, t = row / a.group, seen0 = seen_by_all(a, now.q), count = now.q.count;
+            const int p = row < a.rows && t < count ? stands_at(a, now.q, t) : -1;
             const bool busy = now.block * kWideRows + (warp & 3) * 32 < a.rows;    // (this warp has rows)
             const int last_whole = a.window > 0 ? now.q.length - 1 - a.window : -1;
             float m = -INFINITY, l = 0.0f;
@@ -554,14 +555,28 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
             after_sync();
             const float2 one = s_ml[0][r], two = s_ml[1][r];
             const float top = fmaxf(one.x, two.x), ref = top == -INFINITY ? 0.0f : top;
-            const float f = exp2_of(one.x - ref), g = exp2_of(two.x - ref), sum = p < 0 ? 0.0f : one.y * f + two.y * g, inv = 1.0f / sum;
+            const float f = exp2_of(one.x - ref), g = exp2_of(two.x - ref), sum = p < 0 ? 0.0f : one.y * f + two.y * g;
+            // (with what the row has of a shared beginning: f_all of this, g_all of that)
+            float total_top = top, total = sum, f_all = 1.0f, g_all = 0.0f;
+            if constexpr (kRest) {
+                if (real && all && t < count && __ldcg(a.shared) > 0) {
+                    const float2 ml = __ldcg(&a.begin_ml[at]);
+                    total_top = fmaxf(top, ml.x);
+                    const float ref_all = total_top == -INFINITY ? 0.0f : total_top;
+                    f_all = exp2_of(top - ref_all); g_all = exp2_of(ml.x - ref_all);
+                    total = sum * f_all + ml.y * g_all;
+                }
+            }
+            const float inv = 1.0f / total;
             const bool has_one = C::kTeams == 1 || u1 - u0 > 1 || (u0 & 1) == 0, has_two = C::kTeams == 2 && (u1 - u0 > 1 || (u0 & 1) == 1);
             if (real && team == 0) {
                 a.ml[r * a.pieces + piece] = make_float2(p < 0 ? -INFINITY : top, sum);
-                if (all) {
-                    const float lse = top + log2f(sum * Weights<T>::kUnlift);
-                    if (a.lse != nullptr) a.lse[at] = sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
-                    if (a.books) a.sums[item * kWideRows + r] = sum == 0.0f ? INFINITY : lse;
+                if (all && kBegin) {
+                    if constexpr (kBegin) a.begin_ml[at] = make_float2(top, sum);
+                } else if (all) {
+                    const float lse = total_top + log2f(total * Weights<T>::kUnlift);
+                    if (a.lse != nullptr) a.lse[at] = total == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
+                    if (a.books) a.sums[item * kWideRows + r] = total == 0.0f ? INFINITY : lse;
                 }
             }
             if (busy && going) {
@@ -584,7 +599,25 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
 #pragma unroll
                         for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(fmaf(__uint_as_float(y[i]), g, __uint_as_float(o[i])));
                     }
+                    if constexpr (kRest) {
+                        if (g_all != 0.0f) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4) {
+                                if (c + i >= a.c.head_dim) continue;
+                                const float4 y = __ldcg((const float4 *)(a.begin_o + at * a.c.head_dim + c + i));
+                                const float z[4] = {y.x, y.y, y.z, y.w};
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[i + e] = __float_as_uint(fmaf(__uint_as_float(o[i + e]), f_all, z[e] * g_all));
+                            }
+                        }
+                    }
                     if (!real) {
+                    } else if (all && kBegin) {
+                        if constexpr (kBegin) {
+#pragma unroll
+                            for (int i = 0; i < 32; i += 4)
+                                if (c + i < a.c.head_dim) *(uint4 *)(a.begin_o + at * a.c.head_dim + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                        }
                     } else if (all) {
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
@@ -593,7 +626,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Attend
                                 unsigned *yw = &y.x;
 #pragma unroll
                                 for (int e = 0; e < 4; ++e)          // (sees nothing: zero, whatever the sums hold)
-                                    yw[e] = sum == 0.0f ? 0u : Pair<T>::pack(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
+                                    yw[e] = total == 0.0f ? 0u : Pair<T>::pack(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
                                 *(uint4 *)(a.out + 2 * (at * a.c.head_dim + c + 8 * i)) = y;
                             }
                     } else {
@@ -852,17 +885,17 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
     if (warp == 8) { after_sync(); tmem_give_back(tmem, C::kColumns); }
 }
 
-template <typename T, int kDims>
-cudaError_t launch_wide(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
+template <typename T, int kDims, typename Args>
+cudaError_t launch_wide(const Args &a, const AttendShape &z, cudaStream_t s)
 {
     typedef Wide<kDims> C;
-    const auto kernel = k_cache_attend_wide<T, kDims>;
-    const auto book = k_cache_book_wide<T, kDims>;
+    const auto kernel = k_cache_attend_wide<T, kDims, Args>;
     cudaError_t e;
     const int sms = current_sm_count();
     if (sms < 1) return cudaErrorInvalidDevice;
     if ((e = allow_launch((const void *)kernel, C::kSmem, 1)) != cudaSuccess) return e;
-    if (a.books && (e = allow_launch((const void *)book, Book<kDims>::kSmem, 1)) != cudaSuccess) return e;
+    if constexpr (std::is_same<Args, AttendArgs>::value)
+        if (a.books && (e = allow_launch((const void *)k_cache_book_wide<T, kDims>, Book<kDims>::kSmem, 1)) != cudaSuccess) return e;
     int64_t held = z.tiles < sms ? z.tiles : sms;        // (a block fills an SM)
     held = held < 1 ? 1 : held > kMaxWideBlocks / kCuts ? kMaxWideBlocks / kCuts : held;
     const int64_t grid = z.tiles >= kLong * held ? kCuts * held : held;
@@ -874,13 +907,17 @@ cudaError_t launch_wide(const AttendArgs &a, const AttendShape &z, cudaStream_t 
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
     cfg.gridDim = dim3((unsigned)grid, 4);               // (of the many elements of a piece each takes a part)
-    if ((e = cudaLaunchKernelEx(&cfg, k_cache_join<T>, a, (int)held, C::kDim, kWideRows)) != cudaSuccess || !a.books) return e;
-    cfg.blockDim = dim3(kBookThreads); cfg.dynamicSmemBytes = Book<kDims>::kSmem;
-    cfg.gridDim = dim3((unsigned)held);
-    return cudaLaunchKernelEx(&cfg, book, a);
+    if ((e = cudaLaunchKernelEx(&cfg, k_cache_join<T, Args>, a, (int)held, C::kDim, kWideRows)) != cudaSuccess) return e;
+    if constexpr (std::is_same<Args, AttendArgs>::value) {
+        if (!a.books) return cudaSuccess;
+        cfg.blockDim = dim3(kBookThreads); cfg.dynamicSmemBytes = Book<kDims>::kSmem;
+        cfg.gridDim = dim3((unsigned)held);
+        return cudaLaunchKernelEx(&cfg, k_cache_book_wide<T, kDims>, a);
+    }
+    return cudaSuccess;
 }
-template <typename T>
-cudaError_t launch_wide_type(const AttendArgs &a, const AttendShape &z, cudaStream_t s)
+template <typename T, typename Args>
+cudaError_t launch_wide_type(const Args &a, const AttendShape &z, cudaStream_t s)
 {
     switch (z.padded_dim / 64) {
     case 1: return launch_wide<T, 1>(a, z, s);

@@ -175,7 +175,7 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
         cursor_at(a, now, s_place, begin);
     }
     bad = 0;
-    const int my_s = now.s, my_head = now.head;
+    const int my_s = now.s, my_head = now.head, my_count = now.q.count;
     ahead = now;
     const unsigned ring = smem_of(smem) + part * kStages * C::kPartBytes;
     // where the row of this lane's slot begins (lanes 16 .. 31: as lanes 0 .. 15), in the tile that `ahead` stands at, and its scales
@@ -542,15 +542,7 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
                         *(float4 *)(a.part + (piece * C::kRows + row) * C::kDim + d) = o;
                     } else if (d < a.c.head_dim) {
                         const int64_t at = ((int64_t)now.s * a.new_tokens + row / a.group) * a.q_heads + now.head * a.group + row % a.group;
-                        const float inv = 1.0f / sum;    // (sees nothing: zero, whatever the sums hold)
-                        uint2 w = make_uint2(Pair<T>::pack(o.x * inv, o.y * inv), Pair<T>::pack(o.z * inv, o.w * inv));
-                        if (sum == 0.0f) w = make_uint2(0, 0);
-                        *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
-                        if (d == 0) {
-                            const float lse = best + log2f(sum * Weights<T>::kUnlift);
-                            if (a.lse != nullptr) a.lse[at] = sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
-                            if (a.books) a.sums[item * C::kRows + row] = sum == 0.0f ? INFINITY : lse;
-                        }
+                        give<T>(a, at, d, row / a.group < now.q.count, best, sum, o, item * C::kRows + row);
                     }
                 }
                 __syncthreads();                         // (the ring may be written again)
@@ -578,15 +570,7 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
                 if (ml.y != 0.0f) part_add(p, ml.x, ml.y, o);                      // (a part that saw nothing has no sums)
             }
             const int64_t at = ((int64_t)my_s * a.new_tokens + row / a.group) * a.q_heads + my_head * a.group + row % a.group;
-            const float inv = 1.0f / p.sum;
-            uint2 w = make_uint2(Pair<T>::pack(p.o.x * inv, p.o.y * inv), Pair<T>::pack(p.o.z * inv, p.o.w * inv));
-            if (p.sum == 0.0f) w = make_uint2(0, 0);
-            *(uint2 *)(a.out + 2 * (at * a.c.head_dim + d)) = w;
-            if (d == 0) {
-                const float lse = p.top + log2f(p.sum * Weights<T>::kUnlift);
-                if (a.lse != nullptr) a.lse[at] = p.sum == 0.0f ? -INFINITY : lse * 0.69314718055994531f;
-                if (a.books) a.sums[(int64_t)my_item * C::kRows + row] = p.sum == 0.0f ? INFINITY : lse;
-            }
+            give<T>(a, at, d, row / a.group < my_count, p.top, p.sum, p.o, (int64_t)my_item * C::kRows + row);
         }
         cluster_sync();                                  // (nobody leaves while its memory may still be read)
     }
@@ -598,7 +582,7 @@ cudaError_t launch_packed(const PackedArgs &a, const AttendShape &z, cudaStream_
 {
     typedef PackedConfig<kGroups, kCols> C;
     static int known[kMaxDevices], most_known[kMaxDevices];
-    return launch_few<T, C::kRows, C::kDim>(k_packed_attend<T, Code, kGroups, kCols>, C::kSmem, known, most_known, a, z, s);
+    return launch_few<T, C::kRows, C::kDim, AttendArgs>(k_packed_attend<T, Code, kGroups, kCols>, C::kSmem, known, most_known, a, z, s);
 }
 template <typename T, typename Code, int kGroups>
 cudaError_t launch_packed_rows(const PackedArgs &a, const AttendShape &z, cudaStream_t s)

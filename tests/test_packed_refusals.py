@@ -117,3 +117,20 @@ def test_nothing_to_do(lib):
     assert lib.g10_packed_read(packed(num_seqs=0), rows(), None) == 0
     assert lib.g10_packed_read(packed(), rows(tokens=0), None) == 0
     assert lib.g10_packed_read(packed(), rows(k=None, v=None), None) == 0
+
+
+def test_attend_behind_a_shared_beginning(lib):
+    out = C.c_size_t(0)
+    cache = lambda **change: C.byref(packed(**change)._obj.cache)
+    bytes_of = lambda c, *more: lib.g10_cache_shared_workspace_bytes(c, *more, C.byref(out))
+    call = lambda c, u=None, shared=FAKE, ws=FAKE, n=1 << 40: lib.g10_cache_attend_shared(c, u or queries(), shared, ws, n, None)
+    assert bytes_of(cache(), 1, 8) == 0
+    for ws, n in ((None, 1 << 40), (FAKE + 8, 1 << 40), (FAKE, out.value - 1)):
+        assert call(cache(), ws=ws, n=n) == -3
+    assert call(cache(), shared=None) == -1 and call(None) == -1 and call(cache(dtype=3)) == -1
+    for change, code in ((dict(window=4), -1), (dict(add_scores=1), -1), (dict(q=None), -1), (dict(new_tokens=0), -1), (dict(q_heads=6), -1), (dict(new_tokens=513), -2),
+                         (dict(scale=float("nan")), -1)):
+        assert call(cache(), queries(**change)) == code
+    assert call(cache(num_seqs=0)) == 0
+    assert bytes_of(cache(), 0, 8) == -1 and bytes_of(cache(), 1, 6) == -1 and bytes_of(cache(num_seqs=65535), 512, 8) == 0
+    assert lib.g10_cache_shared_workspace_bytes(cache(), 1, 8, None) == -1
