@@ -20,7 +20,7 @@ SOURCES = ["g10_api.cu", "g10_passes.cu", "g10_planner.cu", "g10_planner_lazy.cu
            "g10_static.cu", "g10_limits.cu", "g10_cache_api.cu", "g10_cache_append.cu", "g10_cache_attend_bf16.cu", "g10_cache_attend_fp16.cu",
            "g10_cache_rows_bf16.cu", "g10_cache_rows_fp16.cu", "g10_cache_evict.cu", "g10_cache_shared_bf16.cu", "g10_cache_shared_fp16.cu",
            "g10_packed_read.cu", "g10_packed_attend_bf16_int8.cu", "g10_packed_attend_bf16_e4m3.cu", "g10_packed_attend_fp16_int8.cu",
-           "g10_packed_attend_fp16_e4m3.cu"]
+           "g10_packed_attend_fp16_e4m3.cu", "g10_packed_rows_bf16.cu", "g10_packed_rows_fp16.cu"]
 HEADERS = ["g10_device.cuh", "g10_internal.h", "g10_planner.cuh", "g10_cache.cuh", "g10_cache_attend.cuh", "g10_cache_rows.cuh", "g10_cache_shared.cuh", "g10_packed.cuh", "g10_packed_attend.cuh"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]
 

@@ -342,7 +342,6 @@ int32_t g10_packed_attend(const g10_packed *packed, const g10_cache_queries *u, 
     int32_t rc = packed_view_of(packed, true, a.c);
     if (rc == G10_OK) rc = attend_args(&packed->cache, u, a, nothing);
     if (rc != G10_OK || nothing) return rc;
-    if (a.rows > 16) return G10_ERR_LIMIT;
     rc = attend_places(packed_shape(a.c, a.rows, a.new_tokens, a.window, a.sinks), ws, ws_bytes, a);
     return rc != G10_OK ? rc : status_of(launch_packed_attend(a, (const float2 *)packed->scales, packed->cache.dtype, packed->code, (cudaStream_t)stream));
 }

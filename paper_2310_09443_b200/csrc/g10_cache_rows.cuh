@@ -14,15 +14,30 @@
 //
 // Warps: 0 - 7 weights and results (a lane per row), 8 issues the products (one thread), 9 and 10 bring the tiles.  Keys and values lie in
 // shared memory as the products want them, 128-byte rows of 64 dimensions with their 16-byte units exchanged by the row's number (the 128-byte swizzle);
-// pages are no whole tiles, so rows are copied one by one, 16 bytes at a time, to their exchanged places.  The product of tile u with the queries is
+// pages are no whole tiles, so rows are copied one by one, 16 bytes at a time, to their exchanged places.  (Rows of 8-bit codes are loaded, turned into what they
+// stand for, rounded to the products' type, and stored there: the next tile's codes are on their way to registers meanwhile.)  The product of tile u with the queries is
 // issued before those of the one or two tiles before it with the values, so that it runs while the weights are worked out.
 #pragma once
 #include <type_traits>
 
 #include "g10_cache_attend.cuh"
+#include "g10_packed.cuh"
 
 namespace g10 {
+
+// Attention over rows of codes.
+template <typename Code_>
+struct PackedRowsArgs : AttendArgs {
+    typedef Code_ Code;
+    const float2 *scales;                // of key and value rows
+};
+
 namespace attend {
+
+template <typename Args>
+struct CodeOf { typedef void type; };
+template <typename Code>
+struct CodeOf<PackedRowsArgs<Code>> { typedef Code type; };
 
 constexpr int kWideRows = 128;           // of a block
 constexpr int kRowThreads = 256, kLoadThreads = 64, kWideThreads = kRowThreads + 32 + kLoadThreads;      // 8 warps of rows, 1 that issues, 2 that load
@@ -216,6 +231,42 @@ __device__ __forceinline__ void bring_queries(const Args &a, const Cursor &u, in
     }
 }
 
+// Rows of codes on their way through a loading warp's registers, 32 of them, 16 codes a lane and step.  `mine`: where the row of this lane's slot begins, in units of 16
+// bytes (all ones: nowhere, zeros).
+template <typename T, typename Code, int kDims>
+struct CodeRows {
+    static constexpr int kChunks = 4 * kDims;
+    uint4 codes[kChunks];
+    __device__ __forceinline__ void ask(const char *base, unsigned mine, int head_dim)
+    {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = i * 32 + lane, row = c / kChunks, chunk = c % kChunks;
+            const unsigned from = __shfl_sync(0xffffffffu, mine, row);
+            codes[i] = make_uint4(0, 0, 0, 0);
+            if (from != 0xffffffffu && chunk * 16 < head_dim) codes[i] = __ldg((const uint4 *)(base + 16 * ((int64_t)from + chunk)));
+        }
+    }
+    // to the rows from `row0` on of blocks of 64 dimensions; scale: of this lane's slot
+    __device__ __forceinline__ void put(unsigned to, int row0, int block, float scale)
+    {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int i = 0; i < kChunks; ++i) {
+            const int c = i * 32 + lane, row = c / kChunks, chunk = c % kChunks;
+            const float by = __shfl_sync(0xffffffffu, scale, row);
+            const unsigned w[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float4 x = Code::unpack(w[2 * h]), y = Code::unpack(w[2 * h + 1]);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + swizzled(row0 + row, 2 * chunk + h, block)), "r"(Pair<T>::pack(x.x * by, x.y * by)),
+                             "r"(Pair<T>::pack(x.z * by, x.w * by)), "r"(Pair<T>::pack(y.x * by, y.y * by)), "r"(Pair<T>::pack(y.z * by, y.w * by)) : "memory");
+            }
+        }
+    }
+};
+
 template <typename T, int kDims, typename Args>
 __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a, int held_blocks)
 {
@@ -284,8 +335,34 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
             if (page < 0 || page >= (int)a.c.num_pages) { bad |= G10_DEV_BAD_PAGE; return kNone; }
             return cache_row(a.c, Spot{page, at_place}, head);
         };
+        typedef typename CodeOf<Args>::type Code;
         look_up();
-        for (int u = 0; u < n; ++u) {
+        if constexpr (!std::is_void<Code>::value) {
+            CodeRows<T, Code, kDims> k, v;
+            auto ask_scale = [&](unsigned mine) -> float2 { return mine != kNone ? __ldg(&a.scales[cache_cell(a.c, Spot{page, at_place}, head)]) : make_float2(0.0f, 0.0f); };
+            unsigned mine = row_found();
+            float2 scale = ask_scale(mine);
+            k.ask(a.c.k, mine, a.c.head_dim);
+            v.ask(a.c.v, mine, a.c.head_dim);
+            for (int u = 0; u < n; ++u) {
+                if (u + 1 < n) { cursor_next(a, now, per); look_up(); }
+                if (!wait(free_ + 8 * stage, round)) break;
+                const unsigned told = full + 8 * stage, to = smem_of(s_ring) + stage * C::kStageBytes;
+                if (++stage == S) { stage = 0; round ^= 1; }
+                float2 next = make_float2(0.0f, 0.0f);
+                k.put(to, part * 32, kBlock, scale.x);
+                if (u + 1 < n) {
+                    mine = row_found();
+                    next = ask_scale(mine);
+                    k.ask(a.c.k, mine, a.c.head_dim);
+                }
+                v.put(to + kDims * kBlock, part * 32, kBlock, scale.y);
+                if (u + 1 < n) v.ask(a.c.v, mine, a.c.head_dim);
+                scale = next;
+                async_sees();
+                if (!muted(a, 1, u)) bar_arrive(told);
+            }
+        } else for (int u = 0; u < n; ++u) {
             const unsigned mine = row_found();
             if (u + 1 < n) { cursor_next(a, now, per); look_up(); }
             if (!wait(free_ + 8 * stage, round)) break;
@@ -660,8 +737,8 @@ struct Book {
     static constexpr unsigned kColumns = 256;            // of tensor memory: S^T twice
     static_assert(kStages >= 2, "two tiles");
 };
-template <typename T, int kDims>
-__global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendArgs a)
+template <typename T, int kDims, typename Args>
+__global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const Args a)
 {
     typedef Book<kDims> C;
     constexpr int S = C::kStages;
@@ -728,8 +805,29 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const AttendAr
             if (page < 0 || page >= (int)a.c.num_pages) { bad |= G10_DEV_BAD_PAGE; return kNone; }
             return cache_row(a.c, Spot{page, at_place}, head);
         };
+        typedef typename CodeOf<Args>::type Code;
         look_up();
-        for (int u = 0; u < n; ++u) {
+        if constexpr (!std::is_void<Code>::value) {
+            CodeRows<T, Code, kDims> k;
+            auto ask_scale = [&](unsigned mine) -> float { return mine != kNone ? __ldg(&a.scales[cache_cell(a.c, Spot{page, at_place}, head)]).x : 0.0f; };
+            unsigned mine = row_found();
+            float scale = ask_scale(mine);
+            k.ask(a.c.k, mine, a.c.head_dim);
+            for (int u = 0; u < n; ++u) {
+                if (u + 1 < n) { cursor_next<2>(one, now, heads); look_up(); }
+                if (!wait(free_ + 8 * stage, round)) break;
+                const unsigned told = full + 8 * stage, to = smem_of(s_ring) + stage * C::kStageBytes;
+                if (++stage == S) { stage = 0; round ^= 1; }
+                k.put(to, part * 32, 128 * 128, scale);
+                if (u + 1 < n) {
+                    mine = row_found();
+                    scale = ask_scale(mine);
+                    k.ask(a.c.k, mine, a.c.head_dim);
+                }
+                async_sees();
+                if (!muted(a, 4, u)) bar_arrive(told);
+            }
+        } else for (int u = 0; u < n; ++u) {
             const unsigned mine = row_found();
             if (u + 1 < n) { cursor_next<2>(one, now, heads); look_up(); }
             if (!wait(free_ + 8 * stage, round)) break;
@@ -894,8 +992,9 @@ cudaError_t launch_wide(const Args &a, const AttendShape &z, cudaStream_t s)
     const int sms = current_sm_count();
     if (sms < 1) return cudaErrorInvalidDevice;
     if ((e = allow_launch((const void *)kernel, C::kSmem, 1)) != cudaSuccess) return e;
-    if constexpr (std::is_same<Args, AttendArgs>::value)
-        if (a.books && (e = allow_launch((const void *)k_cache_book_wide<T, kDims>, Book<kDims>::kSmem, 1)) != cudaSuccess) return e;
+    constexpr bool kPacked = !std::is_void<typename CodeOf<Args>::type>::value, kBooks = kPacked || std::is_same<Args, AttendArgs>::value;
+    if constexpr (kBooks)
+        if (a.books && (e = allow_launch((const void *)k_cache_book_wide<T, kDims, Args>, Book<kDims>::kSmem, 1)) != cudaSuccess) return e;
     int64_t held = z.tiles < sms ? z.tiles : sms;        // (a block fills an SM)
     held = held < 1 ? 1 : held > kMaxWideBlocks / kCuts ? kMaxWideBlocks / kCuts : held;
     const int64_t grid = z.tiles >= kLong * held ? kCuts * held : held;
@@ -907,12 +1006,14 @@ cudaError_t launch_wide(const Args &a, const AttendShape &z, cudaStream_t s)
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
     cfg.gridDim = dim3((unsigned)grid, 4);               // (of the many elements of a piece each takes a part)
-    if ((e = cudaLaunchKernelEx(&cfg, k_cache_join<T, Args>, a, (int)held, C::kDim, kWideRows)) != cudaSuccess) return e;
-    if constexpr (std::is_same<Args, AttendArgs>::value) {
+    typedef typename std::conditional<kPacked, AttendArgs, Args>::type JoinArgs;
+    const JoinArgs &b = a;
+    if ((e = cudaLaunchKernelEx(&cfg, k_cache_join<T, JoinArgs>, b, (int)held, C::kDim, kWideRows)) != cudaSuccess) return e;
+    if constexpr (kBooks) {
         if (!a.books) return cudaSuccess;
         cfg.blockDim = dim3(kBookThreads); cfg.dynamicSmemBytes = Book<kDims>::kSmem;
         cfg.gridDim = dim3((unsigned)held);
-        return cudaLaunchKernelEx(&cfg, k_cache_book_wide<T, kDims>, a);
+        return cudaLaunchKernelEx(&cfg, k_cache_book_wide<T, kDims, Args>, a);
     }
     return cudaSuccess;
 }

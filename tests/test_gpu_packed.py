@@ -91,9 +91,10 @@ def test_attend_head_dims(g10, dim, kind, code):
     c = P.make_packed([0, 1, 63, 64, 65, 200], 2, dim, 16, O.TYPES[kind], code, dim)
     check_attend(g10, c, queries(c, 1, 4, dim), book=True)
     check_attend(g10, c, queries(c, 3, 4, dim), book=True)
+    check_attend(g10, c, queries(c, 9, 4, dim), book=True)
 
 
-@pytest.mark.parametrize("group", [1, 2, 3, 5, 8, 15, 16])
+@pytest.mark.parametrize("group", [1, 2, 3, 5, 8, 15, 16, 17, 40])
 @pytest.mark.parametrize("book", [False, True])
 @both
 def test_attend_groups(g10, group, book, code):
@@ -109,7 +110,7 @@ def test_attend_pages_and_strides(g10, page, layout, code):
     check_attend(g10, c, queries(c, 1, 4, page), book=True)
 
 
-@pytest.mark.parametrize("new,group", [(2, 1), (3, 4), (5, 3), (16, 1), (2, 8)])
+@pytest.mark.parametrize("new,group", [(2, 1), (3, 4), (5, 3), (16, 1), (2, 8), (16, 4), (33, 2), (16, 16), (130, 3)])
 @pytest.mark.parametrize("kind,dim", [("bf16", 128), ("fp16", 80)])
 @both
 def test_attend_several_tokens(g10, new, group, kind, dim, code):
@@ -121,7 +122,7 @@ def test_attend_several_tokens(g10, new, group, kind, dim, code):
 
 
 @pytest.mark.parametrize("window,sinks", [(1, 0), (1, 1), (2, 5), (64, 64), (65, 1), (100, 70), (5000, 5000), (2 ** 31 - 1, 2 ** 31 - 1)])
-@pytest.mark.parametrize("new,group", [(1, 4), (6, 1)])
+@pytest.mark.parametrize("new,group", [(1, 4), (6, 1), (40, 2)])
 @both
 def test_attend_window_and_sinks(g10, window, sinks, new, group, code):
     c = P.make_packed([1, 64, 130, 400, 777, 0], 2, 64, 24, torch.bfloat16, code, min(window, 99))
@@ -129,7 +130,7 @@ def test_attend_window_and_sinks(g10, window, sinks, new, group, code):
 
 
 @pytest.mark.parametrize("dim", [16, 80, 128, 192, 256])
-@pytest.mark.parametrize("group,new", [(1, 1), (4, 1), (7, 2)])
+@pytest.mark.parametrize("group,new", [(1, 1), (4, 1), (7, 2), (3, 30)])
 @both
 def test_attend_with_room_in_the_table(g10, dim, group, new, code):
     lengths = [new + 1, new + 700, 0, 1, new + 64, 330]
@@ -149,7 +150,8 @@ def test_attend_lengths_about_what_a_cluster_takes(g10, tiles, group, code):
         check_attend(g10, c, queries(c, 1, group, tiles), window=100, sinks=3)
 
 
-@pytest.mark.parametrize("lengths,kv,group,dim", [([9001], 1, 8, 128), ([20000, 3, 4000, 0, 900], 2, 4, 64), ([2500] * 7, 8, 16, 128), ([3000, 1], 1, 1, 256), ([5000] * 40, 4, 1, 64)])
+@pytest.mark.parametrize("lengths,kv,group,dim", [([9001], 1, 8, 128), ([20000, 3, 4000, 0, 900], 2, 4, 64), ([2500] * 7, 8, 16, 128), ([3000, 1], 1, 1, 256), ([5000] * 40, 4, 1, 64),
+                                                  ([9001, 300], 2, 40, 128), ([4000] * 30, 2, 20, 80)])
 @both
 def test_attend_long(g10, lengths, kv, group, dim, code):
     c = P.make_packed(lengths, kv, dim, 64, torch.bfloat16, code, kv)
@@ -178,7 +180,7 @@ def test_attend_scales_far_apart(g10, code):
     check_attend(g10, c, queries(c, 1, 4, 1), scale=-0.3)
 
 
-@pytest.mark.parametrize("new,group", [(1, 8), (3, 5)])
+@pytest.mark.parametrize("new,group", [(1, 8), (3, 5), (30, 4)])
 @both
 def test_attend_where_later_slots_outweigh_all_before(g10, new, group, code):
     c = P.make_packed([1500], 1, 64, 16, torch.float16, code, 2, spread=0.0)
@@ -192,7 +194,7 @@ def test_attend_where_later_slots_outweigh_all_before(g10, new, group, code):
     check_attend(g10, c, q, book=True)
 
 
-@pytest.mark.parametrize("new", [2, 5])
+@pytest.mark.parametrize("new", [2, 5, 20])
 @both
 def test_attend_rows_that_are_no_numbers(g10, new, code):
     """A row of NaN makes what sees it NaN, and nothing else."""
@@ -513,7 +515,7 @@ def test_binding_refusals(g10):
 
 
 # ---- as they are used ------------------------------------------------------------------------------------------------
-@pytest.mark.parametrize("new,group", [(1, 4), (3, 4)])
+@pytest.mark.parametrize("new,group", [(1, 4), (3, 4), (8, 7)])
 @both
 def test_captured_steps(g10, new, group, code):
     """A captured run of append, attend with booking, plan, evict and read, replayed twice beside eager calls on another stream, after the contents have moved on."""
@@ -658,3 +660,69 @@ def test_a_conversation_within_a_budget(g10, code):
         if i % room == room - 1:
             evict()
     assert lengths.tolist() == [budget, 28, budget] and int(cache.status.item()) == 0
+
+
+# ---- edges -----------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("new,group", [(1, 2), (1, 12), (4, 6)])
+@pytest.mark.parametrize("pages", [0, 3])
+@pytest.mark.parametrize("columns", [0, 2])
+def test_nothing_to_look_at(g10, new, group, pages, columns):
+    """Before the first page is given out.  Lengths of zero; or, where there are columns, lengths whose pages are none: read as zeros."""
+    on = dict(device=DEV)
+    k = torch.randint(-127, 128, (pages, 16, 2, 64), dtype=torch.int8, **on)
+    cells = (pages, 2, 16)
+    scores, positions, scales = torch.rand(cells, **on), torch.zeros(cells, dtype=torch.int32, **on), torch.rand(cells + (2,), **on)
+    before = [x.clone() for x in (k, scores, scales)]
+    table = torch.full((3, columns), -1, dtype=torch.int32, **on)
+    for lengths in ([0, 0, 0],) if columns == 0 else ([0, 0, 0], [0, 5, 32]):
+        cache = g10.PackedBuffers(k, k.clone(), scales, table, torch.tensor(lengths, dtype=torch.int32, **on), scores=scores, positions=positions)
+        q = torch.randn(3, new, 2 * group, 64, **on).to(torch.bfloat16)
+        out, lse = torch.full_like(q, 9.0), torch.full(q.shape[:3], 9.0, **on)
+        g10.g10_packed_attend(cache, q, add_scores=True, out=out, lse=lse)
+        rows = torch.randn(3, new, 2, 64, **on).to(torch.bfloat16)
+        g10.g10_packed_append(cache, rows, rows, q)
+        p = g10.g10_cache_plan_evictions(cache, 4, 1, 1)
+        g10.g10_packed_evict(cache, p.moves, p.counts)
+        back = g10.g10_packed_read(cache, 40)
+        torch.cuda.synchronize()
+        assert int(cache.status.item()) == (0x400 if any(lengths) else 0)
+        assert not out.any() and not back[0].any() and not back[1].any()
+        for s, n in enumerate(lengths):                  # (a key of zeros has the logit 0)
+            have = [n - min(new, n) + t + 1 for t in range(min(new, n))] + [0] * (new - min(new, n))
+            want = torch.tensor([math.log(m) if m else -math.inf for m in have])
+            got = lse[s].cpu()
+            assert torch.allclose(got, want[:, None].expand_as(got), rtol=1e-6, atol=1e-6)
+        assert same(k, before[0]) and same(scores, before[1]) and same(scales, before[2])
+
+
+@pytest.mark.parametrize("code,dim,new,group", [("int8", 128, 20, 8), ("e4m3", 64, 1, 20), ("int8", 256, 3, 9)])
+def test_a_wait_that_runs_out(monkeypatch, code, dim, new, group):
+    """The test build, in which the first block of the kernels for many rows keeps one of its arrivals to itself (test_gpu_cache_edges.py): the call returns with the
+    timeout bit, nothing is written out of place, and the next call is right."""
+    import time
+    from paper_2310_09443_b200 import binding, build
+    monkeypatch.setattr(binding, "LIB_PATH", build.build(hooks=True))
+    monkeypatch.setattr(binding, "_lib", None)
+    monkeypatch.delenv("G10_TEST_CACHE_MUTE", raising=False)
+    binding.load_library()
+    c = P.make_packed([9000, 700, 2500 + new], 8, dim, 64, torch.bfloat16, code, dim + group)
+    q = queries(c, new, group, 3)
+    dq = q.to(DEV)
+    r, bound = reference(c, q)[:2]
+    around = torch.full((2 * dq.numel(),), 7.0, dtype=dq.dtype, device=DEV)
+    out = around[dq.numel() // 2:][:dq.numel()].view(dq.shape)
+    size = binding.g10_packed_workspace_bytes(P.upload(binding, c), new, 8 * group, add_scores=True)
+    ws = torch.zeros(size + 1024, dtype=torch.uint8, device=DEV)
+    for mute in (0, 1, 2, 3, 4, 5, 6, 0):
+        monkeypatch.setenv("G10_TEST_CACHE_MUTE", str(mute))
+        cache = P.upload(binding, c)
+        t0 = time.perf_counter()
+        binding.g10_packed_attend(cache, dq, out=out, ws=ws[:size], add_scores=True)
+        torch.cuda.synchronize()
+        took = time.perf_counter() - t0
+        assert int(cache.status.item()) == (0 if mute == 0 else 0x80), mute
+        assert took < 1.0, (mute, took)
+        assert (around[:dq.numel() // 2] == 7).all() and (around[dq.numel() // 2 + dq.numel():] == 7).all() and not ws[size:].any()
+        assert same(cache.k, c.kc) and same(cache.v, c.vc)
+        if mute == 0:
+            assert ((out.cpu().double() - r.out).abs() <= bound).all()
