@@ -14,8 +14,11 @@
 //
 // Warps: 0 - 7 weights and results (a lane per row), 8 issues the products (one thread), 9 and 10 bring the tiles.  Keys and values lie in
 // shared memory as the products want them, 128-byte rows of 64 dimensions with their 16-byte units exchanged by the row's number (the 128-byte swizzle);
-// pages are no whole tiles, so rows are copied one by one, 16 bytes at a time, to their exchanged places.  (Rows of 8-bit codes are loaded, turned into what they
-// stand for, rounded to the products' type, and stored there: the next tile's codes are on their way to registers meanwhile.)  The product of tile u with the queries is
+// pages are no whole tiles, so rows are copied one by one, 16 bytes at a time, to their exchanged places.  (Rows of 8-bit codes are loaded, turned into
+// fp16 and stored there; the next tile's codes are on their way to registers meanwhile.)
+//
+// Codes are multiplied as they are, as in g10_packed_attend.cuh: in fp16, with the queries of bf16 times a power of two for each row; a key's scale goes to its logit, a
+// value's to the weight, taken relative to a power of two that no scale so far is above (the same for all rows, so that one exponential does).  The product of tile u with the queries is
 // issued before those of the one or two tiles before it with the values, so that it runs while the weights are worked out.
 #pragma once
 #include <type_traits>
@@ -233,7 +236,7 @@ __device__ __forceinline__ void bring_queries(const Args &a, const Cursor &u, in
 
 // Rows of codes on their way through a loading warp's registers, 32 of them, 16 codes a lane and step.  `mine`: where the row of this lane's slot begins, in units of 16
 // bytes (all ones: nowhere, zeros).
-template <typename T, typename Code, int kDims>
+template <typename Code, int kDims>
 struct CodeRows {
     static constexpr int kChunks = 4 * kDims;
     uint4 codes[kChunks];
@@ -248,24 +251,77 @@ struct CodeRows {
             if (from != 0xffffffffu && chunk * 16 < head_dim) codes[i] = __ldg((const uint4 *)(base + 16 * ((int64_t)from + chunk)));
         }
     }
-    // to the rows from `row0` on of blocks of 64 dimensions; scale: of this lane's slot
-    __device__ __forceinline__ void put(unsigned to, int row0, int block, float scale)
+    // as fp16 to the rows from `row0` on of blocks of 64 dimensions
+    __device__ __forceinline__ void put(unsigned to, int row0, int block)
     {
         const int lane = threadIdx.x & 31;
 #pragma unroll
         for (int i = 0; i < kChunks; ++i) {
             const int c = i * 32 + lane, row = c / kChunks, chunk = c % kChunks;
-            const float by = __shfl_sync(0xffffffffu, scale, row);
             const unsigned w[4] = {codes[i].x, codes[i].y, codes[i].z, codes[i].w};
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float4 x = Code::unpack(w[2 * h]), y = Code::unpack(w[2 * h + 1]);
-                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + swizzled(row0 + row, 2 * chunk + h, block)), "r"(Pair<T>::pack(x.x * by, x.y * by)),
-                             "r"(Pair<T>::pack(x.z * by, x.w * by)), "r"(Pair<T>::pack(y.x * by, y.y * by)), "r"(Pair<T>::pack(y.z * by, y.w * by)) : "memory");
+                unsigned x[4];
+                Code::halves(w[2 * h], x[0], x[1]);
+                Code::halves(w[2 * h + 1], x[2], x[3]);
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(to + swizzled(row0 + row, 2 * chunk + h, block)), "r"(x[0]), "r"(x[1]), "r"(x[2]), "r"(x[3]) : "memory");
             }
         }
     }
 };
+// The same queries for products with codes: as fp16, bf16 ones times a power of two that brings the row's largest to 2^14 .. 2^15.  The logits' factor, to base 2.
+template <typename T, int kDims>
+__device__ __forceinline__ float bring_scaled_queries(const AttendArgs &a, const Cursor &u, int first_row, int r, int part, char *s_q)
+{
+    constexpr int kUnits = 4 * kDims;
+    const int row = first_row + r, t = row / a.group;
+    const bool real = row < a.rows && t < u.q.count;
+    const char *from = (real ? queries_of(a, u.s, t) : a.q) + 2 * (u.head * a.group + row % a.group) * a.q_head;
+    auto unit = [&](int i) -> uint4 { return real && i * 8 < a.c.head_dim ? __ldg((const uint4 *)(from + 16 * i)) : make_uint4(0, 0, 0, 0); };
+    int e = 0;
+    if (std::is_same<T, __nv_bfloat16>::value) {
+        unsigned most = 0;                               // (magnitudes' bits, infinities and NaN left out)
+#pragma unroll 4
+        for (int i = 0; i < 2 * kUnits; ++i) {
+            const uint4 x = unit(i);
+            const unsigned w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const unsigned y = w[j] & 0x7fffu, z = w[j] >> 16 & 0x7fffu;
+                most = max(most, max(y < 0x7f80u ? y : 0u, z < 0x7f80u ? z : 0u));
+            }
+        }
+        e = min(14 + 127 - (int)(most >> 7), 126);
+    }
+    const float times = a.scale_log2 < 0.0f ? -__int_as_float((e + 127) << 23) : __int_as_float((e + 127) << 23);
+#pragma unroll 4
+    for (int j = 0; j < kUnits; ++j) {
+        const int i = part * kUnits + j;
+        const uint4 x = unit(i);
+        const unsigned w[4] = {x.x, x.y, x.z, x.w};
+        unsigned y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float2 f = Pair<T>::unpack(w[k]);
+            y[k] = Pair<__half>::pack(f.x * times, f.y * times);
+        }
+        *(uint4 *)(s_q + swizzled(r, i, kWideRows * 128)) = make_uint4(y[0], y[1], y[2], y[3]);
+    }
+    return fabsf(a.scale_log2) * __int_as_float((127 - e) << 23);
+}
+__device__ __forceinline__ float2 mul2(float2 a, float2 b)
+{
+    float2 d;
+    asm("{\n\t.reg .b64 x, y;\n\tmov.b64 x, {%2, %3};\n\tmov.b64 y, {%4, %5};\n\tmul.rn.f32x2 x, x, y;\n\tmov.b64 {%0, %1}, x;\n\t}"
+        : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
+    return d;
+}
+// Exponent of a power of two above the scales of all lanes (scales that are no numbers left out), within what 32 bits can undo.
+__device__ __forceinline__ int above(float scale)
+{
+    const unsigned bits = __reduce_max_sync(0xffffffffu, scale >= 0.0f && scale <= 3.4028235e38f ? __float_as_uint(scale) : 0u);
+    return max(-100, min((int)(bits >> 23) - 126, 126));
+}
 
 template <typename T, int kDims, typename Args>
 __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a, int held_blocks)
@@ -273,6 +329,11 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
     typedef Wide<kDims> C;
     constexpr int S = C::kStages;
     constexpr bool kBegin = std::is_same<Args, BeginArgs>::value, kRest = std::is_same<Args, RestArgs>::value;
+    typedef typename CodeOf<Args>::type Code;
+    constexpr bool kPacked = !std::is_void<Code>::value;
+    typedef typename std::conditional<kPacked, __half, T>::type M;       // of the products' operands
+    __shared__ __align__(16) float s_scale[kPacked ? 2 : 1][kPacked ? S : 1][kPacked ? kTile : 4];     // of keys and values of each stage
+    __shared__ int s_above[kPacked ? S : 1][2], s_power[2];
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t s_bar[2 * S + 10];
     __shared__ Place s_place;
@@ -335,10 +396,9 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
             if (page < 0 || page >= (int)a.c.num_pages) { bad |= G10_DEV_BAD_PAGE; return kNone; }
             return cache_row(a.c, Spot{page, at_place}, head);
         };
-        typedef typename CodeOf<Args>::type Code;
         look_up();
-        if constexpr (!std::is_void<Code>::value) {
-            CodeRows<T, Code, kDims> k, v;
+        if constexpr (kPacked) {
+            CodeRows<Code, kDims> k, v;
             auto ask_scale = [&](unsigned mine) -> float2 { return mine != kNone ? __ldg(&a.scales[cache_cell(a.c, Spot{page, at_place}, head)]) : make_float2(0.0f, 0.0f); };
             unsigned mine = row_found();
             float2 scale = ask_scale(mine);
@@ -348,17 +408,19 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                 if (u + 1 < n) { cursor_next(a, now, per); look_up(); }
                 if (!wait(free_ + 8 * stage, round)) break;
                 const unsigned told = full + 8 * stage, to = smem_of(s_ring) + stage * C::kStageBytes;
+                s_scale[0][stage][part * 32 + lane] = scale.x;
+                s_scale[1][stage][part * 32 + lane] = scale.y;
+                const int power = above(scale.y);
+                if (lane == 0) s_above[stage][part] = power;
                 if (++stage == S) { stage = 0; round ^= 1; }
-                float2 next = make_float2(0.0f, 0.0f);
-                k.put(to, part * 32, kBlock, scale.x);
+                k.put(to, part * 32, kBlock);
                 if (u + 1 < n) {
                     mine = row_found();
-                    next = ask_scale(mine);
+                    scale = ask_scale(mine);
                     k.ask(a.c.k, mine, a.c.head_dim);
                 }
-                v.put(to + kDims * kBlock, part * 32, kBlock, scale.y);
+                v.put(to + kDims * kBlock, part * 32, kBlock);
                 if (u + 1 < n) v.ask(a.c.v, mine, a.c.head_dim);
-                scale = next;
                 async_sees();
                 if (!muted(a, 1, u)) bar_arrive(told);
             }
@@ -397,7 +459,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
     } else if (warp == 8) {
         // ---- the issuer: the warp goes through the tiles together, one thread of it issues ----
         const bool leads = elected();
-        const unsigned keys = product_of<T, false>(kWideRows, kTile), values = product_of<T, true>(kWideRows, C::kDim);
+        const unsigned keys = product_of<M, false>(kWideRows, kTile), values = product_of<M, true>(kWideRows, C::kDim);
         const unsigned ring = smem_of(s_ring);
         // (descriptors: an address in units of 16 bytes in the lowest bits, so that the operands of later steps and stages are sums)
         const uint64_t q_operand = operand(smem_of(s_q), 16, 1024), k_operand = operand(ring, 16, 1024), v_operand = operand(ring + kDims * kBlock, kBlock, 1024);
@@ -464,10 +526,14 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
         // ---- rows: a thread of each team each ----
         const int r = tid & (kWideRows - 1), team = tid >> 7;
         const unsigned mine = tmem + ((unsigned)((warp & 3) * 32) << 16), own = mine + (C::kTeams == 2 ? team * C::kDim : 0);
-        const float scale = fabsf(a.scale_log2);
+        float scale = fabsf(a.scale_log2);
+        auto bring = [&]() {                             // (for products with codes each row has a factor of its own)
+            if constexpr (kPacked) scale = bring_scaled_queries<T, kDims>(a, now, now.block * kWideRows, r, team, s_q);
+            else bring_queries<kDims>(a, now, now.block * kWideRows, r, team, s_q);
+        };
         constexpr int kHalf = C::kDim / 2;               // columns that this thread joins
         bool going = true;                               // (the warp alike)
-        bring_queries<kDims>(a, now, now.block * kWideRows, r, team, s_q);
+        bring();
         async_sees();
         if (!(muted(a, 6, 1) && tid == 0)) bar_arrive(q_full);
         for (int u0 = 0; u0 < n;) {
@@ -478,6 +544,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
             const bool busy = now.block * kWideRows + (warp & 3) * 32 < a.rows;    // (this warp has rows)
             const int last_whole = a.window > 0 ? now.q.length - 1 - a.window : -1;
             float m = -INFINITY, l = 0.0f;
+            int power = -100;                            // weights are 2^-power times the values' scales
             bool first = true;
             for (int u = C::kTeams == 2 ? u0 + ((u0 ^ team) & 1) : team == 0 ? u0 : u1; u < u1; u += C::kTeams) {
                 const int slot0 = first_slot(now.q, now.idx + u - u0), b = u & 1;
@@ -499,6 +566,18 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                     };
                     load();
                     if (C::kOwnWeights) { before_sync(); bar_arrive(s_free + 8 * b); }
+                    int now_above = power;
+                    if constexpr (kPacked) {
+                        // (told full long ago: its product is done; for the scales)
+                        going = going && wait(full + 8 * (u % S), (u / S) & 1);
+                        const float4 *const ks = (const float4 *)s_scale[0][u % S];
+#pragma unroll
+                        for (int j = 0; j < kTile / 4; ++j) {
+                            const float4 y = ks[j];
+                            x[2 * j] = mul2(x[2 * j], make_float2(y.x, y.y)); x[2 * j + 1] = mul2(x[2 * j + 1], make_float2(y.z, y.w));
+                        }
+                        now_above = max(power, max(s_above[u % S][0], s_above[u % S][1]));
+                    }
                     float2 best[2] = {make_float2(-INFINITY, -INFINITY), make_float2(-INFINITY, -INFINITY)};
                     if (whole) {
 #pragma unroll
@@ -513,10 +592,11 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                     float top = fmaxf(fmaxf(best[0].x, best[1].x), fmaxf(best[0].y, best[1].y));
                     top = top == -INFINITY ? top : top * scale;
                     // (rescaled only where a logit is far above the reference)
-                    if (__any_sync(0xffffffffu, top > m + Weights<T>::kSlack)) {
+                    if (__any_sync(0xffffffffu, top > m + Weights<M>::kSlack) || (kPacked && now_above > power)) {
                         top = fmaxf(top, m);
-                        const float by = exp2_of(m - (top == -INFINITY ? 0.0f : top));
+                        float by = exp2_of(m - (top == -INFINITY ? 0.0f : top));
                         m = top; l *= by;
+                        if (kPacked) { by *= exp2_of((float)(power - now_above)); power = now_above; }
                         if (!first) {
                             products_so_far();
 #pragma unroll 1
@@ -532,7 +612,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                         }
                     }
                     const float ref = m == -INFINITY ? 0.0f : m;
-                    const float2 by = make_float2(scale, scale), off = make_float2(Weights<T>::kLift - ref, Weights<T>::kLift - ref);
+                    const float2 by = make_float2(scale, scale), off = make_float2(Weights<M>::kLift - ref, Weights<M>::kLift - ref);
                     float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
                     if (whole) {
 #pragma unroll
@@ -551,6 +631,23 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                     }
                     part[0] = add2(part[0], part[1]);
                     l += part[0].x + part[0].y;
+                    if constexpr (kPacked) {
+                        const float4 *const vs = (const float4 *)s_scale[1][u % S];
+                        const float f = __int_as_float((127 - power) << 23);
+#pragma unroll
+                        for (int j = 0; j < kTile / 4; ++j) {
+                            const float4 y = vs[j];
+                            x[2 * j] = mul2(x[2 * j], mul2(make_float2(y.x, y.y), make_float2(f, f)));
+                            x[2 * j + 1] = mul2(x[2 * j + 1], mul2(make_float2(y.z, y.w), make_float2(f, f)));
+                        }
+                        if (!whole) {                    // (the scale of a slot that a row does not see may be anything)
+#pragma unroll
+                            for (int j = 0; j < kTile / 2; ++j) {
+                                if (!sees(a, p, slot0 + 2 * j)) x[j].x = 0.0f;
+                                if (!sees(a, p, slot0 + 2 * j + 1)) x[j].y = 0.0f;
+                            }
+                        }
+                    }
                 } else if (C::kOwnWeights) {
                     bar_arrive(s_free + 8 * b);
                 }
@@ -560,7 +657,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                     going = going && wait(full + 8 * (u % S), (u / S) & 1);
                     const char *const values = s_ring + (u % S) * C::kStageBytes + kDims * kBlock;
                     for (int i = r; i < kDims * kBlock / 4; i += 128) {
-                        const float2 f = Pair<T>::unpack(*(const unsigned *)(values + 4 * i));
+                        const float2 f = Pair<M>::unpack(*(const unsigned *)(values + 4 * i));
                         apart |= !(fabsf(f.x) <= 3.4028235e38f) || !(fabsf(f.y) <= 3.4028235e38f);
                     }
                     apart = any_of_team(team, apart);
@@ -584,7 +681,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                                         const unsigned vw[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
                                         for (int e = 0; e < 4; ++e) {
-                                            const float2 f = Pair<T>::unpack(vw[e]);
+                                            const float2 f = Pair<M>::unpack(vw[e]);
                                             o[8 * i + 2 * e] = __float_as_uint(fmaf(weight[j], f.x, __uint_as_float(o[8 * i + 2 * e])));
                                             o[8 * i + 2 * e + 1] = __float_as_uint(fmaf(weight[j], f.y, __uint_as_float(o[8 * i + 2 * e + 1])));
                                         }
@@ -604,7 +701,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                 if (!apart && busy && going) {
                     unsigned w[kTile / 2];
 #pragma unroll
-                    for (int j = 0; j < kTile / 2; ++j) w[j] = Pair<T>::pack(x[j].x, x[j].y);
+                    for (int j = 0; j < kTile / 2; ++j) w[j] = Pair<M>::pack(x[j].x, x[j].y);
                     tmem_store(w, mine + C::kWeights + b * C::kWeightsApart);
                     tmem_stored();
                 }
@@ -617,13 +714,16 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
             const bool ends = now.idx + (u1 - u0) == now.q.tiles, all = now.idx == 0 && ends, real = row < a.rows;         // (real: busy, too)
             const int64_t item = (int64_t)now.s * per + now.item, piece = item + blockIdx.x;
             const int64_t at = ((int64_t)now.s * a.new_tokens + t) * a.q_heads + now.head * a.group + row % a.group;
-            s_ml[team][r] = make_float2(m, l);
+            // (what is left for the joining kernel is as large as sums of T's weights are)
+            constexpr float kAgain = Weights<M>::kUnlift / Weights<T>::kUnlift;
+            s_ml[team][r] = make_float2(m, l * kAgain);
+            if (kPacked && r == 0) s_power[team] = power;
             rows_meet();                                 // (all logits have been read: the products with the queries are done)
             if (u1 < n) {                                // (a piece that is not the last ends with its item)
                 now.idx = now.q.tiles - 1;
                 cursor_next(a, now, per);
                 if (going) {
-                    bring_queries<kDims>(a, now, now.block * kWideRows, r, team, s_q);
+                    bring();
                     async_sees();
                     bar_arrive(q_full);
                 }
@@ -632,7 +732,12 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
             after_sync();
             const float2 one = s_ml[0][r], two = s_ml[1][r];
             const float top = fmaxf(one.x, two.x), ref = top == -INFINITY ? 0.0f : top;
-            const float f = exp2_of(one.x - ref), g = exp2_of(two.x - ref), sum = p < 0 ? 0.0f : one.y * f + two.y * g;
+            float f = exp2_of(one.x - ref), g = exp2_of(two.x - ref);
+            const float sum = p < 0 ? 0.0f : one.y * f + two.y * g;
+            if constexpr (kPacked) {
+                f *= __int_as_float((127 + s_power[0]) << 23) * kAgain;
+                g *= __int_as_float((127 + s_power[1]) << 23) * kAgain;
+            }
             // (with what the row has of a shared beginning: f_all of this, g_all of that)
             float total_top = top, total = sum, f_all = 1.0f, g_all = 0.0f;
             if constexpr (kRest) {
@@ -742,6 +847,10 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const Args a)
 {
     typedef Book<kDims> C;
     constexpr int S = C::kStages;
+    typedef typename CodeOf<Args>::type Code;
+    constexpr bool kPacked = !std::is_void<Code>::value;
+    typedef typename std::conditional<kPacked, __half, T>::type M;       // of the products' operands
+    __shared__ __align__(16) float s_by[kPacked ? kWideRows : 4];        // each row's factor
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t s_bar[2 * S + 6];
     __shared__ Place s_place;
@@ -805,23 +914,19 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const Args a)
             if (page < 0 || page >= (int)a.c.num_pages) { bad |= G10_DEV_BAD_PAGE; return kNone; }
             return cache_row(a.c, Spot{page, at_place}, head);
         };
-        typedef typename CodeOf<Args>::type Code;
         look_up();
-        if constexpr (!std::is_void<Code>::value) {
-            CodeRows<T, Code, kDims> k;
-            auto ask_scale = [&](unsigned mine) -> float { return mine != kNone ? __ldg(&a.scales[cache_cell(a.c, Spot{page, at_place}, head)]).x : 0.0f; };
+        if constexpr (kPacked) {
+            CodeRows<Code, kDims> k;
             unsigned mine = row_found();
-            float scale = ask_scale(mine);
             k.ask(a.c.k, mine, a.c.head_dim);
             for (int u = 0; u < n; ++u) {
                 if (u + 1 < n) { cursor_next<2>(one, now, heads); look_up(); }
                 if (!wait(free_ + 8 * stage, round)) break;
                 const unsigned told = full + 8 * stage, to = smem_of(s_ring) + stage * C::kStageBytes;
                 if (++stage == S) { stage = 0; round ^= 1; }
-                k.put(to, part * 32, 128 * 128, scale);
+                k.put(to, part * 32, 128 * 128);
                 if (u + 1 < n) {
                     mine = row_found();
-                    scale = ask_scale(mine);
                     k.ask(a.c.k, mine, a.c.head_dim);
                 }
                 async_sees();
@@ -874,7 +979,7 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const Args a)
                 after_sync();
                 if (leads) {
                     const int rows = min(kWideRows, a.rows - b * kWideRows);
-                    const unsigned what = product_of<T, false>(128, (rows + 15) & ~15), to = tmem + (d & 1) * 128;
+                    const unsigned what = product_of<M, false>(128, (rows + 15) & ~15), to = tmem + (d & 1) * 128;
                     const uint64_t at = k_operand + (unsigned)(stage * (C::kStageBytes >> 4));
 #pragma unroll
                     for (int k = 0; k < 4 * kDims; ++k)
@@ -902,7 +1007,12 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const Args a)
         auto bring = [&](int b) {                        // queries, lse and places of block b's rows
             const int row = b * kWideRows + r, t = row / a.group;
             if (going) {
-                bring_queries<kDims>(a, now, b * kWideRows, r, team, s_q);
+                if constexpr (kPacked) {
+                    const float by = bring_scaled_queries<T, kDims>(a, now, b * kWideRows, r, team, s_q);
+                    if (team == 0) s_by[r] = by;
+                } else {
+                    bring_queries<kDims>(a, now, b * kWideRows, r, team, s_q);
+                }
                 const bool real = row < a.rows && t < now.q.count;
                 if (team == 0) s_p[r] = real ? now.q.length - now.q.count + t : -1;
                 else s_off[r] = real ? -__ldcg(&a.sums[((int64_t)now.s * heads * blocks + now.head * blocks + b) * kWideRows + r]) : -INFINITY;
@@ -915,7 +1025,7 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const Args a)
             // a run of pairs of one head; for several blocks of rows, whose queries come and go with each, a run is one pair
             const int run = blocks > 1 ? 1 : min(now.q.tiles - now.idx, n - u);
             const int seen0 = now.q.length - now.q.count;
-            float sum = 0.0f;
+            float sum = 0.0f, key_scale = 0.0f;
             Spot spot{-1, 0};
             for (int b = 0; b < blocks; ++b) {
                 bring(b);
@@ -928,16 +1038,24 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const Args a)
                     if (b == 0) {
                         spot = slot < now.q.length ? cache_spot(a.c, now.s, slot, bad) : Spot{-1, 0};
                         sum = 0.0f;
+                        if constexpr (kPacked) key_scale = spot.page >= 0 ? __ldg(&a.scales[cache_cell(a.c, spot, now.head)]).x : 0.0f;
                     }
                     going = going && wait(d_full + 8 * (d & 1), (d >> 1) & 1);
                     if (!going) continue;
                     after_sync();
                     float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-                    const float2 by = make_float2(scale, scale);
+                    const float2 by = kPacked ? make_float2(key_scale, key_scale) : make_float2(scale, scale);
 #pragma unroll 1
                     for (int c = 0; c < rows; c += 32) {
                         float2 x[16];
                         logits_load(x, mine + (d & 1) * 128 + c);
+                        if constexpr (kPacked) {
+#pragma unroll
+                            for (int i = 0; i < 16; i += 2) {
+                                const float4 f = *(const float4 *)&s_by[c + 2 * i];
+                                x[i] = mul2(x[i], make_float2(f.x, f.y)); x[i + 1] = mul2(x[i + 1], make_float2(f.z, f.w));
+                            }
+                        }
                         if (whole && c + 32 <= rows) {
 #pragma unroll
                             for (int i = 0; i < 16; i += 2) {

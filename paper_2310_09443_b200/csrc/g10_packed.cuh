@@ -10,6 +10,13 @@ namespace g10 {
 // left to the logits and the weights.
 struct Int8 {
     static constexpr float kLargest = 127.0f;
+    // four codes to two pairs of fp16 (below 0x64 a byte, its top bit flipped, is 1024 + 128 + code)
+    static __device__ __forceinline__ void halves(unsigned u, unsigned &a, unsigned &b)
+    {
+        const unsigned x = u ^ 0x80808080u, kMore = 0x64806480u, y = __byte_perm(x, kMore, 0x5150), z = __byte_perm(x, kMore, 0x5352);
+        const __half2 p = __hsub2(*(const __half2 *)&y, *(const __half2 *)&kMore), q = __hsub2(*(const __half2 *)&z, *(const __half2 *)&kMore);
+        a = *(const unsigned *)&p; b = *(const unsigned *)&q;
+    }
     // four numbers up to kLargest to four codes
     static __device__ __forceinline__ unsigned pack(float a, float b, float c, float d, float by)
     {
@@ -30,6 +37,12 @@ struct Int8 {
 };
 struct E4m3 {
     static constexpr float kLargest = 448.0f;
+    // four codes to two pairs of fp16
+    static __device__ __forceinline__ void halves(unsigned u, unsigned &a, unsigned &b)
+    {
+        const __half2 x = halves(u & 0xffffu), y = halves(u >> 16);
+        a = *(const unsigned *)&x; b = *(const unsigned *)&y;
+    }
     static __device__ __forceinline__ unsigned pack(float a, float b, float c, float d, float by)
     {
         const unsigned x = __nv_cvt_float2_to_fp8x2(make_float2(a * by, b * by), __NV_SATFINITE, __NV_E4M3);

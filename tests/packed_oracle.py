@@ -82,11 +82,12 @@ def upload(g10, c, device="cuda:0", **more):
 
 
 def attend_bounds(c, r, q, scale):
-    """How far out, lse and a weight (relatively) may be off, for up to 16 rows a key-value head: attend_bounds of cache_oracle.py, with these differences.
+    """How far out, lse and a weight (relatively) may be off: attend_bounds of cache_oracle.py, with these differences.
 
     int8 keys are multiplied 128 too large, and 128 times the sum of the queries is taken off: D more additions, and terms of size (|code| + 128) ks |q|.  bf16 queries lose
     what is below 2^-39 of the row's largest element: far less than one of the units counted.  Weights times the value's scale are rounded to fp16: half a step relative, or 2^-25
-    where the largest of the row is at least 2^10.  They come from a logarithm of the scale off by 2^-22 relatively or absolutely, and an addition."""
+    where the largest of the row (for more than 16 rows its largest weight times the largest scale, or half of that) is at least 2^10.  They come from a logarithm of the scale
+    off by 2^-22 relatively or absolutely, and an addition; or from two products more."""
     seqs, new, heads, dim = q.shape
     group = heads // c.kv_heads
     step = O.half_step(c.dtype)
@@ -102,7 +103,7 @@ def attend_bounds(c, r, q, scale):
             if c.code == "int8":
                 slip[s, :, mine] += 128 * ks.max() * q[s, :, mine].double().abs().sum(-1) * abs(scale)
             logs[s, :, mine] = (torch.log2(vs.clamp(min=2.0 ** -126)).abs()).max()
-            tiny[s, :, mine] = 2.0 ** -35 * vs.max() * c.vc[pg, pl, h].double().abs().sum(0)
+            tiny[s, :, mine] = 2.0 ** -34 * vs.max() * c.vc[pg, pl, h].double().abs().sum(0)
     d = (2 * dim + 8) * 2.0 ** -23 * slip
     rel = 2 * d + 2.0 ** -21 + (r.n_seen + 8) * 2.0 ** -23 + 2.0 ** -22 * (logs + 1)
     out = (2.0 ** -11 + rel[..., None] + (r.n_seen[..., None] + 8) * 2.0 ** -23) * r.weighed * 1.01 + tiny
