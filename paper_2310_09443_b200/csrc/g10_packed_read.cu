@@ -6,49 +6,62 @@ namespace {
 
 constexpr int kReadThreads = 256, kEach = 4;
 
-// Pure traffic: head_dim codes and a scale in, 2 * head_dim bytes out for each row.  A thread takes 8 codes (8 bytes in, 16 out: a warp's accesses lie side by side
-// in both directions) of key and value of a (token, head), kEach of those at a time.  A block takes `run` tokens of a sequence.
-template <typename T, typename Code>
-__global__ void __launch_bounds__(kReadThreads) k_packed_read(const ReadArgs a, int runs, int run, unsigned unit_mul)
+__device__ __forceinline__ void store32(void *to, const uint4 &x, const uint4 &y)
+{
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(to), "r"(x.x), "r"(x.y), "r"(x.z), "r"(x.w), "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w) : "memory");
+}
+
+// Pure traffic: head_dim codes and a scale in, 2 * head_dim bytes out for each row.  A thread takes 16 codes of key and value of a (token, head), always the same place of
+// the same head, and goes through the block's tokens, kEach of them at a time: what it works out for a token is the slot's page.  A token's units (16 codes each) are `per`
+// threads' or, where they are more than a block has, blockIdx.y's part of them; a block takes `run` tokens of a sequence, kReadThreads / per at a time.
+template <typename T, typename Code, bool kWhole>        // kWhole: outputs may be written 32 bytes at a time
+__global__ void __launch_bounds__(kReadThreads) k_packed_read(const ReadArgs a, int runs, int run, int per)
 {
     const CacheView &c = a.c;
-    const int s = (int)(blockIdx.x / (unsigned)runs), t0 = (int)(blockIdx.x - (unsigned)s * (unsigned)runs) * run;
+    const int s = (int)(blockIdx.x / (unsigned)runs), t0 = (int)(blockIdx.x - (unsigned)s * (unsigned)runs) * run, t1 = min(a.tokens, t0 + run);
+    const int chunks = c.head_dim / 16, team = (int)threadIdx.x / per, teams = kReadThreads / per, unit = (int)blockIdx.y * per + (int)threadIdx.x - team * per;
+    const int head = unit / chunks, chunk = unit - head * chunks;
+    if (team >= teams || head >= c.kv_heads) return;
     ull bad = 0;
     const int length = cache_length(c, s, bad);
     const int64_t start = a.starts != nullptr ? __ldg(&a.starts[s]) : 0;
-    const unsigned units = (unsigned)c.head_dim / 8, all = units * (unsigned)c.kv_heads;         // of a row, of a token: 8 codes each
-    const unsigned n = (unsigned)min(run, a.tokens - t0) * all;
+    char *const k_to = a.k + 2 * (s * a.k_seq + head * a.k_head + 16 * chunk), *const v_to = a.v + 2 * (s * a.v_seq + head * a.v_head + 16 * chunk);
 #pragma unroll 1
-    for (unsigned i0 = threadIdx.x; i0 < n; i0 += kReadThreads * kEach) {
-        uint2 x[kEach], y[kEach];
+    for (int t = t0 + team; t < t1; t += kEach * teams) {
+        uint4 x[kEach], y[kEach];
         float2 scale[kEach];
-        int64_t k_at[kEach], v_at[kEach];
+        Spot spot[kEach];
 #pragma unroll
         for (int j = 0; j < kEach; ++j) {
-            const unsigned i = i0 + j * kReadThreads;
-            x[j] = y[j] = make_uint2(0, 0); scale[j] = make_float2(0.0f, 0.0f); k_at[j] = v_at[j] = 0;
-            if (i >= n) continue;
-            const unsigned row = (unsigned)(((ull)i * unit_mul) >> 32), t = row / (unsigned)c.kv_heads, head = row - t * (unsigned)c.kv_heads, unit = i - row * units;
-            k_at[j] = 2 * (s * a.k_seq + (int64_t)(t0 + (int)t) * a.k_token + head * a.k_head + 8 * unit);
-            v_at[j] = 2 * (s * a.v_seq + (int64_t)(t0 + (int)t) * a.v_token + head * a.v_head + 8 * unit);
-            const int64_t slot = start + t0 + (int)t;
-            if (slot < 0 || slot >= length) continue;
-            const Spot spot = cache_spot(c, s, (int)slot, bad);
-            if (spot.page < 0) continue;
-            const int64_t at = 16 * (int64_t)cache_row(c, spot, (int)head) + 8 * unit;
-            if (a.k != nullptr) x[j] = __ldg((const uint2 *)(c.k + at));
-            if (a.v != nullptr) y[j] = __ldg((const uint2 *)(c.v + at));
-            scale[j] = __ldg(&a.scales[cache_cell(c, spot, (int)head)]);
+            const int64_t slot = start + t + j * teams;
+            spot[j] = Spot{-1, 0};
+            if (t + j * teams < t1 && slot >= 0 && slot < length) spot[j] = cache_spot(c, s, (int)slot, bad);
         }
-        auto values = [](uint2 u, float by) -> uint4 {
-            const float4 p = Code::unpack(u.x), q = Code::unpack(u.y);
-            return make_uint4(Pair<T>::pack(p.x * by, p.y * by), Pair<T>::pack(p.z * by, p.w * by), Pair<T>::pack(q.x * by, q.y * by), Pair<T>::pack(q.z * by, q.w * by));
+#pragma unroll
+        for (int j = 0; j < kEach; ++j) {
+            x[j] = y[j] = make_uint4(0, 0, 0, 0); scale[j] = make_float2(0.0f, 0.0f);
+            if (spot[j].page < 0) continue;
+            const int64_t at = 16 * ((int64_t)cache_row(c, spot[j], head) + chunk);
+            if (a.k != nullptr) x[j] = __ldg((const uint4 *)(c.k + at));
+            if (a.v != nullptr) y[j] = __ldg((const uint4 *)(c.v + at));
+            scale[j] = __ldg(&a.scales[cache_cell(c, spot[j], head)]);
+        }
+        auto put = [](char *to, const uint4 &u, float by) {
+            const unsigned w[4] = {u.x, u.y, u.z, u.w};
+            uint4 o[2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float4 p = Code::unpack(w[2 * h]), q = Code::unpack(w[2 * h + 1]);
+                o[h] = make_uint4(Pair<T>::pack(p.x * by, p.y * by), Pair<T>::pack(p.z * by, p.w * by), Pair<T>::pack(q.x * by, q.y * by), Pair<T>::pack(q.z * by, q.w * by));
+            }
+            if (kWhole) store32(to, o[0], o[1]);
+            else { *(uint4 *)to = o[0]; *(uint4 *)(to + 16) = o[1]; }
         };
 #pragma unroll
         for (int j = 0; j < kEach; ++j)
-            if (i0 + j * kReadThreads < n) {
-                if (a.k != nullptr) *(uint4 *)(a.k + k_at[j]) = values(x[j], scale[j].x);
-                if (a.v != nullptr) *(uint4 *)(a.v + v_at[j]) = values(y[j], scale[j].y);
+            if (t + j * teams < t1) {
+                if (a.k != nullptr) put(k_to + 2 * (int64_t)(t + j * teams) * a.k_token, x[j], scale[j].x);
+                if (a.v != nullptr) put(v_to + 2 * (int64_t)(t + j * teams) * a.v_token, y[j], scale[j].y);
             }
     }
     if (bad != 0) raise_status(c.status, bad);
@@ -57,15 +70,16 @@ __global__ void __launch_bounds__(kReadThreads) k_packed_read(const ReadArgs a, 
 template <typename T, typename Code>
 cudaError_t launch(const ReadArgs &a, cudaStream_t s)
 {
-    // (a block does not look beyond 2^32 / units units, for which the product below finds the row exactly; runs are as long as leave 8 blocks for every SM)
-    const unsigned units = (unsigned)a.c.head_dim / 8, all = units * (unsigned)a.c.kv_heads;
-    int run = (int)((kReadThreads * kEach + all - 1) / all);
-    while (run < 64 && 2 * run <= a.tokens && (int64_t)a.c.num_seqs * ((a.tokens + 2 * run - 1) / (2 * run)) >= 148 * 8 && (int64_t)2 * run * all <= 65536) run *= 2;
-    const int runs = (int)(((int64_t)a.tokens + run - 1) / run);
-    const int64_t blocks = (int64_t)a.c.num_seqs * runs;
+    const int units = a.c.kv_heads * (a.c.head_dim / 16), per = units < kReadThreads ? units : kReadThreads, teams = kReadThreads / per;
+    const unsigned parts = (unsigned)((units + per - 1) / per);
+    // (runs of kEach tokens a thread, or as many more as leave 16 blocks for every SM)
+    int64_t run = (int64_t)kEach * teams;
+    while (run < 64 * teams && run < a.tokens && (int64_t)a.c.num_seqs * ((a.tokens + 2 * run - 1) / (2 * run)) * parts >= 148 * 16) run *= 2;
+    const int64_t runs = (a.tokens + run - 1) / run, blocks = a.c.num_seqs * runs;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    const unsigned unit_mul = (unsigned)((((uint64_t)1 << 32) + units - 1) / units);
-    k_packed_read<T, Code><<<(unsigned)blocks, kReadThreads, 0, s>>>(a, runs, run, unit_mul); count_launch();
+    const bool whole = (((uintptr_t)a.k | (uintptr_t)a.v) & 31u) == 0 && ((a.k_seq | a.k_token | a.k_head | a.v_seq | a.v_token | a.v_head) & 15) == 0;
+    const auto kernel = whole ? k_packed_read<T, Code, true> : k_packed_read<T, Code, false>;
+    kernel<<<dim3((unsigned)blocks, parts), kReadThreads, 0, s>>>(a, (int)runs, (int)run, per); count_launch();
     return cudaGetLastError();
 }
 
