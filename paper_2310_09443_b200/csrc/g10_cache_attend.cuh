@@ -159,11 +159,13 @@ struct Share {
 // blocks that wait for a place even it out (424 -> 412 us there, with two blocks an SM; with three it no longer tells).  Shorter ones are not: 320
 // blocks of 24 tiles, where 296 run at a time, take two rounds (49 -> 71 us).
 constexpr int kLong = 128, kCuts = 4;    // tiles
+// (kUnit: as many tiles count as one)
+template <int kUnit = 1>
 __device__ __forceinline__ Share share_of(int64_t tiles, int per, int grid, int held)
 {
     Share r;
     r.total = tiles * per;
-    r.blocks = r.total >= (int64_t)kLong * held ? grid : (int)max((int64_t)1, min((int64_t)held, r.total));
+    r.blocks = r.total >= (int64_t)(kLong / kUnit) * held ? grid : (int)max((int64_t)1, min((int64_t)held, r.total));
     return r;
 }
 // (a division of 32-bit numbers where they are: a third of the instructions)
@@ -792,7 +794,7 @@ __device__ __forceinline__ Pieces pieces_of(int64_t item, int64_t first, int til
 // The second kernel.  (1) An item that was cut into pieces is joined by the blocks whose turn its pieces' shares are, each taking a part of its rows
 // and dimensions; (2) rows of sequences without tiles are written.  What follows from the lengths alone is worked out while the first
 // kernel still runs.
-template <typename T, typename Args>
+template <typename T, int kUnit, typename Args>
 __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const Args a, int held_blocks, int padded_dim, int block_rows)
 {
     __shared__ Place s_place[2];
@@ -800,16 +802,16 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_join(const Args a, int h
     __shared__ Pieces s_pieces[2];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, per = a.c.kv_heads * a.row_blocks;
     ull ignored = 0;
-    const Tally tally = tally_of<kJoinThreads>(a, ignored);
-    const Share share = share_of(tally.total, per, gridDim.x, held_blocks);        // the first kernel's
+    const Tally tally = tally_of<kJoinThreads, kUnit>(a, ignored);
+    const Share share = share_of<kUnit>(tally.total, per, gridDim.x, held_blocks);        // the first kernel's
     const int b = blockIdx.x;
     const int64_t begin = begin_of(share, b), end = begin_of(share, b + 1);
-    if (begin < end) { place_of(a, tally, begin, per, &s_place[0]); place_of(a, tally, end - 1, per, &s_place[1]); }
+    if (begin < end) { place_of<kUnit>(a, tally, begin, per, &s_place[0]); place_of<kUnit>(a, tally, end - 1, per, &s_place[1]); }
     __syncthreads();
     if (warp < 2 && begin < end) {
         const int64_t tile = warp == 0 ? begin : end - 1;
         Cursor u;
-        cursor_at(a, u, s_place[warp], tile);
+        cursor_at<kUnit>(a, u, s_place[warp], tile);
         const Pieces p = pieces_of((int64_t)u.s * per + u.item, tile - u.idx, u.q.tiles, share);
         if (lane == 0) { s_cut[warp] = u; s_pieces[warp] = p; }
     }
@@ -932,7 +934,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_book(const AttendArgs a,
 
 // ---- host ----
 // The three kernels for up to 16 rows.  `kernel`: the first, kRows rows of kDim dims, `smem` bytes of shared memory; known, most_known: what the device holds of it.
-template <typename T, int kRows, int kDim, typename JoinArgs, typename Args>
+template <typename T, int kRows, int kDim, int kUnit, typename JoinArgs, typename Args>
 cudaError_t launch_few(void (*kernel)(const Args, int, int, int), size_t smem, int *known, int *most_known, const Args &a, const AttendShape &z, cudaStream_t s)
 {
     int dev = 0, room = 0;
@@ -947,13 +949,14 @@ cudaError_t launch_few(void (*kernel)(const Args, int, int, int), size_t smem, i
         if (room < 1) return cudaErrorInvalidDevice;
         if (dev < kMaxDevices) __atomic_store_n(&known[dev], room, __ATOMIC_RELEASE);
     }
-    int64_t held = z.tiles < room ? z.tiles : room;
+    const int64_t units = z.tiles / kUnit;
+    int64_t held = units < room ? units : room;
     held = held < 1 ? 1 : held > kMaxBlocks ? kMaxBlocks : held;
     const int64_t grid = z.tiles >= kLong * held && kCuts * held <= kMaxBlocks ? kCuts * held : held;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(kThreads); cfg.dynamicSmemBytes = smem; cfg.stream = s;
-    // Clusters: where every item has at most four tiles a block and all blocks run at a time.
-    const int64_t cap = z.items > 0 ? z.tiles / z.items : 0;
+    // Clusters: where every item has at most four tiles a block (or as many units of them) and all blocks run at a time.
+    const int64_t cap = z.items > 0 ? units / z.items : 0;
     int cluster = 0;
     if (z.items <= room && cap >= 1) {
         const void *const kernels[] = {(const void *)kernel};
@@ -975,7 +978,7 @@ cudaError_t launch_few(void (*kernel)(const Args, int, int, int), size_t smem, i
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
     const JoinArgs &b = a;
-    if (cluster == 0 && (e = cudaLaunchKernelEx(&cfg, k_cache_join<T, JoinArgs>, b, (int)held, kDim, kRows)) != cudaSuccess) return e;
+    if (cluster == 0 && (e = cudaLaunchKernelEx(&cfg, k_cache_join<T, kUnit, JoinArgs>, b, (int)held, kDim, kRows)) != cudaSuccess) return e;
     if (a.logits == nullptr) return cudaSuccess;
     const int64_t warps = kJoinThreads / 32, blocks = (z.tiles + warps - 1) / warps, most = 148 * 6;
     cfg.gridDim = dim3((unsigned)(blocks < 1 ? 1 : blocks < most ? blocks : most));      // (a table without columns: no tile)
@@ -987,7 +990,7 @@ cudaError_t launch(const Args &a, const AttendShape &z, cudaStream_t s)
 {
     typedef Config<T, kSteps, kCols> C;
     static int known[kMaxDevices], most_known[kMaxDevices];
-    return launch_few<T, C::kRows, C::kDim, Args>(k_cache_attend<T, kSteps, kCols, Args>, C::kSmem, known, most_known, a, z, s);
+    return launch_few<T, C::kRows, C::kDim, 1, Args>(k_cache_attend<T, kSteps, kCols, Args>, C::kSmem, known, most_known, a, z, s);
 }
 template <typename T, int kSteps, typename Args>
 cudaError_t launch_steps(const Args &a, const AttendShape &z, cudaStream_t s)

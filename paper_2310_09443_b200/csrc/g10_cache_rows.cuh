@@ -1126,7 +1126,7 @@ cudaError_t launch_wide(const Args &a, const AttendShape &z, cudaStream_t s)
     cfg.gridDim = dim3((unsigned)grid, 4);               // (of the many elements of a piece each takes a part)
     typedef typename std::conditional<kPacked, AttendArgs, Args>::type JoinArgs;
     const JoinArgs &b = a;
-    if ((e = cudaLaunchKernelEx(&cfg, k_cache_join<T, JoinArgs>, b, (int)held, C::kDim, kWideRows)) != cudaSuccess) return e;
+    if ((e = cudaLaunchKernelEx(&cfg, k_cache_join<T, 1, JoinArgs>, b, (int)held, C::kDim, kWideRows)) != cudaSuccess) return e;
     if constexpr (kBooks) {
         if (!a.books) return cudaSuccess;
         cfg.blockDim = dim3(kBookThreads); cfg.dynamicSmemBytes = Book<kDims>::kSmem;

@@ -96,9 +96,14 @@ __device__ __forceinline__ void load_words(unsigned *w, unsigned at)
 template <int kGroups, int kCols>
 struct PackedConfig {
     static constexpr int kDim = 32 * kGroups, kSteps = 2 * kGroups, kRows = 8 * kCols;
-    // bytes of a row in shared memory: an odd number of 16-byte units (the 8 rows of a matrix of keys lie in different banks, and so do four pairs of slots' values)
-    static constexpr int kPitch = kDim + 16;
-    static constexpr int kScalesAt = 2 * 16 * kPitch, kPartBytes = kScalesAt + 16 * 8;     // a warp's part of a tile: 16 keys, 16 values, their scales
+    // Blocks of 16 slots that a warp takes at a time, and with them tiles that the block of four warps takes at a time (a unit).
+    static constexpr int kSub = kGroups <= 4 ? 2 : 1, kSlots = 16 * kSub;
+    // A row in shared memory: 128 bytes with their 16-byte units exchanged by the row's number, or an odd number of those units.  The 8 rows of a matrix of keys lie in
+    // different banks either way, and so do the values that a quarter of a warp loads.
+    static constexpr bool kSwizzled = kDim == 128;
+    static constexpr int kPitch = kSwizzled ? kDim : kDim + 16;
+    static __device__ __forceinline__ unsigned unit_at(int row, int unit) { return row * kPitch + ((kSwizzled ? unit ^ (row & 7) : unit) << 4); }
+    static constexpr int kScalesAt = 2 * kSlots * kPitch, kPartBytes = kScalesAt + kSlots * 8;     // a warp's part of a unit: keys, values, their scales
     static constexpr bool kHeld = kCols * kSteps <= 16;  // the queries stay in registers
     static constexpr int kShared = kRows * kDim * 4 + kRows * 8;
     static constexpr int kQBytes = kHeld ? 0 : kRows * kDim * 2;
@@ -106,14 +111,14 @@ struct PackedConfig {
     static constexpr int kMergePitch = kDim + 4;         // floats
     static_assert(8 * kMergePitch * 4 <= kPartBytes, "a warp's sums of 8 rows fit the part of the ring that it has just left");
     static constexpr int fits(int blocks) { return (226 * 1024 / blocks - kOther - 1024) / (kParts * kPartBytes); }
-    // Blocks that share an SM, and tiles in a block's ring.
-    static constexpr int kBlocks = kGroups > 4 ? (fits(2) >= 2 && kCols == 1 ? 2 : 1) : kCols == 1 && fits(4) >= 2 ? 4 : fits(3) >= 2 && kGroups == 2 ? 3 : 2;
+    // Blocks that share an SM, and units in a block's ring.
+    static constexpr int kBlocks = kGroups > 4 ? (fits(2) >= 2 && kCols == 1 ? 2 : 1) : kCols == 1 && fits(3) >= 2 ? 3 : 2;
     static constexpr int kStages = fits(kBlocks) > 6 ? 6 : fits(kBlocks);
-    static_assert(kStages >= 2, "a tile in use, and one on its way");
+    static_assert(kStages >= 2, "a unit in use, and one on its way");
     static constexpr int kSmem = kParts * kStages * kPartBytes + kOther;
 };
 
-// The structure is k_cache_attend's: four warps side by side, warp p at the 16 slots p of each tile, with a ring of its own.
+// The structure is k_cache_attend's: four warps side by side, each at a quarter of the tile, or of the two, with a ring of its own.
 //   S^T [16 slots x rows] = K Q^T: a lane's words of the keys, as ldmatrix hands them out, are four dimensions of a slot, two pairs of the matrix instruction's; the
 //   queries are brought in the same order, and a sum does not mind it.
 //   O^T [dims x rows] += V^T W^T: a lane reads the words of its four slots where they lie and picks the two slots of a pair out of two words; which dimension of the
@@ -123,7 +128,7 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
 {
     typedef PackedConfig<kGroups, kCols> C;
     typedef Operand<Code> O;
-    constexpr int kStages = C::kStages;
+    constexpr int kStages = C::kStages, kSub = C::kSub;
     constexpr float kLift = Weights<__half>::kLift, kSlack = Weights<__half>::kSlack;
     extern __shared__ __align__(128) char smem[];
     float *const s_join = (float *)(smem + kParts * kStages * C::kPartBytes);          // [kRows][kDim], then [kRows] maximum and sum
@@ -141,15 +146,15 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
     if (cluster > 0) {
         my_item = (int)blockIdx.x / cluster; rank = (int)blockIdx.x % cluster;
         now.s = my_item / per; now.item = now.head = my_item % per; now.block = 0;
-        now.q = seq_of(a, now.s, bad);
+        now.q = units_of<kSub>(a, now.s, bad);
         if (bad != 0) raise_status(a.c.status, bad);
         const int tiles = now.q.tiles;
         now.idx = tiles * rank / cluster;
         n = tiles * (rank + 1) / cluster - now.idx;
         begin = (int64_t)my_item * cap + now.idx;
         if (a.logits != nullptr && rank == 0) {          // (the numbers that the item does not use)
-            for (int i = tiles + tid; i < cap; i += kThreads) a.notes[(int64_t)my_item * cap + i].length = 0;
-            if (my_item == 0 && tid == 0) *a.total = (int64_t)a.c.num_seqs * per * cap;
+            for (int i = kSub * tiles + tid; i < kSub * cap; i += kThreads) a.notes[(int64_t)my_item * kSub * cap + i].length = 0;
+            if (my_item == 0 && tid == 0) *a.total = (int64_t)a.c.num_seqs * per * kSub * cap;
         }
         if (tiles == 0) {                                // (the whole cluster alike)
             const int chunks = a.c.head_dim / 8;
@@ -163,56 +168,61 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
             return;
         }
     } else {
-        const Tally tally = tally_of<kThreads>(a, bad);
-        const Share share = share_of(tally.total, per, gridDim.x, held_blocks);
+        const Tally tally = tally_of<kThreads, kSub>(a, bad);
+        const Share share = share_of<kSub>(tally.total, per, gridDim.x, held_blocks);
         begin = begin_of(share, blockIdx.x);
         n = (int)(begin_of(share, blockIdx.x + 1) - begin);
         if (bad != 0) raise_status(a.c.status, bad);
-        if (a.logits != nullptr && blockIdx.x == 0 && tid == 0) *a.total = share.total;
+        if (a.logits != nullptr && blockIdx.x == 0 && tid == 0) *a.total = kSub * share.total;
         if (n == 0) return;
-        place_of(a, tally, begin, per, &s_place);
+        place_of<kSub>(a, tally, begin, per, &s_place);
         __syncthreads();
-        cursor_at(a, now, s_place, begin);
+        cursor_at<kSub>(a, now, s_place, begin);
     }
     bad = 0;
     const int my_s = now.s, my_head = now.head, my_count = now.q.count;
     ahead = now;
     const unsigned ring = smem_of(smem) + part * kStages * C::kPartBytes;
-    // where the row of this lane's slot begins (lanes 16 .. 31: as lanes 0 .. 15), in the tile that `ahead` stands at, and its scales
+    // the warp's first slot of a unit: which of its tiles, which part of that
+    auto slot_of = [&](const Cursor &u) -> int { return kSub == 2 ? first_slot(u.q, 2 * u.idx + part / 2) + (part & 1) * 32 : first_slot(u.q, u.idx) + part * 16; };
+    // where the row of this lane's slot begins (16 slots: lanes 16 .. 31 as lanes 0 .. 15), in the unit that `ahead` stands at, and its scales
     constexpr unsigned kNone = 0xffffffffu;              // (nothing to read: zeros)
     struct Found {
         unsigned row;
         int64_t cell;
     };
     auto look_up = [&]() -> Found {
-        const int slot = first_slot(ahead.q, ahead.idx) + part * 16 + (lane & 15);
+        const int slot = slot_of(ahead) + (lane & (C::kSlots - 1));
         if (slot >= ahead.q.length || !(a.window == 0 || slot < a.sinks || slot > ahead.q.length - ahead.q.count - a.window)) return Found{kNone, 0};
         const Spot o = cache_spot(a.c, ahead.s, slot, bad);
-        return o.page < 0 ? Found{kNone, 0} : Found{cache_row(a.c, o, ahead.head), cache_cell(a.c, o, ahead.head)};
+        if (o.page < 0) return Found{kNone, 0};
+        // (cache_row() and cache_cell(): a row's number fits 32 bits, whatever its summands do)
+        return Found{(unsigned)o.page * (unsigned)a.c.page_stride + (unsigned)o.place * (unsigned)a.c.slot_stride + (unsigned)ahead.head * (unsigned)a.c.head_stride,
+                     ((int64_t)o.page * a.c.kv_heads + ahead.head) * a.c.page_size + o.place};
     };
     const uint64_t policy = leaves_first();
     auto issue = [&](int stage, const Found &f) {
         constexpr int kChunks = 2 * kGroups;             // of 16 bytes in a row
         const unsigned to = ring + stage * C::kPartBytes;
-        if (lane < 16) copy8_or_zeros(to + C::kScalesAt + 8 * lane, f.row != kNone ? (const void *)(a.scales + f.cell) : (const void *)a.c.k, f.row != kNone);
+        if (C::kSlots == 32 || lane < 16) copy8_or_zeros(to + C::kScalesAt + 8 * lane, f.row != kNone ? (const void *)(a.scales + f.cell) : (const void *)a.c.k, f.row != kNone);
         const bool all = __all_sync(0xffffffffu, f.row != kNone) && a.c.head_dim == C::kDim;
         if (all) {                                       // (nearly always: an address, a shuffle and two copies)
 #pragma unroll
-            for (int i = 0; i < 16 * kChunks / 32; ++i) {
+            for (int i = 0; i < C::kSlots * kChunks / 32; ++i) {
                 const int c = i * 32 + lane, row = c / kChunks, chunk = c % kChunks;
-                const int64_t at = 16 * (int64_t)__shfl_sync(0xffffffffu, f.row, row);
-                copy16(to + row * C::kPitch + chunk * 16, a.c.k + 16 * chunk + at, policy);
-                copy16(to + (16 + row) * C::kPitch + chunk * 16, a.c.v + 16 * chunk + at, policy);
+                const unsigned from = __shfl_sync(0xffffffffu, f.row, row);
+                copy16(to + C::unit_at(row, chunk), a.c.k + 16 * chunk + (uint64_t)from * 16u, policy);
+                copy16(to + C::kSlots * C::kPitch + C::unit_at(row, chunk), a.c.v + 16 * chunk + (uint64_t)from * 16u, policy);
             }
         } else {
 #pragma unroll 1
-            for (int i = 0; i < 16 * kChunks / 32; ++i) {
+            for (int i = 0; i < C::kSlots * kChunks / 32; ++i) {
                 const int c = i * 32 + lane, row = c / kChunks, chunk = c % kChunks;
                 const unsigned from = __shfl_sync(0xffffffffu, f.row, row);
                 const bool there = from != kNone && chunk * 16 < a.c.head_dim;
                 const int64_t at = there ? 16 * ((int64_t)from + chunk) : 0;
-                copy16_or_zeros(to + row * C::kPitch + chunk * 16, a.c.k + at, there);
-                copy16_or_zeros(to + (16 + row) * C::kPitch + chunk * 16, a.c.v + at, there);
+                copy16_or_zeros(to + C::unit_at(row, chunk), a.c.k + at, there);
+                copy16_or_zeros(to + C::kSlots * C::kPitch + C::unit_at(row, chunk), a.c.v + at, there);
             }
         }
     };
@@ -222,7 +232,7 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
 #pragma unroll
         for (int i = 0; i < kStages; ++i) {
             rows[i] = Found{kNone, 0};
-            if (i < n) { rows[i] = look_up(); cursor_next(a, ahead, per); }
+            if (i < n) { rows[i] = look_up(); cursor_next<kSub>(a, ahead, per); }
         }
 #pragma unroll
         for (int i = 0; i < kStages - 1; ++i) {
@@ -232,7 +242,8 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
         next = rows[kStages - 1];
     }
 
-    // m, l: maximum and sum of the weights; top: maximum of weight times vs
+    // m, l: maximum and sum of the weights; top: maximum of weight times vs (kLowest: nothing seen yet, below any logit, and a number so that differences are)
+    constexpr float kLowest = -3.0e38f;
     float acc[C::kSteps][kCols][4], m[kCols][2], l[kCols][2], top[kCols][2];
     float by[kCols][2], off[kCols][2];                   // logit = (product - off) * by * ks
     unsigned held[C::kHeld ? C::kSteps * kCols * 2 : 1];
@@ -307,7 +318,7 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
                     for (int e = 0; e < 4; ++e) acc[k][j][e] = 0.0f;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    m[j][h] = top[j][h] = -INFINITY; l[j][h] = 0.0f;
+                    m[j][h] = top[j][h] = kLowest; l[j][h] = 0.0f;
                     const int row = j * 8 + (lane & 3) * 2 + h, t = row / a.group;
                     p[j][h] = row < a.rows && t < now.q.count ? now.q.length - now.q.count + t : -1;
                 }
@@ -317,128 +328,149 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
         __syncwarp();
         if (u + kStages - 1 < n) issue(stage == 0 ? kStages - 1 : stage - 1, next);
         asm volatile("cp.async.commit_group;" ::: "memory");
-        if (u + kStages < n) { next = look_up(); cursor_next(a, ahead, per); }
+        if (u + kStages < n) { next = look_up(); cursor_next<kSub>(a, ahead, per); }
 
         // ---- S^T ----
-        const unsigned keys = ring + stage * C::kPartBytes, values = keys + 16 * C::kPitch;
-        float x[kCols][4];
+        const unsigned keys = ring + stage * C::kPartBytes, values = keys + C::kSlots * C::kPitch;
+        unsigned kw[kSub][4];
+        float x[kSub][kCols][4];
 #pragma unroll
-        for (int j = 0; j < kCols; ++j)
+        for (int b = 0; b < kSub; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) x[j][e] = 0.0f;
-        const unsigned k_at = keys + ((lane & 7) + ((lane >> 3) & 1) * 8) * C::kPitch + (lane >> 4) * 16;
+            for (int j = 0; j < kCols; ++j)
 #pragma unroll
-        for (int g = 0; g < kGroups; ++g) {
-            unsigned w[4];                               // slots lane / 4 and 8 more; dimensions 32 g + 4 (lane & 3) .. and 16 more
-            ldsm4(w, k_at + g * 32);
+                for (int e = 0; e < 4; ++e) x[b][j][e] = 0.0f;
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g)
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                unsigned ka[4];
-                O::keys(w[2 * i], ka[0], ka[2]);
-                O::keys(w[2 * i + 1], ka[1], ka[3]);
+                const int k = 2 * g + i;
+                uint2 qb[kCols];
+#pragma unroll
+                for (int j = 0; j < kCols; ++j)
+                    qb[j] = C::kHeld ? make_uint2(held[(j * C::kSteps + k) * 2 * C::kHeld], held[((j * C::kSteps + k) * 2 + 1) * C::kHeld])
+                                     : *(const uint2 *)(s_q + ((k * C::kRows + j * 8 + (lane >> 2)) * 4 + (lane & 3)) * 8);
+#pragma unroll
+                for (int b = 0; b < kSub; ++b) {
+                    // words of slots lane / 4 and 8 more; dimensions 32 g + 4 (lane & 3) .. and 16 more
+                    if (i == 0) ldsm4(kw[b], keys + C::unit_at(16 * b + (lane & 15), 2 * g + (lane >> 4)));
+                    unsigned ka[4];
+                    O::keys(kw[b][2 * i], ka[0], ka[2]);
+                    O::keys(kw[b][2 * i + 1], ka[1], ka[3]);
+#pragma unroll
+                    for (int j = 0; j < kCols; ++j) mma<__half>(x[b][j], ka, qb[j].x, qb[j].y);
+                }
+            }
+        // ---- what each row sees ----
+        const int slot0 = slot_of(now), seen0 = now.q.length - now.q.count;
+        const bool whole = slot0 + C::kSlots - 1 <= seen0 && (a.window == 0 || slot0 > now.q.length - 1 - a.window);
+        float more[kSub][2];                             // logarithms of the values' scales, of slots lane / 4 and 8 more
+#pragma unroll
+        for (int b = 0; b < kSub; ++b) {
+            float2 scales[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(scales[i].x), "=f"(scales[i].y) : "r"(keys + C::kScalesAt + 8 * (16 * b + (lane >> 2) + 8 * i)) : "memory");
+                more[b][i] = log2_of(scales[i].y);
+            }
+#pragma unroll
+            for (int j = 0; j < kCols; ++j)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[b][j][e] = (x[b][j][e] - off[j][e & 1]) * (by[j][e & 1] * scales[e >> 1].x);
+                    if (!whole && !sees(a, p[j][e & 1], slot0 + 16 * b + (lane >> 2) + (e >> 1) * 8)) x[b][j][e] = -INFINITY;
+                }
+        }
+        if (a.logits != nullptr) {
+            const int64_t tile = (begin + u) * kSub + (kSub == 2 ? part / 2 : 0);
+            const int in_tile = kSub == 2 ? (part & 1) * 32 : part * 16;
+            if (in_tile == 0 && lane == 0) *(int4 *)&a.notes[tile] = make_int4(now.s, now.head, slot0, now.q.length);
+#pragma unroll
+            for (int b = 0; b < kSub; ++b) {
+                float *const to = a.logits + tile * (int64_t)(logit_pitch * kTile) + (in_tile + 16 * b + (lane >> 2)) * logit_pitch;
 #pragma unroll
                 for (int j = 0; j < kCols; ++j) {
-                    const int k = 2 * g + i;
-                    if (C::kHeld) {
-                        mma<__half>(x[j], ka, held[(j * C::kSteps + k) * 2], held[(j * C::kSteps + k) * 2 + 1]);
-                    } else {
-                        const uint2 qb = *(const uint2 *)(s_q + ((k * C::kRows + j * 8 + (lane >> 2)) * 4 + (lane & 3)) * 8);
-                        mma<__half>(x[j], ka, qb.x, qb.y);
+                    const int r = j * 8 + (lane & 3) * 2;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+                        const float2 w = make_float2(p[j][0] < 0 ? -INFINITY : x[b][j][2 * e], p[j][1] < 0 ? -INFINITY : x[b][j][2 * e + 1]);
+                        float *const at = to + e * 8 * logit_pitch + r;
+                        if (logit_pitch > 1) { if (r < logit_pitch) *(float2 *)at = w; }
+                        else if (r == 0) *at = w.x;
                     }
                 }
             }
         }
-        // ---- what each row sees ----
-        const int slot0 = first_slot(now.q, now.idx) + part * 16, seen0 = now.q.length - now.q.count;
-        const bool whole = slot0 + 15 <= seen0 && (a.window == 0 || slot0 > now.q.length - 1 - a.window);
-        float2 scales[2];                                // of slots lane / 4 and 8 more
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(scales[i].x), "=f"(scales[i].y) : "r"(keys + C::kScalesAt + 8 * ((lane >> 2) + 8 * i)) : "memory");
-        const float more[2] = {log2_of(scales[0].y), log2_of(scales[1].y)};
-#pragma unroll
-        for (int j = 0; j < kCols; ++j)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                x[j][e] = (x[j][e] - off[j][e & 1]) * (by[j][e & 1] * scales[e >> 1].x);
-                if (!whole && !sees(a, p[j][e & 1], slot0 + (lane >> 2) + (e >> 1) * 8)) x[j][e] = -INFINITY;
-            }
-        if (a.logits != nullptr) {
-            if (tid == 0) *(int4 *)&a.notes[begin + u] = make_int4(now.s, now.head, first_slot(now.q, now.idx), now.q.length);
-            float *const to = a.logits + (begin + u) * (int64_t)(logit_pitch * kTile) + (part * 16 + (lane >> 2)) * logit_pitch;
-#pragma unroll
-            for (int j = 0; j < kCols; ++j) {
-                const int r = j * 8 + (lane & 3) * 2;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float2 w = make_float2(p[j][0] < 0 ? -INFINITY : x[j][2 * e], p[j][1] < 0 ? -INFINITY : x[j][2 * e + 1]);
-                    float *const at = to + e * 8 * logit_pitch + r;
-                    if (logit_pitch > 1) { if (r < logit_pitch) *(float2 *)at = w; }
-                    else if (r == 0) *at = w.x;
-                }
-            }
-        }
         // ---- weights ----
-        float y[kCols][4];                               // with the value's scale (an unseen slot's may be anything)
+        float y[kSub][kCols][4];                         // with the value's scale (an unseen slot's may be anything)
         bool over = false;
 #pragma unroll
-        for (int j = 0; j < kCols; ++j) {
+        for (int b = 0; b < kSub; ++b)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) y[j][e] = x[j][e] == -INFINITY ? -INFINITY : x[j][e] + more[e >> 1];
+            for (int j = 0; j < kCols; ++j) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) over |= fmaxf(x[j][h], x[j][h + 2]) > m[j][h] + kSlack || fmaxf(y[j][h], y[j][h + 2]) > top[j][h] + kSlack;
-        }
+                for (int e = 0; e < 4; ++e) {
+                    y[b][j][e] = x[b][j][e] + more[b][e >> 1];
+                    if (!whole) y[b][j][e] = x[b][j][e] == -INFINITY ? -INFINITY : y[b][j][e];
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) over |= fmaxf(fmaxf(x[b][j][h], x[b][j][h + 2]) - m[j][h], fmaxf(y[b][j][h], y[b][j][h + 2]) - top[j][h]) > kSlack;
+            }
         if (__any_sync(0xffffffffu, over)) {
 #pragma unroll
             for (int j = 0; j < kCols; ++j)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    float best = fmaxf(x[j][h], x[j][h + 2]), most = fmaxf(y[j][h], y[j][h + 2]);
+                    float best = m[j][h], most = top[j][h];
+#pragma unroll
+                    for (int b = 0; b < kSub; ++b) {
+                        best = fmaxf(best, fmaxf(x[b][j][h], x[b][j][h + 2]));
+                        most = fmaxf(most, fmaxf(y[b][j][h], y[b][j][h + 2]));
+                    }
 #pragma unroll
                     for (int o = 4; o < 32; o *= 2) {
                         best = fmaxf(best, __shfl_xor_sync(0xffffffffu, best, o));
                         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
                     }
-                    best = fmaxf(best, m[j][h]); most = fmaxf(most, top[j][h]);
-                    l[j][h] *= exp2_of(m[j][h] - (best == -INFINITY ? 0.0f : best));
-                    const float less_now = exp2_of(top[j][h] - (most == -INFINITY ? 0.0f : most));
+                    l[j][h] *= exp2_of(m[j][h] - best);
+                    const float less_now = exp2_of(top[j][h] - most);
                     m[j][h] = best; top[j][h] = most;
 #pragma unroll
                     for (int k = 0; k < C::kSteps; ++k) { acc[k][j][h] *= less_now; acc[k][j][h + 2] *= less_now; }
                 }
         }
 #pragma unroll
-        for (int j = 0; j < kCols; ++j)
+        for (int b = 0; b < kSub; ++b)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const float ref = m[j][h] == -INFINITY ? 0.0f : m[j][h], most = (top[j][h] == -INFINITY ? 0.0f : top[j][h]) - kLift;
-                l[j][h] += exp2_of(x[j][h] - ref) + exp2_of(x[j][h + 2] - ref);
-                x[j][h] = exp2_of(y[j][h] - most); x[j][h + 2] = exp2_of(y[j][h + 2] - most);
-            }
+            for (int j = 0; j < kCols; ++j)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const float most = top[j][h] - kLift;
+                    l[j][h] += exp2_of(x[b][j][h] - m[j][h]) + exp2_of(x[b][j][h + 2] - m[j][h]);
+                    x[b][j][h] = exp2_of(y[b][j][h] - most); x[b][j][h + 2] = exp2_of(y[b][j][h + 2] - most);
+                }
         // ---- O^T ----
         __syncwarp();                                    // (a warp executes what follows as one)
         bool apart = false;
         if (std::is_same<Code, E4m3>::value && !whole && now.q.count > 1) {
             // Slots that only some rows see: a weight of zero times a code that is no number is none.
-            for (int i = lane; i < 16 * C::kDim / 4; i += 32) {
-                unsigned w;
-                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(values + i / (C::kDim / 4) * C::kPitch + i % (C::kDim / 4) * 4) : "memory");
-                apart |= __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
+            for (int i = lane; i < C::kSlots * C::kDim / 16; i += 32) {
+                unsigned w[4];
+                load_words<4>(w, values + C::unit_at(i / (C::kDim / 16), i % (C::kDim / 16)));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) apart |= __vcmpeq4(w[e] & 0x7f7f7f7fu, 0x7f7f7f7fu) != 0;
             }
             apart = __any_sync(0xffffffffu, apart);
         }
-        unsigned wb[kCols][2];
-#pragma unroll
-        for (int j = 0; j < kCols; ++j)
-#pragma unroll
-            for (int e = 0; e < 2; ++e) wb[j][e] = turned8x8(Pair<__half>::pack(x[j][2 * e], x[j][2 * e + 1]));
         const int c = lane & 3, r = lane >> 2;
+        // where bytes `at` .. of a slot's values lie
+        auto value_at = [&](int slot, int at) -> unsigned { return values + C::unit_at(slot, at >> 4) + (at & 15); };
         // words words_ of the lane's slots from dimension `base` + 4 words_ (lane / 4) on: steps k0 .. of the sums
-        auto values_of = [&](auto words_, int base, int k0) {
+        auto values_of = [&](auto words_, int base, int k0, int b, const unsigned (&wb)[kCols][2]) {
             constexpr int kWords = decltype(words_)::value;
             unsigned w[4][kWords];                       // slots 2 c, 2 c + 1, 2 c + 8, 2 c + 9
 #pragma unroll
-            for (int i = 0; i < 4; ++i) load_words<kWords>(w[i], values + (2 * c + (i & 1) + (i >> 1) * 8) * C::kPitch + base + 4 * kWords * r);
+            for (int i = 0; i < 4; ++i) load_words<kWords>(w[i], value_at(16 * b + 2 * c + (i & 1) + (i >> 1) * 8, base + 4 * kWords * r));
 #pragma unroll
             for (int i = 0; i < kWords; ++i) {
                 unsigned lo[4], hi[4];
@@ -460,32 +492,42 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
         };
         if (!apart) {
 #pragma unroll
-            for (int b = 0; b < kGroups / 4; ++b) values_of(std::integral_constant<int, 4>(), 128 * b, 8 * b);
-            if (kGroups % 4 >= 2) values_of(std::integral_constant<int, 2>(), kGroups / 4 * 128, kGroups / 4 * 8);
-            if (kGroups % 2 == 1) values_of(std::integral_constant<int, 1>(), (kGroups - 1) * 32, (kGroups - 1) * 2);
+            for (int b = 0; b < kSub; ++b) {
+                unsigned wb[kCols][2];
+#pragma unroll
+                for (int j = 0; j < kCols; ++j)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) wb[j][e] = turned8x8(Pair<__half>::pack(x[b][j][2 * e], x[b][j][2 * e + 1]));
+#pragma unroll
+                for (int q = 0; q < kGroups / 4; ++q) values_of(std::integral_constant<int, 4>(), 128 * q, 8 * q, b, wb);
+                if (kGroups % 4 >= 2) values_of(std::integral_constant<int, 2>(), kGroups / 4 * 128, kGroups / 4 * 8, b, wb);
+                if (kGroups % 2 == 1) values_of(std::integral_constant<int, 1>(), (kGroups - 1) * 32, (kGroups - 1) * 2, b, wb);
+            }
         } else {
-            for (int o = 0; o < 16; ++o)
 #pragma unroll
-                for (int j = 0; j < kCols; ++j) {
-                    float w[2];
-                    bool in[2];
+            for (int b = 0; b < kSub; ++b)
+                for (int o = 0; o < 16; ++o)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        w[h] = __shfl_sync(0xffffffffu, o < 8 ? x[j][h] : x[j][h + 2], (o & 7) * 4 + c);
-                        in[h] = sees(a, p[j][h], slot0 + o);
-                    }
+                    for (int j = 0; j < kCols; ++j) {
+                        float w[2];
+                        bool in[2];
 #pragma unroll
-                    for (int k = 0; k < C::kSteps; ++k) {
-                        unsigned short v;
-                        asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(values + o * C::kPitch + dim_of(k)) : "memory");
+                        for (int h = 0; h < 2; ++h) {
+                            w[h] = __shfl_sync(0xffffffffu, o < 8 ? x[b][j][h] : x[b][j][h + 2], (o & 7) * 4 + c);
+                            in[h] = sees(a, p[j][h], slot0 + 16 * b + o);
+                        }
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const float f = O::value((unsigned)v >> (8 * e));
+                        for (int k = 0; k < C::kSteps; ++k) {
+                            unsigned short v;
+                            asm volatile("ld.shared.b16 %0, [%1];" : "=h"(v) : "r"(value_at(16 * b + o, dim_of(k))) : "memory");
 #pragma unroll
-                            for (int h = 0; h < 2; ++h) if (in[h]) acc[k][j][2 * e + h] = fmaf(w[h], f, acc[k][j][2 * e + h]);
+                            for (int e = 0; e < 2; ++e) {
+                                const float f = O::value((unsigned)v >> (8 * e));
+#pragma unroll
+                                for (int h = 0; h < 2; ++h) if (in[h]) acc[k][j][2 * e + h] = fmaf(w[h], f, acc[k][j][2 * e + h]);
+                            }
                         }
                     }
-                }
         }
         if (now.idx == now.q.tiles - 1 || u == n - 1) {
             // ---- the piece's end: the parts are joined, eight rows at a time, each warp's sums in the part of its ring that it is done with ----
@@ -497,7 +539,7 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
 #pragma unroll
                     for (int o = 4; o < 32; o *= 2) l[j][h] += __shfl_xor_sync(0xffffffffu, l[j][h], o);
                     l[j][h] /= Weights<T>::kUnlift;      // (what joins expects sums as the other kernel leaves them)
-                    if (lane < 4) s_ml[part * C::kRows + j * 8 + lane * 2 + h] = p[j][h] < 0 ? make_float2(-INFINITY, 0.0f) : make_float2(m[j][h], l[j][h]);
+                    if (lane < 4) s_ml[part * C::kRows + j * 8 + lane * 2 + h] = p[j][h] < 0 || m[j][h] == kLowest ? make_float2(-INFINITY, l[j][h] - l[j][h]) : make_float2(m[j][h], l[j][h]);
                 }
             float *const room = (float *)(smem + stage * C::kPartBytes);
             constexpr int kApart = kStages * C::kPartBytes / 4;      // floats from one warp's to the next's
@@ -509,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     // from the maximum of weight times vs to that of the weights (no value yet: no sums)
-                    const float back = top[j][h] == -INFINITY ? 1.0f : exp2_of(top[j][h] - m[j][h] - kLift + Weights<T>::kLift);
+                    const float back = top[j][h] == kLowest ? 1.0f : exp2_of(top[j][h] - m[j][h] - kLift + Weights<T>::kLift);
 #pragma unroll
                     for (int k = 0; k < C::kSteps; k += 2)
                         *(float4 *)&room[part * kApart + (c * 2 + h) * C::kMergePitch + dim_of(k)] =
@@ -550,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
             fresh = true;
         }
         stage = stage == kStages - 1 ? 0 : stage + 1;
-        cursor_next(a, now, per);
+        cursor_next<kSub>(a, now, per);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (bad != 0) raise_status(a.c.status, bad);
@@ -582,7 +624,7 @@ cudaError_t launch_packed(const PackedArgs &a, const AttendShape &z, cudaStream_
 {
     typedef PackedConfig<kGroups, kCols> C;
     static int known[kMaxDevices], most_known[kMaxDevices];
-    return launch_few<T, C::kRows, C::kDim, AttendArgs>(k_packed_attend<T, Code, kGroups, kCols>, C::kSmem, known, most_known, a, z, s);
+    return launch_few<T, C::kRows, C::kDim, C::kSub, AttendArgs>(k_packed_attend<T, Code, kGroups, kCols>, C::kSmem, known, most_known, a, z, s);
 }
 template <typename T, typename Code, int kGroups>
 cudaError_t launch_packed_rows(const PackedArgs &a, const AttendShape &z, cudaStream_t s)

@@ -12,7 +12,10 @@ AttendShape packed_shape(const CacheView &c, int rows, int new_tokens, int windo
 {
     AttendShape z = attend_shape(c, rows, new_tokens, window, sinks);
     const int groups = (c.head_dim + 31) / 32;
-    if (z.block_rows <= 16) z.padded_dim = 32 * (groups <= 2 ? 2 : groups <= 4 ? groups : groups <= 6 ? 6 : 8);
+    if (z.block_rows <= 16) {
+        z.padded_dim = 32 * (groups <= 2 ? 2 : groups <= 4 ? groups : groups <= 6 ? 6 : 8);
+        if (z.items > 0) z.tiles = (z.tiles / z.items + 1) / 2 * 2 * z.items;    // (they may be taken two at a time)
+    }
     return z;
 }
 
