@@ -197,7 +197,8 @@ struct AttendShape {
 };
 AttendShape attend_shape(const CacheView &c, int rows, int new_tokens, int window, int sinks);
 cudaError_t launch_cache_attend(const AttendArgs &a, int dtype, cudaStream_t s);
-// `begin` has its own room (shape: attend_shape of its sequence); shared: as the caller has it.
+// shared: as the caller has it.  begin_shape: attend_shape for the beginning.
+AttendShape begin_shape(const CacheView &c, int rows, int new_tokens);
 cudaError_t launch_cache_shared(const BeginArgs &begin, const RestArgs &rest, const int32_t *shared, int dtype, cudaStream_t s);
 
 struct EvictArgs {

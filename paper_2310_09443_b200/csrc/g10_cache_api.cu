@@ -239,7 +239,7 @@ int32_t g10_cache_shared_workspace_bytes(const g10_cache *cache, int32_t new_tok
     if (rc == G10_OK) rc = check_shared(c, new_tokens, q_heads);
     if (rc != G10_OK) return rc;
     const int tokens = c.num_seqs * new_tokens, group = q_heads / c.kv_heads;
-    *out_bytes = shared_layout(attend_shape(begin_view(c), tokens * group, tokens, 0, 0), attend_shape(c, new_tokens * group, new_tokens, 0, 0),
+    *out_bytes = shared_layout(begin_shape(begin_view(c), tokens * group, tokens), attend_shape(c, new_tokens * group, new_tokens, 0, 0),
                                (int64_t)tokens * q_heads, c.head_dim).bytes;
     return G10_OK;
 }
@@ -259,7 +259,7 @@ int32_t g10_cache_attend_shared(const g10_cache *cache, const g10_cache_queries 
     static_cast<SharedArgs &>(b) = a;
     b.c = begin_view(a.c);
     b.new_tokens = a.c.num_seqs * a.new_tokens; b.rows = b.new_tokens * b.group; b.counts = nullptr;
-    const AttendShape y = attend_shape(b.c, b.rows, b.new_tokens, 0, 0), z = attend_shape(a.c, a.rows, a.new_tokens, 0, 0);
+    const AttendShape y = begin_shape(b.c, b.rows, b.new_tokens), z = attend_shape(a.c, a.rows, a.new_tokens, 0, 0);
     const SharedLayout l = shared_layout(y, z, (int64_t)b.new_tokens * a.q_heads, a.c.head_dim);
     if (!ws || ((uintptr_t)ws & (kAlign - 1)) || ws_bytes < l.bytes) return G10_ERR_WORKSPACE;
     a.shared = b.shared = (int32_t *)((char *)ws + l.shared);

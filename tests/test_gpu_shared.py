@@ -57,7 +57,7 @@ def test_head_dims(g10, dim, kind, new, group):
 
 
 @pytest.mark.parametrize("common", [0, 16, 48, 64, 112, 128, 192, 640, 4096])
-@pytest.mark.parametrize("seqs,new,group", [(1, 1, 1), (3, 1, 4), (20, 1, 8), (5, 20, 3), (70, 2, 2)])
+@pytest.mark.parametrize("seqs,new,group", [(1, 1, 1), (3, 1, 4), (20, 1, 8), (5, 20, 3), (70, 2, 2), (129, 1, 1), (32, 1, 8), (33, 1, 8), (100, 1, 4)])
 def test_lengths_of_the_beginning(g10, common, seqs, new, group):
     own = [new + (37 * i) % 90 for i in range(seqs)]
     c = make_shared(common, own, 2, 64, 16, torch.bfloat16, common + seqs)
@@ -131,7 +131,8 @@ def test_infinite_logits(g10):
             check(g10, d, q, 128)
 
 
-@pytest.mark.parametrize("seqs,new,group,kv,dim,common", [(64, 1, 8, 2, 128, 9000), (33, 3, 5, 1, 96, 5000), (2, 1, 1, 8, 64, 20000), (9, 60, 8, 1, 128, 3000), (3, 2, 6, 1, 256, 2500)])
+@pytest.mark.parametrize("seqs,new,group,kv,dim,common", [(64, 1, 8, 2, 128, 9000), (33, 3, 5, 1, 96, 5000), (2, 1, 1, 8, 64, 20000), (9, 60, 8, 1, 128, 3000), (3, 2, 6, 1, 256, 2500),
+                                                           (40, 1, 4, 3, 64, 7000), (130, 1, 4, 2, 128, 1280), (65, 2, 2, 2, 40, 6500), (300, 1, 1, 2, 112, 10000)])
 def test_long(g10, seqs, new, group, kv, dim, common):
     page = 20
     c = make_shared(common // page * page, [new + (131 * i) % 400 for i in range(seqs)], kv, dim, page, torch.bfloat16, seqs)
