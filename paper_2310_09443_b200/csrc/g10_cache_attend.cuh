@@ -136,6 +136,7 @@ __device__ __forceinline__ Tally tally_of(const Args &a, ull &bad)
     Tally t;
     t.from = min(a.c.num_seqs, (int)threadIdx.x * each); t.to = min(a.c.num_seqs, t.from + each);
     long long sum = 0;
+#pragma unroll 1
     for (int s = t.from; s < t.to; ++s) sum += units_of<kUnit>(a, s, bad).tiles;
     const long long upto = warp_inclusive_scan_i64(sum, lane);
     if (lane == 31) s_sum[warp] = upto;

@@ -64,9 +64,11 @@ __device__ __forceinline__ bool bar_try(unsigned bar, unsigned parity)
 // copies nor accesses of tensor memory (what those would meet is no longer ordered), and arrives nowhere: loaders and issuer leave their loops, the row
 // threads, which meet one another, go through theirs without.  The block ends when all that it has under way is done, and says so in the status word.
 // Whole warps wait, and leave the wait together with one answer: what follows mostly is an instruction that a warp has to execute as one (a warp that had
-// come apart in a wait read and wrote tensor memory piecemeal, which gave wrong sums and illegal instructions).
+// come apart in a wait read and wrote tensor memory piecemeal, which gave wrong sums and illegal instructions).  Not unrolled: the polls of all waits made up 60 to 90 KB of
+// code, more than the instruction cache keeps, and every role of a kernel waited for its instructions.
 __device__ __forceinline__ bool bar_wait(unsigned bar, unsigned parity, volatile int *s_stop, unsigned limit)
 {
+#pragma unroll 1
     for (unsigned i = 0; i < limit; ++i) {
         if (__all_sync(0xffffffffu, bar_try(bar, parity))) return true;
         if (__any_sync(0xffffffffu, *s_stop != 0)) return false;
@@ -139,6 +141,27 @@ __device__ __forceinline__ void multiply_tmem(unsigned to, unsigned a, uint64_t 
 __device__ __forceinline__ void tell_when_done(unsigned bar)
 {
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// The same by the lane for which `leads` holds, called by the warp as one: where a product's operands are worked out by the whole warp they stay in the registers that all
+// lanes share, from which products take them; in a lane's own branch each is carried there one by one, 75 clocks a product.  at_a, at_b: the lower halves of the
+// operands (operand() has the same upper half for all, given the distance of their rows).
+__device__ __forceinline__ unsigned shared_by_lanes(unsigned x) { return __shfl_sync(0xffffffffu, x, 0); }
+constexpr unsigned kOperandUpper = 1024 >> 4 | 1u << 14 | 2u << 29;
+__device__ __forceinline__ void multiply_by(bool leads, unsigned to, unsigned at_a, unsigned at_b, unsigned what, bool add)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\tmov.b64 a, {%1, %6};\n\tmov.b64 b, {%2, %6};\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}"
+                 ::"r"(to), "r"(at_a), "r"(at_b), "r"(what), "r"(add ? 1u : 0u), "r"(leads ? 1u : 0u), "r"(kOperandUpper) : "memory");
+}
+__device__ __forceinline__ void multiply_tmem_by(bool leads, unsigned to, unsigned a, unsigned at_b, unsigned what, bool add)
+{
+    asm volatile("{\n\t.reg .pred p, q;\n\t.reg .b64 b;\n\tsetp.ne.u32 p, %4, 0;\n\tsetp.ne.u32 q, %5, 0;\n\tmov.b64 b, {%2, %6};\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}"
+                 ::"r"(to), "r"(a), "r"(at_b), "r"(what), "r"(add ? 1u : 0u), "r"(leads ? 1u : 0u), "r"(kOperandUpper) : "memory");
+}
+__device__ __forceinline__ void tell_when_done_by(bool leads, unsigned bar)
+{
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.u32 q, %1, 0;\n\t@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(leads ? 1u : 0u) : "memory");
 }
 __device__ __forceinline__ void tmem_take(unsigned *to, unsigned columns)
 {
@@ -520,6 +543,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
         // another cannot tell them apart)
         if (leads) tell_when_done(at_end);
         __syncwarp();
+#pragma unroll 1
         for (unsigned i = 0; i < kWideSpins && !bar_try(at_end, 0); ++i) {}
         __syncwarp();
     } else {
@@ -995,6 +1019,7 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const Args a)
         }
         if (leads) tell_when_done(at_end);               // (as above)
         __syncwarp();
+#pragma unroll 1
         for (unsigned i = 0; i < kWideSpins && !bar_try(at_end, 0); ++i) {}
         __syncwarp();
     } else {

@@ -35,29 +35,56 @@ static __global__ void __launch_bounds__(kCheckThreads) k_cache_shared(const Res
 }
 
 // ---- the beginning, for more than 128 rows a head: 256 rows at a time ----
-// 512 operations a byte of keys and values: a matter of the tensor cores, and of the exponentials, 16 a clock and SM, which take as long as the products (128 x 128 logits of
-// 128 dims: 1024 clocks either).  So a block has two operands of 128 rows, a team of four warps each, with S and O of their own, and takes 128 slots at a time: while one team
-// works its weights out, the products of the other run.  W lies over the first half of its S (tensor memory is full with S and O twice), so the next S of a team is
-// issued when the product of W with the values is done:
-//   W0 V, S0 of the next slots, W1 V, S1 of the next slots, ...
-// All slots are visible to all rows: there is nothing to mask but the second half of the last unit where the beginning ends on an odd tile.
-// (The kernel that takes 128 rows and 64 slots at a time, two teams in turn: 117 us for 512 rows of 8 heads behind 32 000 slots.)
+// 512 operations a byte of keys and values: a matter of the tensor cores, and of the exponentials, 16 a clock and SM, which take as long as the products (64 x 128 logits of
+// 128 dims: 512 clocks either).  So a block has two operands of 128 rows, a team of four warps each, with one S, two W and an O of their own (that fills tensor memory).
+// The next S of a team is issued once the team has its logits in registers, and runs while it works the weights out; products of W with the values are nothing
+// that a team waits for, but for the W before the last, whose columns come next.  All slots are visible to all rows: there is nothing to mask.
+// (512 rows of 8 heads behind 32 000 slots: 117 us with 128 rows, two teams that take the tiles in turn; 90 us with 128 slots at a time, W over its S; 82 us with two S of 64 slots, W over them:
+// from a W by its product and the S behind it back to the team took longer than the team's other tile.)
 //
-// Warps: 0 - 7 rows, 8 issues, 9 - 12 bring keys and values (32 slots each, rings of two of either), 13 - 15 only make whole groups of four, which registers are handed over
-// by: a row's thread holds its 128 logits.
-constexpr int kBeginRows = 256, kBeginSlots = 128, kBeginThreads = 512, kBeginUnit = kBeginSlots / kTile;
-constexpr int kRowRegisters = 192, kOtherRegisters = 64;             // of a thread: 256 * 192 + 256 * 64 = 65536
+// Warps: 0 - 7 rows, 8 issues the products with the queries, 9 those with the values, 10 and 11 bring keys and values (32 slots each, rings of four tiles of either).  One
+// warp that issued all (24 products, 6 waits a tile) took longer than the products.
+constexpr int kBeginRows = 256, kBeginThreads = 32 * 12;
 template <int kDims>
 struct Begin {
     static constexpr int kDim = 64 * kDims, kUnits = 8 * kDims;
-    static constexpr int kBlockBytes = kBeginSlots * 128;            // 64 dimensions of 128 rows or slots
-    static constexpr int kSideBytes = kDims * kBlockBytes;           // keys or values of a unit, queries of a team
-    static constexpr int kStages = 2;
-    static constexpr int kSmem = 1024 + 2 * kSideBytes + 2 * kStages * kSideBytes;
-    static constexpr int kSums = 2 * kBeginSlots;                    // first column of tensor memory behind the teams' S
-    static constexpr unsigned kColumns = 512;
+    static constexpr int kQBytes = kDims * kWideRows * 128;          // queries of a team
+    static constexpr int kSideBytes = kDims * kBlock;                // keys or values of a tile
+    static constexpr int kStages = 4;
+    static constexpr int kSmem = 1024 + 2 * kQBytes + 2 * kStages * kSideBytes;
+    static constexpr int kWeights = 2 * kTile, kSums = kWeights + 4 * kTile / 2;       // first columns of tensor memory behind the teams' S, their W
+    static constexpr unsigned kColumns = 512, kTmem = 0;             // (all columns are taken: they begin at 0)
     static_assert(kSums + 2 * kDim <= 512, "tensor memory");
 };
+
+// A team's queries (with the sign of the scale), 16 bytes a thread at a time, neighbouring threads at neighbouring ones.
+template <int kDims>
+__device__ __forceinline__ void bring_team_queries(const BeginArgs &a, const Cursor &u, int first_row, int r, char *s_q)
+{
+    constexpr int kUnits = 8 * kDims, kAtOnce = kWideRows / kUnits;
+    const int unit = r % kUnits;
+    const unsigned flip = a.scale_log2 < 0.0f ? 0x80008000u : 0u;
+    constexpr int kAhead = 8;
+#pragma unroll 1
+    for (int j0 = 0; j0 < kUnits; j0 += kAhead) {
+        uint4 x[kAhead];
+        // (sequence, token and head of the group of one row after the other, kAtOnce apart)
+        int row = first_row + j0 * kAtOnce + r / kUnits, t = row / a.group, g = row - t * a.group, s = t / a.each;
+        t -= s * a.each;
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            x[j] = make_uint4(0, 0, 0, 0);
+            if (row < a.rows && unit * 8 < a.c.head_dim) x[j] = __ldg((const uint4 *)(a.q + 2 * (s * a.q_seq + t * a.q_token + (u.head * a.group + g) * a.q_head) + 16 * unit));
+            row += kAtOnce;
+            for (g += kAtOnce; g >= a.group; g -= a.group) if (++t == a.each) { t = 0; ++s; }
+        }
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j) {
+            x[j].x ^= flip; x[j].y ^= flip; x[j].z ^= flip; x[j].w ^= flip;
+            *(uint4 *)(s_q + swizzled((j0 + j) * kAtOnce + r / kUnits, unit, kWideRows * 128)) = x[j];
+        }
+    }
+}
 
 template <typename T, int kDims>
 __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArgs a, int held_blocks)
@@ -65,7 +92,8 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
     typedef Begin<kDims> C;
     constexpr int S = C::kStages;
     extern __shared__ char smem_raw[];
-    __shared__ __align__(8) uint64_t s_bar[4 * S + 9];
+    __shared__ __align__(8) uint64_t s_bar[4 * S + 15];
+    static_assert(C::kSums + 2 * C::kDim <= 512, "tensor memory");
     __shared__ Place s_place;
     __shared__ int s_stop;
     __shared__ unsigned s_tmem;
@@ -73,69 +101,83 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
     const int per = a.c.kv_heads * a.row_blocks;
     ull bad = 0;
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
-    const Tally tally = tally_of<kBeginThreads, kBeginUnit>(a, bad);
-    const Share share = share_of<kBeginUnit>(tally.total, per, gridDim.x, held_blocks);
+    const Tally tally = tally_of<kBeginThreads>(a, bad);
+    const Share share = share_of(tally.total, per, gridDim.x, held_blocks);
     const int64_t begin = begin_of(share, blockIdx.x);
     const int n = (int)(begin_of(share, blockIdx.x + 1) - begin);
     if (n == 0) return;
-    place_of<kBeginUnit>(a, tally, begin, per, &s_place);
+    place_of(a, tally, begin, per, &s_place);
     const unsigned k_full = smem_of(s_bar), k_free = k_full + 8 * S, v_full = k_free + 8 * S, v_free = v_full + 8 * S;
-    const unsigned s_full = v_free + 8 * S, w_full = s_full + 16, w_done = w_full + 16, q_full = w_done + 16, at_end = q_full + 16;        // two each, a team's
+    // (each team's S, its two W and the products with them)
+    const unsigned s_full = v_free + 8 * S, s_free = s_full + 16, w_full = s_free + 16, w_done = w_full + 32, q_full = w_done + 32, at_end = q_full + 16;
     if (tid == 0) {
         s_stop = 0;
-        for (int i = 0; i < S; ++i) { bar_init(k_full + 8 * i, 128); bar_init(k_free + 8 * i, 1); bar_init(v_full + 8 * i, 128); bar_init(v_free + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(w_full + 8 * i, 128); bar_init(w_done + 8 * i, 1); bar_init(q_full + 8 * i, 128); }
-        bar_init(at_end, 1);
+        for (int i = 0; i < S; ++i) { bar_init(k_full + 8 * i, kLoadThreads); bar_init(k_free + 8 * i, 1); bar_init(v_full + 8 * i, kLoadThreads); bar_init(v_free + 8 * i, 1); }
+        for (int i = 0; i < 4; ++i) { bar_init(w_full + 8 * i, 128); bar_init(w_done + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(s_free + 8 * i, 128); bar_init(q_full + 8 * i, 128); }
+        bar_init(at_end, 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 8) tmem_take(&s_tmem, C::kColumns);
+    char *const s_q = smem_raw + ((1024u - (smem_of(smem_raw) & 1023u)) & 1023u);
+    // dimensions behind head_dim: zeros in all stages, which no copy writes to
+    const int units = a.c.head_dim / 8, pad = C::kUnits - units;
+    for (int i = tid; i < 2 * S * kTile * pad; i += kBeginThreads) {
+        const int side = i / (kTile * pad), in = i - side * kTile * pad, row = in / pad;
+        *(uint4 *)(s_q + 2 * C::kQBytes + side * C::kSideBytes + swizzled(row, units + in - row * pad, kBlock)) = make_uint4(0, 0, 0, 0);
+    }
+    async_sees();
     before_sync();
     __syncthreads();
     after_sync();
-    const unsigned tmem = s_tmem, limit = wait_limit(a);
+    const unsigned tmem = C::kTmem, limit = wait_limit(a);
     auto wait = [&](unsigned bar, unsigned parity) -> bool { return bar_wait(bar, parity, &s_stop, limit); };
-    char *const s_q = (char *)(((uintptr_t)smem_raw + 1023) & ~(uintptr_t)1023);
-    const unsigned ring = smem_of(s_q) + 2 * C::kSideBytes;          // keys of each stage, then values of each
+    const unsigned ring = smem_of(s_q) + 2 * C::kQBytes; // keys of each stage, then values of each
     Cursor now;
-    cursor_at<kBeginUnit>(a, now, s_place, begin);
+    cursor_at(a, now, s_place, begin);
     // Does a team have rows in the cursor's block?
     auto has_rows = [&](int team) -> bool { return now.block * kBeginRows + team * kWideRows < a.rows; };
+    // Tile u has W u & 1.  A barrier's phases are counted by whoever passes it: a team takes no part in pieces in which it has no rows.
 
     if (warp < 8) {
-        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kRowRegisters));
+        // ---- rows: a thread each ----
         const int r = tid & (kWideRows - 1), team = tid >> 7;
-        const unsigned logits = tmem + ((unsigned)((warp & 3) * 32) << 16) + team * kBeginSlots, own = tmem + ((unsigned)((warp & 3) * 32) << 16) + C::kSums + team * C::kDim;
+        const unsigned lanes = tmem + ((unsigned)((warp & 3) * 32) << 16), own = lanes + C::kSums + team * C::kDim;
         const float scale = fabsf(a.scale_log2);
         bool going = true;                               // (the warp alike)
-        unsigned units = 0;                              // that this team has seen
+        unsigned count = 0, used[2] = {0, 0};            // tiles of this team, times that each W has been used
+        auto done = [&](unsigned b) -> bool { return wait(w_done + 16 * team + 8 * b, ((b == 0 ? used[0] : used[1]) - 1) & 1); };
         auto bring = [&]() {
             if (!has_rows(team)) return;
-            char *const to = s_q + team * C::kSideBytes;
-            bring_queries<kDims>(a, now, now.block * kBeginRows + team * kWideRows, r, 0, to);
-            bring_queries<kDims>(a, now, now.block * kBeginRows + team * kWideRows, r, 1, to);
+            bring_team_queries<kDims>(a, now, now.block * kBeginRows + team * kWideRows, r, s_q + team * C::kQBytes);
             async_sees();
             if (!(muted(a, 6, 1) && tid == 0)) bar_arrive(q_full + 8 * team);
         };
         bring();
         for (int u0 = 0; u0 < n;) {
+            // ---- a piece: tiles u0 .. u1 - 1 ----
             const int u1 = u0 + min(now.q.tiles - now.idx, n - u0);
             const bool mine = has_rows(team);
             float m = -INFINITY, l = 0.0f;
-            for (int u = u0; u < u1 && mine; ++u, ++units) {
-                going = going && wait(s_full + 8 * team, units & 1);
+            for (int u = u0; u < u1 && mine; ++u, ++count) {
+                const unsigned b = u & 1, logits = lanes + team * kTile;
+                going = going && wait(s_full + 8 * team, count & 1);
                 if (!going) continue;
                 after_sync();
-                const bool half = (now.idx + u - u0) * kBeginSlots + kTile >= now.q.length;        // (the second tile lies behind the end)
-                unsigned x[4][32];
+                float2 x[kTile / 2];
+                {
+                    unsigned raw[kTile];
+                    tmem_load(*(unsigned(*)[32])&raw[0], logits);
+                    tmem_load(*(unsigned(*)[32])&raw[32], logits + 32);
+                    tmem_loaded();
+                    before_sync();
+                    bar_arrive(s_free + 8 * team);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) tmem_load(x[i], logits + 32 * i);
-                tmem_loaded();
+                    for (int j = 0; j < kTile / 2; ++j) x[j] = make_float2(__uint_as_float(raw[2 * j]), __uint_as_float(raw[2 * j + 1]));
+                }
                 float best[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int j = 0; j < 32; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) best[i] = fmaxf(best[i], __uint_as_float(x[i][j]));
-                if (half) best[2] = best[3] = -INFINITY;
+                for (int j = 0; j < kTile / 2; ++j) best[j & 3] = fmaxf(best[j & 3], fmaxf(x[j].x, x[j].y));
                 float top = fmaxf(fmaxf(best[0], best[1]), fmaxf(best[2], best[3]));
                 top = top == -INFINITY ? top : top * scale;
                 // (rescaled only where a logit is far above the reference)
@@ -144,7 +186,7 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
                     const float by = exp2_of(m - (top == -INFINITY ? 0.0f : top));
                     m = top; l *= by;
                     if (u > u0) {
-                        going = wait(w_done + 8 * team, (units - 1) & 1);
+                        going = done(b ^ 1);
                         after_sync();
 #pragma unroll 1
                         for (int c = 0; c < C::kDim && going; c += 32) {
@@ -162,31 +204,26 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
                 const float ref = m == -INFINITY ? 0.0f : m;
                 const float2 by = make_float2(scale, scale), off = make_float2(Weights<T>::kLift - ref, Weights<T>::kLift - ref);
                 float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
+                unsigned w[32];
 #pragma unroll
-                for (int i = 0; i < 4; i += 2) {
-                    unsigned w[32];
-                    if (i == 2 && half) {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) w[j] = 0;
-                        tmem_store(w, logits + 16 * i);
-                        break;
-                    }
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) {
-                            const float2 y = fma2(make_float2(__uint_as_float(x[i + k][2 * j]), __uint_as_float(x[i + k][2 * j + 1])), by, off);
-                            const float2 z = make_float2(exp2_of(y.x), exp2_of(y.y));
-                            part[j & 1] = add2(part[j & 1], z);
-                            w[16 * k + j] = Pair<T>::pack(z.x, z.y);
-                        }
-                    tmem_store(w, logits + 16 * i);
+                for (int j = 0; j < kTile / 2; ++j) {
+                    const float2 y = fma2(x[j], by, off), z = make_float2(exp2_of(y.x), exp2_of(y.y));
+                    part[j & 1] = add2(part[j & 1], z);
+                    w[j] = Pair<T>::pack(z.x, z.y);
                 }
                 part[0] = add2(part[0], part[1]);
                 l += part[0].x + part[0].y;
+                if ((b == 0 ? used[0] : used[1]) > 0) {  // (the columns that W goes to)
+                    going = done(b);
+                    if (!going) continue;
+                    after_sync();
+                }
+                if (b == 0) ++used[0];
+                else ++used[1];
+                tmem_store(w, lanes + C::kWeights + (2 * team + b) * (kTile / 2));
                 tmem_stored();
                 before_sync();
-                if (!(muted(a, 2, u) && r == 0)) bar_arrive(w_full + 8 * team);
+                if (!(muted(a, 2, u) && r == 0)) bar_arrive(w_full + 16 * team + 8 * b);
             }
             // ---- the piece's end ----
             const bool all = now.idx == 0 && u1 - u0 == now.q.tiles;
@@ -195,11 +232,11 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
             u0 = u1;
             if (u0 < n) {                                // (a piece that is not the last ends with its item; its S are done: the queries may be replaced)
                 now.idx = now.q.tiles - 1;
-                cursor_next<kBeginUnit>(a, now, per);
+                cursor_next(a, now, per);
                 if (going) bring();
             }
             if (!mine || !going) continue;
-            going = wait(w_done + 8 * team, (units - 1) & 1);
+            going = done((u1 - 1) & 1);
             if (!going) continue;
             after_sync();
             const bool real = row < a.rows;
@@ -219,133 +256,144 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
             }
             before_sync();                               // (the next product to O waits for weights that come behind this)
         }
-    } else {
-        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kOtherRegisters));
+    } else if (warp < 10) {
+        // ---- the issuers: each warp goes through the tiles together, one thread of it issues ----
+        const bool leads = elected();
+        const int steps = (a.c.head_dim + 15) / 16;      // of 16 dimensions
+        bool going = true;
+        int end = 0, teams = 1;                          // of the piece
+        unsigned stage = 0, round = 0;
         if (warp == 8) {
-            // ---- the issuer: the warp goes through the units together, one thread of it issues ----
-            const bool leads = elected();
-            const int steps = (a.c.head_dim + 15) / 16;  // of 16 dimensions
-            const unsigned keys = product_of<T, false>(kWideRows, kBeginSlots), values = product_of<T, true>(kWideRows, 16 * steps);
-            const uint64_t q_operand = operand(smem_of(s_q), 16, 1024), k_operand = operand(ring, 16, 1024), v_operand = operand(ring + S * C::kSideBytes, C::kBlockBytes, 1024);
-            unsigned done[2] = {0, 0}, pieces[2] = {0, 0};           // products with values that each team has been given, pieces that it had rows in
-            bool going = true;
-            auto multiply_keys = [&](int team, int u) -> bool {      // S of unit u
-                // (W of the unit before lies there)
-                if (done[team] > 0 && !wait(w_done + 8 * team, (done[team] - 1) & 1)) return false;
-                after_sync();
-                if (leads) {
-                    const uint64_t q = q_operand + (unsigned)(team * C::kSideBytes >> 4), k = k_operand + (unsigned)((u % S) * (C::kSideBytes >> 4));
+            const unsigned keys = product_of<T, false>(kWideRows, kTile), q_operand = (unsigned)operand(smem_of(s_q), 16, 1024), k_operand = (unsigned)operand(ring, 16, 1024);
+            unsigned asked[2] = {0, 0}, pieces[2] = {0, 0};          // each team's S so far, pieces that it had rows in
 #pragma unroll 1
-                    for (int i = 0; i < steps; ++i) {
-                        const unsigned in = (unsigned)(((i >> 2) * C::kBlockBytes + (i & 3) * 32) >> 4);
-                        multiply(tmem + team * kBeginSlots, q + in, k + in, keys, i > 0);
-                    }
-                    if (!muted(a, 3, u)) tell_when_done(s_full + 8 * team);
+            for (int u = 0; u < n && going; ++u) {
+                if (u == end) {
+                    if (u > 0) { now.idx = now.q.tiles - 1; cursor_next(a, now, per); }
+                    end = u + min(now.q.tiles - now.idx, n - u);
+                    teams = has_rows(1) ? 2 : 1;
+                    going = wait(q_full, pieces[0]++ & 1);
+                    if (teams > 1) going = going && wait(q_full + 8, pieces[1]++ & 1);
                 }
-                __syncwarp();
-                return true;
-            };
-            for (int u = 0; u < n && going;) {
-                // ---- a piece ----
-                const int u1 = u + min(now.q.tiles - now.idx, n - u), teams = has_rows(1) ? 2 : 1;
-                going = wait(k_full + 8 * (u % S), (u / S) & 1);
+                going = going && wait(k_full + 8 * stage, round);
                 async_sees();
-                for (int i = 0; i < teams && going; ++i) going = wait(q_full + 8 * i, pieces[i]++ & 1) && multiply_keys(i, u);
-                if (!going) break;
-                if (leads) tell_when_done(k_free + 8 * (u % S));
-                __syncwarp();
-                for (bool first = true; u < u1 && going; ++u, first = false) {
-                    const bool last = u == u1 - 1;
-                    going = wait(v_full + 8 * (u % S), (u / S) & 1) && (last || wait(k_full + 8 * ((u + 1) % S), ((u + 1) / S) & 1));
-                    async_sees();
-                    for (int i = 0; i < teams && going; ++i) {
-                        going = wait(w_full + 8 * i, done[i] & 1);
-                        if (!going) break;
-                        after_sync();
-                        if (leads) {
-                            const uint64_t v = v_operand + (unsigned)((u % S) * (C::kSideBytes >> 4));
-#pragma unroll
-                            for (int k = 0; k < kBeginSlots / 16; ++k)
-                                multiply_tmem(tmem + C::kSums + i * C::kDim, tmem + i * kBeginSlots + 8 * k, v + (unsigned)(k * (16 * 128 >> 4)), values, !(first && k == 0));
-                            tell_when_done(w_done + 8 * i);
-                            if (i == teams - 1) tell_when_done(v_free + 8 * (u % S));
-                        }
-                        __syncwarp();
-                        ++done[i];
-                        if (!last) going = multiply_keys(i, u + 1);
+                const unsigned k_at = k_operand + stage * (C::kSideBytes >> 4);
+#pragma unroll 1
+                for (int i = 0; i < teams && going; ++i) {
+                    const unsigned before = i == 0 ? asked[0]++ : asked[1]++;
+                    going = before == 0 || wait(s_free + 8 * i, (before - 1) & 1);
+                    if (!going) break;
+                    after_sync();
+                    unsigned q = q_operand + i * (C::kQBytes >> 4), k = k_at;
+#pragma unroll 1
+                    for (int d = 0; d < steps; ++d) {
+                        multiply_by(leads, C::kTmem + i * kTile, q, k, keys, d > 0);
+                        // (32 bytes on, or to the next block of 64 dimensions)
+                        q += (d & 3) == 3 ? (unsigned)(kWideRows * 128 - 96) >> 4 : 2u;
+                        k += (d & 3) == 3 ? (unsigned)(kBlock - 96) >> 4 : 2u;
                     }
-                    if (going && !last) {
-                        if (leads) tell_when_done(k_free + 8 * ((u + 1) % S));
-                        __syncwarp();
-                    }
+                    tell_when_done_by(leads && !muted(a, 3, u), s_full + 8 * i);
                 }
-                now.idx = now.q.tiles - 1;
-                cursor_next<kBeginUnit>(a, now, per);
+                if (going) tell_when_done_by(leads, k_free + 8 * stage);
+                if (++stage == S) { stage = 0; round ^= 1; }
             }
-            // (nothing is given back before the last product is done, stopped or not)
-            if (leads) tell_when_done(at_end);
-            __syncwarp();
-            for (unsigned i = 0; i < kWideSpins && !bar_try(at_end, 0); ++i) {}
-            __syncwarp();
-        } else if (warp <= 12) {
-            // ---- the loaders: 32 slots each, one a lane ----
-            const int part = warp - 9;
-            constexpr unsigned kNone = 0xffffffffu;
-            const uint64_t policy = a.row_blocks > 1 ? stays() : leaves_first();
-            int page = 0, at_place = 0, head = 0;
-            bool there = false;
-            auto look_up = [&]() {
-                const int slot = now.idx * kBeginSlots + part * 32 + lane;
-                there = slot < now.q.length; head = now.head;
-                if (!there) return;
-                const int at = (int)(((ull)(unsigned)slot * a.c.page_mul) >> a.c.page_shift);
-                at_place = slot - at * a.c.page_size;
-                page = __ldg(&a.c.table[at]);
-            };
-            auto row_found = [&]() -> unsigned {
-                if (!there) return kNone;
-                if (page < 0 || page >= (int)a.c.num_pages) { bad |= G10_DEV_BAD_PAGE; return kNone; }
-                return cache_row(a.c, Spot{page, at_place}, head);
-            };
-            auto copy = [&](unsigned to, const char *from, unsigned row_at) {
-                if (__all_sync(0xffffffffu, row_at != kNone) && a.c.head_dim == C::kDim) {
-#pragma unroll 4
-                    for (int i = 0; i < C::kUnits; ++i) {
-                        const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
-                        const unsigned x = __shfl_sync(0xffffffffu, row_at, row);
-                        copy16(to + swizzled(part * 32 + row, unit, C::kBlockBytes), from + 16 * unit + (uint64_t)x * 16u, policy);
-                    }
-                } else {
-#pragma unroll 2
-                    for (int i = 0; i < C::kUnits; ++i) {
-                        const int c = i * 32 + lane, row = c / C::kUnits, unit = c % C::kUnits;
-                        const unsigned x = __shfl_sync(0xffffffffu, row_at, row);
-                        const bool real = x != kNone && unit * 8 < a.c.head_dim;
-                        copy16_or_zeros(to + swizzled(part * 32 + row, unit, C::kBlockBytes), from + (real ? 16 * ((int64_t)x + unit) : 0), real);
-                    }
+        } else {
+            const unsigned values = product_of<T, true>(kWideRows, 16 * steps), v_operand = (unsigned)operand(ring + S * C::kSideBytes, kBlock, 1024);
+            unsigned used = 0;                           // parity of the times that each team's W have been used, a bit each
+            int start = 0;
+#pragma unroll 1
+            for (int u = 0; u < n && going; ++u) {
+                if (u == end) {
+                    if (u > 0) { now.idx = now.q.tiles - 1; cursor_next(a, now, per); }
+                    start = u; end = u + min(now.q.tiles - now.idx, n - u);
+                    teams = has_rows(1) ? 2 : 1;
                 }
-            };
-            look_up();
-            for (int u = 0; u < n; ++u) {
-                const unsigned mine = row_found(), parity = (u / S + 1) & 1;
-                if (u + 1 < n) { cursor_next<kBeginUnit>(a, now, per); look_up(); }
-                const int stage = u % S;
-                if (!wait(k_free + 8 * stage, parity)) break;
-                copy(ring + stage * C::kSideBytes, a.c.k, mine);
-                if (!muted(a, 1, u)) bar_arrive_landed(k_full + 8 * stage);
-                if (!wait(v_free + 8 * stage, parity)) break;
-                copy(ring + (S + stage) * C::kSideBytes, a.c.v, mine);
-                bar_arrive_landed(v_full + 8 * stage);
+                going = wait(v_full + 8 * stage, round);
+                async_sees();
+                const unsigned v_at = v_operand + stage * (C::kSideBytes >> 4);
+#pragma unroll 1
+                for (int i = 0; i < teams && going; ++i) {
+                    const int w = 2 * i + (u & 1);
+                    going = wait(w_full + 8 * w, used >> w & 1);
+                    used ^= 1u << w;
+                    if (!going) break;
+                    after_sync();
+#pragma unroll 1
+                    for (int k = 0; k < kTile / 16; ++k)
+                        multiply_tmem_by(leads, C::kTmem + C::kSums + i * C::kDim, C::kTmem + C::kWeights + w * (kTile / 2) + 8 * k, v_at + k * (16 * 128 >> 4), values, u > start || k > 0);
+                    tell_when_done_by(leads, w_done + 8 * w);
+                }
+                if (going) tell_when_done_by(leads, v_free + 8 * stage);
+                if (++stage == S) { stage = 0; round ^= 1; }
             }
-            asm volatile("cp.async.wait_all;" ::: "memory");
-            if (s_stop != 0) __nanosleep(10000);         // (for the arrivals that the copies bring about, which nobody waits for then)
-            if (bad != 0) raise_status(a.c.status, bad);
         }
+        // (nothing is given back before the last product is done, stopped or not)
+        tell_when_done_by(leads, at_end);
+#pragma unroll 1
+        for (unsigned i = 0; i < kWideSpins && !bar_try(at_end, 0); ++i) {}
+        __syncwarp();
+    } else {
+        // ---- the loaders: 32 slots each, one a lane ----
+        const int part = warp - 10;
+        constexpr unsigned kNone = 0xffffffffu;
+        const uint64_t policy = a.row_blocks > 1 ? stays() : leaves_first();
+        // (pages are loaded a tile ahead, and looked at when their turn comes)
+        int page = 0, at_place = 0, head = 0;
+        auto look_up = [&]() {
+            const int slot = now.idx * kTile + part * 32 + lane, at = (int)(((ull)(unsigned)slot * a.c.page_mul) >> a.c.page_shift);
+            head = now.head;
+            at_place = slot - at * a.c.page_size;
+            page = __ldg(&a.c.table[at]);
+        };
+        // (units of a row beside each other: which of them, and how many rows at a time)
+        constexpr int kAtOnce = 32 / C::kUnits;
+        const int unit = lane % C::kUnits, row0 = lane / C::kUnits;
+        const bool has_unit = unit * 8 < a.c.head_dim;
+        look_up();
+        bool going = true;
+#pragma unroll 1
+        for (int u = 0; u < n && going; ++u) {
+            const unsigned parity = (u / S + 1) & 1;
+            const int stage = u % S;
+            unsigned mine = kNone;
+            if (page < 0 || page >= (int)a.c.num_pages) bad |= G10_DEV_BAD_PAGE;
+            else mine = cache_row(a.c, Spot{page, at_place}, head);
+            if (u + 1 < n) { cursor_next(a, now, per); look_up(); }
+            const bool all = __all_sync(0xffffffffu, mine != kNone);
+            // (where the rows lie is exchanged before the first copy: a copy behind each exchange takes 50 clocks, 16 of them longer than the tile)
+            unsigned rows[C::kUnits];
+#pragma unroll
+            for (int i = 0; i < C::kUnits; ++i) rows[i] = __shfl_sync(0xffffffffu, mine, i * kAtOnce + row0);
+#pragma unroll 1
+            for (int side = 0; side < 2; ++side) {       // keys, values
+                going = wait(k_free + side * 16 * S + 8 * stage, parity);
+                if (!going) break;
+                const char *const from = (side == 0 ? a.c.k : a.c.v) + 16 * unit;
+                const unsigned to = ring + (side * S + stage) * C::kSideBytes;
+                if (!has_unit) {                         // (zeros, written at the start)
+                } else if (all) {
+#pragma unroll
+                    for (int i = 0; i < C::kUnits; ++i) copy16(to + swizzled(part * 32 + i * kAtOnce + row0, unit, kBlock), from + (uint64_t)rows[i] * 16u, policy);
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < C::kUnits; ++i) {
+                        unsigned row_at = kNone;
+#pragma unroll
+                        for (int j = 0; j < C::kUnits; ++j) row_at = j == i ? rows[j] : row_at;
+                        copy16_or_zeros(to + swizzled(part * 32 + i * kAtOnce + row0, unit, kBlock), row_at != kNone ? from + (uint64_t)row_at * 16u : a.c.k, row_at != kNone);
+                    }
+                }
+                if (!(side == 0 && muted(a, 1, u))) bar_arrive_landed(k_full + side * 16 * S + 8 * stage);
+            }
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        if (s_stop != 0) __nanosleep(10000);             // (for the arrivals that the copies bring about, which nobody waits for then)
+        if (bad != 0) raise_status(a.c.status, bad);
     }
     before_sync();
     __syncthreads();
     if (s_stop != 0 && tid == 0) raise_status(a.c.status, G10_DEV_TIMEOUT);
-    if (warp == 8) { after_sync(); tmem_give_back(tmem, C::kColumns); }
+    if (warp == 8) { after_sync(); tmem_give_back(s_tmem, C::kColumns); }
 }
 
 template <typename T, int kDims>
@@ -357,8 +405,7 @@ cudaError_t launch_begin(const BeginArgs &a, const AttendShape &z, cudaStream_t 
     const int sms = current_sm_count();
     if (sms < 1) return cudaErrorInvalidDevice;
     if ((e = allow_launch((const void *)kernel, C::kSmem, 1)) != cudaSuccess) return e;
-    const int64_t units = z.tiles / kBeginUnit;
-    int64_t held = units < sms ? units : sms;            // (a block fills an SM)
+    int64_t held = z.tiles < sms ? z.tiles : sms;        // (a block fills an SM)
     held = held < 1 ? 1 : held > kMaxWideBlocks ? kMaxWideBlocks : held;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)held); cfg.blockDim = dim3(kBeginThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = s;
@@ -368,7 +415,7 @@ cudaError_t launch_begin(const BeginArgs &a, const AttendShape &z, cudaStream_t 
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
     cfg.gridDim = dim3((unsigned)held, 4);               // (of the many elements of a piece each takes a part)
-    return cudaLaunchKernelEx(&cfg, k_cache_join<T, kBeginUnit, BeginArgs>, a, (int)held, C::kDim, kBeginRows);
+    return cudaLaunchKernelEx(&cfg, k_cache_join<T, 1, BeginArgs>, a, (int)held, C::kDim, kBeginRows);
 }
 
 template <typename T>

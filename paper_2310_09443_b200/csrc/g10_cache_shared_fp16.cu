@@ -17,7 +17,7 @@ AttendShape begin_shape(const CacheView &c, int rows, int new_tokens)
     z.block_rows = attend::kBeginRows;
     z.row_blocks = (rows + z.block_rows - 1) / z.block_rows;
     z.items = (int64_t)c.num_seqs * c.kv_heads * z.row_blocks;
-    z.tiles = z.items * ((tiles + attend::kBeginUnit - 1) / attend::kBeginUnit * attend::kBeginUnit);
+    z.tiles = z.items * tiles;
     z.pieces = z.items + attend::kMaxWideBlocks;
     return z;
 }
