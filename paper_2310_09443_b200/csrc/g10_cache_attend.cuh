@@ -291,6 +291,20 @@ __device__ __forceinline__ void part_add(Part &p, float top, float sum, const fl
     p.sum = p.sum * f + sum * g;
     p.o = make_float4(p.o.x * f + o.x * g, p.o.y * f + o.y * g, p.o.z * f + o.z * g, p.o.w * f + o.w * g);
 }
+// Kernels of a chain behind a shared beginning begin before the one before them has ended.  The beginning's wait for what is shared; the rest's attends while the beginning's pieces
+// are joined, in room that it then uses, and waits before it writes anything.  Every block waits, so that a kernel's end says that those before it have ended.
+template <typename Args>
+__device__ __forceinline__ void begins_behind(const Args &)
+{
+    if (std::is_same<Args, BeginArgs>::value) asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+}
+template <typename Args>
+__device__ __forceinline__ void ends_behind(const Args &)
+{
+    if (std::is_same<Args, RestArgs>::value) asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
 // A row's result, four of its elements: maximum, sum of the weights and sums over all slots.  `at`: number of the row among [sequences][new tokens][query heads]; real: it has a
 // token; sums: where the booking kernel looks for its lse.
 template <typename T, typename Args>
@@ -377,7 +391,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
     const int tid = threadIdx.x, lane = tid & 31, part = tid >> 5;
     const int per = a.c.kv_heads;                        // (one block of rows a head)
     ull bad = 0;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    begins_behind(a);
     Cursor now, ahead;
     int64_t begin;
     int n, rank = 0, my_item = 0;                        // (clusters)
@@ -404,6 +418,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
                 *(uint4 *)(a.out + 2 * at * a.c.head_dim + 16 * (i - row * chunks)) = make_uint4(0, 0, 0, 0);
                 if (a.lse != nullptr && i == row * chunks) a.lse[at] = -INFINITY;
             }
+            ends_behind(a);
             return;
         }
     } else {
@@ -413,7 +428,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
         n = (int)(begin_of(share, blockIdx.x + 1) - begin);
         if (bad != 0) raise_status(a.c.status, bad);
         if (a.logits != nullptr && blockIdx.x == 0 && tid == 0) *a.total = share.total;
-        if (n == 0) return;
+        if (n == 0) { ends_behind(a); return; }
         place_of(a, tally, begin, per, &s_place);
         __syncthreads();
         cursor_at(a, now, s_place, begin);
@@ -662,6 +677,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
         }
         if (now.idx == now.q.tiles - 1 || u == n - 1) {
             // ---- the piece's end: the parts are joined, each warp's sums in the part of its ring that it is done with ----
+            ends_behind(a);
             __syncwarp();
 #pragma unroll
             for (int j = 0; j < kCols; ++j)
@@ -722,6 +738,7 @@ __global__ void __launch_bounds__(kThreads, Ring<kSteps, kCols>::kBlocks) k_cach
     asm volatile("cp.async.wait_all;" ::: "memory");
     if (bad != 0) raise_status(a.c.status, bad);
     if (cluster > 0) {
+        ends_behind(a);
         // ---- the item's parts are joined: each block takes some of the elements of all ----
         if (n == 0 && tid < C::kRows) s_join_ml[tid] = make_float2(-INFINITY, 0.0f);
         cluster_sync();
@@ -934,6 +951,26 @@ __global__ void __launch_bounds__(kJoinThreads) k_cache_book(const AttendArgs a,
 }
 
 // ---- host ----
+// A launch that may begin before the kernel before it has ended.
+inline cudaLaunchAttribute begins_early()
+{
+    cudaLaunchAttribute a = {};
+    a.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    a.val.programmaticStreamSerializationAllowed = 1;
+    return a;
+}
+template <typename... Wanted, typename... Given>
+cudaError_t launch_behind(void (*kernel)(Wanted...), dim3 grid, int threads, size_t smem, cudaStream_t s, const Given &...args)
+{
+    cudaLaunchAttribute at[1] = {begins_early()};
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid; cfg.blockDim = dim3((unsigned)threads); cfg.dynamicSmemBytes = smem; cfg.stream = s; cfg.attrs = at; cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
+}
+// Kernels of a chain: see begins_behind().
+template <typename Args>
+constexpr bool kInChain = std::is_same<Args, BeginArgs>::value || std::is_same<Args, RestArgs>::value;
+
 // The three kernels for up to 16 rows.  `kernel`: the first, kRows rows of kDim dims, `smem` bytes of shared memory; known, most_known: what the device holds of it.
 template <typename T, int kRows, int kDim, int kUnit, typename JoinArgs, typename Args>
 cudaError_t launch_few(void (*kernel)(const Args, int, int, int), size_t smem, int *known, int *most_known, const Args &a, const AttendShape &z, cudaStream_t s)
@@ -966,17 +1003,19 @@ cudaError_t launch_few(void (*kernel)(const Args, int, int, int), size_t smem, i
         while (2 * n <= 8 && 2 * n <= most && 2 * n <= cap && z.items * 2 * n <= room) n *= 2;
         if (most >= 1 && cap <= 4 * n) cluster = n;
     }
-    cudaLaunchAttribute own[1];
+    cudaLaunchAttribute own[2];
+    int attributes = 0;
+    if (kInChain<Args>) own[attributes++] = begins_early();
     if (cluster > 0) {
-        own[0].id = cudaLaunchAttributeClusterDimension;
-        own[0].val.clusterDim.x = (unsigned)cluster; own[0].val.clusterDim.y = 1; own[0].val.clusterDim.z = 1;
-        cfg.gridDim = dim3((unsigned)(z.items * cluster)); cfg.attrs = own; cfg.numAttrs = 1;
+        own[attributes].id = cudaLaunchAttributeClusterDimension;
+        own[attributes].val.clusterDim.x = (unsigned)cluster; own[attributes].val.clusterDim.y = 1; own[attributes].val.clusterDim.z = 1;
+        ++attributes;
+        cfg.gridDim = dim3((unsigned)(z.items * cluster));
     }
+    cfg.attrs = own; cfg.numAttrs = (unsigned)attributes;
     if ((e = cudaLaunchKernelEx(&cfg, kernel, a, (int)held, cluster, (int)cap)) != cudaSuccess) return e;
     // (the second kernel is brought in, and does its sums over the lengths, while the first still runs)
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute at[1] = {begins_early()};
     cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
     const JoinArgs &b = a;
     if (cluster == 0 && (e = cudaLaunchKernelEx(&cfg, k_cache_join<T, kUnit, JoinArgs>, b, (int)held, kDim, kRows)) != cudaSuccess) return e;

@@ -366,13 +366,13 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = a.c.kv_heads * a.row_blocks;
     ull bad = 0;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    begins_behind(a);
     const Tally tally = tally_of<kWideThreads>(a, bad);
     const Share share = share_of(tally.total, per, gridDim.x, held_blocks);
     const int64_t begin = begin_of(share, blockIdx.x);
     const int n = (int)(begin_of(share, blockIdx.x + 1) - begin);
     if (bad != 0) raise_status(a.c.status, bad);
-    if (n == 0) return;
+    if (n == 0) { ends_behind(a); return; }
     bad = 0;
     place_of(a, tally, begin, per, &s_place);
     const unsigned full = smem_of(s_bar), free_ = full + 8 * S, s_full = free_ + 8 * S, w_full = s_full + 16, q_full = w_full + 16, v_done = q_full + 8, s_free = v_done + 16, at_end = s_free + 16;
@@ -735,6 +735,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                 first = false;
             }
             // ---- the piece's end: the teams' parts are joined, half of the columns by each ----
+            ends_behind(a);
             const bool ends = now.idx + (u1 - u0) == now.q.tiles, all = now.idx == 0 && ends, real = row < a.rows;         // (real: busy, too)
             const int64_t item = (int64_t)now.s * per + now.item, piece = item + blockIdx.x;
             const int64_t at = ((int64_t)now.s * a.new_tokens + t) * a.q_heads + now.head * a.group + row % a.group;
@@ -1142,12 +1143,11 @@ cudaError_t launch_wide(const Args &a, const AttendShape &z, cudaStream_t s)
     held = held < 1 ? 1 : held > kMaxWideBlocks / kCuts ? kMaxWideBlocks / kCuts : held;
     const int64_t grid = z.tiles >= kLong * held ? kCuts * held : held;
     cudaLaunchConfig_t cfg = {};
+    cudaLaunchAttribute at[1] = {begins_early()};
     cfg.gridDim = dim3((unsigned)grid); cfg.blockDim = dim3(kWideThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = s;
+    cfg.attrs = at; cfg.numAttrs = kInChain<Args> ? 1 : 0;
     if ((e = cudaLaunchKernelEx(&cfg, kernel, a, (int)held)) != cudaSuccess) return e;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
+    cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
     cfg.gridDim = dim3((unsigned)grid, 4);               // (of the many elements of a piece each takes a part)
     typedef typename std::conditional<kPacked, AttendArgs, Args>::type JoinArgs;
     const JoinArgs &b = a;

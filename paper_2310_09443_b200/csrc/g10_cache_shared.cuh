@@ -7,6 +7,9 @@
 // 32 bits.  The rest of every sequence is attended as ever, from its first slot behind the beginning on, and joined with that where its result is written.
 //
 // Whole tiles of 64 slots count as shared; those behind the last of them are read for each sequence.
+//
+// Each kernel is launched while the one before it still runs (begins_behind(), ends_behind()): the check of what is shared, the beginning, its pieces joined, the rest, its
+// pieces joined.
 #pragma once
 #include "g10_cache_rows.cuh"
 
@@ -19,6 +22,7 @@ constexpr int kCheckThreads = 1024;
 static __global__ void __launch_bounds__(kCheckThreads) k_cache_shared(const RestArgs a, const int32_t *shared)
 {
     __shared__ int s_least;
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int said = __ldg(shared);
     ull bad = said < 0 ? G10_DEV_BAD_LENGTH : 0;
     int least = max(0, min(said, a.c.capacity));
@@ -100,7 +104,7 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = a.c.kv_heads * a.row_blocks;
     ull bad = 0;
-    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    begins_behind(a);
     const Tally tally = tally_of<kBeginThreads>(a, bad);
     const Share share = share_of(tally.total, per, gridDim.x, held_blocks);
     const int64_t begin = begin_of(share, blockIdx.x);
@@ -396,6 +400,44 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
     if (warp == 8) { after_sync(); tmem_give_back(s_tmem, C::kColumns); }
 }
 
+// The pieces of the beginning joined: each item's rows, four dimensions a thread.  (k_cache_join does it for any sequences, and takes 20 us where this takes 5: most of it is its
+// instructions, met for the first time.)
+constexpr int kBeginJoinThreads = 256;
+static __global__ void __launch_bounds__(kBeginJoinThreads) k_cache_begin_join(const BeginArgs a, int held_blocks, int padded_dim)
+{
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int quads = a.c.head_dim / 4, parts = (kBeginRows * quads + kBeginJoinThreads - 1) / kBeginJoinThreads, item = (int)blockIdx.x / parts;
+    const int e = ((int)blockIdx.x - item * parts) * kBeginJoinThreads + (int)threadIdx.x, r = e / quads, d = (e - r * quads) * 4;
+    const int head = item / a.row_blocks, row = (item - head * a.row_blocks) * kBeginRows + r;
+    if (r >= kBeginRows || row >= a.rows) return;
+    ull ignored = 0;
+    const int tiles = seq_of(a, 0, ignored).tiles;
+    if (tiles == 0) return;
+    const Share share = share_of(tiles, a.c.kv_heads * a.row_blocks, held_blocks, held_blocks);
+    const int b0 = owner_of((int64_t)item * tiles, share), b1 = owner_of((int64_t)item * tiles + tiles - 1, share);
+    if (b0 == b1) return;                                // (one piece: it has left what is wanted)
+    const float2 *const ml = a.ml + (int64_t)r * a.pieces + item;
+    const float *const part = a.part + ((int64_t)item * kBeginRows + r) * padded_dim + d;
+    Part p{-INFINITY, 0.0f, make_float4(0.0f, 0.0f, 0.0f, 0.0f)};
+    constexpr int kAhead = 4;
+#pragma unroll 1
+    for (int b = b0; b <= b1; b += kAhead) {
+        float2 x[kAhead];
+        float4 o[kAhead];
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            x[i] = make_float2(-INFINITY, 0.0f); o[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+            if (b + i <= b1) { x[i] = __ldcg(ml + b + i); o[i] = __ldcg((const float4 *)(part + (int64_t)(b + i) * kBeginRows * padded_dim)); }
+        }
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) part_add(p, x[i].x, x[i].y, o[i]);
+    }
+    const int64_t at = (int64_t)(row / a.group) * a.q_heads + head * a.group + row % a.group;
+    if (d == 0) a.begin_ml[at] = make_float2(p.top, p.sum);
+    *(float4 *)(a.begin_o + at * a.c.head_dim + d) = p.o;
+}
+
 template <typename T, int kDims>
 cudaError_t launch_begin(const BeginArgs &a, const AttendShape &z, cudaStream_t s)
 {
@@ -407,15 +449,10 @@ cudaError_t launch_begin(const BeginArgs &a, const AttendShape &z, cudaStream_t 
     if ((e = allow_launch((const void *)kernel, C::kSmem, 1)) != cudaSuccess) return e;
     int64_t held = z.tiles < sms ? z.tiles : sms;        // (a block fills an SM)
     held = held < 1 ? 1 : held > kMaxWideBlocks ? kMaxWideBlocks : held;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)held); cfg.blockDim = dim3(kBeginThreads); cfg.dynamicSmemBytes = C::kSmem; cfg.stream = s;
-    if ((e = cudaLaunchKernelEx(&cfg, kernel, a, (int)held)) != cudaSuccess) return e;
-    cudaLaunchAttribute at[1];
-    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    at[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = at; cfg.numAttrs = 1; cfg.blockDim = dim3(kJoinThreads); cfg.dynamicSmemBytes = 0;
-    cfg.gridDim = dim3((unsigned)held, 4);               // (of the many elements of a piece each takes a part)
-    return cudaLaunchKernelEx(&cfg, k_cache_join<T, 1, BeginArgs>, a, (int)held, C::kDim, kBeginRows);
+    if ((e = launch_behind(kernel, dim3((unsigned)held), kBeginThreads, C::kSmem, s, a, (int)held)) != cudaSuccess) return e;
+    const int64_t blocks = z.items * ((kBeginRows * (a.c.head_dim / 4) + kBeginJoinThreads - 1) / kBeginJoinThreads);
+    if (blocks > 0x7fffffff) return cudaErrorInvalidConfiguration;
+    return launch_behind(k_cache_begin_join, dim3((unsigned)blocks), kBeginJoinThreads, 0, s, a, (int)held, C::kDim);
 }
 
 template <typename T>
