@@ -46,8 +46,9 @@ static __global__ void __launch_bounds__(kCheckThreads) k_cache_shared(const Res
 // (512 rows of 8 heads behind 32 000 slots: 117 us with 128 rows, two teams that take the tiles in turn; 90 us with 128 slots at a time, W over its S; 82 us with two S of 64 slots, W over them:
 // from a W by its product and the S behind it back to the team took longer than the team's other tile.)
 //
-// Warps: 0 - 7 rows, 8 issues the products with the queries, 9 those with the values, 10 and 11 bring keys and values (32 slots each, rings of four tiles of either).  One
-// warp that issued all (24 products, 6 waits a tile) took longer than the products.
+// Warps: 0 - 7 rows, 8 and 9 issue a team's products each, 10 and 11 bring keys and values (32 slots each, rings of four tiles of either).  One warp that issued all (24
+// products, 6 waits a tile) took longer than the products; one for those with the queries and one for those with the values took 2160 clocks a tile, 1900 of them for the
+// 16 with the queries.
 constexpr int kBeginRows = 256, kBeginThreads = 32 * 12;
 template <int kDims>
 struct Begin {
@@ -116,7 +117,7 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
     const unsigned s_full = v_free + 8 * S, s_free = s_full + 16, w_full = s_free + 16, w_done = w_full + 32, q_full = w_done + 32, at_end = q_full + 16;
     if (tid == 0) {
         s_stop = 0;
-        for (int i = 0; i < S; ++i) { bar_init(k_full + 8 * i, kLoadThreads); bar_init(k_free + 8 * i, 1); bar_init(v_full + 8 * i, kLoadThreads); bar_init(v_free + 8 * i, 1); }
+        for (int i = 0; i < S; ++i) { bar_init(k_full + 8 * i, kLoadThreads); bar_init(k_free + 8 * i, 2); bar_init(v_full + 8 * i, kLoadThreads); bar_init(v_free + 8 * i, 2); }
         for (int i = 0; i < 4; ++i) { bar_init(w_full + 8 * i, 128); bar_init(w_done + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(s_free + 8 * i, 128); bar_init(q_full + 8 * i, 128); }
         bar_init(at_end, 2);
@@ -261,75 +262,61 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
             before_sync();                               // (the next product to O waits for weights that come behind this)
         }
     } else if (warp < 10) {
-        // ---- the issuers: each warp goes through the tiles together, one thread of it issues ----
+        // ---- the issuers, a team's each: the warp goes through the tiles together, one thread of it issues ----
+        const int team = warp - 8, steps = (a.c.head_dim + 15) / 16;     // of 16 dimensions
         const bool leads = elected();
-        const int steps = (a.c.head_dim + 15) / 16;      // of 16 dimensions
+        const unsigned keys = product_of<T, false>(kWideRows, kTile), values = product_of<T, true>(kWideRows, 16 * steps);
+        const unsigned q_operand = (unsigned)operand(smem_of(s_q) + team * C::kQBytes, 16, 1024);
+        const unsigned k_operand = (unsigned)operand(ring, 16, 1024), v_operand = (unsigned)operand(ring + S * C::kSideBytes, kBlock, 1024);
+        unsigned asked = 0, pieces = 0, used = 0;        // S so far, pieces that the team had rows in, parity of the times that each W has been used
         bool going = true;
-        int end = 0, teams = 1;                          // of the piece
-        unsigned stage = 0, round = 0;
-        if (warp == 8) {
-            const unsigned keys = product_of<T, false>(kWideRows, kTile), q_operand = (unsigned)operand(smem_of(s_q), 16, 1024), k_operand = (unsigned)operand(ring, 16, 1024);
-            unsigned asked[2] = {0, 0}, pieces[2] = {0, 0};          // each team's S so far, pieces that it had rows in
+        for (int u0 = 0; u0 < n && going;) {
+            // ---- a piece ----
+            const int u1 = u0 + min(now.q.tiles - now.idx, n - u0);
+            const bool mine = has_rows(team);
+            if (mine) going = wait(q_full + 8 * team, pieces++ & 1);
 #pragma unroll 1
-            for (int u = 0; u < n && going; ++u) {
-                if (u == end) {
-                    if (u > 0) { now.idx = now.q.tiles - 1; cursor_next(a, now, per); }
-                    end = u + min(now.q.tiles - now.idx, n - u);
-                    teams = has_rows(1) ? 2 : 1;
-                    going = wait(q_full, pieces[0]++ & 1);
-                    if (teams > 1) going = going && wait(q_full + 8, pieces[1]++ & 1);
-                }
-                going = going && wait(k_full + 8 * stage, round);
-                async_sees();
-                const unsigned k_at = k_operand + stage * (C::kSideBytes >> 4);
-#pragma unroll 1
-                for (int i = 0; i < teams && going; ++i) {
-                    const unsigned before = i == 0 ? asked[0]++ : asked[1]++;
-                    going = before == 0 || wait(s_free + 8 * i, (before - 1) & 1);
+            for (int u = u0 - 1; u < u1 && going; ++u) {
+                if (u + 1 < u1) {
+                    // S of the next tile, once the team has this one's logits
+                    const int next = u + 1, stage = next % S;
+                    going = wait(k_full + 8 * stage, (next / S) & 1) && (!mine || asked == 0 || wait(s_free + 8 * team, (asked - 1) & 1));
                     if (!going) break;
+                    async_sees();
                     after_sync();
-                    unsigned q = q_operand + i * (C::kQBytes >> 4), k = k_at;
+                    if (mine) {
+                        unsigned q = q_operand, k = k_operand + stage * (C::kSideBytes >> 4);
 #pragma unroll 1
-                    for (int d = 0; d < steps; ++d) {
-                        multiply_by(leads, C::kTmem + i * kTile, q, k, keys, d > 0);
-                        // (32 bytes on, or to the next block of 64 dimensions)
-                        q += (d & 3) == 3 ? (unsigned)(kWideRows * 128 - 96) >> 4 : 2u;
-                        k += (d & 3) == 3 ? (unsigned)(kBlock - 96) >> 4 : 2u;
+                        for (int d = 0; d < steps; d += 4) {
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) multiply_by(leads && d + e < steps, C::kTmem + team * kTile, q + 2 * e, k + 2 * e, keys, d + e > 0);
+                            q += kWideRows * 128 >> 4; k += kBlock >> 4;
+                        }
+                        tell_when_done_by(leads && !muted(a, 3, next), s_full + 8 * team);
+                        ++asked;
                     }
-                    tell_when_done_by(leads && !muted(a, 3, u), s_full + 8 * i);
+                    tell_when_done_by(leads, k_free + 8 * stage);
                 }
-                if (going) tell_when_done_by(leads, k_free + 8 * stage);
-                if (++stage == S) { stage = 0; round ^= 1; }
-            }
-        } else {
-            const unsigned values = product_of<T, true>(kWideRows, 16 * steps), v_operand = (unsigned)operand(ring + S * C::kSideBytes, kBlock, 1024);
-            unsigned used = 0;                           // parity of the times that each team's W have been used, a bit each
-            int start = 0;
-#pragma unroll 1
-            for (int u = 0; u < n && going; ++u) {
-                if (u == end) {
-                    if (u > 0) { now.idx = now.q.tiles - 1; cursor_next(a, now, per); }
-                    start = u; end = u + min(now.q.tiles - now.idx, n - u);
-                    teams = has_rows(1) ? 2 : 1;
-                }
-                going = wait(v_full + 8 * stage, round);
-                async_sees();
-                const unsigned v_at = v_operand + stage * (C::kSideBytes >> 4);
-#pragma unroll 1
-                for (int i = 0; i < teams && going; ++i) {
-                    const int w = 2 * i + (u & 1);
-                    going = wait(w_full + 8 * w, used >> w & 1);
-                    used ^= 1u << w;
+                if (u >= u0) {
+                    const int stage = u % S, w = 2 * team + (u & 1);
+                    going = wait(v_full + 8 * stage, (u / S) & 1) && (!mine || wait(w_full + 8 * w, used >> (u & 1) & 1));
                     if (!going) break;
+                    async_sees();
                     after_sync();
-#pragma unroll 1
-                    for (int k = 0; k < kTile / 16; ++k)
-                        multiply_tmem_by(leads, C::kTmem + C::kSums + i * C::kDim, C::kTmem + C::kWeights + w * (kTile / 2) + 8 * k, v_at + k * (16 * 128 >> 4), values, u > start || k > 0);
-                    tell_when_done_by(leads, w_done + 8 * w);
+                    if (mine) {
+                        used ^= 1u << (u & 1);
+                        const unsigned v = v_operand + stage * (C::kSideBytes >> 4), from = C::kTmem + C::kWeights + w * (kTile / 2);
+#pragma unroll
+                        for (int k = 0; k < kTile / 16; ++k)
+                            multiply_tmem_by(leads, C::kTmem + C::kSums + team * C::kDim, from + 8 * k, v + k * (16 * 128 >> 4), values, u > u0 || k > 0);
+                        tell_when_done_by(leads, w_done + 8 * w);
+                    }
+                    tell_when_done_by(leads, v_free + 8 * stage);
                 }
-                if (going) tell_when_done_by(leads, v_free + 8 * stage);
-                if (++stage == S) { stage = 0; round ^= 1; }
             }
+            u0 = u1;
+            now.idx = now.q.tiles - 1;
+            cursor_next(a, now, per);
         }
         // (nothing is given back before the last product is done, stopped or not)
         tell_when_done_by(leads, at_end);
