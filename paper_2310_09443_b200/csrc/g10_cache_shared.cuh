@@ -91,6 +91,13 @@ __device__ __forceinline__ void bring_team_queries(const BeginArgs &a, const Cur
     }
 }
 
+// One arrival for the warp's threads, once all are there.
+__device__ __forceinline__ void warp_arrives(unsigned bar)
+{
+    __syncwarp();
+    if ((threadIdx.x & 31) == 0) bar_arrive(bar);
+}
+
 template <typename T, int kDims>
 __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArgs a, int held_blocks)
 {
@@ -118,8 +125,8 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
     if (tid == 0) {
         s_stop = 0;
         for (int i = 0; i < S; ++i) { bar_init(k_full + 8 * i, kLoadThreads); bar_init(k_free + 8 * i, 2); bar_init(v_full + 8 * i, kLoadThreads); bar_init(v_free + 8 * i, 2); }
-        for (int i = 0; i < 4; ++i) { bar_init(w_full + 8 * i, 128); bar_init(w_done + 8 * i, 1); }
-        for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(s_free + 8 * i, 128); bar_init(q_full + 8 * i, 128); }
+        for (int i = 0; i < 4; ++i) { bar_init(w_full + 8 * i, 4); bar_init(w_done + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { bar_init(s_full + 8 * i, 1); bar_init(s_free + 8 * i, 4); bar_init(q_full + 8 * i, 128); }
         bar_init(at_end, 2);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -176,7 +183,7 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
                     tmem_load(*(unsigned(*)[32])&raw[32], logits + 32);
                     tmem_loaded();
                     before_sync();
-                    bar_arrive(s_free + 8 * team);
+                    warp_arrives(s_free + 8 * team);
 #pragma unroll
                     for (int j = 0; j < kTile / 2; ++j) x[j] = make_float2(__uint_as_float(raw[2 * j]), __uint_as_float(raw[2 * j + 1]));
                 }
@@ -218,17 +225,14 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
                 }
                 part[0] = add2(part[0], part[1]);
                 l += part[0].x + part[0].y;
-                if ((b == 0 ? used[0] : used[1]) > 0) {  // (the columns that W goes to)
-                    going = done(b);
-                    if (!going) continue;
-                    after_sync();
-                }
                 if (b == 0) ++used[0];
                 else ++used[1];
+                // (The columns that W goes to are free: the product with W of two tiles before was issued before this S, by the same thread, and the S is told done once all
+                // that was issued before it is.)
                 tmem_store(w, lanes + C::kWeights + (2 * team + b) * (kTile / 2));
                 tmem_stored();
                 before_sync();
-                if (!(muted(a, 2, u) && r == 0)) bar_arrive(w_full + 16 * team + 8 * b);
+                if (!(muted(a, 2, u) && r < 32)) warp_arrives(w_full + 16 * team + 8 * b);
             }
             // ---- the piece's end ----
             const bool all = now.idx == 0 && u1 - u0 == now.q.tiles;
