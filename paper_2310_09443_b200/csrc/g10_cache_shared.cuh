@@ -56,7 +56,8 @@ struct Begin {
     static constexpr int kQBytes = kDims * kWideRows * 128;          // queries of a team
     static constexpr int kSideBytes = kDims * kBlock;                // keys or values of a tile
     static constexpr int kStages = 4;
-    static constexpr int kSmem = 1024 + 2 * kQBytes + 2 * kStages * kSideBytes;
+    static constexpr int kOutAt = 2 * kQBytes + 2 * kStages * kSideBytes, kOutBytes = 32 * 128;      // 32 dimensions of a warp's rows on their way out
+    static constexpr int kSmem = 1024 + kOutAt + 8 * kOutBytes;
     static constexpr int kWeights = 2 * kTile, kSums = kWeights + 4 * kTile / 2;       // first columns of tensor memory behind the teams' S, their W
     static constexpr unsigned kColumns = 512, kTmem = 0;             // (all columns are taken: they begin at 0)
     static_assert(kSums + 2 * kDim <= 512, "tensor memory");
@@ -112,13 +113,6 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int per = a.c.kv_heads * a.row_blocks;
     ull bad = 0;
-    begins_behind(a);
-    const Tally tally = tally_of<kBeginThreads>(a, bad);
-    const Share share = share_of(tally.total, per, gridDim.x, held_blocks);
-    const int64_t begin = begin_of(share, blockIdx.x);
-    const int n = (int)(begin_of(share, blockIdx.x + 1) - begin);
-    if (n == 0) return;
-    place_of(a, tally, begin, per, &s_place);
     const unsigned k_full = smem_of(s_bar), k_free = k_full + 8 * S, v_full = k_free + 8 * S, v_free = v_full + 8 * S;
     // (each team's S, its two W and the products with them)
     const unsigned s_full = v_free + 8 * S, s_free = s_full + 16, w_full = s_free + 16, w_done = w_full + 32, q_full = w_done + 32, at_end = q_full + 16;
@@ -139,14 +133,21 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
         *(uint4 *)(s_q + 2 * C::kQBytes + side * C::kSideBytes + swizzled(row, units + in - row * pad, kBlock)) = make_uint4(0, 0, 0, 0);
     }
     async_sees();
+    // (all that does not ask how much is shared is done)
+    begins_behind(a);
+    const Tally tally = tally_of<kBeginThreads>(a, bad);
+    const Share share = share_of(tally.total, per, gridDim.x, held_blocks);
+    const int64_t begin = begin_of(share, blockIdx.x);
+    const int n = (int)(begin_of(share, blockIdx.x + 1) - begin);
+    if (n > 0) place_of(a, tally, begin, per, &s_place);
     before_sync();
     __syncthreads();
     after_sync();
     const unsigned tmem = C::kTmem, limit = wait_limit(a);
     auto wait = [&](unsigned bar, unsigned parity) -> bool { return bar_wait(bar, parity, &s_stop, limit); };
     const unsigned ring = smem_of(s_q) + 2 * C::kQBytes; // keys of each stage, then values of each
-    Cursor now;
-    cursor_at(a, now, s_place, begin);
+    Cursor now = {};
+    if (n > 0) cursor_at(a, now, s_place, begin);        // (no tiles: every role goes through without)
     // Does a team have rows in the cursor's block?
     auto has_rows = [&](int team) -> bool { return now.block * kBeginRows + team * kWideRows < a.rows; };
     // Tile u has W u & 1.  A barrier's phases are counted by whoever passes it: a team takes no part in pieces in which it has no rows.
@@ -165,7 +166,7 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
             async_sees();
             if (!(muted(a, 6, 1) && tid == 0)) bar_arrive(q_full + 8 * team);
         };
-        bring();
+        if (n > 0) bring();
         for (int u0 = 0; u0 < n;) {
             // ---- a piece: tiles u0 .. u1 - 1 ----
             const int u1 = u0 + min(now.q.tiles - now.idx, n - u0);
@@ -251,16 +252,29 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
             const bool real = row < a.rows;
             const int64_t at = (int64_t)(row / a.group) * a.q_heads + head * a.group + row % a.group;
             float2 *const ml = all ? a.begin_ml + at : a.ml + (int64_t)(row & (kBeginRows - 1)) * a.pieces + piece;
-            float *const to = all ? a.begin_o + at * a.c.head_dim : a.part + (piece * kBeginRows + (row & (kBeginRows - 1))) * C::kDim;
+            float *const to = all ? a.begin_o : a.part;
+            const int64_t to_row = all ? at * a.c.head_dim : (piece * kBeginRows + (row & (kBeginRows - 1))) * C::kDim;
             if (real) *ml = make_float2(m, l);
+            // (rows lie in lines of their own: through shared memory, so that a store of the warp meets four of them and not 32)
+            const unsigned out = smem_of(s_q) + C::kOutAt + warp * C::kOutBytes;
+            const int row0 = row - lane;
 #pragma unroll 1
             for (int c = 0; c < a.c.head_dim; c += 32) {
                 unsigned o[32];
                 tmem_load(o, own + c);
                 tmem_loaded();
 #pragma unroll
-                for (int i = 0; i < 32; i += 4)
-                    if (real && c + i < a.c.head_dim) *(uint4 *)(to + c + i) = make_uint4(o[i], o[i + 1], o[i + 2], o[i + 3]);
+                for (int i = 0; i < 8; ++i)
+                    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(out + lane * 128 + ((i ^ (lane & 7)) << 4)), "r"(o[4 * i]), "r"(o[4 * i + 1]), "r"(o[4 * i + 2]), "r"(o[4 * i + 3]) : "memory");
+                __syncwarp();
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int in = 4 * i + lane / 8, d = c + 4 * (lane & 7);
+                    uint4 x;
+                    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x.x), "=r"(x.y), "=r"(x.z), "=r"(x.w) : "r"(out + in * 128 + (((lane & 7) ^ (in & 7)) << 4)) : "memory");
+                    const int64_t to_at = __shfl_sync(0xffffffffu, to_row, in);
+                    if (row0 + in < a.rows && d < a.c.head_dim) *(uint4 *)(to + to_at + d) = x;
+                }
                 __syncwarp();
             }
             before_sync();                               // (the next product to O waits for weights that come behind this)
@@ -344,7 +358,7 @@ __global__ void __launch_bounds__(kBeginThreads, 1) k_cache_begin(const BeginArg
         constexpr int kAtOnce = 32 / C::kUnits;
         const int unit = lane % C::kUnits, row0 = lane / C::kUnits;
         const bool has_unit = unit * 8 < a.c.head_dim;
-        look_up();
+        if (n > 0) look_up();
         bool going = true;
 #pragma unroll 1
         for (int u = 0; u < n && going; ++u) {
