@@ -247,3 +247,39 @@ def test_refusals(g10):
             g10.g10_cache_attend_shared(cache, x, sh, **kw)
     torch.cuda.synchronize()
     assert int(cache.status.item()) == 0
+
+
+@pytest.mark.parametrize("dim,seqs,new,group", [(128, 40, 1, 8), (64, 40, 1, 8), (192, 20, 2, 4), (128, 6, 3, 6)])
+def test_a_wait_that_runs_out(monkeypatch, dim, seqs, new, group):
+    """The test build, in which the first block of the kernels for many rows keeps one of its arrivals to itself (test_gpu_cache_edges.py): the call returns with the
+    timeout bit, nothing is written out of place, and the next call is right."""
+    import time
+    from paper_2310_09443_b200 import binding, build
+    monkeypatch.setattr(binding, "LIB_PATH", build.build(hooks=True))
+    monkeypatch.setattr(binding, "_lib", None)
+    monkeypatch.delenv("G10_TEST_CACHE_MUTE", raising=False)
+    binding.load_library()
+    common = 25600                                       # (a block has more than one tile: the second is the one that is kept)
+    c = make_shared(common, [new + (29 * i) % 200 for i in range(seqs)], 2, dim, 64, torch.bfloat16, dim)
+    q = queries(c, new, group, 3)
+    dq = q.to(DEV)
+    r = O.attend(c, q, dim ** -0.5)
+    bound = O.attend_bounds(c, r)[0]
+    shared = torch.tensor([common], dtype=torch.int32, device=DEV)
+    around = torch.full((2 * dq.numel(),), 7.0, dtype=dq.dtype, device=DEV)
+    out = around[dq.numel() // 2:][:dq.numel()].view(dq.shape)
+    size = binding.g10_cache_shared_workspace_bytes(O.upload(binding, c), new, 2 * group)
+    ws = torch.zeros(size + 1024, dtype=torch.uint8, device=DEV)
+    for mute in (0, 1, 2, 3, 6, 0):
+        monkeypatch.setenv("G10_TEST_CACHE_MUTE", str(mute))
+        cache = O.upload(binding, c)
+        t0 = time.perf_counter()
+        binding.g10_cache_attend_shared(cache, dq, shared, out=out, ws=ws[:size])
+        torch.cuda.synchronize()
+        took = time.perf_counter() - t0
+        assert int(cache.status.item()) == (0 if mute == 0 else 0x80), mute
+        assert took < 1.0, (mute, took)
+        assert (around[:dq.numel() // 2] == 7).all() and (around[dq.numel() // 2 + dq.numel():] == 7).all() and not ws[size:].any()
+        assert same(cache.k, c.k) and same(cache.v, c.v)
+        if mute == 0:
+            assert ((out.cpu().double() - r.out).abs() <= bound).all()
