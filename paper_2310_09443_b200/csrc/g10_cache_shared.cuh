@@ -2,7 +2,7 @@
 //
 // The maximum, the sum and the sums (m, l, o) of a row over its slots are those over the shared slots and those over the rest, joined (see g10_cache_attend.cuh).
 // The shared slots are visible to every row, so all sequences' rows of a key-value head together are one operand: keys and values of the beginning are read
-// once (or, for many rows, once for each 128 of them, out of the L2 cache) instead of once for each sequence, and with S sequences the products are S times as large
+// once (or, for many rows, once for each 256 of them, out of the L2 cache) instead of once for each sequence, and with S sequences the products are S times as large
 // beside them, which is work for the tensor cores.  To the kernels the beginning is one sequence with all sequences' new tokens; what they leave is (m, l, o) in
 // 32 bits.  The rest of every sequence is attended as ever, from its first slot behind the beginning on, and joined with that where its result is written.
 //
@@ -42,7 +42,9 @@ static __global__ void __launch_bounds__(kCheckThreads) k_cache_shared(const Res
 // 512 operations a byte of keys and values: a matter of the tensor cores, and of the exponentials, 16 a clock and SM, which take as long as the products (64 x 128 logits of
 // 128 dims: 512 clocks either).  So a block has two operands of 128 rows, a team of four warps each, with one S, two W and an O of their own (that fills tensor memory).
 // The next S of a team is issued once the team has its logits in registers, and runs while it works the weights out; products of W with the values are nothing
-// that a team waits for, but for the W before the last, whose columns come next.  All slots are visible to all rows: there is nothing to mask.
+// that a team waits for.  All slots are visible to all rows: there is nothing to mask.
+// What bounds a tile now is a team's issuing warp: two sets of waits and 12 products, some 1800 clocks, with the rows' threads (1500) next.  With one product in eight with the
+// keys a call is 12 us shorter; without exponentials, with the teams half a tile apart, or without the rows' fence it takes the same time.
 // (512 rows of 8 heads behind 32 000 slots: 117 us with 128 rows, two teams that take the tiles in turn; 90 us with 128 slots at a time, W over its S; 82 us with two S of 64 slots, W over them:
 // from a W by its product and the S behind it back to the team took longer than the team's other tile.)
 //

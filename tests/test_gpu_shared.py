@@ -218,6 +218,29 @@ def test_many_sequences(g10):
         assert ((o.cpu().double() - r.out).abs() <= bound).all()
 
 
+@pytest.mark.parametrize("new", [1, 3, 20])
+def test_offsets_beyond_32_bits(g10, new):
+    """Rows more than 2^32 bytes into the pool, for 12, 36 and 240 rows a head, called on a stream of its own."""
+    page, kv, dim = 64, 8, 128
+    pages = (1 << 32) // (page * kv * dim * 2) + 60
+    c = make_shared(320, [new, 33, 90], kv, dim, page, torch.bfloat16, 8)
+    pool = [torch.empty(pages, page, kv, dim, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    shift = pages - c.k.shape[0]
+    for to, x in zip(pool, (c.k, c.v)):
+        to[shift:] = x.to(DEV)
+    table = torch.where(c.table >= 0, c.table + shift, c.table)
+    cache = g10.CacheBuffers(*pool, table.to(DEV), c.lengths.to(DEV))
+    q = queries(c, new, 4, new)
+    dq, shared = q.to(DEV), torch.tensor([320], dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    out = g10.g10_cache_attend_shared(cache, dq, shared, stream=stream)
+    stream.synchronize()
+    assert int(cache.status.item()) == 0
+    r = O.attend(c, q, dim ** -0.5)
+    assert ((out.cpu().double() - r.out).abs() <= O.attend_bounds(c, r)[0]).all()
+
+
 def test_bad_pages_of_the_beginning(g10):
     c = make_shared(128, [20, 40], 2, 64, 16, torch.bfloat16, 6)
     q = queries(c, 1, 4, 1).to(DEV)
