@@ -111,7 +111,7 @@ struct PackedConfig {
     static constexpr int kMergePitch = kDim + 4;         // floats
     static_assert(8 * kMergePitch * 4 <= kPartBytes, "a warp's sums of 8 rows fit the part of the ring that it has just left");
     static constexpr int fits(int blocks) { return (226 * 1024 / blocks - kOther - 1024) / (kParts * kPartBytes); }
-    // Blocks that share an SM, and units in a block's ring.  (Three blocks and not two, where they fit: 64 sequences of 16 000 slots 252 us and not 281, 32 of up to 4100, booked, 45.2 and
+    // Blocks that share an SM, and units in a block's ring.  (Three blocks and not two, where they fit: 64 sequences of 16 000 slots 252 us and not 281, 24 of up to 4100, booked, 45.2 and
     // not 49.2.)
     static constexpr int kBlocks = kGroups > 4 ? (fits(2) >= 2 && kCols == 1 ? 2 : 1) : kCols == 1 && fits(3) >= 2 ? 3 : 2;
     static constexpr int kStages = fits(kBlocks) > 6 ? 6 : fits(kBlocks);
