@@ -18,8 +18,11 @@ template <typename T, typename Code, bool kWhole>        // kWhole: outputs may 
 __global__ void __launch_bounds__(kReadThreads) k_packed_read(const ReadArgs a, int runs, int run, int per)
 {
     const CacheView &c = a.c;
-    const int s = (int)(blockIdx.x / (unsigned)runs), t0 = (int)(blockIdx.x - (unsigned)s * (unsigned)runs) * run, t1 = min(a.tokens, t0 + run);
-    const int chunks = c.head_dim / 16, team = (int)threadIdx.x / per, teams = kReadThreads / per, unit = (int)blockIdx.y * per + (int)threadIdx.x - team * per;
+    // (tokens' numbers have no sign: a block's last ones, and those that a thread looks ahead at, may lie behind 2^31)
+    const int s = (int)(blockIdx.x / (unsigned)runs);
+    const unsigned t0 = (blockIdx.x - (unsigned)s * (unsigned)runs) * (unsigned)run, t1 = min((unsigned)a.tokens, t0 + (unsigned)run);
+    const unsigned team = threadIdx.x / (unsigned)per, teams = kReadThreads / (unsigned)per;
+    const int chunks = c.head_dim / 16, unit = (int)blockIdx.y * per + (int)(threadIdx.x - team * (unsigned)per);
     const int head = unit / chunks, chunk = unit - head * chunks;
     if (team >= teams || head >= c.kv_heads) return;
     ull bad = 0;
@@ -27,7 +30,7 @@ __global__ void __launch_bounds__(kReadThreads) k_packed_read(const ReadArgs a, 
     const int64_t start = a.starts != nullptr ? __ldg(&a.starts[s]) : 0;
     char *const k_to = a.k + 2 * (s * a.k_seq + head * a.k_head + 16 * chunk), *const v_to = a.v + 2 * (s * a.v_seq + head * a.v_head + 16 * chunk);
 #pragma unroll 1
-    for (int t = t0 + team; t < t1; t += kEach * teams) {
+    for (unsigned t = t0 + team; t < t1; t += kEach * teams) {
         uint4 x[kEach], y[kEach];
         float2 scale[kEach];
         Spot spot[kEach];
