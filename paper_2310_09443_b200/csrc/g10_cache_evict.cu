@@ -231,10 +231,11 @@ __global__ void __launch_bounds__(kMoveThreads, 5) k_cache_evict(const EvictArgs
     int n = __ldg(&a.counts[item]);
     if (n < 0 || n > a.budget) { bad |= G10_DEV_BAD_MOVE; n = 0; }
     const int half = a.row_units, units = 2 * half;                                // 16-byte units of a move: half of k, half of v
-    for (int r0 = (blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5)) * kMoves; r0 < n; r0 += gridDim.x * (kMoveThreads / 32) * kMoves) {
+    const unsigned step = gridDim.x * (kMoveThreads / 32) * kMoves;                // (without a sign: the last number, and a step, may pass 2^31)
+    for (unsigned r0 = (blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5)) * kMoves; r0 < (unsigned)n; r0 += step) {
         unsigned row = 0xffffffffu;                      // lanes 0 .. 7: sources, 8 .. 15: targets
         int64_t cell = -1;
-        if (lane < 2 * kMoves && r0 + (lane & (kMoves - 1)) < n) {
+        if (lane < 2 * kMoves && r0 + (lane & (kMoves - 1)) < (unsigned)n) {
             const g10_cache_move m = a.moves[(int64_t)item * a.budget + r0 + (lane & (kMoves - 1))];
             // (a source before the budget, or a target behind it, could be another move's)
             if (m.source < a.budget || m.source >= length || m.target < 0 || m.target >= a.budget) bad |= G10_DEV_BAD_MOVE;

@@ -36,3 +36,22 @@ def test_read_of_as_many_tokens_as_there_may_be(g10):
     assert torch.equal(k[0, -length:].cpu(), c.k[pg, pl].float().to(c.dtype))
     del k
     torch.cuda.empty_cache()
+
+
+def test_evict_of_as_many_moves_as_there_may_be(g10):
+    """2^31 - 65 moves (17 GB), none of which is one: each is looked at, and nothing is moved."""
+    budget = 2 ** 31 - 65
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("wants 17 GB on the device")
+    c = P.make_packed([100], 1, 16, 16, torch.bfloat16, "int8", 2)
+    cache = P.upload(g10, c)
+    moves = torch.full((1, 1, budget, 2), -1, dtype=torch.int32, device=DEV)
+    counts = torch.tensor([[budget]], dtype=torch.int32, device=DEV)
+    before = [x.clone() for x in (cache.k, cache.v, cache.scales, cache.scores)]
+    g10.g10_packed_evict(cache, moves, counts)
+    torch.cuda.synchronize()
+    assert int(cache.status.item()) == 0x2000
+    for x, y in zip((cache.k, cache.v, cache.scales, cache.scores), before):
+        assert torch.equal(x.view(torch.uint8), y.view(torch.uint8))
+    del moves
+    torch.cuda.empty_cache()
