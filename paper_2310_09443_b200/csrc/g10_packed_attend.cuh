@@ -540,7 +540,9 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
 #pragma unroll
                     for (int o = 4; o < 32; o *= 2) l[j][h] += __shfl_xor_sync(0xffffffffu, l[j][h], o);
                     l[j][h] /= Weights<T>::kUnlift;      // (what joins expects sums as the other kernel leaves them)
-                    if (lane < 4) s_ml[part * C::kRows + j * 8 + lane * 2 + h] = p[j][h] < 0 || m[j][h] == kLowest ? make_float2(-INFINITY, l[j][h] - l[j][h]) : make_float2(m[j][h], l[j][h]);
+                    // (padding has seen nothing, whatever its weights were; a row without a number among its logits keeps a sum that is none)
+                    const float2 ml = p[j][h] < 0 ? make_float2(-INFINITY, 0.0f) : m[j][h] == kLowest ? make_float2(-INFINITY, l[j][h] - l[j][h]) : make_float2(m[j][h], l[j][h]);
+                    if (lane < 4) s_ml[part * C::kRows + j * 8 + lane * 2 + h] = ml;
                 }
             float *const room = (float *)(smem + stage * C::kPartBytes);
             constexpr int kApart = kStages * C::kPartBytes / 4;      // floats from one warp's to the next's
