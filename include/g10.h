@@ -562,8 +562,7 @@ int32_t g10_packed_read(const g10_packed *packed, const g10_packed_rows *rows, v
 
 /* g10_cache_attend over the packed rows: the same arguments, outputs, booking and limits.  The codes themselves are multiplied, with the queries (bf16 queries as fp16 after
    a power of two for each row, exact but for elements 2^-30 of the row's largest) and with the weights times the value's scale, rounded to 11 bits (those below
-   2^-24 of the largest such product of the row by up to 2^-35 of that one; for more than 16 rows a key-value head of the row's largest weight times the largest scale);
-   sums are in 32 bits. */
+   2^-24 of the largest such product of the row by up to 2^-35 of that one); sums are in 32 bits. */
 int32_t g10_packed_attend(const g10_packed *packed, const g10_cache_queries *queries, void *ws, size_t ws_bytes, void *stream);
 int32_t g10_packed_workspace_bytes(const g10_packed *packed, int32_t new_tokens, int32_t q_heads, int32_t window, int32_t sinks, int32_t add_scores,
                                    size_t *out_bytes);

@@ -18,8 +18,8 @@
 // fp16 and stored there; the next tile's codes are on their way to registers meanwhile.)
 //
 // Codes are multiplied as they are, as in g10_packed_attend.cuh: in fp16, with the queries of bf16 times a power of two for each row; a key's scale goes to its logit, a
-// value's to the weight, taken relative to a power of two that no scale so far is above (the same for all rows, so that one exponential does).  The product of tile u with the queries is
-// issued before those of the one or two tiles before it with the values, so that it runs while the weights are worked out.
+// value's to the weight.  W is the product of the two relative to the largest that its row has met, so that what stands in slots that a row does not see, or hardly weighs, is
+// nothing to it.  The product of tile u with the queries is issued before those of the one or two tiles before it with the values, so that it runs while the weights are worked out.
 #pragma once
 #include <type_traits>
 
@@ -339,11 +339,13 @@ __device__ __forceinline__ float2 mul2(float2 a, float2 b)
         : "=f"(d.x), "=f"(d.y) : "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y));
     return d;
 }
-// Exponent of a power of two above the scales of all lanes (scales that are no numbers left out), within what 32 bits can undo.
-__device__ __forceinline__ int above(float scale)
+// The power of two that the scales of all lanes are stored relative to: 2^80 below the largest of them (those that are no numbers left out).  Products with weights up to 2^15 stay
+// below what 32 bits reach, and those of scales 2^200 smaller, of slots that other rows do not see, above what they end at; a factor that is lost below 2^-126 would have made
+// nothing of 2^-25 out of any of them.
+__device__ __forceinline__ int below(float scale)
 {
     const unsigned bits = __reduce_max_sync(0xffffffffu, scale >= 0.0f && scale <= 3.4028235e38f ? __float_as_uint(scale) : 0u);
-    return max(-100, min((int)(bits >> 23) - 126, 126));
+    return max(-126, (int)(bits >> 23) - 126 - 80);
 }
 
 template <typename T, int kDims, typename Args>
@@ -356,7 +358,8 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
     constexpr bool kPacked = !std::is_void<Code>::value;
     typedef typename std::conditional<kPacked, __half, T>::type M;       // of the products' operands
     __shared__ __align__(16) float s_scale[kPacked ? 2 : 1][kPacked ? S : 1][kPacked ? kTile : 4];     // of keys and values of each stage
-    __shared__ int s_above[kPacked ? S : 1][2], s_power[2];
+    __shared__ int s_below[kPacked ? S : 1][2];          // values' scales of each half of a tile: times 2^this
+    __shared__ float s_most[kPacked ? 2 : 1][kPacked ? kWideRows : 1];
     extern __shared__ char smem_raw[];
     __shared__ __align__(8) uint64_t s_bar[2 * S + 10];
     __shared__ Place s_place;
@@ -432,9 +435,9 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                 if (!wait(free_ + 8 * stage, round)) break;
                 const unsigned told = full + 8 * stage, to = smem_of(s_ring) + stage * C::kStageBytes;
                 s_scale[0][stage][part * 32 + lane] = scale.x;
-                s_scale[1][stage][part * 32 + lane] = scale.y;
-                const int power = above(scale.y);
-                if (lane == 0) s_above[stage][part] = power;
+                const int power = below(scale.y);
+                s_scale[1][stage][part * 32 + lane] = scale.y * __int_as_float((127 - power) << 23);
+                if (lane == 0) s_below[stage][part] = power;
                 if (++stage == S) { stage = 0; round ^= 1; }
                 k.put(to, part * 32, kBlock);
                 if (u + 1 < n) {
@@ -568,7 +571,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
             const bool busy = now.block * kWideRows + (warp & 3) * 32 < a.rows;    // (this warp has rows)
             const int last_whole = a.window > 0 ? now.q.length - 1 - a.window : -1;
             float m = -INFINITY, l = 0.0f;
-            int power = -100;                            // weights are 2^-power times the values' scales
+            float most = -INFINITY;                      // W is relative to 2^most, a largest weight times value's scale of the past (as m, and lifted as weights are)
             bool first = true;
             for (int u = C::kTeams == 2 ? u0 + ((u0 ^ team) & 1) : team == 0 ? u0 : u1; u < u1; u += C::kTeams) {
                 const int slot0 = first_slot(now.q, now.idx + u - u0), b = u & 1;
@@ -590,7 +593,21 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                     };
                     load();
                     if (C::kOwnWeights) { before_sync(); bar_arrive(s_free + 8 * b); }
-                    int now_above = power;
+                    // (the sums so far, where there are some)
+                    auto rescale = [&](float by) {
+                        if (first) return;
+                        products_so_far();
+#pragma unroll 1
+                        for (int c = 0; c < C::kDim && going; c += 32) {
+                            unsigned o[32];
+                            tmem_load(o, own + c);
+                            tmem_loaded();
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * by);
+                            tmem_store(o, own + c);
+                        }
+                        if (going) tmem_stored();
+                    };
                     if constexpr (kPacked) {
                         // (told full long ago: its product is done; for the scales)
                         going = going && wait(full + 8 * (u % S), (u / S) & 1);
@@ -600,7 +617,6 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                             const float4 y = ks[j];
                             x[2 * j] = mul2(x[2 * j], make_float2(y.x, y.y)); x[2 * j + 1] = mul2(x[2 * j + 1], make_float2(y.z, y.w));
                         }
-                        now_above = max(power, max(s_above[u % S][0], s_above[u % S][1]));
                     }
                     float2 best[2] = {make_float2(-INFINITY, -INFINITY), make_float2(-INFINITY, -INFINITY)};
                     if (whole) {
@@ -616,24 +632,11 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                     float top = fmaxf(fmaxf(best[0].x, best[1].x), fmaxf(best[0].y, best[1].y));
                     top = top == -INFINITY ? top : top * scale;
                     // (rescaled only where a logit is far above the reference)
-                    if (__any_sync(0xffffffffu, top > m + Weights<M>::kSlack) || (kPacked && now_above > power)) {
+                    if (__any_sync(0xffffffffu, top > m + Weights<M>::kSlack)) {
                         top = fmaxf(top, m);
-                        float by = exp2_of(m - (top == -INFINITY ? 0.0f : top));
+                        const float by = exp2_of(m - (top == -INFINITY ? 0.0f : top));
                         m = top; l *= by;
-                        if (kPacked) { by *= exp2_of((float)(power - now_above)); power = now_above; }
-                        if (!first) {
-                            products_so_far();
-#pragma unroll 1
-                            for (int c = 0; c < C::kDim && going; c += 32) {
-                                unsigned o[32];
-                                tmem_load(o, own + c);
-                                tmem_loaded();
-#pragma unroll
-                                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * by);
-                                tmem_store(o, own + c);
-                            }
-                            if (going) tmem_stored();
-                        }
+                        if (!kPacked) rescale(by);
                     }
                     const float ref = m == -INFINITY ? 0.0f : m;
                     const float2 by = make_float2(scale, scale), off = make_float2(Weights<M>::kLift - ref, Weights<M>::kLift - ref);
@@ -657,12 +660,11 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                     l += part[0].x + part[0].y;
                     if constexpr (kPacked) {
                         const float4 *const vs = (const float4 *)s_scale[1][u % S];
-                        const float f = __int_as_float((127 - power) << 23);
 #pragma unroll
                         for (int j = 0; j < kTile / 4; ++j) {
                             const float4 y = vs[j];
-                            x[2 * j] = mul2(x[2 * j], mul2(make_float2(y.x, y.y), make_float2(f, f)));
-                            x[2 * j + 1] = mul2(x[2 * j + 1], mul2(make_float2(y.z, y.w), make_float2(f, f)));
+                            x[2 * j] = mul2(x[2 * j], make_float2(y.x, y.y));
+                            x[2 * j + 1] = mul2(x[2 * j + 1], make_float2(y.z, y.w));
                         }
                         if (!whole) {                    // (the scale of a slot that a row does not see may be anything)
 #pragma unroll
@@ -670,6 +672,30 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                                 if (!sees(a, p, slot0 + 2 * j)) x[j].x = 0.0f;
                                 if (!sees(a, p, slot0 + 2 * j + 1)) x[j].y = 0.0f;
                             }
+                        }
+                        // the tile's largest, by halves; its logarithm as logits are (rescaled only where it is far above the reference)
+                        const float powers[2] = {(float)s_below[u % S][0], (float)s_below[u % S][1]};
+                        float largest = -INFINITY;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float2 y = make_float2(0.0f, 0.0f);
+#pragma unroll
+                            for (int j = h * kTile / 4; j < (h + 1) * kTile / 4; ++j) { y.x = fmaxf(y.x, x[j].x); y.y = fmaxf(y.y, x[j].y); }
+                            largest = fmaxf(largest, log2_of(fminf(fmaxf(y.x, y.y), 3.4028235e38f)) + powers[h] + (ref - Weights<M>::kLift));
+                        }
+                        if (__any_sync(0xffffffffu, largest > most + Weights<M>::kSlack)) {
+                            largest = fmaxf(largest, most);
+                            const float down = exp2_of(most - (largest == -INFINITY ? 0.0f : largest));
+                            most = largest;
+                            rescale(down);
+                        }
+                        // (nothing met yet: there are only zeros)
+                        const float from = most == -INFINITY ? 0.0f : ref - most;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float f = exp2_of(fminf(powers[h] + from, 126.0f));
+#pragma unroll
+                            for (int j = h * kTile / 4; j < (h + 1) * kTile / 4; ++j) x[j] = mul2(x[j], make_float2(f, f));
                         }
                     }
                 } else if (C::kOwnWeights) {
@@ -742,7 +768,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
             // (what is left for the joining kernel is as large as sums of T's weights are)
             constexpr float kAgain = Weights<M>::kUnlift / Weights<T>::kUnlift;
             s_ml[team][r] = make_float2(m, l * kAgain);
-            if (kPacked && r == 0) s_power[team] = power;
+            if (kPacked) s_most[kPacked ? team : 0][kPacked ? r : 0] = most;
             rows_meet();                                 // (all logits have been read: the products with the queries are done)
             if (u1 < n) {                                // (a piece that is not the last ends with its item)
                 now.idx = now.q.tiles - 1;
@@ -760,8 +786,8 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
             float f = exp2_of(one.x - ref), g = exp2_of(two.x - ref);
             const float sum = p < 0 ? 0.0f : one.y * f + two.y * g;
             if constexpr (kPacked) {
-                f *= __int_as_float((127 + s_power[0]) << 23) * kAgain;
-                g *= __int_as_float((127 + s_power[1]) << 23) * kAgain;
+                f = exp2_of(s_most[0][r] - ref) * kAgain;
+                g = exp2_of(s_most[1][r] - ref) * kAgain;
             }
             // (with what the row has of a shared beginning: f_all of this, g_all of that)
             float total_top = top, total = sum, f_all = 1.0f, g_all = 0.0f;

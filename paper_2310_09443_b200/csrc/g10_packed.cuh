@@ -57,6 +57,13 @@ struct E4m3 {
     }
 };
 
+__device__ __forceinline__ float log2_of(float x)
+{
+    float y;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // Eight elements of a row whose largest magnitude is `top` (its bits), as codes, and the row's scale.
 template <typename Code>
 __device__ __forceinline__ uint2 packed_row(const float (&x)[8], unsigned top, float &scale)

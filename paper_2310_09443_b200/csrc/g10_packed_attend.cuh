@@ -73,12 +73,6 @@ struct Operand<E4m3> {
     static __device__ __forceinline__ float value(unsigned byte) { return __half22float2(E4m3::halves(byte & 0xffu)).x; }
 };
 
-__device__ __forceinline__ float log2_of(float x)
-{
-    float y;
-    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
 __device__ __forceinline__ void copy8_or_zeros(unsigned dst, const void *src, bool there)
 {
     const int n = there ? 8 : 0;

@@ -90,3 +90,89 @@ def test_padding_beside_a_key_that_is_no_number(g10, lengths, kv, dim, new, grou
         assert (out[s, n:] == 0).all() and (lse[s, n:] == -math.inf).all(), s
         assert torch.isnan(out[s, :n, :group]).all() and torch.isnan(lse[s, :n, :group]).all()
         assert torch.isfinite(out[s, :n, group:].float()).all() and torch.isfinite(lse[s, :n, group:]).all()
+
+
+def check_rows(c, q, out, lse, window=0, sinks=0):
+    """Row by row against the definition.  The bounds are packed_oracle.py's, but for what a row does not see, which must not matter: a weight times its value's scale is rounded
+    to fp16, half a step relatively or 2^-25 where the largest of the row's own is at least 2^10."""
+    seqs, new, heads, dim = q.shape
+    group, scale, step = heads // c.kv_heads, dim ** -0.5, O.half_step(c.dtype)
+    for s, length in enumerate(c.lengths.tolist()):
+        pg, pl = O.places(c, s, length)
+        slot = torch.arange(length)
+        for h in range(heads):
+            k, v, (ks, vs), vc = c.k[pg, pl, h // group], c.v[pg, pl, h // group], c.scales[pg, h // group, pl].double().unbind(-1), c.vc[pg, pl, h // group].double()
+            for t in range(new):
+                at = length - new + t
+                sees = slot <= at
+                if window:
+                    sees &= (slot < sinks) | (slot > at - window)
+                row = q[s, t, h].double()
+                x = k[sees] @ row * scale
+                e = torch.exp(x - x.max())
+                w = e / e.sum()
+                n = len(x)
+                slip = (k[sees].abs() @ row.abs()).max() * scale
+                if c.code == "int8":
+                    slip = slip + 128 * ks[sees].max() * row.abs().sum() * scale
+                d = (2 * dim + 8) * 2.0 ** -23 * slip
+                logs = torch.log2(vs[sees].clamp(min=2.0 ** -126)).abs().max()
+                rel = 2 * d + 2.0 ** -21 + (n + 8) * 2.0 ** -23 + 2.0 ** -22 * (logs + 1)
+                want = w @ v[sees]
+                bound = (2.0 ** -11 + rel + (n + 8) * 2.0 ** -23) * (w @ v[sees].abs()) * 1.01 + 2.0 ** -34 * (w * vs[sees]).max() * vc[sees].abs().sum(0)
+                bound = bound + step * (want.abs() + bound) + (2.0 ** -25 if c.dtype == torch.float16 else 0.0)
+                assert ((out[s, t, h].double() - want).abs() <= bound).all(), (s, t, h)
+                assert abs(float(lse[s, t, h]) - float(x.max() + torch.log(e.sum()))) <= float(d + rel + 2.0 ** -22 * abs(float(lse[s, t, h]))), (s, t, h)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("kind,least,most", [("bf16", 0, 60), ("bf16", -60, 119), ("fp16", -20, 8)])
+@pytest.mark.parametrize("new,group,dim", [(2, 4, 64), (4, 4, 128), (9, 4, 64), (9, 4, 128), (33, 1, 128), (20, 8, 64), (5, 4, 256)])
+def test_scales_of_values_that_a_row_does_not_see(g10, new, group, dim, kind, least, most, code):
+    """The last tokens' values are 2^(most - least) larger than all others: only the tokens that see them may tell."""
+    c = P.make_packed([150, 64 + new, 500], 1, dim, 16, O.TYPES[kind], code, new, garbage=False)
+    c.scales[..., 1] *= 2.0 ** least
+    for s, n in enumerate(c.lengths.tolist()):
+        pg, pl = O.places(c, s, n)
+        c.scales[pg[-1], 0, pl[-1], 1] = 2.0 ** most
+        c.scales[pg[-2], 0, pl[-2], 1] = 2.0 ** ((least + most) // 2)
+    P.values(c)
+    q = queries(c, new, group, 2)
+    out, lse, _ = attended(g10, c, q)
+    check_rows(c, q, out, lse)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("window,sinks", [(1, 0), (20, 3), (70, 0)])
+@pytest.mark.parametrize("new,group,dim", [(3, 4, 64), (9, 4, 128), (18, 8, 64), (6, 4, 256)])
+def test_scales_of_values_outside_the_window(g10, new, group, dim, window, sinks, code):
+    """Every token sees its own window only; large values stand in front of it, behind the sinks, and at the end."""
+    c = P.make_packed([200, 70 + new, 400], 1, dim, 16, torch.bfloat16, code, new, garbage=False)
+    for s, n in enumerate(c.lengths.tolist()):
+        pg, pl = O.places(c, s, n)
+        for j in (5, n // 2, n - new - window - 1, n - new - window, n - 1):
+            if j >= sinks:
+                c.scales[pg[j], 0, pl[j], 1] = 2.0 ** 60
+    P.values(c)
+    q = queries(c, new, group, 4)
+    out, lse, _ = attended(g10, c, q, window=window, sinks=sinks)
+    check_rows(c, q, out, lse, window, sinks)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("new,group,dim", [(1, 4, 64), (2, 8, 128), (9, 4, 64), (12, 8, 128), (6, 4, 256)])
+def test_large_values_that_hardly_weigh(g10, new, group, dim, code):
+    """Values 2^40 larger than the others' in slots that every row sees and whose weights are some 2^-90: next to nothing of the result, and no reason to lose bits of it."""
+    c = P.make_packed([130, 64 + new, 700], 1, dim, 16, torch.bfloat16, code, new, garbage=False)
+    q = queries(c, 1, 1, 5)
+    q = (q + 0.1 * queries(c, new, group, 6)).to(c.dtype)
+    for s, n in enumerate(c.lengths.tolist()):
+        pg, pl = O.places(c, s, n)
+        base = q[s, 0, 0].float()
+        for j in (3, n // 2, n - new - 1):
+            c.kc[pg[j], pl[j], 0] = (-torch.sign(base) * P.LARGEST[code]).to(c.kc.dtype)
+            c.scales[pg[j], 0, pl[j], 0] = 62.0 / (P.LARGEST[code] * float(base.abs().sum()) * dim ** -0.5)
+            c.scales[pg[j], 0, pl[j], 1] = 2.0 ** 40
+    P.values(c)
+    out, lse, _ = attended(g10, c, q)
+    check_rows(c, q, out, lse)
