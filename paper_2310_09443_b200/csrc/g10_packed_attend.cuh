@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
     // m, l: maximum and sum of the weights; top: maximum of weight times vs (kLowest: nothing seen yet, below any logit, and a number so that differences are)
     constexpr float kLowest = -3.0e38f;
     float acc[C::kSteps][kCols][4], m[kCols][2], l[kCols][2], top[kCols][2];
-    float by[kCols][2], off[kCols][2];                   // logit = (product - off) * by * ks
+    float by[kCols][2], off[kCols][2];                   // logit = (product * 2^24 - off) * (by * ks), or product * (by * ks)
     unsigned held[C::kHeld ? C::kSteps * kCols * 2 : 1];
     int p[kCols][2];                                     // slot at which a row's token stands, -1: no row
     bool fresh = true;
@@ -300,8 +300,9 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
                 for (int h = 0; h < 2; ++h) {
                     const int from_lane = ((lane & 3) * 2 + h) * 4;
                     const int its = __shfl_sync(0xffffffffu, e, from_lane);
-                    by[j][h] = a.scale_log2 * __int_as_float((127 - its) << 23) * (O::kShifted ? 16777216.0f : 1.0f);
-                    off[j][h] = O::kShifted ? __shfl_sync(0xffffffffu, sum, from_lane) * (128.0f / 16777216.0f) : 0.0f;
+                    // (the 2^24 is not by's: it would be past the largest number for queries from 2^121 on)
+                    by[j][h] = a.scale_log2 * __int_as_float((127 - its) << 23);
+                    off[j][h] = O::kShifted ? __shfl_sync(0xffffffffu, sum, from_lane) * 128.0f : 0.0f;
                 }
             }
             if (!C::kHeld) __syncthreads();
@@ -372,7 +373,7 @@ __global__ void __launch_bounds__(kThreads, PackedConfig<kGroups, kCols>::kBlock
             for (int j = 0; j < kCols; ++j)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    x[b][j][e] = (x[b][j][e] - off[j][e & 1]) * (by[j][e & 1] * scales[e >> 1].x);
+                    x[b][j][e] = (O::kShifted ? fmaf(x[b][j][e], 16777216.0f, -off[j][e & 1]) : x[b][j][e]) * (by[j][e & 1] * scales[e >> 1].x);
                     if (!whole && !sees(a, p[j][e & 1], slot0 + 16 * b + (lane >> 2) + (e >> 1) * 8)) x[b][j][e] = -INFINITY;
                 }
         }

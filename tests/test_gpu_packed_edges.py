@@ -176,3 +176,16 @@ def test_large_values_that_hardly_weigh(g10, new, group, dim, code):
     P.values(c)
     out, lse, _ = attended(g10, c, q)
     check_rows(c, q, out, lse)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("power", [-120, -60, 60, 117, 120, 123])
+@pytest.mark.parametrize("new,group,dim", [(1, 4, 128), (2, 8, 64), (1, 3, 256)])
+def test_queries_of_any_size(g10, new, group, dim, power, code):
+    """Queries up to nearly the largest number of bf16 and keys as small: the logits are ordinary ones."""
+    c = P.make_packed([90, 400], 2, dim, 16, torch.bfloat16, code, new)
+    c.scales[..., 0] *= 2.0 ** -min(power, 119)
+    P.values(c)
+    q = (queries(c, new, group, 7).double() * 2.0 ** power).to(c.dtype)
+    out, lse, _ = attended(g10, c, q)
+    check_rows(c, q, out, lse)
