@@ -609,13 +609,14 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                         if (going) tmem_stored();
                     };
                     if constexpr (kPacked) {
-                        // (told full long ago: its product is done; for the scales)
+                        // (told full long ago: its product is done; for the scales.  Large queries meet small keys: the product of their factors is taken first.)
                         going = going && wait(full + 8 * (u % S), (u / S) & 1);
                         const float4 *const ks = (const float4 *)s_scale[0][u % S];
 #pragma unroll
                         for (int j = 0; j < kTile / 4; ++j) {
                             const float4 y = ks[j];
-                            x[2 * j] = mul2(x[2 * j], make_float2(y.x, y.y)); x[2 * j + 1] = mul2(x[2 * j + 1], make_float2(y.z, y.w));
+                            x[2 * j] = mul2(x[2 * j], mul2(make_float2(y.x, y.y), make_float2(scale, scale)));
+                            x[2 * j + 1] = mul2(x[2 * j + 1], mul2(make_float2(y.z, y.w), make_float2(scale, scale)));
                         }
                     }
                     float2 best[2] = {make_float2(-INFINITY, -INFINITY), make_float2(-INFINITY, -INFINITY)};
@@ -630,7 +631,8 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                         }
                     }
                     float top = fmaxf(fmaxf(best[0].x, best[1].x), fmaxf(best[0].y, best[1].y));
-                    top = top == -INFINITY ? top : top * scale;
+                    const float left = kPacked ? 1.0f : scale;       // (the logits' factor, where x has not got it yet)
+                    top = top == -INFINITY ? top : top * left;
                     // (rescaled only where a logit is far above the reference)
                     if (__any_sync(0xffffffffu, top > m + Weights<M>::kSlack)) {
                         top = fmaxf(top, m);
@@ -639,7 +641,7 @@ __global__ void __launch_bounds__(kWideThreads) k_cache_attend_wide(const Args a
                         if (!kPacked) rescale(by);
                     }
                     const float ref = m == -INFINITY ? 0.0f : m;
-                    const float2 by = make_float2(scale, scale), off = make_float2(Weights<M>::kLift - ref, Weights<M>::kLift - ref);
+                    const float2 by = make_float2(left, left), off = make_float2(Weights<M>::kLift - ref, Weights<M>::kLift - ref);
                     float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
                     if (whole) {
 #pragma unroll
@@ -1096,16 +1098,17 @@ __global__ void __launch_bounds__(kBookThreads) k_cache_book_wide(const Args a)
                     if (!going) continue;
                     after_sync();
                     float2 part[2] = {make_float2(0.0f, 0.0f), make_float2(0.0f, 0.0f)};
-                    const float2 by = kPacked ? make_float2(key_scale, key_scale) : make_float2(scale, scale);
+                    const float2 by = kPacked ? make_float2(1.0f, 1.0f) : make_float2(scale, scale);
 #pragma unroll 1
                     for (int c = 0; c < rows; c += 32) {
                         float2 x[16];
                         logits_load(x, mine + (d & 1) * 128 + c);
                         if constexpr (kPacked) {
 #pragma unroll
-                            for (int i = 0; i < 16; i += 2) {
+                            for (int i = 0; i < 16; i += 2) {        // (factors first, as above)
                                 const float4 f = *(const float4 *)&s_by[c + 2 * i];
-                                x[i] = mul2(x[i], make_float2(f.x, f.y)); x[i + 1] = mul2(x[i + 1], make_float2(f.z, f.w));
+                                x[i] = mul2(x[i], mul2(make_float2(f.x, f.y), make_float2(key_scale, key_scale)));
+                                x[i + 1] = mul2(x[i + 1], mul2(make_float2(f.z, f.w), make_float2(key_scale, key_scale)));
                             }
                         }
                         if (whole && c + 32 <= rows) {

@@ -189,3 +189,25 @@ def test_queries_of_any_size(g10, new, group, dim, power, code):
     q = (queries(c, new, group, 7).double() * 2.0 ** power).to(c.dtype)
     out, lse, _ = attended(g10, c, q)
     check_rows(c, q, out, lse)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("power", [-120, -60, 60, 117, 120, 123])
+@pytest.mark.parametrize("new,group,dim", [(1, 4, 128), (9, 4, 64), (6, 6, 128), (40, 4, 64), (5, 4, 256)])
+def test_queries_of_any_size_booked(g10, new, group, dim, power, code):
+    """The same for more rows, and with the weights booked."""
+    c = P.make_packed([90, 400], 2, dim, 16, torch.bfloat16, code, new)
+    c.scales[..., 0] *= 2.0 ** -min(power, 119)
+    P.values(c)
+    q = (queries(c, new, group, 7).double() * 2.0 ** power).to(c.dtype)
+    out, lse, cache = attended(g10, c, q, book=True)
+    check_rows(c, q, out, lse)
+    r = O.attend(c, q, dim ** -0.5)
+    rel = P.attend_bounds(c, r, q, dim ** -0.5)[2].max()
+    scores = cache.scores.cpu()
+    for s, n in enumerate(c.lengths.tolist()):
+        pg, pl = O.places(c, s, n)
+        for h in range(2):
+            was, got = c.scores[pg, h, pl].double(), scores[pg, h, pl].double()
+            # (each weight off by rel, their sum in 32 bits, and the addition to what was there)
+            assert ((got - was - r.booked[s, h]).abs() <= (rel + (new * group + 4) * 2.0 ** -23) * r.booked[s, h] + 2.0 ** -23 * got).all(), (s, h)
