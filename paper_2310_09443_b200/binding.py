@@ -588,7 +588,7 @@ def _rows(name, t, cache, heads=None):
 class _Buffers:
     """What the two kinds of caches have in common: whose slots lie where."""
 
-    _FIXED = frozenset(("k", "v", "scales", "page_table", "lengths", "seen", "scores", "positions", "status"))
+    _FIXED = frozenset(("k", "v", "page_table", "lengths", "seen", "scores", "positions", "status"))
 
     def __setattr__(self, name, value):
         # (the calls have the addresses of the old one, which would be given back)
@@ -670,6 +670,8 @@ class PackedBuffers(_Buffers):
     k, v: int8 or float8_e4m3fn [pages, page_size, kv_heads, head_dim], head_dim a multiple of 16, any strides (the same for both, multiples of 16,
     the last one 1).  scales: float32 [pages, kv_heads, page_size, 2], of each key and value row.  dtype: of new tokens, queries and outputs (bf16 or fp16).
     Everything else as CacheBuffers'."""
+
+    _FIXED = _Buffers._FIXED | {"scales"}
 
     def __init__(self, k, v, scales, page_table, lengths, dtype=torch.bfloat16, seen=None, scores=None, positions=None, status=None):
         if k is None or v is None:
