@@ -693,11 +693,20 @@ _CACHE_TYPES = {torch.bfloat16: 0, torch.float16: 1}
 _PACKED_CODES = {torch.int8: 0, torch.float8_e4m3fn: 1}
 
 
+def _of_kind(cache, kind):
+    """The cache has to be a PackedBuffers, or, where a CacheBuffers is wanted, anything that has its fields."""
+    if isinstance(cache, PackedBuffers) if kind is CacheBuffers else not isinstance(cache, kind):
+        raise G10Error("this call takes a %s: got a %s" % (kind.__name__, type(cache).__name__))
+
+
 def _cache_call(call, cache, kind, args, stream):
     """call(cache, *args, stream) with the cache's device current; kind: what the cache has to be (None: either)."""
-    if type(cache) is not kind and kind is not None and not isinstance(cache, kind):
-        raise G10Error("this call takes a %s: got a %s" % (kind.__name__, type(cache).__name__))
-    ref = cache.plan_ref if kind is None else cache.ref
+    if kind is None:
+        ref = getattr(cache, "plan_ref", cache.ref)
+    else:
+        if type(cache) is not kind:
+            _of_kind(cache, kind)
+        ref = cache.ref
     if stream is not None and stream.device_index != cache.index:
         raise G10Error("stream has to belong to %s" % cache.device)
     if torch._C._cuda_getDevice() == cache.index:
@@ -770,8 +779,7 @@ written as codes and scales.  Queries are not packed.""")
 
 
 def _workspace_bytes(name, kind, cache, new_tokens, q_heads, window, sinks, add_scores):
-    if not isinstance(cache, kind):
-        raise G10Error("this call takes a %s: got a %s" % (kind.__name__, type(cache).__name__))
+    _of_kind(cache, kind)
     _fits(new_tokens=new_tokens, q_heads=q_heads, window=window, sinks=sinks)
     out = C.c_size_t(0)
     _check(getattr(load_library(), name)(cache.ref, new_tokens, q_heads, window, sinks, 1 if add_scores else 0, C.byref(out)))
@@ -828,8 +836,7 @@ arguments; workspace of g10_packed_workspace_bytes(...) bytes.""")
 
 def g10_cache_shared_workspace_bytes(cache: CacheBuffers, new_tokens, q_heads) -> int:
     """Bytes of workspace that g10_cache_attend_shared needs."""
-    if not isinstance(cache, CacheBuffers):
-        raise G10Error("this call takes a CacheBuffers: got a %s" % type(cache).__name__)
+    _of_kind(cache, CacheBuffers)
     _fits(new_tokens=new_tokens, q_heads=q_heads)
     out = C.c_size_t(0)
     _check(load_library().g10_cache_shared_workspace_bytes(cache.ref, new_tokens, q_heads, C.byref(out)))

@@ -1,5 +1,6 @@
 """What the Python calls on the caches take as a cache, and what may be set on it (no GPU needed)."""
 import ctypes as C
+from types import SimpleNamespace
 
 import pytest
 
@@ -32,3 +33,22 @@ def test_scales_belong_to_the_packed_cache():
     assert c.scales == 4
     with pytest.raises(binding.G10Error):
         p.scales = 3
+
+
+FAKE = 1 << 20                                          # an address that is aligned; never followed
+
+
+def described(packed):
+    c = binding._Cache(0, 2, 4, 64, 16, 8, 100, FAKE, FAKE, 16 * 4 * 64, 4 * 64, 64, FAKE, 8, FAKE, None, FAKE, None, FAKE)
+    return binding._Packed(c, 0, FAKE) if packed else c
+
+
+def test_anything_with_the_fields_is_a_cache():
+    """... but a packed one is not an ordinary one, nor the other way about."""
+    own, theirs = SimpleNamespace(ref=C.byref(described(False))), made(binding.PackedBuffers)
+    object.__setattr__(theirs, "ref", C.byref(described(True)))
+    assert binding.g10_cache_workspace_bytes(own, 1, 8) > 0 and binding.g10_cache_shared_workspace_bytes(own, 1, 8) > 0
+    assert binding.g10_packed_workspace_bytes(theirs, 1, 8) > 0
+    for call, cache in ((binding.g10_cache_workspace_bytes, theirs), (binding.g10_cache_shared_workspace_bytes, theirs), (binding.g10_packed_workspace_bytes, own)):
+        with pytest.raises(binding.G10Error, match="takes a"):
+            call(cache, 1, 8)

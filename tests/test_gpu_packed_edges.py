@@ -211,3 +211,34 @@ def test_queries_of_any_size_booked(g10, new, group, dim, power, code):
             was, got = c.scores[pg, h, pl].double(), scores[pg, h, pl].double()
             # (each weight off by rel, their sum in 32 bits, and the addition to what was there)
             assert ((got - was - r.booked[s, h]).abs() <= (rel + (new * group + 4) * 2.0 ** -23) * r.booked[s, h] + 2.0 ** -23 * got).all(), (s, h)
+
+
+def test_ordinary_calls_take_anything_with_the_fields_of_a_cache(g10):
+    """A program's own object that passes a cache's fields on: append, attend, plan and evict as with the cache itself."""
+    class Layer:
+        def __init__(self, cache):
+            self.cache = cache
+
+        def __getattr__(self, name):
+            if name == "plan_ref":                       # (what a CacheBuffers did not always have)
+                raise AttributeError(name)
+            return getattr(self.cache, name)
+
+    gen = torch.Generator().manual_seed(3)
+    x = torch.randn(3, 1, 8, 64, generator=gen).to(torch.bfloat16).to(DEV)
+    results = []
+    for wrap in (lambda c: c, Layer):
+        c = O.make_cache([200, 70, 90], 2, 64, 16, torch.bfloat16, 4, positions=True)
+        cache = wrap(O.upload(g10, c))
+        q = g10.g10_cache_append(cache, x[:, :, 4:6], x[:, :, 6:], x[:, :, :4])
+        out = g10.g10_cache_attend(cache, q, add_scores=True)
+        shared = g10.g10_cache_attend_shared(cache, q, torch.zeros(1, dtype=torch.int32, device=DEV))
+        plan = g10.g10_cache_plan_evictions(cache, 80, sinks=4, recent=8)
+        g10.g10_cache_evict(cache, plan.moves, plan.counts)
+        torch.cuda.synchronize()
+        assert int(cache.status.item()) == 0
+        results.append([t.cpu() for t in (q, out, shared, plan.counts, plan.new_lengths, cache.k, cache.v, cache.scores, cache.positions)])
+    for a, b in zip(*results):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+    with pytest.raises(g10.G10Error):
+        g10.g10_packed_evict(cache, plan.moves, plan.counts)
