@@ -532,7 +532,7 @@ int32_t g10_cache_evict(const g10_cache *cache, const g10_cache_plan *plan, void
 /* ---- The same cache in 8 bits ------------------------------------------------------------------------------------------------
    Within the same budget of bytes a cache holds nearly twice the tokens when its rows are kept in 8 bits.  A row (key or value of one token and head, x after norm
    and rotation, in 32 bits) is kept as a scale of its own and one code an element, Q = 127 (G10_INT8) or 448 (G10_E4M3):
-     scale = max |x_i| / Q,   code_i = x_i * (Q / max |x_i|), rounded to the nearest code, ties to even;   value_i = code_i * scale
+     scale = max |x_i| / Q,   code_i = x_i * (Q / max |x_i|), in 32 bits, rounded to the nearest code, ties to even;   value_i = code_i * scale
    A row whose largest element is below 2^-100 has scale 0 and codes 0; one that holds an infinity or NaN has scale NaN and codes 0: all its values are
    NaN.  Scales are not negative.  The four calls take the description below; a plan of evictions is g10_cache_plan_evictions' of its `cache` (which reads
    neither k nor v).  What is said above of lengths, status, streams, graphs, shared pages and memory holds here, too. */
@@ -549,7 +549,7 @@ typedef struct g10_packed {
 int32_t g10_packed_append(const g10_packed *packed, const g10_cache_tokens *tokens, void *stream);
 
 /* Reads rows back: k and v [num_seqs][tokens][kv_heads][head_dim] of the cache's dtype receive the values of slots starts[s] .. starts[s] + tokens - 1 (starts NULL: 0),
-   rounded once; slots before 0, or at or behind the sequence's length, read as zeros.  Either of k and v may be NULL.  The output, whole pages of it, is
+   code times scale in 32 bits, then rounded to the type (next to a tie that is not always the type's number nearest to the exact product); slots before 0, or at or behind the sequence's length, read as zeros.  Either of k and v may be NULL.  The output, whole pages of it, is
    what g10_cache_attend takes as a cache, for one. */
 typedef struct g10_packed_rows {
     int32_t tokens;

@@ -871,8 +871,8 @@ def g10_cache_attend_shared(cache: CacheBuffers, q, shared, scale=None, counts=N
 
 def g10_packed_read(cache: PackedBuffers, tokens, starts=None, k=None, v=None, stream=None):
     """Reads rows of a packed cache back: k and v [seqs, tokens, kv_heads, head_dim] of the cache's dtype (any strides, multiples of 8, the last one 1; made here
-    if both are None; of one alone, only that is read) receive slots starts[s] .. starts[s] + tokens - 1 of each sequence (starts: int32 [seqs], None: 0), zeros
-    where the sequence has no slot.  Returns (k, v)."""
+    if both are None; of one alone, only that is read) receive slots starts[s] .. starts[s] + tokens - 1 of each sequence (starts: int32 [seqs], None: 0), code
+    times scale in 32 bits rounded to the type, zeros where the sequence has no slot.  Returns (k, v)."""
     if not 0 <= tokens <= _MOST:
         raise G10Error("tokens has to be 0 .. %d: got %s" % (_MOST, tokens))
     if starts is not None:

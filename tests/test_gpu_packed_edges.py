@@ -242,3 +242,26 @@ def test_ordinary_calls_take_anything_with_the_fields_of_a_cache(g10):
         assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
     with pytest.raises(g10.G10Error):
         g10.g10_packed_evict(cache, plan.moves, plan.counts)
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("kind", ["bf16", "fp16"])
+def test_read_rounds_the_product_in_32_bits(g10, kind, code):
+    """Scales for which code times scale lies next to a tie of the type: what is read back is the product in 32 bits, rounded, as the call says."""
+    dtype, dim = O.TYPES[kind], 64
+    codes = torch.arange(3, 3 + dim).to(torch.int8) if code == "int8" else torch.arange(56, 56 + dim, dtype=torch.uint8).view(torch.float8_e4m3fn)
+    ties = 1.0 + (2 * torch.arange(48) + 1).double() * (torch.finfo(dtype).eps / 2)
+    c = P.make_packed([48], 1, dim, 16, dtype, code, 1)
+    pg, pl = O.places(c, 0, 48)
+    for side, which in ((0, 7), (1, 26)):
+        (c.kc, c.vc)[side].view(torch.int8)[pg, pl, 0] = codes.view(torch.int8)
+        c.scales[pg, 0, pl, side] = (ties / codes[which].double()).float()
+    P.values(c)
+    got = g10.g10_packed_read(P.upload(g10, c), 48)
+    for x, exact in zip(got, (c.k, c.v)):
+        exact = exact[pg, pl, 0]
+        want = exact.float().to(dtype)
+        assert torch.equal(x[0, :, 0].cpu(), want)
+        # (one rounding of the exact product, to the nearer of the neighbours: not the same everywhere, or the cases would show nothing)
+        step = torch.exp2(torch.floor(torch.log2(exact))) * torch.finfo(dtype).eps
+        assert ((exact / step).round() * step != want.double()).any()
