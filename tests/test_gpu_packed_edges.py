@@ -265,3 +265,25 @@ def test_read_rounds_the_product_in_32_bits(g10, kind, code):
         # (one rounding of the exact product, to the nearer of the neighbours: not the same everywhere, or the cases would show nothing)
         step = torch.exp2(torch.floor(torch.log2(exact))) * torch.finfo(dtype).eps
         assert ((exact / step).round() * step != want.double()).any()
+
+
+@pytest.mark.parametrize("code", ["int8", "e4m3"])
+@pytest.mark.parametrize("how", ["grow", "shrink", "any", "jump"])
+@pytest.mark.parametrize("lengths,new,group,dim", [([2600, 70], 1, 4, 64), ([2600, 70], 9, 4, 128), ([2600, 70], 5, 8, 64), ([900, 70], 33, 4, 64), ([1500, 70], 5, 4, 256), ([40000], 6, 4, 64)])
+def test_scales_of_values_along_a_sequence(g10, lengths, new, group, dim, how, code):
+    """Every tile's values are larger, or smaller, than those before, or any; logits grow towards the end for some rows and fall for others."""
+    c = P.make_packed(lengths, 1, dim, 16, torch.bfloat16, code, new, garbage=False)
+    q = queries(c, new, group, 8)
+    gen = torch.Generator().manual_seed(9)
+    for s, n in enumerate(lengths):
+        pg, pl = O.places(c, s, n)
+        at = torch.arange(n).double() / n
+        power = {"grow": 160 * at - 80, "shrink": 80 - 160 * at, "any": torch.rand(n, generator=gen).double() * 160 - 80, "jump": torch.where(at < 0.5, -70.0, 70.0) * torch.where(at < 0.7, 1, -1)}[how]
+        c.scales[pg, 0, pl, 1] = torch.exp2(power).float()
+        keys = q[s, 0, 0].double()[None] * (at[:, None] * 2 - 1) + 0.2 * torch.randn(n, dim, generator=gen).double()
+        kc, scale = P.packed(keys, code)
+        c.kc.view(torch.int8)[pg, pl, 0] = kc.view(torch.int8)
+        c.scales[pg, 0, pl, 0] = scale
+    P.values(c)
+    out, lse, _ = attended(g10, c, q)
+    check_rows(c, q, out, lse)
