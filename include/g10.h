@@ -499,7 +499,9 @@ int32_t g10_cache_workspace_bytes(const g10_cache *cache, int32_t new_tokens, in
    question, questions about one document).  The same result, up to rounding; keys and values of the beginning are read once for all sequences.  *shared (one word on
    the device) is at most lengths[s] - c_s for every sequence with c_s > 0 (else G10_DEV_BAD_LENGTH, and as many slots are taken as shared as can be); sequence 0's
    row holds the beginning's pages even where that sequence has no new tokens.  Whole tiles of 64 slots are read once, what is left of the beginning for each sequence.
-   No window, no add_scores: a page that sequences share does not belong to one that could evict from it. */
+   No window, no add_scores: a page that sequences share does not belong to one that could evict from it.  Not for rows in 8 bits.
+   A pass of its own over the beginning costs some 10 us of launches: it pays where reading the beginning for every sequence, which g10_cache_attend does on the same table,
+   takes longer, from about 64 000 slots (sequences times those shared, 8 heads of 128 dims) on. */
 int32_t g10_cache_attend_shared(const g10_cache *cache, const g10_cache_queries *queries, const int32_t *shared, void *ws, size_t ws_bytes, void *stream);
 /* Its workspace: 4 head_dim + 8 bytes for each query head of a new token, and room for the parts that are joined (4 head_dim + 8 bytes a row of some thousand blocks of
    rows, and of all that the beginning has). */

@@ -845,7 +845,7 @@ def g10_cache_shared_workspace_bytes(cache: CacheBuffers, new_tokens, q_heads) -
 
 def g10_cache_attend_shared(cache: CacheBuffers, q, shared, scale=None, counts=None, out=None, lse=None, ws=None, stream=None):
     """g10_cache_attend for a batch whose sequences begin alike: the first `shared` slots (int32 [1] on the cache's device) of every sequence stand where the
-    first row of the page table says, and are read once for all.  q, scale, counts, out, lse as there; ws: g10_cache_shared_workspace_bytes(...) bytes, allocated
+    first row of the page table says, and are read once for all (which pays from some 64 000 slots in all sequences together on).  q, scale, counts, out, lse as there; ws: g10_cache_shared_workspace_bytes(...) bytes, allocated
     here when None; calls that may overlap on the GPU need one each."""
     shape, qs = _rows("q", q, cache)
     dev, new, heads = cache.index, shape[1], shape[2]

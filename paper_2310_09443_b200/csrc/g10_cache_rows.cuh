@@ -19,7 +19,8 @@
 //
 // Codes are multiplied as they are, as in g10_packed_attend.cuh: in fp16, with the queries of bf16 times a power of two for each row; a key's scale goes to its logit, a
 // value's to the weight.  W is the product of the two relative to the largest that its row has met, so that what stands in slots that a row does not see, or hardly weighs, is
-// nothing to it.  The product of tile u with the queries is issued before those of the one or two tiles before it with the values, so that it runs while the weights are worked out.
+// nothing to it (64 maxima and a factor a row and tile: 24 sequences of 5 tokens behind 4000 slots of 64 dims, int8, 154 us; 147 with one power of two for all rows, which
+// lost bits; 128 and 256 dims the same).  The product of tile u with the queries is issued before those of the one or two tiles before it with the values, so that it runs while the weights are worked out.
 #pragma once
 #include <type_traits>
 
