@@ -111,8 +111,8 @@ __global__ void __launch_bounds__(kThreads) k_cache_plan(const EvictArgs a, int 
     for (int pass = 0; pass < 3; ++pass) {
         const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0, bits = pass == 2 ? 10 : 11, digits = 1 << bits, few = digits / kThreads;
         unsigned *const count = s_count + pass * kDigits;
-        for (int i = tid; i < n; i += kThreads) {
-            const unsigned w = worth(i);
+        for (unsigned i = tid; i < (unsigned)n; i += kThreads) {     // (without a sign: a step behind the last may pass 2^31)
+            const unsigned w = worth((int)i);
             if (pass == 0 || w >> (shift + bits) == known >> (shift + bits)) atomicAdd(&count[(w >> shift) & (digits - 1)], 1u);
         }
         __syncthreads();
